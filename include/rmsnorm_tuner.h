@@ -247,7 +247,9 @@ typedef enum {
     RT_ERR_BUDGET = 8,         /* the budget allows no evaluation */
     RT_ERR_DEVICE_TIMEOUT = 9, /* a bounded device-side wait expired (read through rt_device_status) */
     RT_ERR_CAPACITY = 10,      /* a caller-provided array or workspace is too small */
-    RT_ERR_NO_DEVICE = 11      /* no CUDA device is available */
+    RT_ERR_NO_DEVICE = 11,     /* no CUDA device is available */
+    RT_ERR_INDEX = 12          /* a kernel met a slot, page or length outside the cache or its page table and skipped
+                                  it (read through rt_device_status) */
 } rt_status;
 
 /* ---- 1. the template kernel ------------------------------------------------- */
@@ -355,6 +357,115 @@ int rmsnorm_allreduce_template_launch(const rt_params* p, const void* const* x_p
 int merge_attn_states_template_launch(const rt_params* p, const void* v_a, const float* s_a, const void* v_b,
                                       const float* s_b, void* v_out, float* s_out, int64_t n_tokens,
                                       int64_t heads, int64_t head_dim, int dtype, void* stream);
+
+/* ---- 1b. the paged key/value cache and the attention that reads it --------------------------------- */
+
+/* How the entries of a key/value cache are held. */
+typedef enum {
+    RT_KV_PLAIN = 0, /* elements of rt_kv_cache.dtype */
+    RT_KV_E4M3 = 1,  /* e4m3 codes and one binary32 scale per token and head */
+    RT_KV_INT8 = 2   /* int8 codes -127..127 and one binary32 scale per token and head */
+} rt_kv_format;
+
+/* Largest head_dim of a cache, and most query tokens per sequence of shared_prefix_attention_launch. */
+#define RT_KV_MAX_HEAD_DIM 256
+#define RT_MAX_QUERY_LEN 16
+
+/*
+ * A paged key/value cache: device tensors k and v of logical shape [n_pages, page_size, kv_heads, head_dim], the last
+ * axis contiguous, and for the quantised formats k_scale and v_scale of shape [n_pages, page_size, kv_heads].  k and
+ * v share one set of strides, k_scale and v_scale another; any order of the outer axes and any gaps between them are
+ * allowed (a stride may be zero only where its axis has length 1).  Slot s is token s % page_size of page
+ * s / page_size.  The struct itself lives in host memory and is copied by the calls.
+ */
+typedef struct {
+    void* k;
+    void* v;
+    float* k_scale; /* NULL for RT_KV_PLAIN */
+    float* v_scale;
+    int64_t n_pages;
+    int32_t page_size; /* 1 .. 65536 */
+    int32_t kv_heads;
+    int32_t head_dim; /* 1 .. RT_KV_MAX_HEAD_DIM */
+    int32_t format;   /* rt_kv_format */
+    int32_t dtype;    /* rt_dtype of the entries of a plain cache; ignored for the other formats */
+    int32_t reserved; /* 0 */
+    int64_t page_stride, token_stride, head_stride; /* of k and v, in elements (bytes for the quantised formats) */
+    int64_t scale_page_stride, scale_token_stride, scale_head_stride; /* of k_scale and v_scale, in floats */
+} rt_kv_cache;
+
+/*
+ * Writes the keys and values of n_tokens tokens into the cache, quantising them on the way:
+ *     amax = max(max_j |x_j|, 1e-12);  scale = amax / M;  code_j = round_to_nearest_even(x_j * (M / amax))
+ * per token and head, apart for keys and values, each step one binary32 operation, M = 448 (e4m3) or 127 (int8).  A
+ * vector that holds an infinity or a NaN gets a NaN scale and reads back as NaN throughout.  A plain cache holds the
+ * elements bit for bit; its dtype must be the tokens' (RT_ERR_DTYPE otherwise).
+ *   key, value  device, [n_tokens, kv_heads, head_dim] of `dtype`, the last axis contiguous, outer strides in elements
+ *               (slices of a fused projection need no copy).
+ *   slots       device, int64 [n_tokens]: the slot of each token.  Negative: the token is padding, nothing is written.
+ *               Beyond the cache: skipped, and RT_ERR_INDEX is left in the device status word.  Two tokens of one
+ *               call must not name the same slot (that slot's content would be a mixture of the two).
+ * Asynchronous on `stream`, allocates nothing.  n_tokens == 0 is a successful no-op.
+ */
+int kv_cache_write_launch(const rt_kv_cache* cache, const void* key, int64_t key_token_stride, int64_t key_head_stride,
+                          const void* value, int64_t value_token_stride, int64_t value_head_stride,
+                          const int64_t* slots, int64_t n_tokens, int dtype, void* stream);
+
+/*
+ * Reads entries back: key_out[t], value_out[t] = code * scale of slot slots[t], one binary32 product rounded once to
+ * `dtype` (a plain cache must hold `dtype` and is copied bit for bit).  Rows whose slot is negative are left as they
+ * were; rows whose slot is beyond the cache too, and RT_ERR_INDEX is left in the device status word.  A slot may be named
+ * any number of times.  Layouts as for kv_cache_write_launch; asynchronous, allocates nothing.
+ */
+int kv_cache_read_launch(const rt_kv_cache* cache, const int64_t* slots, int64_t n_tokens, void* key_out,
+                         int64_t key_token_stride, int64_t key_head_stride, void* value_out,
+                         int64_t value_token_stride, int64_t value_head_stride, int dtype, void* stream);
+
+/* The sequences of one step: a prefix that all of them share and a suffix of each one's own, both paged. */
+typedef struct {
+    const int32_t* prefix_pages; /* device, the prefix's pages in order (NULL when prefix_len == 0) */
+    const int32_t* page_table;   /* device, [n_seqs, page_table_width], row stride page_table_stride: the pages of each
+                                    sequence's suffix, which starts at the first token of its first page.  Entries past
+                                    a sequence's length are not read.  NULL when max_suffix_len == 0 */
+    const int32_t* suffix_lens;  /* device, [n_seqs]: keys in each suffix, the query tokens' own included;
+                                    negative = a padded sequence, whose rows of out and lse are left as they were */
+    int64_t prefix_len;          /* 0 .. 2^30 */
+    int64_t max_suffix_len;      /* no suffix is longer (0 .. 2^30); longer ones are cut there and RT_ERR_INDEX reported */
+    int64_t n_seqs;
+    int64_t page_table_stride; /* elements */
+    int32_t page_table_width;
+    int32_t n_prefix_pages; /* entries of prefix_pages */
+    int32_t q_len;          /* query tokens per sequence, 1 .. RT_MAX_QUERY_LEN */
+    int32_t reserved;       /* 0 */
+} rt_prefix_batch;
+
+/*
+ * Attention of every sequence's query tokens to the shared prefix, read once for the whole batch, and to the sequence's
+ * own suffix:  with s_j = softmax_scale * <q, k_j> over the keys that the row sees,
+ *     out = round_dtype(sum_j e^(s_j) v_j / sum_j e^(s_j)),   lse = ln sum_j e^(s_j).
+ * Query token i of a sequence whose suffix has n keys sees the whole prefix and the suffix keys j <= n - q_len + i.  A
+ * row that sees no key gets out = 0 and lse = -inf, the convention of merge_attn_states_template_launch, so the
+ * result can be merged with that of further keys.  Query head h reads key/value head h / (q_heads / kv_heads).  Keys
+ * that a row does not see have no influence on it, whatever their values (infinities and NaN included).
+ *   cache      format plain (dtype as q), e4m3 or int8; head_dim a multiple of 8 (plain) or 16 (quantised); k, v and
+ *              their strides multiples of 16 bytes (RT_ERR_ALIGN otherwise).  The suffix keys of the query tokens are
+ *              in it already.
+ *   q          device, [n_seqs * q_len, q_heads, head_dim] of `dtype` (bf16 or fp16), outer strides in elements, pointer and
+ *              strides multiples of 16 bytes.
+ *   out        device, [n_seqs * q_len, q_heads, head_dim] contiguous, 16-byte aligned.  lse: device, binary32
+ *              [n_seqs * q_len, q_heads] contiguous, or NULL.
+ *   workspace  device memory of shared_prefix_attention_workspace_bytes(...) bytes, 16-byte aligned, for the partial
+ *              results.  It carries nothing from one call to the next; calls that may overlap on the device need one each.
+ * A page number outside the cache hides its keys and leaves RT_ERR_INDEX in the device status word.  The results do not
+ * depend on the other work of the device, from call to call they are bit-identical.  Asynchronous on `stream`, allocates
+ * nothing.
+ */
+int shared_prefix_attention_launch(const rt_kv_cache* cache, const rt_prefix_batch* batch, const void* q,
+                                   int64_t q_token_stride, int64_t q_head_stride, int32_t q_heads, void* out, float* lse,
+                                   float softmax_scale, int dtype, void* workspace, int64_t workspace_bytes, void* stream);
+/* Bytes of workspace for a batch of this geometry on the current device (0 is possible), -1 when it is not served
+ * (rt_last_error has the reason).  The pointers of `cache` and `batch` are not read. */
+int64_t shared_prefix_attention_workspace_bytes(const rt_kv_cache* cache, const rt_prefix_batch* batch, int32_t q_heads);
 
 /* ---- 2. the feasible region ----------------------------------------------------- */
 
@@ -586,7 +697,7 @@ int tuner_compare_static(const void* got, const void* ref, int64_t n, int dtype,
 
 const char* rt_status_string(int status);
 const char* rt_last_error(void);
-/* Reads and clears the device status word (0, or RT_ERR_DEVICE_TIMEOUT).  Synchronises the device. */
+/* Reads and clears the device status word (0, RT_ERR_DEVICE_TIMEOUT or RT_ERR_INDEX).  Synchronises the device. */
 int rt_device_status(void);
 /* Number of compiled instances of the template, and the i-th one's coordinates (host query). */
 int32_t rt_num_kernel_instances(void);

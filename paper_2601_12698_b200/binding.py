@@ -28,7 +28,9 @@ RT_PRUNE_DEFAULT = 63
 RT_SEARCH_GUIDED, RT_SEARCH_EXHAUSTIVE = 0, 1
 RT_CMP_BITS, RT_CMP_ULP16, RT_CMP_REL32 = 0, 1, 2
 (RT_OK, RT_ERR_NULL, RT_ERR_DTYPE, RT_ERR_SHAPE, RT_ERR_ALIGN, RT_ERR_INFEASIBLE, RT_ERR_CUDA, RT_ERR_MISMATCH,
- RT_ERR_BUDGET, RT_ERR_DEVICE_TIMEOUT, RT_ERR_CAPACITY, RT_ERR_NO_DEVICE) = range(12)
+ RT_ERR_BUDGET, RT_ERR_DEVICE_TIMEOUT, RT_ERR_CAPACITY, RT_ERR_NO_DEVICE, RT_ERR_INDEX) = range(13)
+RT_KV_PLAIN, RT_KV_E4M3, RT_KV_INT8 = 0, 1, 2
+RT_KV_MAX_HEAD_DIM, RT_MAX_QUERY_LEN = 256, 16
 PHASE_NAMES = {0: "seed", 1: "grid", 2: "climb", 3: "topk", 4: "sweep"}
 STAGE_NAMES = {0: "reg", 1: "smem_ldg", 2: "smem_tma", 3: "reg_realign", 4: "tma_pipeline"}
 REDUCE_NAMES = {0: "shfl", 1: "smem", 2: "cluster"}
@@ -109,6 +111,20 @@ class rt_spec_entry(Structure):
     _fields_ = [("shape", rt_shape), ("best", rt_params), ("best_us", c_float), ("reserved", c_int32)]
 
 
+class rt_kv_cache(Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p), ("n_pages", c_int64),
+                ("page_size", c_int32), ("kv_heads", c_int32), ("head_dim", c_int32), ("format", c_int32),
+                ("dtype", c_int32), ("reserved", c_int32), ("page_stride", c_int64), ("token_stride", c_int64),
+                ("head_stride", c_int64), ("scale_page_stride", c_int64), ("scale_token_stride", c_int64),
+                ("scale_head_stride", c_int64)]
+
+
+class rt_prefix_batch(Structure):
+    _fields_ = [("prefix_pages", c_void_p), ("page_table", c_void_p), ("suffix_lens", c_void_p), ("prefix_len", c_int64),
+                ("max_suffix_len", c_int64), ("n_seqs", c_int64), ("page_table_stride", c_int64),
+                ("page_table_width", c_int32), ("n_prefix_pages", c_int32), ("q_len", c_int32), ("reserved", c_int32)]
+
+
 SOURCE_NAMES = {0: "table_exact", 1: "table_nearest", 2: "general", 3: "feasible_set"}
 
 rt_evaluate_fn = ctypes.CFUNCTYPE(c_double, POINTER(rt_params), c_void_p)
@@ -122,6 +138,13 @@ _SIGNATURES = {
     "rmsnorm_allreduce_template_launch": (c_int, [POINTER(rt_params), POINTER(c_void_p), c_int32, c_void_p, c_void_p,
                                                   POINTER(c_void_p), c_int32, POINTER(c_void_p), c_int32, c_int64,
                                                   c_int64, c_int64, c_float, c_int, c_void_p]),
+    "kv_cache_write_launch": (c_int, [POINTER(rt_kv_cache), c_void_p, c_int64, c_int64, c_void_p, c_int64, c_int64, c_void_p,
+                                      c_int64, c_int, c_void_p]),
+    "kv_cache_read_launch": (c_int, [POINTER(rt_kv_cache), c_void_p, c_int64, c_void_p, c_int64, c_int64, c_void_p, c_int64,
+                                     c_int64, c_int, c_void_p]),
+    "shared_prefix_attention_launch": (c_int, [POINTER(rt_kv_cache), POINTER(rt_prefix_batch), c_void_p, c_int64, c_int64,
+                                               c_int32, c_void_p, c_void_p, c_float, c_int, c_void_p, c_int64, c_void_p]),
+    "shared_prefix_attention_workspace_bytes": (c_int64, [POINTER(rt_kv_cache), POINTER(rt_prefix_batch), c_int32]),
     "rt_kernel_instance_parts": (c_int32, [c_int32]),
     "rt_set_option": (c_int, [c_int32, c_int32]),
     "rt_get_option": (c_int32, [c_int32]),
@@ -333,6 +356,207 @@ def merge_attn_states_template_launch(params: rt_params, v_a, s_a, v_b, s_b, v_o
                                                  s_b.data_ptr(), v_out.data_ptr(), s_out.data_ptr(), n, h, d,
                                                  _dtype_code(v_a), _stream_ptr(stream)),
            "merge_attn_states_template_launch")
+
+
+# ---- 1b. the paged key/value cache and the attention that reads it ------------------------------------------
+
+def _device_and_stream(tensor, stream):
+    """(device index, cudaStream_t): the tensor's device and the given stream of it, or its current one."""
+    import torch
+    index = tensor.get_device()
+    if stream is None:
+        return index, torch._C._cuda_getCurrentRawStream(index)
+    if stream.device_index != index:
+        raise ValueError(f"the stream belongs to device {stream.device_index}, the tensors to device {index}")
+    return index, stream.cuda_stream
+
+
+def _call_on(index: int, fn, *args) -> int:
+    """fn(*args) with `index` as the current device (the library works on the current one)."""
+    import torch
+    if torch.cuda.current_device() == index:
+        return fn(*args)
+    with torch.cuda.device(index):
+        return fn(*args)
+
+
+def _no_overlap(t, name: str):
+    if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the last axis must be contiguous")
+    if any(n > 1 and st == 0 for n, st in zip(t.shape, t.stride())):
+        raise ValueError(f"{name}: an expanded tensor cannot be used here")
+
+
+class KvCache:
+    """A paged key/value cache: k and v of shape [n_pages, page_size, kv_heads, head_dim] with any outer strides (views of
+    a combined or head-major tensor included), and float32 scales [n_pages, page_size, kv_heads] for the quantised formats.
+    The element type names the format: bf16, fp16, fp32 are plain, float8_e4m3fn (or uint8 bytes of it) and int8 quantised.
+    The object keeps the tensors alive and holds the struct that the library's calls take."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        import torch
+        formats = {torch.float8_e4m3fn: RT_KV_E4M3, torch.uint8: RT_KV_E4M3, torch.int8: RT_KV_INT8, torch.bfloat16: RT_KV_PLAIN,
+                   torch.float16: RT_KV_PLAIN, torch.float32: RT_KV_PLAIN}
+        if k.dim() != 4 or not k.is_cuda or k.dtype not in formats:
+            raise ValueError("k must be a CUDA tensor [n_pages, page_size, kv_heads, head_dim] of a cache element type")
+        if v.shape != k.shape or v.dtype != k.dtype or v.stride() != k.stride() or v.device != k.device:
+            raise ValueError("v must be like k: shape, strides, dtype and device")
+        _no_overlap(k, "k and v")
+        self.format = formats[k.dtype]
+        if self.format == RT_KV_PLAIN:
+            if k_scale is not None or v_scale is not None:
+                raise ValueError("a plain cache has no scales")
+        else:
+            for t in (k_scale, v_scale):
+                if t is None or t.shape != k.shape[:3] or t.dtype != torch.float32 or t.device != k.device or t.stride() != k_scale.stride():
+                    raise ValueError("a quantised cache needs float32 scales [n_pages, page_size, kv_heads], alike for k and v")
+                if any(n > 1 and st == 0 for n, st in zip(t.shape, t.stride())):
+                    raise ValueError("scales: an expanded tensor cannot be used here")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_pages, self.page_size, self.kv_heads, self.head_dim = k.shape
+        if not (1 <= self.head_dim <= RT_KV_MAX_HEAD_DIM and self.kv_heads >= 1 and 1 <= self.page_size <= 65536):
+            raise ValueError(f"page_size {self.page_size}, kv_heads {self.kv_heads} or head_dim {self.head_dim} out of range")
+        self.device_index = k.get_device()
+        scale_strides = k_scale.stride() if k_scale is not None else (0, 0, 0)
+        self.struct = rt_kv_cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if k_scale is not None else None,
+                                  v_scale.data_ptr() if v_scale is not None else None, self.n_pages, self.page_size, self.kv_heads,
+                                  self.head_dim, self.format, _dtype_code(k) if self.format == RT_KV_PLAIN else 0, 0,
+                                  *k.stride()[:3], *scale_strides)
+        self._ref = byref(self.struct)
+
+    @classmethod
+    def allocate(cls, n_pages: int, page_size: int, kv_heads: int, head_dim: int, dtype, device="cuda") -> "KvCache":
+        """A zero-filled cache of `dtype` (bf16, fp16, fp32: plain; float8_e4m3fn, int8: quantised)."""
+        import torch
+        shape = (n_pages, page_size, kv_heads, head_dim)
+        quantised = dtype in (torch.float8_e4m3fn, torch.uint8, torch.int8)
+        held = [torch.zeros(shape, dtype=torch.uint8 if quantised else dtype, device=device).view(dtype) for _ in range(2)]
+        scales = [torch.zeros(shape[:3], dtype=torch.float32, device=device) for _ in range(2)] if quantised else (None, None)
+        return cls(*held, *scales)
+
+
+def _cache_call_args(cache: KvCache, key, value, slots, name: str):
+    import torch
+    n_tokens = slots.shape[0] if slots.dim() == 1 else -1
+    shape = (n_tokens, cache.kv_heads, cache.head_dim)
+    if slots.dtype != torch.int64 or not slots.is_contiguous() or slots.get_device() != cache.device_index:
+        raise ValueError(f"{name}: slots must be a contiguous int64 [n_tokens] tensor on the cache's device")
+    for t in (key, value):
+        if t.shape != shape or t.dtype != key.dtype or t.get_device() != cache.device_index:
+            raise ValueError(f"{name}: key and value must be {list(shape)} tensors of one dtype on the cache's device")
+        if t.stride(2) != 1 and t.shape[2] > 1:
+            raise ValueError(f"{name}: the last axis of key and value must be contiguous")
+    return n_tokens
+
+
+def kv_cache_write_launch(cache: KvCache, key, value, slots, stream=None) -> None:
+    """Write (quantising on the way) keys and values [n_tokens, kv_heads, head_dim] of n_tokens tokens into the cache at
+    their slots (int64 [n_tokens], page * page_size + offset; negative = padding, skipped).  Asynchronous."""
+    n_tokens = _cache_call_args(cache, key, value, slots, "kv_cache_write_launch")
+    index, s = _device_and_stream(slots, stream)
+    _check(_call_on(index, lib.kv_cache_write_launch, cache._ref, key.data_ptr(), key.stride(0), key.stride(1), value.data_ptr(),
+                    value.stride(0), value.stride(1), slots.data_ptr(), n_tokens, _dtype_code(key), s), "kv_cache_write_launch")
+
+
+def kv_cache_read_launch(cache: KvCache, slots, key_out, value_out, stream=None) -> None:
+    """Read entries of the cache back into key_out and value_out [n_tokens, kv_heads, head_dim]; rows whose slot is
+    negative are left as they were.  Asynchronous."""
+    n_tokens = _cache_call_args(cache, key_out, value_out, slots, "kv_cache_read_launch")
+    _no_overlap(key_out, "key_out")
+    _no_overlap(value_out, "value_out")
+    index, s = _device_and_stream(slots, stream)
+    _check(_call_on(index, lib.kv_cache_read_launch, cache._ref, slots.data_ptr(), n_tokens, key_out.data_ptr(), key_out.stride(0),
+                    key_out.stride(1), value_out.data_ptr(), value_out.stride(0), value_out.stride(1), _dtype_code(key_out), s),
+           "kv_cache_read_launch")
+
+
+class PrefixBatch:
+    """The sequences of one step: the pages of the prefix that all of them share (int32, in order), its length, and for every
+    sequence the pages of its own suffix (int32 [n_seqs, width]) and the number of keys in it (int32 [n_seqs], the query
+    tokens' own included; negative = a padded sequence).  max_suffix_len bounds the lengths on the host's side: the launch
+    shape follows it, the lengths themselves are read on the device.  q_len query tokens per sequence, 1 to 16.  One object
+    serves every layer of the step."""
+
+    def __init__(self, prefix_pages, prefix_len: int, page_table, suffix_lens, max_suffix_len: int, q_len: int = 1):
+        import torch
+        if suffix_lens.dim() != 1 or suffix_lens.dtype != torch.int32 or not suffix_lens.is_cuda or not suffix_lens.is_contiguous():
+            raise ValueError("suffix_lens must be a contiguous int32 [n_seqs] CUDA tensor")
+        device, n_seqs = suffix_lens.device, suffix_lens.shape[0]
+        if prefix_pages is None:
+            n_prefix_pages = 0
+        else:
+            if prefix_pages.dim() != 1 or prefix_pages.dtype != torch.int32 or prefix_pages.device != device or not prefix_pages.is_contiguous():
+                raise ValueError("prefix_pages must be a contiguous int32 tensor on the device of suffix_lens")
+            n_prefix_pages = prefix_pages.shape[0]
+        if page_table is None:
+            width = stride = 0
+        else:
+            if (page_table.dim() != 2 or page_table.dtype != torch.int32 or page_table.device != device or page_table.shape[0] != n_seqs
+                    or (page_table.shape[1] > 1 and page_table.stride(1) != 1)):
+                raise ValueError("page_table must be an int32 [n_seqs, width] tensor on the device of suffix_lens, rows contiguous")
+            width, stride = page_table.shape[1], page_table.stride(0)
+        self.prefix_pages, self.page_table, self.suffix_lens = prefix_pages, page_table, suffix_lens
+        self.n_seqs, self.q_len, self.device_index = n_seqs, int(q_len), suffix_lens.get_device()
+        self.struct = rt_prefix_batch(prefix_pages.data_ptr() if n_prefix_pages else None, page_table.data_ptr() if width else None,
+                                      suffix_lens.data_ptr(), int(prefix_len), int(max_suffix_len), n_seqs, stride, width, n_prefix_pages,
+                                      self.q_len, 0)
+        self._ref = byref(self.struct)
+
+
+def shared_prefix_attention_workspace_bytes(cache: KvCache, batch: PrefixBatch, q_heads: int) -> int:
+    n = _call_on(cache.device_index, lib.shared_prefix_attention_workspace_bytes, cache._ref, batch._ref, q_heads)
+    if n < 0:
+        raise ValueError(f"shared_prefix_attention: {lib.rt_last_error().decode()}")
+    return int(n)
+
+
+def shared_prefix_attention_workspace(cache: KvCache, batch: PrefixBatch, q_heads: int):
+    """A uint8 tensor of the size that calls of this geometry need."""
+    import torch
+    return torch.empty(shared_prefix_attention_workspace_bytes(cache, batch, q_heads), dtype=torch.uint8, device=cache.k.device)
+
+
+def shared_prefix_attention_launch(cache: KvCache, batch: PrefixBatch, q, out, lse=None, workspace=None, softmax_scale=None,
+                                   stream=None) -> None:
+    """Attention of q [n_seqs, q_len, q_heads, head_dim] (or [n_seqs, q_heads, head_dim] for one query token) to the shared
+    prefix and to each sequence's own suffix; out like q and contiguous, lse float32 [..., q_heads] or None.  softmax_scale
+    defaults to head_dim ** -0.5.  workspace: a uint8 tensor of shared_prefix_attention_workspace_bytes(...) bytes, made
+    here when it is None.  Asynchronous."""
+    shape = q.shape
+    n_seqs, q_len, head_dim = batch.n_seqs, batch.q_len, cache.head_dim
+    if len(shape) == 4 and shape[1] == q_len:
+        token_stride, head_stride = q.stride(1) if q_len > 1 else q.stride(0), q.stride(2)
+        if q_len > 1 and n_seqs > 1 and q.stride(0) != q_len * token_stride:
+            raise ValueError("q: the query tokens of all sequences must be evenly spaced")
+    elif len(shape) == 3 and q_len == 1:
+        token_stride, head_stride = q.stride(0), q.stride(1)
+    else:
+        raise ValueError("q must be [n_seqs, q_len, q_heads, head_dim], or [n_seqs, q_heads, head_dim] when q_len is 1")
+    if shape[0] != n_seqs or shape[-1] != head_dim or (head_dim > 1 and q.stride(-1) != 1):
+        raise ValueError(f"q must hold {n_seqs} sequences and heads of {head_dim}, the last axis contiguous")
+    if out.shape != shape or out.dtype != q.dtype or not out.is_contiguous():
+        raise ValueError("out must be contiguous and of q's shape and dtype")
+    index = cache.device_index
+    if not (q.get_device() == out.get_device() == batch.device_index == index):
+        raise ValueError("cache, batch, q and out must be on one CUDA device")
+    q_heads = shape[-2]
+    lse_ptr = None
+    if lse is not None:
+        import torch
+        if lse.shape != shape[:-1] or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.get_device() != index:
+            raise ValueError("lse must be a contiguous float32 tensor of q's shape without head_dim, on q's device")
+        lse_ptr = lse.data_ptr()
+    if workspace is None:
+        workspace = shared_prefix_attention_workspace(cache, batch, q_heads)
+        if stream is not None and workspace.numel():
+            workspace.record_stream(stream)
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the cache's device")
+    _, s = _device_and_stream(q, stream)
+    _check(_call_on(index, lib.shared_prefix_attention_launch, cache._ref, batch._ref, q.data_ptr(), token_stride, head_stride, q_heads,
+                    out.data_ptr(), lse_ptr, head_dim ** -0.5 if softmax_scale is None else softmax_scale, _dtype_code(q),
+                    workspace.data_ptr() if workspace.numel() else None, workspace.numel() * workspace.element_size(), s),
+           "shared_prefix_attention_launch")
 
 
 def rmsnorm_host_workspace_bytes(n_tokens: int, hidden: int, dtype, chunk_tokens: int = 0) -> int:

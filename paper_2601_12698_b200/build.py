@@ -28,7 +28,11 @@ LIB_PATH = os.path.join(HERE, "librmsnorm_tuner.so")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-std=c++17", "-O3", "-lineinfo",
               "-Xcompiler", "-fPIC", "-I", CSRC, "-I", INCLUDE]
-HOST_UNITS = ["launch.cu", "feasible.cu", "search.cu", "host_run.cu", "table.cu", "trace.cu"]
+HOST_UNITS = ["launch.cu", "feasible.cu", "search.cu", "host_run.cu", "table.cu", "trace.cu", "kv_cache.cu",
+              "shared_prefix_attention.cu"]
+KV_FORMATS = {"plain": 0, "e4m3": 1, "int8": 2}
+# attend_instances.cu is compiled once for each of these: <query type>_<cache format>
+ATTEND_UNITS = [f"{t}_{f}" for t in ("bf16", "fp16") for f in KV_FORMATS]
 ELEMENT_TYPES = {"bf16": ("__nv_bfloat16", 0), "fp16": ("__half", 1), "fp32": ("float", 2)}
 GROUPS = {"reg": 0, "smem": 1, "narrow": 2, "silu": 3, "merge": 4, "fp8out": 5, "allreduce": 6, "realign": 7}
 
@@ -48,6 +52,11 @@ def unit_flags(name: str) -> list[str]:
     if m.group(4) is not None:
         flags.append(f"-DRT_UNIT_REDUCE={m.group(4)}")
     return flags
+
+
+def attend_unit_flags(name: str) -> list[str]:
+    dtype, fmt = name.split("_")
+    return [f"-DRT_UNIT_NAME={name}", f"-DRT_UNIT_T={ELEMENT_TYPES[dtype][0]}", f"-DRT_UNIT_FMT={KV_FORMATS[fmt]}"]
 
 
 # (the plain instances: TRACE = false, mangled Lb0E; the instrumented ones of trace.cu are not part of the table)
@@ -157,6 +166,11 @@ def build(force: bool = False, verbose: bool = False, jobs: int | None = None) -
         host_objs.append(obj)
         if stale(obj) or (src == "launch.cu" and os.path.getmtime(obj) < os.path.getmtime(table)):
             work.append((os.path.join(CSRC, src), obj, [], verbose))
+    for name in ATTEND_UNITS:
+        obj = os.path.join(OBJ_DIR, f"attend_{name}.o")
+        host_objs.append(obj)
+        if stale(obj):
+            work.append((os.path.join(CSRC, "attend_instances.cu"), obj, attend_unit_flags(name), verbose))
     if work:
         rebuilt = True
         with ThreadPoolExecutor(max_workers=pool_size) as pool:

@@ -1,0 +1,138 @@
+// What the attention kernels over a paged key/value cache share: arguments, places in the cache, 16-bit matrix products.
+#pragma once
+
+#include <cuda_fp8.h>
+
+#include "add_rmsnorm_kernel.cuh"
+#include "kv_cache_kernels.cuh"
+
+namespace rt {
+
+// One call of shared_prefix_attention_launch.  A "row" is one query head of one query token; the rows of one key/value
+// head (all its query heads of all query tokens) attend to the same keys of the prefix.  Every key range that one CTA works
+// through is a "part": it leaves a normalised output and the base-2 logarithm of its softmax denominator, and
+// merge_parts_kernel joins the parts of a row.  Parts 0 .. prefix_parts-1 belong to the prefix, the rest to the suffix.
+struct AttendArgs {
+    const unsigned char* k;
+    const unsigned char* v;
+    const float* k_scale;
+    const float* v_scale;
+    long long page_stride, token_stride, head_stride;  // of the cache, in elements (bytes when quantised)
+    long long scale_page_stride, scale_token_stride, scale_head_stride;
+    long long n_pages;
+    unsigned page_size;
+    int page_shift;  // log2(page_size), or -1
+    const int32_t* prefix_pages;
+    const int32_t* page_table;
+    const int32_t* suffix_lens;
+    long long page_table_stride;
+    int page_table_width;
+    int prefix_len;
+    int max_suffix_len;
+    int n_seqs;
+    int q_len;
+    int kv_heads;
+    int group;  // query heads per key/value head
+    int dim;
+    const unsigned char* q;
+    long long q_token_stride, q_head_stride;  // elements
+    float score_scale;                        // softmax_scale * log2(e)
+    int prefix_parts, prefix_keys;            // parts of the prefix and keys in each (the last may have fewer)
+    int suffix_parts, suffix_keys;
+    float* part_out;  // [part][token][head][dim]
+    float* part_lse;  // [part][token][head]
+    void* out;        // [token][head][dim]
+    float* lse;       // [token][head] or NULL
+    int* status;
+};
+
+// Offset of token `pos` of a page list in k and v (`scales`: in the scale tensors), -1 when its page is not in the cache.
+__device__ __forceinline__ long long entry_offset(const AttendArgs& a, int page, unsigned in_page, int head, bool scales)
+{
+    if (scales) return (long long)page * a.scale_page_stride + (long long)in_page * a.scale_token_stride + (long long)head * a.scale_head_stride;
+    return (long long)page * a.page_stride + (long long)in_page * a.token_stride + (long long)head * a.head_stride;
+}
+__device__ __forceinline__ void split_position(const AttendArgs& a, int pos, int& list_index, unsigned& in_page)
+{
+    if (a.page_shift >= 0) {
+        list_index = pos >> a.page_shift;
+        in_page = (unsigned)pos & (a.page_size - 1u);
+    } else {
+        list_index = (int)((unsigned)pos / a.page_size);
+        in_page = (unsigned)pos - (unsigned)list_index * a.page_size;
+    }
+}
+
+// Number of keys in the suffix of `seq` that the page table can name; -1 for a padded sequence.
+__device__ __forceinline__ int suffix_length(const AttendArgs& a, int seq)
+{
+    int len = __ldg(a.suffix_lens + seq);
+    if (len > a.max_suffix_len) {
+        atomicExch(a.status, kDeviceIndexCode);
+        len = a.max_suffix_len;
+    }
+    return len;
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi)
+{
+    return Codec<T, 16>::from_float16x2(lo, hi);
+}
+
+// 2^x, 2 ulp; results below 2^-126 are zero.
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// D += A B, A 16x16 and B 16x8 of 16-bit elements, D in binary32.
+template <typename T>
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    } else {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+}
+
+// Two codes, in the low two bytes of `pair`, as two fp16 values.  Both formats fit fp16 exactly.
+template <int FMT>
+__device__ __forceinline__ uint32_t codes_to_half2(uint32_t pair_lo_bytes)
+{
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)pair_lo_bytes, __NV_E4M3);
+    return (uint32_t)h.x | ((uint32_t)h.y << 16);
+}
+// Bytes i and j of the word pair (a: bytes 0-3, b: bytes 4-7) as fp16 values (low half from i).
+template <int FMT, int I, int J>
+__device__ __forceinline__ uint32_t pick_half2(uint32_t a, uint32_t b)
+{
+    if constexpr (FMT == kKvE4m3) {
+        return codes_to_half2<FMT>(__byte_perm(a, b, I | (J << 4)));
+    } else {
+        // 1024 + (code + 128) as fp16 bits, minus 1152: exact for -128 .. 127
+        const uint32_t w = (__byte_perm(a, b, I | (J << 8)) & 0x00FF00FFu) ^ 0x64806480u;
+        const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&w), __half2half2(__ushort_as_half((unsigned short)0x6480)));
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+}
+
+// The power of two that brings a row's largest magnitude into [2^14, 2^15), so that a bf16 row fits fp16 without loss
+// (elements 2^-28 below the largest lose bits, which no binary32 sum would keep either).  Its inverse is exact too.
+__device__ __forceinline__ float fp16_row_factor(float amax)
+{
+    if (!(amax < INFINITY) || amax == 0.f) return 1.0f;
+    int e = (int)((__float_as_uint(amax) >> 23) & 0xFFu) - 127;
+    e = max(e, -112);
+    return __uint_as_float((uint32_t)(127 + 14 - e) << 23);
+}
+
+// A value scale as the weights use it: log2 and reciprocal are taken of it, so a zero (an entry never written) becomes tiny.
+__device__ __forceinline__ float usable_scale(float s) { return s < 1e-30f ? 1e-30f : s; }
+
+}  // namespace rt

@@ -35,7 +35,7 @@ std::atomic<int> g_wait_polls{(int)kMbarrierPollLimit};
 std::atomic<int> g_drop_tma_copies{0};
 std::mutex g_mutex;
 
-constexpr int kMaxDevices = 64;
+constexpr int kMaxDevices = kDeviceSlots;
 struct DeviceCache {
     bool limits_ready = false;
     rt_limits limits;
@@ -598,6 +598,34 @@ static void set_launch_attrs(cudaLaunchConfig_t* cfg, LaunchAttrs* la, int clust
     cfg->attrs = cfg->numAttrs ? la->a : nullptr;
 }
 
+int launch_kernel(const void* fn, dim3 grid, dim3 block, size_t dyn_smem, cudaStream_t stream, void** params)
+{
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = dyn_smem;
+    cfg.stream = stream;
+    LaunchAttrs la;
+    set_launch_attrs(&cfg, &la, 1);
+    cudaError_t e = cudaLaunchKernelExC(&cfg, fn, params);
+    if (e != cudaSuccess) {
+        (void)cudaGetLastError();
+        set_error("kernel launch failed: %s", cudaGetErrorString(e));
+        return RT_ERR_CUDA;
+    }
+    count_launch();
+    return RT_OK;
+}
+
+int current_device_index(int* index)
+{
+    DeviceCache* dc;
+    const int st = current_device_cache(&dc);
+    if (st == RT_OK) *index = (int)(dc - g_dev);
+    return st;
+}
+
 int launch_fp8_plan(const Plan& plan, const void* x, const void* r, const void* w, void* q, float* scale, void* r_out,
                     int64_t n_tokens, int64_t hidden, float eps, cudaStream_t stream)
 {
@@ -1068,6 +1096,7 @@ const char* rt_status_string(int status)
         case RT_ERR_DEVICE_TIMEOUT: return "a bounded device-side wait expired";
         case RT_ERR_CAPACITY: return "caller-provided buffer too small";
         case RT_ERR_NO_DEVICE: return "no CUDA device";
+        case RT_ERR_INDEX: return "a slot, page or length outside the cache or its page table";
         default: return "unknown status";
     }
 }

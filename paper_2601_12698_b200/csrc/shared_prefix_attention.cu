@@ -1,0 +1,229 @@
+// Entry point of the attention over a shared prefix: argument checks, the split of the work into parts, the launches.
+#include <string.h>
+
+#include "attend_common.cuh"
+#include "attend_host.h"
+#include "attend_rows_kernel.cuh"
+#include "tuner_internal.h"
+
+namespace rt {
+
+int check_cache(const rt_kv_cache* c, bool pointers);
+int log2_or_minus1(unsigned v);
+
+namespace {
+
+constexpr int kMaxLen = 1 << 30;
+constexpr int kMaxParts = 64;  // of the prefix, and of the suffix
+
+struct AttendPlan {
+    int padded_dim;
+    int group;
+    long long tokens;
+    int prefix_parts, prefix_keys, suffix_parts, suffix_keys;
+    long long prefix_ctas, suffix_ctas;
+    int64_t workspace;
+};
+
+AttendKernels kernels_of(int dtype, int format, int padded_dim)
+{
+    typedef AttendKernels (*Get)(int);
+    static const Get get[2][3] = {{rt_attend_kernels_bf16_plain, rt_attend_kernels_bf16_e4m3, rt_attend_kernels_bf16_int8},
+                                  {rt_attend_kernels_fp16_plain, rt_attend_kernels_fp16_e4m3, rt_attend_kernels_fp16_int8}};
+    return get[dtype][format](padded_dim);
+}
+
+long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
+// Parts of `keys` keys such that `tiles` tiles times the parts give about `want` CTAs, none of fewer than `least` keys.
+void split_keys(long long keys, long long tiles, long long want, int least, int* parts, int* part_keys)
+{
+    long long n = std::max<long long>(1, want / std::max<long long>(1, tiles));
+    n = std::min<long long>(n, std::min<long long>(kMaxParts, ceil_div(keys, least)));
+    const long long each = ceil_div(ceil_div(keys, n), least) * least;
+    *part_keys = (int)std::min<long long>(each, kMaxLen);
+    *parts = (int)ceil_div(keys, each);
+}
+
+// Geometry checks and the split.  The same for the workspace query and the launch.
+int make_attend_plan(const rt_kv_cache* c, const rt_prefix_batch* b, int q_heads, AttendPlan* p)
+{
+    int st = check_cache(c, false);
+    if (st != RT_OK) return st;
+    if (!b) {
+        set_error("batch is NULL");
+        return RT_ERR_NULL;
+    }
+    const int step = c->format == RT_KV_PLAIN ? 8 : 16;
+    if (c->head_dim % step != 0) {
+        set_error("head_dim=%d is not a multiple of %d", (int)c->head_dim, step);
+        return RT_ERR_SHAPE;
+    }
+    if (q_heads < 1 || q_heads % c->kv_heads != 0) {
+        set_error("q_heads=%d is not a multiple of kv_heads=%d", q_heads, (int)c->kv_heads);
+        return RT_ERR_SHAPE;
+    }
+    if (b->q_len < 1 || b->q_len > RT_MAX_QUERY_LEN) {
+        set_error("q_len=%d outside 1..%d", (int)b->q_len, RT_MAX_QUERY_LEN);
+        return RT_ERR_SHAPE;
+    }
+    if (b->n_seqs < 0 || b->prefix_len < 0 || b->prefix_len > kMaxLen || b->max_suffix_len < 0 || b->max_suffix_len > kMaxLen ||
+        b->page_table_width < 0 || b->page_table_stride < 0 || b->n_prefix_pages < 0) {
+        set_error("n_seqs=%lld prefix_len=%lld max_suffix_len=%lld or a page table size out of range", (long long)b->n_seqs,
+                  (long long)b->prefix_len, (long long)b->max_suffix_len);
+        return RT_ERR_SHAPE;
+    }
+    if (b->n_seqs > 0x7fffffffLL / ((long long)b->q_len * q_heads)) {
+        set_error("n_seqs=%lld times q_len times q_heads exceeds 2^31 - 1", (long long)b->n_seqs);
+        return RT_ERR_SHAPE;
+    }
+    if ((long long)b->n_prefix_pages * c->page_size < b->prefix_len) {
+        set_error("%d prefix pages of %d tokens do not hold %lld", (int)b->n_prefix_pages, (int)c->page_size, (long long)b->prefix_len);
+        return RT_ERR_SHAPE;
+    }
+    if ((long long)b->page_table_width * c->page_size < b->max_suffix_len) {
+        set_error("%d pages of %d tokens do not hold %lld", (int)b->page_table_width, (int)c->page_size, (long long)b->max_suffix_len);
+        return RT_ERR_SHAPE;
+    }
+    rt_limits L;
+    st = current_limits(&L);
+    if (st != RT_OK) return st;
+    memset(p, 0, sizeof(*p));
+    p->padded_dim = c->head_dim <= 64 ? 64 : c->head_dim <= 128 ? 128 : 256;
+    p->group = q_heads / c->kv_heads;
+    p->tokens = b->n_seqs * b->q_len;
+    if (p->tokens == 0) return RT_OK;
+    const long long want = (long long)L.sm_count * 4;
+    if (b->prefix_len > 0) {
+        const long long tiles = ceil_div(p->tokens * p->group, 16) * c->kv_heads;
+        split_keys(b->prefix_len, tiles, want, 128, &p->prefix_parts, &p->prefix_keys);
+        p->prefix_ctas = tiles * p->prefix_parts;
+    }
+    if (b->max_suffix_len > 0) {
+        const long long tiles = ceil_div((long long)b->q_len * p->group, 16) * c->kv_heads * b->n_seqs;
+        split_keys(b->max_suffix_len, tiles, want, 128, &p->suffix_parts, &p->suffix_keys);
+        p->suffix_ctas = tiles * p->suffix_parts;
+    }
+    if (p->prefix_ctas > 0x7fffffffLL || p->suffix_ctas > 0x7fffffffLL) {
+        set_error("the batch needs too many CTAs");
+        return RT_ERR_SHAPE;
+    }
+    const int parts = p->prefix_parts + p->suffix_parts;
+    const int64_t rows = p->tokens * q_heads;
+    if (parts > 1) p->workspace = (int64_t)parts * rows * c->head_dim * 4 + ((int64_t)parts * rows * 4 + 15) / 16 * 16;
+    return RT_OK;
+}
+
+}  // namespace
+}  // namespace rt
+
+extern "C" {
+
+int64_t shared_prefix_attention_workspace_bytes(const rt_kv_cache* cache, const rt_prefix_batch* batch, int32_t q_heads)
+{
+    rt::AttendPlan p;
+    if (rt::make_attend_plan(cache, batch, q_heads, &p) != RT_OK) return -1;
+    return p.workspace;
+}
+
+int shared_prefix_attention_launch(const rt_kv_cache* c, const rt_prefix_batch* b, const void* q, int64_t q_token_stride,
+                                   int64_t q_head_stride, int32_t q_heads, void* out, float* lse, float softmax_scale, int dtype,
+                                   void* workspace, int64_t workspace_bytes, void* stream)
+{
+    using namespace rt;
+    if (dtype != RT_BF16 && dtype != RT_FP16) {
+        set_error("dtype %d is not bf16 or fp16", dtype);
+        return RT_ERR_DTYPE;
+    }
+    AttendPlan p;
+    int st = make_attend_plan(c, b, q_heads, &p);
+    if (st != RT_OK) return st;
+    if (c->format == RT_KV_PLAIN && c->dtype != dtype) {
+        set_error("a plain cache of dtype %d does not serve queries of dtype %d", (int)c->dtype, dtype);
+        return RT_ERR_DTYPE;
+    }
+    if (p.tokens == 0) return RT_OK;
+    const int parts = p.prefix_parts + p.suffix_parts;
+    if (!q || !out || !b->suffix_lens || (b->prefix_len > 0 && !b->prefix_pages) || (b->max_suffix_len > 0 && !b->page_table) ||
+        (p.workspace > 0 && !workspace)) {
+        set_error("a tensor pointer is NULL");
+        return RT_ERR_NULL;
+    }
+    if (parts > 0 && (st = check_cache(c, true)) != RT_OK) return st;
+    if (workspace_bytes < p.workspace) {
+        set_error("workspace of %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)p.workspace);
+        return RT_ERR_CAPACITY;
+    }
+    if (q_token_stride < 0 || q_head_stride < 0) {
+        set_error("negative q stride");
+        return RT_ERR_SHAPE;
+    }
+    const int64_t es = c->format == RT_KV_PLAIN ? 2 : 1;
+    const int64_t strides = (c->n_pages > 1 ? c->page_stride * es : 0) | (c->page_size > 1 ? c->token_stride * es : 0) |
+                            (c->kv_heads > 1 ? c->head_stride * es : 0) | (p.tokens > 1 ? q_token_stride * 2 : 0) |
+                            (q_heads > 1 ? q_head_stride * 2 : 0);
+    if ((((uintptr_t)c->k | (uintptr_t)c->v | (uintptr_t)q | (uintptr_t)out | (uintptr_t)workspace) & 15u) || (strides & 15) ||
+        (((uintptr_t)lse | (uintptr_t)b->suffix_lens | (uintptr_t)b->page_table | (uintptr_t)b->prefix_pages) & 3u)) {
+        set_error("k, v, q, out, workspace and their strides must be multiples of 16 bytes, the other tensors of 4");
+        return RT_ERR_ALIGN;
+    }
+    AttendArgs a;
+    memset(&a, 0, sizeof(a));
+    a.k = (const unsigned char*)c->k;
+    a.v = (const unsigned char*)c->v;
+    a.k_scale = c->k_scale;
+    a.v_scale = c->v_scale;
+    a.page_stride = c->page_stride;
+    a.token_stride = c->token_stride;
+    a.head_stride = c->head_stride;
+    a.scale_page_stride = c->scale_page_stride;
+    a.scale_token_stride = c->scale_token_stride;
+    a.scale_head_stride = c->scale_head_stride;
+    a.n_pages = c->n_pages;
+    a.page_size = (unsigned)c->page_size;
+    a.page_shift = log2_or_minus1((unsigned)c->page_size);
+    a.prefix_pages = b->prefix_pages;
+    a.page_table = b->page_table;
+    a.suffix_lens = b->suffix_lens;
+    a.page_table_stride = b->page_table_stride;
+    a.page_table_width = b->page_table_width;
+    a.prefix_len = (int)b->prefix_len;
+    a.max_suffix_len = (int)b->max_suffix_len;
+    a.n_seqs = (int)b->n_seqs;
+    a.q_len = b->q_len;
+    a.kv_heads = c->kv_heads;
+    a.group = p.group;
+    a.dim = c->head_dim;
+    a.q = (const unsigned char*)q;
+    a.q_token_stride = q_token_stride;
+    a.q_head_stride = q_head_stride;
+    a.score_scale = softmax_scale * 1.4426950408889634f;
+    a.prefix_parts = p.prefix_parts;
+    a.prefix_keys = p.prefix_keys;
+    a.suffix_parts = p.suffix_parts;
+    a.suffix_keys = p.suffix_keys;
+    a.part_out = (float*)workspace;
+    a.part_lse = parts > 1 ? (float*)workspace + (int64_t)parts * p.tokens * q_heads * c->head_dim : nullptr;
+    a.out = out;
+    a.lse = lse;
+    a.status = device_status_word();
+    if (!a.status) return RT_ERR_NO_DEVICE;
+    const AttendKernels k = kernels_of(dtype, c->format, p.padded_dim);
+    void* params[] = {&a};
+    const cudaStream_t s = (cudaStream_t)stream;
+    if (p.prefix_ctas > 0) {
+        st = launch_kernel(k.prefix_rows, dim3((unsigned)p.prefix_ctas), dim3(kRowsThreads), k.rows_smem, s, params);
+        if (st != RT_OK) return st;
+    }
+    if (p.suffix_ctas > 0) {
+        st = launch_kernel(k.suffix_rows, dim3((unsigned)p.suffix_ctas), dim3(kRowsThreads), k.rows_smem, s, params);
+        if (st != RT_OK) return st;
+    }
+    if (parts != 1) {
+        const int64_t ctas = ceil_div(p.tokens * q_heads, kMergePartsThreads / 32);
+        st = launch_kernel(k.merge, dim3((unsigned)ctas), dim3(kMergePartsThreads), 0, s, params);
+    }
+    return st;
+}
+
+}  // extern "C"

@@ -88,6 +88,10 @@ int ensure_dynamic_smem(int index, size_t bytes);
 int* device_status_word();
 void host_pipe_shutdown();  // streams and events of the host-buffer pipeline
 void count_launch(int64_t n = 1);
+// Launches `fn` with the library's launch attributes and counts it.
+int launch_kernel(const void* fn, dim3 grid, dim3 block, size_t dyn_smem, cudaStream_t stream, void** params);
+constexpr int kDeviceSlots = 64;           // devices the library keeps state for
+int current_device_index(int* index);      // 0 .. kDeviceSlots - 1
 
 // Raw grid and feasible set (feasible.cu).  counts, when given, has kRejectReasons + 3 entries:
 // [0..7] hard rejections by reason, [8] heuristic rejections, [9] feasible, [10] raw.
