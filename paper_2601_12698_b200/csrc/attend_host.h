@@ -10,6 +10,8 @@ struct AttendKernels {
     const void* suffix_rows = nullptr;
     const void* merge = nullptr;
     size_t rows_smem = 0;
+    const void* prefix_tc = nullptr;  // tensor-core form of the prefix; NULL for heads that it does not serve
+    size_t tc_smem = 0;
 };
 
 }  // namespace rt

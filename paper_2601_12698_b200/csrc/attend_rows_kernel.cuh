@@ -24,6 +24,7 @@
 #pragma once
 
 #include "attend_common.cuh"
+#include "attend_split.h"
 
 namespace rt {
 
@@ -534,7 +535,7 @@ __global__ void __launch_bounds__(kRowsThreads) attend_rows_kernel(const AttendA
 // Joins the parts of every row: weights 2^(lse_p - max) / sum.  One warp per row; parts that saw no key are not read.
 constexpr int kMergePartsThreads = 128;
 template <typename T>
-__global__ void __launch_bounds__(kMergePartsThreads) merge_parts_kernel(const AttendArgs a)
+__global__ void __launch_bounds__(kMergePartsThreads) merge_parts_kernel(const AttendArgs a, const PrefixSplit split)
 {
     const int lane = threadIdx.x & 31;
     const long long row = (long long)blockIdx.x * (kMergePartsThreads / 32) + (threadIdx.x >> 5);
@@ -542,11 +543,18 @@ __global__ void __launch_bounds__(kMergePartsThreads) merge_parts_kernel(const A
     const long long n_rows = (long long)a.n_seqs * a.q_len * n_heads;
     wait_for_previous_kernel();
     if (row >= n_rows) return;
-    const int seq = (int)((unsigned)(row / n_heads) / (unsigned)a.q_len);
+    const int token = (int)(row / n_heads), head = (int)(row - (long long)token * n_heads);
+    const int seq = (int)((unsigned)token / (unsigned)a.q_len);
     if (__ldg(a.suffix_lens + seq) < 0) return;
-    const int parts = a.prefix_parts + a.suffix_parts;
+    int prefix_parts = a.prefix_parts;
+    if (split.run > 0) {  // the prefix was dealt out by tiles: the row's unit has so many parts
+        const int kv_head = head / a.group, block = (token * a.group + (head - kv_head * a.group)) / kTcBlockRows;
+        prefix_parts = parts_of_unit(split, kv_head * split.blocks + block, block);
+    }
+    const int skip = a.prefix_parts - prefix_parts;  // parts of the workspace that this row does not use
+    const int parts = prefix_parts + a.suffix_parts;
     float top = -INFINITY;
-    for (int p = lane; p < parts; p += 32) top = fmaxf(top, a.part_lse[(long long)p * n_rows + row]);
+    for (int p = lane; p < parts; p += 32) top = fmaxf(top, a.part_lse[(long long)(p < prefix_parts ? p : p + skip) * n_rows + row]);
 #pragma unroll
     for (int s = 16; s >= 1; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
     // lse may be NaN in one part (a NaN score): fmaxf skips it, the sums below do not
@@ -554,7 +562,8 @@ __global__ void __launch_bounds__(kMergePartsThreads) merge_parts_kernel(const A
     const float base = top == -INFINITY ? 0.f : top;
     float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     const int d = lane * 8;
-    for (int p = 0; p < parts; ++p) {
+    for (int i = 0; i < parts; ++i) {
+        const int p = i < prefix_parts ? i : i + skip;
         const float lse = a.part_lse[(long long)p * n_rows + row];
         if (lse == -INFINITY) continue;
         const float w = ex2(lse - base);

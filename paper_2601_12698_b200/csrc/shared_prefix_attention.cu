@@ -1,9 +1,13 @@
 // Entry point of the attention over a shared prefix: argument checks, the split of the work into parts, the launches.
 #include <string.h>
 
+#include <atomic>
+
 #include "attend_common.cuh"
 #include "attend_host.h"
+#include "attend_prefix_kernel.cuh"
 #include "attend_rows_kernel.cuh"
+#include "attend_split.h"
 #include "tuner_internal.h"
 
 namespace rt {
@@ -14,6 +18,7 @@ int log2_or_minus1(unsigned v);
 namespace {
 
 constexpr int kMaxLen = 1 << 30;
+constexpr int kRowsKernelMost = 32;  // rows per key/value head up to which the prefix goes to the 16-row kernel
 constexpr int kMaxParts = 64;  // of the prefix, and of the suffix
 
 struct AttendPlan {
@@ -21,9 +26,25 @@ struct AttendPlan {
     int group;
     long long tokens;
     int prefix_parts, prefix_keys, suffix_parts, suffix_keys;
+    PrefixSplit split;  // run > 0: the prefix goes to the tensor-core kernel
     long long prefix_ctas, suffix_ctas;
     int64_t workspace;
 };
+
+// The kernel's dynamic shared memory is beyond the default limit: raised once per device and kernel.
+int allow_smem(const AttendKernels& k, int dtype, int format, int padded_dim)
+{
+    static std::atomic<unsigned char> done[kDeviceSlots][2][3][2];
+    int device;
+    int st = current_device_index(&device);
+    if (st != RT_OK) return st;
+    std::atomic<unsigned char>& flag = done[device][dtype][format][padded_dim > 64];
+    if (!flag.load(std::memory_order_acquire)) {
+        RT_CUDA_OK(cudaFuncSetAttribute(k.prefix_tc, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)k.tc_smem));
+        flag.store(1, std::memory_order_release);
+    }
+    return RT_OK;
+}
 
 AttendKernels kernels_of(int dtype, int format, int padded_dim)
 {
@@ -94,7 +115,18 @@ int make_attend_plan(const rt_kv_cache* c, const rt_prefix_batch* b, int q_heads
     p->tokens = b->n_seqs * b->q_len;
     if (p->tokens == 0) return RT_OK;
     const long long want = (long long)L.sm_count * 4;
-    if (b->prefix_len > 0) {
+    const long long rows_per_kv_head = p->tokens * p->group;
+    if (b->prefix_len > 0 && p->padded_dim <= 128 && rows_per_kv_head > kRowsKernelMost) {
+        PrefixSplit& s = p->split;
+        s.tiles = (int)ceil_div(b->prefix_len, kTcTile);
+        s.rows = (int)rows_per_kv_head;
+        s.blocks = (int)ceil_div(rows_per_kv_head, kTcBlockRows);
+        const long long total = (long long)s.tiles * s.blocks * c->kv_heads;
+        const long long run = ceil_div(total, L.sm_count);
+        s.run = (int)std::min<long long>(run, 1 << 30);
+        p->prefix_ctas = ceil_div(total, s.run);
+        p->prefix_parts = most_parts(s);
+    } else if (b->prefix_len > 0) {
         const long long tiles = ceil_div(p->tokens * p->group, 16) * c->kv_heads;
         split_keys(b->prefix_len, tiles, want, 128, &p->prefix_parts, &p->prefix_keys);
         p->prefix_ctas = tiles * p->prefix_parts;
@@ -209,9 +241,13 @@ int shared_prefix_attention_launch(const rt_kv_cache* c, const rt_prefix_batch* 
     a.status = device_status_word();
     if (!a.status) return RT_ERR_NO_DEVICE;
     const AttendKernels k = kernels_of(dtype, c->format, p.padded_dim);
-    void* params[] = {&a};
+    void* params[] = {&a, &p.split};
     const cudaStream_t s = (cudaStream_t)stream;
-    if (p.prefix_ctas > 0) {
+    if (p.split.run > 0) {
+        st = allow_smem(k, dtype, c->format, p.padded_dim);
+        if (st == RT_OK) st = launch_kernel(k.prefix_tc, dim3((unsigned)p.prefix_ctas), dim3(kTcThreads), k.tc_smem, s, params);
+        if (st != RT_OK) return st;
+    } else if (p.prefix_ctas > 0) {
         st = launch_kernel(k.prefix_rows, dim3((unsigned)p.prefix_ctas), dim3(kRowsThreads), k.rows_smem, s, params);
         if (st != RT_OK) return st;
     }

@@ -381,3 +381,124 @@ def test_cache_then_attention_then_merge(B, oracle_lib):
     assert oracle_lib.compare_mixed(merged.cpu(), v_ref, tol=2.0, tol_abs=1e-5)[1] == 0
     assert oracle_lib.compare_mixed(s.cpu(), s_ref, tol=1e-5, tol_abs=1e-5)[1] == 0
     assert B.rt_device_status() == 0
+
+
+# ---- batches large enough for the tensor-core form of the prefix -------------------------------------------------------
+
+MANY = [  # seqs, prefix, heads, kv_heads, dim, page, q_len
+    (40, 128, 1, 1, 128, 16, 1),        # one tile: the second stream has none
+    (40, 500, 8, 8, 64, 16, 1),         # 40 rows: narrow blocks
+    (33, 1000, 8, 2, 128, 24, 1),       # 132 rows: the second stream has 4
+    (70, 700, 4, 1, 96, 16, 2),         # 560 rows: two wide blocks and a narrow one
+    (300, 5121, 8, 8, 64, 64, 1),       # more tiles than SMs: runs that end one unit and begin the next
+    (64, 1537, 16, 4, 128, 1, 1),
+    (9, 3000, 40, 8, 80, 16, 5),        # 225 rows, prefix ends inside a tile and a page
+    (20, 130, 64, 1, 128, 128, 1),      # 1280 rows of one key/value head
+]
+
+
+@pytest.mark.parametrize("fmt", ["plain", "e4m3", "int8"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("shape", MANY, ids=[f"{s[0]}x{s[6]}_p{s[1]}_{s[2]}of{s[3]}x{s[4]}_page{s[5]}" for s in MANY])
+def test_many_rows_match_the_plain_form(B, dtype, fmt, shape):
+    seqs, prefix, heads, kv_heads, dim, page, q_len = shape
+    lens = [-1 if i % 11 == 7 else (i * 5) % 23 for i in range(seqs)]
+    p = Problem(B, lens, prefix, heads, kv_heads, dim, page, dtype, fmt, q_len, seed=prefix)
+    out, lse = p.launch()
+    assert B.rt_device_status() == 0
+    p.check(out, lse)
+    again, lse_again = p.launch()
+    assert torch.equal(out.view(torch.int16), again.view(torch.int16)) and torch.equal(lse, lse_again)
+
+
+@pytest.mark.parametrize("fmt", ["plain", "e4m3", "int8"])
+@pytest.mark.parametrize("scale", [0.0, -0.3, 20.0])
+def test_many_rows_scales_of_the_scores(B, fmt, scale):
+    p = Problem(B, [3] * 40, 700, 4, 1, 64, 16, "bf16", fmt, seed=9, scale=scale)
+    p.check(*p.launch())
+
+
+@pytest.mark.parametrize("fmt,spread", [("plain", 1e-20), ("plain", 1e4), ("e4m3", 1e-9), ("e4m3", 3e4), ("int8", 3e4), ("int8", 1e-9)])
+def test_many_rows_magnitudes(B, fmt, spread):
+    p = Problem(B, [3] * 40, 700, 4, 1, 64, 16, "bf16", fmt, seed=10, spread=spread, scale=0.1 / spread if spread > 1 else 0.1)
+    p.check(*p.launch())
+
+
+@pytest.mark.parametrize("fmt", ["plain", "e4m3"])
+def test_rising_scores_move_the_reference(B, fmt):
+    """Keys whose scores rise through the prefix by far more than the margin at which a row's reference is moved."""
+    p = Problem(B, [2] * 70, 1500, 4, 1, 64, 16, "bf16", fmt, seed=12)
+    q = torch.ones(70, 1, 4, 64).bfloat16()
+    q[::2] = -1.0
+    p.q = q
+    ramp = torch.linspace(-30, 30, 1500)
+    for i in range(1500):
+        at = int(p.prefix_pages[i // 16]), i % 16
+        x = torch.full((1, 64), float(ramp[i])).bfloat16()
+        if fmt == "plain":
+            p.cache.k[at] = x.cuda()
+            p.kv64[0][at] = x.double()
+        else:
+            codes, unit = R.quantise(x, fmt)
+            p.cache.k.view(torch.uint8)[at] = codes.view(torch.uint8).cuda()
+            p.cache.k_scale[at] = unit.cuda()
+            p.kv64[0][at] = R.dequantise(codes, unit)
+    p.check(*p.launch())
+
+
+def test_many_rows_pages_outside_the_cache(B):
+    p = Problem(B, [5] * 40, 16 * 20, 4, 1, 128, 16, seed=6)
+    bad = [3, 4, 19]
+    p.prefix_pages[bad] = torch.tensor([-1, 10 ** 6, p.cache.n_pages], dtype=torch.int32)
+    p.batch = p.make_batch()
+    assert B.rt_device_status() == 0
+    out, lse = p.launch()
+    assert B.rt_device_status() == B.RT_ERR_INDEX
+    kept = [i for i in range(20) if i not in bad]
+    k, v = p.kv64
+    p.check(out, lse, R.attend(k, v, p.prefix_pages[kept], 16 * 17, p.table, p.lens, p.q, p.scale))
+    p.prefix_pages[:] = -1  # nothing of the prefix is there
+    p.batch = p.make_batch()
+    out, lse = p.launch()
+    assert B.rt_device_status() == B.RT_ERR_INDEX
+    p.check(out, lse, R.attend(k, v, p.prefix_pages, 0, p.table, p.lens, p.q, p.scale))
+
+
+def test_many_rows_visible_infinities_and_nan(B):
+    p = Problem(B, [5] * 40, 400, 4, 1, 64, 16, seed=4)
+    out0, lse0 = p.launch()
+    p.cache.v[int(p.prefix_pages[20]), 2, 0, 11] = float("inf")
+    out, lse = p.launch()
+    assert bool((out[..., 11].float() == math.inf).all()) and torch.equal(lse, lse0)
+    rest = torch.ones(64, dtype=torch.bool)
+    rest[11] = False
+    assert torch.equal(out[..., rest], out0[..., rest])
+    q = p.q.cuda()
+    q[7, 0, 1, 5] = float("nan")
+    out, lse = p.launch(q=q)
+    assert bool(torch.isnan(out[7, 0, 1].float()).all()) and bool(torch.isnan(lse[7, 0, 1]))
+    assert int(torch.isnan(lse).sum()) == 1
+
+
+def test_many_rows_in_a_graph_with_the_options(B):
+    p = Problem(B, [3, 0, 9, -1] * 20, 900, 8, 2, 128, 16, seed=30)
+    out, lse = p.launch()
+    p.check(out, lse)
+    q, ws = p.q.cuda(), B.shared_prefix_attention_workspace(p.cache, p.batch, p.heads)
+    got, got_lse = torch.full_like(out, 3.0), torch.full_like(lse, 3.0)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        for _ in range(3):
+            B.shared_prefix_attention_launch(p.cache, p.batch, q, got, got_lse, ws, softmax_scale=p.scale)
+    for _ in range(2):
+        ws.fill_(255)  # NaN: nothing of it may survive
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, out) and torch.equal(got_lse, lse)
+    try:
+        assert B.lib.rt_set_option(B.RT_OPTION_PROGRAMMATIC_LAUNCH, 0) == B.RT_OK
+        serial, lse_serial = p.launch()
+    finally:
+        assert B.lib.rt_set_option(B.RT_OPTION_PROGRAMMATIC_LAUNCH, 1) == B.RT_OK
+    assert torch.equal(serial, out) and torch.equal(lse_serial, lse)
