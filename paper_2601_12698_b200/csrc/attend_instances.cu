@@ -28,6 +28,7 @@ rt::AttendKernels RT_CONCAT(rt_attend_kernels_, RT_UNIT_NAME)(int padded_dim)
         k.prefix_rows = (const void*)attend_rows_kernel<RT_UNIT_T, RT_UNIT_FMT, DP, true>;                   \
         k.suffix_rows = (const void*)attend_rows_kernel<RT_UNIT_T, RT_UNIT_FMT, DP, false>;                  \
         k.rows_smem = RowsShape<RT_UNIT_FMT, DP>::kSmem;                                                     \
+        k.merge = (const void*)merge_parts_kernel<RT_UNIT_T, DP>;                                            \
         tensor_core_kernel<DP>(&k);                                                                          \
         break;
         RT_CASE(64)
@@ -35,6 +36,5 @@ rt::AttendKernels RT_CONCAT(rt_attend_kernels_, RT_UNIT_NAME)(int padded_dim)
         RT_CASE(256)
 #undef RT_CASE
     }
-    k.merge = (const void*)merge_parts_kernel<RT_UNIT_T>;
     return k;
 }

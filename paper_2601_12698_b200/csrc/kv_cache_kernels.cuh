@@ -182,6 +182,15 @@ __device__ __forceinline__ Chunk<E> encode(const float (&f)[E], float inv)
 template <int FMT, int E>
 __device__ __forceinline__ void decode(const Chunk<E>& c, float (&f)[E])
 {
+    if constexpr (FMT == kKvE4m3 && E % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < E; i += 2) {
+            const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(c.w[i / 4] >> (8 * (i % 4))), __NV_E4M3);
+            f[i] = __half2float(__half(__half_raw{h.x}));
+            f[i + 1] = __half2float(__half(__half_raw{h.y}));
+        }
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < E; ++i) {
         const uint32_t b = (c.w[i / 4] >> (8 * (i % 4))) & 0xFFu;
@@ -200,54 +209,60 @@ __device__ __forceinline__ constexpr float code_max()
     return FMT == kKvE4m3 ? 448.0f : 127.0f;
 }
 
-// Group, vector and place arithmetic shared by both kernels: vector v of the CTA (v counts token, side, head).
+// Vector v of a CTA: v counts token, side, head.
 struct CacheVector {
     bool live;
-    int side, head;
-    long long token;
-    size_t entry, scale_entry;  // element offsets of the entry and of its scale in the cache
+    int side, head, token;  // token: within the CTA
 };
-__device__ __forceinline__ CacheVector cache_vector(const CacheArgs& a, int v, int per_token, long long first_token, long long n_here)
+__device__ __forceinline__ CacheVector cache_vector(const CacheArgs& a, int v, int per_token, int n_vec)
 {
     CacheVector c;
-    const int t = (int)((unsigned)v / (unsigned)per_token), in_token = v - t * per_token;
+    c.live = v < n_vec;
+    c.token = (int)((unsigned)(c.live ? v : 0) / (unsigned)per_token);
+    const int in_token = (c.live ? v : 0) - c.token * per_token;
     c.side = in_token >= a.heads;
     c.head = in_token - (c.side ? a.heads : 0);
-    c.token = first_token + t;
-    c.live = t < n_here;
-    const long long slot = c.live ? __ldg(a.slots + c.token) : -1;
-    if (slot >= a.n_slots) atomicExch(a.status, kDeviceIndexCode);
-    c.live = slot >= 0 && slot < a.n_slots;
-    const SlotPlace p = place_of(c.live ? slot : 0, a.page_size, a.page_shift);
-    c.entry = (size_t)p.page * a.page_stride + (size_t)p.offset * a.entry_stride + (size_t)c.head * a.head_stride;
-    c.scale_entry = (size_t)p.page * a.scale_page_stride + (size_t)p.offset * a.scale_entry_stride + (size_t)c.head * a.scale_head_stride;
     return c;
+}
+// Where the entry and its scale lie; false: no such entry (padding, or a slot beyond the cache).
+__device__ __forceinline__ bool cache_place(const CacheArgs& a, long long slot, int head, size_t& entry, size_t& scale_entry)
+{
+    if (slot >= a.n_slots) atomicExch(a.status, kDeviceIndexCode);
+    if (slot < 0 || slot >= a.n_slots) return false;
+    const SlotPlace p = place_of(slot, a.page_size, a.page_shift);
+    entry = (size_t)p.page * a.page_stride + (size_t)p.offset * a.entry_stride + (size_t)head * a.head_stride;
+    scale_entry = (size_t)p.page * a.scale_page_stride + (size_t)p.offset * a.scale_entry_stride + (size_t)head * a.scale_head_stride;
+    return true;
 }
 
 // T: type of key and value.  E elements per lane and chunk, NCH chunks per lane, U vectors in flight per group.
+// The key and value vectors do not depend on the slots, so both are fetched at once.  The two divisions of a vector are
+// made by one lane for each of the U vectors at a time, not by all lanes for all of them: they are correctly rounded ones
+// (the codes are the definition's bit for bit) and cost as much as the rest of a vector.
 template <typename T, int FMT, int E, int LANES, int NCH, int U>
 __global__ void __launch_bounds__(kCacheThreads) kv_cache_write_kernel(const CacheArgs a)
 {
     constexpr int IN = E * (int)sizeof(T);
+    static_assert(U <= LANES, "a lane for every vector in flight");
     const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
     constexpr int GROUPS = kCacheThreads / LANES;
     const int per_token = 2 * a.heads;
     const long long first = (long long)blockIdx.x * a.tokens_per_cta;
-    const int n_here = (int)min((long long)a.tokens_per_cta, a.n_tokens - first);
-    const int n_vec = n_here * per_token;
+    const int n_vec = (int)min((long long)a.tokens_per_cta, a.n_tokens - first) * per_token;
     wait_for_previous_kernel();
     for (int v0 = 0; v0 < n_vec; v0 += GROUPS * U) {  // uniform over the CTA: whole warps take part in the shuffles
         Chunk<IN> x[U][NCH];
-        CacheVector cv[U];
+        long long slot[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            cv[u] = cache_vector(a, v0 + u * GROUPS + group, per_token, first, n_here);
-            const unsigned char* src = a.tokens[cv[u].side] +
-                ((size_t)cv[u].token * a.token_stride[cv[u].side] + (size_t)cv[u].head * a.token_head_stride[cv[u].side]) * sizeof(T);
+            const CacheVector c = cache_vector(a, v0 + u * GROUPS + group, per_token, n_vec);
+            slot[u] = c.live ? __ldg(a.slots + first + c.token) : -1;
+            const unsigned char* src = a.tokens[c.side] +
+                ((size_t)(first + c.token) * a.token_stride[c.side] + (size_t)c.head * a.token_head_stride[c.side]) * sizeof(T);
 #pragma unroll
             for (int i = 0; i < NCH; ++i) {
                 const int e = (i * LANES + lane) * E;
-                if (cv[u].live && e < a.dim) {
+                if (c.live && e < a.dim) {
                     x[u][i] = ld_chunk<IN>(src + (size_t)e * sizeof(T));
                 } else {
 #pragma unroll
@@ -255,17 +270,11 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_write_kernel(const Cac
                 }
             }
         }
+        float my_inv = 0.f, my_scale = 0.f;  // of the vector that this lane divides for: lane % U
+        if constexpr (FMT != kKvPlain) {
+            uint32_t my_top = 0;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if constexpr (FMT == kKvPlain) {
-                if (!cv[u].live) continue;
-                unsigned char* dst = a.side[cv[u].side] + cv[u].entry * sizeof(T);
-#pragma unroll
-                for (int i = 0; i < NCH; ++i) {
-                    const int e = (i * LANES + lane) * E;
-                    if (e < a.dim) st_chunk<IN>(dst + (size_t)e * sizeof(T), x[u][i]);
-                }
-            } else {
+            for (int u = 0; u < U; ++u) {
                 uint32_t top = 0;
 #pragma unroll
                 for (int i = 0; i < NCH; ++i) top = join_magnitude<T, IN>(top, x[u][i]);
@@ -275,14 +284,30 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_write_kernel(const Cac
                     if constexpr (sizeof(T) == 4) top = max(top, other);
                     else top = __vmaxu2(top, other);
                 }
-                if (!cv[u].live) continue;
-                float amax = magnitude_of<T>(top);
-                amax = amax < 1e-12f ? 1e-12f : amax;  // keeps a NaN
-                // correctly rounded divisions: the codes are the definition's bit for bit
-                const float inv = __fdiv_rn(code_max<FMT>(), amax);
-                float scale = __fdiv_rn(amax, code_max<FMT>());
-                if (!(amax < INFINITY)) scale = __uint_as_float(0x7FC00000u);
-                unsigned char* dst = a.side[cv[u].side] + cv[u].entry;
+                if (u == 0 || lane % U == u) my_top = top;
+            }
+            float amax = magnitude_of<T>(my_top);
+            amax = amax < 1e-12f ? 1e-12f : amax;  // keeps a NaN
+            my_inv = __fdiv_rn(code_max<FMT>(), amax);
+            my_scale = __fdiv_rn(amax, code_max<FMT>());
+            if (!(amax < INFINITY)) my_scale = __uint_as_float(0x7FC00000u);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const CacheVector c = cache_vector(a, v0 + u * GROUPS + group, per_token, n_vec);
+            const int from = (threadIdx.x & 31) - lane + u;  // lane u of this group
+            const float inv = __shfl_sync(0xFFFFFFFFu, my_inv, from), scale = __shfl_sync(0xFFFFFFFFu, my_scale, from);
+            size_t entry, scale_entry;
+            if (!cache_place(a, slot[u], c.head, entry, scale_entry)) continue;
+            if constexpr (FMT == kKvPlain) {
+                unsigned char* dst = a.side[c.side] + entry * sizeof(T);
+#pragma unroll
+                for (int i = 0; i < NCH; ++i) {
+                    const int e = (i * LANES + lane) * E;
+                    if (e < a.dim) st_chunk<IN>(dst + (size_t)e * sizeof(T), x[u][i]);
+                }
+            } else {
+                unsigned char* dst = a.side[c.side] + entry;
 #pragma unroll
                 for (int i = 0; i < NCH; ++i) {
                     const int e = (i * LANES + lane) * E;
@@ -292,7 +317,7 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_write_kernel(const Cac
                         st_chunk<E>(dst + e, encode<FMT, E>(f, inv));
                     }
                 }
-                if (lane == 0) a.scale[cv[u].side][cv[u].scale_entry] = scale;
+                if (lane == 0) a.scale[c.side][scale_entry] = scale;
             }
         }
     }
@@ -308,30 +333,40 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_read_kernel(const Cach
     constexpr int GROUPS = kCacheThreads / LANES;
     const int per_token = 2 * a.heads;
     const long long first = (long long)blockIdx.x * a.tokens_per_cta;
-    const int n_here = (int)min((long long)a.tokens_per_cta, a.n_tokens - first);
-    const int n_vec = n_here * per_token;
+    const int n_vec = (int)min((long long)a.tokens_per_cta, a.n_tokens - first) * per_token;
     wait_for_previous_kernel();
     for (int v0 = 0; v0 < n_vec; v0 += GROUPS * U) {
         Chunk<HELD> x[U][NCH];
         float scale[U];
-        CacheVector cv[U];
+        long long slot[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            cv[u] = cache_vector(a, v0 + u * GROUPS + group, per_token, first, n_here);
-            const unsigned char* src = a.side[cv[u].side] + cv[u].entry * HELD_SIZE;
+            const CacheVector c = cache_vector(a, v0 + u * GROUPS + group, per_token, n_vec);
+            slot[u] = c.live ? __ldg(a.slots + first + c.token) : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const CacheVector c = cache_vector(a, v0 + u * GROUPS + group, per_token, n_vec);
+            size_t entry, scale_entry;
             scale[u] = 0.f;
-            if (FMT != kKvPlain && cv[u].live) scale[u] = __ldg(a.scale[cv[u].side] + cv[u].scale_entry);
+            if (!cache_place(a, slot[u], c.head, entry, scale_entry)) {
+                slot[u] = -1;
+                continue;
+            }
+            const unsigned char* src = a.side[c.side] + entry * HELD_SIZE;
+            if (FMT != kKvPlain) scale[u] = __ldg(a.scale[c.side] + scale_entry);
 #pragma unroll
             for (int i = 0; i < NCH; ++i) {
                 const int e = (i * LANES + lane) * E;
-                if (cv[u].live && e < a.dim) x[u][i] = ld_chunk<HELD>(src + (size_t)e * HELD_SIZE);
+                if (e < a.dim) x[u][i] = ld_chunk<HELD>(src + (size_t)e * HELD_SIZE);
             }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (!cv[u].live) continue;
-            unsigned char* dst = a.tokens[cv[u].side] +
-                ((size_t)cv[u].token * a.token_stride[cv[u].side] + (size_t)cv[u].head * a.token_head_stride[cv[u].side]) * sizeof(T);
+            if (slot[u] < 0) continue;
+            const CacheVector c = cache_vector(a, v0 + u * GROUPS + group, per_token, n_vec);
+            unsigned char* dst = a.tokens[c.side] +
+                ((size_t)(first + c.token) * a.token_stride[c.side] + (size_t)c.head * a.token_head_stride[c.side]) * sizeof(T);
 #pragma unroll
             for (int i = 0; i < NCH; ++i) {
                 const int e = (i * LANES + lane) * E;
