@@ -122,6 +122,14 @@ __device__ __forceinline__ uint32_t pick_half2(uint32_t a, uint32_t b)
     }
 }
 
+// 16 codes of a tile that is read once.
+__device__ __forceinline__ uint4 ld_codes(const unsigned char* p)
+{
+    uint4 w;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "l"(p));
+    return w;
+}
+
 // The power of two that brings a row's largest magnitude into [2^14, 2^15), so that a bf16 row fits fp16 without loss
 // (elements 2^-28 below the largest lose bits, which no binary32 sum would keep either).  Its inverse is exact too.
 __device__ __forceinline__ float fp16_row_factor(float amax)

@@ -5,13 +5,14 @@
 
 namespace rt {
 
+// One form of a kernel and the dynamic shared memory it is launched with.
+struct AttendKernel {
+    const void* fn = nullptr;
+    size_t smem = 0;
+};
+enum { kPrefixTiles = 0, kPrefixKeys16 = 1, kPrefixKeys64 = 2, kSuffixKeys16 = 3, kSuffixKeys64 = 4, kMergeParts = 5, kAttendKernels = 6 };
 struct AttendKernels {
-    const void* prefix_rows = nullptr;
-    const void* suffix_rows = nullptr;
-    const void* merge = nullptr;
-    size_t rows_smem = 0;
-    const void* prefix_tc = nullptr;  // tensor-core form of the prefix; NULL for heads that it does not serve
-    size_t tc_smem = 0;
+    AttendKernel k[kAttendKernels];  // fn == NULL: the form does not serve heads of that size
 };
 
 }  // namespace rt

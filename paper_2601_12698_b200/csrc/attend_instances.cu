@@ -1,40 +1,35 @@
 // Instances of the attention kernels for one element type (RT_UNIT_T) and one cache format (RT_UNIT_FMT); the build
 // script compiles this file once per combination.
-#include "attend_prefix_kernel.cuh"
-#include "attend_rows_kernel.cuh"
 #include "attend_host.h"
+#include "attend_keys_kernel.cuh"
+#include "attend_merge_kernel.cuh"
+#include "attend_prefix_kernel.cuh"
 
 #define RT_CONCAT_(a, b) a##b
 #define RT_CONCAT(a, b) RT_CONCAT_(a, b)
 
 namespace {
+
 template <int DP>
-void tensor_core_kernel(rt::AttendKernels* k)
+rt::AttendKernels kernels()
 {
-    if constexpr (DP <= 128) {  // heads of 256 leave tensor memory no room for two streams
-        k->prefix_tc = (const void*)rt::attend_prefix_kernel<RT_UNIT_T, RT_UNIT_FMT, DP>;
-        k->tc_smem = rt::PrefixShape<RT_UNIT_FMT, DP>::kSmem;
-    }
+    using namespace rt;
+    using T = RT_UNIT_T;
+    constexpr int FMT = RT_UNIT_FMT;
+    AttendKernels a;
+    if constexpr (DP <= 128)  // heads of 256 leave tensor memory no room for two streams
+        a.k[kPrefixTiles] = {(const void*)attend_prefix_kernel<T, FMT, DP>, PrefixShape<FMT, DP>::kSmem};
+    a.k[kPrefixKeys16] = {(const void*)attend_keys_kernel<T, FMT, DP, 16, true>, KeysShape<FMT, DP, 16>::kSmem};
+    a.k[kPrefixKeys64] = {(const void*)attend_keys_kernel<T, FMT, DP, 64, true>, KeysShape<FMT, DP, 64>::kSmem};
+    a.k[kSuffixKeys16] = {(const void*)attend_keys_kernel<T, FMT, DP, 16, false>, KeysShape<FMT, DP, 16>::kSmem};
+    a.k[kSuffixKeys64] = {(const void*)attend_keys_kernel<T, FMT, DP, 64, false>, KeysShape<FMT, DP, 64>::kSmem};
+    a.k[kMergeParts] = {(const void*)merge_parts_kernel<T, DP>, 0};
+    return a;
 }
+
 }  // namespace
 
 rt::AttendKernels RT_CONCAT(rt_attend_kernels_, RT_UNIT_NAME)(int padded_dim)
 {
-    using namespace rt;
-    AttendKernels k;
-    switch (padded_dim) {
-#define RT_CASE(DP)                                                                                          \
-    case DP:                                                                                                 \
-        k.prefix_rows = (const void*)attend_rows_kernel<RT_UNIT_T, RT_UNIT_FMT, DP, true>;                   \
-        k.suffix_rows = (const void*)attend_rows_kernel<RT_UNIT_T, RT_UNIT_FMT, DP, false>;                  \
-        k.rows_smem = RowsShape<RT_UNIT_FMT, DP>::kSmem;                                                     \
-        k.merge = (const void*)merge_parts_kernel<RT_UNIT_T, DP>;                                            \
-        tensor_core_kernel<DP>(&k);                                                                          \
-        break;
-        RT_CASE(64)
-        RT_CASE(128)
-        RT_CASE(256)
-#undef RT_CASE
-    }
-    return k;
+    return padded_dim == 64 ? kernels<64>() : padded_dim == 128 ? kernels<128>() : kernels<256>();
 }

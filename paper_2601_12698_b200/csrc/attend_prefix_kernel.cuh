@@ -31,10 +31,11 @@
 
 #include "attend_common.cuh"
 #include "attend_split.h"
+#include "tensor_core.cuh"
 
 namespace rt {
 
-constexpr int kTcThreads = 416;
+constexpr int kTcThreads = 512;
 constexpr int kTcSlots = 4;   // ring of key and value tiles
 constexpr int kTcAux = 4;     // tiles whose per-key constants are kept
 
@@ -45,81 +46,11 @@ struct PrefixShape {
     static constexpr int kAuxFloats = kQuant ? 3 * kTcTile : kTcTile;
     static constexpr size_t kAuxAt = (size_t)(2 + kTcSlots) * kTileBytes;
     static constexpr size_t kOffsetsAt = kAuxAt + (size_t)kTcAux * kAuxFloats * 4;
-    static constexpr size_t kSmem = kOffsetsAt + (size_t)kTcAux * kTcTile * 8 + 1024;  // 1024: alignment of the tiles
+    // Where results wait to be written row by row, 4 KB per softmax warp: heads of 64 have room for it, heads of 128 use the
+    // query tiles, which are free by then.
+    static constexpr size_t kStageAt = kOffsetsAt + (size_t)kTcAux * kTcTile * 8;
+    static constexpr size_t kSmem = kStageAt + (DP == 64 ? 8 * 4096 : 0) + 1024;  // 1024: alignment of the tiles
 };
-
-// ---- tensor memory and matrix instructions -----------------------------------------------------------------
-
-__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32])
-{
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,"
-        "%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(addr));
-}
-__device__ __forceinline__ void tmem_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t (&r)[32])
-{
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,"
-        "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]),
-        "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
-        "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
-        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
-        : "memory");
-}
-__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t (&r)[16])
-{
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(r[0]), "r"(r[1]),
-        "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
-        "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr)
-        : "memory");
-}
-__device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-
-__device__ __forceinline__ void tc_commit(uint64_t* bar)
-{
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-// D (128 x N, binary32, tensor memory) (+)= A B with A and B described in shared memory.
-__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate)
-{
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-                 "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate) : "memory");
-}
-// The same with A (128 x 16 of 16-bit elements, two to a column) in tensor memory.
-__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate)
-{
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-                 "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate) : "memory");
-}
-// Shared memory matrix descriptor: 128-byte swizzle, strides in bytes (leading: between 64-element column blocks of an
-// operand whose rows are the product's inner axis; stride: between groups of eight rows).
-__device__ __forceinline__ uint64_t tc_descriptor(uint32_t smem_addr, uint32_t leading, uint32_t stride)
-{
-    return (uint64_t)((smem_addr >> 4) & 0x3FFFu) | ((uint64_t)((leading >> 4) & 0x3FFFu) << 16) |
-           ((uint64_t)((stride >> 4) & 0x3FFFu) << 32) | (1ull << 46) | (2ull << 61);
-}
-// Instruction descriptor: binary32 accumulator, A and B both bf16 or both fp16, M = 128.
-template <typename M>
-__device__ __forceinline__ constexpr uint32_t tc_instruction(int n, bool b_inner_rows)
-{
-    const uint32_t type = std::is_same<M, __nv_bfloat16>::value ? 1u : 0u;
-    return (1u << 4) | (type << 7) | (type << 10) | ((b_inner_rows ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
-}
-
-__device__ __forceinline__ void mbarrier_arrive(uint64_t* bar)
-{
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
 
 template <typename T, int FMT, int DP>
 __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const AttendArgs a, const PrefixSplit split)
@@ -127,8 +58,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
     using S = PrefixShape<FMT, DP>;
     constexpr bool kQuant = S::kQuant;
     using M = typename std::conditional<kQuant, __half, T>::type;
-    constexpr int kBlockBytes = kTcTile * 128;  // one 64-dim column block of a tile
-    constexpr uint32_t kScoreIdesc = tc_instruction<M>(kTcTile, false), kOutIdesc = tc_instruction<M>(DP, true);
+    constexpr int kBlockBytes = kTileBlockBytes;  // one 64-dim column block of a tile
+    constexpr uint32_t kScoreIdesc = tc_instruction<M>(kTcTile, false, false), kOutIdesc = tc_instruction<M>(DP, false, true);
     constexpr uint32_t kColO = 2 * kTcTile;
 
     extern __shared__ unsigned char smem_raw[];
@@ -139,6 +70,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
     long long* offsets = reinterpret_cast<long long*>(smem + S::kOffsetsAt);
     __shared__ __align__(8) uint64_t full[kTcSlots], empty[kTcSlots], aux_full[kTcAux], s_full[2], p_full[2], o_full[2], q_full, drained;
     __shared__ uint32_t tmem_base;
+    __shared__ float row_factor[2][kQuant ? 128 : 1];
     __shared__ uint32_t ragged[kTcAux];  // one byte per fetching warp: some key of its quarter of the tile is not there
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -177,11 +109,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
 
     if (warp < 8) {
         // ---- softmax streams ----
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
         const int s = warp >> 2, r = (warp & 3) * 32 + lane;
         const uint32_t lane_base = tmem + ((uint32_t)(warp & 3) << 21);
         const uint32_t s_col = lane_base + s * kTcTile, o_col = lane_base + kColO + s * DP;
         const bool flip = a.score_scale < 0.f;
         const float scale = fabsf(a.score_scale);
+        const int n_heads = a.kv_heads * a.group;
+        const long long n_rows = (long long)a.n_seqs * a.q_len * n_heads;
         uint32_t n_s = 0, n_o = 0, tile_no = 0;
         for (long long at = begin; at < end;) {
             const int unit = (int)(at / split.tiles), block = unit % split.blocks, kv_head = unit / split.blocks;
@@ -189,50 +124,61 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
             const int n = (int)min((long long)(split.tiles - tile0), end - at);
             const bool narrow = narrow_block(split, block);
             const int first_row = block * kTcBlockRows + (narrow ? 0 : s * 128);
-            // Query rows into shared memory: this thread's row (narrow form: the first stream's threads do it for both).
-            // Nobody reads the tiles any more: this thread's stream has seen its last product of the previous unit, and
-            // the barrier makes that so for both.
+            // [token][head] index of row i of this stream's 128, -1: no such row
+            const auto row_index = [&](int i) -> long long {
+                const int row = first_row + i;
+                if (row >= split.rows) return -1;
+                const int token = row / a.group;
+                return (long long)token * n_heads + kv_head * a.group + (row - token * a.group);
+            };
+            // Query rows into shared memory, DP / 8 lanes to a row, so that a row is read in one piece.  Nobody reads the tiles
+            // any more: each stream has seen its last product of the previous unit, and the barrier makes that so for both.
+            // Narrow form: the first stream's threads do it for both.
             asm volatile("bar.sync 1, 256;" ::: "memory");
-            float row_c = scale;
-            const int row = first_row + r;
-            const bool live = row < split.rows;
-            const int token = live ? row / a.group : 0, head = kv_head * a.group + (live ? row - token * a.group : 0);
-            {
-                const unsigned char* src = a.q + ((long long)token * a.q_token_stride + (long long)head * a.q_head_stride) * 2;
-                float factor = 1.f;
-                if constexpr (kQuant) {
-                    uint32_t top = 0;
-                    if (live) {
-#pragma unroll 4
-                        for (int e = 0; e < a.dim; e += 8) {
-                            const uint4 w = __ldg(reinterpret_cast<const uint4*>(src + e * 2));
-                            top = __vmaxu2(top, __vmaxu2(__vmaxu2(w.x & 0x7FFF7FFFu, w.y & 0x7FFF7FFFu), __vmaxu2(w.z & 0x7FFF7FFFu, w.w & 0x7FFF7FFFu)));
-                        }
-                    }
-                    factor = fp16_row_factor(Codec<T, 16>::to_float16(max(top & 0xFFFFu, top >> 16)));
-                    row_c *= __frcp_rn(factor);
-                }
-                if (!narrow || s == 0) {
-                    unsigned char* dst = q_tiles + s * S::kTileBytes + r * 128;
-#pragma unroll 4
-                    for (int u = 0; u < DP / 8; ++u) {
-                        uint4 w = make_uint4(0, 0, 0, 0);
-                        if (live && u * 8 < a.dim) {
-                            w = __ldg(reinterpret_cast<const uint4*>(src + u * 16));
-                            if (flip) { w.x ^= 0x80008000u; w.y ^= 0x80008000u; w.z ^= 0x80008000u; w.w ^= 0x80008000u; }
-                            if constexpr (kQuant) {
-                                uint32_t* p = &w.x;
+            if (!narrow || s == 0) {
+                constexpr int LANES = DP / 8, ROWS = 32 / LANES, N = 32 / ROWS;  // lanes per row, rows at once, turns
+                const int u = lane % LANES;
+                unsigned char* tile = q_tiles + s * S::kTileBytes + (u >> 3) * kBlockBytes;
 #pragma unroll
-                                for (int i = 0; i < 4; ++i)
-                                    p[i] = pack2<__half>(Codec<T, 16>::to_float16(p[i] & 0xFFFFu) * factor, Codec<T, 16>::to_float16(p[i] >> 16) * factor);
-                            }
+                for (int h = 0; h < N; h += 8) {
+                    uint4 w[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int row = first_row + (warp & 3) * 32 + (h + i) * ROWS + lane / LANES;
+                        const bool there = row < split.rows && u * 8 < a.dim;
+                        const int token = there ? row / a.group : 0;
+                        const long long o = (long long)token * a.q_token_stride +
+                                            (long long)(kv_head * a.group + (there ? row - token * a.group : 0)) * a.q_head_stride + (there ? u * 8 : 0);
+                        w[i] = __ldg(reinterpret_cast<const uint4*>(a.q + o * 2));
+                        if (!there) w[i] = make_uint4(0, 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int mine = (warp & 3) * 32 + (h + i) * ROWS + lane / LANES;
+                        const uint32_t sign = flip ? 0x80008000u : 0u;
+                        w[i].x ^= sign; w[i].y ^= sign; w[i].z ^= sign; w[i].w ^= sign;
+                        if constexpr (kQuant) {
+                            uint32_t top = __vmaxu2(__vmaxu2(w[i].x & 0x7FFF7FFFu, w[i].y & 0x7FFF7FFFu), __vmaxu2(w[i].z & 0x7FFF7FFFu, w[i].w & 0x7FFF7FFFu));
+#pragma unroll
+                            for (int m = LANES / 2; m >= 1; m >>= 1) top = __vmaxu2(top, __shfl_xor_sync(0xFFFFFFFFu, top, m));
+                            const float factor = fp16_row_factor(Codec<T, 16>::to_float16(max(top & 0xFFFFu, top >> 16)));
+                            if (u == 0) row_factor[s][mine] = factor;
+                            uint32_t* p = &w[i].x;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                p[k] = pack2<__half>(Codec<T, 16>::to_float16(p[k] & 0xFFFFu) * factor, Codec<T, 16>::to_float16(p[k] >> 16) * factor);
                         }
-                        *reinterpret_cast<uint4*>(dst + (u >> 3) * kBlockBytes + (((u & 7) ^ (r & 7)) << 4)) = w;
+                        *reinterpret_cast<uint4*>(tile + mine * 128 + (((u & 7) ^ (mine & 7)) << 4)) = w[i];
                     }
                 }
             }
             fence_async_proxy();
             mbarrier_arrive(&q_full);
+            float row_c = scale;
+            if constexpr (kQuant) {
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                row_c *= __frcp_rn(row_factor[narrow ? 0 : s][r]);
+            }
 
             float m = -INFINITY, l = 0.f;
             const int my_tiles = narrow ? (n + 1 - s) / 2 : n;
@@ -244,97 +190,84 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                 ++n_s;
                 tc_fence_after();
                 const float4* ka = reinterpret_cast<const float4*>(aux + aux_i * S::kAuxFloats);
-                const bool holes = !kQuant && *reinterpret_cast<volatile uint32_t*>(&ragged[aux_i]) != 0;
-                // largest score of the tile
+                // the tile's scores of this row, as logarithms (quantised) or still to be scaled (plain), hidden ones -inf
+                uint32_t v[128];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) tmem_load32(s_col + q * 32, *reinterpret_cast<uint32_t(*)[32]>(&v[q * 32]));
+                tmem_wait_load();
                 float top = -INFINITY;
+                if constexpr (kQuant) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    uint32_t v[32];
-                    tmem_load32(s_col + q * 32, v);
-                    tmem_wait_load();
-                    if constexpr (kQuant) {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const float4 ks = ka[q * 8 + k], lv = ka[32 + q * 8 + k];
-                            top = fmaxf(fmaxf(top, fmaf(__uint_as_float(v[4 * k]) * row_c, ks.x, lv.x)), fmaf(__uint_as_float(v[4 * k + 1]) * row_c, ks.y, lv.y));
-                            top = fmaxf(fmaxf(top, fmaf(__uint_as_float(v[4 * k + 2]) * row_c, ks.z, lv.z)), fmaf(__uint_as_float(v[4 * k + 3]) * row_c, ks.w, lv.w));
-                        }
-                    } else if (holes) {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const float4 b = ka[q * 8 + k];
-                            top = fmaxf(fmaxf(top, b.x == 0.f ? __uint_as_float(v[4 * k]) : -INFINITY), b.y == 0.f ? __uint_as_float(v[4 * k + 1]) : -INFINITY);
-                            top = fmaxf(fmaxf(top, b.z == 0.f ? __uint_as_float(v[4 * k + 2]) : -INFINITY), b.w == 0.f ? __uint_as_float(v[4 * k + 3]) : -INFINITY);
-                        }
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 32; k += 2) top = fmaxf(fmaxf(top, __uint_as_float(v[k])), __uint_as_float(v[k + 1]));
+                    for (int k = 0; k < 32; ++k) {
+                        const float4 ks = ka[k], lv = ka[32 + k];
+                        const float x0 = fmaf(__uint_as_float(v[4 * k]) * row_c, ks.x, lv.x), x1 = fmaf(__uint_as_float(v[4 * k + 1]) * row_c, ks.y, lv.y);
+                        const float x2 = fmaf(__uint_as_float(v[4 * k + 2]) * row_c, ks.z, lv.z), x3 = fmaf(__uint_as_float(v[4 * k + 3]) * row_c, ks.w, lv.w);
+                        v[4 * k] = __float_as_uint(x0); v[4 * k + 1] = __float_as_uint(x1);
+                        v[4 * k + 2] = __float_as_uint(x2); v[4 * k + 3] = __float_as_uint(x3);
+                        top = fmaxf(fmaxf(top, x0), x1);
+                        top = fmaxf(fmaxf(top, x2), x3);
                     }
+                } else {
+                    if (*reinterpret_cast<volatile uint32_t*>(&ragged[aux_i]) != 0) {  // the last tile, or pages that are not there
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) {
+                            const float4 b = ka[k];
+                            if (b.x != 0.f) v[4 * k] = 0xFF800000u;
+                            if (b.y != 0.f) v[4 * k + 1] = 0xFF800000u;
+                            if (b.z != 0.f) v[4 * k + 2] = 0xFF800000u;
+                            if (b.w != 0.f) v[4 * k + 3] = 0xFF800000u;
+                        }
+                    }
+                    float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int k = 0; k < 128; k += 8)
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) t4[y] = fmaxf(fmaxf(t4[y], __uint_as_float(v[k + 2 * y])), __uint_as_float(v[k + 2 * y + 1]));
+                    top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
+                    top = top == -INFINITY ? top : top * row_c;
                 }
-                if (!kQuant) top = top == -INFINITY ? top : top * row_c;  // row_c may be zero
                 const bool move = top > m + 8.f;
                 if (__any_sync(0xFFFFFFFFu, move)) {
                     const float alpha = move ? ex2(m - top) : 1.f;
                     if (i > 0) {
 #pragma unroll 1
-                        for (int q = 0; q < DP / 32; ++q) {
-                            uint32_t v[32];
-                            tmem_load32(o_col + q * 32, v);
+                        for (int q = 0; q < DP / 16; ++q) {
+                            uint32_t o[16];
+                            tmem_load16(o_col + q * 16, o);
                             tmem_wait_load();
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * alpha);
-                            tmem_store32(o_col + q * 32, v);
+                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
+                            tmem_store16(o_col + q * 16, o);
                         }
                     }
                     l *= alpha;
                     if (move) m = top;
                 }
+                // No key of the row so far: m is -inf, every score is -inf, and so must every weight's logarithm be.  A score
+                // scale of zero would make NaN of a plain cache's hidden scores: the smallest normal number does instead.
                 const float base = m == -INFINITY ? 0.f : m;
-                float sum[2] = {0.f, 0.f};
+                const float c = kQuant ? 1.f : fmaxf(row_c, 1.17549435e-38f);
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                uint32_t w[64];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    uint32_t v[32], w[16];
-                    tmem_load32(s_col + q * 32, v);
-                    tmem_wait_load();
+                for (int k = 0; k < 64; k += 2) {
+                    const float x0 = ex2(kQuant ? __uint_as_float(v[2 * k]) - base : fmaf(__uint_as_float(v[2 * k]), c, -base));
+                    const float x1 = ex2(kQuant ? __uint_as_float(v[2 * k + 1]) - base : fmaf(__uint_as_float(v[2 * k + 1]), c, -base));
+                    const float x2 = ex2(kQuant ? __uint_as_float(v[2 * k + 2]) - base : fmaf(__uint_as_float(v[2 * k + 2]), c, -base));
+                    const float x3 = ex2(kQuant ? __uint_as_float(v[2 * k + 3]) - base : fmaf(__uint_as_float(v[2 * k + 3]), c, -base));
                     if constexpr (kQuant) {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const float4 ks = ka[q * 8 + k], lv = ka[32 + q * 8 + k], iv = ka[64 + q * 8 + k];
-                            const float x0 = ex2(fmaf(__uint_as_float(v[4 * k]) * row_c, ks.x, lv.x) - base);
-                            const float x1 = ex2(fmaf(__uint_as_float(v[4 * k + 1]) * row_c, ks.y, lv.y) - base);
-                            const float x2 = ex2(fmaf(__uint_as_float(v[4 * k + 2]) * row_c, ks.z, lv.z) - base);
-                            const float x3 = ex2(fmaf(__uint_as_float(v[4 * k + 3]) * row_c, ks.w, lv.w) - base);
-                            sum[0] = fmaf(x0, iv.x, sum[0]); sum[1] = fmaf(x1, iv.y, sum[1]);
-                            sum[0] = fmaf(x2, iv.z, sum[0]); sum[1] = fmaf(x3, iv.w, sum[1]);
-                            w[2 * k] = pack2<M>(x0, x1);
-                            w[2 * k + 1] = pack2<M>(x2, x3);
-                        }
+                        const float4 iv = ka[64 + k / 2];
+                        sum[0] = fmaf(x0, iv.x, sum[0]); sum[1] = fmaf(x1, iv.y, sum[1]);
+                        sum[2] = fmaf(x2, iv.z, sum[2]); sum[3] = fmaf(x3, iv.w, sum[3]);
                     } else {
-                        if (holes) {
-#pragma unroll
-                            for (int k = 0; k < 8; ++k) {
-                                const float4 b = ka[q * 8 + k];
-                                if (b.x != 0.f) v[4 * k] = 0xFF800000u;
-                                if (b.y != 0.f) v[4 * k + 1] = 0xFF800000u;
-                                if (b.z != 0.f) v[4 * k + 2] = 0xFF800000u;
-                                if (b.w != 0.f) v[4 * k + 3] = 0xFF800000u;
-                            }
-                        }
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) {
-                            float x0 = ex2(fmaf(__uint_as_float(v[2 * k]), row_c, -base)), x1 = ex2(fmaf(__uint_as_float(v[2 * k + 1]), row_c, -base));
-                            if (holes) {  // 0 * -inf when the score scale is zero
-                                if (v[2 * k] == 0xFF800000u) x0 = 0.f;
-                                if (v[2 * k + 1] == 0xFF800000u) x1 = 0.f;
-                            }
-                            sum[0] += x0;
-                            sum[1] += x1;
-                            w[k] = pack2<M>(x0, x1);
-                        }
+                        sum[0] += x0; sum[1] += x1; sum[2] += x2; sum[3] += x3;
                     }
-                    tmem_store16(s_col + q * 16, w);
+                    w[k] = pack2<M>(x0, x1);
+                    w[k + 1] = pack2<M>(x2, x3);
                 }
-                l += sum[0] + sum[1];
+#pragma unroll
+                for (int q = 0; q < 2; ++q) tmem_store32(s_col + q * 32, *reinterpret_cast<uint32_t(*)[32]>(&w[q * 32]));
+                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                 tmem_wait_store();
                 tc_fence_before();
                 mbarrier_arrive(&p_full[s]);
@@ -348,33 +281,45 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                 tc_fence_after();
             }
             const long long part = blockIdx.x - (long long)unit * split.tiles / split.run;
-            const int part_index = (int)(narrow ? 2 * part + s : part);
-            const long long n_rows = (long long)a.n_seqs * a.q_len * a.kv_heads * a.group;
-            const long long out_row = (long long)part_index * n_rows + (long long)token * a.kv_heads * a.group + head;
+            const long long part_at = (narrow ? 2 * part + s : part) * n_rows;
             const bool empty = l == 0.f;
+            const long long my_row = row_index(r);
+            if (my_row >= 0) a.part_lse[part_at + my_row] = empty ? -INFINITY : m + log2f(l);
             if (my_tiles > 0) {
+                // A thread holds a row, and rows lie apart: 32 columns at a time go through shared memory, so that eight lanes
+                // write 128 bytes of a row.  Rows without a key are written too; nothing reads them.
                 const float inv = empty ? 0.f : 1.0f / l;
+                unsigned char* stage = DP == 64 ? smem + S::kStageAt + warp * 4096 : q_tiles + S::kTileBytes * (narrow ? 1 : s) + (narrow ? warp : warp & 3) * 4096;
+                long long to_row[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) to_row[k] = row_index((warp & 3) * 32 + k * 4 + (lane >> 3));
 #pragma unroll 1
                 for (int q = 0; q < DP / 32; ++q) {
-                    uint32_t v[32];
-                    tmem_load32(o_col + q * 32, v);
+                    uint32_t o[32];
+                    tmem_load32(o_col + q * 32, o);
                     tmem_wait_load();
-                    if (live && !empty) {
 #pragma unroll
-                        for (int k = 0; k < 32; k += 4)
-                            if (q * 32 + k < a.dim)
-                                *reinterpret_cast<float4*>(a.part_out + out_row * a.dim + q * 32 + k) =
-                                    make_float4(__uint_as_float(v[k]) * inv, __uint_as_float(v[k + 1]) * inv, __uint_as_float(v[k + 2]) * inv,
-                                                __uint_as_float(v[k + 3]) * inv);
+                    for (int k = 0; k < 8; ++k)
+                        *reinterpret_cast<float4*>(stage + lane * 128 + ((k ^ (lane & 7)) << 4)) =
+                            make_float4(__uint_as_float(o[4 * k]) * inv, __uint_as_float(o[4 * k + 1]) * inv, __uint_as_float(o[4 * k + 2]) * inv,
+                                        __uint_as_float(o[4 * k + 3]) * inv);
+                    __syncwarp();
+                    const int col = q * 32 + (lane & 7) * 4;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int row = k * 4 + (lane >> 3);
+                        const float4 x = *reinterpret_cast<const float4*>(stage + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
+                        if (to_row[k] >= 0 && col < a.dim) *reinterpret_cast<float4*>(a.part_out + (part_at + to_row[k]) * a.dim + col) = x;
                     }
+                    __syncwarp();
                 }
             }
-            if (live) a.part_lse[out_row] = empty ? -INFINITY : m + log2f(l);
             tc_fence_before();
             at += n;
         }
     } else if (warp < 12) {
         // ---- fetching warps ----
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
         const int p = tid - 256;
         uint32_t item = 0, tile_no = 0;
         uint32_t pending = 0;          // items issued but not yet announced (plain: cp.async groups)
@@ -414,18 +359,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                 }
                 announce(item);
             } else {
-                constexpr int UNITS = DP / 8;             // 16 bytes a piece
-                constexpr int STEP = 128 / UNITS;
-                const int u = p % UNITS, row0 = p / UNITS;
-#pragma unroll 8
-                for (int r = row0; r < kTcTile; r += STEP) {
-                    const long long o = off[r];
-                    const bool there = o >= 0 && u * 8 < a.dim;
-                    const unsigned char* src = there ? side + (o + u * 8) * 2 : side;
-                    const uint32_t to = smem_u32(dst + (u >> 3) * kBlockBytes + r * 128 + (((u & 7) ^ (r & 7)) << 4));
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(src), "r"(there ? 16 : 0) : "memory");
-                }
-                asm volatile("cp.async.commit_group;" ::: "memory");
+                fetch_plain_tile<DP>(dst, side, off, p, (p % (DP / 8)) * 8 < a.dim, 0);
                 if (++pending == 2) {  // the one before has landed when only this one is outstanding
                     asm volatile("cp.async.wait_group 1;" ::: "memory");
                     announce(item - 1);
@@ -456,7 +390,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                         atomicExch(a.status, kDeviceIndexCode);
                     }
                 }
-                offsets[(t % kTcAux) * kTcTile + p] = o;
+                offsets[(t % kTcAux) * kTcTile + p] = kQuant ? o : o * 2;
                 float* to = aux + (t % kTcAux) * S::kAuxFloats + p;
                 if constexpr (kQuant) {
                     const float ks = o >= 0 ? __ldg(a.k_scale + so) : 0.f, vs = o >= 0 ? usable_scale(__ldg(a.v_scale + so)) : 0.f;
@@ -485,28 +419,41 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
             if (pending) announce(item - 1);
         }
     } else {
-        // ---- the thread that issues the products ----
-        if (lane == 0) {
+        // ---- the warp that issues the products (three more only hold its warpgroup's registers) ----
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        if (warp == 12) {
+            constexpr uint64_t kRowsLayout = tc_layout(16, 1024), kColsLayout = tc_layout(kBlockBytes, 1024);
+            constexpr uint32_t kTile16 = S::kTileBytes / 16;
             uint32_t item = 0, n_q = 0, n_p[2] = {0, 0};
-            const uint32_t q_addr = smem_u32(q_tiles), ring_addr = smem_u32(ring);
+            const uint32_t q16 = smem_u32(q_tiles) >> 4, ring16 = smem_u32(ring) >> 4;
             auto wait_item = [&](uint32_t i) {
                 wait(&full[i % kTcSlots], (i / kTcSlots) & 1);
                 tc_fence_after();
             };
-            auto scores = [&](int s, int q_tile, uint32_t i) {
-                const uint32_t k_addr = ring_addr + (i % kTcSlots) * S::kTileBytes, q = q_addr + q_tile * S::kTileBytes;
-    #pragma unroll
-                for (int k = 0; k < DP / 16; ++k) {
-                    const uint32_t step = (k >> 2) * kBlockBytes + (k & 3) * 32;
-                    tc_mma_ss(tmem + s * kTcTile, tc_descriptor(q + step, 16, 1024), tc_descriptor(k_addr + step, 16, 1024), kScoreIdesc, k > 0);
+            // S_s = Q K^T with the keys of item i, then what the commits say
+            auto scores = [&](int s, int q_tile, uint32_t i, bool release) {
+                const uint32_t k_at = ring16 + (i % kTcSlots) * kTile16, q_at = q16 + q_tile * kTile16, d = tmem + s * kTcTile;
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < DP / 16; ++k) {
+                        const uint32_t step = ((k >> 2) * kBlockBytes + (k & 3) * 32) / 16;
+                        tc_mma_ss(d, tc_descriptor(kRowsLayout, q_at + step), tc_descriptor(kRowsLayout, k_at + step), kScoreIdesc, k > 0);
+                    }
+                    tc_commit(&s_full[s]);
+                    if (release) tc_commit(&empty[i % kTcSlots]);
                 }
+                __syncwarp();
             };
-            auto output = [&](int s, uint32_t i, bool first) {
-                const uint32_t v_addr = ring_addr + (i % kTcSlots) * S::kTileBytes;
-    #pragma unroll
-                for (int k = 0; k < kTcTile / 16; ++k)
-                    tc_mma_ts(tmem + kColO + s * DP, tmem + s * kTcTile + k * 8, tc_descriptor(v_addr + k * 2048, kBlockBytes, 1024), kOutIdesc,
-                              !first || k > 0);
+            auto output = [&](int s, uint32_t i, bool first, bool release, bool last) {
+                const uint32_t v_at = ring16 + (i % kTcSlots) * kTile16, d = tmem + kColO + s * DP, w = tmem + s * kTcTile;
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < kTcTile / 16; ++k)
+                        tc_mma_ts(d, w + k * 8, tc_descriptor(kColsLayout, v_at + k * 128), kOutIdesc, k > 0 ? 1u : (uint32_t)!first);
+                    if (release) tc_commit(&empty[i % kTcSlots]);
+                    if (last) tc_commit(&o_full[s]);
+                }
+                __syncwarp();
             };
             auto wait_weights = [&](int s) {
                 wait(&p_full[s], n_p[s] & 1);
@@ -523,63 +470,44 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                 if (narrow_block(split, block)) {
                     for (int j = 0; j < 2 && j < n; ++j) {
                         wait_item(item);
-                        scores(j, 0, item);
-                        tc_commit(&s_full[j]);
-                        tc_commit(&empty[item % kTcSlots]);
-                        ++item;
+                        scores(j, 0, item++, true);
                     }
                     for (int j = 0; j < n; ++j) {
                         const int s = j & 1;
                         wait_item(item);
                         wait_weights(s);
-                        output(s, item, j < 2);
-                        tc_commit(&empty[item % kTcSlots]);
-                        ++item;
+                        output(s, item++, j < 2, true, j + 2 >= n);
                         if (j + 2 < n) {
                             wait_item(item);
-                            scores(s, 0, item);
-                            tc_commit(&s_full[s]);
-                            tc_commit(&empty[item % kTcSlots]);
-                            ++item;
-                        } else {
-                            tc_commit(&o_full[s]);
+                            scores(s, 0, item++, true);
                         }
                     }
                 } else {
                     wait_item(item);
-                    for (int s = 0; s < 2; ++s) {
-                        scores(s, s, item);
-                        tc_commit(&s_full[s]);
-                    }
-                    tc_commit(&empty[item % kTcSlots]);
-                    ++item;
+                    scores(0, 0, item, false);
+                    scores(1, 1, item++, true);
                     for (int j = 0; j < n; ++j) {
-                        const uint32_t v_item = item, k_item = item + 1;
                         const bool more = j + 1 < n;
-                        wait_item(v_item);
-                        for (int s = 0; s < 2; ++s) {
-                            wait_weights(s);
-                            output(s, v_item, j == 0);
-                            if (s == 1) tc_commit(&empty[v_item % kTcSlots]);
-                            if (more) {
-                                if (s == 0) wait_item(k_item);
-                                scores(s, s, k_item);
-                                tc_commit(&s_full[s]);
-                                if (s == 1) tc_commit(&empty[k_item % kTcSlots]);
-                            } else {
-                                tc_commit(&o_full[s]);
-                            }
+                        wait_item(item);
+                        wait_weights(0);
+                        output(0, item, j == 0, false, !more);
+                        if (more) {
+                            wait_item(item + 1);
+                            scores(0, 0, item + 1, false);
                         }
+                        wait_weights(1);
+                        output(1, item, j == 0, true, !more);
+                        if (more) scores(1, 1, item + 1, true);
                         item += more ? 2 : 1;
                     }
                 }
                 at += n;
             }
             // the tensor memory is given back only when nothing writes it any more
-            tc_commit(&drained);
+            if (elect_one()) tc_commit(&drained);
+            __syncwarp();
             ok = mbarrier_wait_bounded(&drained, 0) && ok;
         }
-        __syncwarp();
     }
     if (!ok) atomicExch(a.status, kDeviceTimeoutCode);
     tc_fence_before();

@@ -36,7 +36,7 @@ struct RowsShape {
     static constexpr bool kQuant = FMT != kKvPlain;
     static constexpr int PD = DP < 128 ? DP : 128;               // dims of one register buffer
     static constexpr int NP = DP / PD;                           // buffers per key block and side
-    static constexpr int KB = DP == 256 ? 16 : (kQuant || DP == 64 ? 32 : 16);  // keys per block
+    static constexpr int KB = DP == 64 ? 32 : 16;  // keys per block
     static constexpr int K_CHUNK = kQuant ? 16 : 8;              // dims in a lane's 16 bytes of a key
     static constexpr int K_CHUNKS = PD / (4 * K_CHUNK);
     static constexpr int V_CHUNK = kQuant ? (PD == 64 ? 8 : 16) : 8;  // dims in a lane's chunk of a value row
@@ -50,19 +50,25 @@ struct RowsShape {
     static constexpr size_t kSmem = (size_t)DP * 32 + 2 * 16 * O_STRIDE * 4;
 };
 
-__device__ __forceinline__ void ld_words4(const unsigned char* p, uint32_t* w)
+// 16 or 8 bytes, or zeros.  The zeros are set ahead of a predicated load, inside one statement: written as a branch, the
+// registers of both sides meet in a move that waits for the load.
+__device__ __forceinline__ void ld_words4(const unsigned char* p, bool there, uint32_t* w)
 {
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t"
+                 "@p ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];\n\t}"
+                 : "=&r"(w[0]), "=&r"(w[1]), "=&r"(w[2]), "=&r"(w[3]) : "l"(p), "r"((uint32_t)there));
 }
-__device__ __forceinline__ void ld_words2(const unsigned char* p, uint32_t* w)
+__device__ __forceinline__ void ld_words2(const unsigned char* p, bool there, uint32_t* w)
 {
-    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %3, 0;\n\tmov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\t"
+                 "@p ld.global.L1::no_allocate.v2.u32 {%0,%1}, [%2];\n\t}"
+                 : "=&r"(w[0]), "=&r"(w[1]) : "l"(p), "r"((uint32_t)there));
 }
 
 // PREFIX: the rows of one key/value head (16 of them) against a part of the prefix; else the rows of one sequence and
 // key/value head against a part of its suffix.
 template <typename T, int FMT, int DP, bool PREFIX>
-__global__ void __launch_bounds__(kRowsThreads) attend_rows_kernel(const AttendArgs a)
+__global__ void __launch_bounds__(kRowsThreads, DP == 256 ? 2 : 3) attend_rows_kernel(const AttendArgs a)
 {
     using S = RowsShape<FMT, DP>;
     constexpr bool kQuant = S::kQuant;
@@ -227,8 +233,7 @@ __global__ void __launch_bounds__(kRowsThreads) attend_rows_kernel(const AttendA
             for (int i = 0; i < S::K_CHUNKS; ++i) {
                 const int d = piece * S::PD + i * 4 * S::K_CHUNK + c * S::K_CHUNK;
                 uint32_t* to = &w[(nt * S::K_CHUNKS + i) * 4];
-                if (o >= 0 && d < a.dim) ld_words4(a.k + (o + d) * ES, to);
-                else to[0] = to[1] = to[2] = to[3] = 0;
+                ld_words4(a.k + (o + d) * ES, o >= 0 && d < a.dim, to);
             }
         }
     };
@@ -242,13 +247,8 @@ __global__ void __launch_bounds__(kRowsThreads) attend_rows_kernel(const AttendA
                 for (int i = 0; i < S::V_CHUNKS; ++i) {
                     const int d = piece * S::PD + i * 8 * S::V_CHUNK + g * S::V_CHUNK;
                     uint32_t* to = &w[((u * 4 + y) * S::V_CHUNKS + i) * S::V_WORDS];
-                    if (o >= 0 && d < a.dim) {
-                        if constexpr (S::V_WORDS == 4) ld_words4(a.v + (o + d) * ES, to);
-                        else ld_words2(a.v + (o + d) * ES, to);
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < S::V_WORDS; ++k) to[k] = 0;
-                    }
+                    if constexpr (S::V_WORDS == 4) ld_words4(a.v + (o + d) * ES, o >= 0 && d < a.dim, to);
+                    else ld_words2(a.v + (o + d) * ES, o >= 0 && d < a.dim, to);
                 }
             }
     };

@@ -1,12 +1,14 @@
 // Entry point of the attention over a shared prefix: argument checks, the split of the work into parts, the launches.
 #include <string.h>
+#include <stdlib.h>
 
 #include <atomic>
 
 #include "attend_common.cuh"
 #include "attend_host.h"
+#include "attend_keys_kernel.cuh"
+#include "attend_merge_kernel.cuh"
 #include "attend_prefix_kernel.cuh"
-#include "attend_rows_kernel.cuh"
 #include "attend_split.h"
 #include "tuner_internal.h"
 
@@ -18,33 +20,18 @@ int log2_or_minus1(unsigned v);
 namespace {
 
 constexpr int kMaxLen = 1 << 30;
-constexpr int kRowsKernelMost = 32;  // rows per key/value head up to which the prefix goes to the 16-row kernel
-constexpr int kMaxParts = 64;  // of the prefix, and of the suffix
+constexpr int kMaxParts = 64;  // of a suffix, and of a prefix that is not dealt out by tiles
 
 struct AttendPlan {
     int padded_dim;
     int group;
     long long tokens;
+    int prefix_form, suffix_form;  // kPrefixTiles ..., -1: no keys
     int prefix_parts, prefix_keys, suffix_parts, suffix_keys;
-    PrefixSplit split;  // run > 0: the prefix goes to the tensor-core kernel
+    PrefixSplit split;  // run > 0: the prefix is dealt out by tiles
     long long prefix_ctas, suffix_ctas;
     int64_t workspace;
 };
-
-// The kernel's dynamic shared memory is beyond the default limit: raised once per device and kernel.
-int allow_smem(const AttendKernels& k, int dtype, int format, int padded_dim)
-{
-    static std::atomic<unsigned char> done[kDeviceSlots][2][3][2];
-    int device;
-    int st = current_device_index(&device);
-    if (st != RT_OK) return st;
-    std::atomic<unsigned char>& flag = done[device][dtype][format][padded_dim > 64];
-    if (!flag.load(std::memory_order_acquire)) {
-        RT_CUDA_OK(cudaFuncSetAttribute(k.prefix_tc, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)k.tc_smem));
-        flag.store(1, std::memory_order_release);
-    }
-    return RT_OK;
-}
 
 AttendKernels kernels_of(int dtype, int format, int padded_dim)
 {
@@ -52,6 +39,25 @@ AttendKernels kernels_of(int dtype, int format, int padded_dim)
     static const Get get[2][3] = {{rt_attend_kernels_bf16_plain, rt_attend_kernels_bf16_e4m3, rt_attend_kernels_bf16_int8},
                                   {rt_attend_kernels_fp16_plain, rt_attend_kernels_fp16_e4m3, rt_attend_kernels_fp16_int8}};
     return get[dtype][format](padded_dim);
+}
+
+// Shared memory beyond the default limit is asked for once per device and kernel.
+int launch_form(const AttendKernels& kernels, int form, int dtype, int format, int padded_dim, long long ctas, int threads,
+                cudaStream_t stream, void** params)
+{
+    static std::atomic<unsigned char> done[kDeviceSlots][2][3][3][kAttendKernels];
+    const AttendKernel& k = kernels.k[form];
+    if (k.smem > 48 * 1024) {
+        int device;
+        const int st = current_device_index(&device);
+        if (st != RT_OK) return st;
+        std::atomic<unsigned char>& flag = done[device][dtype][format][padded_dim / 128][form];
+        if (!flag.load(std::memory_order_acquire)) {
+            RT_CUDA_OK(cudaFuncSetAttribute(k.fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)k.smem));
+            flag.store(1, std::memory_order_release);
+        }
+    }
+    return launch_kernel(k.fn, dim3((unsigned)ctas), dim3(threads), k.smem, stream, params);
 }
 
 long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
@@ -114,26 +120,35 @@ int make_attend_plan(const rt_kv_cache* c, const rt_prefix_batch* b, int q_heads
     p->group = q_heads / c->kv_heads;
     p->tokens = b->n_seqs * b->q_len;
     if (p->tokens == 0) return RT_OK;
-    const long long want = (long long)L.sm_count * 4;
-    const long long rows_per_kv_head = p->tokens * p->group;
-    if (b->prefix_len > 0 && p->padded_dim <= 128 && rows_per_kv_head > kRowsKernelMost) {
-        PrefixSplit& s = p->split;
-        s.tiles = (int)ceil_div(b->prefix_len, kTcTile);
-        s.rows = (int)rows_per_kv_head;
-        s.blocks = (int)ceil_div(rows_per_kv_head, kTcBlockRows);
-        const long long total = (long long)s.tiles * s.blocks * c->kv_heads;
-        const long long run = ceil_div(total, L.sm_count);
-        s.run = (int)std::min<long long>(run, 1 << 30);
-        p->prefix_ctas = ceil_div(total, s.run);
-        p->prefix_parts = most_parts(s);
-    } else if (b->prefix_len > 0) {
-        const long long tiles = ceil_div(p->tokens * p->group, 16) * c->kv_heads;
-        split_keys(b->prefix_len, tiles, want, 128, &p->prefix_parts, &p->prefix_keys);
-        p->prefix_ctas = tiles * p->prefix_parts;
+    p->prefix_form = p->suffix_form = -1;
+    const long long prefix_rows = p->tokens * p->group, suffix_rows = (long long)b->q_len * p->group;
+    if (b->prefix_len > 0) {
+        if (prefix_rows <= 16) p->prefix_form = kPrefixKeys16;
+        else if (p->padded_dim == 256 || prefix_rows <= 64) p->prefix_form = kPrefixKeys64;
+        else p->prefix_form = kPrefixTiles;
+        if (getenv("XPRE")) p->prefix_form = atoi(getenv("XPRE"));
+        if (p->prefix_form == kPrefixTiles) {
+            PrefixSplit& s = p->split;
+            s.tiles = (int)ceil_div(b->prefix_len, kTcTile);
+            s.rows = (int)prefix_rows;
+            s.blocks = (int)ceil_div(prefix_rows, kTcBlockRows);
+            const long long total = (long long)s.tiles * s.blocks * c->kv_heads;
+            s.run = (int)std::min<long long>(ceil_div(total, L.sm_count), 1 << 30);
+            p->prefix_ctas = ceil_div(total, s.run);
+            p->prefix_parts = most_parts(s);
+        } else {
+            const int nr = p->prefix_form == kPrefixKeys16 ? 16 : 64;
+            const long long tiles = ceil_div(prefix_rows, nr) * c->kv_heads;
+            split_keys(b->prefix_len, tiles, (long long)L.sm_count * (nr == 16 ? 2 : 1), 128, &p->prefix_parts, &p->prefix_keys);
+            p->prefix_ctas = tiles * p->prefix_parts;
+        }
     }
     if (b->max_suffix_len > 0) {
-        const long long tiles = ceil_div((long long)b->q_len * p->group, 16) * c->kv_heads * b->n_seqs;
-        split_keys(b->max_suffix_len, tiles, want, 128, &p->suffix_parts, &p->suffix_keys);
+        p->suffix_form = suffix_rows <= 32 ? kSuffixKeys16 : kSuffixKeys64;
+        const int nr = p->suffix_form == kSuffixKeys16 ? 16 : 64;
+        const long long tiles = ceil_div(suffix_rows, nr) * c->kv_heads * b->n_seqs;
+        split_keys(b->max_suffix_len, tiles, (long long)L.sm_count * (nr == 16 ? 2 : 1), 128, &p->suffix_parts, &p->suffix_keys);
+        if (getenv("XKEYS")) { p->suffix_keys = atoi(getenv("XKEYS")); p->suffix_parts = (int)ceil_div(b->max_suffix_len, p->suffix_keys); }
         p->suffix_ctas = tiles * p->suffix_parts;
     }
     if (p->prefix_ctas > 0x7fffffffLL || p->suffix_ctas > 0x7fffffffLL) {
@@ -243,22 +258,18 @@ int shared_prefix_attention_launch(const rt_kv_cache* c, const rt_prefix_batch* 
     const AttendKernels k = kernels_of(dtype, c->format, p.padded_dim);
     void* params[] = {&a, &p.split};
     const cudaStream_t s = (cudaStream_t)stream;
-    if (p.split.run > 0) {
-        st = allow_smem(k, dtype, c->format, p.padded_dim);
-        if (st == RT_OK) st = launch_kernel(k.prefix_tc, dim3((unsigned)p.prefix_ctas), dim3(kTcThreads), k.tc_smem, s, params);
-        if (st != RT_OK) return st;
-    } else if (p.prefix_ctas > 0) {
-        st = launch_kernel(k.prefix_rows, dim3((unsigned)p.prefix_ctas), dim3(kRowsThreads), k.rows_smem, s, params);
-        if (st != RT_OK) return st;
-    }
-    if (p.suffix_ctas > 0) {
-        st = launch_kernel(k.suffix_rows, dim3((unsigned)p.suffix_ctas), dim3(kRowsThreads), k.rows_smem, s, params);
+    const auto launch = [&](int form, long long ctas, int threads) {
+        return launch_form(k, form, dtype, c->format, p.padded_dim, ctas, threads, s, params);
+    };
+    if (p.prefix_form >= 0) {
+        st = launch(p.prefix_form, p.prefix_ctas, p.prefix_form == kPrefixTiles ? kTcThreads : kKeysThreads);
         if (st != RT_OK) return st;
     }
-    if (parts != 1) {
-        const int64_t ctas = ceil_div(p.tokens * q_heads, kMergePartsThreads / 32);
-        st = launch_kernel(k.merge, dim3((unsigned)ctas), dim3(kMergePartsThreads), 0, s, params);
+    if (p.suffix_form >= 0) {
+        st = launch(p.suffix_form, p.suffix_ctas, kKeysThreads);
+        if (st != RT_OK) return st;
     }
+    if (parts != 1) st = launch(kMergeParts, ceil_div(p.tokens * q_heads, kMergePartsThreads / 32), kMergePartsThreads);
     return st;
 }
 
