@@ -122,12 +122,43 @@ __device__ __forceinline__ uint32_t pick_half2(uint32_t a, uint32_t b)
     }
 }
 
-// 16 codes of a tile that is read once.
-__device__ __forceinline__ uint4 ld_codes(const unsigned char* p)
+// 16 codes of a tile that is read once, or zeros.  The zeros are set ahead of a predicated load, inside one statement: written
+// as a branch, the registers of both sides meet in a move that waits for the load.
+__device__ __forceinline__ uint4 ld_codes(const unsigned char* p, bool there)
 {
     uint4 w;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "l"(p));
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t"
+                 "@p ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];\n\t}"
+                 : "=&r"(w.x), "=&r"(w.y), "=&r"(w.z), "=&r"(w.w) : "l"(p), "r"((uint32_t)there));
     return w;
+}
+
+// Two binary32 numbers in one register pair: the packed operations of sm_100 do both at once.
+typedef unsigned long long float2x;
+__device__ __forceinline__ float2x pack_f2(float lo, float hi)
+{
+    float2x r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpack_f2(float2x x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
+__device__ __forceinline__ float2x fma_f2(float2x a, float2x b, float2x c)
+{
+    float2x r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ float2x mul_f2(float2x a, float2x b)
+{
+    float2x r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float2x add_f2(float2x a, float2x b)
+{
+    float2x r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
 }
 
 // The power of two that brings a row's largest magnitude into [2^14, 2^15), so that a bf16 row fits fp16 without loss

@@ -309,36 +309,45 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
             const int hidden = PREFIX ? 0 : max(0, k0 + j * 128 + tid - (len - a.q_len)) * a.group - row0;
             wait(&s_full[j & 1], (j >> 1) & 1);
             tc_fence_after();
-            uint32_t v[NR];
-            if constexpr (NR == 16) tmem_load16(tmem + lanes + (j & 1) * NR, v);
-            else {
+            // 16 rows' scores of this thread's key, as logarithms; more rows than that are read again where they are needed
+            float t[16];
+            auto scores = [&](int r0) {
+                uint32_t v[16];
+                tmem_load16(tmem + lanes + (j & 1) * NR + r0, v);
+                tmem_wait_load(v);
 #pragma unroll
-                for (int q = 0; q < NR / 32; ++q) tmem_load32(tmem + lanes + (j & 1) * NR + q * 32, *reinterpret_cast<uint32_t(*)[32]>(&v[q * 32]));
-            }
-            tmem_wait_load();
+                for (int k = 0; k < 16; k += 4) {
+                    float4 c4;
+                    if constexpr (kQuant) c4 = *reinterpret_cast<const float4*>(&row_c[r0 + k]);
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        float x;
+                        if constexpr (kQuant) x = fmaf(__uint_as_float(v[k + y]) * ks, (&c4.x)[y], lvs);
+                        else x = __uint_as_float(v[k + y]) * a.score_scale;
+                        t[k + y] = !there || r0 + k + y < hidden ? -INFINITY : x;
+                    }
+                }
+            };
             float over = -INFINITY;
 #pragma unroll
-            for (int r0 = 0; r0 < NR; r0 += 4) {
-                const float4 m4 = *reinterpret_cast<const float4*>(&row_ref[r0]);
-                float4 c4;
-                if constexpr (kQuant) c4 = *reinterpret_cast<const float4*>(&row_c[r0]);
+            for (int r0 = 0; r0 < NR; r0 += 16) {
+                scores(r0);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int r = r0 + k;
-                    float t;
-                    if constexpr (kQuant) t = fmaf(__uint_as_float(v[r]) * ks, (&c4.x)[k], lvs);
-                    else t = __uint_as_float(v[r]) * a.score_scale;
-                    if (!there || r < hidden) t = -INFINITY;
-                    v[r] = __float_as_uint(t);
-                    over = fmaxf(over, t - (&m4.x)[k]);
+                for (int k = 0; k < 16; k += 4) {
+                    const float4 m4 = *reinterpret_cast<const float4*>(&row_ref[r0 + k]);
+                    over = fmaxf(over, fmaxf(fmaxf(t[k] - m4.x, t[k + 1] - m4.y), fmaxf(t[k + 2] - m4.z, t[k + 3] - m4.w)));
                 }
             }
             if (vote_any_128(over > 8.f)) {
                 // the tile's largest score of every row, over the warp and then over the four
+#pragma unroll 1
+                for (int r0 = 0; r0 < NR; r0 += 16) {
+                    if (NR > 16) scores(r0);
 #pragma unroll
-                for (int r = 0; r < NR; ++r) {
-                    const float top = warp_max(__uint_as_float(v[r]));
-                    if (lane == r % 32) row_m[warp][r] = top;
+                    for (int r = 0; r < 16; ++r) {
+                        const float top = warp_max(t[r]);
+                        if (lane == r) row_m[warp][r0 + r] = top;
+                    }
                 }
                 sync_128();
                 if (j > 0) {  // the products so far are complete before they are rescaled
@@ -360,7 +369,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
                         for (int i = 0; i < NI; ++i) {
                             uint32_t o[16];
                             tmem_load16(tmem_o + lanes + i * NR + r0, o);
-                            tmem_wait_load();
+                            tmem_wait_load(o);
 #pragma unroll
                             for (int r = 0; r < 16; ++r) o[r] = __float_as_uint(__uint_as_float(o[r]) * alpha[r]);
                             tmem_store16(tmem_o + lanes + i * NR + r0, o);
@@ -378,24 +387,28 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
             if (j >= 2) wait(&o_done[j & 1], ((j - 2) >> 1) & 1);  // this weight buffer's last product is complete
             unsigned char* to = weights + (j & 1) * S::kWBytes + tid * RB;
 #pragma unroll
-            for (int u = 0; u < NR / 8; ++u) {
-                uint32_t p[4];
-                const float4 m4[2] = {*reinterpret_cast<const float4*>(&row_ref[u * 8]), *reinterpret_cast<const float4*>(&row_ref[u * 8 + 4])};
-                const float* m = &m4[0].x;
+            for (int r0 = 0; r0 < NR; r0 += 16) {
+                if (NR > 16) scores(r0);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int r = u * 8 + 2 * k;
-                    const float x0 = ex2(__uint_as_float(v[r]) - m[2 * k]), x1 = ex2(__uint_as_float(v[r + 1]) - m[2 * k + 1]);
-                    if constexpr (kQuant) {  // a hidden key's scale may be NaN
-                        if (there && r >= hidden) l[r] = fmaf(x0, ivs, l[r]);
-                        if (there && r + 1 >= hidden) l[r + 1] = fmaf(x1, ivs, l[r + 1]);
-                    } else {
-                        l[r] += x0;
-                        l[r + 1] += x1;
+                for (int u = 0; u < 2; ++u) {
+                    uint32_t p[4];
+                    const float4 m4[2] = {*reinterpret_cast<const float4*>(&row_ref[r0 + u * 8]), *reinterpret_cast<const float4*>(&row_ref[r0 + u * 8 + 4])};
+                    const float* m = &m4[0].x;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int r = u * 8 + 2 * k;
+                        const float x0 = ex2(t[r] - m[2 * k]), x1 = ex2(t[r + 1] - m[2 * k + 1]);
+                        if constexpr (kQuant) {  // a hidden key's scale may be NaN
+                            if (there && r0 + r >= hidden) l[r0 + r] = fmaf(x0, ivs, l[r0 + r]);
+                            if (there && r0 + r + 1 >= hidden) l[r0 + r + 1] = fmaf(x1, ivs, l[r0 + r + 1]);
+                        } else {
+                            l[r0 + r] += x0;
+                            l[r0 + r + 1] += x1;
+                        }
+                        p[k] = pack2<M>(x0, x1);
                     }
-                    p[k] = pack2<M>(x0, x1);
+                    *reinterpret_cast<uint4*>(to + (((r0 / 8 + u) ^ (((tid * RB) >> 7) & (RB / 16 - 1))) << 4)) = make_uint4(p[0], p[1], p[2], p[3]);
                 }
-                *reinterpret_cast<uint4*>(to + ((u ^ (((tid * RB) >> 7) & (RB / 16 - 1))) << 4)) = make_uint4(p[0], p[1], p[2], p[3]);
             }
             fence_async_proxy();
             tc_fence_before();
@@ -434,7 +447,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
             for (int i = 0; i < NI; ++i) {
                 uint32_t o[16];
                 tmem_load16(tmem_o + lanes + i * NR + r0, o);
-                tmem_wait_load();
+                tmem_wait_load(o);
                 const int d = i * 128 + tid;
                 const bool mine = d < a.dim && (DI == 128 || tid < DI);
 #pragma unroll
@@ -465,67 +478,102 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
     } else if (warp < 8) {
         // ---- fetching warps ----
         const int p = tid - 128;
-        uint32_t item = 0;
-        bool pending = false;  // an item whose copies are under way has not been announced yet
-        auto announce = [&](uint32_t i) {
-            fence_async_proxy();
-            mbarrier_arrive(&full[i % SLOTS]);
+        // Items in the order in which the products want them, NI of each: K0, K1, V0, K2, V1, ... K(n-1), V(n-2), V(n-1).
+        const int items = 2 * n * NI;
+        struct Item {
+            int tile, part_of_dims;
+            bool values;
         };
-        auto fetch = [&](const unsigned char* side, int j, int part_of_dims, bool values) {
-            wait(&empty[item % SLOTS], ((item / SLOTS) & 1) ^ 1);
-            unsigned char* dst = ring + (item % SLOTS) * S::kItemBytes;
-            const long long* off = offsets + (j % 3) * 128;
-            const int dim0 = part_of_dims * DI;
-            // Some rows do not see the last keys, and 0 * infinity would reach them through the product: such values become
-            // zero in the tile and are added to the rows that do see them at the end.
-            const bool guard = values && !PREFIX && a.q_len > 1 && k0 + j * 128 + 128 > all_see;
-            bool hit_any = false;
-            if constexpr (kQuant) {
-                constexpr int UNITS = DI / 16, STEP = 128 / UNITS, N = 128 / STEP;
-                const int u = p % UNITS, r0 = p / UNITS;
-                uint4 w[N];
+        auto item_at = [&](int q) -> Item {
+            const int g = q / NI, half = (g + 1) >> 1;
+            const bool values = g > 0 && (!(g & 1) || half == n);
+            return {g == 0 ? 0 : (g & 1) ? (values ? n - 1 : half) : half - 1, q % NI, values};
+        };
+        // Places of a tile's keys, one thread to a key, published when the tile's first keys are fetched; its page number was
+        // read two tiles earlier.  Tile j + 2 is published when every thread is past the values of tile j - 1.
+        long long off_n = place_of_key(0, p, page_of(0, p), false);
+        int page_n = page_of(1, p);
+        auto begin_item = [&](const Item& it) -> const long long* {
+            const int j = it.tile;
+            if (!it.values && it.part_of_dims == 0) {
+                offsets[(j % 3) * 128 + p] = off_n < 0 ? -1 : off_n * ES;
+                if (j + 1 < n) off_n = place_of_key(j + 1, p, page_n, false);
+                if (j + 2 < n) page_n = page_of(j + 2, p);
+                asm volatile("barrier.cta.sync 2, 128;" ::: "memory");
+            }
+            return offsets + (j % 3) * 128;
+        };
+        auto slot_of = [&](int q) -> unsigned char* {
+            wait(&empty[q % SLOTS], ((q / SLOTS) & 1) ^ 1);
+            return ring + (q % SLOTS) * S::kItemBytes;
+        };
+        auto announce = [&](int q) {
+            fence_async_proxy();
+            mbarrier_arrive(&full[q % SLOTS]);
+        };
+        // Some rows do not see the last keys, and 0 * infinity would reach them through the product: such values become zero in
+        // the tile and are added to the rows that do see them at the end.
+        auto guarded = [&](const Item& it) { return it.values && !PREFIX && a.q_len > 1 && k0 + it.tile * 128 + 128 > all_see; };
+        if constexpr (kQuant) {
+            using C = CodePieces<DI>;
+            const int u = p % C::UNITS, r0 = p / C::UNITS;
+            const int to = (u >> 2) * kTileBlockBytes + r0 * 128, lo = (((u & 3) * 2) ^ (r0 & 7)) << 4, hi = (((u & 3) * 2 + 1) ^ (r0 & 7)) << 4;
+            uint4 w[C::N];
+            Item it = item_at(0);
+            {
+                const long long* off = begin_item(it) + r0;
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const long long o = off[r0 + i * STEP];
-                    w[i] = make_uint4(0, 0, 0, 0);
-                    if (o >= 0 && dim0 + u * 16 < a.dim) w[i] = ld_codes(side + o + dim0 + u * 16);
-                }
+                for (int i = 0; i < C::N; ++i) w[i] = ld_codes(a.k + off[i * C::STEP] + u * 16, off[i * C::STEP] >= 0 && u * 16 < a.dim);
+            }
+#pragma unroll 1
+            for (int q = 0; q < items; ++q) {
+                const bool guard = FMT == kKvE4m3 && guarded(it);
+                const int first_pos = k0 + it.tile * 128 + r0;
+                const bool more = q + 1 < items;
+                if (more) it = item_at(q + 1);
+                const long long* off = more ? begin_item(it) + r0 : offsets;
+                const unsigned char* side = (it.values ? a.v : a.k) + it.part_of_dims * DI + u * 16;
+                const bool dims_there = more && it.part_of_dims * DI + u * 16 < a.dim;
+                unsigned char* dst = slot_of(q) + to;
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const int r = r0 + i * STEP;
-                    if (FMT == kKvE4m3 && guard && k0 + j * 128 + r >= all_see) {
+                for (int i = 0; i < C::N; ++i) {
+                    if (guard && first_pos + i * C::STEP >= all_see) {
                         uint32_t* x = &w[i].x;
+                        uint32_t hits = 0;
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
                             const uint32_t hit = __vcmpeq4(x[k] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
-                            hit_any = hit_any || hit != 0;
+                            hits |= hit;
                             x[k] &= ~hit;
                         }
+                        if (hits) poisoned = 1;
                     }
-                    unsigned char* base = dst + (u >> 2) * kTileBlockBytes + r * 128;
-                    const uint4 lo = make_uint4(pick_half2<FMT, 0, 1>(w[i].x, w[i].x), pick_half2<FMT, 2, 3>(w[i].x, w[i].x),
-                                                pick_half2<FMT, 0, 1>(w[i].y, w[i].y), pick_half2<FMT, 2, 3>(w[i].y, w[i].y));
-                    const uint4 hi = make_uint4(pick_half2<FMT, 0, 1>(w[i].z, w[i].z), pick_half2<FMT, 2, 3>(w[i].z, w[i].z),
-                                                pick_half2<FMT, 0, 1>(w[i].w, w[i].w), pick_half2<FMT, 2, 3>(w[i].w, w[i].w));
-                    *reinterpret_cast<uint4*>(base + ((((u & 3) * 2) ^ (r & 7)) << 4)) = lo;
-                    *reinterpret_cast<uint4*>(base + ((((u & 3) * 2 + 1) ^ (r & 7)) << 4)) = hi;
+                    store_codes<FMT>(dst + lo + i * C::STEP * 128, dst + hi + i * C::STEP * 128, w[i]);
+                    const long long o = off[i * C::STEP];
+                    w[i] = ld_codes(side + o, o >= 0 && dims_there);
                 }
-                if (hit_any) poisoned = 1;
-                announce(item);
-            } else {
+                announce(q);
+            }
+        } else {
+#pragma unroll 1
+            for (int q = 0; q < items; ++q) {
+                const Item it = item_at(q);
+                const long long* off = begin_item(it);
+                const int dim0 = it.part_of_dims * DI;
                 constexpr int UNITS = DI / 8, STEP = 128 / UNITS;
                 const int u = p % UNITS, r0 = p / UNITS;
-                fetch_plain_tile<DI>(dst, side, off, p, dim0 + u * 8 < a.dim, dim0 * 2);
-                if (pending) {  // the one before has landed when only this one is outstanding
+                unsigned char* dst = slot_of(q);
+                fetch_plain_tile<DI>(dst, it.values ? a.v : a.k, off, p, dim0 + u * 8 < a.dim, dim0 * 2);
+                if (q > 0) {  // the one before has landed when only this one is outstanding
                     asm volatile("cp.async.wait_group 1;" ::: "memory");
-                    announce(item - 1);
+                    announce(q - 1);
                 }
-                pending = true;
-                if (guard) {
+                if (guarded(it)) {
+                    bool hit_any = false;
                     asm volatile("cp.async.wait_group 0;" ::: "memory");
 #pragma unroll 1
                     for (int r = r0; r < 128; r += STEP) {
-                        if (k0 + j * 128 + r < all_see) continue;
+                        if (k0 + it.tile * 128 + r < all_see) continue;
                         uint4* at = reinterpret_cast<uint4*>(dst + (u >> 3) * kTileBlockBytes + r * 128 + (((u & 7) ^ (r & 7)) << 4));
                         uint4 w = *at;
                         uint32_t* x = &w.x;
@@ -541,25 +589,8 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
                     if (hit_any) poisoned = 1;
                 }
             }
-            ++item;
-        };
-        // places of a tile's keys, one thread to a key; tile j + 2 is placed when every thread is past the values of tile j - 1
-        int page_n = page_of(0, p);
-        auto keys = [&](int j) {
-            const long long o = place_of_key(j, p, page_n, false);
-            if (j + 1 < n) page_n = page_of(j + 1, p);
-            offsets[(j % 3) * 128 + p] = o * ES;
-            asm volatile("barrier.cta.sync 2, 128;" ::: "memory");
-            for (int i = 0; i < NI; ++i) fetch(a.k, j, i, false);
-        };
-        keys(0);
-        for (int j = 0; j < n; ++j) {
-            if (j + 1 < n) keys(j + 1);
-            for (int i = 0; i < NI; ++i) fetch(a.v, j, i, true);
-        }
-        if constexpr (!kQuant) {
             asm volatile("cp.async.wait_all;" ::: "memory");
-            if (pending) announce(item - 1);
+            announce(items - 1);
         }
     } else {
         // ---- the warp that issues the products ----

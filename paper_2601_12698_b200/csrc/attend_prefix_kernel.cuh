@@ -7,14 +7,15 @@
 // one CTA to an SM, so the SMs finish together whatever the number of heads and rows; a run may end one unit and begin the
 // next.  What a CTA finds out about a unit is one part (two in the narrow form below), joined by merge_parts_kernel.
 //
-// Inside a CTA (13 warps):
+// Inside a CTA (16 warps):
 //   warps 0-3, 4-7   two softmax streams of 128 rows, one row to a thread (tensor memory lane = row): they read S from
 //                    tensor memory, keep m and the sum in registers, and write the weights back over S as the 16-bit
 //                    left operand of the second product;
 //   warps 8-11       fetch the paged tiles: keys and values with cp.async, 16 bytes a piece, into the 128-byte-swizzled
 //                    layout that the matrix unit reads (pages may have any size, so one copy per row is the widest that
 //                    always works); quantised tiles are fetched into registers, turned into fp16 and stored;
-//   warp 12          one thread issues the matrix products.
+//   warp 12          issues the matrix products;
+//   warps 14, 15     look up the pages and scales of the tiles to come.
 // The two streams take turns on the tensor cores: while one's scores are exponentiated the other's products run.  Blocks of
 // more than 128 rows (wide form): a stream is one half of the rows, both use the same tiles.  Blocks of up to 128 rows
 // (narrow form): both streams use the same rows and alternate the tiles, and leave a part each.
@@ -37,11 +38,13 @@ namespace rt {
 
 constexpr int kTcThreads = 512;
 constexpr int kTcSlots = 4;   // ring of key and value tiles
-constexpr int kTcAux = 4;     // tiles whose per-key constants are kept
+constexpr int kTcAux = 4;     // tiles whose places and constants are kept: the two under way and two ahead
 
 template <int FMT, int DP>
 struct PrefixShape {
     static constexpr bool kQuant = FMT != kKvPlain;
+    // Registers per softmax thread; half the threads are softmax threads, and the other half gets the rest of 2 * 128.
+    static constexpr int kSoftmaxRegs = 144;
     static constexpr int kTileBytes = kTcTile * DP * 2;
     static constexpr int kAuxFloats = kQuant ? 3 * kTcTile : kTcTile;
     static constexpr size_t kAuxAt = (size_t)(2 + kTcSlots) * kTileBytes;
@@ -68,10 +71,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
     unsigned char* ring = smem + 2 * S::kTileBytes;
     float* aux = reinterpret_cast<float*>(smem + S::kAuxAt);
     long long* offsets = reinterpret_cast<long long*>(smem + S::kOffsetsAt);
-    __shared__ __align__(8) uint64_t full[kTcSlots], empty[kTcSlots], aux_full[kTcAux], s_full[2], p_full[2], o_full[2], q_full, drained;
+    __shared__ __align__(8) uint64_t full[kTcSlots], empty[kTcSlots], aux_full[kTcAux], aux_free[kTcAux], s_full[2], p_full[2], o_full[2], q_full, drained;
     __shared__ uint32_t tmem_base;
     __shared__ float row_factor[2][kQuant ? 128 : 1];
-    __shared__ uint32_t ragged[kTcAux];  // one byte per fetching warp: some key of its quarter of the tile is not there
+    __shared__ uint32_t ragged[kTcAux];  // one byte for each half of the lookup: some key is not there
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
@@ -79,7 +82,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
             mbarrier_init(&full[i], 128);
             mbarrier_init(&empty[i], 1);
         }
-        for (int i = 0; i < kTcAux; ++i) mbarrier_init(&aux_full[i], 128);
+        for (int i = 0; i < kTcAux; ++i) {
+            mbarrier_init(&aux_full[i], 64);
+            mbarrier_init(&aux_free[i], 1);
+            ragged[i] = 0;
+        }
         for (int i = 0; i < 2; ++i) {
             mbarrier_init(&s_full[i], 1);
             mbarrier_init(&p_full[i], 128);
@@ -98,8 +105,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
     const uint32_t tmem = tmem_base;
     wait_for_previous_kernel();
 
-    const long long total = (long long)split.tiles * split.blocks * a.kv_heads;
-    const long long begin = (long long)blockIdx.x * split.run, end = min(total, begin + split.run);
+    const int total = split.tiles * split.blocks * a.kv_heads;  // the host checked that it fits
+    const int begin = (int)blockIdx.x * split.run, end = min(total - begin, split.run) + begin;
     // Every wait is bounded.  A thread whose wait has run out stops waiting and goes on through the same loops, so that every
     // barrier is still met and the tensor memory is given back; the status word says that the results are not valid.
     bool ok = true;
@@ -109,7 +116,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
 
     if (warp < 8) {
         // ---- softmax streams ----
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kSoftmaxRegs));
         const int s = warp >> 2, r = (warp & 3) * 32 + lane;
         const uint32_t lane_base = tmem + ((uint32_t)(warp & 3) << 21);
         const uint32_t s_col = lane_base + s * kTcTile, o_col = lane_base + kColO + s * DP;
@@ -118,10 +125,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
         const int n_heads = a.kv_heads * a.group;
         const long long n_rows = (long long)a.n_seqs * a.q_len * n_heads;
         uint32_t n_s = 0, n_o = 0, tile_no = 0;
-        for (long long at = begin; at < end;) {
-            const int unit = (int)(at / split.tiles), block = unit % split.blocks, kv_head = unit / split.blocks;
-            const int tile0 = (int)(at - (long long)unit * split.tiles);
-            const int n = (int)min((long long)(split.tiles - tile0), end - at);
+        for (int at = begin; at < end;) {
+            const int unit = at / split.tiles, block = unit % split.blocks, kv_head = unit / split.blocks;
+            const int tile0 = at - unit * split.tiles;
+            const int n = min(split.tiles - tile0, end - at);
             const bool narrow = narrow_block(split, block);
             const int first_row = block * kTcBlockRows + (narrow ? 0 : s * 128);
             // [token][head] index of row i of this stream's 128, -1: no such row
@@ -139,12 +146,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                 constexpr int LANES = DP / 8, ROWS = 32 / LANES, N = 32 / ROWS;  // lanes per row, rows at once, turns
                 const int u = lane % LANES;
                 unsigned char* tile = q_tiles + s * S::kTileBytes + (u >> 3) * kBlockBytes;
+                {
+                    uint4 w[N];  // all at once: behind the first tiles' copies every further round trip would take its turn
 #pragma unroll
-                for (int h = 0; h < N; h += 8) {
-                    uint4 w[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int row = first_row + (warp & 3) * 32 + (h + i) * ROWS + lane / LANES;
+                    for (int i = 0; i < N; ++i) {
+                        const int row = first_row + (warp & 3) * 32 + i * ROWS + lane / LANES;
                         const bool there = row < split.rows && u * 8 < a.dim;
                         const int token = there ? row / a.group : 0;
                         const long long o = (long long)token * a.q_token_stride +
@@ -153,8 +159,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                         if (!there) w[i] = make_uint4(0, 0, 0, 0);
                     }
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int mine = (warp & 3) * 32 + (h + i) * ROWS + lane / LANES;
+                    for (int i = 0; i < N; ++i) {
+                        const int mine = (warp & 3) * 32 + i * ROWS + lane / LANES;
                         const uint32_t sign = flip ? 0x80008000u : 0u;
                         w[i].x ^= sign; w[i].y ^= sign; w[i].z ^= sign; w[i].w ^= sign;
                         if constexpr (kQuant) {
@@ -190,51 +196,77 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                 ++n_s;
                 tc_fence_after();
                 const float4* ka = reinterpret_cast<const float4*>(aux + aux_i * S::kAuxFloats);
-                // the tile's scores of this row, as logarithms (quantised) or still to be scaled (plain), hidden ones -inf
-                uint32_t v[128];
+                // One pass over the tile's scores of this row, 32 at a time, gives their maximum and, with the reference as it is, the
+                // weights and their sum.  Only when the maximum turns out to be more than 8 above the reference is the pass made
+                // again, with a reference that has been moved there; the scores are still in tensor memory, the weights go over them
+                // at the end.  (The row's first tile has no reference yet and always takes two passes.)
+                uint32_t w[4][16];
+                float2x sum[2];
+                for (;;) {
+                    // No key of the row so far: the reference is -inf, every score is -inf, and so must every weight's logarithm be.
+                    const float base = m == -INFINITY ? 0.f : m;
+                    // A score scale of zero would make NaN of a plain cache's hidden scores: the smallest normal number does instead.
+                    const float c = kQuant ? row_c : fmaxf(row_c, 1.17549435e-38f);
+                    const float2x c2 = pack_f2(c, c), minus2 = pack_f2(-base, -base);
+                    float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    sum[0] = sum[1] = pack_f2(0.f, 0.f);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) tmem_load32(s_col + q * 32, *reinterpret_cast<uint32_t(*)[32]>(&v[q * 32]));
-                tmem_wait_load();
-                float top = -INFINITY;
-                if constexpr (kQuant) {
+                    for (int q = 0; q < 4; ++q) {
+                        uint32_t v[32];
+                        tmem_load32(s_col + q * 32, v);
+                        tmem_wait_load(v);
+                        if (!kQuant && *reinterpret_cast<volatile uint32_t*>(&ragged[aux_i]) != 0) {  // the last tile, or pages that are not there
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) {
-                        const float4 ks = ka[k], lv = ka[32 + k];
-                        const float x0 = fmaf(__uint_as_float(v[4 * k]) * row_c, ks.x, lv.x), x1 = fmaf(__uint_as_float(v[4 * k + 1]) * row_c, ks.y, lv.y);
-                        const float x2 = fmaf(__uint_as_float(v[4 * k + 2]) * row_c, ks.z, lv.z), x3 = fmaf(__uint_as_float(v[4 * k + 3]) * row_c, ks.w, lv.w);
-                        v[4 * k] = __float_as_uint(x0); v[4 * k + 1] = __float_as_uint(x1);
-                        v[4 * k + 2] = __float_as_uint(x2); v[4 * k + 3] = __float_as_uint(x3);
-                        top = fmaxf(fmaxf(top, x0), x1);
-                        top = fmaxf(fmaxf(top, x2), x3);
-                    }
-                } else {
-                    if (*reinterpret_cast<volatile uint32_t*>(&ragged[aux_i]) != 0) {  // the last tile, or pages that are not there
+                            for (int k = 0; k < 8; ++k) {
+                                const float4 b = ka[q * 8 + k];
+                                if (b.x != 0.f) v[4 * k] = 0xFF800000u;
+                                if (b.y != 0.f) v[4 * k + 1] = 0xFF800000u;
+                                if (b.z != 0.f) v[4 * k + 2] = 0xFF800000u;
+                                if (b.w != 0.f) v[4 * k + 3] = 0xFF800000u;
+                            }
+                        }
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) {
-                            const float4 b = ka[k];
-                            if (b.x != 0.f) v[4 * k] = 0xFF800000u;
-                            if (b.y != 0.f) v[4 * k + 1] = 0xFF800000u;
-                            if (b.z != 0.f) v[4 * k + 2] = 0xFF800000u;
-                            if (b.w != 0.f) v[4 * k + 3] = 0xFF800000u;
+                        for (int k = 0; k < 8; ++k) {
+                            float2x t0 = pack_f2(__uint_as_float(v[4 * k]), __uint_as_float(v[4 * k + 1]));
+                            float2x t1 = pack_f2(__uint_as_float(v[4 * k + 2]), __uint_as_float(v[4 * k + 3]));
+                            if constexpr (kQuant) {
+                                const ulonglong2* k2 = reinterpret_cast<const ulonglong2*>(ka) + q * 8 + k;
+                                const ulonglong2 ks = k2[0], lv = k2[32];
+                                t0 = fma_f2(mul_f2(t0, c2), ks.x, lv.x);
+                                t1 = fma_f2(mul_f2(t1, c2), ks.y, lv.y);
+                            }
+                            float x[4];
+                            unpack_f2(t0, x[0], x[1]);
+                            unpack_f2(t1, x[2], x[3]);
+                            t4[0] = fmaxf(fmaxf(t4[0], x[0]), x[1]);
+                            t4[1] = fmaxf(fmaxf(t4[1], x[2]), x[3]);
+                            unpack_f2(kQuant ? add_f2(t0, minus2) : fma_f2(t0, c2, minus2), x[0], x[1]);
+                            unpack_f2(kQuant ? add_f2(t1, minus2) : fma_f2(t1, c2, minus2), x[2], x[3]);
+#pragma unroll
+                            for (int y = 0; y < 4; ++y) x[y] = ex2(x[y]);
+                            if constexpr (kQuant) {
+                                const ulonglong2 iv = reinterpret_cast<const ulonglong2*>(ka)[64 + q * 8 + k];
+                                sum[0] = fma_f2(pack_f2(x[0], x[1]), iv.x, sum[0]);
+                                sum[1] = fma_f2(pack_f2(x[2], x[3]), iv.y, sum[1]);
+                            } else {
+                                sum[0] = add_f2(pack_f2(x[0], x[1]), sum[0]);
+                                sum[1] = add_f2(pack_f2(x[2], x[3]), sum[1]);
+                            }
+                            w[q][2 * k] = pack2<M>(x[0], x[1]);
+                            w[q][2 * k + 1] = pack2<M>(x[2], x[3]);
                         }
                     }
-                    float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                    for (int k = 0; k < 128; k += 8)
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) t4[y] = fmaxf(fmaxf(t4[y], __uint_as_float(v[k + 2 * y])), __uint_as_float(v[k + 2 * y + 1]));
-                    top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
-                    top = top == -INFINITY ? top : top * row_c;
-                }
-                const bool move = top > m + 8.f;
-                if (__any_sync(0xFFFFFFFFu, move)) {
+                    float top = fmaxf(t4[0], t4[1]);
+                    if (!kQuant) top = top == -INFINITY ? top : top * row_c;
+                    const bool move = top > m + 8.f;
+                    if (!__any_sync(0xFFFFFFFFu, move)) break;
                     const float alpha = move ? ex2(m - top) : 1.f;
                     if (i > 0) {
 #pragma unroll 1
                         for (int q = 0; q < DP / 16; ++q) {
                             uint32_t o[16];
                             tmem_load16(o_col + q * 16, o);
-                            tmem_wait_load();
+                            tmem_wait_load(o);
 #pragma unroll
                             for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
                             tmem_store16(o_col + q * 16, o);
@@ -243,31 +275,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                     l *= alpha;
                     if (move) m = top;
                 }
-                // No key of the row so far: m is -inf, every score is -inf, and so must every weight's logarithm be.  A score
-                // scale of zero would make NaN of a plain cache's hidden scores: the smallest normal number does instead.
-                const float base = m == -INFINITY ? 0.f : m;
-                const float c = kQuant ? 1.f : fmaxf(row_c, 1.17549435e-38f);
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
-                uint32_t w[64];
 #pragma unroll
-                for (int k = 0; k < 64; k += 2) {
-                    const float x0 = ex2(kQuant ? __uint_as_float(v[2 * k]) - base : fmaf(__uint_as_float(v[2 * k]), c, -base));
-                    const float x1 = ex2(kQuant ? __uint_as_float(v[2 * k + 1]) - base : fmaf(__uint_as_float(v[2 * k + 1]), c, -base));
-                    const float x2 = ex2(kQuant ? __uint_as_float(v[2 * k + 2]) - base : fmaf(__uint_as_float(v[2 * k + 2]), c, -base));
-                    const float x3 = ex2(kQuant ? __uint_as_float(v[2 * k + 3]) - base : fmaf(__uint_as_float(v[2 * k + 3]), c, -base));
-                    if constexpr (kQuant) {
-                        const float4 iv = ka[64 + k / 2];
-                        sum[0] = fmaf(x0, iv.x, sum[0]); sum[1] = fmaf(x1, iv.y, sum[1]);
-                        sum[2] = fmaf(x2, iv.z, sum[2]); sum[3] = fmaf(x3, iv.w, sum[3]);
-                    } else {
-                        sum[0] += x0; sum[1] += x1; sum[2] += x2; sum[3] += x3;
-                    }
-                    w[k] = pack2<M>(x0, x1);
-                    w[k + 1] = pack2<M>(x2, x3);
-                }
-#pragma unroll
-                for (int q = 0; q < 2; ++q) tmem_store32(s_col + q * 32, *reinterpret_cast<uint32_t(*)[32]>(&w[q * 32]));
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                for (int q = 0; q < 4; ++q) tmem_store16(s_col + q * 16, w[q]);
+                float part_sum[2];
+                unpack_f2(add_f2(sum[0], sum[1]), part_sum[0], part_sum[1]);
+                l += part_sum[0] + part_sum[1];
                 tmem_wait_store();
                 tc_fence_before();
                 mbarrier_arrive(&p_full[s]);
@@ -297,7 +309,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                 for (int q = 0; q < DP / 32; ++q) {
                     uint32_t o[32];
                     tmem_load32(o_col + q * 32, o);
-                    tmem_wait_load();
+                    tmem_wait_load(o);
 #pragma unroll
                     for (int k = 0; k < 8; ++k)
                         *reinterpret_cast<float4*>(stage + lane * 128 + ((k ^ (lane & 7)) << 4)) =
@@ -319,108 +331,89 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
         }
     } else if (warp < 12) {
         // ---- fetching warps ----
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(256 - S::kSoftmaxRegs));
         const int p = tid - 256;
-        uint32_t item = 0, tile_no = 0;
-        uint32_t pending = 0;          // items issued but not yet announced (plain: cp.async groups)
-        auto announce = [&](uint32_t i) {
-            fence_async_proxy();
-            mbarrier_arrive(&full[i % kTcSlots]);
+        // Items in the order in which the products want them.  Wide units: K0, V0, K1, V1, ...; narrow ones: K0, K1, V0, K2, V1,
+        // ... V(n-1).
+        int at = begin, n = 0, g = 0, lead = 0, tile_no = 0;  // unit: first tile, tiles in this run, next item, form; tiles before it
+        auto enter = [&]() {
+            const int unit = at / split.tiles;
+            n = min(split.tiles - (at - unit * split.tiles), end - at);
+            lead = narrow_block(split, unit % split.blocks) ? 2 : 1;
+            g = 0;
         };
-        // One tile of keys or values; `t` numbers the tile, whose places are in offsets[t % kTcAux].
-        auto fetch = [&](const unsigned char* side, uint32_t t) {
-            wait(&empty[item % kTcSlots], ((item / kTcSlots) & 1) ^ 1);
-            unsigned char* dst = ring + (item % kTcSlots) * S::kTileBytes;
-            const long long* off = offsets + (t % kTcAux) * kTcTile;
-            if constexpr (kQuant) {
-                constexpr int UNITS = DP / 16;            // 16 codes a piece
-                constexpr int STEP = 128 / UNITS, N = kTcTile / STEP;
-                const int u = p % UNITS, row0 = p / UNITS;
-#pragma unroll
-                for (int h = 0; h < N; h += 8) {
-                    uint4 w[8];
-#pragma unroll
-                    for (int i = 0; i < 8 && i < N; ++i) {
-                        const long long o = off[row0 + (h + i) * STEP];
-                        w[i] = make_uint4(0, 0, 0, 0);
-                        if (o >= 0 && u * 16 < a.dim) w[i] = __ldg(reinterpret_cast<const uint4*>(side + o + u * 16));
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8 && i < N; ++i) {
-                        const int r = row0 + (h + i) * STEP;
-                        unsigned char* base = dst + (u >> 2) * kBlockBytes + r * 128;
-                        const uint4 lo = make_uint4(pick_half2<FMT, 0, 1>(w[i].x, w[i].x), pick_half2<FMT, 2, 3>(w[i].x, w[i].x),
-                                                    pick_half2<FMT, 0, 1>(w[i].y, w[i].y), pick_half2<FMT, 2, 3>(w[i].y, w[i].y));
-                        const uint4 hi = make_uint4(pick_half2<FMT, 0, 1>(w[i].z, w[i].z), pick_half2<FMT, 2, 3>(w[i].z, w[i].z),
-                                                    pick_half2<FMT, 0, 1>(w[i].w, w[i].w), pick_half2<FMT, 2, 3>(w[i].w, w[i].w));
-                        *reinterpret_cast<uint4*>(base + ((((u & 3) * 2) ^ (r & 7)) << 4)) = lo;
-                        *reinterpret_cast<uint4*>(base + ((((u & 3) * 2 + 1) ^ (r & 7)) << 4)) = hi;
-                    }
-                }
-                announce(item);
+        enter();
+        bool values;
+        auto next_item = [&]() -> const long long* {  // the places of the item's tile
+            const int half = (g + 1) >> 1;
+            int tile;
+            if (lead == 1) {
+                values = g & 1;
+                tile = g >> 1;
             } else {
-                fetch_plain_tile<DP>(dst, side, off, p, (p % (DP / 8)) * 8 < a.dim, 0);
-                if (++pending == 2) {  // the one before has landed when only this one is outstanding
-                    asm volatile("cp.async.wait_group 1;" ::: "memory");
-                    announce(item - 1);
-                    --pending;
-                }
+                values = g > 0 && (!(g & 1) || half == n);
+                tile = g == 0 ? 0 : (g & 1) ? (values ? n - 1 : half) : half - 1;
             }
-            ++item;
+            const int t = tile_no + tile;
+            if (!values) wait(&aux_full[t % kTcAux], (t / kTcAux) & 1);
+            if (++g == 2 * n) {
+                at += n;
+                tile_no += n;
+                if (at < end) enter();
+            }
+            return offsets + (t % kTcAux) * kTcTile;
         };
-        for (long long at = begin; at < end;) {
-            const int unit = (int)(at / split.tiles), block = unit % split.blocks, kv_head = unit / split.blocks;
-            const int tile0 = (int)(at - (long long)unit * split.tiles);
-            const int n = (int)min((long long)(split.tiles - tile0), end - at);
-            const int lead = narrow_block(split, block) ? 2 : 1;
-            // order of the tiles in the ring: K0 (K1), then V0 K(lead) V1 K(lead + 1) ...
-            auto keys = [&](int j) {
-                const uint32_t t = tile_no + j;
-                const int pos = (tile0 + j) * kTcTile + p;
-                long long o = -1, so = -1;
-                if (pos < a.prefix_len) {
-                    int li;
-                    unsigned in_page;
-                    split_position(a, pos, li, in_page);
-                    const int page = __ldg(a.prefix_pages + li);
-                    if (page >= 0 && page < a.n_pages) {
-                        o = entry_offset(a, page, in_page, kv_head, false);
-                        so = entry_offset(a, page, in_page, kv_head, true);
-                    } else {
-                        atomicExch(a.status, kDeviceIndexCode);
-                    }
-                }
-                offsets[(t % kTcAux) * kTcTile + p] = kQuant ? o : o * 2;
-                float* to = aux + (t % kTcAux) * S::kAuxFloats + p;
-                if constexpr (kQuant) {
-                    const float ks = o >= 0 ? __ldg(a.k_scale + so) : 0.f, vs = o >= 0 ? usable_scale(__ldg(a.v_scale + so)) : 0.f;
-                    to[0] = ks;
-                    to[kTcTile] = o >= 0 ? log2f(vs) : -INFINITY;
-                    to[2 * kTcTile] = o >= 0 ? __frcp_rn(vs) : 0.f;
-                } else {
-                    to[0] = o >= 0 ? 0.f : 1.f;
-                    const uint32_t there = __ballot_sync(0xFFFFFFFFu, o >= 0);
-                    if (lane == 0) reinterpret_cast<unsigned char*>(&ragged[t % kTcAux])[warp - 8] = there != 0xFFFFFFFFu;
-                }
-                mbarrier_arrive(&aux_full[t % kTcAux]);
-                asm volatile("bar.sync 2, 128;" ::: "memory");
-                fetch(a.k, t);
-            };
-            for (int j = 0; j < lead && j < n; ++j) keys(j);
-            for (int j = 0; j < n; ++j) {
-                fetch(a.v, tile_no + j);
-                if (j + lead < n) keys(j + lead);
+        auto slot_of = [&](int q) -> unsigned char* {
+            wait(&empty[q % kTcSlots], ((q / kTcSlots) & 1) ^ 1);
+            return ring + (q % kTcSlots) * S::kTileBytes;
+        };
+        auto announce = [&](int q) {
+            fence_async_proxy();
+            mbarrier_arrive(&full[q % kTcSlots]);
+        };
+        const int items = 2 * (end - begin);
+        if constexpr (kQuant) {
+            using C = CodePieces<DP>;
+            const int u = p % C::UNITS, r0 = p / C::UNITS;
+            const int to = (u >> 2) * kTileBlockBytes + r0 * 128, lo = (((u & 3) * 2) ^ (r0 & 7)) << 4, hi = (((u & 3) * 2 + 1) ^ (r0 & 7)) << 4;
+            const bool dims_there = u * 16 < a.dim;
+            uint4 w[C::N];
+            {
+                const long long* off = next_item() + r0;
+#pragma unroll
+                for (int i = 0; i < C::N; ++i) w[i] = ld_codes(a.k + off[i * C::STEP] + u * 16, off[i * C::STEP] >= 0 && dims_there);
             }
-            tile_no += n;
-            at += n;
-        }
-        if constexpr (!kQuant) {
+#pragma unroll 1
+            for (int q = 0; q < items; ++q) {
+                const bool more = q + 1 < items;
+                const long long* off = more ? next_item() + r0 : offsets;
+                const unsigned char* side = (values ? a.v : a.k) + u * 16;
+                unsigned char* dst = slot_of(q) + to;
+#pragma unroll
+                for (int i = 0; i < C::N; ++i) {
+                    store_codes<FMT>(dst + lo + i * C::STEP * 128, dst + hi + i * C::STEP * 128, w[i]);
+                    const long long o = off[i * C::STEP];
+                    w[i] = ld_codes(side + o, o >= 0 && dims_there && more);
+                }
+                announce(q);
+            }
+        } else {
+            const bool dims_there = (p % (DP / 8)) * 8 < a.dim;
+#pragma unroll 1
+            for (int q = 0; q < items; ++q) {
+                const long long* off = next_item();
+                fetch_plain_tile<DP>(slot_of(q), values ? a.v : a.k, off, p, dims_there, 0);
+                if (q > 0) {  // the one before has landed when only this one is outstanding
+                    asm volatile("cp.async.wait_group 1;" ::: "memory");
+                    announce(q - 1);
+                }
+            }
             asm volatile("cp.async.wait_all;" ::: "memory");
-            if (pending) announce(item - 1);
+            announce(items - 1);
         }
     } else {
-        // ---- the warp that issues the products (three more only hold its warpgroup's registers) ----
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        // ---- warp 12 issues the products, warps 14 and 15 look up the places ----
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(256 - S::kSoftmaxRegs));
         if (warp == 12) {
             constexpr uint64_t kRowsLayout = tc_layout(16, 1024), kColsLayout = tc_layout(kBlockBytes, 1024);
             constexpr uint32_t kTile16 = S::kTileBytes / 16;
@@ -444,15 +437,20 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                 }
                 __syncwarp();
             };
+            uint32_t outputs = 0;  // tiles whose last product has been issued
             auto output = [&](int s, uint32_t i, bool first, bool release, bool last) {
                 const uint32_t v_at = ring16 + (i % kTcSlots) * kTile16, d = tmem + kColO + s * DP, w = tmem + s * kTcTile;
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < kTcTile / 16; ++k)
                         tc_mma_ts(d, w + k * 8, tc_descriptor(kColsLayout, v_at + k * 128), kOutIdesc, k > 0 ? 1u : (uint32_t)!first);
-                    if (release) tc_commit(&empty[i % kTcSlots]);
+                    if (release) {  // the tile is done with: its values, its places and its constants
+                        tc_commit(&empty[i % kTcSlots]);
+                        tc_commit(&aux_free[outputs % kTcAux]);
+                    }
                     if (last) tc_commit(&o_full[s]);
                 }
+                if (release) ++outputs;
                 __syncwarp();
             };
             auto wait_weights = [&](int s) {
@@ -460,10 +458,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                 ++n_p[s];
                 tc_fence_after();
             };
-            for (long long at = begin; at < end;) {
-                const int unit = (int)(at / split.tiles), block = unit % split.blocks;
-                const int tile0 = (int)(at - (long long)unit * split.tiles);
-                const int n = (int)min((long long)(split.tiles - tile0), end - at);
+            for (int at = begin; at < end;) {
+                const int unit = at / split.tiles, block = unit % split.blocks;
+                const int tile0 = at - unit * split.tiles;
+                const int n = min(split.tiles - tile0, end - at);
                 wait(&q_full, n_q & 1);
                 ++n_q;
                 tc_fence_after();
@@ -507,6 +505,70 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
             if (elect_one()) tc_commit(&drained);
             __syncwarp();
             ok = mbarrier_wait_bounded(&drained, 0) && ok;
+        } else if (warp >= 14) {
+            // Places of the tiles' keys and what the softmax wants to know of them, two keys to a thread, up to kTcAux tiles ahead.
+            // A tile's page numbers are read while the tile before it is published.
+            const int p = tid - 448;
+            int page_n[2];
+            auto read_pages = [&](int g) {
+                const int pos = (g % split.tiles) * kTcTile + p;
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    page_n[y] = -1;  // no such key
+                    if (pos + 64 * y >= a.prefix_len) continue;
+                    int li;
+                    unsigned in_page;
+                    split_position(a, pos + 64 * y, li, in_page);
+                    const int page = __ldg(a.prefix_pages + li);
+                    page_n[y] = page < 0 ? -2 : page;
+                }
+            };
+            read_pages(begin);
+#pragma unroll 1
+            for (int g = begin; g < end; ++g) {
+                const int t = g - begin, slot = t % kTcAux, unit = g / split.tiles, tile = g - unit * split.tiles, kv_head = unit / split.blocks;
+                long long o[2];
+                float ks[2] = {0.f, 0.f}, vs[2] = {1.f, 1.f};
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    o[y] = -1;
+                    if (page_n[y] == -1) continue;
+                    if (page_n[y] < 0 || page_n[y] >= a.n_pages) {
+                        atomicExch(a.status, kDeviceIndexCode);
+                        continue;
+                    }
+                    int li;
+                    unsigned in_page;
+                    split_position(a, tile * kTcTile + p + 64 * y, li, in_page);
+                    o[y] = entry_offset(a, page_n[y], in_page, kv_head, false) * (kQuant ? 1 : 2);
+                    if constexpr (kQuant) {
+                        const long long so = entry_offset(a, page_n[y], in_page, kv_head, true);
+                        ks[y] = __ldg(a.k_scale + so);
+                        vs[y] = __ldg(a.v_scale + so);
+                    }
+                }
+                if (g + 1 < end) read_pages(g + 1);
+                wait(&aux_free[slot], ((t / kTcAux) & 1) ^ 1);
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const bool there = o[y] >= 0;
+                    offsets[slot * kTcTile + p + 64 * y] = o[y];
+                    float* to = aux + slot * S::kAuxFloats + p + 64 * y;
+                    if constexpr (kQuant) {
+                        const float u = usable_scale(vs[y]);
+                        to[0] = ks[y];
+                        to[kTcTile] = there ? log2f(u) : -INFINITY;
+                        to[2 * kTcTile] = there ? __frcp_rn(u) : 0.f;
+                    } else {
+                        to[0] = there ? 0.f : 1.f;
+                    }
+                }
+                if constexpr (!kQuant) {
+                    const uint32_t all = __ballot_sync(0xFFFFFFFFu, o[0] >= 0 && o[1] >= 0);
+                    if (lane == 0) reinterpret_cast<unsigned char*>(&ragged[slot])[warp - 14] = all != 0xFFFFFFFFu;
+                }
+                mbarrier_arrive(&aux_full[slot]);
+            }
         }
     }
     if (!ok) atomicExch(a.status, kDeviceTimeoutCode);

@@ -133,7 +133,11 @@ int make_attend_plan(const rt_kv_cache* c, const rt_prefix_batch* b, int q_heads
             s.rows = (int)prefix_rows;
             s.blocks = (int)ceil_div(prefix_rows, kTcBlockRows);
             const long long total = (long long)s.tiles * s.blocks * c->kv_heads;
-            s.run = (int)std::min<long long>(ceil_div(total, L.sm_count), 1 << 30);
+            if (total > 1LL << 30) {
+                set_error("prefix of %lld tokens for %lld rows is too large", (long long)b->prefix_len, (long long)prefix_rows);
+                return RT_ERR_SHAPE;
+            }
+            s.run = (int)ceil_div(total, L.sm_count);
             p->prefix_ctas = ceil_div(total, s.run);
             p->prefix_parts = most_parts(s);
         } else {

@@ -1,7 +1,7 @@
 // The fifth-generation tensor cores (sm_100a): tensor memory, matrix products, descriptors.
 #pragma once
 
-#include "add_rmsnorm_kernel.cuh"
+#include "attend_common.cuh"
 
 namespace rt {
 
@@ -18,7 +18,25 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&r)[32])
           "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(addr));
 }
-__device__ __forceinline__ void tmem_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Waits for this thread's loads.  The registers are named, so that nothing that uses them is moved ahead of the wait.
+__device__ __forceinline__ void tmem_wait_load(uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                   "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]),
+                   "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27])
+                 :
+                 : "memory");
+    asm volatile("" : "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]));
+}
+__device__ __forceinline__ void tmem_wait_load(uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                   "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                 :
+                 : "memory");
+}
 __device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t (&r)[32])
 {
     asm volatile(
@@ -133,6 +151,22 @@ __device__ __forceinline__ void fetch_plain_tile(unsigned char* dst, const unsig
         }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
+}
+
+// The same for codes: 16 a piece, turned into fp16 (two 16-byte pieces) on the way through registers.  N pieces per thread and
+// tile; piece i of the next tile is asked for as soon as piece i of this one has been stored, so the loads never stop.
+template <int COLS>
+struct CodePieces {
+    static constexpr int UNITS = COLS / 16, STEP = 128 / UNITS, N = 128 / STEP;
+    static_assert(STEP % 8 == 0, "rows of a thread share the swizzle");
+};
+template <int FMT>
+__device__ __forceinline__ void store_codes(unsigned char* lo, unsigned char* hi, const uint4& x)
+{
+    *reinterpret_cast<uint4*>(lo) =
+        make_uint4(pick_half2<FMT, 0, 1>(x.x, x.x), pick_half2<FMT, 2, 3>(x.x, x.x), pick_half2<FMT, 0, 1>(x.y, x.y), pick_half2<FMT, 2, 3>(x.y, x.y));
+    *reinterpret_cast<uint4*>(hi) =
+        make_uint4(pick_half2<FMT, 0, 1>(x.z, x.z), pick_half2<FMT, 2, 3>(x.z, x.z), pick_half2<FMT, 0, 1>(x.w, x.w), pick_half2<FMT, 2, 3>(x.w, x.w));
 }
 
 }  // namespace rt
