@@ -101,27 +101,35 @@ __device__ __forceinline__ void mma_16x8x16(float (&d)[4], const uint32_t (&a)[4
     }
 }
 
-// Two codes, in the low two bytes of `pair`, as two fp16 values.  Both formats fit fp16 exactly.
-template <int FMT>
-__device__ __forceinline__ uint32_t codes_to_half2(uint32_t pair_lo_bytes)
+// Two e4m3 codes as two fp16 values.  Both formats fit fp16 exactly.
+__device__ __forceinline__ uint32_t e4m3_to_half2(uint32_t low_bytes)
 {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)pair_lo_bytes, __NV_E4M3);
-    return (uint32_t)h.x | ((uint32_t)h.y << 16);
+    uint32_t h;
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\t}" : "=r"(h) : "r"(low_bytes));
+    return h;
 }
-// Bytes i and j of the word pair (a: bytes 0-3, b: bytes 4-7) as fp16 values (low half from i).
-template <int FMT, int I, int J>
-__device__ __forceinline__ uint32_t pick_half2(uint32_t a, uint32_t b)
+__device__ __forceinline__ uint32_t e4m3_high_to_half2(uint32_t word)
+{
+    uint32_t h;
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, hi;\n\t}" : "=r"(h) : "r"(word));
+    return h;
+}
+// Four codes as four fp16 values.
+template <int FMT>
+__device__ __forceinline__ void codes_to_half4(uint32_t w, uint32_t& lo, uint32_t& hi)
 {
     if constexpr (FMT == kKvE4m3) {
-        return codes_to_half2<FMT>(__byte_perm(a, b, I | (J << 4)));
+        lo = e4m3_to_half2(w);
+        hi = e4m3_high_to_half2(w);
     } else {
         // 1024 + (code + 128) as fp16 bits, minus 1152: exact for -128 .. 127
-        const uint32_t w = (__byte_perm(a, b, I | (J << 8)) & 0x00FF00FFu) ^ 0x64806480u;
-        const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&w), __half2half2(__ushort_as_half((unsigned short)0x6480)));
-        return *reinterpret_cast<const uint32_t*>(&h);
+        const __half2 bias = __half2half2(__ushort_as_half((unsigned short)0x6480));
+        const uint32_t x = w ^ 0x80808080u, a = __byte_perm(x, 0x64646464u, 0x4140), b = __byte_perm(x, 0x64646464u, 0x4342);
+        const __half2 p = __hsub2(*reinterpret_cast<const __half2*>(&a), bias), q = __hsub2(*reinterpret_cast<const __half2*>(&b), bias);
+        lo = *reinterpret_cast<const uint32_t*>(&p);
+        hi = *reinterpret_cast<const uint32_t*>(&q);
     }
 }
-
 // 16 codes of a tile that is read once, or zeros.  The zeros are set ahead of a predicated load, inside one statement: written
 // as a branch, the registers of both sides meet in a move that waits for the load.
 __device__ __forceinline__ uint4 ld_codes(const unsigned char* p, bool there)

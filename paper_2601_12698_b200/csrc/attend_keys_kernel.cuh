@@ -207,13 +207,14 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
     tc_fence_after();
     const uint32_t tmem = tmem_base, tmem_o = tmem + 2 * NR;
     const int n = (k1 - k0 + 127) / 128;
+    const int live_rows = min(NR, n_rows - row0);  // the rest of the tile is padding: nothing is computed for it beyond the products
     const int all_see = PREFIX ? len : len - a.q_len + 1;  // keys below it are seen by every row
 
     // Every wait is bounded.  A thread whose wait has run out stops waiting and goes on through the same loops, so that every
     // barrier is still met and the tensor memory is given back; the status word says that the results are not valid.
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-        if (ok) ok = mbarrier_wait_bounded(bar, parity);
+        if (ok) ok = mbarrier_wait_sleeping(bar, parity);
     };
     // Page number of key `i` of tile j; -1: there is no such key.
     auto page_of = [&](int j, int i) -> int {
@@ -317,6 +318,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
                 tmem_wait_load(v);
 #pragma unroll
                 for (int k = 0; k < 16; k += 4) {
+                    if (r0 + k >= live_rows) break;
                     float4 c4;
                     if constexpr (kQuant) c4 = *reinterpret_cast<const float4*>(&row_c[r0 + k]);
 #pragma unroll
@@ -331,9 +333,11 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
             float over = -INFINITY;
 #pragma unroll
             for (int r0 = 0; r0 < NR; r0 += 16) {
+                if (r0 >= live_rows) break;
                 scores(r0);
 #pragma unroll
                 for (int k = 0; k < 16; k += 4) {
+                    if (r0 + k >= live_rows) break;
                     const float4 m4 = *reinterpret_cast<const float4*>(&row_ref[r0 + k]);
                     over = fmaxf(over, fmaxf(fmaxf(t[k] - m4.x, t[k + 1] - m4.y), fmaxf(t[k + 2] - m4.z, t[k + 3] - m4.w)));
                 }
@@ -341,12 +345,16 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
             if (vote_any_128(over > 8.f)) {
                 // the tile's largest score of every row, over the warp and then over the four
 #pragma unroll 1
-                for (int r0 = 0; r0 < NR; r0 += 16) {
+                for (int r0 = 0; r0 < live_rows; r0 += 16) {
                     if (NR > 16) scores(r0);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const float top = warp_max(t[r]);
-                        if (lane == r) row_m[warp][r0 + r] = top;
+                    for (int k = 0; k < 16; k += 4) {
+                        if (r0 + k >= live_rows) break;
+#pragma unroll
+                        for (int r = k; r < k + 4; ++r) {
+                            const float top = warp_max(t[r]);
+                            if (lane == r) row_m[warp][r0 + r] = top;
+                        }
                     }
                 }
                 sync_128();
@@ -356,6 +364,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
                 }
 #pragma unroll
                 for (int r0 = 0; r0 < NR; r0 += 16) {
+                    if (r0 >= live_rows) break;
                     float alpha[16];
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
@@ -388,26 +397,25 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
             unsigned char* to = weights + (j & 1) * S::kWBytes + tid * RB;
 #pragma unroll
             for (int r0 = 0; r0 < NR; r0 += 16) {
+                if (r0 >= live_rows) break;
                 if (NR > 16) scores(r0);
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    uint32_t p[4];
-                    const float4 m4[2] = {*reinterpret_cast<const float4*>(&row_ref[r0 + u * 8]), *reinterpret_cast<const float4*>(&row_ref[r0 + u * 8 + 4])};
-                    const float* m = &m4[0].x;
+                for (int k = 0; k < 16; k += 4) {
+                    if (r0 + k >= live_rows) break;
+                    const float4 m4 = *reinterpret_cast<const float4*>(&row_ref[r0 + k]);
+                    float x[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int r = u * 8 + 2 * k;
-                        const float x0 = ex2(t[r] - m[2 * k]), x1 = ex2(t[r + 1] - m[2 * k + 1]);
+                    for (int y = 0; y < 4; ++y) {
+                        x[y] = ex2(t[k + y] - (&m4.x)[y]);
                         if constexpr (kQuant) {  // a hidden key's scale may be NaN
-                            if (there && r0 + r >= hidden) l[r0 + r] = fmaf(x0, ivs, l[r0 + r]);
-                            if (there && r0 + r + 1 >= hidden) l[r0 + r + 1] = fmaf(x1, ivs, l[r0 + r + 1]);
+                            if (there && r0 + k + y >= hidden) l[r0 + k + y] = fmaf(x[y], ivs, l[r0 + k + y]);
                         } else {
-                            l[r0 + r] += x0;
-                            l[r0 + r + 1] += x1;
+                            l[r0 + k + y] += x[y];
                         }
-                        p[k] = pack2<M>(x0, x1);
                     }
-                    *reinterpret_cast<uint4*>(to + (((r0 / 8 + u) ^ (((tid * RB) >> 7) & (RB / 16 - 1))) << 4)) = make_uint4(p[0], p[1], p[2], p[3]);
+                    const int u = (r0 + k) / 8;
+                    *reinterpret_cast<uint2*>(to + ((u ^ (((tid * RB) >> 7) & (RB / 16 - 1))) << 4) + ((k & 4) << 1)) =
+                        make_uint2(pack2<M>(x[0], x[1]), pack2<M>(x[2], x[3]));
                 }
             }
             fence_async_proxy();
@@ -418,6 +426,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
         // the sums of the weights, over the warp and then over the four
 #pragma unroll
         for (int r0 = 0; r0 < NR; r0 += 16) {
+            if (r0 >= live_rows) break;
             const float sum = warp_sums16(&l[r0], lane);
             if ((lane & 1) == 0) row_sum[warp][r0 + (lane >> 1)] = sum;
         }
@@ -437,40 +446,34 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
                 else if (a.lse) a.lse[at] = lse * 0.69314718055994531f;
             }
             // a part that saw no key is not read by the merge, the result of a call is zero
+            // (a padding row is neither)
             row_c[tid] = !write || (empty && !direct) ? -1.f : empty ? 0.f : 1.0f / total;
         }
         sync_128();
         const bool fix = !PREFIX && *reinterpret_cast<volatile int*>(&poisoned) != 0;
-#pragma unroll
-        for (int r0 = 0; r0 < NR; r0 += 16) {
-#pragma unroll
-            for (int i = 0; i < NI; ++i) {
+#pragma unroll 1
+        for (int i = 0; i < NI; ++i) {
+            const int d = i * 128 + tid;
+            const bool mine = d < a.dim && (DI == 128 || tid < DI);
+#pragma unroll 1
+            for (int r0 = 0; r0 < live_rows; r0 += 16) {
                 uint32_t o[16];
                 tmem_load16(tmem_o + lanes + i * NR + r0, o);
                 tmem_wait_load(o);
-                const int d = i * 128 + tid;
-                const bool mine = d < a.dim && (DI == 128 || tid < DI);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float inv = row_c[r0 + r];
-                    o[r] = inv == 0.f ? 0u : __float_as_uint(__uint_as_float(o[r]) * inv);
-                }
-                if (fix && mine) {
-#pragma unroll 1
-                    for (int r = 0; r < 16; ++r) {
-                        const float e = hidden_poison_of<T, FMT>(a, pages, list_len, kv_head, d, max(k0, all_see), min(k1, len - a.q_len + (row0 + r0 + r) / a.group + 1));
+                for (int k = 0; k < 16; k += 4) {
+                    if (r0 + k >= live_rows) break;
+                    const float4 f4 = *reinterpret_cast<const float4*>(&row_c[r0 + k]);
 #pragma unroll
-                        for (int x = 0; x < 16; ++x)
-                            if (x == r) o[x] = __float_as_uint(__uint_as_float(o[x]) + e);
-                    }
-                }
-                if (mine) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        if (row_c[r0 + r] == -1.f) continue;  // (a NaN row is written)
-                        const long long at = row_at[r0 + r];
-                        if (direct) reinterpret_cast<unsigned short*>(a.out)[at * a.dim + d] = (unsigned short)Codec<T, 16>::from_float16(__uint_as_float(o[r]));
-                        else a.part_out[((long long)part_index * all_rows + at) * a.dim + d] = __uint_as_float(o[r]);
+                    for (int y = 0; y < 4; ++y) {
+                        const int r = r0 + k + y;
+                        const float f = (&f4.x)[y];
+                        if (f == -1.f || !mine) continue;  // (a NaN row is written)
+                        float x = f == 0.f ? 0.f : __uint_as_float(o[k + y]) * f;
+                        if (fix) x += hidden_poison_of<T, FMT>(a, pages, list_len, kv_head, d, max(k0, all_see), min(k1, len - a.q_len + (row0 + r) / a.group + 1));
+                        const long long at = row_at[r];
+                        if (direct) reinterpret_cast<unsigned short*>(a.out)[at * a.dim + d] = (unsigned short)Codec<T, 16>::from_float16(x);
+                        else a.part_out[((long long)part_index * all_rows + at) * a.dim + d] = x;
                     }
                 }
             }
@@ -645,7 +648,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
             }
         }
         // the tensor memory is given back only when nothing writes it any more
-        ok = mbarrier_wait_bounded(&o_done[(n - 1) & 1], ((n - 1) >> 1) & 1) && ok;
+        ok = mbarrier_wait_sleeping(&o_done[(n - 1) & 1], ((n - 1) >> 1) & 1) && ok;
     }
     if (!ok) atomicExch(a.status, kDeviceTimeoutCode);
     tc_fence_before();

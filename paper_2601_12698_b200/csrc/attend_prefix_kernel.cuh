@@ -38,7 +38,7 @@ namespace rt {
 
 constexpr int kTcThreads = 512;
 constexpr int kTcSlots = 4;   // ring of key and value tiles
-constexpr int kTcAux = 4;     // tiles whose places and constants are kept: the two under way and two ahead
+constexpr int kTcAux = 8;     // tiles whose places and constants are kept: the two under way and two ahead
 
 template <int FMT, int DP>
 struct PrefixShape {
@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
     // barrier is still met and the tensor memory is given back; the status word says that the results are not valid.
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-        if (ok) ok = mbarrier_wait_bounded(bar, parity);
+        if (ok) ok = mbarrier_wait_sleeping(bar, parity);
     };
 
     if (warp < 8) {
@@ -504,7 +504,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
             // the tensor memory is given back only when nothing writes it any more
             if (elect_one()) tc_commit(&drained);
             __syncwarp();
-            ok = mbarrier_wait_bounded(&drained, 0) && ok;
+            ok = mbarrier_wait_sleeping(&drained, 0) && ok;
         } else if (warp >= 14) {
             // Places of the tiles' keys and what the softmax wants to know of them, two keys to a thread, up to kTcAux tiles ahead.
             // A tile's page numbers are read while the tile before it is published.

@@ -117,6 +117,26 @@ __device__ __forceinline__ constexpr uint32_t tc_instruction(int n, bool a_rows,
            ((128u >> 4) << 24);
 }
 
+// Bounded wait whose polls sleep in hardware for up to kWaitSleepNs each: many roles wait most of the time, and warps that poll
+// without pause take a third of the issue slots from those that work.  Gives up after about a second, as mbarrier_wait_bounded.
+constexpr uint32_t kWaitSleepNs = 20000;
+__device__ __forceinline__ bool mbarrier_wait_sleeping(uint64_t* bar, uint32_t parity)
+{
+    const uint32_t addr = smem_u32(bar);
+    long long t0 = 0;
+    for (unsigned it = 0;; ++it) {
+        uint32_t done;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done) : "r"(addr), "r"(parity), "r"(kWaitSleepNs) : "memory");
+        if (done) return true;
+        if (it == 0) t0 = clock64();
+        if (it >= kMbarrierPollLimit || clock64() - t0 > kMbarrierCycleLimit) return false;
+    }
+}
+
 __device__ __forceinline__ void mbarrier_arrive(uint64_t* bar)
 {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
@@ -163,10 +183,13 @@ struct CodePieces {
 template <int FMT>
 __device__ __forceinline__ void store_codes(unsigned char* lo, unsigned char* hi, const uint4& x)
 {
-    *reinterpret_cast<uint4*>(lo) =
-        make_uint4(pick_half2<FMT, 0, 1>(x.x, x.x), pick_half2<FMT, 2, 3>(x.x, x.x), pick_half2<FMT, 0, 1>(x.y, x.y), pick_half2<FMT, 2, 3>(x.y, x.y));
-    *reinterpret_cast<uint4*>(hi) =
-        make_uint4(pick_half2<FMT, 0, 1>(x.z, x.z), pick_half2<FMT, 2, 3>(x.z, x.z), pick_half2<FMT, 0, 1>(x.w, x.w), pick_half2<FMT, 2, 3>(x.w, x.w));
+    uint4 a, b;
+    codes_to_half4<FMT>(x.x, a.x, a.y);
+    codes_to_half4<FMT>(x.y, a.z, a.w);
+    codes_to_half4<FMT>(x.z, b.x, b.y);
+    codes_to_half4<FMT>(x.w, b.z, b.w);
+    *reinterpret_cast<uint4*>(lo) = a;
+    *reinterpret_cast<uint4*>(hi) = b;
 }
 
 }  // namespace rt
