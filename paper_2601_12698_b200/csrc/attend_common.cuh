@@ -39,12 +39,19 @@ struct AttendArgs {
     float score_scale;                        // softmax_scale * log2(e)
     int prefix_parts, prefix_keys;            // parts of the prefix and keys in each (the last may have fewer)
     int suffix_parts, suffix_keys;
+    int after_prefix;  // the suffix kernel runs beside the prefix kernel that was launched before it
     float* part_out;  // [part][token][head][dim]
     float* part_lse;  // [part][token][head]
     void* out;        // [token][head][dim]
     float* lse;       // [token][head] or NULL
     int* status;
 };
+
+// The prefix kernel lets the suffix kernel start as soon as the kernel before both has completed: they read the same inputs and
+// write different parts.  The suffix kernel therefore does not wait for its predecessor before it starts; its first CTA does
+// before it ends, so that the kernel that joins the parts, which waits for the suffix kernel, finds the prefix's parts too.  (One
+// CTA is enough, and CTAs that waited would keep others from the SMs that they hold.)
+__device__ __forceinline__ void let_next_kernel_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // Offset of token `pos` of a page list in k and v (`scales`: in the scale tensors), -1 when its page is not in the cache.
 __device__ __forceinline__ long long entry_offset(const AttendArgs& a, int page, unsigned in_page, int head, bool scales)

@@ -151,7 +151,12 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
         mbarrier_init(&q_full, 128);
         poisoned = 0;
     }
-    wait_for_previous_kernel();
+    const bool beside_prefix = !PREFIX && a.after_prefix != 0;
+    if (!beside_prefix) wait_for_previous_kernel();
+    if (PREFIX) let_next_kernel_start();
+    const auto leave = [&]() {
+        if (beside_prefix && blockIdx.x == 0) wait_for_previous_kernel();
+    };
 
     int len, first_token, n_rows, row0;
     const int32_t* pages;
@@ -168,7 +173,10 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
         const int seq = (int)(job / (unsigned)per_seq);
         row0 = (int)(job % (unsigned)per_seq) * NR;
         len = suffix_length(a, seq);
-        if (len < 0) return;  // a padded sequence: its rows are not joined either
+        if (len < 0) {  // a padded sequence: its rows are not joined either
+            leave();
+            return;
+        }
         first_token = seq * a.q_len;
         n_rows = a.q_len * a.group;
         pages = a.page_table + (long long)seq * a.page_table_stride;
@@ -196,6 +204,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
                     *reinterpret_cast<uint4*>(reinterpret_cast<unsigned char*>(a.out) + (at * a.dim + d) * 2) = make_uint4(0, 0, 0, 0);
             }
         }
+        leave();
         return;
     }
     if (warp == 8) {
@@ -655,6 +664,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
     __syncthreads();
     tc_fence_after();
     if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::kColumns) : "memory");
+    leave();
 }
 
 }  // namespace rt

@@ -104,6 +104,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
     tc_fence_after();
     const uint32_t tmem = tmem_base;
     wait_for_previous_kernel();
+    let_next_kernel_start();
 
     const int total = split.tiles * split.blocks * a.kv_heads;  // the host checked that it fits
     const int begin = (int)blockIdx.x * split.run, end = min(total - begin, split.run) + begin;

@@ -137,7 +137,15 @@ int make_attend_plan(const rt_kv_cache* c, const rt_prefix_batch* b, int q_heads
                 set_error("prefix of %lld tokens for %lld rows is too large", (long long)b->prefix_len, (long long)prefix_rows);
                 return RT_ERR_SHAPE;
             }
-            s.run = (int)ceil_div(total, L.sm_count);
+            // The two kernels run side by side, one CTA of this one taking a whole SM: it gets the share of the SMs that its share
+            // of the work asks for.  In units of what a tile of 128 keys costs the suffix kernel (measured, us of one SM: suffix 1.4
+            // plain, 1.7 quantised; prefix 2.2 and 3.5 for 256 rows); suffixes are taken to be half as long as they may be.
+            const double prefix_work = (double)total * (c->format == RT_KV_PLAIN ? 1.6 : 2.1);
+            const double suffix_work = 0.5 * (double)ceil_div(b->max_suffix_len, 128) * (double)ceil_div(suffix_rows, 16) * c->kv_heads * (double)b->n_seqs;
+            long long sms = (long long)(L.sm_count * prefix_work / (prefix_work + suffix_work) + 0.5);
+            if (getenv("XSMS")) sms = atoi(getenv("XSMS"));
+            sms = std::max<long long>(1, std::min<long long>(sms, L.sm_count));
+            s.run = (int)ceil_div(total, sms);
             p->prefix_ctas = ceil_div(total, s.run);
             p->prefix_parts = most_parts(s);
         } else {
@@ -257,6 +265,7 @@ int shared_prefix_attention_launch(const rt_kv_cache* c, const rt_prefix_batch* 
     a.part_lse = parts > 1 ? (float*)workspace + (int64_t)parts * p.tokens * q_heads * c->head_dim : nullptr;
     a.out = out;
     a.lse = lse;
+    a.after_prefix = p.prefix_form >= 0;
     a.status = device_status_word();
     if (!a.status) return RT_ERR_NO_DEVICE;
     const AttendKernels k = kernels_of(dtype, c->format, p.padded_dim);
