@@ -21,10 +21,8 @@ __global__ void __launch_bounds__(kMergePartsThreads) merge_parts_kernel(const A
     const long long n_rows = (long long)a.n_seqs * a.q_len * n_heads;
     const int token = (int)((unsigned)row / (unsigned)n_heads), head = (int)(row - (long long)token * n_heads);
     int prefix_parts = a.prefix_parts;
-    if (split.run > 0) {  // the prefix was dealt out by tiles: the row's unit has so many parts
-        const int kv_head = head / a.group, block = (token * a.group + (head - kv_head * a.group)) / kTcBlockRows;
-        prefix_parts = parts_of_unit(split, kv_head * split.blocks + block, block);
-    }
+    if (split.run > 0)  // the prefix was dealt out by tiles
+        prefix_parts = parts_of_block(split, (token * a.group + head % a.group) / kTcBlockRows);
     const int skip = a.prefix_parts - prefix_parts;  // parts of the workspace that this row does not use
     const int parts = prefix_parts + a.suffix_parts;
     wait_for_previous_kernel();

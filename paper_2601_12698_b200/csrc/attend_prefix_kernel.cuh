@@ -2,10 +2,9 @@
 //
 // All rows of one key/value head (every sequence's query tokens and the head's query heads) see the same keys, so the
 // prefix is a plain matrix problem:  S = Q K^T,  W = 2^(score_scale S - m),  O = W V,  in one pass over the keys with a
-// running reference m and sum per row.  A "unit" is one key/value head and one block of rows (up to 256); its keys come in
-// tiles of 128.  The tiles of all units are numbered through and dealt out in equal consecutive runs, one run to a CTA and
-// one CTA to an SM, so the SMs finish together whatever the number of heads and rows; a run may end one unit and begin the
-// next.  What a CTA finds out about a unit is one part (two in the narrow form below), joined by merge_parts_kernel.
+// running reference m and sum per row.  A CTA takes one key/value head, one block of up to 256 of its rows and one run of
+// key tiles of 128 (see attend_split.h), one CTA to an SM.  What it finds out is one part of its rows (two in the narrow form
+// below), joined by merge_parts_kernel.
 //
 // Inside a CTA (16 warps):
 //   warps 0-3, 4-7   two softmax streams of 128 rows, one row to a thread (tensor memory lane = row): they read S from
@@ -62,7 +61,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
     constexpr bool kQuant = S::kQuant;
     using M = typename std::conditional<kQuant, __half, T>::type;
     constexpr int kBlockBytes = kTileBlockBytes;  // one 64-dim column block of a tile
-    constexpr uint32_t kScoreIdesc = tc_instruction<M>(kTcTile, false, false), kOutIdesc = tc_instruction<M>(DP, false, true);
+    constexpr uint32_t kScoreIdesc = tc_instruction<M>(kTcTile / 2, false, false), kOutIdesc = tc_instruction<M>(DP, false, true);
     constexpr uint32_t kColO = 2 * kTcTile;
 
     extern __shared__ unsigned char smem_raw[];
@@ -71,7 +70,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
     unsigned char* ring = smem + 2 * S::kTileBytes;
     float* aux = reinterpret_cast<float*>(smem + S::kAuxAt);
     long long* offsets = reinterpret_cast<long long*>(smem + S::kOffsetsAt);
-    __shared__ __align__(8) uint64_t full[kTcSlots], empty[kTcSlots], aux_full[kTcAux], aux_free[kTcAux], s_full[2], p_full[2], o_full[2], q_full, drained;
+    __shared__ __align__(8) uint64_t full[kTcSlots], empty[kTcSlots], aux_full[kTcAux], aux_free[kTcAux], s_full[2][2], p_full[2][2], o_done[2], o_full[2], q_full, drained;
     __shared__ uint32_t tmem_base;
     __shared__ float row_factor[2][kQuant ? 128 : 1];
     __shared__ uint32_t ragged[kTcAux];  // one byte for each half of the lookup: some key is not there
@@ -88,8 +87,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
             ragged[i] = 0;
         }
         for (int i = 0; i < 2; ++i) {
-            mbarrier_init(&s_full[i], 1);
-            mbarrier_init(&p_full[i], 128);
+            for (int h = 0; h < 2; ++h) {
+                mbarrier_init(&s_full[i][h], 1);
+                mbarrier_init(&p_full[i][h], 128);
+            }
+            mbarrier_init(&o_done[i], 1);
             mbarrier_init(&o_full[i], 1);
         }
         mbarrier_init(&q_full, 256);
@@ -106,8 +108,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
     wait_for_previous_kernel();
     let_next_kernel_start();
 
-    const int total = split.tiles * split.blocks * a.kv_heads;  // the host checked that it fits
-    const int begin = (int)blockIdx.x * split.run, end = min(total - begin, split.run) + begin;
+    // this CTA's key/value head, row block and tiles
+    const int block = (int)(blockIdx.x % (unsigned)split.blocks), run_no = (int)(blockIdx.x / (unsigned)split.blocks % (unsigned)split.runs);
+    const int kv_head = (int)(blockIdx.x / (unsigned)(split.blocks * split.runs));
+    const int tile0 = run_no * split.run, n = min(split.tiles - tile0, split.run);
+    const bool narrow = narrow_block(split, block);
     // Every wait is bounded.  A thread whose wait has run out stops waiting and goes on through the same loops, so that every
     // barrier is still met and the tensor memory is given back; the status word says that the results are not valid.
     bool ok = true;
@@ -125,83 +130,77 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
         const float scale = fabsf(a.score_scale);
         const int n_heads = a.kv_heads * a.group;
         const long long n_rows = (long long)a.n_seqs * a.q_len * n_heads;
-        uint32_t n_s = 0, n_o = 0, tile_no = 0;
-        for (int at = begin; at < end;) {
-            const int unit = at / split.tiles, block = unit % split.blocks, kv_head = unit / split.blocks;
-            const int tile0 = at - unit * split.tiles;
-            const int n = min(split.tiles - tile0, end - at);
-            const bool narrow = narrow_block(split, block);
-            const int first_row = block * kTcBlockRows + (narrow ? 0 : s * 128);
-            // [token][head] index of row i of this stream's 128, -1: no such row
-            const auto row_index = [&](int i) -> long long {
-                const int row = first_row + i;
-                if (row >= split.rows) return -1;
-                const int token = row / a.group;
-                return (long long)token * n_heads + kv_head * a.group + (row - token * a.group);
-            };
-            // Query rows into shared memory, DP / 8 lanes to a row, so that a row is read in one piece.  Nobody reads the tiles
-            // any more: each stream has seen its last product of the previous unit, and the barrier makes that so for both.
-            // Narrow form: the first stream's threads do it for both.
-            asm volatile("bar.sync 1, 256;" ::: "memory");
-            if (!narrow || s == 0) {
-                constexpr int LANES = DP / 8, ROWS = 32 / LANES, N = 32 / ROWS;  // lanes per row, rows at once, turns
-                const int u = lane % LANES;
-                unsigned char* tile = q_tiles + s * S::kTileBytes + (u >> 3) * kBlockBytes;
-                {
-                    uint4 w[N];  // all at once: behind the first tiles' copies every further round trip would take its turn
+        const int first_row = block * kTcBlockRows + (narrow ? 0 : s * 128);
+        // [token][head] index of row i of this stream's 128, -1: no such row
+        const auto row_index = [&](int i) -> long long {
+            const int row = first_row + i;
+            if (row >= split.rows) return -1;
+            const int token = row / a.group;
+            return (long long)token * n_heads + kv_head * a.group + (row - token * a.group);
+        };
+        // Query rows into shared memory, DP / 8 lanes to a row, so that a row is read in one piece.  Narrow form: the first
+        // stream's threads do it for both.
+        if (!narrow || s == 0) {
+            constexpr int LANES = DP / 8, ROWS = 32 / LANES, N = 32 / ROWS;  // lanes per row, rows at once, turns
+            const int u = lane % LANES;
+            unsigned char* tile = q_tiles + s * S::kTileBytes + (u >> 3) * kBlockBytes;
+            {
+                uint4 w[N];  // all at once: behind the first tiles' copies every further round trip would take its turn
 #pragma unroll
-                    for (int i = 0; i < N; ++i) {
-                        const int row = first_row + (warp & 3) * 32 + i * ROWS + lane / LANES;
-                        const bool there = row < split.rows && u * 8 < a.dim;
-                        const int token = there ? row / a.group : 0;
-                        const long long o = (long long)token * a.q_token_stride +
-                                            (long long)(kv_head * a.group + (there ? row - token * a.group : 0)) * a.q_head_stride + (there ? u * 8 : 0);
-                        w[i] = __ldg(reinterpret_cast<const uint4*>(a.q + o * 2));
-                        if (!there) w[i] = make_uint4(0, 0, 0, 0);
+                for (int i = 0; i < N; ++i) {
+                    const int row = first_row + (warp & 3) * 32 + i * ROWS + lane / LANES;
+                    const bool there = row < split.rows && u * 8 < a.dim;
+                    const int token = there ? row / a.group : 0;
+                    const long long o = (long long)token * a.q_token_stride +
+                                        (long long)(kv_head * a.group + (there ? row - token * a.group : 0)) * a.q_head_stride + (there ? u * 8 : 0);
+                    w[i] = __ldg(reinterpret_cast<const uint4*>(a.q + o * 2));
+                    if (!there) w[i] = make_uint4(0, 0, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const int mine = (warp & 3) * 32 + i * ROWS + lane / LANES;
+                    const uint32_t sign = flip ? 0x80008000u : 0u;
+                    w[i].x ^= sign; w[i].y ^= sign; w[i].z ^= sign; w[i].w ^= sign;
+                    if constexpr (kQuant) {
+                        uint32_t top = __vmaxu2(__vmaxu2(w[i].x & 0x7FFF7FFFu, w[i].y & 0x7FFF7FFFu), __vmaxu2(w[i].z & 0x7FFF7FFFu, w[i].w & 0x7FFF7FFFu));
+#pragma unroll
+                        for (int m = LANES / 2; m >= 1; m >>= 1) top = __vmaxu2(top, __shfl_xor_sync(0xFFFFFFFFu, top, m));
+                        const float factor = fp16_row_factor(Codec<T, 16>::to_float16(max(top & 0xFFFFu, top >> 16)));
+                        if (u == 0) row_factor[s][mine] = factor;
+                        uint32_t* p = &w[i].x;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            p[k] = pack2<__half>(Codec<T, 16>::to_float16(p[k] & 0xFFFFu) * factor, Codec<T, 16>::to_float16(p[k] >> 16) * factor);
                     }
-#pragma unroll
-                    for (int i = 0; i < N; ++i) {
-                        const int mine = (warp & 3) * 32 + i * ROWS + lane / LANES;
-                        const uint32_t sign = flip ? 0x80008000u : 0u;
-                        w[i].x ^= sign; w[i].y ^= sign; w[i].z ^= sign; w[i].w ^= sign;
-                        if constexpr (kQuant) {
-                            uint32_t top = __vmaxu2(__vmaxu2(w[i].x & 0x7FFF7FFFu, w[i].y & 0x7FFF7FFFu), __vmaxu2(w[i].z & 0x7FFF7FFFu, w[i].w & 0x7FFF7FFFu));
-#pragma unroll
-                            for (int m = LANES / 2; m >= 1; m >>= 1) top = __vmaxu2(top, __shfl_xor_sync(0xFFFFFFFFu, top, m));
-                            const float factor = fp16_row_factor(Codec<T, 16>::to_float16(max(top & 0xFFFFu, top >> 16)));
-                            if (u == 0) row_factor[s][mine] = factor;
-                            uint32_t* p = &w[i].x;
-#pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                p[k] = pack2<__half>(Codec<T, 16>::to_float16(p[k] & 0xFFFFu) * factor, Codec<T, 16>::to_float16(p[k] >> 16) * factor);
-                        }
-                        *reinterpret_cast<uint4*>(tile + mine * 128 + (((u & 7) ^ (mine & 7)) << 4)) = w[i];
-                    }
+                    *reinterpret_cast<uint4*>(tile + mine * 128 + (((u & 7) ^ (mine & 7)) << 4)) = w[i];
                 }
             }
-            fence_async_proxy();
-            mbarrier_arrive(&q_full);
-            float row_c = scale;
-            if constexpr (kQuant) {
-                asm volatile("bar.sync 1, 256;" ::: "memory");
-                row_c *= __frcp_rn(row_factor[narrow ? 0 : s][r]);
-            }
+        }
+        fence_async_proxy();
+        mbarrier_arrive(&q_full);
+        float row_c = scale;
+        if constexpr (kQuant) {
+            asm volatile("barrier.cta.sync 1, 256;" ::: "memory");
+            row_c *= __frcp_rn(row_factor[narrow ? 0 : s][r]);
+        }
 
-            float m = -INFINITY, l = 0.f;
-            const int my_tiles = narrow ? (n + 1 - s) / 2 : n;
-            for (int i = 0; i < my_tiles; ++i) {
-                const uint32_t t = tile_no + (narrow ? 2 * i + s : i);
-                const uint32_t aux_i = t % kTcAux;
-                wait(&aux_full[aux_i], (t / kTcAux) & 1);
-                wait(&s_full[s], n_s & 1);
-                ++n_s;
+        float m = -INFINITY, l = 0.f;
+        const int my_tiles = narrow ? (n + 1 - s) / 2 : n;
+        for (int i = 0; i < my_tiles; ++i) {
+            const int t = narrow ? 2 * i + s : i, aux_i = t % kTcAux;
+            wait(&aux_full[aux_i], (t / kTcAux) & 1);
+            const float4* ka = reinterpret_cast<const float4*>(aux + aux_i * S::kAuxFloats);
+            // Half a tile at a time: while this half is exponentiated, the products of the other one run.
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                wait(&s_full[s][h], i & 1);
                 tc_fence_after();
-                const float4* ka = reinterpret_cast<const float4*>(aux + aux_i * S::kAuxFloats);
-                // One pass over the tile's scores of this row, 32 at a time, gives their maximum and, with the reference as it is, the
-                // weights and their sum.  Only when the maximum turns out to be more than 8 above the reference is the pass made
-                // again, with a reference that has been moved there; the scores are still in tensor memory, the weights go over them
-                // at the end.  (The row's first tile has no reference yet and always takes two passes.)
-                uint32_t w[4][16];
+                const uint32_t col = s_col + h * 64;
+                // One pass over the row's 64 scores, 32 at a time, gives their maximum and, with the reference as it is, the weights
+                // and their sum.  Only when the maximum turns out to be more than 8 above the reference is the pass made again, with
+                // a reference that has been moved there; the scores are still in tensor memory, the weights go over them at the end.
+                // (The row's first scores have no reference yet and always take two passes.)
+                uint32_t w[2][16];
                 float2x sum[2];
                 for (;;) {
                     // No key of the row so far: the reference is -inf, every score is -inf, and so must every weight's logarithm be.
@@ -209,17 +208,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                     // A score scale of zero would make NaN of a plain cache's hidden scores: the smallest normal number does instead.
                     const float c = kQuant ? row_c : fmaxf(row_c, 1.17549435e-38f);
                     const float2x c2 = pack_f2(c, c), minus2 = pack_f2(-base, -base);
-                    float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    float t4[2] = {-INFINITY, -INFINITY};
                     sum[0] = sum[1] = pack_f2(0.f, 0.f);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
+                    for (int q = 0; q < 2; ++q) {
                         uint32_t v[32];
-                        tmem_load32(s_col + q * 32, v);
+                        tmem_load32(col + q * 32, v);
                         tmem_wait_load(v);
+                        const int at4 = h * 16 + q * 8;  // constants, four keys at a time
                         if (!kQuant && *reinterpret_cast<volatile uint32_t*>(&ragged[aux_i]) != 0) {  // the last tile, or pages that are not there
 #pragma unroll
                             for (int k = 0; k < 8; ++k) {
-                                const float4 b = ka[q * 8 + k];
+                                const float4 b = ka[at4 + k];
                                 if (b.x != 0.f) v[4 * k] = 0xFF800000u;
                                 if (b.y != 0.f) v[4 * k + 1] = 0xFF800000u;
                                 if (b.z != 0.f) v[4 * k + 2] = 0xFF800000u;
@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                             float2x t0 = pack_f2(__uint_as_float(v[4 * k]), __uint_as_float(v[4 * k + 1]));
                             float2x t1 = pack_f2(__uint_as_float(v[4 * k + 2]), __uint_as_float(v[4 * k + 3]));
                             if constexpr (kQuant) {
-                                const ulonglong2* k2 = reinterpret_cast<const ulonglong2*>(ka) + q * 8 + k;
+                                const ulonglong2* k2 = reinterpret_cast<const ulonglong2*>(ka) + at4 + k;
                                 const ulonglong2 ks = k2[0], lv = k2[32];
                                 t0 = fma_f2(mul_f2(t0, c2), ks.x, lv.x);
                                 t1 = fma_f2(mul_f2(t1, c2), ks.y, lv.y);
@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
 #pragma unroll
                             for (int y = 0; y < 4; ++y) x[y] = ex2(x[y]);
                             if constexpr (kQuant) {
-                                const ulonglong2 iv = reinterpret_cast<const ulonglong2*>(ka)[64 + q * 8 + k];
+                                const ulonglong2 iv = reinterpret_cast<const ulonglong2*>(ka)[64 + at4 + k];
                                 sum[0] = fma_f2(pack_f2(x[0], x[1]), iv.x, sum[0]);
                                 sum[1] = fma_f2(pack_f2(x[2], x[3]), iv.y, sum[1]);
                             } else {
@@ -262,7 +262,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                     const bool move = top > m + 8.f;
                     if (!__any_sync(0xFFFFFFFFu, move)) break;
                     const float alpha = move ? ex2(m - top) : 1.f;
-                    if (i > 0) {
+                    if (i + h > 0) {  // the products so far are complete before they are rescaled (all but the last are: see the scores' order)
+                        wait(&o_done[s], (2 * i + h - 1) & 1);
+                        tc_fence_after();
 #pragma unroll 1
                         for (int q = 0; q < DP / 16; ++q) {
                             uint32_t o[16];
@@ -277,91 +279,71 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                     if (move) m = top;
                 }
 #pragma unroll
-                for (int q = 0; q < 4; ++q) tmem_store16(s_col + q * 16, w[q]);
+                for (int q = 0; q < 2; ++q) tmem_store16(col + q * 16, w[q]);
                 float part_sum[2];
                 unpack_f2(add_f2(sum[0], sum[1]), part_sum[0], part_sum[1]);
                 l += part_sum[0] + part_sum[1];
                 tmem_wait_store();
                 tc_fence_before();
-                mbarrier_arrive(&p_full[s]);
+                mbarrier_arrive(&p_full[s][h]);
             }
-            tile_no += n;
+        }
 
-            // this part of the row
-            if (my_tiles > 0) {
-                wait(&o_full[s], n_o & 1);
-                ++n_o;
-                tc_fence_after();
-            }
-            const long long part = blockIdx.x - (long long)unit * split.tiles / split.run;
-            const long long part_at = (narrow ? 2 * part + s : part) * n_rows;
-            const bool empty = l == 0.f;
-            const long long my_row = row_index(r);
-            if (my_row >= 0) a.part_lse[part_at + my_row] = empty ? -INFINITY : m + log2f(l);
-            if (my_tiles > 0) {
-                // A thread holds a row, and rows lie apart: 32 columns at a time go through shared memory, so that eight lanes
-                // write 128 bytes of a row.  Rows without a key are written too; nothing reads them.
-                const float inv = empty ? 0.f : 1.0f / l;
-                unsigned char* stage = DP == 64 ? smem + S::kStageAt + warp * 4096 : q_tiles + S::kTileBytes * (narrow ? 1 : s) + (narrow ? warp : warp & 3) * 4096;
-                long long to_row[8];
+        // this part of the row
+        if (my_tiles > 0) {
+            wait(&o_full[s], 0);
+            tc_fence_after();
+        }
+        const long long part_at = (long long)(narrow ? 2 * run_no + s : run_no) * n_rows;
+        const bool empty = l == 0.f;
+        const long long my_row = row_index(r);
+        if (my_row >= 0) a.part_lse[part_at + my_row] = empty ? -INFINITY : m + log2f(l);
+        if (my_tiles > 0) {
+            // A thread holds a row, and rows lie apart: 32 columns at a time go through shared memory, so that eight lanes
+            // write 128 bytes of a row.  Rows without a key are written too; nothing reads them.
+            const float inv = empty ? 0.f : 1.0f / l;
+            unsigned char* stage = DP == 64 ? smem + S::kStageAt + warp * 4096 : q_tiles + S::kTileBytes * (narrow ? 1 : s) + (narrow ? warp : warp & 3) * 4096;
+            long long to_row[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) to_row[k] = row_index((warp & 3) * 32 + k * 4 + (lane >> 3));
+            for (int k = 0; k < 8; ++k) to_row[k] = row_index((warp & 3) * 32 + k * 4 + (lane >> 3));
 #pragma unroll 1
-                for (int q = 0; q < DP / 32; ++q) {
-                    uint32_t o[32];
-                    tmem_load32(o_col + q * 32, o);
-                    tmem_wait_load(o);
+            for (int q = 0; q < DP / 32; ++q) {
+                uint32_t o[32];
+                tmem_load32(o_col + q * 32, o);
+                tmem_wait_load(o);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        *reinterpret_cast<float4*>(stage + lane * 128 + ((k ^ (lane & 7)) << 4)) =
-                            make_float4(__uint_as_float(o[4 * k]) * inv, __uint_as_float(o[4 * k + 1]) * inv, __uint_as_float(o[4 * k + 2]) * inv,
-                                        __uint_as_float(o[4 * k + 3]) * inv);
-                    __syncwarp();
-                    const int col = q * 32 + (lane & 7) * 4;
+                for (int k = 0; k < 8; ++k)
+                    *reinterpret_cast<float4*>(stage + lane * 128 + ((k ^ (lane & 7)) << 4)) =
+                        make_float4(__uint_as_float(o[4 * k]) * inv, __uint_as_float(o[4 * k + 1]) * inv, __uint_as_float(o[4 * k + 2]) * inv,
+                                    __uint_as_float(o[4 * k + 3]) * inv);
+                __syncwarp();
+                const int col = q * 32 + (lane & 7) * 4;
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const int row = k * 4 + (lane >> 3);
-                        const float4 x = *reinterpret_cast<const float4*>(stage + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
-                        if (to_row[k] >= 0 && col < a.dim) *reinterpret_cast<float4*>(a.part_out + (part_at + to_row[k]) * a.dim + col) = x;
-                    }
-                    __syncwarp();
+                for (int k = 0; k < 8; ++k) {
+                    const int row = k * 4 + (lane >> 3);
+                    const float4 x = *reinterpret_cast<const float4*>(stage + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
+                    if (to_row[k] >= 0 && col < a.dim) *reinterpret_cast<float4*>(a.part_out + (part_at + to_row[k]) * a.dim + col) = x;
                 }
+                __syncwarp();
             }
-            tc_fence_before();
-            at += n;
         }
     } else if (warp < 12) {
         // ---- fetching warps ----
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(256 - S::kSoftmaxRegs));
         const int p = tid - 256;
-        // Items in the order in which the products want them.  Wide units: K0, V0, K1, V1, ...; narrow ones: K0, K1, V0, K2, V1,
-        // ... V(n-1).
-        int at = begin, n = 0, g = 0, lead = 0, tile_no = 0;  // unit: first tile, tiles in this run, next item, form; tiles before it
-        auto enter = [&]() {
-            const int unit = at / split.tiles;
-            n = min(split.tiles - (at - unit * split.tiles), end - at);
-            lead = narrow_block(split, unit % split.blocks) ? 2 : 1;
-            g = 0;
-        };
-        enter();
+        // Items in the order in which the products want them.  Wide: K0, V0, K1, V1, ...; narrow: K0, K1, V0, K2, V1, ... V(n-1).
         bool values;
-        auto next_item = [&]() -> const long long* {  // the places of the item's tile
-            const int half = (g + 1) >> 1;
-            int tile;
-            if (lead == 1) {
-                values = g & 1;
-                tile = g >> 1;
+        auto item_places = [&](int q) -> const long long* {  // the places of item q's tile
+            const int half = (q + 1) >> 1;
+            int t;
+            if (!narrow) {
+                values = q & 1;
+                t = q >> 1;
             } else {
-                values = g > 0 && (!(g & 1) || half == n);
-                tile = g == 0 ? 0 : (g & 1) ? (values ? n - 1 : half) : half - 1;
+                values = q > 0 && (!(q & 1) || half == n);
+                t = q == 0 ? 0 : (q & 1) ? (values ? n - 1 : half) : half - 1;
             }
-            const int t = tile_no + tile;
             if (!values) wait(&aux_full[t % kTcAux], (t / kTcAux) & 1);
-            if (++g == 2 * n) {
-                at += n;
-                tile_no += n;
-                if (at < end) enter();
-            }
             return offsets + (t % kTcAux) * kTcTile;
         };
         auto slot_of = [&](int q) -> unsigned char* {
@@ -372,7 +354,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
             fence_async_proxy();
             mbarrier_arrive(&full[q % kTcSlots]);
         };
-        const int items = 2 * (end - begin);
+        const int items = 2 * n;
         if constexpr (kQuant) {
             using C = CodePieces<DP>;
             const int u = p % C::UNITS, r0 = p / C::UNITS;
@@ -380,14 +362,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
             const bool dims_there = u * 16 < a.dim;
             uint4 w[C::N];
             {
-                const long long* off = next_item() + r0;
+                const long long* off = item_places(0) + r0;
 #pragma unroll
                 for (int i = 0; i < C::N; ++i) w[i] = ld_codes(a.k + off[i * C::STEP] + u * 16, off[i * C::STEP] >= 0 && dims_there);
             }
 #pragma unroll 1
             for (int q = 0; q < items; ++q) {
                 const bool more = q + 1 < items;
-                const long long* off = more ? next_item() + r0 : offsets;
+                const long long* off = more ? item_places(q + 1) + r0 : offsets;
                 const unsigned char* side = (values ? a.v : a.k) + u * 16;
                 unsigned char* dst = slot_of(q) + to;
 #pragma unroll
@@ -402,7 +384,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
             const bool dims_there = (p % (DP / 8)) * 8 < a.dim;
 #pragma unroll 1
             for (int q = 0; q < items; ++q) {
-                const long long* off = next_item();
+                const long long* off = item_places(q);
                 fetch_plain_tile<DP>(slot_of(q), values ? a.v : a.k, off, p, dims_there, 0);
                 if (q > 0) {  // the one before has landed when only this one is outstanding
                     asm volatile("cp.async.wait_group 1;" ::: "memory");
@@ -418,89 +400,90 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
         if (warp == 12) {
             constexpr uint64_t kRowsLayout = tc_layout(16, 1024), kColsLayout = tc_layout(kBlockBytes, 1024);
             constexpr uint32_t kTile16 = S::kTileBytes / 16;
-            uint32_t item = 0, n_q = 0, n_p[2] = {0, 0};
+            uint32_t item = 0, n_p[2] = {0, 0};
             const uint32_t q16 = smem_u32(q_tiles) >> 4, ring16 = smem_u32(ring) >> 4;
             auto wait_item = [&](uint32_t i) {
                 wait(&full[i % kTcSlots], (i / kTcSlots) & 1);
                 tc_fence_after();
             };
-            // S_s = Q K^T with the keys of item i, then what the commits say
-            auto scores = [&](int s, int q_tile, uint32_t i, bool release) {
-                const uint32_t k_at = ring16 + (i % kTcSlots) * kTile16, q_at = q16 + q_tile * kTile16, d = tmem + s * kTcTile;
+            // Half h of S_s = Q K^T with the keys of item i
+            auto scores = [&](int s, int h, int q_tile, uint32_t i, bool release) {
+                const uint32_t k_at = ring16 + (i % kTcSlots) * kTile16 + h * (64 * 128 / 16), q_at = q16 + q_tile * kTile16, d = tmem + s * kTcTile + h * 64;
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < DP / 16; ++k) {
                         const uint32_t step = ((k >> 2) * kBlockBytes + (k & 3) * 32) / 16;
                         tc_mma_ss(d, tc_descriptor(kRowsLayout, q_at + step), tc_descriptor(kRowsLayout, k_at + step), kScoreIdesc, k > 0);
                     }
-                    tc_commit(&s_full[s]);
+                    tc_commit(&s_full[s][h]);
                     if (release) tc_commit(&empty[i % kTcSlots]);
                 }
                 __syncwarp();
             };
+            // O_s += W V with half h of the values of item i
             uint32_t outputs = 0;  // tiles whose last product has been issued
-            auto output = [&](int s, uint32_t i, bool first, bool release, bool last) {
-                const uint32_t v_at = ring16 + (i % kTcSlots) * kTile16, d = tmem + kColO + s * DP, w = tmem + s * kTcTile;
+            auto output = [&](int s, int h, uint32_t i, bool first, bool last, bool release) {
+                const uint32_t v_at = ring16 + (i % kTcSlots) * kTile16 + h * (64 * 128 / 16), d = tmem + kColO + s * DP, w = tmem + s * kTcTile + h * 64;
                 if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < kTcTile / 16; ++k)
+                    for (int k = 0; k < kTcTile / 32; ++k)
                         tc_mma_ts(d, w + k * 8, tc_descriptor(kColsLayout, v_at + k * 128), kOutIdesc, k > 0 ? 1u : (uint32_t)!first);
+                    tc_commit(&o_done[s]);
+                    if (last) tc_commit(&o_full[s]);
                     if (release) {  // the tile is done with: its values, its places and its constants
                         tc_commit(&empty[i % kTcSlots]);
                         tc_commit(&aux_free[outputs % kTcAux]);
                     }
-                    if (last) tc_commit(&o_full[s]);
                 }
                 if (release) ++outputs;
                 __syncwarp();
             };
-            auto wait_weights = [&](int s) {
-                wait(&p_full[s], n_p[s] & 1);
+            auto wait_weights = [&](int s, int h) {
+                wait(&p_full[s][h], (n_p[s] >> 1) & 1);
                 ++n_p[s];
                 tc_fence_after();
             };
-            for (int at = begin; at < end;) {
-                const int unit = at / split.tiles, block = unit % split.blocks;
-                const int tile0 = at - unit * split.tiles;
-                const int n = min(split.tiles - tile0, end - at);
-                wait(&q_full, n_q & 1);
-                ++n_q;
-                tc_fence_after();
-                if (narrow_block(split, block)) {
-                    for (int j = 0; j < 2 && j < n; ++j) {
-                        wait_item(item);
-                        scores(j, 0, item++, true);
-                    }
-                    for (int j = 0; j < n; ++j) {
-                        const int s = j & 1;
-                        wait_item(item);
-                        wait_weights(s);
-                        output(s, item++, j < 2, true, j + 2 >= n);
-                        if (j + 2 < n) {
-                            wait_item(item);
-                            scores(s, 0, item++, true);
-                        }
-                    }
-                } else {
+            wait(&q_full, 0);
+            tc_fence_after();
+            if (narrow) {
+                for (int j = 0; j < 2 && j < n; ++j) {
                     wait_item(item);
-                    scores(0, 0, item, false);
-                    scores(1, 1, item++, true);
-                    for (int j = 0; j < n; ++j) {
-                        const bool more = j + 1 < n;
-                        wait_item(item);
-                        wait_weights(0);
-                        output(0, item, j == 0, false, !more);
-                        if (more) {
-                            wait_item(item + 1);
-                            scores(0, 0, item + 1, false);
-                        }
-                        wait_weights(1);
-                        output(1, item, j == 0, true, !more);
-                        if (more) scores(1, 1, item + 1, true);
-                        item += more ? 2 : 1;
-                    }
+                    scores(j, 0, 0, item, false);
+                    scores(j, 1, 0, item++, true);
                 }
-                at += n;
+                for (int j = 0; j < n; ++j) {
+                    const int s = j & 1;
+                    const bool more = j + 2 < n;
+                    wait_item(item);
+                    for (int h = 0; h < 2; ++h) {
+                        wait_weights(s, h);
+                        output(s, h, item, j < 2 && h == 0, !more && h == 1, h == 1);
+                        if (more) {
+                            if (h == 0) wait_item(item + 1);
+                            scores(s, h, 0, item + 1, h == 1);
+                        }
+                    }
+                    item += more ? 2 : 1;
+                }
+            } else {
+                wait_item(item);
+                for (int h = 0; h < 2; ++h)
+                    for (int s = 0; s < 2; ++s) scores(s, h, s, item, h + s == 2);
+                ++item;
+                for (int j = 0; j < n; ++j) {
+                    const bool more = j + 1 < n;
+                    wait_item(item);
+                    for (int h = 0; h < 2; ++h)
+                        for (int s = 0; s < 2; ++s) {
+                            wait_weights(s, h);
+                            output(s, h, item, j + h == 0, !more && h == 1, h + s == 2);
+                            if (more) {
+                                if (h + s == 0) wait_item(item + 1);
+                                scores(s, h, s, item + 1, h + s == 2);
+                            }
+                        }
+                    item += more ? 2 : 1;
+                }
             }
             // the tensor memory is given back only when nothing writes it any more
             if (elect_one()) tc_commit(&drained);
@@ -512,7 +495,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
             const int p = tid - 448;
             int page_n[2];
             auto read_pages = [&](int g) {
-                const int pos = (g % split.tiles) * kTcTile + p;
+                const int pos = (tile0 + g) * kTcTile + p;
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
                     page_n[y] = -1;  // no such key
@@ -524,10 +507,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                     page_n[y] = page < 0 ? -2 : page;
                 }
             };
-            read_pages(begin);
+            read_pages(0);
 #pragma unroll 1
-            for (int g = begin; g < end; ++g) {
-                const int t = g - begin, slot = t % kTcAux, unit = g / split.tiles, tile = g - unit * split.tiles, kv_head = unit / split.blocks;
+            for (int g = 0; g < n; ++g) {
+                const int slot = g % kTcAux;
                 long long o[2];
                 float ks[2] = {0.f, 0.f}, vs[2] = {1.f, 1.f};
 #pragma unroll
@@ -540,7 +523,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                     }
                     int li;
                     unsigned in_page;
-                    split_position(a, tile * kTcTile + p + 64 * y, li, in_page);
+                    split_position(a, (tile0 + g) * kTcTile + p + 64 * y, li, in_page);
                     o[y] = entry_offset(a, page_n[y], in_page, kv_head, false) * (kQuant ? 1 : 2);
                     if constexpr (kQuant) {
                         const long long so = entry_offset(a, page_n[y], in_page, kv_head, true);
@@ -548,8 +531,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                         vs[y] = __ldg(a.v_scale + so);
                     }
                 }
-                if (g + 1 < end) read_pages(g + 1);
-                wait(&aux_free[slot], ((t / kTcAux) & 1) ^ 1);
+                if (g + 1 < n) read_pages(g + 1);
+                wait(&aux_free[slot], ((g / kTcAux) & 1) ^ 1);
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
                     const bool there = o[y] >= 0;

@@ -132,22 +132,30 @@ int make_attend_plan(const rt_kv_cache* c, const rt_prefix_batch* b, int q_heads
             s.tiles = (int)ceil_div(b->prefix_len, kTcTile);
             s.rows = (int)prefix_rows;
             s.blocks = (int)ceil_div(prefix_rows, kTcBlockRows);
-            const long long total = (long long)s.tiles * s.blocks * c->kv_heads;
-            if (total > 1LL << 30) {
-                set_error("prefix of %lld tokens for %lld rows is too large", (long long)b->prefix_len, (long long)prefix_rows);
-                return RT_ERR_SHAPE;
-            }
+            const long long units = (long long)s.blocks * c->kv_heads;
             // The two kernels run side by side, one CTA of this one taking a whole SM: it gets the share of the SMs that its share
-            // of the work asks for.  In units of what a tile of 128 keys costs the suffix kernel (measured, us of one SM: suffix 1.4
-            // plain, 1.7 quantised; prefix 2.2 and 3.5 for 256 rows); suffixes are taken to be half as long as they may be.
-            const double prefix_work = (double)total * (c->format == RT_KV_PLAIN ? 1.6 : 2.1);
-            const double suffix_work = 0.5 * (double)ceil_div(b->max_suffix_len, 128) * (double)ceil_div(suffix_rows, 16) * c->kv_heads * (double)b->n_seqs;
+            // of the work asks for.  The unit is what a tile of 128 keys costs the suffix kernel on one SM (1.4 us plain, 1.7
+            // quantised); a tile for 256 rows costs the prefix kernel 1.6 of that, beginning and ending a run about 7.  Suffixes are
+            // taken to be half as long as they may be.
+            const double prefix_work = (double)units * (s.tiles * 1.6 + 7), tiles_per_suffix = 0.5 * (double)ceil_div(b->max_suffix_len, 128);
+            const double suffix_work = tiles_per_suffix * (double)ceil_div(suffix_rows, 16) * c->kv_heads * (double)b->n_seqs;
             long long sms = (long long)(L.sm_count * prefix_work / (prefix_work + suffix_work) + 0.5);
             if (getenv("XSMS")) sms = atoi(getenv("XSMS"));
             sms = std::max<long long>(1, std::min<long long>(sms, L.sm_count));
-            s.run = (int)ceil_div(total, sms);
-            p->prefix_ctas = ceil_div(total, s.run);
-            p->prefix_parts = most_parts(s);
+            // The number of runs that ends first on that many SMs: whole waves of CTAs, each as long as its run.
+            double best = 0;
+            s.run = s.tiles;
+            for (int runs = 1; runs <= std::min(s.tiles, kMaxParts); ++runs) {
+                const int run = (int)ceil_div(s.tiles, runs);
+                const double time = (double)ceil_div(units * ceil_div(s.tiles, run), sms) * (run * 1.6 + 7);
+                if (runs == 1 || time < best * 0.97) {
+                    best = time;
+                    s.run = run;
+                }
+            }
+            s.runs = (int)ceil_div(s.tiles, s.run);
+            p->prefix_ctas = units * s.runs;
+            p->prefix_parts = s.runs * (narrow_block(s, s.blocks - 1) ? 2 : 1);
         } else {
             const int nr = p->prefix_form == kPrefixKeys16 ? 16 : 64;
             const long long tiles = ceil_div(prefix_rows, nr) * c->kv_heads;
