@@ -131,7 +131,8 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
     __shared__ long long row_at[NR];  // [token][head] index of a row, -1: no such row
     __shared__ int poisoned;
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    // (the warp's number by shuffle: the compiler then knows that a role is taken by whole warps)
+    const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
     unsigned job = blockIdx.x;
     const int kv_head = (int)(job % (unsigned)a.kv_heads);
     job /= (unsigned)a.kv_heads;

@@ -13,7 +13,7 @@
 //   warps 8-11       fetch the paged tiles: keys and values with cp.async, 16 bytes a piece, into the 128-byte-swizzled
 //                    layout that the matrix unit reads (pages may have any size, so one copy per row is the widest that
 //                    always works); quantised tiles are fetched into registers, turned into fp16 and stored;
-//   warp 12          issues the matrix products;
+//   warps 12, 13     issue the matrix products, each for its stream;
 //   warps 14, 15     look up the pages and scales of the tiles to come.
 // The two streams take turns on the tensor cores: while one's scores are exponentiated the other's products run.  Blocks of
 // more than 128 rows (wide form): a stream is one half of the rows, both use the same tiles.  Blocks of up to 128 rows
@@ -43,7 +43,7 @@ template <int FMT, int DP>
 struct PrefixShape {
     static constexpr bool kQuant = FMT != kKvPlain;
     // Registers per softmax thread; half the threads are softmax threads, and the other half gets the rest of 2 * 128.
-    static constexpr int kSoftmaxRegs = 144;
+    static constexpr int kSoftmaxRegs = 136;
     static constexpr int kTileBytes = kTcTile * DP * 2;
     static constexpr int kAuxFloats = kQuant ? 3 * kTcTile : kTcTile;
     static constexpr size_t kAuxAt = (size_t)(2 + kTcSlots) * kTileBytes;
@@ -70,20 +70,21 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
     unsigned char* ring = smem + 2 * S::kTileBytes;
     float* aux = reinterpret_cast<float*>(smem + S::kAuxAt);
     long long* offsets = reinterpret_cast<long long*>(smem + S::kOffsetsAt);
-    __shared__ __align__(8) uint64_t full[kTcSlots], empty[kTcSlots], aux_full[kTcAux], aux_free[kTcAux], s_full[2][2], p_full[2][2], o_done[2], o_full[2], q_full, drained;
+    __shared__ __align__(8) uint64_t full[kTcSlots], empty[kTcSlots], aux_full[kTcAux], aux_free[kTcAux], s_full[2][2], p_full[2][2], o_done[2], o_full[2], q_full, drained[2];
     __shared__ uint32_t tmem_base;
     __shared__ float row_factor[2][kQuant ? 128 : 1];
     __shared__ uint32_t ragged[kTcAux];  // one byte for each half of the lookup: some key is not there
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    // (the warp's number by shuffle: the compiler then knows that a role is taken by whole warps)
+    const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
     if (tid == 0) {
         for (int i = 0; i < kTcSlots; ++i) {
             mbarrier_init(&full[i], 128);
-            mbarrier_init(&empty[i], 1);
+            mbarrier_init(&empty[i], 2);
         }
         for (int i = 0; i < kTcAux; ++i) {
             mbarrier_init(&aux_full[i], 64);
-            mbarrier_init(&aux_free[i], 1);
+            mbarrier_init(&aux_free[i], 2);
             ragged[i] = 0;
         }
         for (int i = 0; i < 2; ++i) {
@@ -93,9 +94,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
             }
             mbarrier_init(&o_done[i], 1);
             mbarrier_init(&o_full[i], 1);
+            mbarrier_init(&drained[i], 1);
         }
         mbarrier_init(&q_full, 256);
-        mbarrier_init(&drained, 1);
     }
     if (warp == 12) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_base)) : "memory");
@@ -395,101 +396,97 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
             announce(items - 1);
         }
     } else {
-        // ---- warp 12 issues the products, warps 14 and 15 look up the places ----
+        // ---- warps 12 and 13 issue the products of the two streams, warps 14 and 15 look up the places ----
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(256 - S::kSoftmaxRegs));
-        if (warp == 12) {
+        if (warp < 14) {
+            const int s = warp - 12;
             constexpr uint64_t kRowsLayout = tc_layout(16, 1024), kColsLayout = tc_layout(kBlockBytes, 1024);
-            constexpr uint32_t kTile16 = S::kTileBytes / 16;
-            uint32_t item = 0, n_p[2] = {0, 0};
+            constexpr uint32_t kTile16 = S::kTileBytes / 16, kBlock = kBlockBytes / 16, kHalf16 = 64 * 128 / 16;
             const uint32_t q16 = smem_u32(q_tiles) >> 4, ring16 = smem_u32(ring) >> 4;
-            auto wait_item = [&](uint32_t i) {
+            // Descriptors of this stream's query tile and of the first ring slot; everything else is a constant away where the slot is one.
+            const uint64_t q_at = tc_descriptor(kRowsLayout, q16 + (narrow ? 0 : s) * kTile16);
+            const uint64_t k_base = tc_descriptor(kRowsLayout, ring16), v_base = tc_descriptor(kColsLayout, ring16);
+            const uint32_t d_scores = tmem + s * kTcTile, d_out = tmem + kColO + s * DP;
+            auto wait_item = [&](int i) {
                 wait(&full[i % kTcSlots], (i / kTcSlots) & 1);
                 tc_fence_after();
             };
-            // Half h of S_s = Q K^T with the keys of item i
-            auto scores = [&](int s, int h, int q_tile, uint32_t i, bool release) {
-                const uint32_t k_at = ring16 + (i % kTcSlots) * kTile16 + h * (64 * 128 / 16), q_at = q16 + q_tile * kTile16, d = tmem + s * kTcTile + h * 64;
+            // A slot is free when both streams have released it; in the narrow form one of them does it for both.
+            auto release = [&](uint64_t* bar) {
+                tc_commit(bar);
+                if (narrow) tc_commit(bar);
+            };
+            // Half h of S = Q K^T with the keys in `slot`
+            auto scores = [&](int h, uint32_t slot) {
+                const uint64_t k_at = k_base + (slot * kTile16 + h * kHalf16);
                 if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < DP / 16; ++k) {
-                        const uint32_t step = ((k >> 2) * kBlockBytes + (k & 3) * 32) / 16;
-                        tc_mma_ss(d, tc_descriptor(kRowsLayout, q_at + step), tc_descriptor(kRowsLayout, k_at + step), kScoreIdesc, k > 0);
-                    }
+                    for (int k = 0; k < DP / 16; ++k)
+                        tc_mma_ss(d_scores + h * 64, q_at + ((k >> 2) * kBlock + (k & 3) * 2), k_at + ((k >> 2) * kBlock + (k & 3) * 2), kScoreIdesc, k > 0);
                     tc_commit(&s_full[s][h]);
-                    if (release) tc_commit(&empty[i % kTcSlots]);
+                    if (h == 1) release(&empty[slot]);
                 }
                 __syncwarp();
             };
-            // O_s += W V with half h of the values of item i
-            uint32_t outputs = 0;  // tiles whose last product has been issued
-            auto output = [&](int s, int h, uint32_t i, bool first, bool last, bool release) {
-                const uint32_t v_at = ring16 + (i % kTcSlots) * kTile16 + h * (64 * 128 / 16), d = tmem + kColO + s * DP, w = tmem + s * kTcTile + h * 64;
+            // O += W V with half h of the values in `slot`, of this stream's tile `t` (`first`, `last` of its tiles)
+            auto output = [&](int h, uint32_t slot, int t, bool first, bool last) {
+                const uint64_t v_at = v_base + (slot * kTile16 + h * kHalf16);
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < kTcTile / 32; ++k)
-                        tc_mma_ts(d, w + k * 8, tc_descriptor(kColsLayout, v_at + k * 128), kOutIdesc, k > 0 ? 1u : (uint32_t)!first);
+                        tc_mma_ts(d_out, d_scores + h * 64 + k * 8, v_at + k * 128, kOutIdesc, k + h > 0 ? 1u : (uint32_t)!first);
                     tc_commit(&o_done[s]);
-                    if (last) tc_commit(&o_full[s]);
-                    if (release) {  // the tile is done with: its values, its places and its constants
-                        tc_commit(&empty[i % kTcSlots]);
-                        tc_commit(&aux_free[outputs % kTcAux]);
+                    if (h == 1) {  // the tile is done with: its values, its places and its constants
+                        release(&empty[slot]);
+                        release(&aux_free[t % kTcAux]);
+                        if (last) tc_commit(&o_full[s]);
                     }
                 }
-                if (release) ++outputs;
                 __syncwarp();
             };
-            auto wait_weights = [&](int s, int h) {
-                wait(&p_full[s][h], (n_p[s] >> 1) & 1);
-                ++n_p[s];
-                tc_fence_after();
+            // Tile number i of this stream: products with its values, then the scores of the next one.
+            auto tile = [&](int i, int t, uint32_t v_item, uint32_t v_slot, bool more, uint32_t k_item, uint32_t k_slot) {
+                wait_item(v_item);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    wait(&p_full[s][h], i & 1);
+                    tc_fence_after();
+                    output(h, v_slot, t, i == 0, !more);
+                    if (more) {
+                        if (h == 0) wait_item(k_item);
+                        scores(h, k_slot);
+                    }
+                }
             };
             wait(&q_full, 0);
             tc_fence_after();
             if (narrow) {
-                for (int j = 0; j < 2 && j < n; ++j) {
-                    wait_item(item);
-                    scores(j, 0, 0, item, false);
-                    scores(j, 1, 0, item++, true);
+                // items: K_t is 0 or 2 t - 1, V_t is 2 t + 2, the last one 2 n - 1
+                if (s < n) {
+                    wait_item(s);
+                    scores(0, s);
+                    scores(1, s);
                 }
-                for (int j = 0; j < n; ++j) {
-                    const int s = j & 1;
-                    const bool more = j + 2 < n;
-                    wait_item(item);
-                    for (int h = 0; h < 2; ++h) {
-                        wait_weights(s, h);
-                        output(s, h, item, j < 2 && h == 0, !more && h == 1, h == 1);
-                        if (more) {
-                            if (h == 0) wait_item(item + 1);
-                            scores(s, h, 0, item + 1, h == 1);
-                        }
-                    }
-                    item += more ? 2 : 1;
+                for (int t = s; t < n; t += 2) {
+                    const uint32_t v_item = t == n - 1 ? 2 * n - 1 : 2 * t + 2, k_item = 2 * t + 3;
+                    tile(t >> 1, t, v_item, v_item % kTcSlots, t + 2 < n, k_item, k_item % kTcSlots);
                 }
             } else {
-                wait_item(item);
-                for (int h = 0; h < 2; ++h)
-                    for (int s = 0; s < 2; ++s) scores(s, h, s, item, h + s == 2);
-                ++item;
-                for (int j = 0; j < n; ++j) {
-                    const bool more = j + 1 < n;
-                    wait_item(item);
-                    for (int h = 0; h < 2; ++h)
-                        for (int s = 0; s < 2; ++s) {
-                            wait_weights(s, h);
-                            output(s, h, item, j + h == 0, !more && h == 1, h + s == 2);
-                            if (more) {
-                                if (h + s == 0) wait_item(item + 1);
-                                scores(s, h, s, item + 1, h + s == 2);
-                            }
-                        }
-                    item += more ? 2 : 1;
+                // items: K_t is 2 t, V_t is 2 t + 1
+                static_assert(kTcSlots == 4, "keys of even tiles in slot 0, of odd ones in slot 2");
+                wait_item(0);
+                scores(0, 0);
+                scores(1, 0);
+                for (int t = 0; t < n; t += 2) {
+                    tile(t, t, 2 * t + 1, 1, t + 1 < n, 2 * t + 2, 2);
+                    if (t + 1 < n) tile(t + 1, t + 1, 2 * t + 3, 3, t + 2 < n, 2 * t + 4, 0);
                 }
             }
             // the tensor memory is given back only when nothing writes it any more
-            if (elect_one()) tc_commit(&drained);
+            if (elect_one()) tc_commit(&drained[s]);
             __syncwarp();
-            ok = mbarrier_wait_sleeping(&drained, 0) && ok;
-        } else if (warp >= 14) {
+            ok = mbarrier_wait_sleeping(&drained[s], 0) && ok;
+        } else {
             // Places of the tiles' keys and what the softmax wants to know of them, two keys to a thread, up to kTcAux tiles ahead.
             // A tile's page numbers are read while the tile before it is published.
             const int p = tid - 448;
