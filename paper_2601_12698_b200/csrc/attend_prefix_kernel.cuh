@@ -42,6 +42,9 @@ constexpr int kTcAux = 8;     // tiles whose places and constants are kept: the 
 template <int FMT, int DP>
 struct PrefixShape {
     static constexpr bool kQuant = FMT != kKvPlain;
+    // Of eight pairs of every 32 exponentials, so many go to the multiply-add pipe (see ex2_by_polynomial): the SM's special
+    // function unit alone needs 2048 cycles for the two streams' tiles, as long as the tensor cores.
+    static constexpr int kPolynomial = 4;
     // Registers per softmax thread; half the threads are softmax threads, and the other half gets the rest of 2 * 128.
     static constexpr int kSoftmaxRegs = 136;
     static constexpr int kTileBytes = kTcTile * DP * 2;
@@ -211,13 +214,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                     const float2x c2 = pack_f2(c, c), minus2 = pack_f2(-base, -base);
                     float t4[2] = {-INFINITY, -INFINITY};
                     sum[0] = sum[1] = pack_f2(0.f, 0.f);
+                    uint32_t v2[2][32];
+                    tmem_load32(col, v2[0]);
+                    tmem_load32(col + 32, v2[1]);
+                    tmem_wait_load(v2[0]);
+                    tmem_loaded(v2[1]);
+                    const bool holes = !kQuant && *reinterpret_cast<volatile uint32_t*>(&ragged[aux_i]) != 0;  // the last tile, or pages that are not there
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
-                        uint32_t v[32];
-                        tmem_load32(col + q * 32, v);
-                        tmem_wait_load(v);
+                        uint32_t(&v)[32] = v2[q];
                         const int at4 = h * 16 + q * 8;  // constants, four keys at a time
-                        if (!kQuant && *reinterpret_cast<volatile uint32_t*>(&ragged[aux_i]) != 0) {  // the last tile, or pages that are not there
+                        if (holes) {
 #pragma unroll
                             for (int k = 0; k < 8; ++k) {
                                 const float4 b = ka[at4 + k];
@@ -242,10 +249,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                             unpack_f2(t1, x[2], x[3]);
                             t4[0] = fmaxf(fmaxf(t4[0], x[0]), x[1]);
                             t4[1] = fmaxf(fmaxf(t4[1], x[2]), x[3]);
-                            unpack_f2(kQuant ? add_f2(t0, minus2) : fma_f2(t0, c2, minus2), x[0], x[1]);
-                            unpack_f2(kQuant ? add_f2(t1, minus2) : fma_f2(t1, c2, minus2), x[2], x[3]);
-#pragma unroll
-                            for (int y = 0; y < 4; ++y) x[y] = ex2(x[y]);
+                            t0 = kQuant ? add_f2(t0, minus2) : fma_f2(t0, c2, minus2);
+                            t1 = kQuant ? add_f2(t1, minus2) : fma_f2(t1, c2, minus2);
+                            if (k % 8 < S::kPolynomial) t1 = ex2_by_polynomial(t1);
+                            unpack_f2(t0, x[0], x[1]);
+                            unpack_f2(t1, x[2], x[3]);
+                            x[0] = ex2(x[0]);
+                            x[1] = ex2(x[1]);
+                            if (k % 8 >= S::kPolynomial) {
+                                x[2] = ex2(x[2]);
+                                x[3] = ex2(x[3]);
+                            }
                             if constexpr (kQuant) {
                                 const ulonglong2 iv = reinterpret_cast<const ulonglong2*>(ka)[64 + at4 + k];
                                 sum[0] = fma_f2(pack_f2(x[0], x[1]), iv.x, sum[0]);
