@@ -360,23 +360,24 @@ def merge_attn_states_template_launch(params: rt_params, v_a, s_a, v_b, s_b, v_o
 
 # ---- 1b. the paged key/value cache and the attention that reads it ------------------------------------------
 
-def _device_and_stream(tensor, stream):
-    """(device index, cudaStream_t): the tensor's device and the given stream of it, or its current one."""
-    import torch
-    index = tensor.get_device()
+_TORCH_CODES: dict = {}  # torch dtype -> rt_dtype
+_torch = None  # set by the first KvCache: a serving loop's calls should not pay for an import statement each
+
+
+def _stream_of(index: int, stream) -> int:
+    """cudaStream_t: the given stream of device `index`, or that device's current one."""
     if stream is None:
-        return index, torch._C._cuda_getCurrentRawStream(index)
+        return _torch._C._cuda_getCurrentRawStream(index)
     if stream.device_index != index:
         raise ValueError(f"the stream belongs to device {stream.device_index}, the tensors to device {index}")
-    return index, stream.cuda_stream
+    return stream.cuda_stream
 
 
 def _call_on(index: int, fn, *args) -> int:
     """fn(*args) with `index` as the current device (the library works on the current one)."""
-    import torch
-    if torch.cuda.current_device() == index:
+    if _torch._C._cuda_getDevice() == index:
         return fn(*args)
-    with torch.cuda.device(index):
+    with _torch.cuda.device(index):
         return fn(*args)
 
 
@@ -395,6 +396,8 @@ class KvCache:
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
         import torch
+        global _torch
+        _torch = torch
         formats = {torch.float8_e4m3fn: RT_KV_E4M3, torch.uint8: RT_KV_E4M3, torch.int8: RT_KV_INT8, torch.bfloat16: RT_KV_PLAIN,
                    torch.float16: RT_KV_PLAIN, torch.float32: RT_KV_PLAIN}
         if k.dim() != 4 or not k.is_cuda or k.dtype not in formats:
@@ -417,6 +420,8 @@ class KvCache:
         if not (1 <= self.head_dim <= RT_KV_MAX_HEAD_DIM and self.kv_heads >= 1 and 1 <= self.page_size <= 65536):
             raise ValueError(f"page_size {self.page_size}, kv_heads {self.kv_heads} or head_dim {self.head_dim} out of range")
         self.device_index = k.get_device()
+        self._entry = k.shape[2:]
+        _TORCH_CODES.update({torch.bfloat16: RT_BF16, torch.float16: RT_FP16, torch.float32: RT_FP32})
         scale_strides = k_scale.stride() if k_scale is not None else (0, 0, 0)
         self.struct = rt_kv_cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if k_scale is not None else None,
                                   v_scale.data_ptr() if v_scale is not None else None, self.n_pages, self.page_size, self.kv_heads,
@@ -435,39 +440,43 @@ class KvCache:
         return cls(*held, *scales)
 
 
-def _cache_call_args(cache: KvCache, key, value, slots, name: str):
-    import torch
-    n_tokens = slots.shape[0] if slots.dim() == 1 else -1
-    shape = (n_tokens, cache.kv_heads, cache.head_dim)
-    if slots.dtype != torch.int64 or not slots.is_contiguous() or slots.get_device() != cache.device_index:
+def _refuse_cache_call(cache: KvCache, key, value, slots, name: str):
+    if slots.dim() != 1 or slots.dtype != _torch.int64 or not slots.is_contiguous() or slots.get_device() != cache.device_index:
         raise ValueError(f"{name}: slots must be a contiguous int64 [n_tokens] tensor on the cache's device")
-    for t in (key, value):
-        if t.shape != shape or t.dtype != key.dtype or t.get_device() != cache.device_index:
-            raise ValueError(f"{name}: key and value must be {list(shape)} tensors of one dtype on the cache's device")
-        if t.stride(2) != 1 and t.shape[2] > 1:
-            raise ValueError(f"{name}: the last axis of key and value must be contiguous")
-    return n_tokens
+    raise ValueError(f"{name}: key and value must be [{slots.shape[0]}, {cache.kv_heads}, {cache.head_dim}] tensors of one dtype on the "
+                     "cache's device, the last axis contiguous")
 
 
 def kv_cache_write_launch(cache: KvCache, key, value, slots, stream=None) -> None:
     """Write (quantising on the way) keys and values [n_tokens, kv_heads, head_dim] of n_tokens tokens into the cache at
     their slots (int64 [n_tokens], page * page_size + offset; negative = padding, skipped).  Asynchronous."""
-    n_tokens = _cache_call_args(cache, key, value, slots, "kv_cache_write_launch")
-    index, s = _device_and_stream(slots, stream)
-    _check(_call_on(index, lib.kv_cache_write_launch, cache._ref, key.data_ptr(), key.stride(0), key.stride(1), value.data_ptr(),
-                    value.stride(0), value.stride(1), slots.data_ptr(), n_tokens, _dtype_code(key), s), "kv_cache_write_launch")
+    index, shape, ks, vs, dtype = cache.device_index, key.shape, key.stride(), value.stride(), key.dtype
+    if not (slots.dtype is _torch.int64 and slots.shape == shape[:1] and slots.is_contiguous() and len(shape) == 3
+            and shape[1:] == cache._entry and value.shape == shape and value.dtype is dtype and dtype in _TORCH_CODES
+            and (ks[2] == vs[2] == 1 or shape[2] == 1) and key.get_device() == value.get_device() == slots.get_device() == index):
+        _refuse_cache_call(cache, key, value, slots, "kv_cache_write_launch")
+    status = _call_on(index, lib.kv_cache_write_launch, cache._ref, key.data_ptr(), ks[0], ks[1], value.data_ptr(), vs[0], vs[1],
+                      slots.data_ptr(), shape[0], _TORCH_CODES[dtype], _stream_of(index, stream))
+    if status:
+        raise TunerError(status, "kv_cache_write_launch")
 
 
 def kv_cache_read_launch(cache: KvCache, slots, key_out, value_out, stream=None) -> None:
     """Read entries of the cache back into key_out and value_out [n_tokens, kv_heads, head_dim]; rows whose slot is
     negative are left as they were.  Asynchronous."""
-    n_tokens = _cache_call_args(cache, key_out, value_out, slots, "kv_cache_read_launch")
-    _no_overlap(key_out, "key_out")
-    _no_overlap(value_out, "value_out")
-    index, s = _device_and_stream(slots, stream)
-    _check(_call_on(index, lib.kv_cache_read_launch, cache._ref, slots.data_ptr(), n_tokens, key_out.data_ptr(), key_out.stride(0),
-                    key_out.stride(1), value_out.data_ptr(), value_out.stride(0), value_out.stride(1), _dtype_code(key_out), s),
-           "kv_cache_read_launch")
+    index, shape, ks, vs, dtype = cache.device_index, key_out.shape, key_out.stride(), value_out.stride(), key_out.dtype
+    if not (slots.dtype is _torch.int64 and slots.shape == shape[:1] and slots.is_contiguous() and len(shape) == 3
+            and shape[1:] == cache._entry and value_out.shape == shape and value_out.dtype is dtype and dtype in _TORCH_CODES
+            and (ks[2] == vs[2] == 1 or shape[2] == 1)
+            and key_out.get_device() == value_out.get_device() == slots.get_device() == index):
+        _refuse_cache_call(cache, key_out, value_out, slots, "kv_cache_read_launch")
+    if 0 in ks or 0 in vs:
+        _no_overlap(key_out, "key_out")
+        _no_overlap(value_out, "value_out")
+    status = _call_on(index, lib.kv_cache_read_launch, cache._ref, slots.data_ptr(), shape[0], key_out.data_ptr(), ks[0], ks[1],
+                      value_out.data_ptr(), vs[0], vs[1], _TORCH_CODES[dtype], _stream_of(index, stream))
+    if status:
+        raise TunerError(status, "kv_cache_read_launch")
 
 
 class PrefixBatch:
@@ -522,28 +531,26 @@ def shared_prefix_attention_launch(cache: KvCache, batch: PrefixBatch, q, out, l
     prefix and to each sequence's own suffix; out like q and contiguous, lse float32 [..., q_heads] or None.  softmax_scale
     defaults to head_dim ** -0.5.  workspace: a uint8 tensor of shared_prefix_attention_workspace_bytes(...) bytes, made
     here when it is None.  Asynchronous."""
-    shape = q.shape
-    n_seqs, q_len, head_dim = batch.n_seqs, batch.q_len, cache.head_dim
+    shape, strides, dtype = q.shape, q.stride(), q.dtype
+    n_seqs, q_len, head_dim, index = batch.n_seqs, batch.q_len, cache.head_dim, cache.device_index
     if len(shape) == 4 and shape[1] == q_len:
-        token_stride, head_stride = q.stride(1) if q_len > 1 else q.stride(0), q.stride(2)
-        if q_len > 1 and n_seqs > 1 and q.stride(0) != q_len * token_stride:
+        token_stride = strides[1] if q_len > 1 else strides[0]
+        if q_len > 1 and n_seqs > 1 and strides[0] != q_len * token_stride:
             raise ValueError("q: the query tokens of all sequences must be evenly spaced")
     elif len(shape) == 3 and q_len == 1:
-        token_stride, head_stride = q.stride(0), q.stride(1)
+        token_stride = strides[0]
     else:
         raise ValueError("q must be [n_seqs, q_len, q_heads, head_dim], or [n_seqs, q_heads, head_dim] when q_len is 1")
-    if shape[0] != n_seqs or shape[-1] != head_dim or (head_dim > 1 and q.stride(-1) != 1):
+    if shape[0] != n_seqs or shape[-1] != head_dim or (head_dim > 1 and strides[-1] != 1):
         raise ValueError(f"q must hold {n_seqs} sequences and heads of {head_dim}, the last axis contiguous")
-    if out.shape != shape or out.dtype != q.dtype or not out.is_contiguous():
+    if out.shape != shape or out.dtype is not dtype or not out.is_contiguous():
         raise ValueError("out must be contiguous and of q's shape and dtype")
-    index = cache.device_index
     if not (q.get_device() == out.get_device() == batch.device_index == index):
         raise ValueError("cache, batch, q and out must be on one CUDA device")
     q_heads = shape[-2]
     lse_ptr = None
     if lse is not None:
-        import torch
-        if lse.shape != shape[:-1] or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.get_device() != index:
+        if lse.shape != shape[:-1] or lse.dtype is not _torch.float32 or not lse.is_contiguous() or lse.get_device() != index:
             raise ValueError("lse must be a contiguous float32 tensor of q's shape without head_dim, on q's device")
         lse_ptr = lse.data_ptr()
     if workspace is None:
@@ -552,11 +559,14 @@ def shared_prefix_attention_launch(cache: KvCache, batch: PrefixBatch, q, out, l
             workspace.record_stream(stream)
     elif workspace.get_device() != index or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the cache's device")
-    _, s = _device_and_stream(q, stream)
-    _check(_call_on(index, lib.shared_prefix_attention_launch, cache._ref, batch._ref, q.data_ptr(), token_stride, head_stride, q_heads,
-                    out.data_ptr(), lse_ptr, head_dim ** -0.5 if softmax_scale is None else softmax_scale, _dtype_code(q),
-                    workspace.data_ptr() if workspace.numel() else None, workspace.numel() * workspace.element_size(), s),
-           "shared_prefix_attention_launch")
+    code = _TORCH_CODES.get(dtype)
+    if code is None:
+        raise ValueError("q must be bf16 or fp16")
+    status = _call_on(index, lib.shared_prefix_attention_launch, cache._ref, batch._ref, q.data_ptr(), token_stride, strides[-2], q_heads,
+                      out.data_ptr(), lse_ptr, head_dim ** -0.5 if softmax_scale is None else softmax_scale, code, workspace.data_ptr(),
+                      workspace.nbytes, _stream_of(index, stream))
+    if status:
+        raise TunerError(status, "shared_prefix_attention_launch")
 
 
 def rmsnorm_host_workspace_bytes(n_tokens: int, hidden: int, dtype, chunk_tokens: int = 0) -> int:

@@ -10,7 +10,7 @@ struct AttendKernel {
     const void* fn = nullptr;
     size_t smem = 0;
 };
-enum { kPrefixTiles = 0, kPrefixKeys16 = 1, kPrefixKeys64 = 2, kSuffixKeys16 = 3, kSuffixKeys64 = 4, kMergeParts = 5, kAttendKernels = 6 };
+enum { kPrefixTiles = 0, kKeys16 = 1, kKeys64 = 2, kMergeParts = 3, kAttendKernels = 4 };
 struct AttendKernels {
     AttendKernel k[kAttendKernels];  // fn == NULL: the form does not serve heads of that size
 };

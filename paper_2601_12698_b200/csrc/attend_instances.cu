@@ -19,10 +19,8 @@ rt::AttendKernels kernels()
     AttendKernels a;
     if constexpr (DP <= 128)  // heads of 256 leave tensor memory no room for two streams
         a.k[kPrefixTiles] = {(const void*)attend_prefix_kernel<T, FMT, DP>, PrefixShape<FMT, DP>::kSmem};
-    a.k[kPrefixKeys16] = {(const void*)attend_keys_kernel<T, FMT, DP, 16, true>, KeysShape<FMT, DP, 16>::kSmem};
-    a.k[kPrefixKeys64] = {(const void*)attend_keys_kernel<T, FMT, DP, 64, true>, KeysShape<FMT, DP, 64>::kSmem};
-    a.k[kSuffixKeys16] = {(const void*)attend_keys_kernel<T, FMT, DP, 16, false>, KeysShape<FMT, DP, 16>::kSmem};
-    a.k[kSuffixKeys64] = {(const void*)attend_keys_kernel<T, FMT, DP, 64, false>, KeysShape<FMT, DP, 64>::kSmem};
+    a.k[kKeys16] = {(const void*)attend_keys_kernel<T, FMT, DP, 16>, KeysShape<FMT, DP, 16>::kSmem};
+    a.k[kKeys64] = {(const void*)attend_keys_kernel<T, FMT, DP, 64>, KeysShape<FMT, DP, 64>::kSmem};
     a.k[kMergeParts] = {(const void*)merge_parts_kernel<T, DP>, 0};
     return a;
 }

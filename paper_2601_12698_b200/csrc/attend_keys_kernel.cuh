@@ -105,10 +105,10 @@ __device__ __noinline__ float hidden_poison_of(const AttendArgs& a, const int32_
     return sum;
 }
 
-// PREFIX: NR rows of one key/value head (over all sequences) against a part of the prefix; else NR rows of one sequence and
-// key/value head against a part of its suffix.
-template <typename T, int FMT, int DP, int NR, bool PREFIX>
-__global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) attend_keys_kernel(const AttendArgs a)
+// The first prefix_ctas CTAs: NR rows of one key/value head (over all sequences) against a part of the prefix; the others: NR rows
+// of one sequence and key/value head against a part of its suffix.
+template <typename T, int FMT, int DP, int NR>
+__global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) attend_keys_kernel(const AttendArgs a, const int prefix_ctas)
 {
     using S = KeysShape<FMT, DP, NR>;
     constexpr bool kQuant = S::kQuant;
@@ -133,10 +133,11 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
 
     // (the warp's number by shuffle: the compiler then knows that a role is taken by whole warps)
     const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
-    unsigned job = blockIdx.x;
+    const bool prefix = (int)blockIdx.x < prefix_ctas;
+    unsigned job = prefix ? blockIdx.x : blockIdx.x - (unsigned)prefix_ctas;
     const int kv_head = (int)(job % (unsigned)a.kv_heads);
     job /= (unsigned)a.kv_heads;
-    const unsigned parts = PREFIX ? a.prefix_parts : a.suffix_parts;
+    const unsigned parts = prefix ? a.prefix_parts : a.suffix_parts;
     const int part = (int)(job % parts);
     job /= parts;
     if (tid == 0) {
@@ -152,9 +153,9 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
         mbarrier_init(&q_full, 128);
         poisoned = 0;
     }
-    const bool beside_prefix = !PREFIX && a.after_prefix != 0;
+    const bool beside_prefix = a.after_prefix != 0;  // that of another launch
     if (!beside_prefix) wait_for_previous_kernel();
-    if (PREFIX) let_next_kernel_start();
+    if (a.before_suffix) let_next_kernel_start();
     const auto leave = [&]() {
         if (beside_prefix && blockIdx.x == 0) wait_for_previous_kernel();
     };
@@ -162,7 +163,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
     int len, first_token, n_rows, row0;
     const int32_t* pages;
     int list_len;
-    if constexpr (PREFIX) {
+    if (prefix) {
         len = a.prefix_len;
         first_token = 0;
         n_rows = a.n_seqs * a.q_len * a.group;
@@ -183,9 +184,9 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
         pages = a.page_table + (long long)seq * a.page_table_stride;
         list_len = a.page_table_width;
     }
-    const int part_keys = PREFIX ? a.prefix_keys : a.suffix_keys;
+    const int part_keys = prefix ? a.prefix_keys : a.suffix_keys;
     const int k0 = part * part_keys, k1 = min(len, k0 + part_keys);
-    const int part_index = (PREFIX ? 0 : a.prefix_parts) + part;
+    const int part_index = (prefix ? 0 : a.prefix_parts) + part;
     const bool direct = a.prefix_parts + a.suffix_parts == 1;
     const int n_heads = a.kv_heads * a.group;
     const long long all_rows = (long long)a.n_seqs * a.q_len * n_heads;
@@ -218,7 +219,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
     const uint32_t tmem = tmem_base, tmem_o = tmem + 2 * NR;
     const int n = (k1 - k0 + 127) / 128;
     const int live_rows = min(NR, n_rows - row0);  // the rest of the tile is padding: nothing is computed for it beyond the products
-    const int all_see = PREFIX ? len : len - a.q_len + 1;  // keys below it are seen by every row
+    const int all_see = prefix ? len : len - a.q_len + 1;  // keys below it are seen by every row
 
     // Every wait is bounded.  A thread whose wait has run out stops waiting and goes on through the same loops, so that every
     // barrier is still met and the tensor memory is given back; the status word says that the results are not valid.
@@ -317,7 +318,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
                 ivs = __frcp_rn(vs);
             }
             // rows below it do not see this thread's key
-            const int hidden = PREFIX ? 0 : max(0, k0 + j * 128 + tid - (len - a.q_len)) * a.group - row0;
+            const int hidden = prefix ? 0 : max(0, k0 + j * 128 + tid - (len - a.q_len)) * a.group - row0;
             wait(&s_full[j & 1], (j >> 1) & 1);
             tc_fence_after();
             // 16 rows' scores of this thread's key, as logarithms; more rows than that are read again where they are needed
@@ -449,7 +450,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
             const float total = row_sum[0][tid] + row_sum[1][tid] + row_sum[2][tid] + row_sum[3][tid];
             const bool empty = total == 0.f;  // a row that sees a key has a sum above zero, or NaN
             bool write = at >= 0;
-            if (PREFIX && direct && write) write = __ldg(a.suffix_lens + (int)((unsigned)(at / n_heads) / (unsigned)a.q_len)) >= 0;
+            if (prefix && direct && write) write = __ldg(a.suffix_lens + (int)((unsigned)(at / n_heads) / (unsigned)a.q_len)) >= 0;
             if (write) {
                 const float lse = empty ? -INFINITY : row_ref[tid] + log2f(total);
                 if (!direct) a.part_lse[(long long)part_index * all_rows + at] = lse;
@@ -460,7 +461,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
             row_c[tid] = !write || (empty && !direct) ? -1.f : empty ? 0.f : 1.0f / total;
         }
         sync_128();
-        const bool fix = !PREFIX && *reinterpret_cast<volatile int*>(&poisoned) != 0;
+        const bool fix = !prefix && *reinterpret_cast<volatile int*>(&poisoned) != 0;
 #pragma unroll 1
         for (int i = 0; i < NI; ++i) {
             const int d = i * 128 + tid;
@@ -526,7 +527,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
         };
         // Some rows do not see the last keys, and 0 * infinity would reach them through the product: such values become zero in
         // the tile and are added to the rows that do see them at the end.
-        auto guarded = [&](const Item& it) { return it.values && !PREFIX && a.q_len > 1 && k0 + it.tile * 128 + 128 > all_see; };
+        auto guarded = [&](const Item& it) { return it.values && !prefix && a.q_len > 1 && k0 + it.tile * 128 + 128 > all_see; };
         if constexpr (kQuant) {
             using C = CodePieces<DI>;
             const int u = p % C::UNITS, r0 = p / C::UNITS;

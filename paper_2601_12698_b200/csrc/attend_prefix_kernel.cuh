@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
     tc_fence_after();
     const uint32_t tmem = tmem_base;
     wait_for_previous_kernel();
-    let_next_kernel_start();
+    if (a.before_suffix) let_next_kernel_start();
 
     // this CTA's key/value head, row block and tiles
     const int block = (int)(blockIdx.x % (unsigned)split.blocks), run_no = (int)(blockIdx.x / (unsigned)split.blocks % (unsigned)split.runs);

@@ -26,7 +26,7 @@ struct AttendPlan {
     int padded_dim;
     int group;
     long long tokens;
-    int prefix_form, suffix_form;  // kPrefixTiles ..., -1: no keys
+    int prefix_form, suffix_form;  // kPrefixTiles, kKeys16, kKeys64; -1: no keys
     int prefix_parts, prefix_keys, suffix_parts, suffix_keys;
     PrefixSplit split;  // run > 0: the prefix is dealt out by tiles
     long long prefix_ctas, suffix_ctas;
@@ -123,8 +123,8 @@ int make_attend_plan(const rt_kv_cache* c, const rt_prefix_batch* b, int q_heads
     p->prefix_form = p->suffix_form = -1;
     const long long prefix_rows = p->tokens * p->group, suffix_rows = (long long)b->q_len * p->group;
     if (b->prefix_len > 0) {
-        if (prefix_rows <= 16) p->prefix_form = kPrefixKeys16;
-        else if (p->padded_dim == 256 || prefix_rows <= 64) p->prefix_form = kPrefixKeys64;
+        if (prefix_rows <= 16) p->prefix_form = kKeys16;
+        else if (p->padded_dim == 256 || prefix_rows <= 64) p->prefix_form = kKeys64;
         else p->prefix_form = kPrefixTiles;
         if (getenv("XPRE")) p->prefix_form = atoi(getenv("XPRE"));
         if (p->prefix_form == kPrefixTiles) {
@@ -157,15 +157,15 @@ int make_attend_plan(const rt_kv_cache* c, const rt_prefix_batch* b, int q_heads
             p->prefix_ctas = units * s.runs;
             p->prefix_parts = s.runs * (narrow_block(s, s.blocks - 1) ? 2 : 1);
         } else {
-            const int nr = p->prefix_form == kPrefixKeys16 ? 16 : 64;
+            const int nr = p->prefix_form == kKeys16 ? 16 : 64;
             const long long tiles = ceil_div(prefix_rows, nr) * c->kv_heads;
             split_keys(b->prefix_len, tiles, (long long)L.sm_count * (nr == 16 ? 2 : 1), 128, &p->prefix_parts, &p->prefix_keys);
             p->prefix_ctas = tiles * p->prefix_parts;
         }
     }
     if (b->max_suffix_len > 0) {
-        p->suffix_form = suffix_rows <= 32 ? kSuffixKeys16 : kSuffixKeys64;
-        const int nr = p->suffix_form == kSuffixKeys16 ? 16 : 64;
+        p->suffix_form = suffix_rows <= 32 ? kKeys16 : kKeys64;
+        const int nr = p->suffix_form == kKeys16 ? 16 : 64;
         const long long tiles = ceil_div(suffix_rows, nr) * c->kv_heads * b->n_seqs;
         split_keys(b->max_suffix_len, tiles, (long long)L.sm_count * (nr == 16 ? 2 : 1), 128, &p->suffix_parts, &p->suffix_keys);
         if (getenv("XKEYS")) { p->suffix_keys = atoi(getenv("XKEYS")); p->suffix_parts = (int)ceil_div(b->max_suffix_len, p->suffix_keys); }
@@ -273,24 +273,35 @@ int shared_prefix_attention_launch(const rt_kv_cache* c, const rt_prefix_batch* 
     a.part_lse = parts > 1 ? (float*)workspace + (int64_t)parts * p.tokens * q_heads * c->head_dim : nullptr;
     a.out = out;
     a.lse = lse;
-    a.after_prefix = p.prefix_form >= 0;
     a.status = device_status_word();
     if (!a.status) return RT_ERR_NO_DEVICE;
     const AttendKernels k = kernels_of(dtype, c->format, p.padded_dim);
-    void* params[] = {&a, &p.split};
     const cudaStream_t s = (cudaStream_t)stream;
-    const auto launch = [&](int form, long long ctas, int threads) {
+    const auto launch = [&](int form, long long ctas, int threads, void* second) {
+        void* params[] = {&a, second};
         return launch_form(k, form, dtype, c->format, p.padded_dim, ctas, threads, s, params);
     };
-    if (p.prefix_form >= 0) {
-        st = launch(p.prefix_form, p.prefix_ctas, p.prefix_form == kPrefixTiles ? kTcThreads : kKeysThreads);
+    if (p.prefix_form == p.suffix_form && p.prefix_form >= 0 && p.prefix_ctas + p.suffix_ctas <= 0x7fffffffLL) {
+        int prefix_ctas = (int)p.prefix_ctas;  // one launch serves both
+        st = launch(p.prefix_form, p.prefix_ctas + p.suffix_ctas, kKeysThreads, &prefix_ctas);
         if (st != RT_OK) return st;
+    } else {
+        if (p.prefix_form >= 0) {
+            int prefix_ctas = (int)p.prefix_ctas;
+            a.before_suffix = p.suffix_form >= 0;
+            if (p.prefix_form == kPrefixTiles) st = launch(kPrefixTiles, p.prefix_ctas, kTcThreads, &p.split);
+            else st = launch(p.prefix_form, p.prefix_ctas, kKeysThreads, &prefix_ctas);
+            if (st != RT_OK) return st;
+        }
+        if (p.suffix_form >= 0) {
+            int prefix_ctas = 0;
+            a.after_prefix = p.prefix_form >= 0;
+            a.before_suffix = 0;
+            st = launch(p.suffix_form, p.suffix_ctas, kKeysThreads, &prefix_ctas);
+            if (st != RT_OK) return st;
+        }
     }
-    if (p.suffix_form >= 0) {
-        st = launch(p.suffix_form, p.suffix_ctas, kKeysThreads);
-        if (st != RT_OK) return st;
-    }
-    if (parts != 1) st = launch(kMergeParts, ceil_div(p.tokens * q_heads, kMergePartsThreads / 32), kMergePartsThreads);
+    if (parts != 1) st = launch(kMergeParts, ceil_div(p.tokens * q_heads, kMergePartsThreads / 32), kMergePartsThreads, &p.split);
     return st;
 }
 
