@@ -1,4 +1,4 @@
-// What the attention kernels over a paged key/value cache share: arguments, places in the cache, 16-bit matrix products.
+// What the attention kernels over a paged key/value cache share: arguments, places in the cache, codes, exponentials.
 #pragma once
 
 #include <cuda_fp8.h>
@@ -96,19 +96,6 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
-// D += A B, A 16x16 and B 16x8 of 16-bit elements, D in binary32.
-template <typename T>
-__device__ __forceinline__ void mma_16x8x16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
-{
-    if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    } else {
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    }
-}
-
 // Two e4m3 codes as two fp16 values.  Both formats fit fp16 exactly.
 __device__ __forceinline__ uint32_t e4m3_to_half2(uint32_t low_bytes)
 {
@@ -149,36 +136,7 @@ __device__ __forceinline__ uint4 ld_codes(const unsigned char* p, bool there)
     return w;
 }
 
-// Two binary32 numbers in one register pair: the packed operations of sm_100 do both at once.
-typedef unsigned long long float2x;
-__device__ __forceinline__ float2x pack_f2(float lo, float hi)
-{
-    float2x r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ void unpack_f2(float2x x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
-__device__ __forceinline__ float2x fma_f2(float2x a, float2x b, float2x c)
-{
-    float2x r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ float2x mul_f2(float2x a, float2x b)
-{
-    float2x r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ float2x add_f2(float2x a, float2x b)
-{
-    float2x r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-
-// 2^x for two numbers on the multiply-add pipe, which is idle while the special function unit (16 exponentials a cycle per SM)
-// is the bound of a softmax: x = n + f with n the nearest integer, 2^f by the polynomial of degree 4 of least relative error on
+// 2^x for two numbers on the multiply-add pipe, beside the special function unit (16 exponentials a cycle per SM): x = n + f with n the nearest integer, 2^f by the polynomial of degree 4 of least relative error on
 // [-1/2, 1/2] (found by exchange of the extrema; 2.7e-6 in binary32, 4e-8 on average), times 2^n.  Below -126: 2^-126.
 __device__ __forceinline__ float2x ex2_by_polynomial(float2x x)
 {

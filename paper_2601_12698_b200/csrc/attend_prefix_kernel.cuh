@@ -23,7 +23,7 @@
 // output row in tensor memory are rescaled by the row's own thread.  Weights are thus at most 256, which bf16 and fp16 hold
 // with their full relative precision, and the quotient is the same.
 //
-// Quantised caches: both products run in fp16 on codes, with the scales in the exponent, as in attend_rows_kernel.cuh.
+// Quantised caches: both products run in fp16 on codes, with the scales in the exponent (see attend_keys_kernel.cuh).
 //
 // Bounds: 4 * 128 * 128 * dim flops and 128 * 128 exponentials per tile and stream; at dim 128 the tensor cores need 1024
 // cycles for that and the SM's 16 exponentials a cycle 1024 as well.
@@ -43,7 +43,8 @@ template <int FMT, int DP>
 struct PrefixShape {
     static constexpr bool kQuant = FMT != kKvPlain;
     // Of eight pairs of every 32 exponentials, so many go to the multiply-add pipe (see ex2_by_polynomial): the SM's special
-    // function unit alone needs 2048 cycles for the two streams' tiles, as long as the tensor cores.
+    // function unit alone needs 2048 cycles for the two streams' tiles, as long as the tensor cores.  Measured against none: 64
+    // sequences, prefix 8192, int8: 77 us, not 79.5; heads of 64: 164, not 167; 256 sequences, prefix 32768: no difference.
     static constexpr int kPolynomial = 4;
     // Registers per softmax thread; half the threads are softmax threads, and the other half gets the rest of 2 * 128.
     static constexpr int kSoftmaxRegs = 136;

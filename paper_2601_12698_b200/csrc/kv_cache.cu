@@ -64,7 +64,7 @@ int launch_shape(const CacheArgs& args, cudaStream_t stream)
 {
     CacheArgs a = args;
     constexpr int GROUPS = kCacheThreads / LANES;
-    constexpr int U = E == 8 && NCH == 1 ? 4 : 1;
+    constexpr int U = NCH > 1 ? 1 : E == 16 ? 2 : 4;
     // A CTA takes as many tokens as fill its groups: once over while the device has SMs to spare, U times once it is
     // covered (the vectors of one batch are then in flight together).
     const int per_token = 2 * a.heads;
@@ -88,11 +88,16 @@ int launch_shape(const CacheArgs& args, cudaStream_t stream)
     return launch_kernel((const void*)fn, dim3((unsigned)ctas), dim3(kCacheThreads), 0, stream, params);
 }
 
-// Eight elements to a lane where sizes, strides and pointers allow it, else four, else one: a vector of 128 is then one
-// chunk on 16 lanes; single elements serve what is left (odd head sizes).
+// Sixteen elements to a lane where sizes, strides and pointers allow it (the kernels are bound by instructions, and those that
+// find a vector's places are shared by more elements: 16384 x 8 x 128 bf16 to e4m3 took 30 us with eight), else eight, four, one.
 template <bool WRITE, typename T, int FMT>
 int launch_typed(const CacheArgs& a, int align_elems, cudaStream_t stream)
 {
+    if (align_elems >= 16) {
+        if (a.dim <= 64) return launch_shape<WRITE, T, FMT, 16, 4, 1>(a, stream);
+        if (a.dim <= 128) return launch_shape<WRITE, T, FMT, 16, 8, 1>(a, stream);
+        return launch_shape<WRITE, T, FMT, 16, 16, 1>(a, stream);
+    }
     if (align_elems >= 8) {
         if (a.dim <= 64) return launch_shape<WRITE, T, FMT, 8, 8, 1>(a, stream);
         if (a.dim <= 128) return launch_shape<WRITE, T, FMT, 8, 16, 1>(a, stream);
@@ -112,14 +117,13 @@ int launch_format(int format, const CacheArgs& a, int align_elems, cudaStream_t 
     }
 }
 
-// Largest of 8, 4, 1 such that a chunk of that many elements is aligned everywhere: chunks of token tensors want
+// Largest of 16, 8, 4, 1 such that a chunk of that many elements is aligned everywhere: chunks of token tensors want
 // min(16, elements * size) bytes, chunks of the cache min(16, elements * held size).
 int shared_alignment(const rt_kv_cache* c, const void* key, long long kts, long long khs, const void* value, long long vts,
                      long long vhs, int dtype, long long n_tokens)
 {
     const long long size = elem_bytes_of(dtype), held = c->format == RT_KV_PLAIN ? size : 1;
-    for (int e = 8; e > 1; e >>= 1) {
-        if (e == 2) break;
+    for (int e = 16; e > 2; e >>= 1) {
         const long long tok = std::min<long long>(16, e * size), kv = std::min<long long>(16, e * held);
         bool ok = c->head_dim % e == 0;
         ok = ok && (uintptr_t)key % tok == 0 && (uintptr_t)value % tok == 0 && (uintptr_t)c->k % kv == 0 && (uintptr_t)c->v % kv == 0;
@@ -183,6 +187,7 @@ int cache_launch(const rt_kv_cache* c, const void* key, int64_t kts, int64_t khs
     a.scale_head_stride = c->scale_head_stride;
     a.page_size = (unsigned)c->page_size;
     a.page_shift = log2_or_minus1((unsigned)c->page_size);
+    a.vec_shift = log2_or_minus1(2u * (unsigned)c->kv_heads);
     a.heads = c->kv_heads;
     a.dim = c->head_dim;
     a.status = device_status_word();

@@ -36,6 +36,7 @@ struct CacheArgs {
     long long scale_page_stride, scale_entry_stride, scale_head_stride;
     unsigned page_size;
     int page_shift;   // log2(page_size), or -1
+    int vec_shift;    // log2(2 * heads), or -1
     int heads;
     int dim;
     int tokens_per_cta;
@@ -43,25 +44,25 @@ struct CacheArgs {
 };
 
 struct SlotPlace {
-    long long page;
-    unsigned offset;
+    unsigned page, offset;  // the host checked that there are fewer than 2^31 pages
 };
 __device__ __forceinline__ SlotPlace place_of(long long slot, unsigned page_size, int page_shift)
 {
     SlotPlace p;
     if (page_shift >= 0) {
-        p.page = slot >> page_shift;
+        p.page = (unsigned)(slot >> page_shift);
         p.offset = (unsigned)slot & (page_size - 1u);
     } else if (slot < (1LL << 32)) {
-        const unsigned q = (unsigned)slot / page_size;
-        p.page = q;
-        p.offset = (unsigned)slot - q * page_size;
+        p.page = (unsigned)slot / page_size;
+        p.offset = (unsigned)slot - p.page * page_size;
     } else {
-        p.page = slot / page_size;
-        p.offset = (unsigned)(slot - p.page * page_size);
+        p.page = (unsigned)(slot / page_size);
+        p.offset = (unsigned)(slot - (long long)p.page * page_size);
     }
     return p;
 }
+// index * stride: two multiplications, not the three or four of a 64-bit product.
+__device__ __forceinline__ size_t times(unsigned index, long long stride) { return (size_t)index * (size_t)stride; }
 
 // E consecutive elements of type T as 32-bit words (E * sizeof(T) is 1, 2, 4, 8, 16 or 32 bytes).
 template <int BYTES>
@@ -76,10 +77,13 @@ __device__ __forceinline__ Chunk<BYTES> ld_chunk(const unsigned char* p)
         unsigned short h;
         asm volatile("ld.global.L1::no_allocate.u8 %0, [%1];" : "=h"(h) : "l"(p));
         c.w[0] = h;
-    } else if constexpr (BYTES == 32) {  // two 16-byte accesses: rows of a cache are 16-byte aligned at best
-        const Vec<16> a = ld_stream<16>(p), b = ld_stream<16>(p + 16);
+    } else if constexpr (BYTES > 16) {  // rows of a cache are 16-byte aligned at best
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { c.w[i] = a.w[i]; c.w[4 + i] = b.w[i]; }
+        for (int k = 0; k < BYTES / 16; ++k) {
+            const Vec<16> a = ld_stream<16>(p + 16 * k);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c.w[4 * k + i] = a.w[i];
+        }
     } else {
         const Vec<BYTES> a = ld_stream<BYTES>(p);
 #pragma unroll
@@ -92,12 +96,14 @@ __device__ __forceinline__ void st_chunk(unsigned char* p, const Chunk<BYTES>& c
 {
     if constexpr (BYTES == 1) {
         asm volatile("st.global.u8 [%0], %1;" ::"l"(p), "h"((unsigned short)c.w[0]) : "memory");
-    } else if constexpr (BYTES == 32) {
-        Vec<16> a, b;
+    } else if constexpr (BYTES > 16) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { a.w[i] = c.w[i]; b.w[i] = c.w[4 + i]; }
-        st_stream<16>(p, a);
-        st_stream<16>(p + 16, b);
+        for (int k = 0; k < BYTES / 16; ++k) {
+            Vec<16> a;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a.w[i] = c.w[4 * k + i];
+            st_stream<16>(p + 16 * k, a);
+        }
     } else {
         Vec<BYTES> a;
 #pragma unroll
@@ -109,21 +115,47 @@ __device__ __forceinline__ void st_chunk(unsigned char* p, const Chunk<BYTES>& c
 template <typename T, int E>
 __device__ __forceinline__ void chunk_to_float(const Chunk<E * (int)sizeof(T)>& c, float (&f)[E])
 {
-    using C = Codec<T, (E * (int)sizeof(T) > 32 ? 32 : E * (int)sizeof(T))>;
-    Vec<E * (int)sizeof(T)> v;
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < (E * (int)sizeof(T) + 3) / 4; ++i) v.w[i] = c.w[i];
-    C::unpack(v, f);
+        for (int i = 0; i < E; ++i) f[i] = __uint_as_float(c.w[i]);
+    } else if constexpr (E == 1) {
+        f[0] = Codec<T, 16>::to_float16(c.w[0] & 0xFFFFu);
+    } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+            f[2 * i] = __uint_as_float(c.w[i] << 16);
+            f[2 * i + 1] = __uint_as_float(c.w[i] & 0xFFFF0000u);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+            const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&c.w[i]));
+            f[2 * i] = x.x;
+            f[2 * i + 1] = x.y;
+        }
+    }
 }
 template <typename T, int E>
 __device__ __forceinline__ Chunk<E * (int)sizeof(T)> chunk_from_float(const float (&f)[E])
 {
-    using C = Codec<T, E * (int)sizeof(T)>;
-    const Vec<E * (int)sizeof(T)> v = C::pack(f);
     Chunk<E * (int)sizeof(T)> c;
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < (E * (int)sizeof(T) + 3) / 4; ++i) c.w[i] = v.w[i];
+        for (int i = 0; i < E; ++i) c.w[i] = __float_as_uint(f[i]);
+    } else if constexpr (E == 1) {
+        c.w[0] = Codec<T, 16>::from_float16(f[0]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) c.w[i] = Codec<T, 16>::from_float16x2(f[2 * i], f[2 * i + 1]);
+    }
     return c;
+}
+
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
 }
 
 // Magnitudes of E elements joined into `top` as bit patterns: patterns of non-negative floats order like the values, with
@@ -137,7 +169,7 @@ __device__ __forceinline__ uint32_t join_magnitude(uint32_t top, const Chunk<BYT
         for (int i = 0; i < BYTES / 4; ++i) top = max(top, c.w[i] & 0x7FFFFFFFu);
     } else {
 #pragma unroll
-        for (int i = 0; i < (BYTES + 3) / 4; ++i) top = __vmaxu2(top, c.w[i] & 0x7FFF7FFFu);
+        for (int i = 0; i < (BYTES + 3) / 4; ++i) top = max_u16x2(top, c.w[i] & 0x7FFF7FFFu);
     }
     return top;
 }
@@ -148,57 +180,97 @@ __device__ __forceinline__ float magnitude_of(uint32_t top)
     else return Codec<T, 16>::to_float16(max(top & 0xFFFFu, top >> 16));
 }
 
+// Two binary32 numbers in one register pair: the packed operations of sm_100 do both at once, each correctly rounded.
+typedef unsigned long long float2x;
+__device__ __forceinline__ float2x pack_f2(float lo, float hi)
+{
+    float2x r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpack_f2(float2x x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
+__device__ __forceinline__ float2x fma_f2(float2x a, float2x b, float2x c)
+{
+    float2x r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ float2x mul_f2(float2x a, float2x b)
+{
+    float2x r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float2x add_f2(float2x a, float2x b)
+{
+    float2x r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 // E binary32 values to E codes.
 template <int FMT, int E>
 __device__ __forceinline__ Chunk<E> encode(const float (&f)[E], float inv)
 {
     Chunk<E> c;
-    if constexpr (FMT == kKvE4m3) {
-        if constexpr (E == 1) {
-            c.w[0] = __nv_cvt_float_to_fp8(f[0] * inv, __NV_SATFINITE, __NV_E4M3);
-        } else {
-#pragma unroll
-            for (int i = 0; i < E; i += 4) {
-                const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(f[i] * inv, f[i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
-                const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(f[i + 2] * inv, f[i + 3] * inv), __NV_SATFINITE, __NV_E4M3);
-                c.w[i / 4] = lo | (hi << 16);
-            }
-        }
+    if constexpr (E == 1) {
+        if constexpr (FMT == kKvE4m3) c.w[0] = __nv_cvt_float_to_fp8(__fmul_rn(f[0], inv), __NV_SATFINITE, __NV_E4M3);
+        else c.w[0] = __float_as_uint(__fadd_rn(__fmul_rn(f[0], inv), 12582912.0f)) & 0xFFu;
     } else {
-        // |x * inv| <= 127 after rounding, so adding 1.5 * 2^23 leaves the nearest even integer in the low byte
-        uint32_t b[E];
+        const float2x inv2 = pack_f2(inv, inv);
 #pragma unroll
-        for (int i = 0; i < E; ++i) b[i] = __float_as_uint(__fadd_rn(__fmul_rn(f[i], inv), 12582912.0f));
-        if constexpr (E == 1) {
-            c.w[0] = b[0] & 0xFFu;
-        } else {
+        for (int i = 0; i < E; i += 4) {
+            float x[4];
+            float2x a = mul_f2(pack_f2(f[i], f[i + 1]), inv2), b = mul_f2(pack_f2(f[i + 2], f[i + 3]), inv2);
+            if constexpr (FMT == kKvE4m3) {
+                unpack_f2(a, x[0], x[1]);
+                unpack_f2(b, x[2], x[3]);
+                asm("{\n\t.reg .b16 lo, hi;\n\tcvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\tmov.b32 %0, {lo, hi};\n\t}"
+                    : "=r"(c.w[i / 4]) : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]));
+            } else {
+                // |x * inv| <= 127 after rounding, so adding 1.5 * 2^23 leaves the nearest even integer in the low byte
+                // (added one by one: a packed addition behind a packed product came out as one rounding, not two)
+                unpack_f2(a, x[0], x[1]);
+                unpack_f2(b, x[2], x[3]);
 #pragma unroll
-            for (int i = 0; i < E; i += 4)
-                c.w[i / 4] = __byte_perm(__byte_perm(b[i], b[i + 1], 0x0040), __byte_perm(b[i + 2], b[i + 3], 0x0040), 0x5410);
+                for (int k = 0; k < 4; ++k) x[k] = __fadd_rn(x[k], 12582912.0f);
+                c.w[i / 4] = __byte_perm(__byte_perm(__float_as_uint(x[0]), __float_as_uint(x[1]), 0x0040),
+                                         __byte_perm(__float_as_uint(x[2]), __float_as_uint(x[3]), 0x0040), 0x5410);
+            }
         }
     }
     return c;
 }
+// E codes times the scale.
 template <int FMT, int E>
-__device__ __forceinline__ void decode(const Chunk<E>& c, float (&f)[E])
+__device__ __forceinline__ void decode(const Chunk<E>& c, float scale, float (&f)[E])
 {
-    if constexpr (FMT == kKvE4m3 && E % 2 == 0) {
+    if constexpr (E == 1) {
+        const uint32_t b = c.w[0] & 0xFFu;
+        if constexpr (FMT == kKvE4m3) f[0] = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)b, __NV_E4M3)));
+        else f[0] = (float)(signed char)b;
+        f[0] = __fmul_rn(f[0], scale);
+    } else {
+        const float2x scale2 = pack_f2(scale, scale);
 #pragma unroll
-        for (int i = 0; i < E; i += 2) {
-            const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(c.w[i / 4] >> (8 * (i % 4))), __NV_E4M3);
-            f[i] = __half2float(__half(__half_raw{h.x}));
-            f[i + 1] = __half2float(__half(__half_raw{h.y}));
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < E; ++i) {
-        const uint32_t b = (c.w[i / 4] >> (8 * (i % 4))) & 0xFFu;
-        if constexpr (FMT == kKvE4m3) {
-            const __half_raw h = __nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)b, __NV_E4M3);
-            f[i] = __half2float(__half(h));
-        } else {
-            f[i] = (float)(signed char)b;
+        for (int i = 0; i < E; i += 4) {
+            float x[4];
+            if constexpr (FMT == kKvE4m3) {
+                uint32_t lo, hi;
+                asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+                    : "=r"(lo), "=r"(hi) : "r"(c.w[i / 4]));
+                const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&lo)), q = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+                x[0] = p.x; x[1] = p.y; x[2] = q.x; x[3] = q.y;
+            } else {
+                // 2^23 + (code + 128) as binary32 bits, minus 2^23 + 128: exact
+                const uint32_t w = c.w[i / 4] ^ 0x80808080u;
+                x[0] = __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7650)) - 8388736.0f;
+                x[1] = __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7651)) - 8388736.0f;
+                x[2] = __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7652)) - 8388736.0f;
+                x[3] = __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7653)) - 8388736.0f;
+            }
+            unpack_f2(mul_f2(pack_f2(x[0], x[1]), scale2), f[i], f[i + 1]);
+            unpack_f2(mul_f2(pack_f2(x[2], x[3]), scale2), f[i + 2], f[i + 3]);
         }
     }
 }
@@ -212,26 +284,33 @@ __device__ __forceinline__ constexpr float code_max()
 // Vector v of a CTA: v counts token, side, head.
 struct CacheVector {
     bool live;
-    int side, head, token;  // token: within the CTA
+    unsigned side, head, token;  // token: within the CTA
 };
-__device__ __forceinline__ CacheVector cache_vector(const CacheArgs& a, int v, int per_token, int n_vec)
+__device__ __forceinline__ CacheVector cache_vector(const CacheArgs& a, unsigned v, unsigned n_vec)
 {
     CacheVector c;
     c.live = v < n_vec;
-    c.token = (int)((unsigned)(c.live ? v : 0) / (unsigned)per_token);
-    const int in_token = (c.live ? v : 0) - c.token * per_token;
-    c.side = in_token >= a.heads;
-    c.head = in_token - (c.side ? a.heads : 0);
+    v = c.live ? v : 0;
+    const unsigned heads = (unsigned)a.heads;
+    c.token = a.vec_shift >= 0 ? v >> a.vec_shift : v / (2 * heads);
+    const unsigned in_token = v - c.token * 2 * heads;
+    c.side = in_token >= heads;
+    c.head = in_token - (c.side ? heads : 0);
     return c;
 }
+__device__ __forceinline__ unsigned char* token_vector(const CacheArgs& a, const CacheVector& c, long long first, int size)
+{
+    const long long ts = c.side ? a.token_stride[1] : a.token_stride[0], hs = c.side ? a.token_head_stride[1] : a.token_head_stride[0];
+    return (c.side ? a.tokens[1] : a.tokens[0]) + ((size_t)(first * ts) + times(c.token, ts) + times(c.head, hs)) * size;
+}
 // Where the entry and its scale lie; false: no such entry (padding, or a slot beyond the cache).
-__device__ __forceinline__ bool cache_place(const CacheArgs& a, long long slot, int head, size_t& entry, size_t& scale_entry)
+__device__ __forceinline__ bool cache_place(const CacheArgs& a, long long slot, unsigned head, size_t& entry, size_t& scale_entry)
 {
     if (slot >= a.n_slots) atomicExch(a.status, kDeviceIndexCode);
     if (slot < 0 || slot >= a.n_slots) return false;
     const SlotPlace p = place_of(slot, a.page_size, a.page_shift);
-    entry = (size_t)p.page * a.page_stride + (size_t)p.offset * a.entry_stride + (size_t)head * a.head_stride;
-    scale_entry = (size_t)p.page * a.scale_page_stride + (size_t)p.offset * a.scale_entry_stride + (size_t)head * a.scale_head_stride;
+    entry = times(p.page, a.page_stride) + times(p.offset, a.entry_stride) + times(head, a.head_stride);
+    scale_entry = times(p.page, a.scale_page_stride) + times(p.offset, a.scale_entry_stride) + times(head, a.scale_head_stride);
     return true;
 }
 
@@ -246,19 +325,17 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_write_kernel(const Cac
     static_assert(U <= LANES, "a lane for every vector in flight");
     const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
     constexpr int GROUPS = kCacheThreads / LANES;
-    const int per_token = 2 * a.heads;
     const long long first = (long long)blockIdx.x * a.tokens_per_cta;
-    const int n_vec = (int)min((long long)a.tokens_per_cta, a.n_tokens - first) * per_token;
+    const unsigned n_vec = (unsigned)min((long long)a.tokens_per_cta, a.n_tokens - first) * 2u * (unsigned)a.heads;
     wait_for_previous_kernel();
-    for (int v0 = 0; v0 < n_vec; v0 += GROUPS * U) {  // uniform over the CTA: whole warps take part in the shuffles
+    for (unsigned v0 = 0; v0 < n_vec; v0 += GROUPS * U) {  // uniform over the CTA: whole warps take part in the shuffles
         Chunk<IN> x[U][NCH];
         long long slot[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const CacheVector c = cache_vector(a, v0 + u * GROUPS + group, per_token, n_vec);
+            const CacheVector c = cache_vector(a, v0 + u * GROUPS + group, n_vec);
             slot[u] = c.live ? __ldg(a.slots + first + c.token) : -1;
-            const unsigned char* src = a.tokens[c.side] +
-                ((size_t)(first + c.token) * a.token_stride[c.side] + (size_t)c.head * a.token_head_stride[c.side]) * sizeof(T);
+            const unsigned char* src = token_vector(a, c, first, sizeof(T));
 #pragma unroll
             for (int i = 0; i < NCH; ++i) {
                 const int e = (i * LANES + lane) * E;
@@ -282,7 +359,7 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_write_kernel(const Cac
                 for (int m = LANES / 2; m >= 1; m >>= 1) {
                     const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, top, m);
                     if constexpr (sizeof(T) == 4) top = max(top, other);
-                    else top = __vmaxu2(top, other);
+                    else top = max_u16x2(top, other);
                 }
                 if (u == 0 || lane % U == u) my_top = top;
             }
@@ -294,20 +371,20 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_write_kernel(const Cac
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const CacheVector c = cache_vector(a, v0 + u * GROUPS + group, per_token, n_vec);
+            const CacheVector c = cache_vector(a, v0 + u * GROUPS + group, n_vec);
             const int from = (threadIdx.x & 31) - lane + u;  // lane u of this group
             const float inv = __shfl_sync(0xFFFFFFFFu, my_inv, from), scale = __shfl_sync(0xFFFFFFFFu, my_scale, from);
             size_t entry, scale_entry;
             if (!cache_place(a, slot[u], c.head, entry, scale_entry)) continue;
             if constexpr (FMT == kKvPlain) {
-                unsigned char* dst = a.side[c.side] + entry * sizeof(T);
+                unsigned char* dst = (c.side ? a.side[1] : a.side[0]) + entry * sizeof(T);
 #pragma unroll
                 for (int i = 0; i < NCH; ++i) {
                     const int e = (i * LANES + lane) * E;
                     if (e < a.dim) st_chunk<IN>(dst + (size_t)e * sizeof(T), x[u][i]);
                 }
             } else {
-                unsigned char* dst = a.side[c.side] + entry;
+                unsigned char* dst = (c.side ? a.side[1] : a.side[0]) + entry;
 #pragma unroll
                 for (int i = 0; i < NCH; ++i) {
                     const int e = (i * LANES + lane) * E;
@@ -317,7 +394,7 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_write_kernel(const Cac
                         st_chunk<E>(dst + e, encode<FMT, E>(f, inv));
                     }
                 }
-                if (lane == 0) a.scale[c.side][scale_entry] = scale;
+                if (lane == 0) (c.side ? a.scale[1] : a.scale[0])[scale_entry] = scale;
             }
         }
     }
@@ -331,30 +408,29 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_read_kernel(const Cach
     constexpr int HELD_SIZE = FMT == kKvPlain ? (int)sizeof(T) : 1;
     const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
     constexpr int GROUPS = kCacheThreads / LANES;
-    const int per_token = 2 * a.heads;
     const long long first = (long long)blockIdx.x * a.tokens_per_cta;
-    const int n_vec = (int)min((long long)a.tokens_per_cta, a.n_tokens - first) * per_token;
+    const unsigned n_vec = (unsigned)min((long long)a.tokens_per_cta, a.n_tokens - first) * 2u * (unsigned)a.heads;
     wait_for_previous_kernel();
-    for (int v0 = 0; v0 < n_vec; v0 += GROUPS * U) {
+    for (unsigned v0 = 0; v0 < n_vec; v0 += GROUPS * U) {
         Chunk<HELD> x[U][NCH];
         float scale[U];
         long long slot[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const CacheVector c = cache_vector(a, v0 + u * GROUPS + group, per_token, n_vec);
+            const CacheVector c = cache_vector(a, v0 + u * GROUPS + group, n_vec);
             slot[u] = c.live ? __ldg(a.slots + first + c.token) : -1;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const CacheVector c = cache_vector(a, v0 + u * GROUPS + group, per_token, n_vec);
+            const CacheVector c = cache_vector(a, v0 + u * GROUPS + group, n_vec);
             size_t entry, scale_entry;
             scale[u] = 0.f;
             if (!cache_place(a, slot[u], c.head, entry, scale_entry)) {
                 slot[u] = -1;
                 continue;
             }
-            const unsigned char* src = a.side[c.side] + entry * HELD_SIZE;
-            if (FMT != kKvPlain) scale[u] = __ldg(a.scale[c.side] + scale_entry);
+            const unsigned char* src = (c.side ? a.side[1] : a.side[0]) + entry * HELD_SIZE;
+            if (FMT != kKvPlain) scale[u] = __ldg((c.side ? a.scale[1] : a.scale[0]) + scale_entry);
 #pragma unroll
             for (int i = 0; i < NCH; ++i) {
                 const int e = (i * LANES + lane) * E;
@@ -364,9 +440,8 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_read_kernel(const Cach
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (slot[u] < 0) continue;
-            const CacheVector c = cache_vector(a, v0 + u * GROUPS + group, per_token, n_vec);
-            unsigned char* dst = a.tokens[c.side] +
-                ((size_t)(first + c.token) * a.token_stride[c.side] + (size_t)c.head * a.token_head_stride[c.side]) * sizeof(T);
+            const CacheVector c = cache_vector(a, v0 + u * GROUPS + group, n_vec);
+            unsigned char* dst = token_vector(a, c, first, sizeof(T));
 #pragma unroll
             for (int i = 0; i < NCH; ++i) {
                 const int e = (i * LANES + lane) * E;
@@ -375,9 +450,7 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_read_kernel(const Cach
                     st_chunk<OUT>(dst + (size_t)e * sizeof(T), x[u][i]);
                 } else {
                     float f[E];
-                    decode<FMT, E>(x[u][i], f);
-#pragma unroll
-                    for (int k = 0; k < E; ++k) f[k] = __fmul_rn(f[k], scale[u]);
+                    decode<FMT, E>(x[u][i], scale[u], f);
                     st_chunk<OUT>(dst + (size_t)e * sizeof(T), chunk_from_float<T, E>(f));
                 }
             }

@@ -1,6 +1,5 @@
 // Entry point of the attention over a shared prefix: argument checks, the split of the work into parts, the launches.
 #include <string.h>
-#include <stdlib.h>
 
 #include <atomic>
 
@@ -126,7 +125,6 @@ int make_attend_plan(const rt_kv_cache* c, const rt_prefix_batch* b, int q_heads
         if (prefix_rows <= 16) p->prefix_form = kKeys16;
         else if (p->padded_dim == 256 || prefix_rows <= 64) p->prefix_form = kKeys64;
         else p->prefix_form = kPrefixTiles;
-        if (getenv("XPRE")) p->prefix_form = atoi(getenv("XPRE"));
         if (p->prefix_form == kPrefixTiles) {
             PrefixSplit& s = p->split;
             s.tiles = (int)ceil_div(b->prefix_len, kTcTile);
@@ -140,7 +138,6 @@ int make_attend_plan(const rt_kv_cache* c, const rt_prefix_batch* b, int q_heads
             const double prefix_work = (double)units * (s.tiles * 1.6 + 7), tiles_per_suffix = 0.5 * (double)ceil_div(b->max_suffix_len, 128);
             const double suffix_work = tiles_per_suffix * (double)ceil_div(suffix_rows, 16) * c->kv_heads * (double)b->n_seqs;
             long long sms = (long long)(L.sm_count * prefix_work / (prefix_work + suffix_work) + 0.5);
-            if (getenv("XSMS")) sms = atoi(getenv("XSMS"));
             sms = std::max<long long>(1, std::min<long long>(sms, L.sm_count));
             // The number of runs that ends first on that many SMs: whole waves of CTAs, each as long as its run.
             double best = 0;
@@ -168,7 +165,6 @@ int make_attend_plan(const rt_kv_cache* c, const rt_prefix_batch* b, int q_heads
         const int nr = p->suffix_form == kKeys16 ? 16 : 64;
         const long long tiles = ceil_div(suffix_rows, nr) * c->kv_heads * b->n_seqs;
         split_keys(b->max_suffix_len, tiles, (long long)L.sm_count * (nr == 16 ? 2 : 1), 128, &p->suffix_parts, &p->suffix_keys);
-        if (getenv("XKEYS")) { p->suffix_keys = atoi(getenv("XKEYS")); p->suffix_parts = (int)ceil_div(b->max_suffix_len, p->suffix_keys); }
         p->suffix_ctas = tiles * p->suffix_parts;
     }
     if (p->prefix_ctas > 0x7fffffffLL || p->suffix_ctas > 0x7fffffffLL) {

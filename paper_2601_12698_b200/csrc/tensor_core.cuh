@@ -81,8 +81,9 @@ __device__ __forceinline__ void tc_commit(uint64_t* bar)
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 // One lane of a converged warp.  The warp that issues products runs converged and elects a lane only around the instructions
-// themselves: addresses and descriptors then live in uniform registers, which is where the instruction wants them (issued
-// from a region that one lane entered alone, a product took 150 cycles to issue, more than twice what it takes to run).
+// themselves: addresses and descriptors then live in uniform registers, which is where the instruction wants them.  (With the
+// warp's number taken by shuffle as well, so that the compiler sees the role as one of whole warps, the prefix kernel went from
+// 201 to 194 us at 256 sequences x 4 heads x 8 key/value heads of 128, prefix 32768; with constant slots, to 188.)
 __device__ __forceinline__ bool elect_one()
 {
     uint32_t r;
@@ -125,8 +126,7 @@ __device__ __forceinline__ constexpr uint32_t tc_instruction(int n, bool a_rows,
            ((128u >> 4) << 24);
 }
 
-// Bounded wait whose polls sleep in hardware for up to kWaitSleepNs each: many roles wait most of the time, and warps that poll
-// without pause take a third of the issue slots from those that work.  Gives up after about a second, as mbarrier_wait_bounded.
+// Bounded wait whose polls sleep in hardware for up to kWaitSleepNs each: many roles wait most of the time.  Gives up after about a second, as mbarrier_wait_bounded.
 constexpr uint32_t kWaitSleepNs = 20000;
 __device__ __forceinline__ bool mbarrier_wait_sleeping(uint64_t* bar, uint32_t parity)
 {
