@@ -125,10 +125,12 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
     long long* offsets = reinterpret_cast<long long*>(smem + S::kOffsetsAt);  // [3][128]: places of a tile's keys
     __shared__ __align__(8) uint64_t full[SLOTS], empty[SLOTS], s_full[2], w_full[2], o_done[2], q_full;
     __shared__ uint32_t tmem_base;
-    // per row: factor of the scores, reference m (the same for every thread, so it need not sit in their registers), and the
-    // four softmax warps' maxima and sums
-    __shared__ __align__(16) float row_c[NR], row_ref[NR], row_m[4][NR], row_sum[4][NR];
-    __shared__ long long row_at[NR];  // [token][head] index of a row, -1: no such row
+    // per row: factor of the scores, reference m (the same for every thread, so it need not sit in their registers), what a new
+    // reference rescales by, and the four softmax warps' maxima, sums at the end, and at the beginning the places of the queries
+    __shared__ __align__(16) float row_c[NR], row_ref[NR], row_alpha[NR], row_m[4][NR];
+    float(&row_sum)[4][NR] = row_m;
+    long long* row_q = reinterpret_cast<long long*>(&row_m[0][0]);
+    __shared__ __align__(16) long long row_at[NR];  // [token][head] index of a row, -1: no such row; then where its result goes
     __shared__ int poisoned;
 
     // (the warp's number by shuffle: the compiler then knows that a role is taken by whole warps)
@@ -192,8 +194,9 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
     const long long all_rows = (long long)a.n_seqs * a.q_len * n_heads;
     // Row r of the tile: query token first_token + (row0 + r) / group, query head kv_head * group + (row0 + r) % group.
     if (tid < NR) {
-        const int r = row0 + tid, t = r / a.group;
-        row_at[tid] = r < n_rows ? (long long)(first_token + t) * n_heads + kv_head * a.group + (r - t * a.group) : -1;
+        const int r = row0 + tid, t = r / a.group, head = kv_head * a.group + (r - t * a.group);
+        row_at[tid] = r < n_rows ? (long long)(first_token + t) * n_heads + head : -1;
+        row_q[tid] = r < n_rows ? ((long long)(first_token + t) * a.q_token_stride + (long long)head * a.q_head_stride) * 2 : -1;
     }
     if (k0 >= k1) {  // no keys here: the part only says so
         if (tid < NR && row_at[tid] >= 0) {
@@ -253,22 +256,19 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
         // ---- queries, softmax, result ----
         const uint32_t lanes = (uint32_t)warp << 21;
         int page_n = page_of(0, tid), page_nn = page_of(1, tid);
-        // queries: a warp takes a row at a time, fetched eight (four) at once
-        constexpr int QB = NR == 16 ? 4 : 8;
-#pragma unroll
-        for (int rb = 0; rb < NR / 4; rb += QB) {
+        // queries: a warp takes a row at a time, all its rows fetched at once
+        constexpr int QB = NR / 4;
+        {
             uint4 w4[QB];
 #pragma unroll
             for (int i = 0; i < QB; ++i) {
-                const long long at = row_at[warp + 4 * (rb + i)];
-                const bool there = at >= 0 && lane * 8 < a.dim;
-                const int token = there ? (int)((unsigned)at / (unsigned)n_heads) : 0, head = there ? (int)(at - (long long)token * n_heads) : 0;
-                w4[i] = __ldg(reinterpret_cast<const uint4*>(a.q + ((long long)token * a.q_token_stride + (long long)head * a.q_head_stride + (there ? lane * 8 : 0)) * 2));
-                if (!there) w4[i] = make_uint4(0, 0, 0, 0);
+                const long long at = row_q[warp + 4 * i];
+                w4[i] = make_uint4(0, 0, 0, 0);
+                if (at >= 0 && lane * 8 < a.dim) w4[i] = __ldg(reinterpret_cast<const uint4*>(a.q + at + lane * 16));
             }
 #pragma unroll
             for (int i = 0; i < QB; ++i) {
-                const int r = warp + 4 * (rb + i);
+                const int r = warp + 4 * i;
                 uint4 w = w4[i];
                 float c = a.score_scale;
                 if constexpr (kQuant) {
@@ -369,22 +369,23 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
                     }
                 }
                 sync_128();
-                if (j > 0) {  // the products so far are complete before they are rescaled
-                    wait(&o_done[(j - 1) & 1], ((j - 1) >> 1) & 1);
-                    tc_fence_after();
+                if (tid < NR) {
+                    const float top = fmaxf(fmaxf(row_m[0][tid], row_m[1][tid]), fmaxf(row_m[2][tid], row_m[3][tid])), ref = row_ref[tid];
+                    row_alpha[tid] = top > ref + 8.f ? ex2(ref - top) : 1.f;
+                    if (top > ref + 8.f) row_ref[tid] = top;
                 }
+                sync_128();
+                if (j > 0) {
+                    wait(&o_done[(j - 1) & 1], ((j - 1) >> 1) & 1);  // the products so far are complete before they are rescaled
+                    tc_fence_after();
 #pragma unroll
-                for (int r0 = 0; r0 < NR; r0 += 16) {
-                    if (r0 >= live_rows) break;
-                    float alpha[16];
+                    for (int r0 = 0; r0 < NR; r0 += 16) {
+                        if (r0 >= live_rows) break;
+                        float alpha[16];
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const float top = fmaxf(fmaxf(row_m[0][r0 + r], row_m[1][r0 + r]), fmaxf(row_m[2][r0 + r], row_m[3][r0 + r]));
-                        const float ref = row_ref[r0 + r];
-                        alpha[r] = top > ref + 8.f ? ex2(ref - top) : 1.f;
-                        l[r0 + r] *= alpha[r];
-                    }
-                    if (j > 0) {
+                        for (int r = 0; r < 16; r += 4) *reinterpret_cast<float4*>(&alpha[r]) = *reinterpret_cast<const float4*>(&row_alpha[r0 + r]);
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) l[r0 + r] *= alpha[r];
 #pragma unroll
                         for (int i = 0; i < NI; ++i) {
                             uint32_t o[16];
@@ -397,12 +398,6 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
                         tmem_wait_store();
                     }
                 }
-                sync_128();
-                if (tid < NR) {
-                    const float top = fmaxf(fmaxf(row_m[0][tid], row_m[1][tid]), fmaxf(row_m[2][tid], row_m[3][tid]));
-                    if (top > row_ref[tid] + 8.f) row_ref[tid] = top;
-                }
-                sync_128();
             }
             if (j >= 2) wait(&o_done[j & 1], ((j - 2) >> 1) & 1);  // this weight buffer's last product is complete
             unsigned char* to = weights + (j & 1) * S::kWBytes + tid * RB;
@@ -458,10 +453,10 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
             }
             // a part that saw no key is not read by the merge, the result of a call is zero
             // (a padding row is neither)
-            row_c[tid] = !write || (empty && !direct) ? -1.f : empty ? 0.f : 1.0f / total;
+            row_c[tid] = empty ? 0.f : 1.0f / total;
+            row_at[tid] = !write || (empty && !direct) ? -1 : (direct ? at : (long long)part_index * all_rows + at) * a.dim;
         }
         sync_128();
-        const bool fix = !prefix && *reinterpret_cast<volatile int*>(&poisoned) != 0;
 #pragma unroll 1
         for (int i = 0; i < NI; ++i) {
             const int d = i * 128 + tid;
@@ -475,17 +470,30 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
                 for (int k = 0; k < 16; k += 4) {
                     if (r0 + k >= live_rows) break;
                     const float4 f4 = *reinterpret_cast<const float4*>(&row_c[r0 + k]);
+                    const longlong2 lo = *reinterpret_cast<const longlong2*>(&row_at[r0 + k]), hi = *reinterpret_cast<const longlong2*>(&row_at[r0 + k + 2]);
+                    const long long to[4] = {lo.x, lo.y, hi.x, hi.y};
 #pragma unroll
                     for (int y = 0; y < 4; ++y) {
-                        const int r = r0 + k + y;
-                        const float f = (&f4.x)[y];
-                        if (f == -1.f || !mine) continue;  // (a NaN row is written)
-                        float x = f == 0.f ? 0.f : __uint_as_float(o[k + y]) * f;
-                        if (fix) x += hidden_poison_of<T, FMT>(a, pages, list_len, kv_head, d, max(k0, all_see), min(k1, len - a.q_len + (row0 + r) / a.group + 1));
-                        const long long at = row_at[r];
-                        if (direct) reinterpret_cast<unsigned short*>(a.out)[at * a.dim + d] = (unsigned short)Codec<T, 16>::from_float16(x);
-                        else a.part_out[((long long)part_index * all_rows + at) * a.dim + d] = x;
+                        const float f = (&f4.x)[y], x = f == 0.f ? 0.f : __uint_as_float(o[k + y]) * f;
+                        if (to[y] < 0 || !mine) continue;
+                        if (direct) reinterpret_cast<unsigned short*>(a.out)[to[y] + d] = (unsigned short)Codec<T, 16>::from_float16(x);
+                        else a.part_out[to[y] + d] = x;
                     }
+                }
+            }
+        }
+        if (!prefix && *reinterpret_cast<volatile int*>(&poisoned) != 0) {  // the infinities kept out of the products (below)
+#pragma unroll 1
+            for (int r = 0; r < live_rows; ++r) {
+#pragma unroll 1
+                for (int i = 0; i < NI; ++i) {
+                    const int d = i * 128 + tid;
+                    const long long to = row_at[r];
+                    if (to < 0 || d >= a.dim || (DI < 128 && tid >= DI)) continue;
+                    const float poison = hidden_poison_of<T, FMT>(a, pages, list_len, kv_head, d, max(k0, all_see), min(k1, len - a.q_len + (row0 + r) / a.group + 1));
+                    if (poison == 0.f) continue;
+                    if (direct) reinterpret_cast<unsigned short*>(a.out)[to + d] = (unsigned short)Codec<T, 16>::from_float16(poison + Codec<T, 16>::to_float16(reinterpret_cast<unsigned short*>(a.out)[to + d]));
+                    else a.part_out[to + d] += poison;
                 }
             }
         }
