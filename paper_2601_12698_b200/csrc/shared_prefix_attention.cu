@@ -297,7 +297,7 @@ int shared_prefix_attention_launch(const rt_kv_cache* c, const rt_prefix_batch* 
             if (st != RT_OK) return st;
         }
     }
-    if (parts != 1) st = launch(kMergeParts, ceil_div(p.tokens * q_heads, kMergePartsThreads / 32), kMergePartsThreads, &p.split);
+    if (parts != 1) st = launch(kMergeParts, ceil_div(p.tokens * q_heads * (p.padded_dim == 256 ? 2 : 1), kMergePartsThreads / 32), kMergePartsThreads, &p.split);
     return st;
 }
 
