@@ -58,13 +58,13 @@ namespace {
 
 typedef void (*CacheKernel)(CacheArgs);
 
-// Launch shape of one call: elements per lane and chunk, lanes per vector, chunks per lane.
-template <bool WRITE, typename T, int FMT, int E, int LANES, int NCH>
+// Launch shape of one call: elements per lane and chunk, elements per access, lanes per vector, chunks per lane.
+template <bool WRITE, typename T, int FMT, int E, int AL, int LANES, int NCH>
 int launch_shape(const CacheArgs& args, cudaStream_t stream)
 {
     CacheArgs a = args;
     constexpr int GROUPS = kCacheThreads / LANES;
-    constexpr int U = NCH > 1 ? 1 : E == 16 ? 2 : 4;
+    constexpr int U = NCH > 1 ? 1 : 2;
     // A CTA takes as many tokens as fill its groups: once over while the device has SMs to spare, U times once it is
     // covered (the vectors of one batch are then in flight together).
     const int per_token = 2 * a.heads;
@@ -80,31 +80,32 @@ int launch_shape(const CacheArgs& args, cudaStream_t stream)
         set_error("n_tokens=%lld needs too many CTAs", (long long)a.n_tokens);
         return RT_ERR_SHAPE;
     }
-    const CacheKernel fn = WRITE ? (deep ? (CacheKernel)kv_cache_write_kernel<T, FMT, E, LANES, NCH, U>
-                                         : (CacheKernel)kv_cache_write_kernel<T, FMT, E, LANES, NCH, 1>)
-                                 : (deep ? (CacheKernel)kv_cache_read_kernel<T, FMT, E, LANES, NCH, U>
-                                         : (CacheKernel)kv_cache_read_kernel<T, FMT, E, LANES, NCH, 1>);
+    const CacheKernel fn = WRITE ? (deep ? (CacheKernel)kv_cache_write_kernel<T, FMT, E, AL, LANES, NCH, U>
+                                         : (CacheKernel)kv_cache_write_kernel<T, FMT, E, AL, LANES, NCH, 1>)
+                                 : (deep ? (CacheKernel)kv_cache_read_kernel<T, FMT, E, AL, LANES, NCH, U>
+                                         : (CacheKernel)kv_cache_read_kernel<T, FMT, E, AL, LANES, NCH, 1>);
     void* params[] = {&a};
     return launch_kernel((const void*)fn, dim3((unsigned)ctas), dim3(kCacheThreads), 0, stream, params);
 }
 
-// Sixteen elements to a lane where sizes, strides and pointers allow it (the kernels are bound by instructions, and those that
-// find a vector's places are shared by more elements: 16384 x 8 x 128 bf16 to e4m3 took 30 us with eight), else eight, four, one.
+// Sixteen elements to a lane (the kernels are bound by instructions, and those that find a vector's places are shared by more
+// elements: 16384 x 8 x 128 bf16 to e4m3 took 30 us with eight, 20 with sixteen), in accesses as wide as sizes, strides and
+// pointers allow, the last lane's ending with the vector.  Places that are not even multiples of four elements (odd head
+// sizes): one element to a lane.
+template <bool WRITE, typename T, int FMT, int AL>
+int launch_aligned(const CacheArgs& a, cudaStream_t stream)
+{
+    if (a.dim <= 64) return launch_shape<WRITE, T, FMT, 16, AL, 4, 1>(a, stream);
+    if (a.dim <= 128) return launch_shape<WRITE, T, FMT, 16, AL, 8, 1>(a, stream);
+    return launch_shape<WRITE, T, FMT, 16, AL, 16, 1>(a, stream);
+}
 template <bool WRITE, typename T, int FMT>
 int launch_typed(const CacheArgs& a, int align_elems, cudaStream_t stream)
 {
-    if (align_elems >= 16) {
-        if (a.dim <= 64) return launch_shape<WRITE, T, FMT, 16, 4, 1>(a, stream);
-        if (a.dim <= 128) return launch_shape<WRITE, T, FMT, 16, 8, 1>(a, stream);
-        return launch_shape<WRITE, T, FMT, 16, 16, 1>(a, stream);
-    }
-    if (align_elems >= 8) {
-        if (a.dim <= 64) return launch_shape<WRITE, T, FMT, 8, 8, 1>(a, stream);
-        if (a.dim <= 128) return launch_shape<WRITE, T, FMT, 8, 16, 1>(a, stream);
-        return launch_shape<WRITE, T, FMT, 8, 32, 1>(a, stream);
-    }
-    if (align_elems >= 4) return launch_shape<WRITE, T, FMT, 4, 32, 2>(a, stream);
-    return launch_shape<WRITE, T, FMT, 1, 32, 8>(a, stream);
+    if (align_elems >= 16) return launch_aligned<WRITE, T, FMT, 16>(a, stream);
+    if (align_elems >= 8) return launch_aligned<WRITE, T, FMT, 8>(a, stream);
+    if (align_elems >= 4) return launch_aligned<WRITE, T, FMT, 4>(a, stream);
+    return launch_shape<WRITE, T, FMT, 1, 1, 32, 8>(a, stream);
 }
 
 template <bool WRITE, typename T>
@@ -117,8 +118,8 @@ int launch_format(int format, const CacheArgs& a, int align_elems, cudaStream_t 
     }
 }
 
-// Largest of 16, 8, 4, 1 such that a chunk of that many elements is aligned everywhere: chunks of token tensors want
-// min(16, elements * size) bytes, chunks of the cache min(16, elements * held size).
+// Largest of 16, 8, 4, 1 such that accesses of that many elements are aligned everywhere: those to token tensors want
+// min(16, elements * size) bytes, those to the cache min(16, elements * held size).
 int shared_alignment(const rt_kv_cache* c, const void* key, long long kts, long long khs, const void* value, long long vts,
                      long long vhs, int dtype, long long n_tokens)
 {

@@ -64,51 +64,50 @@ __device__ __forceinline__ SlotPlace place_of(long long slot, unsigned page_size
 // index * stride: two multiplications, not the three or four of a 64-bit product.
 __device__ __forceinline__ size_t times(unsigned index, long long stride) { return (size_t)index * (size_t)stride; }
 
-// E consecutive elements of type T as 32-bit words (E * sizeof(T) is 1, 2, 4, 8, 16 or 32 bytes).
+// Consecutive elements as 32-bit words.
 template <int BYTES>
 struct Chunk {
     uint32_t w[(BYTES + 3) / 4];
 };
-template <int BYTES>
-__device__ __forceinline__ Chunk<BYTES> ld_chunk(const unsigned char* p)
+// Bytes of one access to a chunk whose places are multiples of AL elements of `size` bytes.
+__host__ __device__ constexpr int access_bytes(int al, int size) { return al * size < 16 ? al * size : 16; }
+// A chunk in accesses of ACCESS bytes.  RAGGED: only the first `there` bytes exist, the rest reads as zero.
+template <int BYTES, int ACCESS, bool RAGGED>
+__device__ __forceinline__ Chunk<BYTES> ld_chunk(const unsigned char* p, int there)
 {
     Chunk<BYTES> c;
     if constexpr (BYTES == 1) {
         unsigned short h;
         asm volatile("ld.global.L1::no_allocate.u8 %0, [%1];" : "=h"(h) : "l"(p));
         c.w[0] = h;
-    } else if constexpr (BYTES > 16) {  // rows of a cache are 16-byte aligned at best
-#pragma unroll
-        for (int k = 0; k < BYTES / 16; ++k) {
-            const Vec<16> a = ld_stream<16>(p + 16 * k);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) c.w[4 * k + i] = a.w[i];
-        }
     } else {
-        const Vec<BYTES> a = ld_stream<BYTES>(p);
+        constexpr int WORDS = (ACCESS + 3) / 4;
 #pragma unroll
-        for (int i = 0; i < (BYTES + 3) / 4; ++i) c.w[i] = a.w[i];
+        for (int k = 0; k < BYTES / ACCESS; ++k) {
+            Vec<ACCESS> a;
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) a.w[i] = 0;
+            if (!RAGGED || k * ACCESS < there) a = ld_stream<ACCESS>(p + ACCESS * k);
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) c.w[WORDS * k + i] = a.w[i];
+        }
     }
     return c;
 }
-template <int BYTES>
-__device__ __forceinline__ void st_chunk(unsigned char* p, const Chunk<BYTES>& c)
+template <int BYTES, int ACCESS, bool RAGGED>
+__device__ __forceinline__ void st_chunk(unsigned char* p, const Chunk<BYTES>& c, int there)
 {
     if constexpr (BYTES == 1) {
         asm volatile("st.global.u8 [%0], %1;" ::"l"(p), "h"((unsigned short)c.w[0]) : "memory");
-    } else if constexpr (BYTES > 16) {
-#pragma unroll
-        for (int k = 0; k < BYTES / 16; ++k) {
-            Vec<16> a;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) a.w[i] = c.w[4 * k + i];
-            st_stream<16>(p + 16 * k, a);
-        }
     } else {
-        Vec<BYTES> a;
+        constexpr int WORDS = (ACCESS + 3) / 4;
 #pragma unroll
-        for (int i = 0; i < (BYTES + 3) / 4; ++i) a.w[i] = c.w[i];
-        st_stream<BYTES>(p, a);
+        for (int k = 0; k < BYTES / ACCESS; ++k) {
+            Vec<ACCESS> a;
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) a.w[i] = c.w[WORDS * k + i];
+            if (!RAGGED || k * ACCESS < there) st_stream<ACCESS>(p + ACCESS * k, a);
+        }
     }
 }
 
@@ -318,10 +317,11 @@ __device__ __forceinline__ bool cache_place(const CacheArgs& a, long long slot, 
 // The key and value vectors do not depend on the slots, so both are fetched at once.  The two divisions of a vector are
 // made by one lane for each of the U vectors at a time, not by all lanes for all of them: they are correctly rounded ones
 // (the codes are the definition's bit for bit) and cost as much as the rest of a vector.
-template <typename T, int FMT, int E, int LANES, int NCH, int U>
+template <typename T, int FMT, int E, int AL, int LANES, int NCH, int U>
 __global__ void __launch_bounds__(kCacheThreads) kv_cache_write_kernel(const CacheArgs a)
 {
-    constexpr int IN = E * (int)sizeof(T);
+    constexpr int IN = E * (int)sizeof(T), SIZE = (int)sizeof(T), CODE = FMT == kKvPlain ? SIZE : 1;
+    constexpr bool RAGGED = AL < E;
     static_assert(U <= LANES, "a lane for every vector in flight");
     const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
     constexpr int GROUPS = kCacheThreads / LANES;
@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_write_kernel(const Cac
             for (int i = 0; i < NCH; ++i) {
                 const int e = (i * LANES + lane) * E;
                 if (c.live && e < a.dim) {
-                    x[u][i] = ld_chunk<IN>(src + (size_t)e * sizeof(T));
+                    x[u][i] = ld_chunk<IN, access_bytes(AL, SIZE), RAGGED>(src + (size_t)e * SIZE, (a.dim - e) * SIZE);
                 } else {
 #pragma unroll
                     for (int k = 0; k < (IN + 3) / 4; ++k) x[u][i].w[k] = 0;
@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_write_kernel(const Cac
 #pragma unroll
                 for (int i = 0; i < NCH; ++i) {
                     const int e = (i * LANES + lane) * E;
-                    if (e < a.dim) st_chunk<IN>(dst + (size_t)e * sizeof(T), x[u][i]);
+                    if (e < a.dim) st_chunk<IN, access_bytes(AL, SIZE), RAGGED>(dst + (size_t)e * SIZE, x[u][i], (a.dim - e) * SIZE);
                 }
             } else {
                 unsigned char* dst = (c.side ? a.side[1] : a.side[0]) + entry;
@@ -391,7 +391,7 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_write_kernel(const Cac
                     if (e < a.dim) {
                         float f[E];
                         chunk_to_float<T, E>(x[u][i], f);
-                        st_chunk<E>(dst + e, encode<FMT, E>(f, inv));
+                        st_chunk<E, access_bytes(AL, CODE), RAGGED>(dst + e, encode<FMT, E>(f, inv), a.dim - e);
                     }
                 }
                 if (lane == 0) (c.side ? a.scale[1] : a.scale[0])[scale_entry] = scale;
@@ -400,10 +400,11 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_write_kernel(const Cac
     }
 }
 
-template <typename T, int FMT, int E, int LANES, int NCH, int U>
+template <typename T, int FMT, int E, int AL, int LANES, int NCH, int U>
 __global__ void __launch_bounds__(kCacheThreads) kv_cache_read_kernel(const CacheArgs a)
 {
-    constexpr int OUT = E * (int)sizeof(T);
+    constexpr int OUT = E * (int)sizeof(T), SIZE = (int)sizeof(T);
+    constexpr bool RAGGED = AL < E;
     constexpr int HELD = FMT == kKvPlain ? OUT : E;
     constexpr int HELD_SIZE = FMT == kKvPlain ? (int)sizeof(T) : 1;
     const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
@@ -434,7 +435,7 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_read_kernel(const Cach
 #pragma unroll
             for (int i = 0; i < NCH; ++i) {
                 const int e = (i * LANES + lane) * E;
-                if (e < a.dim) x[u][i] = ld_chunk<HELD>(src + (size_t)e * HELD_SIZE);
+                if (e < a.dim) x[u][i] = ld_chunk<HELD, access_bytes(AL, HELD_SIZE), RAGGED>(src + (size_t)e * HELD_SIZE, (a.dim - e) * HELD_SIZE);
             }
         }
 #pragma unroll
@@ -447,11 +448,11 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_read_kernel(const Cach
                 const int e = (i * LANES + lane) * E;
                 if (e >= a.dim) continue;
                 if constexpr (FMT == kKvPlain) {
-                    st_chunk<OUT>(dst + (size_t)e * sizeof(T), x[u][i]);
+                    st_chunk<OUT, access_bytes(AL, SIZE), RAGGED>(dst + (size_t)e * SIZE, x[u][i], (a.dim - e) * SIZE);
                 } else {
                     float f[E];
                     decode<FMT, E>(x[u][i], scale[u], f);
-                    st_chunk<OUT>(dst + (size_t)e * sizeof(T), chunk_from_float<T, E>(f));
+                    st_chunk<OUT, access_bytes(AL, SIZE), RAGGED>(dst + (size_t)e * SIZE, chunk_from_float<T, E>(f), (a.dim - e) * SIZE);
                 }
             }
         }
