@@ -103,9 +103,11 @@ def test_write_then_read_matches_the_definition(B, dtype, fmt, n, heads, dim, pa
         assert torch.equal(base[0][..., dim:], before[0][..., dim:])
     # read back, out of order, one slot twice, a padded row left as it was
     order = torch.cat([slots[slots >= 0].flip(0), slots[slots >= 0][:1], torch.tensor([-1], device="cuda")])
-    k_out = torch.full((order.shape[0], heads, dim + 8), 5.0, dtype=TD[dtype], device="cuda")[..., :dim]
+    wide = torch.full((order.shape[0], heads, dim + 8), 5.0, dtype=TD[dtype], device="cuda")
+    k_out = wide[..., :dim]
     v_out = torch.full((order.shape[0], heads, dim), 5.0, dtype=TD[dtype], device="cuda")
     B.kv_cache_read_launch(cache, order, k_out, v_out)
+    assert bool((wide[..., dim:] == 5.0).all())
     for out, held, scale in ((k_out, cache.k, cache.k_scale), (v_out, cache.v, cache.v_scale)):
         assert bool((out[-1] == 5.0).all())
         rows = (held if fmt == "plain" else held.view(torch.uint8)).reshape(-1, heads, dim)[order[:-1]].cpu()
@@ -116,6 +118,13 @@ def test_write_then_read_matches_the_definition(B, dtype, fmt, n, heads, dim, pa
             want = R.dequantise(rows.view(R.CODE_TYPE[fmt]), unit).float().to(TD[dtype])  # one binary32 product, rounded once
             assert R.same(out[:-1].cpu(), want)
     assert B.rt_device_status() == 0
+
+
+@pytest.mark.parametrize("fmt", ["plain", "e4m3", "int8"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("dim", [4, 8, 12, 16, 20, 24, 40, 48, 60, 68, 72, 112, 124, 132, 136, 144, 248, 252])
+def test_vectors_that_end_inside_a_lanes_share(B, dtype, fmt, dim):
+    test_write_then_read_matches_the_definition(B, dtype, fmt, 37, 3, dim, 5, "gap" if dim % 16 else "token", dim % 3 == 0)
 
 
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])

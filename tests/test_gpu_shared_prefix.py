@@ -130,6 +130,8 @@ SHAPES = [  # lens, prefix, heads, kv_heads, dim, page, q_len
     ([600, 599, 1], 300, 5, 5, 64, 128, 16),
     ([7, 12], 20, 40, 8, 128, 7, 1),
     ([1, 2, 3, 4, 5, 6, 7, 8, 9, 10] * 7, 129, 16, 2, 64, 16, 1),
+    ([75], 300, 16, 1, 64, 16, 3),
+    ([300], 400, 24, 1, 256, 16, 2),
 ]
 
 
@@ -319,6 +321,9 @@ def test_refusals(B):
     with pytest.raises(B.TunerError) as e:
         launch(p.cache, p.batch, odd, out)
     assert e.value.status == B.RT_ERR_ALIGN
+    with pytest.raises(B.TunerError) as e:  # no pages at all
+        launch(B.KvCache.allocate(0, 16, 2, 64, torch.bfloat16), p.batch, q, out, workspace=torch.empty(1 << 20, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == B.RT_ERR_SHAPE
     assert B.rt_launch_count() == before
     for kw in ({"prefix_pages": p.prefix_pages.cuda().long()}, {"page_table": p.table.cuda()[:1]}, {"suffix_lens": p.dev_lens.long()},
                {"suffix_lens": p.dev_lens.cpu()}):
@@ -394,6 +399,9 @@ MANY = [  # seqs, prefix, heads, kv_heads, dim, page, q_len
     (64, 1537, 16, 4, 128, 1, 1),
     (9, 3000, 40, 8, 80, 16, 5),        # 225 rows, prefix ends inside a tile and a page
     (20, 130, 64, 1, 128, 128, 1),      # 1280 rows of one key/value head
+    (40, 700, 8, 2, 256, 16, 1),        # heads of 256: 64 rows at a time, keys first
+    (11, 500, 16, 2, 240, 24, 2),
+    (4, 600, 64, 2, 128, 16, 2),        # 64 rows to a suffix
 ]
 
 
