@@ -10,6 +10,7 @@ namespace rt {
 // one part in 32; the outputs of the parts are then fetched U at a time, independently of one another (the parts come out of
 // L2, so what counts is how many of its round trips follow one another).  A row of DP = 64 takes half a warp's lanes, so that
 // two parts are fetched at once; a row of DP = 256 takes two warps, one for each half.  Parts that saw no key are not read.
+// Bound by latency: 8 parts of 1024 rows of 256 (8.4 MB) take about 8 us under the profiler, which empties the caches.
 constexpr int kMergePartsThreads = 128;
 template <typename T, int DP>
 __global__ void __launch_bounds__(kMergePartsThreads) merge_parts_kernel(const AttendArgs a, const PrefixSplit split)

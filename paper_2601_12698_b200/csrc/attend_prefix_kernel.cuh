@@ -13,7 +13,8 @@
 //   warps 8-11       fetch the paged tiles: keys and values with cp.async, 16 bytes a piece, into the 128-byte-swizzled
 //                    layout that the matrix unit reads (pages may have any size, so one copy per row is the widest that
 //                    always works); quantised tiles are fetched into registers, turned into fp16 and stored;
-//   warps 12, 13     issue the matrix products, each for its stream;
+//   warps 12, 13     issue the matrix products, each for its stream (half a tile of 64 keys at a time, so that one half's
+//                    products run while the other is exponentiated);
 //   warps 14, 15     look up the pages and scales of the tiles to come.
 // The two streams take turns on the tensor cores: while one's scores are exponentiated the other's products run.  Blocks of
 // more than 128 rows (wide form): a stream is one half of the rows, both use the same tiles.  Blocks of up to 128 rows
@@ -27,6 +28,12 @@
 //
 // Bounds: 4 * 128 * 128 * dim flops and 128 * 128 exponentials per tile and stream; at dim 128 the tensor cores need 1024
 // cycles for that and the SM's 16 exponentials a cycle 1024 as well.
+//
+// Measured: 1024 rows x 8 key/value heads of 128, prefix 32768, bf16: 177 us with the rest of the call for 137 GFLOP, 0.78 PFLOP/s
+// or 0.48 of the measured matrix rate (steps: both streams' whole tiles in turn 217, CTAs that share tiles numbered
+// together 201, the warp's number by shuffle 194, constant slots 188, an issuing warp per stream 177).  e4m3 codes: 241 us, the
+// scales' products and sums in the softmax warps.  256 rows: 71 us, heads of 64: 162 us (half the flops for the same
+// exponentials).
 #pragma once
 
 #include "attend_common.cuh"

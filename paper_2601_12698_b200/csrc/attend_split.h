@@ -11,7 +11,7 @@ constexpr int kTcBlockRows = 256;  // rows per CTA
 
 // A CTA takes one key/value head, one block of its rows and one run of key tiles.  CTAs are numbered with the block fastest: those
 // that read the same tiles run at the same time and share them in L2 (numbered the other way, a prefix of 32768 tokens for 1024
-// rows per key/value head was read from memory almost four times, 504 MB instead of 134).
+// rows per key/value head was read from memory almost four times, 504 MB instead of 137).
 struct PrefixSplit {
     int tiles;   // key tiles of the prefix
     int blocks;  // row blocks per key/value head

@@ -8,8 +8,12 @@
 // the vector is touched once.  A CTA takes the 2 * kv_heads vectors (keys, then values) of a few consecutive tokens:
 // neighbouring groups then read neighbouring heads of one token.
 //
-// Both kernels are bound by HBM at the large sizes and by one round of latency (slot, then vector, then store) at the
-// small ones.  U vectors per group are loaded before the first is used.
+// The large sizes want HBM's time and come near it once little is done per element: with 8 elements to a lane, 64-bit products for
+// every place and conversions one at a time, the write kernel issued 26.6 M warp instructions for 16384 tokens x 8 heads of
+// 128 (0.79 a cycle and scheduler) and took 30 us; with 16 elements to a lane, places in 32-bit factors and packed products and
+// conversions it takes 19.6 us (write) and 19.8 us (read) when repeated on the same tensors, 22.3 and 22.1 us on tensors that
+// have left L2: 102 MB at 4.6 TB/s, 0.70 of the measured copy bandwidth.  The small ones take one round of latency (slot, then
+// vector, then store): 1.8 us a launch in a graph for 64 tokens.  U vectors per group are loaded before the first is used.
 #pragma once
 
 #include <cuda_fp8.h>
