@@ -39,8 +39,8 @@ struct AttendArgs {
     float score_scale;                        // softmax_scale * log2(e)
     int prefix_parts, prefix_keys;            // parts of the prefix and keys in each (the last may have fewer)
     int suffix_parts, suffix_keys;
-    int after_prefix;   // the suffix kernel runs beside the prefix kernel that was launched before it
-    int before_suffix;  // set in that prefix kernel's arguments
+    int before_suffix;  // for the prefix kernel: the suffix kernel is launched behind it
+    int after_prefix;   // for the suffix kernel: it runs beside that prefix kernel
     float* part_out;  // [part][token][head][dim]
     float* part_lse;  // [part][token][head]
     void* out;        // [token][head][dim]

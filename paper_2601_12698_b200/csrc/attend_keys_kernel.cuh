@@ -20,7 +20,7 @@
 // 256 take two items a side.  With NR = 16 two CTAs share an SM, so that one streams while the other begins or ends.
 //
 // NR = 64 (one CTA per SM) serves heads of 256 with many rows, whose two streams would not fit tensor memory in
-// attend_prefix_kernel.
+// attend_prefix_kernel, and suffixes that many rows of their sequence read.
 //
 // Measured: 256 suffixes of 1 .. 2048 keys x 8 heads of 128, bf16 (1.07 GB): 206 us with the rest of the call, 5.2 TB/s; the same in
 // e4m3 (0.55 GB): 247 us, bound by the chain from a tile's codes to its product, not by any unit (64 suffixes: the schedulers issue
@@ -165,7 +165,6 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
     }
     const bool beside_prefix = a.after_prefix != 0;  // that of another launch
     if (!beside_prefix) wait_for_previous_kernel();
-    if (a.before_suffix) let_next_kernel_start();
     const auto leave = [&]() {
         if (beside_prefix && blockIdx.x == 0) wait_for_previous_kernel();
     };

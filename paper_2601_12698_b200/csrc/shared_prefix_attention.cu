@@ -122,9 +122,11 @@ int make_attend_plan(const rt_kv_cache* c, const rt_prefix_batch* b, int q_heads
     p->prefix_form = p->suffix_form = -1;
     const long long prefix_rows = p->tokens * p->group, suffix_rows = (long long)b->q_len * p->group;
     if (b->prefix_len > 0) {
-        if (prefix_rows <= 16) p->prefix_form = kKeys16;
-        else if (p->padded_dim == 256 || prefix_rows <= 64) p->prefix_form = kKeys64;
-        else p->prefix_form = kPrefixTiles;
+        // Heads up to 128: 16 rows to a CTA and one launch with the suffixes up to 64 rows (64 rows, prefix 8192, int8: 31 us, 37 with
+        // the tiles kernel, 34 with 64 rows to a CTA; 96 rows: 42, 37 and 46).  Heads of 256: 64 rows to a CTA (128 rows, prefix 8192:
+        // 57 us, 103 with 16), but for few rows and keys (32 rows, prefix 600: 12.1 us with 16, 14.4 with 64; prefix 8192: 37.4 and 31.4).
+        if (p->padded_dim == 256) p->prefix_form = prefix_rows <= 32 && b->prefix_len <= 2048 ? kKeys16 : kKeys64;
+        else p->prefix_form = prefix_rows <= 64 ? kKeys16 : kPrefixTiles;
         if (p->prefix_form == kPrefixTiles) {
             PrefixSplit& s = p->split;
             s.tiles = (int)ceil_div(b->prefix_len, kTcTile);
@@ -161,7 +163,11 @@ int make_attend_plan(const rt_kv_cache* c, const rt_prefix_batch* b, int q_heads
         }
     }
     if (b->max_suffix_len > 0) {
-        p->suffix_form = suffix_rows <= 32 ? kKeys16 : kKeys64;
+        // Of the prefix's form, and then in its launch, where that is keys first.  Otherwise 16 rows to a CTA up to three times that
+        // many (heads of 128, 40 suffixes of 1 .. 700 keys: 48 rows 72 us, 68 with 64 to a CTA; in int8 68 and 74; 64 rows 93 and
+        // 81), for heads of 256 up to 16 (20 rows: 110 us, 73 with 64).
+        if (p->prefix_form > kPrefixTiles) p->suffix_form = p->prefix_form;
+        else p->suffix_form = suffix_rows <= (p->padded_dim == 256 ? 16 : 48) ? kKeys16 : kKeys64;
         const int nr = p->suffix_form == kKeys16 ? 16 : 64;
         const long long tiles = ceil_div(suffix_rows, nr) * c->kv_heads * b->n_seqs;
         // Two CTAs of 16 rows share an SM; beside the tiles kernel, which takes SMs of its own, fewer and longer parts are better
@@ -170,7 +176,7 @@ int make_attend_plan(const rt_kv_cache* c, const rt_prefix_batch* b, int q_heads
         split_keys(b->max_suffix_len, tiles, (long long)L.sm_count * (pairs ? 2 : 1), 128, &p->suffix_parts, &p->suffix_keys);
         p->suffix_ctas = tiles * p->suffix_parts;
     }
-    if (p->prefix_ctas > 0x7fffffffLL || p->suffix_ctas > 0x7fffffffLL) {
+    if (p->prefix_ctas + p->suffix_ctas > 0x7fffffffLL) {
         set_error("the batch needs too many CTAs");
         return RT_ERR_SHAPE;
     }
@@ -284,25 +290,16 @@ int shared_prefix_attention_launch(const rt_kv_cache* c, const rt_prefix_batch* 
         void* params[] = {&a, second};
         return launch_form(k, form, dtype, c->format, p.padded_dim, ctas, threads, s, params);
     };
-    if (p.prefix_form == p.suffix_form && p.prefix_form >= 0 && p.prefix_ctas + p.suffix_ctas <= 0x7fffffffLL) {
-        int prefix_ctas = (int)p.prefix_ctas;  // one launch serves both
-        st = launch(p.prefix_form, p.prefix_ctas + p.suffix_ctas, kKeysThreads, &prefix_ctas);
+    int prefix_ctas = p.prefix_form > kPrefixTiles ? (int)p.prefix_ctas : 0;
+    if (p.prefix_form == kPrefixTiles) {
+        a.before_suffix = a.after_prefix = p.suffix_form >= 0;
+        st = launch(kPrefixTiles, p.prefix_ctas, kTcThreads, &p.split);
         if (st != RT_OK) return st;
-    } else {
-        if (p.prefix_form >= 0) {
-            int prefix_ctas = (int)p.prefix_ctas;
-            a.before_suffix = p.suffix_form >= 0;
-            if (p.prefix_form == kPrefixTiles) st = launch(kPrefixTiles, p.prefix_ctas, kTcThreads, &p.split);
-            else st = launch(p.prefix_form, p.prefix_ctas, kKeysThreads, &prefix_ctas);
-            if (st != RT_OK) return st;
-        }
-        if (p.suffix_form >= 0) {
-            int prefix_ctas = 0;
-            a.after_prefix = p.prefix_form >= 0;
-            a.before_suffix = 0;
-            st = launch(p.suffix_form, p.suffix_ctas, kKeysThreads, &prefix_ctas);
-            if (st != RT_OK) return st;
-        }
+    }
+    const int keys_form = p.suffix_form >= 0 ? p.suffix_form : prefix_ctas > 0 ? p.prefix_form : -1;
+    if (keys_form >= 0) {  // suffixes, and the prefix where it takes the same form
+        st = launch(keys_form, prefix_ctas + p.suffix_ctas, kKeysThreads, &prefix_ctas);
+        if (st != RT_OK) return st;
     }
     if (parts != 1) st = launch(kMergeParts, ceil_div(p.tokens * q_heads * (p.padded_dim == 256 ? 2 : 1), kMergePartsThreads / 32), kMergePartsThreads, &p.split);
     return st;
