@@ -58,13 +58,13 @@ namespace {
 
 typedef void (*CacheKernel)(CacheArgs);
 
-// Launch shape of one call: elements per lane and chunk, elements per access, lanes per vector, chunks per lane.
-template <bool WRITE, typename T, int FMT, int E, int AL, int LANES, int NCH>
+// Launch shape of one call: elements per lane, elements per access, lanes per vector.
+template <bool WRITE, typename T, int FMT, int E, int AL, int LANES>
 int launch_shape(const CacheArgs& args, cudaStream_t stream)
 {
     CacheArgs a = args;
     constexpr int GROUPS = kCacheThreads / LANES;
-    constexpr int U = NCH > 1 ? 1 : 2;
+    constexpr int U = 2;
     // A CTA takes as many tokens as fill its groups: once over while the device has SMs to spare, U times once it is
     // covered (the vectors of one batch are then in flight together).
     const int per_token = 2 * a.heads;
@@ -72,7 +72,7 @@ int launch_shape(const CacheArgs& args, cudaStream_t stream)
     int st = current_limits(&L);
     if (st != RT_OK) return st;
     const long long groups_wanted = a.n_tokens * per_token;
-    const bool deep = U > 1 && groups_wanted > (long long)L.sm_count * 4 * GROUPS;
+    const bool deep = groups_wanted > (long long)L.sm_count * 4 * GROUPS;
     const int want = GROUPS * (deep ? U : 1);
     a.tokens_per_cta = std::max(1, want / per_token);
     const long long ctas = (a.n_tokens + a.tokens_per_cta - 1) / a.tokens_per_cta;
@@ -80,10 +80,10 @@ int launch_shape(const CacheArgs& args, cudaStream_t stream)
         set_error("n_tokens=%lld needs too many CTAs", (long long)a.n_tokens);
         return RT_ERR_SHAPE;
     }
-    const CacheKernel fn = WRITE ? (deep ? (CacheKernel)kv_cache_write_kernel<T, FMT, E, AL, LANES, NCH, U>
-                                         : (CacheKernel)kv_cache_write_kernel<T, FMT, E, AL, LANES, NCH, 1>)
-                                 : (deep ? (CacheKernel)kv_cache_read_kernel<T, FMT, E, AL, LANES, NCH, U>
-                                         : (CacheKernel)kv_cache_read_kernel<T, FMT, E, AL, LANES, NCH, 1>);
+    const CacheKernel fn = WRITE ? (deep ? (CacheKernel)kv_cache_write_kernel<T, FMT, E, AL, LANES, U>
+                                         : (CacheKernel)kv_cache_write_kernel<T, FMT, E, AL, LANES, 1>)
+                                 : (deep ? (CacheKernel)kv_cache_read_kernel<T, FMT, E, AL, LANES, U>
+                                         : (CacheKernel)kv_cache_read_kernel<T, FMT, E, AL, LANES, 1>);
     void* params[] = {&a};
     return launch_kernel((const void*)fn, dim3((unsigned)ctas), dim3(kCacheThreads), 0, stream, params);
 }
@@ -91,13 +91,14 @@ int launch_shape(const CacheArgs& args, cudaStream_t stream)
 // Sixteen elements to a lane (the kernels are bound by instructions, and those that find a vector's places are shared by more
 // elements: 16384 x 8 x 128 bf16 to e4m3 took 30 us with eight, 20 with sixteen), in accesses as wide as sizes, strides and
 // pointers allow, the last lane's ending with the vector.  Places that are not even multiples of four elements (odd head
-// sizes): one element to a lane.
+// sizes): accesses of one element, eight to a lane, neighbouring elements in neighbouring lanes (16384 x 8 x 33 bf16 to e4m3: 19
+// us, 83 with one element to a lane).
 template <bool WRITE, typename T, int FMT, int AL>
 int launch_aligned(const CacheArgs& a, cudaStream_t stream)
 {
-    if (a.dim <= 64) return launch_shape<WRITE, T, FMT, 16, AL, 4, 1>(a, stream);
-    if (a.dim <= 128) return launch_shape<WRITE, T, FMT, 16, AL, 8, 1>(a, stream);
-    return launch_shape<WRITE, T, FMT, 16, AL, 16, 1>(a, stream);
+    if (a.dim <= 64) return launch_shape<WRITE, T, FMT, 16, AL, 4>(a, stream);
+    if (a.dim <= 128) return launch_shape<WRITE, T, FMT, 16, AL, 8>(a, stream);
+    return launch_shape<WRITE, T, FMT, 16, AL, 16>(a, stream);
 }
 template <bool WRITE, typename T, int FMT>
 int launch_typed(const CacheArgs& a, int align_elems, cudaStream_t stream)
@@ -105,7 +106,9 @@ int launch_typed(const CacheArgs& a, int align_elems, cudaStream_t stream)
     if (align_elems >= 16) return launch_aligned<WRITE, T, FMT, 16>(a, stream);
     if (align_elems >= 8) return launch_aligned<WRITE, T, FMT, 8>(a, stream);
     if (align_elems >= 4) return launch_aligned<WRITE, T, FMT, 4>(a, stream);
-    return launch_shape<WRITE, T, FMT, 1, 1, 32, 8>(a, stream);
+    if (a.dim <= 64) return launch_shape<WRITE, T, FMT, 8, 1, 8>(a, stream);
+    if (a.dim <= 128) return launch_shape<WRITE, T, FMT, 8, 1, 16>(a, stream);
+    return launch_shape<WRITE, T, FMT, 8, 1, 32>(a, stream);
 }
 
 template <bool WRITE, typename T>

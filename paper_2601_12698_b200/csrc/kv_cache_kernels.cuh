@@ -4,7 +4,7 @@
 //   read:   x_j = round(code_j * scale)
 //
 // An entry is a vector of head_dim elements.  A group of LANES lanes (a power of two, at most a warp) holds one vector in
-// registers, E elements to a lane and chunk, so that the largest magnitude is found with shuffles inside the group and
+// registers, E elements to a lane, so that the largest magnitude is found with shuffles inside the group and
 // the vector is touched once.  A CTA takes the 2 * kv_heads vectors (keys, then values) of a few consecutive tokens:
 // neighbouring groups then read neighbouring heads of one token.
 //
@@ -71,46 +71,63 @@ __device__ __forceinline__ size_t times(unsigned index, long long stride) { retu
 // Consecutive elements as 32-bit words.
 template <int BYTES>
 struct Chunk {
-    uint32_t w[(BYTES + 3) / 4];
+    uint32_t w[BYTES / 4];
 };
-// Bytes of one access to a chunk whose places are multiples of AL elements of `size` bytes.
+// Bytes of one access to a chunk whose places are multiples of AL elements of `size` bytes, and from one access to the next: a
+// lane's elements are neighbours, but for accesses of one element, where the neighbours are other lanes'.
 __host__ __device__ constexpr int access_bytes(int al, int size) { return al * size < 16 ? al * size : 16; }
-// A chunk in accesses of ACCESS bytes.  RAGGED: only the first `there` bytes exist, the rest reads as zero.
-template <int BYTES, int ACCESS, bool RAGGED>
+__host__ __device__ constexpr int access_stride(int al, int size, int lanes) { return al == 1 ? lanes * size : access_bytes(al, size); }
+// A chunk in accesses of ACCESS bytes, STRIDE bytes apart.  RAGGED: accesses from byte `there` on do not exist, they read as zero.
+template <int BYTES, int ACCESS, int STRIDE, bool RAGGED>
 __device__ __forceinline__ Chunk<BYTES> ld_chunk(const unsigned char* p, int there)
 {
     Chunk<BYTES> c;
-    if constexpr (BYTES == 1) {
-        unsigned short h;
-        asm volatile("ld.global.L1::no_allocate.u8 %0, [%1];" : "=h"(h) : "l"(p));
-        c.w[0] = h;
+    if constexpr (ACCESS < 4) {  // lanes and accesses share sectors: these loads go through L1
+#pragma unroll
+        for (int k = 0; k < BYTES / ACCESS; ++k) {
+            uint32_t x = 0;
+            if (k * STRIDE < there) {
+                if constexpr (ACCESS == 1) x = *(p + STRIDE * k);
+                else x = *reinterpret_cast<const unsigned short*>(p + STRIDE * k);
+            }
+            constexpr int PER = 4 / ACCESS;
+            c.w[k / PER] = k % PER == 0 ? x : c.w[k / PER] | x << (k % PER * 8 * ACCESS);
+        }
     } else {
-        constexpr int WORDS = (ACCESS + 3) / 4;
+        constexpr int WORDS = ACCESS / 4;
 #pragma unroll
         for (int k = 0; k < BYTES / ACCESS; ++k) {
             Vec<ACCESS> a;
 #pragma unroll
             for (int i = 0; i < WORDS; ++i) a.w[i] = 0;
-            if (!RAGGED || k * ACCESS < there) a = ld_stream<ACCESS>(p + ACCESS * k);
+            if (!RAGGED || k * STRIDE < there) a = ld_stream<ACCESS>(p + STRIDE * k);
 #pragma unroll
             for (int i = 0; i < WORDS; ++i) c.w[WORDS * k + i] = a.w[i];
         }
     }
     return c;
 }
-template <int BYTES, int ACCESS, bool RAGGED>
+template <int BYTES, int ACCESS, int STRIDE, bool RAGGED>
 __device__ __forceinline__ void st_chunk(unsigned char* p, const Chunk<BYTES>& c, int there)
 {
-    if constexpr (BYTES == 1) {
-        asm volatile("st.global.u8 [%0], %1;" ::"l"(p), "h"((unsigned short)c.w[0]) : "memory");
+    if constexpr (ACCESS < 4) {
+#pragma unroll
+        for (int k = 0; k < BYTES / ACCESS; ++k) {
+            constexpr int PER = 4 / ACCESS;
+            const uint32_t x = c.w[k / PER] >> (k % PER * 8 * ACCESS);
+            if (k * STRIDE < there) {
+                if constexpr (ACCESS == 1) *(p + STRIDE * k) = (unsigned char)x;
+                else *reinterpret_cast<unsigned short*>(p + STRIDE * k) = (unsigned short)x;
+            }
+        }
     } else {
-        constexpr int WORDS = (ACCESS + 3) / 4;
+        constexpr int WORDS = ACCESS / 4;
 #pragma unroll
         for (int k = 0; k < BYTES / ACCESS; ++k) {
             Vec<ACCESS> a;
 #pragma unroll
             for (int i = 0; i < WORDS; ++i) a.w[i] = c.w[WORDS * k + i];
-            if (!RAGGED || k * ACCESS < there) st_stream<ACCESS>(p + ACCESS * k, a);
+            if (!RAGGED || k * STRIDE < there) st_stream<ACCESS>(p + STRIDE * k, a);
         }
     }
 }
@@ -121,8 +138,6 @@ __device__ __forceinline__ void chunk_to_float(const Chunk<E * (int)sizeof(T)>& 
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
         for (int i = 0; i < E; ++i) f[i] = __uint_as_float(c.w[i]);
-    } else if constexpr (E == 1) {
-        f[0] = Codec<T, 16>::to_float16(c.w[0] & 0xFFFFu);
     } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) {
@@ -145,8 +160,6 @@ __device__ __forceinline__ Chunk<E * (int)sizeof(T)> chunk_from_float(const floa
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
         for (int i = 0; i < E; ++i) c.w[i] = __float_as_uint(f[i]);
-    } else if constexpr (E == 1) {
-        c.w[0] = Codec<T, 16>::from_float16(f[0]);
     } else {
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) c.w[i] = Codec<T, 16>::from_float16x2(f[2 * i], f[2 * i + 1]);
@@ -165,14 +178,15 @@ __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b)
 // infinity and then NaN on top, so an integer maximum propagates both.  16-bit types keep two running maxima in one
 // word (joined by magnitude_of at the end).
 template <typename T, int BYTES>
-__device__ __forceinline__ uint32_t join_magnitude(uint32_t top, const Chunk<BYTES>& c)
+__device__ __forceinline__ uint32_t join_magnitude(const Chunk<BYTES>& c)
 {
+    uint32_t top = 0;
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
         for (int i = 0; i < BYTES / 4; ++i) top = max(top, c.w[i] & 0x7FFFFFFFu);
     } else {
 #pragma unroll
-        for (int i = 0; i < (BYTES + 3) / 4; ++i) top = max_u16x2(top, c.w[i] & 0x7FFF7FFFu);
+        for (int i = 0; i < BYTES / 4; ++i) top = max_u16x2(top, c.w[i] & 0x7FFF7FFFu);
     }
     return top;
 }
@@ -216,30 +230,25 @@ template <int FMT, int E>
 __device__ __forceinline__ Chunk<E> encode(const float (&f)[E], float inv)
 {
     Chunk<E> c;
-    if constexpr (E == 1) {
-        if constexpr (FMT == kKvE4m3) c.w[0] = __nv_cvt_float_to_fp8(__fmul_rn(f[0], inv), __NV_SATFINITE, __NV_E4M3);
-        else c.w[0] = __float_as_uint(__fadd_rn(__fmul_rn(f[0], inv), 12582912.0f)) & 0xFFu;
-    } else {
-        const float2x inv2 = pack_f2(inv, inv);
+    const float2x inv2 = pack_f2(inv, inv);
 #pragma unroll
-        for (int i = 0; i < E; i += 4) {
-            float x[4];
-            float2x a = mul_f2(pack_f2(f[i], f[i + 1]), inv2), b = mul_f2(pack_f2(f[i + 2], f[i + 3]), inv2);
-            if constexpr (FMT == kKvE4m3) {
-                unpack_f2(a, x[0], x[1]);
-                unpack_f2(b, x[2], x[3]);
-                asm("{\n\t.reg .b16 lo, hi;\n\tcvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\tmov.b32 %0, {lo, hi};\n\t}"
-                    : "=r"(c.w[i / 4]) : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]));
-            } else {
-                // |x * inv| <= 127 after rounding, so adding 1.5 * 2^23 leaves the nearest even integer in the low byte
-                // (added one by one: a packed addition behind a packed product came out as one rounding, not two)
-                unpack_f2(a, x[0], x[1]);
-                unpack_f2(b, x[2], x[3]);
+    for (int i = 0; i < E; i += 4) {
+        float x[4];
+        float2x a = mul_f2(pack_f2(f[i], f[i + 1]), inv2), b = mul_f2(pack_f2(f[i + 2], f[i + 3]), inv2);
+        if constexpr (FMT == kKvE4m3) {
+            unpack_f2(a, x[0], x[1]);
+            unpack_f2(b, x[2], x[3]);
+            asm("{\n\t.reg .b16 lo, hi;\n\tcvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\tmov.b32 %0, {lo, hi};\n\t}"
+                : "=r"(c.w[i / 4]) : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]));
+        } else {
+            // |x * inv| <= 127 after rounding, so adding 1.5 * 2^23 leaves the nearest even integer in the low byte
+            // (added one by one: a packed addition behind a packed product came out as one rounding, not two)
+            unpack_f2(a, x[0], x[1]);
+            unpack_f2(b, x[2], x[3]);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) x[k] = __fadd_rn(x[k], 12582912.0f);
-                c.w[i / 4] = __byte_perm(__byte_perm(__float_as_uint(x[0]), __float_as_uint(x[1]), 0x0040),
-                                         __byte_perm(__float_as_uint(x[2]), __float_as_uint(x[3]), 0x0040), 0x5410);
-            }
+            for (int k = 0; k < 4; ++k) x[k] = __fadd_rn(x[k], 12582912.0f);
+            c.w[i / 4] = __byte_perm(__byte_perm(__float_as_uint(x[0]), __float_as_uint(x[1]), 0x0040),
+                                     __byte_perm(__float_as_uint(x[2]), __float_as_uint(x[3]), 0x0040), 0x5410);
         }
     }
     return c;
@@ -248,33 +257,26 @@ __device__ __forceinline__ Chunk<E> encode(const float (&f)[E], float inv)
 template <int FMT, int E>
 __device__ __forceinline__ void decode(const Chunk<E>& c, float scale, float (&f)[E])
 {
-    if constexpr (E == 1) {
-        const uint32_t b = c.w[0] & 0xFFu;
-        if constexpr (FMT == kKvE4m3) f[0] = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)b, __NV_E4M3)));
-        else f[0] = (float)(signed char)b;
-        f[0] = __fmul_rn(f[0], scale);
-    } else {
-        const float2x scale2 = pack_f2(scale, scale);
+    const float2x scale2 = pack_f2(scale, scale);
 #pragma unroll
-        for (int i = 0; i < E; i += 4) {
-            float x[4];
-            if constexpr (FMT == kKvE4m3) {
-                uint32_t lo, hi;
-                asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
-                    : "=r"(lo), "=r"(hi) : "r"(c.w[i / 4]));
-                const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&lo)), q = __half22float2(*reinterpret_cast<const __half2*>(&hi));
-                x[0] = p.x; x[1] = p.y; x[2] = q.x; x[3] = q.y;
-            } else {
-                // 2^23 + (code + 128) as binary32 bits, minus 2^23 + 128: exact
-                const uint32_t w = c.w[i / 4] ^ 0x80808080u;
-                x[0] = __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7650)) - 8388736.0f;
-                x[1] = __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7651)) - 8388736.0f;
-                x[2] = __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7652)) - 8388736.0f;
-                x[3] = __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7653)) - 8388736.0f;
-            }
-            unpack_f2(mul_f2(pack_f2(x[0], x[1]), scale2), f[i], f[i + 1]);
-            unpack_f2(mul_f2(pack_f2(x[2], x[3]), scale2), f[i + 2], f[i + 3]);
+    for (int i = 0; i < E; i += 4) {
+        float x[4];
+        if constexpr (FMT == kKvE4m3) {
+            uint32_t lo, hi;
+            asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+                : "=r"(lo), "=r"(hi) : "r"(c.w[i / 4]));
+            const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&lo)), q = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+            x[0] = p.x; x[1] = p.y; x[2] = q.x; x[3] = q.y;
+        } else {
+            // 2^23 + (code + 128) as binary32 bits, minus 2^23 + 128: exact
+            const uint32_t w = c.w[i / 4] ^ 0x80808080u;
+            x[0] = __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7650)) - 8388736.0f;
+            x[1] = __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7651)) - 8388736.0f;
+            x[2] = __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7652)) - 8388736.0f;
+            x[3] = __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7653)) - 8388736.0f;
         }
+        unpack_f2(mul_f2(pack_f2(x[0], x[1]), scale2), f[i], f[i + 1]);
+        unpack_f2(mul_f2(pack_f2(x[2], x[3]), scale2), f[i + 2], f[i + 3]);
     }
 }
 
@@ -317,38 +319,34 @@ __device__ __forceinline__ bool cache_place(const CacheArgs& a, long long slot, 
     return true;
 }
 
-// T: type of key and value.  E elements per lane and chunk, NCH chunks per lane, U vectors in flight per group.
+// T: type of key and value.  E elements to a lane, AL of them to an access, U vectors in flight per group.
 // The key and value vectors do not depend on the slots, so both are fetched at once.  The two divisions of a vector are
 // made by one lane for each of the U vectors at a time, not by all lanes for all of them: they are correctly rounded ones
 // (the codes are the definition's bit for bit) and cost as much as the rest of a vector.
-template <typename T, int FMT, int E, int AL, int LANES, int NCH, int U>
+template <typename T, int FMT, int E, int AL, int LANES, int U>
 __global__ void __launch_bounds__(kCacheThreads) kv_cache_write_kernel(const CacheArgs a)
 {
     constexpr int IN = E * (int)sizeof(T), SIZE = (int)sizeof(T), CODE = FMT == kKvPlain ? SIZE : 1;
     constexpr bool RAGGED = AL < E;
     static_assert(U <= LANES, "a lane for every vector in flight");
-    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
+    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, e = AL == 1 ? lane : lane * E;
     constexpr int GROUPS = kCacheThreads / LANES;
     const long long first = (long long)blockIdx.x * a.tokens_per_cta;
     const unsigned n_vec = (unsigned)min((long long)a.tokens_per_cta, a.n_tokens - first) * 2u * (unsigned)a.heads;
     wait_for_previous_kernel();
     for (unsigned v0 = 0; v0 < n_vec; v0 += GROUPS * U) {  // uniform over the CTA: whole warps take part in the shuffles
-        Chunk<IN> x[U][NCH];
+        Chunk<IN> x[U];
         long long slot[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const CacheVector c = cache_vector(a, v0 + u * GROUPS + group, n_vec);
             slot[u] = c.live ? __ldg(a.slots + first + c.token) : -1;
             const unsigned char* src = token_vector(a, c, first, sizeof(T));
+            if (c.live && e < a.dim) {
+                x[u] = ld_chunk<IN, access_bytes(AL, SIZE), access_stride(AL, SIZE, LANES), RAGGED>(src + (size_t)e * SIZE, (a.dim - e) * SIZE);
+            } else {
 #pragma unroll
-            for (int i = 0; i < NCH; ++i) {
-                const int e = (i * LANES + lane) * E;
-                if (c.live && e < a.dim) {
-                    x[u][i] = ld_chunk<IN, access_bytes(AL, SIZE), RAGGED>(src + (size_t)e * SIZE, (a.dim - e) * SIZE);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < (IN + 3) / 4; ++k) x[u][i].w[k] = 0;
-                }
+                for (int k = 0; k < IN / 4; ++k) x[u].w[k] = 0;
             }
         }
         float my_inv = 0.f, my_scale = 0.f;  // of the vector that this lane divides for: lane % U
@@ -356,9 +354,7 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_write_kernel(const Cac
             uint32_t my_top = 0;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                uint32_t top = 0;
-#pragma unroll
-                for (int i = 0; i < NCH; ++i) top = join_magnitude<T, IN>(top, x[u][i]);
+                uint32_t top = join_magnitude<T, IN>(x[u]);
 #pragma unroll
                 for (int m = LANES / 2; m >= 1; m >>= 1) {
                     const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, top, m);
@@ -382,21 +378,13 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_write_kernel(const Cac
             if (!cache_place(a, slot[u], c.head, entry, scale_entry)) continue;
             if constexpr (FMT == kKvPlain) {
                 unsigned char* dst = (c.side ? a.side[1] : a.side[0]) + entry * sizeof(T);
-#pragma unroll
-                for (int i = 0; i < NCH; ++i) {
-                    const int e = (i * LANES + lane) * E;
-                    if (e < a.dim) st_chunk<IN, access_bytes(AL, SIZE), RAGGED>(dst + (size_t)e * SIZE, x[u][i], (a.dim - e) * SIZE);
-                }
+                if (e < a.dim) st_chunk<IN, access_bytes(AL, SIZE), access_stride(AL, SIZE, LANES), RAGGED>(dst + (size_t)e * SIZE, x[u], (a.dim - e) * SIZE);
             } else {
                 unsigned char* dst = (c.side ? a.side[1] : a.side[0]) + entry;
-#pragma unroll
-                for (int i = 0; i < NCH; ++i) {
-                    const int e = (i * LANES + lane) * E;
-                    if (e < a.dim) {
-                        float f[E];
-                        chunk_to_float<T, E>(x[u][i], f);
-                        st_chunk<E, access_bytes(AL, CODE), RAGGED>(dst + e, encode<FMT, E>(f, inv), a.dim - e);
-                    }
+                if (e < a.dim) {
+                    float f[E];
+                    chunk_to_float<T, E>(x[u], f);
+                    st_chunk<E, access_bytes(AL, CODE), access_stride(AL, CODE, LANES), RAGGED>(dst + e, encode<FMT, E>(f, inv), a.dim - e);
                 }
                 if (lane == 0) (c.side ? a.scale[1] : a.scale[0])[scale_entry] = scale;
             }
@@ -404,20 +392,20 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_write_kernel(const Cac
     }
 }
 
-template <typename T, int FMT, int E, int AL, int LANES, int NCH, int U>
+template <typename T, int FMT, int E, int AL, int LANES, int U>
 __global__ void __launch_bounds__(kCacheThreads) kv_cache_read_kernel(const CacheArgs a)
 {
     constexpr int OUT = E * (int)sizeof(T), SIZE = (int)sizeof(T);
     constexpr bool RAGGED = AL < E;
     constexpr int HELD = FMT == kKvPlain ? OUT : E;
     constexpr int HELD_SIZE = FMT == kKvPlain ? (int)sizeof(T) : 1;
-    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
+    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, e = AL == 1 ? lane : lane * E;
     constexpr int GROUPS = kCacheThreads / LANES;
     const long long first = (long long)blockIdx.x * a.tokens_per_cta;
     const unsigned n_vec = (unsigned)min((long long)a.tokens_per_cta, a.n_tokens - first) * 2u * (unsigned)a.heads;
     wait_for_previous_kernel();
     for (unsigned v0 = 0; v0 < n_vec; v0 += GROUPS * U) {
-        Chunk<HELD> x[U][NCH];
+        Chunk<HELD> x[U];
         float scale[U];
         long long slot[U];
 #pragma unroll
@@ -436,28 +424,20 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_read_kernel(const Cach
             }
             const unsigned char* src = (c.side ? a.side[1] : a.side[0]) + entry * HELD_SIZE;
             if (FMT != kKvPlain) scale[u] = __ldg((c.side ? a.scale[1] : a.scale[0]) + scale_entry);
-#pragma unroll
-            for (int i = 0; i < NCH; ++i) {
-                const int e = (i * LANES + lane) * E;
-                if (e < a.dim) x[u][i] = ld_chunk<HELD, access_bytes(AL, HELD_SIZE), RAGGED>(src + (size_t)e * HELD_SIZE, (a.dim - e) * HELD_SIZE);
-            }
+            if (e < a.dim) x[u] = ld_chunk<HELD, access_bytes(AL, HELD_SIZE), access_stride(AL, HELD_SIZE, LANES), RAGGED>(src + (size_t)e * HELD_SIZE, (a.dim - e) * HELD_SIZE);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (slot[u] < 0) continue;
             const CacheVector c = cache_vector(a, v0 + u * GROUPS + group, n_vec);
             unsigned char* dst = token_vector(a, c, first, sizeof(T));
-#pragma unroll
-            for (int i = 0; i < NCH; ++i) {
-                const int e = (i * LANES + lane) * E;
-                if (e >= a.dim) continue;
-                if constexpr (FMT == kKvPlain) {
-                    st_chunk<OUT, access_bytes(AL, SIZE), RAGGED>(dst + (size_t)e * SIZE, x[u][i], (a.dim - e) * SIZE);
-                } else {
-                    float f[E];
-                    decode<FMT, E>(x[u][i], scale[u], f);
-                    st_chunk<OUT, access_bytes(AL, SIZE), RAGGED>(dst + (size_t)e * SIZE, chunk_from_float<T, E>(f), (a.dim - e) * SIZE);
-                }
+            if (e >= a.dim) continue;
+            if constexpr (FMT == kKvPlain) {
+                st_chunk<OUT, access_bytes(AL, SIZE), access_stride(AL, SIZE, LANES), RAGGED>(dst + (size_t)e * SIZE, x[u], (a.dim - e) * SIZE);
+            } else {
+                float f[E];
+                decode<FMT, E>(x[u], scale[u], f);
+                st_chunk<OUT, access_bytes(AL, SIZE), access_stride(AL, SIZE, LANES), RAGGED>(dst + (size_t)e * SIZE, chunk_from_float<T, E>(f), (a.dim - e) * SIZE);
             }
         }
     }
