@@ -90,9 +90,9 @@ int launch_shape(const CacheArgs& args, cudaStream_t stream)
 
 // Sixteen elements to a lane (the kernels are bound by instructions, and those that find a vector's places are shared by more
 // elements: 16384 x 8 x 128 bf16 to e4m3 took 30 us with eight, 20 with sixteen), in accesses as wide as sizes, strides and
-// pointers allow, the last lane's ending with the vector.  Places that are not even multiples of four elements (odd head
-// sizes): accesses of one element, eight to a lane, neighbouring elements in neighbouring lanes (16384 x 8 x 33 bf16 to e4m3: 19
-// us, 83 with one element to a lane).
+// pointers allow.  Accesses that are less than a lane's share go round the lanes (16384 x 8 x 100 bf16, plain: 17 us, 30 with
+// a lane's accesses side by side).  Places that are not even multiples of four elements (odd head sizes): accesses of one
+// element, eight to a lane (16384 x 8 x 33 bf16 to e4m3: 19 us, 83 with one to a lane).
 template <bool WRITE, typename T, int FMT, int AL>
 int launch_aligned(const CacheArgs& a, cudaStream_t stream)
 {
@@ -104,7 +104,9 @@ template <bool WRITE, typename T, int FMT>
 int launch_typed(const CacheArgs& a, int align_elems, cudaStream_t stream)
 {
     if (align_elems >= 16) return launch_aligned<WRITE, T, FMT, 16>(a, stream);
-    if (align_elems >= 8) return launch_aligned<WRITE, T, FMT, 8>(a, stream);
+    if constexpr (sizeof(T) < 4) {
+        if (align_elems >= 8) return launch_aligned<WRITE, T, FMT, 8>(a, stream);
+    }
     if (align_elems >= 4) return launch_aligned<WRITE, T, FMT, 4>(a, stream);
     if (a.dim <= 64) return launch_shape<WRITE, T, FMT, 8, 1, 8>(a, stream);
     if (a.dim <= 128) return launch_shape<WRITE, T, FMT, 8, 1, 16>(a, stream);

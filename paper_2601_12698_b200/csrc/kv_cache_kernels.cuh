@@ -73,10 +73,10 @@ template <int BYTES>
 struct Chunk {
     uint32_t w[BYTES / 4];
 };
-// Bytes of one access to a chunk whose places are multiples of AL elements of `size` bytes, and from one access to the next: a
-// lane's elements are neighbours, but for accesses of one element, where the neighbours are other lanes'.
+// Bytes of one access to a chunk of E elements whose places are multiples of AL elements of `size` bytes, and from one access to
+// the next: where AL elements are less than a chunk, neighbouring accesses are those of neighbouring lanes.
 __host__ __device__ constexpr int access_bytes(int al, int size) { return al * size < 16 ? al * size : 16; }
-__host__ __device__ constexpr int access_stride(int al, int size, int lanes) { return al == 1 ? lanes * size : access_bytes(al, size); }
+__host__ __device__ constexpr int access_stride(int al, int e, int size, int lanes) { return al < e ? lanes * al * size : access_bytes(al, size); }
 // A chunk in accesses of ACCESS bytes, STRIDE bytes apart.  RAGGED: accesses from byte `there` on do not exist, they read as zero.
 template <int BYTES, int ACCESS, int STRIDE, bool RAGGED>
 __device__ __forceinline__ Chunk<BYTES> ld_chunk(const unsigned char* p, int there)
@@ -328,8 +328,9 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_write_kernel(const Cac
 {
     constexpr int IN = E * (int)sizeof(T), SIZE = (int)sizeof(T), CODE = FMT == kKvPlain ? SIZE : 1;
     constexpr bool RAGGED = AL < E;
+    static_assert(AL == E || AL * SIZE <= 16, "AL elements are one access");
     static_assert(U <= LANES, "a lane for every vector in flight");
-    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, e = AL == 1 ? lane : lane * E;
+    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, e = lane * (AL < E ? AL : E);
     constexpr int GROUPS = kCacheThreads / LANES;
     const long long first = (long long)blockIdx.x * a.tokens_per_cta;
     const unsigned n_vec = (unsigned)min((long long)a.tokens_per_cta, a.n_tokens - first) * 2u * (unsigned)a.heads;
@@ -343,7 +344,7 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_write_kernel(const Cac
             slot[u] = c.live ? __ldg(a.slots + first + c.token) : -1;
             const unsigned char* src = token_vector(a, c, first, sizeof(T));
             if (c.live && e < a.dim) {
-                x[u] = ld_chunk<IN, access_bytes(AL, SIZE), access_stride(AL, SIZE, LANES), RAGGED>(src + (size_t)e * SIZE, (a.dim - e) * SIZE);
+                x[u] = ld_chunk<IN, access_bytes(AL, SIZE), access_stride(AL, E, SIZE, LANES), RAGGED>(src + (size_t)e * SIZE, (a.dim - e) * SIZE);
             } else {
 #pragma unroll
                 for (int k = 0; k < IN / 4; ++k) x[u].w[k] = 0;
@@ -378,13 +379,13 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_write_kernel(const Cac
             if (!cache_place(a, slot[u], c.head, entry, scale_entry)) continue;
             if constexpr (FMT == kKvPlain) {
                 unsigned char* dst = (c.side ? a.side[1] : a.side[0]) + entry * sizeof(T);
-                if (e < a.dim) st_chunk<IN, access_bytes(AL, SIZE), access_stride(AL, SIZE, LANES), RAGGED>(dst + (size_t)e * SIZE, x[u], (a.dim - e) * SIZE);
+                if (e < a.dim) st_chunk<IN, access_bytes(AL, SIZE), access_stride(AL, E, SIZE, LANES), RAGGED>(dst + (size_t)e * SIZE, x[u], (a.dim - e) * SIZE);
             } else {
                 unsigned char* dst = (c.side ? a.side[1] : a.side[0]) + entry;
                 if (e < a.dim) {
                     float f[E];
                     chunk_to_float<T, E>(x[u], f);
-                    st_chunk<E, access_bytes(AL, CODE), access_stride(AL, CODE, LANES), RAGGED>(dst + e, encode<FMT, E>(f, inv), a.dim - e);
+                    st_chunk<E, access_bytes(AL, CODE), access_stride(AL, E, CODE, LANES), RAGGED>(dst + e, encode<FMT, E>(f, inv), a.dim - e);
                 }
                 if (lane == 0) (c.side ? a.scale[1] : a.scale[0])[scale_entry] = scale;
             }
@@ -397,9 +398,10 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_read_kernel(const Cach
 {
     constexpr int OUT = E * (int)sizeof(T), SIZE = (int)sizeof(T);
     constexpr bool RAGGED = AL < E;
+    static_assert(AL == E || AL * SIZE <= 16, "AL elements are one access");
     constexpr int HELD = FMT == kKvPlain ? OUT : E;
     constexpr int HELD_SIZE = FMT == kKvPlain ? (int)sizeof(T) : 1;
-    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, e = AL == 1 ? lane : lane * E;
+    const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES, e = lane * (AL < E ? AL : E);
     constexpr int GROUPS = kCacheThreads / LANES;
     const long long first = (long long)blockIdx.x * a.tokens_per_cta;
     const unsigned n_vec = (unsigned)min((long long)a.tokens_per_cta, a.n_tokens - first) * 2u * (unsigned)a.heads;
@@ -424,7 +426,7 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_read_kernel(const Cach
             }
             const unsigned char* src = (c.side ? a.side[1] : a.side[0]) + entry * HELD_SIZE;
             if (FMT != kKvPlain) scale[u] = __ldg((c.side ? a.scale[1] : a.scale[0]) + scale_entry);
-            if (e < a.dim) x[u] = ld_chunk<HELD, access_bytes(AL, HELD_SIZE), access_stride(AL, HELD_SIZE, LANES), RAGGED>(src + (size_t)e * HELD_SIZE, (a.dim - e) * HELD_SIZE);
+            if (e < a.dim) x[u] = ld_chunk<HELD, access_bytes(AL, HELD_SIZE), access_stride(AL, E, HELD_SIZE, LANES), RAGGED>(src + (size_t)e * HELD_SIZE, (a.dim - e) * HELD_SIZE);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -433,11 +435,11 @@ __global__ void __launch_bounds__(kCacheThreads) kv_cache_read_kernel(const Cach
             unsigned char* dst = token_vector(a, c, first, sizeof(T));
             if (e >= a.dim) continue;
             if constexpr (FMT == kKvPlain) {
-                st_chunk<OUT, access_bytes(AL, SIZE), access_stride(AL, SIZE, LANES), RAGGED>(dst + (size_t)e * SIZE, x[u], (a.dim - e) * SIZE);
+                st_chunk<OUT, access_bytes(AL, SIZE), access_stride(AL, E, SIZE, LANES), RAGGED>(dst + (size_t)e * SIZE, x[u], (a.dim - e) * SIZE);
             } else {
                 float f[E];
                 decode<FMT, E>(x[u], scale[u], f);
-                st_chunk<OUT, access_bytes(AL, SIZE), access_stride(AL, SIZE, LANES), RAGGED>(dst + (size_t)e * SIZE, chunk_from_float<T, E>(f), (a.dim - e) * SIZE);
+                st_chunk<OUT, access_bytes(AL, SIZE), access_stride(AL, E, SIZE, LANES), RAGGED>(dst + (size_t)e * SIZE, chunk_from_float<T, E>(f), (a.dim - e) * SIZE);
             }
         }
     }
