@@ -127,6 +127,31 @@ def test_vectors_that_end_inside_a_lanes_share(B, dtype, fmt, dim):
     test_write_then_read_matches_the_definition(B, dtype, fmt, 37, 3, dim, 5, "gap" if dim % 16 else "token", dim % 3 == 0)
 
 
+@pytest.mark.parametrize("fmt", ["plain", "e4m3", "int8"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("off", [1, 2, 4, 8])
+def test_slices_that_start_off_the_vector_alignment(B, dtype, fmt, off):
+    n, heads, dim, page = 45, 3, 64, 8
+    g = torch.Generator().manual_seed(off)
+    base = torch.randn(n, 2 * heads, dim + 16, generator=g).to(TD[dtype]).cuda()
+    key, value = base[:, :heads, off:off + dim], base[:, heads:, off:off + dim]
+    cache, _ = _cache(B, "token", 8, page, heads, dim, dtype, fmt)
+    slots = torch.randperm(8 * page, generator=g)[:n].cuda()
+    B.kv_cache_write_launch(cache, key, value, slots)
+    wide = [torch.full((n, heads, dim + 16), 5.0, dtype=TD[dtype], device="cuda") for _ in range(2)]
+    out = [t[..., off:off + dim] for t in wide]
+    B.kv_cache_read_launch(cache, slots, *out)
+    for x, y, t in ((key, out[0], wide[0]), (value, out[1], wide[1])):
+        if fmt == "plain":
+            want = x.cpu()
+        else:
+            codes, scales = R.quantise(x.cpu(), fmt)
+            want = R.dequantise(codes, scales).float().to(TD[dtype])
+        assert torch.equal(y.cpu(), want)
+        assert bool((t[..., :off] == 5.0).all()) and bool((t[..., off + dim:] == 5.0).all())
+    assert B.rt_device_status() == 0
+
+
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
 def test_values_that_are_hard_to_quantise(B, dtype, fmt):
