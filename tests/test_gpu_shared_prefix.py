@@ -510,3 +510,33 @@ def test_many_rows_in_a_graph_with_the_options(B):
     finally:
         assert B.lib.rt_set_option(B.RT_OPTION_PROGRAMMATIC_LAUNCH, 1) == B.RT_OK
     assert torch.equal(serial, out) and torch.equal(lse_serial, lse)
+
+
+@pytest.mark.parametrize("shapes", [((40, 500, 8, 8, 64, 16, 1), (64, 1537, 16, 4, 128, 1, 1)), ((33, 1000, 8, 2, 128, 24, 1), (3, 200, 8, 2, 128, 16, 2)),
+                                    ((40, 700, 8, 2, 256, 16, 1), (33, 1000, 8, 2, 128, 24, 1))])
+def test_calls_behind_one_another_and_side_by_side(B, shapes):
+    """Calls on one stream take turns with one workspace; calls on two streams have one each.  The results are those of a call alone."""
+    problems = [Problem(B, [(7 * i) % 40 for i in range(s[0])], s[1], *s[2:6], "bf16", "plain" if n else "e4m3", s[6], seed=n) for n, s in enumerate(shapes)]
+    alone = []
+    for p in problems:
+        alone.append(p.launch())
+        torch.cuda.synchronize()
+    size = max(B.shared_prefix_attention_workspace_bytes(p.cache, p.batch, p.q.shape[-2]) for p in problems)
+    q = [p.q.cuda() for p in problems]
+    shared = torch.empty(size, dtype=torch.uint8, device="cuda")
+    behind = [[(torch.full_like(x, 3.0), torch.full(x.shape[:-1], 3.0, device="cuda")) for x in q] for _ in range(6)]
+    for outs in behind:
+        for p, x, (out, lse) in zip(problems, q, outs):
+            B.shared_prefix_attention_launch(p.cache, p.batch, x, out, lse, workspace=shared, softmax_scale=p.scale)
+    torch.cuda.synchronize()
+    streams, own = [torch.cuda.Stream() for _ in problems], [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in problems]
+    beside = [[(torch.full_like(x, 3.0), torch.full(x.shape[:-1], 3.0, device="cuda")) for x in q] for _ in range(6)]
+    torch.cuda.synchronize()
+    for outs in beside:
+        for p, x, (out, lse), s, w in zip(problems, q, outs, streams, own):
+            B.shared_prefix_attention_launch(p.cache, p.batch, x, out, lse, workspace=w, softmax_scale=p.scale, stream=s)
+    torch.cuda.synchronize()
+    for outs in behind + beside:
+        for (out, lse), (want, want_lse) in zip(outs, alone):
+            assert torch.equal(out.view(torch.int16), want.view(torch.int16)) and torch.equal(lse, want_lse)
+    assert B.rt_device_status() == 0
