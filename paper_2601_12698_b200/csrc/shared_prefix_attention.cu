@@ -29,6 +29,7 @@ struct AttendPlan {
     int prefix_parts, prefix_keys, suffix_parts, suffix_keys;
     PrefixSplit split;  // run > 0: the prefix is dealt out by tiles
     long long prefix_ctas, suffix_ctas;
+    bool joined;  // results lie in parts, which merge_parts_kernel joins; otherwise the only part is the result
     int64_t workspace;
 };
 
@@ -182,7 +183,9 @@ int make_attend_plan(const rt_kv_cache* c, const rt_prefix_batch* b, int q_heads
     }
     const int parts = p->prefix_parts + p->suffix_parts;
     const int64_t rows = p->tokens * q_heads;
-    if (parts > 1) p->workspace = (int64_t)parts * rows * c->head_dim * 4 + ((int64_t)parts * rows * 4 + 15) / 16 * 16;
+    // Without any part the merge kernel writes the empty result.  The tiles kernel leaves parts even where it leaves only one.
+    p->joined = parts != 1 || p->prefix_form == kPrefixTiles;
+    if (p->joined && parts > 0) p->workspace = (int64_t)parts * rows * c->head_dim * 4 + ((int64_t)parts * rows * 4 + 15) / 16 * 16;
     return RT_OK;
 }
 
@@ -279,7 +282,7 @@ int shared_prefix_attention_launch(const rt_kv_cache* c, const rt_prefix_batch* 
     a.suffix_parts = p.suffix_parts;
     a.suffix_keys = p.suffix_keys;
     a.part_out = (float*)workspace;
-    a.part_lse = parts > 1 ? (float*)workspace + (int64_t)parts * p.tokens * q_heads * c->head_dim : nullptr;
+    a.part_lse = p.workspace > 0 ? (float*)workspace + (int64_t)parts * p.tokens * q_heads * c->head_dim : nullptr;
     a.out = out;
     a.lse = lse;
     a.status = device_status_word();
@@ -301,7 +304,7 @@ int shared_prefix_attention_launch(const rt_kv_cache* c, const rt_prefix_batch* 
         st = launch(keys_form, prefix_ctas + p.suffix_ctas, kKeysThreads, &prefix_ctas);
         if (st != RT_OK) return st;
     }
-    if (parts != 1) st = launch(kMergeParts, ceil_div(p.tokens * q_heads * (p.padded_dim == 256 ? 2 : 1), kMergePartsThreads / 32), kMergePartsThreads, &p.split);
+    if (p.joined) st = launch(kMergeParts, ceil_div(p.tokens * q_heads * (p.padded_dim == 256 ? 2 : 1), kMergePartsThreads / 32), kMergePartsThreads, &p.split);
     return st;
 }
 
