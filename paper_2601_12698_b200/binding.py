@@ -530,7 +530,7 @@ def shared_prefix_attention_launch(cache: KvCache, batch: PrefixBatch, q, out, l
     """Attention of q [n_seqs, q_len, q_heads, head_dim] (or [n_seqs, q_heads, head_dim] for one query token) to the shared
     prefix and to each sequence's own suffix; out like q and contiguous, lse float32 [..., q_heads] or None.  softmax_scale
     defaults to head_dim ** -0.5.  workspace: a uint8 tensor of shared_prefix_attention_workspace_bytes(...) bytes, made
-    here when it is None.  Asynchronous."""
+    here, in the memory of the stream that the call runs on, when it is None.  Asynchronous."""
     shape, strides, dtype = q.shape, q.stride(), q.dtype
     n_seqs, q_len, head_dim, index = batch.n_seqs, batch.q_len, cache.head_dim, cache.device_index
     if len(shape) == 4 and shape[1] == q_len:
@@ -553,18 +553,19 @@ def shared_prefix_attention_launch(cache: KvCache, batch: PrefixBatch, q, out, l
         if lse.shape != shape[:-1] or lse.dtype is not _torch.float32 or not lse.is_contiguous() or lse.get_device() != index:
             raise ValueError("lse must be a contiguous float32 tensor of q's shape without head_dim, on q's device")
         lse_ptr = lse.data_ptr()
-    if workspace is None:
-        workspace = shared_prefix_attention_workspace(cache, batch, q_heads)
-        if stream is not None and workspace.numel():
-            workspace.record_stream(stream)
-    elif workspace.get_device() != index or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous tensor on the cache's device")
     code = _TORCH_CODES.get(dtype)
     if code is None:
         raise ValueError("q must be bf16 or fp16")
+    handle = _stream_of(index, stream)
+    if workspace is None:
+        # From the memory of the stream that uses it: a block of the caller's current stream may have work of that stream pending.
+        with _torch.cuda.stream(stream):
+            workspace = shared_prefix_attention_workspace(cache, batch, q_heads)
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the cache's device")
     status = _call_on(index, lib.shared_prefix_attention_launch, cache._ref, batch._ref, q.data_ptr(), token_stride, strides[-2], q_heads,
                       out.data_ptr(), lse_ptr, head_dim ** -0.5 if softmax_scale is None else softmax_scale, code, workspace.data_ptr(),
-                      workspace.nbytes, _stream_of(index, stream))
+                      workspace.nbytes, handle)
     if status:
         raise TunerError(status, "shared_prefix_attention_launch")
 
