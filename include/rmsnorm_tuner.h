@@ -720,10 +720,12 @@ int32_t rt_kernel_instance_parts(int32_t i);
  * RT_OPTION_TMA_WAIT_POLL_LIMIT (1 .. 2^24, default 2^24): how many times a thread of add_rmsnorm's TMA stages polls
  * its row's mbarrier before it gives up, writes RT_ERR_DEVICE_TIMEOUT into the device status word, waits once more
  * with the same limit and then carries on to every barrier of the CTA (the launch completes; its outputs are not
- * valid).  The default is about a second of polling; a copy that has not landed by then never will.
+ * valid).  The default is about a second of polling; a copy that has not landed by then never will.  The kernels of
+ * shared_prefix_attention_launch wait in the same bounded way, a poll there lasting up to 20 us: a thread whose wait runs out
+ * waits no more in that launch, which completes, gives back its tensor memory and reports RT_ERR_DEVICE_TIMEOUT.
  * RT_OPTION_DEBUG_DROP_TMA_COPIES (0 or 1, default 0): diagnostic switch for exercising that path without a
- * fault - the TMA stages of add_rmsnorm initialise their mbarriers but post no copy, so every wait runs out at the
- * poll limit and the launch reports RT_ERR_DEVICE_TIMEOUT.  Nothing out of bounds is read or written.  Lower the
+ * fault - the TMA stages of add_rmsnorm initialise their mbarriers but post no copy, and the attention kernels announce
+ * no tile, so waits run out at the poll limit and the launch reports RT_ERR_DEVICE_TIMEOUT.  Nothing out of bounds is read or written.  Lower the
  * poll limit to a few thousand first, or every row waits the full default.
  */
 enum { RT_OPTION_PROGRAMMATIC_LAUNCH = 0, RT_OPTION_TMA_WAIT_POLL_LIMIT = 1, RT_OPTION_DEBUG_DROP_TMA_COPIES = 2 };

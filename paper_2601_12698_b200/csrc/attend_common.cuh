@@ -46,6 +46,8 @@ struct AttendArgs {
     void* out;        // [token][head][dim]
     float* lse;       // [token][head] or NULL
     int* status;
+    unsigned wait_polls;  // polls a bounded wait may take (kMbarrierPollLimit unless the caller lowered it)
+    int drop_copies;      // diagnostic: 1 = no tile is announced, so that waits run out and report it
 };
 
 // The prefix kernel lets the suffix kernel start as soon as the kernel before both has completed: they read the same inputs and

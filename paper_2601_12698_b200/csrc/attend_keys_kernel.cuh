@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
     unsigned char* q_tile = smem + S::kQAt;
     unsigned char* weights = smem + S::kWAt;
     long long* offsets = reinterpret_cast<long long*>(smem + S::kOffsetsAt);  // [3][128]: places of a tile's keys
-    __shared__ __align__(8) uint64_t full[SLOTS], empty[SLOTS], s_full[2], w_full[2], o_done[2], q_full;
+    __shared__ __align__(8) uint64_t full[SLOTS], empty[SLOTS], s_full[2], w_full[2], o_done[2], q_full, drained;
     __shared__ uint32_t tmem_base;
     // per row: factor of the scores, reference m (the same for every thread, so it need not sit in their registers), what a new
     // reference rescales by, and the four softmax warps' maxima, sums at the end, and at the beginning the places of the queries
@@ -161,6 +161,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
             mbarrier_init(&o_done[i], 1);
         }
         mbarrier_init(&q_full, 128);
+        mbarrier_init(&drained, 1);
         poisoned = 0;
     }
     const bool beside_prefix = a.after_prefix != 0;  // that of another launch
@@ -235,7 +236,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
     // barrier is still met and the tensor memory is given back; the status word says that the results are not valid.
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-        if (ok) ok = mbarrier_wait_sleeping(bar, parity);
+        if (ok) ok = mbarrier_wait_sleeping(bar, parity, a.wait_polls);
     };
     // Page number of key `i` of tile j; -1: there is no such key.
     auto page_of = [&](int j, int i) -> int {
@@ -538,7 +539,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
         };
         auto announce = [&](int q) {
             fence_async_proxy();
-            mbarrier_arrive(&full[q % SLOTS]);
+            if (!a.drop_copies) mbarrier_arrive(&full[q % SLOTS]);
         };
         // Some rows do not see the last keys, and 0 * infinity would reach them through the product: such values become zero in
         // the tile and are added to the rows that do see them at the end.
@@ -673,8 +674,11 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
                 ++item;
             }
         }
-        // the tensor memory is given back only when nothing writes it any more
-        ok = mbarrier_wait_sleeping(&o_done[(n - 1) & 1], ((n - 1) >> 1) & 1) && ok;
+        // The tensor memory is given back only when nothing writes it any more.  (A barrier of its own: when a wait has run out, the
+        // products ran ahead of the roles that o_done keeps in step, and its parity says nothing about the last of them.)
+        if (elect_one()) tc_commit(&drained);
+        __syncwarp();
+        ok = mbarrier_wait_sleeping(&drained, 0) && ok;
     }
     if (!ok) atomicExch(a.status, kDeviceTimeoutCode);
     tc_fence_before();

@@ -109,6 +109,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
         }
         mbarrier_init(&q_full, 256);
     }
+    for (int i = tid; i < kTcAux * kTcTile; i += kTcThreads) offsets[i] = -1;  // what is read here was published, now or for an earlier tile, or is no place
     if (warp == 12) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_base)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -126,10 +127,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
     const int tile0 = run_no * split.run, n = min(split.tiles - tile0, split.run);
     const bool narrow = narrow_block(split, block);
     // Every wait is bounded.  A thread whose wait has run out stops waiting and goes on through the same loops, so that every
-    // barrier is still met and the tensor memory is given back; the status word says that the results are not valid.
+    // barrier is still met and the tensor memory is given back; the status word says that the results are not valid.  Nothing that
+    // it goes on with leads outside the tensors: places are those of some tile's keys, or none, from the beginning.
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-        if (ok) ok = mbarrier_wait_sleeping(bar, parity);
+        if (ok) ok = mbarrier_wait_sleeping(bar, parity, a.wait_polls);
     };
 
     if (warp < 8) {
@@ -551,6 +553,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                     }
                 }
                 if (g + 1 < n) read_pages(g + 1);
+                if (a.drop_copies) continue;
                 wait(&aux_free[slot], ((g / kTcAux) & 1) ^ 1);
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {

@@ -618,6 +618,9 @@ int launch_kernel(const void* fn, dim3 grid, dim3 block, size_t dyn_smem, cudaSt
     return RT_OK;
 }
 
+unsigned wait_poll_limit() { return (unsigned)g_wait_polls.load(std::memory_order_relaxed); }
+int drop_copies() { return g_drop_tma_copies.load(std::memory_order_relaxed); }
+
 int current_device_index(int* index)
 {
     DeviceCache* dc;

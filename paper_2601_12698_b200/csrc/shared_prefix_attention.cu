@@ -287,6 +287,8 @@ int shared_prefix_attention_launch(const rt_kv_cache* c, const rt_prefix_batch* 
     a.lse = lse;
     a.status = device_status_word();
     if (!a.status) return RT_ERR_NO_DEVICE;
+    a.wait_polls = wait_poll_limit();
+    a.drop_copies = drop_copies();
     const AttendKernels k = kernels_of(dtype, c->format, p.padded_dim);
     const cudaStream_t s = (cudaStream_t)stream;
     const auto launch = [&](int form, long long ctas, int threads, void* second) {

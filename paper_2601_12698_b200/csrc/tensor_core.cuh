@@ -116,9 +116,10 @@ __device__ __forceinline__ constexpr uint32_t tc_instruction(int n, bool a_rows,
            ((128u >> 4) << 24);
 }
 
-// Bounded wait whose polls sleep in hardware for up to kWaitSleepNs each: many roles wait most of the time.  Gives up after about a second, as mbarrier_wait_bounded.
+// Bounded wait whose polls sleep in hardware for up to kWaitSleepNs each: many roles wait most of the time.  Gives up after
+// poll_limit polls or about a second, as mbarrier_wait_bounded.
 constexpr uint32_t kWaitSleepNs = 20000;
-__device__ __forceinline__ bool mbarrier_wait_sleeping(uint64_t* bar, uint32_t parity)
+__device__ __forceinline__ bool mbarrier_wait_sleeping(uint64_t* bar, uint32_t parity, unsigned poll_limit = kMbarrierPollLimit)
 {
     const uint32_t addr = smem_u32(bar);
     long long t0 = 0;
@@ -131,7 +132,7 @@ __device__ __forceinline__ bool mbarrier_wait_sleeping(uint64_t* bar, uint32_t p
             : "=r"(done) : "r"(addr), "r"(parity), "r"(kWaitSleepNs) : "memory");
         if (done) return true;
         if (it == 0) t0 = clock64();
-        if (it >= kMbarrierPollLimit || clock64() - t0 > kMbarrierCycleLimit) return false;
+        if (it >= poll_limit || clock64() - t0 > kMbarrierCycleLimit) return false;
     }
 }
 

@@ -91,6 +91,8 @@ void count_launch(int64_t n = 1);
 // Launches `fn` with the library's launch attributes and counts it.
 int launch_kernel(const void* fn, dim3 grid, dim3 block, size_t dyn_smem, cudaStream_t stream, void** params);
 constexpr int kDeviceSlots = 64;           // devices the library keeps state for
+unsigned wait_poll_limit();                // RT_OPTION_TMA_WAIT_POLL_LIMIT
+int drop_copies();                         // RT_OPTION_DEBUG_DROP_TMA_COPIES
 int current_device_index(int* index);      // 0 .. kDeviceSlots - 1
 
 // Raw grid and feasible set (feasible.cu).  counts, when given, has kRejectReasons + 3 entries:

@@ -32,6 +32,8 @@ namespace rt {
 void set_error(const char*, ...) {}
 int check_cache(const rt_kv_cache*, bool) { return RT_OK; }
 int log2_or_minus1(unsigned) { return -1; }
+unsigned wait_poll_limit() { return kMbarrierPollLimit; }
+int drop_copies() { return 0; }
 int* device_status_word() { return &g_status; }
 int current_device_index(int* index) { *index = 0; return RT_OK; }
 int current_limits(rt_limits* out)
