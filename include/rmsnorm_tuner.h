@@ -446,7 +446,8 @@ typedef struct {
  * Query token i of a sequence whose suffix has n keys sees the whole prefix and the suffix keys j <= n - q_len + i.  A
  * row that sees no key gets out = 0 and lse = -inf, the convention of merge_attn_states_template_launch, so the
  * result can be merged with that of further keys.  Query head h reads key/value head h / (q_heads / kv_heads).  Keys
- * that a row does not see have no influence on it, whatever their values (infinities and NaN included).
+ * that a row does not see have no influence on it, whatever their values (infinities and NaN included).  In a quantised
+ * cache a seen value whose scale is not finite makes the row of out NaN; lse, which has no value in it, is not touched.
  *   cache      format plain (dtype as q), e4m3 or int8; head_dim a multiple of 8 (plain) or 16 (quantised); k, v and
  *              their strides multiples of 16 bytes (RT_ERR_ALIGN otherwise).  The suffix keys of the query tokens are
  *              in it already.

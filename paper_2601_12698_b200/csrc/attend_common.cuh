@@ -169,7 +169,10 @@ __device__ __forceinline__ float fp16_row_factor(float amax)
     return __uint_as_float((uint32_t)(127 + 14 - e) << 23);
 }
 
-// A value scale as the weights use it: log2 and reciprocal are taken of it, so a zero (an entry never written) becomes tiny.
-__device__ __forceinline__ float usable_scale(float s) { return s < 1e-30f ? 1e-30f : s; }
+// A value scale as the weights use it: log2 and reciprocal are taken of it, so a zero (an entry never written) becomes tiny, and one
+// that is not finite 1: the log-sum-exp, which values have no part in, stays that of the scores, and the rows that see such a key
+// are made NaN when they are written.
+__device__ __forceinline__ bool finite_scale(float s) { return s < INFINITY; }  // false for a NaN
+__device__ __forceinline__ float usable_scale(float s) { return !finite_scale(s) ? 1.f : s < 1e-30f ? 1e-30f : s; }
 
 }  // namespace rt

@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
     float(&row_sum)[4][NR] = row_m;
     long long* row_q = reinterpret_cast<long long*>(&row_m[0][0]);
     __shared__ __align__(16) long long row_at[NR];  // [token][head] index of a row, -1: no such row; then where its result goes
-    __shared__ int poisoned;
+    __shared__ int poisoned, first_nan_row;  // first_nan_row: from it on, rows see a value whose scale is not finite
 
     // (the warp's number by shuffle: the compiler then knows that a role is taken by whole warps)
     const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
@@ -163,6 +163,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
         mbarrier_init(&q_full, 128);
         mbarrier_init(&drained, 1);
         poisoned = 0;
+        first_nan_row = NR;
     }
     const bool beside_prefix = a.after_prefix != 0;  // that of another launch
     if (!beside_prefix) wait_for_previous_kernel();
@@ -317,6 +318,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
         for (int j = 0; j < n; ++j) {
             const bool there = there_n;
             const float ks = ks_n, vs = usable_scale(vs_n);
+            const bool value_there = finite_scale(vs_n);
             page_n = page_nn;
             if (j + 1 < n) key_constants(j + 1, page_n);
             if (j + 2 < n) page_nn = page_of(j + 2, tid);
@@ -327,6 +329,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
             }
             // rows below it do not see this thread's key
             const int hidden = prefix ? 0 : max(0, k0 + j * 128 + tid - (len - a.q_len)) * a.group - row0;
+            if (kQuant && !value_there) atomicMin(&first_nan_row, hidden);
             wait(&s_full[j & 1], (j >> 1) & 1);
             tc_fence_after();
             // 16 rows' scores of this thread's key, as logarithms; more rows than that are read again where they are needed
@@ -461,7 +464,8 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
             }
             // a part that saw no key is not read by the merge, the result of a call is zero
             // (a padding row is neither)
-            row_c[tid] = empty ? 0.f : 1.0f / total;
+            const bool nan = kQuant && tid >= *reinterpret_cast<volatile int*>(&first_nan_row);
+            row_c[tid] = empty ? 0.f : nan ? __uint_as_float(0x7FC00000u) : 1.0f / total;
             row_at[tid] = !write || (empty && !direct) ? -1 : (direct ? at : (long long)part_index * all_rows + at) * a.dim;
         }
         sync_128();

@@ -85,6 +85,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
     __shared__ uint32_t tmem_base;
     __shared__ float row_factor[2][kQuant ? 128 : 1];
     __shared__ uint32_t ragged[kTcAux];  // one byte for each half of the lookup: some key is not there
+    __shared__ int nan_values[2];        // of a quantised cache: among a stream's tiles is a value whose scale is not finite
 
     // (the warp's number by shuffle: the compiler then knows that a role is taken by whole warps)
     const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
@@ -106,6 +107,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
             mbarrier_init(&o_done[i], 1);
             mbarrier_init(&o_full[i], 1);
             mbarrier_init(&drained[i], 1);
+            nan_values[i] = 0;
         }
         mbarrier_init(&q_full, 256);
     }
@@ -326,7 +328,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
         if (my_tiles > 0) {
             // A thread holds a row, and rows lie apart: 32 columns at a time go through shared memory, so that eight lanes
             // write 128 bytes of a row.  Rows without a key are written too; nothing reads them.
-            const float inv = empty ? 0.f : 1.0f / l;
+            float inv = empty ? 0.f : 1.0f / l;
+            if (kQuant && *reinterpret_cast<volatile int*>(&nan_values[s]) != 0) inv = __uint_as_float(0x7FC00000u);
             unsigned char* stage = DP == 64 ? smem + S::kStageAt + warp * 4096 : q_tiles + S::kTileBytes * (narrow ? 1 : s) + (narrow ? warp : warp & 3) * 4096;
             long long to_row[8];
 #pragma unroll
@@ -562,6 +565,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_prefix_kernel(const Atte
                     float* to = aux + slot * S::kAuxFloats + p + 64 * y;
                     if constexpr (kQuant) {
                         const float u = usable_scale(vs[y]);
+                        if (!finite_scale(vs[y])) {
+                            if (!narrow || (g & 1) == 0) nan_values[0] = 1;
+                            if (!narrow || (g & 1) == 1) nan_values[1] = 1;
+                        }
                         to[0] = ks[y];
                         to[kTcTile] = there ? log2f(u) : -INFINITY;
                         to[2 * kTcTile] = there ? __frcp_rn(u) : 0.f;
