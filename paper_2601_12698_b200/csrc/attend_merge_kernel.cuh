@@ -40,7 +40,10 @@ __global__ void __launch_bounds__(kMergePartsThreads) merge_parts_kernel(const A
         for (int s = 16; s >= 1; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
         const float base = top == -INFINITY ? 0.f : top;
         // A NaN among the parts (a NaN score) is skipped by the maximum and kept by the weights.
-        const float w = lse == -INFINITY ? 0.f : ex2(lse - base), keep = m == -INFINITY ? 0.f : ex2(m - base);
+        // A part that saw keys never weighs nothing, or a NaN among its values would be lost with it: 2^-149 where the exponential is zero.
+        float w = lse == -INFINITY ? 0.f : ex2(lse - base);
+        if (w == 0.f && lse != -INFINITY) w = __uint_as_float(1u);
+        const float keep = m == -INFINITY ? 0.f : ex2(m - base);
         float sum = w;
 #pragma unroll
         for (int s = 16; s >= 1; s >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, s);

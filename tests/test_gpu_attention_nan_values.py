@@ -70,3 +70,33 @@ def test_an_infinite_value_written_into_the_cache(B, fmt, seqs):
     assert bool(torch.isnan(out[..., :4, :].float()).all()) and bool(torch.isfinite(out[..., 4:, :].float()).all())
     _check_lse(p, lse, ref)
     assert B.rt_device_status() == 0
+
+
+@pytest.mark.parametrize("fmt", ["plain", "e4m3", "int8"])
+@pytest.mark.parametrize("seqs", [3, 40])
+def test_a_nan_value_in_a_part_that_weighs_next_to_nothing(B, fmt, seqs):
+    """A key's weight is above zero however low its score: its NaN reaches the row although the part that holds it is some 2^-400 of
+    the other."""
+    p = Problem(B, [5] * seqs, 130, 8, 2, 64, 16, "bf16", fmt, seed=5)
+    q = torch.zeros(seqs, 1, 8, 64).bfloat16()
+    q[..., 0] = 300.0
+    p.q, p.scale = q, 1.0
+    k = p.cache.k if fmt == "plain" else p.cache.k.view(torch.uint8)
+    for b in range(seqs):
+        if fmt == "plain":
+            k[int(p.table[b, 0]), :5, :, 0] = 1.0
+        else:
+            p.cache.k_scale[int(p.table[b, 0]), :5] = 1.0
+            k[int(p.table[b, 0]), :5, :, 0] = 0x38 if fmt == "e4m3" else 1  # 1.0 either way
+    pages = p.prefix_pages.long().cuda()
+    if fmt == "plain":
+        k[pages, :, :, 0] = 0.0
+        p.cache.v[int(p.prefix_pages[2]), 3, 0, 9] = float("nan")
+    else:
+        k[pages, :, :, 0] = 0
+        p.cache.v_scale[int(p.prefix_pages[2]), 3, 0] = float("nan")
+    out, lse = p.launch()
+    hit = out[:, 0, :4].float()
+    assert bool(torch.isnan(hit[..., 9] if fmt == "plain" else hit).all())
+    assert bool(torch.isfinite(out[:, 0, 4:].float()).all()) and bool(torch.isfinite(lse).all())
+    assert B.rt_device_status() == 0
