@@ -73,7 +73,8 @@ __device__ __forceinline__ void split_position(const AttendArgs& a, int pos, int
     }
 }
 
-// Number of keys in the suffix of `seq` that the page table can name; -1 for a padded sequence.
+// Number of keys in the suffix of `seq` that the page table can name; below 0 for a padded sequence.  A longer one is reported by every
+// kernel that asks: there may be no suffix kernel.
 __device__ __forceinline__ int suffix_length(const AttendArgs& a, int seq)
 {
     int len = __ldg(a.suffix_lens + seq);

@@ -456,7 +456,7 @@ __global__ void __launch_bounds__(kKeysThreads, KeysShape<FMT, DP, NR>::kCtas) a
             const float total = row_sum[0][tid] + row_sum[1][tid] + row_sum[2][tid] + row_sum[3][tid];
             const bool empty = total == 0.f;  // a row that sees a key has a sum above zero, or NaN
             bool write = at >= 0;
-            if (prefix && direct && write) write = __ldg(a.suffix_lens + (int)((unsigned)(at / n_heads) / (unsigned)a.q_len)) >= 0;
+            if (prefix && direct && write) write = suffix_length(a, (int)((unsigned)(at / n_heads) / (unsigned)a.q_len)) >= 0;
             if (write) {
                 const float lse = empty ? -INFINITY : row_ref[tid] + log2f(total);
                 if (!direct) a.part_lse[(long long)part_index * all_rows + at] = lse;

@@ -27,7 +27,7 @@ __global__ void __launch_bounds__(kMergePartsThreads) merge_parts_kernel(const A
     const int skip = a.prefix_parts - prefix_parts;  // parts of the workspace that this row does not use
     const int parts = prefix_parts + a.suffix_parts;
     wait_for_previous_kernel();
-    if (row >= n_rows || __ldg(a.suffix_lens + (unsigned)token / (unsigned)a.q_len) < 0) return;
+    if (row >= n_rows || suffix_length(a, (int)((unsigned)token / (unsigned)a.q_len)) < 0) return;
     const int side = lane / LANES, d = (int)(warp % WARPS) * 128 + (lane % LANES) * 4;
     float m = -INFINITY, total = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
