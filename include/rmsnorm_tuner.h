@@ -448,6 +448,13 @@ typedef struct {
  * result can be merged with that of further keys.  Query head h reads key/value head h / (q_heads / kv_heads).  Keys
  * that a row does not see have no influence on it, whatever their values (infinities and NaN included).  In a quantised
  * cache a seen value whose scale is not finite makes the row of out NaN; lse, which has no value in it, is not touched.
+ *
+ * Arithmetic: scores, sums, parts and lse are binary32.  The weights e^(s_j) are rounded to 16 bits for the product with the
+ * values - to `dtype`, or to fp16 over a quantised cache - which moves out by half a step of that type (bf16 2^-8, fp16 2^-11)
+ * of the weighted mean of |v_j|, as much again as the rounding of the result (fp16 weights below 2^-14 are off by up to 2^-25);
+ * a quarter of the exponentials over a long prefix comes from a polynomial (2.7e-6 relative).  Weights reach 2^8 before the
+ * division, so the sums hold values up to about 2^119 / keys in magnitude.
+ *
  *   cache      format plain (dtype as q), e4m3 or int8; head_dim a multiple of 8 (plain) or 16 (quantised); k, v and
  *              their strides multiples of 16 bytes (RT_ERR_ALIGN otherwise).  The suffix keys of the query tokens are
  *              in it already.
@@ -456,7 +463,8 @@ typedef struct {
  *   out        device, [n_seqs * q_len, q_heads, head_dim] contiguous, 16-byte aligned.  lse: device, binary32
  *              [n_seqs * q_len, q_heads] contiguous, or NULL.
  *   workspace  device memory of shared_prefix_attention_workspace_bytes(...) bytes, 16-byte aligned, for the partial
- *              results.  It carries nothing from one call to the next; calls that may overlap on the device need one each.
+ *              results (a prefix alone can need one too).  It carries nothing from one call to the next; calls that may
+ *              overlap on the device need one each.
  * A page number outside the cache hides its keys and leaves RT_ERR_INDEX in the device status word.  The results do not
  * depend on the other work of the device, from call to call they are bit-identical.  Asynchronous on `stream`, allocates
  * nothing.
@@ -726,8 +734,9 @@ int32_t rt_kernel_instance_parts(int32_t i);
  * waits no more in that launch, which completes, gives back its tensor memory and reports RT_ERR_DEVICE_TIMEOUT.
  * RT_OPTION_DEBUG_DROP_TMA_COPIES (0 or 1, default 0): diagnostic switch for exercising that path without a
  * fault - the TMA stages of add_rmsnorm initialise their mbarriers but post no copy, and the attention kernels announce
- * no tile, so waits run out at the poll limit and the launch reports RT_ERR_DEVICE_TIMEOUT.  Nothing out of bounds is read or written.  Lower the
- * poll limit to a few thousand first, or every row waits the full default.
+ * no tile, so waits run out at the poll limit and the launch reports RT_ERR_DEVICE_TIMEOUT.  Nothing out of bounds is
+ * read or written.  Lower the poll limit to a few thousand first (a few dozen for the attention kernels), or every row
+ * waits the full default.
  */
 enum { RT_OPTION_PROGRAMMATIC_LAUNCH = 0, RT_OPTION_TMA_WAIT_POLL_LIMIT = 1, RT_OPTION_DEBUG_DROP_TMA_COPIES = 2 };
 int rt_set_option(int32_t option, int32_t value);

@@ -444,7 +444,7 @@ __device__ __forceinline__ bool mbarrier_wait_bounded(uint64_t* bar, uint32_t pa
 // attribute, its CTAs may be scheduled while the previous kernel of the stream is still draining; everything above
 // this call (index arithmetic) overlaps that kernel's tail, and the call returns once that kernel has completed
 // and its writes are visible, so nothing below it can see unfinished data.  Without the attribute it is a no-op.
-// The kernels never signal their own dependents early (no griddepcontrol.launch_dependents): measured on B200,
+// The norm's kernels and their variants never signal their own dependents early (no griddepcontrol.launch_dependents): measured on B200,
 // dependents that start while this kernel still streams only take SM slots from it.
 __device__ __forceinline__ void wait_for_previous_kernel()
 {

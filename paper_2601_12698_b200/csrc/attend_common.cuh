@@ -50,8 +50,8 @@ struct AttendArgs {
     int drop_copies;      // diagnostic: 1 = no tile is announced, so that waits run out and report it
 };
 
-// The prefix kernel lets the suffix kernel start as soon as the kernel before both has completed: they read the same inputs and
-// write different parts.  The suffix kernel therefore does not wait for its predecessor before it starts; its first CTA does
+// The prefix kernel lets the suffix kernel start once all its own CTAs have started and the kernel before both has completed: they
+// read the same inputs and write different parts.  (With more CTAs than SMs that is its last wave.)  The suffix kernel therefore does not wait for its predecessor before it starts; its first CTA does
 // before it ends, so that the kernel that joins the parts, which waits for the suffix kernel, finds the prefix's parts too.  (One
 // CTA is enough, and CTAs that waited would keep others from the SMs that they hold.)
 __device__ __forceinline__ void let_next_kernel_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
@@ -139,8 +139,8 @@ __device__ __forceinline__ uint4 ld_codes(const unsigned char* p, bool there)
     return w;
 }
 
-// 2^x for two numbers on the multiply-add pipe, beside the special function unit (16 exponentials a cycle per SM): x = n + f with n the nearest integer, 2^f by the polynomial of degree 4 of least relative error on
-// [-1/2, 1/2] (found by exchange of the extrema; 2.7e-6 in binary32, 4e-8 on average), times 2^n.  Below -126: 2^-126.
+// 2^x for two numbers on the multiply-add pipe, beside the special function unit (16 exponentials a cycle per SM): x = n + f with
+// n the nearest integer, 2^f by the polynomial of degree 4 of least relative error on [-1/2, 1/2] (found by exchange of the extrema; 2.7e-6 in binary32, 4e-8 on average), times 2^n.  Below -126: 2^-126.
 __device__ __forceinline__ float2x ex2_by_polynomial(float2x x)
 {
     float lo, hi;

@@ -134,10 +134,12 @@ int make_attend_plan(const rt_kv_cache* c, const rt_prefix_batch* b, int q_heads
             s.rows = (int)prefix_rows;
             s.blocks = (int)ceil_div(prefix_rows, kTcBlockRows);
             const long long units = (long long)s.blocks * c->kv_heads;
-            // The two kernels run side by side, one CTA of this one taking a whole SM: it gets the share of the SMs that its share
-            // of the work asks for.  The unit is what a tile of 128 keys costs the suffix kernel on one SM (1.4 us plain, 1.7
+            // The two kernels run side by side, one CTA of this one taking a whole SM, where its CTAs are no more than the SMs (with
+            // more, the suffix kernel starts in their last wave, and the model is only a bound on the runs): it gets the share of the
+            // SMs that its share of the work asks for.  The unit is what a tile of 128 keys costs the suffix kernel on one SM (1.4 us plain, 1.7
             // quantised); a tile for 256 rows costs the prefix kernel 1.6 of that, beginning and ending a run about 7.  Suffixes are
-            // taken to be half as long as they may be.
+            // taken to be half as long as they may be: a max_suffix_len far above the lengths leaves the prefix too few SMs (64
+            // sequences of up to 100 keys, prefix 8192: 50 us where it is 100, 71 at 2048, 150 at 8192).
             const double prefix_work = (double)units * (s.tiles * 1.6 + 7), tiles_per_suffix = 0.5 * (double)ceil_div(b->max_suffix_len, 128);
             const double suffix_work = tiles_per_suffix * (double)ceil_div(suffix_rows, 16) * c->kv_heads * (double)b->n_seqs;
             long long sms = (long long)(L.sm_count * prefix_work / (prefix_work + suffix_work) + 0.5);
