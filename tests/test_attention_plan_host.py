@@ -35,13 +35,17 @@ def harness(tmp_path_factory):
     return lib
 
 
-def _plan(lib, seqs, prefix, suffix, heads, kv_heads, dim, q_len=1, fmt=None, page=16, sm_count=148):
-    """(bytes of workspace, the launches) of one call."""
-    fmt = B.RT_KV_PLAIN if fmt is None else fmt
+def _structs(seqs, prefix, suffix, kv_heads, dim, q_len, fmt, page):
     cache = B.rt_kv_cache(P, P, P, P, 1 << 20, page, kv_heads, dim, fmt, B.RT_BF16, 0, page * kv_heads * dim, kv_heads * dim, dim,
                           page * kv_heads, kv_heads, 1)
     width = -(-suffix // page)
     batch = B.rt_prefix_batch(P if prefix else None, P if suffix else None, P, prefix, suffix, seqs, width, width, -(-prefix // page), q_len, 0)
+    return cache, batch
+
+
+def _plan(lib, seqs, prefix, suffix, heads, kv_heads, dim, q_len=1, fmt=B.RT_KV_PLAIN, page=16, sm_count=148):
+    """(bytes of workspace, the launches) of one call."""
+    cache, batch = _structs(seqs, prefix, suffix, kv_heads, dim, q_len, fmt, page)
     lib.harness_reset(sm_count)
     size = lib.shared_prefix_attention_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), heads)
     assert size >= 0
@@ -92,3 +96,17 @@ def test_parts_of_any_geometry_lie_inside_the_workspace(harness):
         size, launches = _plan(harness, seqs, prefix, suffix, heads, kv_heads, dim, q_len, rng.choice([0, 1, 2]), rng.choice([1, 16, 24, 128]),
                                rng.choice([148, 148, 132, 1]))
         _check(seqs, dim, heads, q_len, size, launches)
+
+
+def test_a_workspace_that_is_missing_or_too_small_is_refused(harness):
+    for seqs, prefix, suffix in ((40, 128, 0), (256, 32768, 0), (40, 128, 100), (2, 512, 64), (1, 0, 5000)):
+        cache, batch = _structs(seqs, prefix, suffix, 8, 128, 1, B.RT_KV_PLAIN, 16)
+        harness.harness_reset(148)
+        size = harness.shared_prefix_attention_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), 32)
+        call = lambda at, n: harness.shared_prefix_attention_launch(ctypes.byref(cache), ctypes.byref(batch), P, 32 * 128, 128, 32, P, P, 0.1,
+                                                                    B.RT_BF16, at, n, None)
+        assert size > 0
+        assert call(None, 0) == B.RT_ERR_NULL and call(WORKSPACE, 0) == B.RT_ERR_CAPACITY and call(WORKSPACE, size - 1) == B.RT_ERR_CAPACITY
+        assert call(WORKSPACE + 4, size) == B.RT_ERR_ALIGN
+        assert harness.harness_launches((Launch * 8)()) == 0
+        assert call(WORKSPACE, size) == B.RT_OK
