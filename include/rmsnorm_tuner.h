@@ -476,6 +476,130 @@ int shared_prefix_attention_launch(const rt_kv_cache* cache, const rt_prefix_bat
  * (rt_last_error has the reason).  The pointers of `cache` and `batch` are not read. */
 int64_t shared_prefix_attention_workspace_bytes(const rt_kv_cache* cache, const rt_prefix_batch* batch, int32_t q_heads);
 
+/* ---- 1c. rotary positions, attention over packed prompts, moves inside a cache ------------------------ */
+
+/* How the frequencies of rotary positions are stretched for contexts longer than the trained one. */
+typedef enum {
+    RT_ROTARY_NONE = 0,
+    RT_ROTARY_LINEAR = 1, /* every frequency divided by `factor` */
+    RT_ROTARY_NTK = 2,    /* base * factor^(rot_dim / (rot_dim - 2)) */
+    RT_ROTARY_BANDS = 3,  /* by the turns n_j that pair j makes over original_len: divided by `factor` below low_turns, kept above
+                             high_turns, between them a line in n_j */
+    RT_ROTARY_YARN = 4    /* a line in j between the whole numbers around the pairs that make fast_turns (kept) and slow_turns
+                             (divided) over original_len, and a magnitude of 0.1 ln(factor) + 1 */
+} rt_rotary_scaling;
+
+typedef struct {
+    double base;                   /* theta_j = base^(-2 j / rot_dim); > 1 */
+    double factor;                 /* > 0; 1 for RT_ROTARY_NONE (ignored there) */
+    double original_len;           /* BANDS and YARN: the trained context length, > 0 */
+    double low_turns, high_turns;  /* BANDS: 0 < low < high */
+    double fast_turns, slow_turns; /* YARN: fast > slow > 0 */
+    int32_t rot_dim;               /* even, 2 .. RT_KV_MAX_HEAD_DIM (4 at least for RT_ROTARY_NTK) */
+    int32_t scaling;               /* rt_rotary_scaling */
+} rt_rotary_spec;
+
+/*
+ * The frequencies of a spec, host only: turns[j] (rot_dim / 2 of them) is the part of a full turn that pair j makes per
+ * position, as a 64-bit binary fraction.  Position p's angle is then the product p * turns[j] modulo 2^64, exact at any
+ * distance, where a binary32 angle is off by 0.06 at a million.
+ */
+int rotary_frequencies(const rt_rotary_spec* spec, uint64_t* turns, float* magnitude);
+
+typedef struct {
+    const uint64_t* turns; /* device, [rot_dim / 2], from rotary_frequencies */
+    int32_t rot_dim;       /* the first rot_dim elements of a head are turned */
+    int32_t interleaved;   /* 0: pairs (j, j + rot_dim / 2); 1: pairs (2 j, 2 j + 1) */
+    int32_t backward;      /* 1: the gradient (the opposite angle, the same magnitude) */
+    float magnitude;
+} rt_rotary;
+
+/*
+ * Turns the pairs of every head of every token by its position's angles:  y1 = m (x1 cos - x2 sin), y2 = m (x2 cos + x1 sin),
+ * in binary32, rounded once to `dtype`; elements from rot_dim on are copied.
+ *   positions  device, int64 [n_tokens]; negative = a padded token, whose rows of out are left as they were.
+ *   q, k       device, [n_tokens, q_heads or k_heads, head_dim] of `dtype`, the last axis contiguous, outer strides in elements; q_out
+ *              and k_out likewise.  Either side may have no heads (its pointers are then ignored).  q_out may be q with the same
+ *              strides, and k_out k; otherwise the tensors must not overlap.
+ * Asynchronous on `stream`, allocates nothing.  n_tokens == 0 is a successful no-op.
+ */
+int rotary_launch(const rt_rotary* rotary, const int64_t* positions, int64_t n_tokens, int32_t head_dim, const void* q,
+                  int64_t q_token_stride, int64_t q_head_stride, void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride,
+                  int32_t q_heads, const void* k, int64_t k_token_stride, int64_t k_head_stride, void* k_out,
+                  int64_t k_out_token_stride, int64_t k_out_head_stride, int32_t k_heads, int dtype, void* stream);
+
+/* Sequences packed behind one another: sequence b has the query rows q_starts[b] .. q_starts[b + 1] - 1 and the key rows
+ * k_starts[b] .. k_starts[b + 1] - 1.  More keys than queries: the queries are the sequence's last tokens. */
+typedef struct {
+    const int32_t* q_starts; /* device, [n_seqs + 1], not descending, 0 .. q_tokens */
+    const int32_t* k_starts; /* device, [n_seqs + 1], not descending, 0 .. k_tokens; may be q_starts */
+    int64_t n_seqs;          /* 0 .. 2^24 */
+    int64_t q_tokens;        /* rows of q, out and lse: 0 .. 2^30 */
+    int64_t k_tokens;        /* rows of k and v: 0 .. 2^30 */
+    int64_t max_q_len;       /* about the largest number of queries and of keys of a sequence; the launch shape follows */
+    int64_t max_k_len;       /* them, the results do not */
+    int32_t causal;          /* 1: query i of n_q sees the keys j <= n_k - n_q + i; 0: all keys of its sequence */
+    int32_t reserved;        /* 0 */
+} rt_prompt_batch;
+
+/*
+ * Attention over whole prompts:  with s_j = softmax_scale * <q, k_j> over the keys that the row sees,
+ *     out = round_dtype(sum_j e^(s_j) v_j / sum_j e^(s_j)),   lse = ln sum_j e^(s_j).
+ * A row that sees no key gets out = 0 and lse = -inf, the convention of merge_attn_states_template_launch.  Rows of no
+ * sequence are left as they were.  Query head h reads key/value head h / (q_heads / kv_heads).  Keys that a row does not see have no
+ * influence on it, whatever their values (infinities and NaN included).
+ * Arithmetic as in shared_prefix_attention_launch: binary32, the weights rounded to `dtype` for the product with the values, a part
+ * of the exponentials from a polynomial (2.7e-6 relative).
+ *   q          device, [q_tokens, q_heads, head_dim] of `dtype` (bf16 or fp16); k, v: [k_tokens, kv_heads, head_dim]; outer strides in
+ *              elements, none of them 0 (unless its axis has one entry), pointers and strides multiples of 16 bytes.
+ *   head_dim   a multiple of 8 up to RT_KV_MAX_HEAD_DIM; q_heads / kv_heads up to 128; softmax_scale finite and not negative.
+ *   out        device, [q_tokens, q_heads, head_dim] contiguous, 16-byte aligned.  lse: device, binary32 [q_tokens, q_heads]
+ *              contiguous, or NULL.
+ *   workspace  device memory of prompt_attention_workspace_bytes(...) bytes, 16-byte aligned.  It carries nothing from one call to the
+ *              next; calls that may overlap on the device need one each.
+ * Starts that descend or lie outside the tensors are cut to them and leave RT_ERR_INDEX in the device status word; nothing outside the
+ * tensors is read or written.  From call to call the results are bit-identical.  Asynchronous on `stream`, allocates nothing.
+ */
+int prompt_attention_launch(const rt_prompt_batch* batch, const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t q_heads,
+                            const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
+                            int64_t v_head_stride, int32_t kv_heads, int32_t head_dim, void* out, float* lse, float softmax_scale,
+                            int dtype, void* workspace, int64_t workspace_bytes, void* stream);
+/* Bytes of workspace for a batch of this geometry on the current device (0 is possible), -1 when it is not served
+ * (rt_last_error has the reason).  The pointers of `batch` are not read. */
+int64_t prompt_attention_workspace_bytes(const rt_prompt_batch* batch, int32_t q_heads, int32_t kv_heads, int32_t head_dim);
+
+/* Most caches (layers) that one call of the two below takes. */
+#define RT_MAX_LAYERS 128
+
+/*
+ * Copies pages inside caches: in each of the n_caches caches (host array; alike in everything but their pointers) the first
+ * tokens[i] entries of page src[i] become those of page dst[i], scales included, the rest of the page stays.
+ *   src, dst  device, int32 [n_pages].  A page may be a source any number of times; a destination must be neither a source nor another
+ *             destination of the same call (its content would be a mixture).  A pair with a negative number is skipped; one
+ *             beyond the cache is skipped and reported as RT_ERR_INDEX in the device status word.
+ *   tokens    device, int32 [n_pages], or NULL for whole pages; outside 0 .. page_size: cut there and reported as RT_ERR_INDEX.
+ * Asynchronous on `stream`, allocates nothing.  n_pages == 0 is a successful no-op.
+ */
+int kv_cache_copy_pages_launch(const rt_kv_cache* caches, int32_t n_caches, const int32_t* src, const int32_t* dst,
+                               const int32_t* tokens, int64_t n_pages, void* stream);
+
+/*
+ * Closes the gaps that given-up tokens leave: of the tokens starts[b] .. lens[b] - 1 of sequence b those whose keep[b, i] is not 0
+ * (token starts[b] + i) move, in every cache, to the positions starts[b], starts[b] + 1, ... in their order;
+ * new_lens[b] = starts[b] + their number.  In place; what lies behind the new length is not defined.
+ *   page_table      device, int32 [n_seqs, page_table_width], row stride page_table_stride: the pages of each sequence from its
+ *                   first token on.  Pages that hold any of the tokens from starts[b] on must belong to the sequence alone.
+ *   starts, lens, new_lens  device, int32 [n_seqs]; new_lens must overlap none of the inputs.
+ *   keep            device, bytes [n_seqs, window], row stride keep_stride.
+ * lens[b] < 0 is a padded sequence: new_lens[b] = lens[b].  A sequence with starts[b] outside 0 .. lens[b], more than `window` tokens
+ * behind it or more than its table row has pages for, or a page number outside the cache is reported as RT_ERR_INDEX: of the latter only that
+ * token is not moved, the others are left as they are with new_lens[b] = lens[b].
+ * Asynchronous on `stream`, allocates nothing.  n_seqs == 0 is a successful no-op.
+ */
+int kv_cache_compact_launch(const rt_kv_cache* caches, int32_t n_caches, const int32_t* page_table, int64_t page_table_stride,
+                            int32_t page_table_width, const int32_t* starts, const int32_t* lens, const unsigned char* keep,
+                            int64_t keep_stride, int64_t window, int32_t* new_lens, int64_t n_seqs, void* stream);
+
 /* ---- 2. the feasible region ----------------------------------------------------- */
 
 /* r(h) of the current CUDA device.  RT_ERR_NO_DEVICE when there is none. */

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_void_p
+from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_uint64, c_void_p
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "librmsnorm_tuner.so")
@@ -31,6 +31,8 @@ RT_CMP_BITS, RT_CMP_ULP16, RT_CMP_REL32 = 0, 1, 2
  RT_ERR_BUDGET, RT_ERR_DEVICE_TIMEOUT, RT_ERR_CAPACITY, RT_ERR_NO_DEVICE, RT_ERR_INDEX) = range(13)
 RT_KV_PLAIN, RT_KV_E4M3, RT_KV_INT8 = 0, 1, 2
 RT_KV_MAX_HEAD_DIM, RT_MAX_QUERY_LEN = 256, 16
+RT_ROTARY_NONE, RT_ROTARY_LINEAR, RT_ROTARY_NTK, RT_ROTARY_BANDS, RT_ROTARY_YARN = 0, 1, 2, 3, 4
+RT_MAX_LAYERS = 128
 PHASE_NAMES = {0: "seed", 1: "grid", 2: "climb", 3: "topk", 4: "sweep"}
 STAGE_NAMES = {0: "reg", 1: "smem_ldg", 2: "smem_tma", 3: "reg_realign", 4: "tma_pipeline"}
 REDUCE_NAMES = {0: "shfl", 1: "smem", 2: "cluster"}
@@ -125,6 +127,20 @@ class rt_prefix_batch(Structure):
                 ("page_table_width", c_int32), ("n_prefix_pages", c_int32), ("q_len", c_int32), ("reserved", c_int32)]
 
 
+class rt_rotary_spec(Structure):
+    _fields_ = [("base", c_double), ("factor", c_double), ("original_len", c_double), ("low_turns", c_double), ("high_turns", c_double),
+                ("fast_turns", c_double), ("slow_turns", c_double), ("rot_dim", c_int32), ("scaling", c_int32)]
+
+
+class rt_rotary(Structure):
+    _fields_ = [("turns", c_void_p), ("rot_dim", c_int32), ("interleaved", c_int32), ("backward", c_int32), ("magnitude", c_float)]
+
+
+class rt_prompt_batch(Structure):
+    _fields_ = [("q_starts", c_void_p), ("k_starts", c_void_p), ("n_seqs", c_int64), ("q_tokens", c_int64), ("k_tokens", c_int64),
+                ("max_q_len", c_int64), ("max_k_len", c_int64), ("causal", c_int32), ("reserved", c_int32)]
+
+
 SOURCE_NAMES = {0: "table_exact", 1: "table_nearest", 2: "general", 3: "feasible_set"}
 
 rt_evaluate_fn = ctypes.CFUNCTYPE(c_double, POINTER(rt_params), c_void_p)
@@ -145,6 +161,15 @@ _SIGNATURES = {
     "shared_prefix_attention_launch": (c_int, [POINTER(rt_kv_cache), POINTER(rt_prefix_batch), c_void_p, c_int64, c_int64,
                                                c_int32, c_void_p, c_void_p, c_float, c_int, c_void_p, c_int64, c_void_p]),
     "shared_prefix_attention_workspace_bytes": (c_int64, [POINTER(rt_kv_cache), POINTER(rt_prefix_batch), c_int32]),
+    "rotary_frequencies": (c_int, [POINTER(rt_rotary_spec), POINTER(c_uint64), POINTER(c_float)]),
+    "rotary_launch": (c_int, [POINTER(rt_rotary), c_void_p, c_int64, c_int32, c_void_p, c_int64, c_int64, c_void_p, c_int64, c_int64, c_int32,
+                              c_void_p, c_int64, c_int64, c_void_p, c_int64, c_int64, c_int32, c_int, c_void_p]),
+    "prompt_attention_launch": (c_int, [POINTER(rt_prompt_batch), c_void_p, c_int64, c_int64, c_int32, c_void_p, c_int64, c_int64, c_void_p,
+                                        c_int64, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_float, c_int, c_void_p, c_int64, c_void_p]),
+    "prompt_attention_workspace_bytes": (c_int64, [POINTER(rt_prompt_batch), c_int32, c_int32, c_int32]),
+    "kv_cache_copy_pages_launch": (c_int, [POINTER(rt_kv_cache), c_int32, c_void_p, c_void_p, c_void_p, c_int64, c_void_p]),
+    "kv_cache_compact_launch": (c_int, [POINTER(rt_kv_cache), c_int32, c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_void_p, c_int64, c_int64,
+                                        c_void_p, c_int64, c_void_p]),
     "rt_kernel_instance_parts": (c_int32, [c_int32]),
     "rt_set_option": (c_int, [c_int32, c_int32]),
     "rt_get_option": (c_int32, [c_int32]),
@@ -568,6 +593,217 @@ def shared_prefix_attention_launch(cache: KvCache, batch: PrefixBatch, q, out, l
                       workspace.nbytes, handle)
     if status:
         raise TunerError(status, "shared_prefix_attention_launch")
+
+
+# ---- 1c. rotary positions, attention over packed prompts, moves inside a cache -------------------------------
+
+def _torch_ready():
+    """torch and its dtype codes, for calls that can come before the first cache."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    if not _TORCH_CODES:
+        _TORCH_CODES.update({_torch.bfloat16: RT_BF16, _torch.float16: RT_FP16, _torch.float32: RT_FP32})
+
+
+_ROTARY_SCALINGS = {"none": RT_ROTARY_NONE, "linear": RT_ROTARY_LINEAR, "ntk": RT_ROTARY_NTK, "bands": RT_ROTARY_BANDS, "yarn": RT_ROTARY_YARN}
+
+
+class RotaryTable:
+    """The frequencies of rotary positions for heads whose first rot_dim elements are turned: theta_j = base^(-2 j / rot_dim),
+    stretched for long contexts by `scaling`: "linear", "ntk" (both by `factor`), "bands" (`factor`, `original_len`, `low_turns`,
+    `high_turns`) or "yarn" (`factor`, `original_len`, `fast_turns`, `slow_turns`; `magnitude` 0.1 ln(factor) + 1 unless given).
+    Pairs are (j, j + rot_dim / 2), or (2 j, 2 j + 1) when interleaved.  One object serves every layer and every call."""
+
+    def __init__(self, rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original_len: float = 0.0,
+                 low_turns: float = 1.0, high_turns: float = 4.0, fast_turns: float = 32.0, slow_turns: float = 1.0, magnitude: float | None = None,
+                 interleaved: bool = False, device="cuda"):
+        if scaling not in _ROTARY_SCALINGS:
+            raise ValueError(f"scaling must be one of {', '.join(_ROTARY_SCALINGS)}")
+        spec = rt_rotary_spec(base, factor, original_len, low_turns, high_turns, fast_turns, slow_turns, rot_dim, _ROTARY_SCALINGS[scaling])
+        fractions, m = (c_uint64 * (RT_KV_MAX_HEAD_DIM // 2))(), c_float(1.0)
+        _check(lib.rotary_frequencies(byref(spec), fractions, byref(m)), "rotary_frequencies")
+        _torch_ready()
+        self.rot_dim, self.interleaved = int(rot_dim), bool(interleaved)
+        self.magnitude = m.value if magnitude is None else float(magnitude)
+        self.fractions = list(fractions)[:self.rot_dim // 2]  # of a turn, times 2^64
+        signed = [f - (1 << 64) if f >> 63 else f for f in self.fractions]
+        self.turns = _torch.tensor(signed, dtype=_torch.int64, device=device)
+        self.device_index = self.turns.get_device()
+        self._refs = [byref(rt_rotary(self.turns.data_ptr(), self.rot_dim, int(self.interleaved), backward, self.magnitude)) for backward in (0, 1)]
+
+
+def _refuse_rotary(positions, x, out, index: int):
+    if positions.dim() != 1 or positions.dtype != _torch.int64 or not positions.is_contiguous() or positions.get_device() != index:
+        raise ValueError("rotary_launch: positions must be a contiguous int64 [n_tokens] tensor on the table's device")
+    if x.dim() == 3 and out.shape == x.shape and out.dtype is x.dtype and x.dtype in _TORCH_CODES and x.get_device() == out.get_device() == index:
+        _no_overlap(out, "rotary_launch: out")
+    raise ValueError("rotary_launch: q, k and their outputs must be [n_tokens, heads, head_dim] tensors of one dtype (bf16, fp16, fp32) and "
+                     "head_dim on the table's device, the last axis contiguous")
+
+
+def rotary_launch(table: RotaryTable, positions, q, k=None, q_out=None, k_out=None, backward: bool = False, stream=None) -> None:
+    """Turn the heads of q [n_tokens, q_heads, head_dim] and k [n_tokens, k_heads, head_dim] (or of q alone) by the positions
+    (int64 [n_tokens]; negative = a padded token, whose rows are left as they were) into q_out and k_out, by default in place.
+    `backward` is the gradient: the opposite angle.  Asynchronous."""
+    index = table.device_index
+    if q_out is None:
+        q_out = q
+    shape, qs, os, dtype = q.shape, q.stride(), q_out.stride(), q.dtype
+    code = _TORCH_CODES.get(dtype)
+    if not (len(shape) == 3 and code is not None and q_out.shape == shape and q_out.dtype is dtype and (qs[2] == os[2] == 1 or shape[2] == 1)
+            and positions.dtype is _torch.int64 and positions.shape == shape[:1] and positions.is_contiguous()
+            and (0 not in os or 1 in shape or 0 in shape) and q.get_device() == q_out.get_device() == positions.get_device() == index):
+        _refuse_rotary(positions, q, q_out, index)
+    if k is None:
+        if k_out is not None:
+            raise ValueError("rotary_launch: k_out without k")
+        side = (None, 0, 0, None, 0, 0, 0)
+    else:
+        if k_out is None:
+            k_out = k
+        k_shape, ks, kos = k.shape, k.stride(), k_out.stride()
+        if not (len(k_shape) == 3 and k_shape[0] == shape[0] and k_shape[2] == shape[2] and k.dtype is dtype and k_out.shape == k_shape
+                and k_out.dtype is dtype and (ks[2] == kos[2] == 1 or k_shape[2] == 1) and (0 not in kos or 1 in k_shape or 0 in k_shape)
+                and k.get_device() == k_out.get_device() == index):
+            _refuse_rotary(positions, k, k_out, index)
+        side = (k.data_ptr(), ks[0], ks[1], k_out.data_ptr(), kos[0], kos[1], k_shape[1])
+    status = _call_on(index, lib.rotary_launch, table._refs[1 if backward else 0], positions.data_ptr(), shape[0], shape[2], q.data_ptr(), qs[0],
+                      qs[1], q_out.data_ptr(), os[0], os[1], shape[1], *side, code, _stream_of(index, stream))
+    if status:
+        raise TunerError(status, "rotary_launch")
+
+
+class PromptBatch:
+    """Sequences packed behind one another: the first query row of each and, last, the row behind them all (int32 [n_seqs + 1], not
+    descending), and the same for keys (k_starts None: the queries' own).  max_q_len and max_k_len are about the largest lengths, on the
+    host's side: the launch shape follows them, the results do not.  causal: the queries are the last tokens of their sequence and see the
+    keys up to their own; otherwise all of the sequence's.  One object serves every layer of the step."""
+
+    def __init__(self, q_starts, max_q_len: int, k_starts=None, max_k_len: int | None = None, causal: bool = True):
+        _torch_ready()
+        for t in (q_starts,) if k_starts is None else (q_starts, k_starts):
+            if t.dim() != 1 or t.dtype != _torch.int32 or not t.is_cuda or not t.is_contiguous() or t.shape != q_starts.shape or t.shape[0] < 1:
+                raise ValueError("q_starts and k_starts must be contiguous int32 [n_seqs + 1] CUDA tensors")
+            if t.device != q_starts.device:
+                raise ValueError("q_starts and k_starts must be on one device")
+        if max_q_len < 0 or (max_k_len is not None and max_k_len < 0):
+            raise ValueError("negative length")
+        self.q_starts, self.k_starts = q_starts, q_starts if k_starts is None else k_starts
+        self.n_seqs, self.device_index, self.causal = q_starts.shape[0] - 1, q_starts.get_device(), bool(causal)
+        self.max_q_len = int(max_q_len)
+        self.max_k_len = self.max_q_len if max_k_len is None else int(max_k_len)
+        self._fixed = (self.q_starts.data_ptr(), self.k_starts.data_ptr(), self.n_seqs)
+
+    def _struct(self, q_tokens: int, k_tokens: int):
+        return rt_prompt_batch(*self._fixed, q_tokens, k_tokens, self.max_q_len, self.max_k_len, self.causal, 0)
+
+
+def prompt_attention_workspace_bytes(batch: PromptBatch, q, k) -> int:
+    """Bytes of workspace of a call with queries like q and keys like k."""
+    n = _call_on(batch.device_index, lib.prompt_attention_workspace_bytes, byref(batch._struct(q.shape[0], k.shape[0])), q.shape[1], k.shape[1], q.shape[2])
+    if n < 0:
+        raise ValueError(f"prompt_attention: {lib.rt_last_error().decode()}")
+    return int(n)
+
+
+def prompt_attention_workspace(batch: PromptBatch, q, k):
+    """A uint8 tensor of the size that calls with queries like q and keys like k need."""
+    return _torch.empty(prompt_attention_workspace_bytes(batch, q, k), dtype=_torch.uint8, device=q.device)
+
+
+def prompt_attention_launch(batch: PromptBatch, q, k, v, out, lse=None, workspace=None, softmax_scale=None, stream=None) -> None:
+    """Attention of the packed queries q [q_tokens, q_heads, head_dim] to their sequences' keys k and values v [k_tokens, kv_heads,
+    head_dim] (bf16 or fp16, any outer strides that are multiples of 16 bytes); out like q and contiguous, lse float32 [q_tokens, q_heads]
+    or None.  softmax_scale defaults to head_dim ** -0.5.  workspace: a uint8 tensor of prompt_attention_workspace_bytes(...) bytes, made
+    here, in the memory of the stream that the call runs on, when it is None.  Asynchronous."""
+    shape, k_shape, dtype, index = q.shape, k.shape, q.dtype, batch.device_index
+    if len(shape) != 3 or len(k_shape) != 3 or v.shape != k_shape or k_shape[2] != shape[2]:
+        raise ValueError("q must be [q_tokens, q_heads, head_dim], k and v [k_tokens, kv_heads, head_dim]")
+    if not (k.dtype is v.dtype is dtype) or dtype not in (_torch.bfloat16, _torch.float16):
+        raise ValueError("q, k and v must be bf16 or fp16, all three the same")
+    if out.shape != shape or out.dtype is not dtype or not out.is_contiguous():
+        raise ValueError("out must be contiguous and of q's shape and dtype")
+    if not (q.get_device() == k.get_device() == v.get_device() == out.get_device() == index):
+        raise ValueError("batch, q, k, v and out must be on one CUDA device")
+    qs, ks, vs = q.stride(), k.stride(), v.stride()
+    if shape[2] > 1 and not qs[2] == ks[2] == vs[2] == 1:
+        raise ValueError("q, k and v: the last axis must be contiguous")
+    lse_ptr = None
+    if lse is not None:
+        if lse.shape != shape[:2] or lse.dtype is not _torch.float32 or not lse.is_contiguous() or lse.get_device() != index:
+            raise ValueError("lse must be a contiguous float32 [q_tokens, q_heads] tensor on q's device")
+        lse_ptr = lse.data_ptr()
+    handle = _stream_of(index, stream)
+    if workspace is None:
+        if stream is None:
+            workspace = prompt_attention_workspace(batch, q, k)
+        else:  # from the memory of the stream that uses it: a block of the caller's current stream may have work of that stream pending
+            with _torch.cuda.stream(stream):
+                workspace = prompt_attention_workspace(batch, q, k)
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on q's device")
+    status = _call_on(index, lib.prompt_attention_launch, byref(batch._struct(shape[0], k_shape[0])), q.data_ptr(), qs[0], qs[1], shape[1],
+                      k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], k_shape[1], shape[2], out.data_ptr(), lse_ptr,
+                      shape[2] ** -0.5 if softmax_scale is None else softmax_scale, _TORCH_CODES[dtype], workspace.data_ptr(), workspace.nbytes, handle)
+    if status:
+        raise TunerError(status, "prompt_attention_launch")
+
+
+class KvCacheStack:
+    """The caches of all layers of a model, alike in everything but their memory: what moves entries moves them in every layer."""
+
+    def __init__(self, caches):
+        self.caches = list(caches)
+        if not 1 <= len(self.caches) <= RT_MAX_LAYERS:
+            raise ValueError(f"a stack has 1 to {RT_MAX_LAYERS} caches")
+        first = self.caches[0]
+        alike = [n for n, _ in rt_kv_cache._fields_ if n not in ("k", "v", "k_scale", "v_scale")]
+        for c in self.caches:
+            if c.device_index != first.device_index or any(getattr(c.struct, n) != getattr(first.struct, n) for n in alike):
+                raise ValueError("the caches of a stack must have one device, shape, format and strides")
+        self.device_index = first.device_index
+        self._array = (rt_kv_cache * len(self.caches))(*[c.struct for c in self.caches])
+
+
+def _page_list(t, shape, index: int, name: str):
+    if t.shape != shape or t.dtype is not _torch.int32 or not t.is_contiguous() or t.get_device() != index:
+        raise ValueError(f"{name} must be a contiguous int32 {list(shape)} tensor on the caches' device")
+
+
+def kv_cache_copy_pages_launch(stack: KvCacheStack, src, dst, tokens=None, stream=None) -> None:
+    """In every cache of the stack, copy page src[i] to page dst[i] (int32 [n]; negative = skipped), or only its first tokens[i]
+    entries.  A destination must be neither a source nor another destination of the call.  Asynchronous."""
+    index = stack.device_index
+    for t, name in ((src, "src"), (dst, "dst"), (tokens, "tokens")):
+        if t is not None or name != "tokens":
+            _page_list(t, src.shape[:1] if len(src.shape) == 1 else (0,), index, name)
+    status = _call_on(index, lib.kv_cache_copy_pages_launch, stack._array, len(stack.caches), src.data_ptr(), dst.data_ptr(),
+                      None if tokens is None else tokens.data_ptr(), src.shape[0], _stream_of(index, stream))
+    if status:
+        raise TunerError(status, "kv_cache_copy_pages_launch")
+
+
+def kv_cache_compact_launch(stack: KvCacheStack, page_table, starts, lens, keep, new_lens, stream=None) -> None:
+    """In every cache of the stack, close the gaps that given-up tokens leave: of the tokens starts[b] .. lens[b] - 1 of sequence b those
+    with keep[b, i] (bool or uint8 [n_seqs, window]; token starts[b] + i) move to starts[b], starts[b] + 1, ...; new_lens[b] is the new
+    length.  page_table: int32 [n_seqs, width], the sequence's pages from its first token on.  lens[b] < 0: a padded sequence.
+    Asynchronous."""
+    index, n = stack.device_index, starts.shape[0] if starts.dim() == 1 else -1
+    for t, name in ((starts, "starts"), (lens, "lens"), (new_lens, "new_lens")):
+        _page_list(t, (n,), index, name)
+    if (page_table.dim() != 2 or page_table.dtype is not _torch.int32 or page_table.shape[0] != n or page_table.get_device() != index
+            or (page_table.shape[1] > 1 and page_table.stride(1) != 1)):
+        raise ValueError("page_table must be an int32 [n_seqs, width] tensor on the caches' device, rows contiguous")
+    if (keep.dim() != 2 or keep.dtype not in (_torch.bool, _torch.uint8) or keep.shape[0] != n or keep.get_device() != index
+            or (keep.shape[1] > 1 and keep.stride(1) != 1)):
+        raise ValueError("keep must be a bool or uint8 [n_seqs, window] tensor on the caches' device, rows contiguous")
+    status = _call_on(index, lib.kv_cache_compact_launch, stack._array, len(stack.caches), page_table.data_ptr(), page_table.stride(0),
+                      page_table.shape[1], starts.data_ptr(), lens.data_ptr(), keep.data_ptr(), keep.stride(0), keep.shape[1], new_lens.data_ptr(),
+                      n, _stream_of(index, stream))
+    if status:
+        raise TunerError(status, "kv_cache_compact_launch")
 
 
 def rmsnorm_host_workspace_bytes(n_tokens: int, hidden: int, dtype, chunk_tokens: int = 0) -> int:

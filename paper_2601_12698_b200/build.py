@@ -29,10 +29,11 @@ LIB_PATH = os.path.join(HERE, "librmsnorm_tuner.so")
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-std=c++17", "-O3", "-lineinfo",
               "-Xcompiler", "-fPIC", "-I", CSRC, "-I", INCLUDE]
 HOST_UNITS = ["launch.cu", "feasible.cu", "search.cu", "host_run.cu", "table.cu", "trace.cu", "kv_cache.cu",
-              "shared_prefix_attention.cu"]
+              "shared_prefix_attention.cu", "rotary.cu", "kv_move.cu", "prompt_attention.cu"]
 KV_FORMATS = {"plain": 0, "e4m3": 1, "int8": 2}
 # attend_instances.cu is compiled once for each of these: <query type>_<cache format>
 ATTEND_UNITS = [f"{t}_{f}" for t in ("bf16", "fp16") for f in KV_FORMATS]
+PROMPT_UNITS = ("bf16", "fp16")  # prompt_instances.cu is compiled once for each of these element types
 ELEMENT_TYPES = {"bf16": ("__nv_bfloat16", 0), "fp16": ("__half", 1), "fp32": ("float", 2)}
 GROUPS = {"reg": 0, "smem": 1, "narrow": 2, "silu": 3, "merge": 4, "fp8out": 5, "allreduce": 6, "realign": 7}
 
@@ -171,6 +172,11 @@ def build(force: bool = False, verbose: bool = False, jobs: int | None = None) -
         host_objs.append(obj)
         if stale(obj):
             work.append((os.path.join(CSRC, "attend_instances.cu"), obj, attend_unit_flags(name), verbose))
+    for name in PROMPT_UNITS:
+        obj = os.path.join(OBJ_DIR, f"prompt_{name}.o")
+        host_objs.append(obj)
+        if stale(obj):
+            work.append((os.path.join(CSRC, "prompt_instances.cu"), obj, [f"-DRT_UNIT_NAME={name}", f"-DRT_UNIT_T={ELEMENT_TYPES[name][0]}"], verbose))
     if work:
         rebuilt = True
         with ThreadPoolExecutor(max_workers=pool_size) as pool:

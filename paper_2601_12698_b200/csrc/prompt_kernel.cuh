@@ -1,0 +1,820 @@
+// Attention of whole prompts on the fifth-generation tensor cores (sm_100a, tcgen05 + tensor memory + TMA).
+//
+//     S = Q K^T,  W = 2^(score_scale S - m),  O = W V      in one pass over the keys, a running reference m and sum per row.
+//
+// A "row" is one query head of one query token.  The rows of one key/value head are packed token by token, its `group` query heads
+// side by side, so that a tile of 128 rows is 128 / group tokens: short sequences and single tokens fill tiles as well as the
+// grouping lets them, and a causal block spans few keys.  An item of work is a block of 256 rows (two tiles, one for each softmax
+// stream) of one sequence and key/value head, and a range of its key tiles of 128.
+//
+// One CTA to an SM, 16 warps, each CTA working through items:
+//   warps 0-3, 4-7   two softmax streams of 128 rows, one row to a thread (tensor memory lane = row): scores from tensor memory, m and
+//                    the sum in registers, the weights back over the scores as the 16-bit left operand of the second product;
+//   warps 8-11       look through the values of tiles that not every row sees (see below);
+//   warps 12, 13     issue the products, each for its stream;
+//   warp 14          fetches queries, keys and values with TMA into a ring of 128-byte-swizzled tiles;
+//   warp 15          works out the items.
+// The streams share keys and values and take turns on the tensor cores: while one's scores are exponentiated the other's products
+// run.  The queries and first tiles of the next item are fetched, and its first scores computed, while this one's results leave.
+//
+// Heads of more than 128 (DP = 256): both streams take the same 128 rows, each all scores and one half of the dims, as tensor memory
+// has no room for two outputs of 256 (a quarter of the products is done twice).
+//
+// The reference m is moved only when a score exceeds it by 8, as in the prefix kernel: weights reach 2^8.
+//
+// Values that a row does not see meet a weight of zero in the product, and 0 * inf is NaN.  Where a tile has such values (the diagonal, the
+// sequence's end), warps 8-11 replace infinities and NaN among the keys that not all rows see by zeros before the product, and
+// the rows that do see them add them when they are written.
+//
+// Bounds: 4 * 128 * 128 * dim flops and 128 * 128 exponentials per tile and stream; at dim 128 the tensor cores need 1024
+// cycles for that and the SM's 16 exponentials a cycle 1024 as well.
+#pragma once
+
+#include <cuda.h>
+
+#include "attend_common.cuh"
+#include "tensor_core.cuh"
+
+namespace rt {
+
+constexpr int kPromptThreads = 512;
+constexpr int kPromptTile = 128;  // keys of a tile, rows of a stream
+constexpr int kPromptItems = 4;   // ring of items
+constexpr int kPromptMaxParts = 32;
+
+struct PromptArgs {
+    const int32_t* q_starts;
+    const int32_t* k_starts;
+    int n_seqs;
+    int q_tokens, k_tokens;
+    int causal;
+    int kv_heads, group, dim;
+    int stream_tokens;  // tokens of a stream's 128 rows
+    int block_tokens;   // tokens of an item
+    int parts;          // ranges of key tiles that every block is cut into
+    float score_scale;  // softmax_scale * log2(e)
+    const unsigned char* v;
+    long long v_token_stride, v_head_stride;  // bytes
+    void* out;        // [token][head][dim]
+    float* lse;       // [token][head] or NULL
+    float* part_out;  // parts > 1: [part][token][head][dim], normalised
+    float* part_lse;  // [part][token][head], base 2
+    int* status;
+    unsigned wait_polls;
+    int drop_copies;
+};
+
+struct PromptItem {
+    int valid;
+    int q_row, tokens;    // first query row and number of query tokens
+    int k_row;            // first key row of the sequence
+    int last_key;         // last key that the first token sees (may be negative)
+    int key_step;         // 1: every further token sees one key more (causal)
+    int end_key;          // keys of the sequence
+    int tile0, tile1;     // this part's key tiles
+    int masked_from;      // first tile with keys that not every row sees
+    int kv_head, part;
+    int bad_values;       // infinities or NaN were taken out of the masked tiles' values
+};
+
+template <int DP>
+struct PromptShape {
+    static constexpr int kHalves = DP == 256 ? 2 : 1;      // column halves of a tile of keys or values, a ring slot each
+    static constexpr int kCols = DP == 256 ? 128 : DP;     // columns of a slot, and dims of a stream's output
+    static constexpr int kSlotBytes = kPromptTile * kCols * 2;
+    static constexpr int kSlots = DP == 64 ? 8 : 4;
+    static constexpr int kQueryBytes = kPromptTile * DP * 2;  // of one stream
+    static constexpr int kQueries = DP == 256 ? 1 : 2;
+    static constexpr size_t kRingAt = (size_t)kQueries * kQueryBytes;
+    static constexpr size_t kStageAt = kRingAt + (size_t)kSlots * kSlotBytes;  // 4 KB per softmax warp, where results wait to be written row by row
+    static constexpr size_t kSmem = kStageAt + 8 * 4096 + 1024;                // 1024: alignment of the tiles
+    // Of eight pairs of every 32 exponentials, so many go to the multiply-add pipe (see ex2_by_polynomial).
+    static constexpr int kPolynomial = 4;
+    static constexpr int kSoftmaxRegs = 160;  // of 2 * 128 for a softmax thread and one of another role
+};
+
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
+                 "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z) : "memory");
+}
+
+// A sequence as the items see it: its rows cut to the tensors, its number of blocks and what its first block costs.
+struct PromptSequence {
+    int q_row, q_len, k_row, k_len;
+};
+__device__ __forceinline__ PromptSequence prompt_sequence(const PromptArgs& a, int i)
+{
+    const int q0 = min(max(__ldg(a.q_starts + i), 0), a.q_tokens), q1 = min(max(__ldg(a.q_starts + i + 1), 0), a.q_tokens);
+    const int k0 = min(max(__ldg(a.k_starts + i), 0), a.k_tokens), k1 = min(max(__ldg(a.k_starts + i + 1), 0), a.k_tokens);
+    return {q0, max(q1 - q0, 0), k0, max(k1 - k0, 0)};
+}
+
+// The order in which blocks are taken, whole warps: the most expensive first, so that the CTAs end together.  A block's cost is
+// counted in blocks of keys: causal blocks of a sequence cost base, base + 1, ...; otherwise all the same.
+struct PromptOrder {
+    static constexpr int kKept = 4;  // sequences that a lane keeps in registers; further ones are looked up every time
+    const PromptArgs& a;
+    int blocks[kKept], base[kKept];
+    long long total;
+    int cost;              // the cost found last: no further block costs more
+    long long dearer;      // blocks that cost more than `cost`
+    long long not_cheaper; // blocks that cost `cost` or more
+
+    __device__ __forceinline__ void shape(int i, int& n, int& first) const
+    {
+        const PromptSequence s = prompt_sequence(a, i);
+        n = (s.q_len + a.block_tokens - 1) / a.block_tokens;
+        first = a.causal ? max(s.k_len - s.q_len, 0) / a.block_tokens : s.k_len / a.block_tokens;
+    }
+    __device__ __forceinline__ int count(int n, int first, int c) const  // blocks that cost c or more
+    {
+        return a.causal ? min(max(first + n - c, 0), n) : (first >= c ? n : 0);
+    }
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const  // f(sequence, blocks, base); sequences of 32 lanes at a time
+    {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int j = 0; j < kKept; ++j)
+            if (j * 32 < a.n_seqs) f(j * 32 + lane, blocks[j], base[j]);
+        for (int i0 = kKept * 32; i0 < a.n_seqs; i0 += 32) {
+            int n = 0, first = 0;
+            if (i0 + lane < a.n_seqs) shape(i0 + lane, n, first);
+            f(i0 + lane, n, first);
+        }
+    }
+    __device__ __forceinline__ long long all(int c) const
+    {
+        long long sum = 0;
+        each([&](int, int n, int first) { sum += __reduce_add_sync(0xFFFFFFFFu, (unsigned)count(n, first, c)); });
+        return sum;
+    }
+    __device__ __forceinline__ explicit PromptOrder(const PromptArgs& args) : a(args)
+    {
+        const int lane = threadIdx.x & 31;
+        int top = 0;
+#pragma unroll
+        for (int j = 0; j < kKept; ++j) {
+            blocks[j] = base[j] = 0;
+            if (j * 32 + lane < a.n_seqs) shape(j * 32 + lane, blocks[j], base[j]);
+        }
+        each([&](int, int n, int first) { top = max(top, first + (a.causal ? n : 0)); });
+        cost = (int)__reduce_max_sync(0xFFFFFFFFu, (unsigned)top);
+        total = all(0);
+        dearer = 0;
+        not_cheaper = all(cost);
+        if (blockIdx.x == 0) {  // starts that descend or lie outside
+            bool bad = false;
+            for (int i = lane; i <= a.n_seqs; i += 32) {
+                const int q = __ldg(a.q_starts + i), k = __ldg(a.k_starts + i);
+                bad = bad || q < 0 || q > a.q_tokens || k < 0 || k > a.k_tokens ||
+                      (i < a.n_seqs && (__ldg(a.q_starts + i + 1) < q || __ldg(a.k_starts + i + 1) < k));
+            }
+            if (bad) atomicExch(a.status, kDeviceIndexCode);
+        }
+    }
+    // Sequence and block of place `rank`; ranks ascend from call to call.
+    __device__ __forceinline__ void find(long long rank, int& seq, int& block)
+    {
+        if (rank >= not_cheaper) {
+            // the largest cost with more than `rank` blocks that cost it or more: mostly the next one down
+            int lo = 0, hi = cost;  // all(lo) > rank >= all(hi)
+            int step = 1;
+            while (hi - step > 0) {
+                if (all(hi - step) > rank) {
+                    lo = hi - step;
+                    break;
+                }
+                hi -= step;
+                step *= 2;
+            }
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) / 2;
+                if (all(mid) > rank) lo = mid;
+                else hi = mid;
+            }
+            cost = lo;
+            dearer = all(lo + 1);
+            not_cheaper = all(lo);
+        }
+        int left = (int)(rank - dearer);
+        int found_seq = -1, found_block = 0;
+        each([&](int i, int n, int first) {
+            // blocks of this sequence that cost exactly `cost`
+            const int here = count(n, first, cost) - count(n, first, cost + 1);
+            int before = here;
+#pragma unroll
+            for (int s = 1; s < 32; s <<= 1) {
+                const int x = __shfl_up_sync(0xFFFFFFFFu, before, s);
+                if ((int)(threadIdx.x & 31) >= s) before += x;
+            }
+            const int sum = __shfl_sync(0xFFFFFFFFu, before, 31);
+            before -= here;
+            const unsigned mine = __ballot_sync(0xFFFFFFFFu, found_seq < 0 && left >= before && left < before + here);
+            if (mine) {
+                const int from = __ffs(mine) - 1;
+                found_seq = __shfl_sync(0xFFFFFFFFu, i, from);
+                found_block = __shfl_sync(0xFFFFFFFFu, a.causal ? cost - first : left - before, from);
+            } else if (found_seq < 0) {
+                left -= sum;
+            }
+        });
+        seq = found_seq;
+        block = found_block;
+    }
+};
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
+                                                                            const __grid_constant__ CUtensorMap v_map, const __grid_constant__ PromptArgs a)
+{
+    using S = PromptShape<DP>;
+    constexpr bool kSplitDims = DP == 256;
+    constexpr int kBlockBytes = kTileBlockBytes;  // one 64-dim column block of a tile
+    constexpr uint32_t kScoreIdesc = tc_instruction<T>(kPromptTile, false, false);
+    constexpr uint32_t kColO = 2 * kPromptTile;
+
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    unsigned char* ring = smem + S::kRingAt;
+    __shared__ __align__(8) uint64_t full[S::kSlots], empty[S::kSlots], item_full[kPromptItems], item_free[kPromptItems], landed[4], q_full, q_free, s_full[2],
+        p_full[2][2], o_done[2], o_full[2], drained[2];
+    __shared__ PromptItem items[kPromptItems];
+    __shared__ uint32_t tmem_base;
+
+    const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
+    if (tid == 0) {
+        for (int i = 0; i < S::kSlots; ++i) {
+            mbarrier_init(&full[i], 1);
+            mbarrier_init(&empty[i], 2);
+        }
+        for (int i = 0; i < kPromptItems; ++i) {
+            mbarrier_init(&item_full[i], 1);
+            mbarrier_init(&item_free[i], 15);  // warps that read it: 8 softmax, 4 looking, 2 issuing, 1 fetching
+            mbarrier_init(&landed[i], 1);
+            items[i].valid = 0;
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbarrier_init(&s_full[i], 1);
+            mbarrier_init(&p_full[i][0], 128);
+            mbarrier_init(&p_full[i][1], 128);
+            mbarrier_init(&o_done[i], 1);
+            mbarrier_init(&o_full[i], 1);
+            mbarrier_init(&drained[i], 1);
+        }
+        mbarrier_init(&q_full, 1);
+        mbarrier_init(&q_free, 2);
+    }
+    if (warp == 12) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_base)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_base;
+    wait_for_previous_kernel();
+
+    // Every wait is bounded.  A thread whose wait has run out stops waiting, goes on to the end of the item, so that barriers and votes
+    // are still met, and then ends; the status word says that the results are not valid.  Nothing that it goes on with leads outside
+    // the tensors: items are published ones, or none.
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+        if (ok) ok = mbarrier_wait_sleeping(bar, parity, a.wait_polls);
+    };
+    // The next item (`n`-th of this CTA); false: there is none.
+    auto next_item = [&](int n, PromptItem& item) -> bool {
+        wait(&item_full[n % kPromptItems], (n / kPromptItems) & 1);
+        if (!__all_sync(0xFFFFFFFFu, ok)) return false;
+        item = items[n % kPromptItems];
+        return item.valid != 0;
+    };
+    auto done_with_item = [&](int n) {
+        __syncwarp();
+        if (lane == 0) mbarrier_arrive(&item_free[n % kPromptItems]);
+    };
+    // Key tiles that a stream's rows see: all of the item's but the last ones, or none.
+    auto stream_tiles = [&](const PromptItem& item, int s) -> int {
+        const int first = kSplitDims ? 0 : s * a.stream_tokens;
+        if (first >= item.tokens) return 0;
+        const int last_token = kSplitDims ? item.tokens - 1 : min(item.tokens, first + a.stream_tokens) - 1;
+        const int last = min(item.last_key + item.key_step * last_token, item.end_key - 1);
+        return min(item.tile1, (last + kPromptTile) / kPromptTile) - item.tile0;  // (last >= -kPromptTile where it matters: none is cut to 0 by its users)
+    };
+
+    if (warp < 8) {
+        // ---- softmax streams ----
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kSoftmaxRegs));
+        const int s = warp >> 2, r = (warp & 3) * 32 + lane;
+        const uint32_t lane_base = tmem + ((uint32_t)(warp & 3) << 21);
+        const uint32_t s_col = lane_base + s * kPromptTile, o_col = lane_base + kColO + s * S::kCols;
+        const int n_heads = a.kv_heads * a.group;
+        const float c = fmaxf(a.score_scale, 1.17549435e-38f);  // (a scale of zero would make NaN of hidden scores: the smallest normal number does instead)
+        const float2x c2 = pack_f2(c, c);
+        const int row_token = r / a.group;
+        unsigned char* stage = smem + S::kStageAt + warp * 4096;
+        const long long n_rows = (long long)a.q_tokens * n_heads;
+        uint32_t tiles_done = 0, results_done = 0;  // of this stream
+        PromptItem item;
+        for (int n = 0; next_item(n, item); ++n) {
+            const int first_token = kSplitDims ? 0 : s * a.stream_tokens;
+            const int my_tiles = max(stream_tiles(item, s), 0);
+            // [token][head] index of row i of this stream's 128, -1: no such row
+            const auto row_index = [&](int i) -> long long {
+                const int t = i / a.group, token = first_token + t;
+                if (t >= a.stream_tokens || token >= item.tokens) return -1;
+                return (long long)(item.q_row + token) * n_heads + item.kv_head * a.group + (i - t * a.group);
+            };
+            // last key that this row sees; rows that are not there see all
+            const bool there = row_token < a.stream_tokens && first_token + row_token < item.tokens;
+            const int last = there ? min(item.last_key + item.key_step * (first_token + row_token), item.end_key - 1) : item.end_key - 1;
+            float m = -INFINITY, l = 0.f;
+            for (int i = 0; i < my_tiles; ++i) {
+                const int tile = item.tile0 + i;
+                const bool masked = tile >= item.masked_from;
+                const int lim = last - tile * kPromptTile;  // columns up to this one are seen
+                const uint32_t half0 = 2 * (tiles_done + i);
+                wait(&s_full[s], (tiles_done + i) & 1);
+                tc_fence_after();
+                // Half a tile at a time: its product with the values runs while the other half is exponentiated.
+#pragma unroll 1
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t col = s_col + h * 64;
+                    // One pass over the row's 64 scores gives their maximum and, with the reference as it is, the weights and their sum.
+                    // Only when the maximum turns out to be more than 8 above the reference is the pass made again, with a reference
+                    // that has been moved there; the scores are still in tensor memory, the weights go over them at the end.
+                    uint32_t w[2][16];
+                    float2x sum[2];
+                    for (;;) {
+                        // No key of the row so far: the reference is -inf, every score is -inf, and so must every weight's logarithm be.
+                        const float reference = m == -INFINITY ? 0.f : m;
+                        const float2x minus2 = pack_f2(-reference, -reference);
+                        float t4[2] = {-INFINITY, -INFINITY};
+                        sum[0] = sum[1] = pack_f2(0.f, 0.f);
+                        uint32_t v2[2][32];
+                        tmem_load32(col, v2[0]);
+                        tmem_load32(col + 32, v2[1]);
+                        tmem_wait_load(v2[0]);
+                        tmem_loaded(v2[1]);
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            uint32_t(&v)[32] = v2[q];
+                            if (masked) {
+                                const int seen = lim - h * 64 - q * 32;
+#pragma unroll
+                                for (int k = 0; k < 32; ++k)
+                                    if (k > seen) v[k] = 0xFF800000u;
+                            }
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                float2x t0 = pack_f2(__uint_as_float(v[4 * k]), __uint_as_float(v[4 * k + 1]));
+                                float2x t1 = pack_f2(__uint_as_float(v[4 * k + 2]), __uint_as_float(v[4 * k + 3]));
+                                float x[4];
+                                unpack_f2(t0, x[0], x[1]);
+                                unpack_f2(t1, x[2], x[3]);
+                                t4[0] = fmaxf(fmaxf(t4[0], x[0]), x[1]);
+                                t4[1] = fmaxf(fmaxf(t4[1], x[2]), x[3]);
+                                t0 = fma_f2(t0, c2, minus2);
+                                t1 = fma_f2(t1, c2, minus2);
+                                if (k % 8 < S::kPolynomial) t1 = ex2_by_polynomial<-127>(t1);  // (a key that is not seen weighs nothing, or a huge value of it would count)
+                                unpack_f2(t0, x[0], x[1]);
+                                unpack_f2(t1, x[2], x[3]);
+                                x[0] = ex2(x[0]);
+                                x[1] = ex2(x[1]);
+                                if (k % 8 >= S::kPolynomial) {
+                                    x[2] = ex2(x[2]);
+                                    x[3] = ex2(x[3]);
+                                }
+                                sum[0] = add_f2(pack_f2(x[0], x[1]), sum[0]);
+                                sum[1] = add_f2(pack_f2(x[2], x[3]), sum[1]);
+                                w[q][2 * k] = pack2<T>(x[0], x[1]);
+                                w[q][2 * k + 1] = pack2<T>(x[2], x[3]);
+                            }
+                        }
+                        float top = fmaxf(t4[0], t4[1]);
+                        top = top == -INFINITY ? top : top * c;
+                        const bool move = top > m + 8.f;
+                        if (!__any_sync(0xFFFFFFFFu, move)) break;
+                        const float alpha = move ? ex2(m - top) : 1.f;
+                        if (i + h > 0) {  // the products so far are complete before they are rescaled
+                            wait(&o_done[s], (half0 + h - 1) & 1);
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int q = 0; q < S::kCols / 16; ++q) {
+                                uint32_t o[16];
+                                tmem_load16(o_col + q * 16, o);
+                                tmem_wait_load(o);
+#pragma unroll
+                                for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
+                                tmem_store16(o_col + q * 16, o);
+                            }
+                        }
+                        l *= alpha;
+                        if (move) m = top;
+                    }
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) tmem_store16(col + q * 16, w[q]);
+                    float part_sum[2];
+                    unpack_f2(add_f2(sum[0], sum[1]), part_sum[0], part_sum[1]);
+                    l += part_sum[0] + part_sum[1];
+                    tmem_wait_store();
+                    tc_fence_before();
+                    mbarrier_arrive(&p_full[s][h]);
+                }
+            }
+            tiles_done += my_tiles;
+
+            // the item's rows
+            if (my_tiles > 0) {
+                wait(&o_full[s], results_done & 1);
+                ++results_done;
+                tc_fence_after();
+                if (*reinterpret_cast<volatile int*>(&items[n % kPromptItems].bad_values) != 0) {
+                    // Infinities and NaN among the keys that not all rows see were left out of the product: the rows that see them get them now.
+                    const int from = max(item.last_key + 1, item.tile0 * kPromptTile);
+                    const int to = there ? min(last + 1, item.tile1 * kPromptTile) : from;
+                    const unsigned char* values = a.v + (long long)item.k_row * a.v_token_stride + (long long)item.kv_head * a.v_head_stride + (kSplitDims ? s * 256 : 0);
+                    const int dims = min(a.dim - (kSplitDims ? s * 128 : 0), S::kCols);
+#pragma unroll 1
+                    for (int q = 0; q < S::kCols / 16; ++q) {
+                        uint32_t o[16];
+                        tmem_load16(o_col + q * 16, o);
+                        tmem_wait_load(o);
+                        for (int key = max(from, 0); key < to; ++key) {
+                            const unsigned short* p = reinterpret_cast<const unsigned short*>(values + (long long)key * a.v_token_stride) + q * 16;
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) {
+                                if (q * 16 + k < dims) {
+                                    const float x = Codec<T, 16>::to_float16(__ldg(p + k));
+                                    if (!(fabsf(x) < INFINITY)) o[k] = __float_as_uint(__uint_as_float(o[k]) + x);
+                                }
+                            }
+                        }
+                        tmem_store16(o_col + q * 16, o);
+                    }
+                    tmem_wait_store();
+                }
+            }
+            if (first_token >= item.tokens) {  // no rows for this stream
+                done_with_item(n);
+                continue;
+            }
+            const long long my_row = row_index(r);
+            const bool none = l == 0.f;
+            const float inv = none ? 0.f : 1.0f / l, total = none ? -INFINITY : m + log2f(l);
+            if (my_row >= 0 && (!kSplitDims || s == 0)) {
+                if (a.parts > 1) a.part_lse[item.part * n_rows + my_row] = total;
+                else if (a.lse) a.lse[my_row] = total * 0.69314718055994531f;
+            }
+            // A thread holds a row, and rows lie apart: 128 bytes of every row at a time go through shared memory, so that eight lanes
+            // write them side by side.
+            long long to_row[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) to_row[k] = row_index((warp & 3) * 32 + k * 4 + (lane >> 3));
+            const int dim0 = kSplitDims ? s * 128 : 0;
+            if (a.parts > 1) {
+#pragma unroll 1
+                for (int q = 0; q < S::kCols / 32; ++q) {
+                    uint32_t o[32];
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) o[k] = 0;
+                    if (my_tiles > 0) {
+                        tmem_load32(o_col + q * 32, o);
+                        tmem_wait_load(o);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        float4 x = make_float4(__uint_as_float(o[4 * k]) * inv, __uint_as_float(o[4 * k + 1]) * inv, __uint_as_float(o[4 * k + 2]) * inv, __uint_as_float(o[4 * k + 3]) * inv);
+                        if (none) x = make_float4(0.f, 0.f, 0.f, 0.f);
+                        *reinterpret_cast<float4*>(stage + lane * 128 + ((k ^ (lane & 7)) << 4)) = x;
+                    }
+                    __syncwarp();
+                    const int col = dim0 + q * 32 + (lane & 7) * 4;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int row = k * 4 + (lane >> 3);
+                        const float4 x = *reinterpret_cast<const float4*>(stage + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
+                        if (to_row[k] >= 0 && col < a.dim) *reinterpret_cast<float4*>(a.part_out + (item.part * n_rows + to_row[k]) * a.dim + col) = x;
+                    }
+                    __syncwarp();
+                }
+            } else {
+#pragma unroll 1
+                for (int q = 0; q < S::kCols / 64; ++q) {
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        uint32_t o[32];
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) o[k] = 0;
+                        if (my_tiles > 0) {
+                            tmem_load32(o_col + q * 64 + half * 32, o);
+                            tmem_wait_load(o);
+                        }
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            uint32_t y[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                y[j] = none ? 0u : pack2<T>(__uint_as_float(o[8 * k + 2 * j]) * inv, __uint_as_float(o[8 * k + 2 * j + 1]) * inv);
+                            *reinterpret_cast<uint4*>(stage + lane * 128 + (((half * 4 + k) ^ (lane & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+                        }
+                    }
+                    __syncwarp();
+                    const int col = dim0 + q * 64 + (lane & 7) * 8;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int row = k * 4 + (lane >> 3);
+                        const uint4 x = *reinterpret_cast<const uint4*>(stage + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
+                        if (to_row[k] >= 0 && col < a.dim) *reinterpret_cast<uint4*>(reinterpret_cast<unsigned char*>(a.out) + (to_row[k] * a.dim + col) * 2) = x;
+                    }
+                    __syncwarp();
+                }
+            }
+            tc_fence_before();  // the output's columns have been read before the next item's weights are announced
+            done_with_item(n);
+        }
+    } else {
+        // (one instruction for all of a warpgroup's warps, whatever their role)
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(256 - S::kSoftmaxRegs));
+    }
+    if (warp >= 8 && warp < 12) {
+        // ---- warps that look through the values of tiles that not every row sees ----
+        const int p = tid - 256;  // the tile's key
+        constexpr uint32_t kExponent = std::is_same<T, __nv_bfloat16>::value ? 0x7F807F80u : 0x7C007C00u;
+        uint32_t tiles_before = 0, looked_at = 0;  // (tiles that every row sees go past these warps: a barrier of their own tells them of the others)
+        PromptItem item;
+        for (int n = 0; next_item(n, item); ++n) {
+            for (int tile = max(item.tile0, item.masked_from); tile < item.tile1; ++tile) {
+                bool found = false;
+                wait(&landed[looked_at % 4], (looked_at / 4) & 1);
+                ++looked_at;
+#pragma unroll
+                for (int half = 0; half < S::kHalves; ++half) {
+                    const uint32_t unit = (tiles_before + tile - item.tile0) * 2 * S::kHalves + S::kHalves + half, slot = unit % S::kSlots;
+                    if (tile * kPromptTile + p > item.last_key) {
+#pragma unroll
+                        for (int b = 0; b < S::kCols / 64; ++b) {
+#pragma unroll
+                            for (int u = 0; u < 8; ++u) {
+                                uint4* at = reinterpret_cast<uint4*>(ring + slot * S::kSlotBytes + b * kBlockBytes + p * 128 + ((u ^ (p & 7)) << 4));
+                                uint4 x = *at;
+                                const uint4 bad = make_uint4(__vcmpeq2(x.x & kExponent, kExponent), __vcmpeq2(x.y & kExponent, kExponent),
+                                                             __vcmpeq2(x.z & kExponent, kExponent), __vcmpeq2(x.w & kExponent, kExponent));
+                                if (bad.x | bad.y | bad.z | bad.w) {
+                                    *at = make_uint4(x.x & ~bad.x, x.y & ~bad.y, x.z & ~bad.z, x.w & ~bad.w);
+                                    found = true;
+                                }
+                            }
+                        }
+                    }
+                }
+                if (found && tile * kPromptTile + p < item.end_key) *reinterpret_cast<volatile int*>(&items[n % kPromptItems].bad_values) = 1;
+                fence_async_proxy();
+                asm volatile("barrier.cta.sync 1, 128;" ::: "memory");
+                if (p < S::kHalves) mbarrier_arrive(&full[((tiles_before + tile - item.tile0) * 2 * S::kHalves + S::kHalves + p) % S::kSlots]);
+            }
+            tiles_before += item.tile1 - item.tile0;
+            done_with_item(n);
+        }
+    } else if (warp >= 12 && warp < 14) {
+        // ---- warps that issue the products of the two streams ----
+        const int s = warp - 12;
+        constexpr uint64_t kRowsLayout = tc_layout(16, 1024), kColsLayout = tc_layout(kBlockBytes, 1024);
+        constexpr uint32_t kSlot16 = S::kSlotBytes / 16, kBlock = kBlockBytes / 16;
+        const uint32_t q16 = smem_u32(smem) >> 4, ring16 = smem_u32(ring) >> 4;
+        const uint64_t q_at = tc_descriptor(kRowsLayout, q16 + (kSplitDims ? 0 : s) * (S::kQueryBytes / 16));
+        const uint64_t k_base = tc_descriptor(kRowsLayout, ring16), v_base = tc_descriptor(kColsLayout, ring16);
+        const uint32_t d_scores = tmem + s * kPromptTile, d_out = tmem + kColO + s * S::kCols;
+        const int steps = (a.dim + 15) / 16;  // of 16 dims
+        const int out_dims = max(16, min((a.dim - (kSplitDims ? s * 128 : 0) + 15) / 16 * 16, S::kCols));
+        const uint32_t out_idesc = tc_instruction<T>(out_dims, false, true);
+        uint32_t tiles_before = 0, my_tiles_before = 0, items_before = 0;
+        auto unit_of = [&](uint32_t tile, int which) { return tile * 2 * S::kHalves + which; };
+        auto wait_unit = [&](uint32_t unit) {
+            wait(&full[unit % S::kSlots], (unit / S::kSlots) & 1);
+            tc_fence_after();
+        };
+        auto skip_unit = [&](uint32_t unit) {  // a tile that this stream does not need
+            wait(&full[unit % S::kSlots], (unit / S::kSlots) & 1);
+            if (lane == 0) mbarrier_arrive(&empty[unit % S::kSlots]);
+            __syncwarp();
+        };
+        PromptItem item;
+        for (int n = 0; next_item(n, item); ++n) {
+            const int tiles = item.tile1 - item.tile0, mine = max(stream_tiles(item, s), 0);
+            if (tiles > 0) {
+                wait(&q_full, items_before & 1);
+                tc_fence_after();
+            }
+            // S = Q K^T with the item's tile number i
+            auto scores = [&](int i) {
+                const uint32_t unit = unit_of(tiles_before + i, 0);
+#pragma unroll
+                for (int half = 0; half < S::kHalves; ++half) wait_unit(unit + half);
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < DP / 16; ++k) {
+                        const uint32_t slot = (unit + k / 8) % S::kSlots;  // (heads of 256: dims from 128 on are in the second half's slot)
+                        if (k < steps)
+                            tc_mma_ss(d_scores, q_at + ((k >> 2) * kBlock + (k & 3) * 2), k_base + (slot * kSlot16 + ((k >> 2) & 1) * kBlock + (k & 3) * 2), kScoreIdesc, k > 0);
+                    }
+                    tc_commit(&s_full[s]);
+#pragma unroll
+                    for (int half = 0; half < S::kHalves; ++half) tc_commit(&empty[(unit + half) % S::kSlots]);
+                    if (i + 1 == mine) tc_commit(&q_free);
+                }
+                __syncwarp();
+            };
+            if (mine > 0) scores(0);
+            else if (tiles > 0 && lane == 0) mbarrier_arrive(&q_free);
+            for (int i = 0; i < tiles; ++i) {
+                const uint32_t unit = unit_of(tiles_before + i, S::kHalves);
+                if (i >= mine) {
+#pragma unroll
+                    for (int half = 0; half < S::kHalves; ++half) skip_unit(unit - S::kHalves + half);
+#pragma unroll
+                    for (int half = 0; half < S::kHalves; ++half) {
+                        skip_unit(unit + half);
+                    }
+                    continue;
+                }
+                // O += W V.  Heads of 256: this stream's half of the dims; the other half is the other stream's.
+                const uint32_t my_unit = unit + (kSplitDims ? s : 0), slot = my_unit % S::kSlots;
+                wait_unit(my_unit);
+                const uint64_t v_at = v_base + slot * kSlot16;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    wait(&p_full[s][h], (my_tiles_before + i) & 1);
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < kPromptTile / 32; ++k)
+                            tc_mma_ts(d_out, d_scores + h * 64 + k * 8, v_at + (h * 64 * 128 / 16 + k * 128), out_idesc, i + h + k > 0);
+                        tc_commit(&o_done[s]);
+                        if (h == 1) {
+                            tc_commit(&empty[slot]);
+                            if (kSplitDims) tc_commit(&empty[slot]);  // (the only stream that reads it)
+                            if (i + 1 == mine) tc_commit(&o_full[s]);
+                        }
+                    }
+                    __syncwarp();
+                }
+                if (i + 1 < mine) scores(i + 1);
+            }
+            tiles_before += tiles;
+            my_tiles_before += mine;
+            if (tiles > 0) ++items_before;
+            done_with_item(n);
+        }
+        // the tensor memory is given back only when nothing writes it any more
+        if (elect_one()) tc_commit(&drained[s]);
+        __syncwarp();
+        ok = mbarrier_wait_sleeping(&drained[s], 0) && ok;
+    } else if (warp == 14) {
+        // ---- the warp that fetches ----
+        uint32_t units = 0, items_before = 0, looks = 0;
+        bool posted = false;
+        const uint32_t query_bytes = (uint32_t)(a.stream_tokens * a.group) * 128u * (DP / 64);
+        // One half of a tile; `bar` is told of its bytes, and first of how many to expect (0: it knows).
+        auto fetch = [&](const CUtensorMap* map, int col0, const PromptItem& item, int tile, uint64_t* bar, uint32_t expected) {
+            const uint32_t slot = units % S::kSlots;
+            wait(&empty[slot], ((units / S::kSlots) & 1) ^ 1);
+            if (!a.drop_copies && elect_one()) {
+                if (!bar) bar = &full[slot];
+                if (expected) mbarrier_expect_tx(bar, expected);
+#pragma unroll
+                for (int b = 0; b < S::kCols / 64; ++b)
+                    tma_load_3d(ring + slot * S::kSlotBytes + b * kBlockBytes, map, col0 + b * 64, item.kv_head, item.k_row + tile * kPromptTile, bar);
+            }
+            __syncwarp();
+            ++units;
+        };
+        PromptItem item;
+        for (int n = 0; next_item(n, item); ++n) {
+            const int tiles = item.tile1 - item.tile0;
+            if (tiles > 0) {
+                wait(&q_free, (items_before & 1) ^ 1);
+                if (!a.drop_copies && elect_one()) {
+                    mbarrier_expect_tx(&q_full, query_bytes * S::kQueries);
+#pragma unroll
+                    for (int s = 0; s < S::kQueries; ++s)
+#pragma unroll
+                        for (int b = 0; b < DP / 64; ++b)
+                            tma_load_3d(smem + s * S::kQueryBytes + b * kBlockBytes, &q_map, b * 64, item.kv_head * a.group, item.q_row + s * a.stream_tokens, &q_full);
+                }
+                __syncwarp();
+                posted = !a.drop_copies;
+                ++items_before;
+            }
+            for (int i = 0; i < tiles; ++i) {
+#pragma unroll
+                for (int half = 0; half < S::kHalves; ++half) fetch(&k_map, half * 128, item, item.tile0 + i, nullptr, S::kSlotBytes);
+                const bool masked = item.tile0 + i >= item.masked_from;  // then those who look through the values tell the others
+#pragma unroll
+                for (int half = 0; half < S::kHalves; ++half)
+                    fetch(&v_map, half * 128, item, item.tile0 + i, masked ? &landed[looks % 4] : nullptr,
+                          masked ? (half == 0 ? S::kSlotBytes * S::kHalves : 0) : S::kSlotBytes);
+                if (masked) ++looks;
+            }
+            done_with_item(n);
+        }
+        // no copy is under way when the CTA ends
+        if (posted) {
+            for (uint32_t m = looks > 4 ? looks - 4 : 0; m < looks; ++m) ok = mbarrier_wait_sleeping(&landed[m % 4], (m / 4) & 1) && ok;
+            ok = mbarrier_wait_sleeping(&q_full, (items_before - 1) & 1) && ok;
+            for (uint32_t u = units > S::kSlots ? units - S::kSlots : 0; u < units; ++u) ok = mbarrier_wait_sleeping(&full[u % S::kSlots], (u / S::kSlots) & 1) && ok;
+        }
+    } else if (warp == 15) {
+        // ---- the warp that works out the items ----
+        PromptOrder order(a);
+        const int per_block = a.kv_heads * a.parts;
+        const long long ids = order.total * per_block;
+        for (int n = 0;; ++n) {
+            // there and back again, so that the CTA that had the dearest item of one round has the cheapest of the next
+            const long long id = (long long)n * gridDim.x + ((n & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+            PromptItem item;
+            item.valid = 0;
+            if (id < ids) {
+                const long long rank = id / per_block;
+                const int rest = (int)(id - rank * per_block);
+                int seq, block;
+                order.find(rank, seq, block);
+                PromptSequence q = {0, 0, 0, 0};
+                if (seq >= 0) q = prompt_sequence(a, seq);  // (starts that descend can count more blocks than there are)
+                else block = 0;
+                item.valid = 1;
+                item.tokens = min(a.block_tokens, q.q_len - block * a.block_tokens);
+                item.q_row = q.q_row + block * a.block_tokens;
+                item.k_row = q.k_row;
+                item.end_key = q.k_len;
+                item.key_step = a.causal ? 1 : 0;
+                item.last_key = a.causal ? min(q.k_len - q.q_len + block * a.block_tokens, q.k_len - 1) : q.k_len - 1;
+                const int last_key = min(item.last_key + item.key_step * (item.tokens - 1), q.k_len - 1);
+                const int tiles = last_key < 0 ? 0 : last_key / kPromptTile + 1;
+                item.masked_from = max(item.last_key + 1, 0) / kPromptTile;
+                item.kv_head = rest / a.parts;
+                item.part = rest - item.kv_head * a.parts;
+                const int run = (tiles + a.parts - 1) / a.parts;
+                item.tile0 = min(item.part * run, tiles);
+                item.tile1 = min(item.tile0 + run, tiles);
+                item.bad_values = 0;
+            }
+            wait(&item_free[n % kPromptItems], ((n / kPromptItems) & 1) ^ 1);
+            if (!__all_sync(0xFFFFFFFFu, ok)) break;
+            if (lane == 0) {
+                items[n % kPromptItems] = item;
+                mbarrier_arrive(&item_full[n % kPromptItems]);
+            }
+            __syncwarp();
+            if (!item.valid) break;
+        }
+    }
+    if (!ok) atomicExch(a.status, kDeviceTimeoutCode);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+// Joins the parts of every row: weights 2^(lse_p - max) / sum.  One warp per row; a lane looks after the weight of one part, the
+// parts' outputs are fetched independently of one another.  A part that saw keys never weighs nothing, or a NaN among its values would be lost with it.
+constexpr int kPromptMergeThreads = 128;
+template <typename T>
+__global__ void __launch_bounds__(kPromptMergeThreads) prompt_merge_kernel(const __grid_constant__ PromptArgs a)
+{
+    const int lane = threadIdx.x & 31, n_heads = a.kv_heads * a.group;
+    const long long row = (long long)blockIdx.x * (kPromptMergeThreads / 32) + (threadIdx.x >> 5), n_rows = (long long)a.q_tokens * n_heads;
+    wait_for_previous_kernel();
+    const int token = (int)(row / n_heads);
+    if (row >= n_rows || token < __ldg(a.q_starts) || token >= __ldg(a.q_starts + a.n_seqs)) return;  // a row of no sequence
+    const float lse = lane < a.parts ? a.part_lse[lane * n_rows + row] : -INFINITY;
+    float top = lse;
+#pragma unroll
+    for (int s = 16; s >= 1; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
+    const float base = top == -INFINITY ? 0.f : top;
+    float w = lse == -INFINITY ? 0.f : ex2(lse - base);
+    if (w == 0.f && lse != -INFINITY) w = __uint_as_float(1u);
+    float total = w;
+#pragma unroll
+    for (int s = 16; s >= 1; s >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, s);
+    const float inv = total == 0.f ? 0.f : 1.0f / total;
+    for (int d0 = 0; d0 < a.dim; d0 += 128) {
+        const int d = d0 + lane * 4;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int p = 0; p < a.parts; ++p) {
+            const float wp = __shfl_sync(0xFFFFFFFFu, w, p);
+            if (wp == 0.f || d >= a.dim) continue;
+            const float4 x = *reinterpret_cast<const float4*>(a.part_out + (p * n_rows + row) * a.dim + d);
+            o.x = fmaf(wp, x.x, o.x); o.y = fmaf(wp, x.y, o.y);
+            o.z = fmaf(wp, x.z, o.z); o.w = fmaf(wp, x.w, o.w);
+        }
+        if (d < a.dim)
+            *reinterpret_cast<uint2*>(reinterpret_cast<unsigned char*>(a.out) + (row * a.dim + d) * 2) =
+                make_uint2(pack2<T>(o.x * inv, o.y * inv), pack2<T>(o.z * inv, o.w * inv));
+    }
+    if (lane == 0 && a.lse) a.lse[row] = total == 0.f ? -INFINITY : (top + log2f(total)) * 0.69314718055994531f;
+}
+
+}  // namespace rt

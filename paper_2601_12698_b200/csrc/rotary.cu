@@ -1,0 +1,215 @@
+// Entry points of the rotary positions: frequencies, argument checks, the launch rule and the kernel's instances.
+#include <math.h>
+#include <string.h>
+
+#include "rotary_kernel.cuh"
+#include "tuner_internal.h"
+
+namespace rt {
+namespace {
+
+constexpr double kTwoPi = 6.283185307179586476925286766559;
+
+bool positive(double x) { return x > 0 && x < INFINITY; }
+
+int check_spec(const rt_rotary_spec* s)
+{
+    if (s->rot_dim < 2 || s->rot_dim > RT_KV_MAX_HEAD_DIM || s->rot_dim % 2 || s->scaling < RT_ROTARY_NONE || s->scaling > RT_ROTARY_YARN) {
+        set_error("rot_dim=%d or scaling=%d out of range", (int)s->rot_dim, (int)s->scaling);
+        return RT_ERR_SHAPE;
+    }
+    const bool stretched = s->scaling != RT_ROTARY_NONE, by_length = s->scaling == RT_ROTARY_BANDS || s->scaling == RT_ROTARY_YARN;
+    if (!(s->base > 1 && s->base < INFINITY) || (stretched && !positive(s->factor)) || (by_length && !positive(s->original_len)) ||
+        (s->scaling == RT_ROTARY_NTK && s->rot_dim < 4) ||
+        (s->scaling == RT_ROTARY_BANDS && !(positive(s->low_turns) && positive(s->high_turns) && s->low_turns < s->high_turns)) ||
+        (s->scaling == RT_ROTARY_YARN && !(positive(s->slow_turns) && positive(s->fast_turns) && s->slow_turns < s->fast_turns))) {
+        set_error("base, factor, original_len or turns out of range for scaling %d", (int)s->scaling);
+        return RT_ERR_SHAPE;
+    }
+    return RT_OK;
+}
+
+double between_0_and_1(double x) { return x < 0 ? 0 : x > 1 ? 1 : x; }
+
+typedef void (*RotaryKernel)(RotaryArgs);
+
+template <typename T, int P>
+int launch_rotary(RotaryArgs a, int rot, int tail_elems, bool interleaved, cudaStream_t stream)
+{
+    constexpr int VB = P * (int)sizeof(T);
+    a.items = rot / 2 / P;
+    a.second = interleaved ? VB : rot / 2 * (int)sizeof(T);
+    a.interleaved = interleaved;
+    a.first_step = interleaved ? 2 * VB : VB;
+    a.tail = tail_elems / P;
+    rt_limits L;
+    const int st = current_limits(&L);
+    if (st != RT_OK) return st;
+    // A token's heads go to as few threads as still fill the device: every thread computes its own P sines and cosines, which is
+    // what few heads a thread cost, and U heads of a thread are in flight at once.
+    const int heads = a.side[0].heads + a.side[1].heads;
+    const int groups = kRotaryThreads / a.items;
+    constexpr int U = 4;
+    a.split = 1;
+    while (a.split * 2 <= groups && a.split * U < heads &&
+           a.n_tokens * a.split * a.items < (long long)L.sm_count * 1024)
+        a.split *= 2;
+    a.tokens_per_cta = groups / a.split;
+    const long long ctas = (a.n_tokens + a.tokens_per_cta - 1) / a.tokens_per_cta;
+    if (ctas > 0x7fffffffLL) {
+        set_error("n_tokens=%lld needs too many CTAs", (long long)a.n_tokens);
+        return RT_ERR_SHAPE;
+    }
+    const int threads = (a.tokens_per_cta * a.split * a.items + 31) / 32 * 32;
+    void* params[] = {&a};
+    return launch_kernel((const void*)(RotaryKernel)rotary_kernel<T, P, U>, dim3((unsigned)ctas), dim3((unsigned)threads), 0, stream, params);
+}
+
+template <typename T>
+int launch_typed(const RotaryArgs& a, int width, int rot, int tail, bool interleaved, cudaStream_t stream)
+{
+    if constexpr (sizeof(T) == 2) {
+        if (width == 8) return launch_rotary<T, 8>(a, rot, tail, interleaved, stream);
+    }
+    if (width >= 4) return launch_rotary<T, 4>(a, rot, tail, interleaved, stream);
+    if (width >= 2) return launch_rotary<T, 2>(a, rot, tail, interleaved, stream);
+    return launch_rotary<T, 1>(a, rot, tail, interleaved, stream);
+}
+
+}  // namespace
+}  // namespace rt
+
+extern "C" {
+
+int rotary_frequencies(const rt_rotary_spec* s, uint64_t* turns, float* magnitude)
+{
+    using namespace rt;
+    if (!s || !turns || !magnitude) {
+        set_error("spec, turns or magnitude is NULL");
+        return RT_ERR_NULL;
+    }
+    const int st = check_spec(s);
+    if (st != RT_OK) return st;
+    const int rot = s->rot_dim;
+    const double base = s->scaling == RT_ROTARY_NTK ? s->base * pow(s->factor, (double)rot / (rot - 2)) : s->base;
+    double first = 0, last = 0;
+    if (s->scaling == RT_ROTARY_YARN) {
+        const auto pair = [&](double n) { return rot * log(s->original_len / (kTwoPi * n)) / (2 * log(base)); };
+        first = fmax(0.0, floor(pair(s->fast_turns)));
+        last = fmin(rot - 1.0, ceil(pair(s->slow_turns)));
+    }
+    for (int j = 0; j < rot / 2; ++j) {
+        double theta = pow(base, -2.0 * j / rot);
+        if (s->scaling == RT_ROTARY_LINEAR) theta /= s->factor;
+        if (s->scaling == RT_ROTARY_BANDS) {
+            const double keep = between_0_and_1((s->original_len * theta / kTwoPi - s->low_turns) / (s->high_turns - s->low_turns));
+            theta = theta * keep + theta / s->factor * (1 - keep);
+        }
+        if (s->scaling == RT_ROTARY_YARN) {
+            const double divided = between_0_and_1((j - first) / fmax(last - first, 0.001));
+            theta = theta / s->factor * divided + theta * (1 - divided);
+        }
+        double part = theta / kTwoPi;
+        part -= floor(part);
+        const double scaled = ldexp(part, 64);
+        turns[j] = scaled >= 18446744073709551616.0 ? 0 : (uint64_t)scaled;
+    }
+    *magnitude = s->scaling == RT_ROTARY_YARN ? (float)(0.1 * log(s->factor) + 1) : 1.0f;
+    return RT_OK;
+}
+
+int rotary_launch(const rt_rotary* r, const int64_t* positions, int64_t n_tokens, int32_t head_dim, const void* q, int64_t q_token_stride,
+                  int64_t q_head_stride, void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, int32_t q_heads, const void* k,
+                  int64_t k_token_stride, int64_t k_head_stride, void* k_out, int64_t k_out_token_stride, int64_t k_out_head_stride,
+                  int32_t k_heads, int dtype, void* stream)
+{
+    using namespace rt;
+    if (!r) {
+        set_error("rotary is NULL");
+        return RT_ERR_NULL;
+    }
+    if (dtype < RT_BF16 || dtype > RT_FP32) {
+        set_error("dtype %d is not an rt_dtype", dtype);
+        return RT_ERR_DTYPE;
+    }
+    if (n_tokens < 0 || head_dim < 2 || head_dim > RT_KV_MAX_HEAD_DIM || r->rot_dim < 2 || r->rot_dim > head_dim || r->rot_dim % 2) {
+        set_error("n_tokens=%lld head_dim=%d rot_dim=%d out of range", (long long)n_tokens, (int)head_dim, (int)r->rot_dim);
+        return RT_ERR_SHAPE;
+    }
+    const struct {
+        const void* in;
+        void* out;
+        int64_t in_token_stride, in_head_stride, out_token_stride, out_head_stride;
+        int32_t heads;
+    } sides[2] = {{q, q_out, q_token_stride, q_head_stride, q_out_token_stride, q_out_head_stride, q_heads},
+                  {k, k_out, k_token_stride, k_head_stride, k_out_token_stride, k_out_head_stride, k_heads}};
+    const int64_t size = elem_bytes_of(dtype);
+    RotaryArgs a;
+    memset(&a, 0, sizeof(a));
+    // The widest vectors of P elements that rot / 2, the tail, the pointers and the strides allow.
+    int width = size == 2 ? 8 : 4;
+    while (width > 1 && (r->rot_dim / 2 % width || (head_dim - r->rot_dim) % width)) width /= 2;
+    uintptr_t places = 0;
+    bool copies = false;
+    for (int i = 0; i < 2; ++i) {
+        const auto* s = &sides[i];
+        if (s->heads == 0) continue;
+        if (s->heads < 0 || s->heads > 65535 || s->in_token_stride < 0 || s->in_head_stride < 0 || s->out_token_stride < 0 || s->out_head_stride < 0 ||
+            (n_tokens > 1 && s->out_token_stride == 0) || (s->heads > 1 && s->out_head_stride == 0)) {
+            set_error("heads=%d or a stride out of range", (int)s->heads);
+            return RT_ERR_SHAPE;
+        }
+        if (n_tokens == 0) continue;
+        if (!s->in || !s->out) {
+            set_error("a tensor pointer is NULL");
+            return RT_ERR_NULL;
+        }
+        if (((uintptr_t)s->in | (uintptr_t)s->out) & (uintptr_t)(size - 1)) {
+            set_error("a tensor is not aligned to its element size");
+            return RT_ERR_ALIGN;
+        }
+        RotarySide& d = a.side[i];
+        d.in = (const unsigned char*)s->in;
+        d.out = (unsigned char*)s->out;
+        d.in_token = s->in_token_stride * size;
+        d.in_head = s->in_head_stride * size;
+        d.out_token = s->out_token_stride * size;
+        d.out_head = s->out_head_stride * size;
+        d.heads = s->heads;
+        const bool same = s->in == s->out && (n_tokens == 1 || d.in_token == d.out_token) && (d.heads == 1 || d.in_head == d.out_head);
+        if (s->in == s->out && !same) {
+            set_error("in and out overlap with different strides");
+            return RT_ERR_SHAPE;
+        }
+        d.copy_tail = !same;
+        copies = copies || !same;
+        places |= (uintptr_t)s->in | (uintptr_t)s->out;
+        if (n_tokens > 1) places |= (uintptr_t)d.in_token | (uintptr_t)d.out_token;
+        if (d.heads > 1) places |= (uintptr_t)d.in_head | (uintptr_t)d.out_head;
+    }
+    if (n_tokens == 0 || a.side[0].heads + a.side[1].heads == 0) return RT_OK;
+    if (!positions || !r->turns) {
+        set_error("positions or turns is NULL");
+        return RT_ERR_NULL;
+    }
+    if (((uintptr_t)positions | (uintptr_t)r->turns) & 7u) {
+        set_error("positions or turns is not aligned to 8 bytes");
+        return RT_ERR_ALIGN;
+    }
+    while (width > 1 && (places & (uintptr_t)(width * size - 1))) width /= 2;
+    a.turns = (const unsigned long long*)r->turns;
+    a.positions = (const long long*)positions;
+    a.n_tokens = n_tokens;
+    a.rot_bytes = r->rot_dim * (int)size;
+    a.magnitude = r->magnitude;
+    a.sign = r->backward ? -1.f : 1.f;
+    const int tail = copies ? head_dim - r->rot_dim : 0;
+    const bool inter = r->interleaved != 0;
+    switch (dtype) {
+        case RT_BF16: return launch_typed<__nv_bfloat16>(a, width, r->rot_dim, tail, inter, (cudaStream_t)stream);
+        case RT_FP16: return launch_typed<__half>(a, width, r->rot_dim, tail, inter, (cudaStream_t)stream);
+        default: return launch_typed<float>(a, width, r->rot_dim, tail, inter, (cudaStream_t)stream);
+    }
+}
+
+}  // extern "C"
