@@ -232,13 +232,13 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
     using S = PromptShape<DP>;
     constexpr bool kSplitDims = DP == 256;
     constexpr int kBlockBytes = kTileBlockBytes;  // one 64-dim column block of a tile
-    constexpr uint32_t kScoreIdesc = tc_instruction<T>(kPromptTile, false, false);
+    constexpr uint32_t kScoreIdesc = tc_instruction<T>(kPromptTile / 2, false, false);
     constexpr uint32_t kColO = 2 * kPromptTile;
 
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     unsigned char* ring = smem + S::kRingAt;
-    __shared__ __align__(8) uint64_t full[S::kSlots], empty[S::kSlots], item_full[kPromptItems], item_free[kPromptItems], landed[4], q_full, q_free, s_full[2],
+    __shared__ __align__(8) uint64_t full[S::kSlots], empty[S::kSlots], item_full[kPromptItems], item_free[kPromptItems], landed[4], q_full, q_free, s_full[2][2],
         p_full[2][2], o_done[2], o_full[2], drained[2];
     __shared__ PromptItem items[kPromptItems];
     __shared__ uint32_t tmem_base;
@@ -256,7 +256,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
             items[i].valid = 0;
         }
         for (int i = 0; i < 2; ++i) {
-            mbarrier_init(&s_full[i], 1);
+            mbarrier_init(&s_full[i][0], 1);
+            mbarrier_init(&s_full[i][1], 1);
             mbarrier_init(&p_full[i][0], 128);
             mbarrier_init(&p_full[i][1], 128);
             mbarrier_init(&o_done[i], 1);
@@ -335,11 +336,12 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                 const bool masked = tile >= item.masked_from;
                 const int lim = last - tile * kPromptTile;  // columns up to this one are seen
                 const uint32_t half0 = 2 * (tiles_done + i);
-                wait(&s_full[s], (tiles_done + i) & 1);
-                tc_fence_after();
-                // Half a tile at a time: its product with the values runs while the other half is exponentiated.
+                // Half a tile at a time: its product with the values and the next tile's scores of that half run while the other half is
+                // exponentiated.
 #pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
+                    wait(&s_full[s][h], (tiles_done + i) & 1);
+                    tc_fence_after();
                     const uint32_t col = s_col + h * 64;
                     // One pass over the row's 64 scores gives their maximum and, with the reference as it is, the weights and their sum.
                     // Only when the maximum turns out to be more than 8 above the reference is the pass made again, with a reference
@@ -607,27 +609,34 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                 wait(&q_full, items_before & 1);
                 tc_fence_after();
             }
-            // S = Q K^T with the item's tile number i
-            auto scores = [&](int i) {
+            // Half h of S = Q K^T with the item's tile number i
+            auto scores = [&](int i, int h) {
                 const uint32_t unit = unit_of(tiles_before + i, 0);
+                if (h == 0) {
 #pragma unroll
-                for (int half = 0; half < S::kHalves; ++half) wait_unit(unit + half);
+                    for (int half = 0; half < S::kHalves; ++half) wait_unit(unit + half);
+                }
                 if (elect_one()) {
 #pragma unroll
                     for (int k = 0; k < DP / 16; ++k) {
                         const uint32_t slot = (unit + k / 8) % S::kSlots;  // (heads of 256: dims from 128 on are in the second half's slot)
                         if (k < steps)
-                            tc_mma_ss(d_scores, q_at + ((k >> 2) * kBlock + (k & 3) * 2), k_base + (slot * kSlot16 + ((k >> 2) & 1) * kBlock + (k & 3) * 2), kScoreIdesc, k > 0);
+                            tc_mma_ss(d_scores + h * 64, q_at + ((k >> 2) * kBlock + (k & 3) * 2),
+                                      k_base + (slot * kSlot16 + ((k >> 2) & 1) * kBlock + (k & 3) * 2 + h * (64 * 128 / 16)), kScoreIdesc, k > 0);
                     }
-                    tc_commit(&s_full[s]);
+                    tc_commit(&s_full[s][h]);
+                    if (h == 1) {
 #pragma unroll
-                    for (int half = 0; half < S::kHalves; ++half) tc_commit(&empty[(unit + half) % S::kSlots]);
-                    if (i + 1 == mine) tc_commit(&q_free);
+                        for (int half = 0; half < S::kHalves; ++half) tc_commit(&empty[(unit + half) % S::kSlots]);
+                        if (i + 1 == mine) tc_commit(&q_free);
+                    }
                 }
                 __syncwarp();
             };
-            if (mine > 0) scores(0);
-            else if (tiles > 0 && lane == 0) mbarrier_arrive(&q_free);
+            if (mine > 0) {
+                scores(0, 0);
+                scores(0, 1);
+            } else if (tiles > 0 && lane == 0) mbarrier_arrive(&q_free);
             for (int i = 0; i < tiles; ++i) {
                 const uint32_t unit = unit_of(tiles_before + i, S::kHalves);
                 if (i >= mine) {
@@ -659,8 +668,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                         }
                     }
                     __syncwarp();
+                    if (i + 1 < mine) scores(i + 1, h);
                 }
-                if (i + 1 < mine) scores(i + 1);
             }
             tiles_before += tiles;
             my_tiles_before += mine;
