@@ -140,15 +140,13 @@ __device__ __forceinline__ uint4 ld_codes(const unsigned char* p, bool there)
 }
 
 // 2^x for two numbers on the multiply-add pipe, beside the special function unit (16 exponentials a cycle per SM): x = n + f with
-// n the nearest integer, 2^f by the polynomial of degree 4 of least relative error on [-1/2, 1/2] (found by exchange of the extrema; 2.7e-6 in binary32, 4e-8 on average), times 2^n.  Below LOWEST = -126: 2^-126; with
-// LOWEST = -127, for keys that must not weigh anything (-inf): below -126.5 zero, as n = -127 makes a factor of zero.
-template <int LOWEST = -126>
+// n the nearest integer, 2^f by the polynomial of degree 4 of least relative error on [-1/2, 1/2] (found by exchange of the extrema; 2.7e-6 in binary32, 4e-8 on average), times 2^n.  Below -126: 2^-126.
 __device__ __forceinline__ float2x ex2_by_polynomial(float2x x)
 {
     float lo, hi;
     unpack_f2(x, lo, hi);
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(lo) : "f"(lo), "f"((float)LOWEST));
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(hi) : "f"(hi), "f"((float)LOWEST));
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(lo) : "f"(lo), "f"(-126.f));
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(hi) : "f"(hi), "f"(-126.f));
     x = pack_f2(lo, hi);
     const float2x magic = pack_f2(12582912.f, 12582912.f), minus_magic = pack_f2(-12582912.f, -12582912.f), minus_one = pack_f2(-1.f, -1.f);
     const float2x y = add_f2(x, magic);  // n in the low bits

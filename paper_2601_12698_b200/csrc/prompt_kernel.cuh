@@ -88,8 +88,6 @@ struct PromptShape {
     static constexpr size_t kRingAt = (size_t)kQueries * kQueryBytes;
     static constexpr size_t kStageAt = kRingAt + (size_t)kSlots * kSlotBytes;  // 4 KB per softmax warp, where results wait to be written row by row
     static constexpr size_t kSmem = kStageAt + 8 * 4096 + 1024;                // 1024: alignment of the tiles
-    // Of eight pairs of every 32 exponentials, so many go to the multiply-add pipe (see ex2_by_polynomial).
-    static constexpr int kPolynomial = 4;
     static constexpr int kSoftmaxRegs = 160;  // of 2 * 128 for a softmax thread and one of another role
 };
 
@@ -379,15 +377,12 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                                 t4[1] = fmaxf(fmaxf(t4[1], x[2]), x[3]);
                                 t0 = fma_f2(t0, c2, minus2);
                                 t1 = fma_f2(t1, c2, minus2);
-                                if (k % 8 < S::kPolynomial) t1 = ex2_by_polynomial<-127>(t1);  // (a key that is not seen weighs nothing, or a huge value of it would count)
                                 unpack_f2(t0, x[0], x[1]);
                                 unpack_f2(t1, x[2], x[3]);
                                 x[0] = ex2(x[0]);
                                 x[1] = ex2(x[1]);
-                                if (k % 8 >= S::kPolynomial) {
-                                    x[2] = ex2(x[2]);
-                                    x[3] = ex2(x[3]);
-                                }
+                                x[2] = ex2(x[2]);
+                                x[3] = ex2(x[3]);
                                 sum[0] = add_f2(pack_f2(x[0], x[1]), sum[0]);
                                 sum[1] = add_f2(pack_f2(x[2], x[3]), sum[1]);
                                 w[q][2 * k] = pack2<T>(x[0], x[1]);
