@@ -187,6 +187,7 @@ int prompt_attention_launch(const rt_prompt_batch* b, const void* q, int64_t q_t
     a.causal = b->causal != 0;
     a.kv_heads = kv_heads;
     a.group = p.group;
+    a.group_inverse = (65536 + p.group - 1) / p.group;
     a.dim = head_dim;
     a.stream_tokens = p.stream_tokens;
     a.block_tokens = p.block_tokens;

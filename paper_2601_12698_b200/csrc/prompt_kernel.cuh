@@ -49,6 +49,7 @@ struct PromptArgs {
     int q_tokens, k_tokens;
     int causal;
     int kv_heads, group, dim;
+    int group_inverse;  // 2^16 / group, rounded up: i / group is (i * group_inverse) >> 16 for i < 128
     int stream_tokens;  // tokens of a stream's 128 rows
     int block_tokens;   // tokens of an item
     int parts;          // ranges of key tiles that every block is cut into
@@ -151,30 +152,56 @@ struct PromptOrder {
     __device__ __forceinline__ explicit PromptOrder(const PromptArgs& args) : a(args)
     {
         const int lane = threadIdx.x & 31;
-        int top = 0;
 #pragma unroll
         for (int j = 0; j < kKept; ++j) {
             blocks[j] = base[j] = 0;
             if (j * 32 + lane < a.n_seqs) shape(j * 32 + lane, blocks[j], base[j]);
         }
-        each([&](int, int n, int first) { top = max(top, first + (a.causal ? n : 0)); });
-        cost = (int)__reduce_max_sync(0xFFFFFFFFu, (unsigned)top);
         total = all(0);
-        dearer = 0;
-        not_cheaper = all(cost);
-        if (blockIdx.x == 0) {  // starts that descend or lie outside
-            bool bad = false;
-            for (int i = lane; i <= a.n_seqs; i += 32) {
-                const int q = __ldg(a.q_starts + i), k = __ldg(a.k_starts + i);
-                bad = bad || q < 0 || q > a.q_tokens || k < 0 || k > a.k_tokens ||
-                      (i < a.n_seqs && (__ldg(a.q_starts + i + 1) < q || __ldg(a.k_starts + i + 1) < k));
-            }
-            if (bad) atomicExch(a.status, kDeviceIndexCode);
+        cost = -1;
+        dearer = not_cheaper = 0;
+    }
+    // Starts that descend or lie outside are reported (by one warp of the grid).
+    __device__ __forceinline__ void report() const
+    {
+        bool bad = false;
+        for (int i = threadIdx.x & 31; i <= a.n_seqs; i += 32) {
+            const int q = __ldg(a.q_starts + i), k = __ldg(a.k_starts + i);
+            bad = bad || q < 0 || q > a.q_tokens || k < 0 || k > a.k_tokens ||
+                  (i < a.n_seqs && (__ldg(a.q_starts + i + 1) < q || __ldg(a.k_starts + i + 1) < k));
         }
+        if (bad) atomicExch(a.status, kDeviceIndexCode);
+    }
+    // The same without an order, for a grid that takes all blocks at once.
+    __device__ __forceinline__ void find_any(long long rank, int& seq, int& block) const
+    {
+        long long before = 0;
+        seq = -1;
+        each([&](int i, int n, int) {
+            int upto = n;
+#pragma unroll
+            for (int s = 1; s < 32; s <<= 1) {
+                const int x = __shfl_up_sync(0xFFFFFFFFu, upto, s);
+                if ((int)(threadIdx.x & 31) >= s) upto += x;
+            }
+            const unsigned mine = __ballot_sync(0xFFFFFFFFu, seq < 0 && rank < before + upto);
+            if (mine && seq < 0) {
+                const int from = __ffs(mine) - 1;
+                block = (int)(rank - before) - __shfl_sync(0xFFFFFFFFu, upto - n, from);
+                seq = __shfl_sync(0xFFFFFFFFu, i, from);
+            }
+            before += __shfl_sync(0xFFFFFFFFu, upto, 31);
+        });
     }
     // Sequence and block of place `rank`; ranks ascend from call to call.
     __device__ __forceinline__ void find(long long rank, int& seq, int& block)
     {
+        if (cost < 0) {
+            int top = 0;
+            each([&](int, int n, int first) { top = max(top, first + (a.causal ? n : 0)); });
+            cost = (int)__reduce_max_sync(0xFFFFFFFFu, (unsigned)top);
+            not_cheaper = all(cost);
+        }
         if (rank >= not_cheaper) {
             // the largest cost with more than `rank` blocks that cost it or more: mostly the next one down
             int lo = 0, hi = cost;  // all(lo) > rank >= all(hi)
@@ -311,7 +338,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         const int n_heads = a.kv_heads * a.group;
         const float c = fmaxf(a.score_scale, 1.17549435e-38f);  // (a scale of zero would make NaN of hidden scores: the smallest normal number does instead)
         const float2x c2 = pack_f2(c, c);
-        const int row_token = r / a.group;
+        const int row_token = r * a.group_inverse >> 16;
         unsigned char* stage = smem + S::kStageAt + warp * 4096;
         const long long n_rows = (long long)a.q_tokens * n_heads;
         uint32_t tiles_done = 0, results_done = 0;  // of this stream
@@ -321,7 +348,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
             const int my_tiles = max(stream_tiles(item, s), 0);
             // [token][head] index of row i of this stream's 128, -1: no such row
             const auto row_index = [&](int i) -> long long {
-                const int t = i / a.group, token = first_token + t;
+                const int t = i * a.group_inverse >> 16, token = first_token + t;
                 if (t >= a.stream_tokens || token >= item.tokens) return -1;
                 return (long long)(item.q_row + token) * n_heads + item.kv_head * a.group + (i - t * a.group);
             };
@@ -329,6 +356,26 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
             const bool there = row_token < a.stream_tokens && first_token + row_token < item.tokens;
             const int last = there ? min(item.last_key + item.key_step * (first_token + row_token), item.end_key - 1) : item.end_key - 1;
             float m = -INFINITY, l = 0.f;
+            const auto hide = [](uint32_t(&v)[32], int seen) {  // the keys that a row does not see
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+                    if (k > seen) v[k] = 0xFF800000u;
+            };
+            if (my_tiles > 0) {  // the row's first scores give it its first reference
+                wait(&s_full[s][0], tiles_done & 1);
+                tc_fence_after();
+                float top = -INFINITY;
+#pragma unroll 1
+                for (int q = 0; q < 2; ++q) {
+                    uint32_t v[32];
+                    tmem_load32(s_col + q * 32, v);
+                    tmem_wait_load(v);
+                    if (item.tile0 >= item.masked_from) hide(v, last - item.tile0 * kPromptTile - q * 32);
+#pragma unroll
+                    for (int k = 0; k < 32; k += 2) top = fmaxf(fmaxf(top, __uint_as_float(v[k])), __uint_as_float(v[k + 1]));
+                }
+                if (top != -INFINITY) m = top * c;
+            }
             for (int i = 0; i < my_tiles; ++i) {
                 const int tile = item.tile0 + i;
                 const bool masked = tile >= item.masked_from;
@@ -360,12 +407,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
 #pragma unroll
                         for (int q = 0; q < 2; ++q) {
                             uint32_t(&v)[32] = v2[q];
-                            if (masked) {
-                                const int seen = lim - h * 64 - q * 32;
-#pragma unroll
-                                for (int k = 0; k < 32; ++k)
-                                    if (k > seen) v[k] = 0xFF800000u;
-                            }
+                            if (masked) hide(v, lim - h * 64 - q * 32);
 #pragma unroll
                             for (int k = 0; k < 8; ++k) {
                                 float2x t0 = pack_f2(__uint_as_float(v[4 * k]), __uint_as_float(v[4 * k + 1]));
@@ -743,7 +785,14 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                 const long long rank = id / per_block;
                 const int rest = (int)(id - rank * per_block);
                 int seq, block;
-                order.find(rank, seq, block);
+                if (a.n_seqs == 1) {
+                    seq = 0;
+                    block = (int)(order.total - 1 - rank);  // the last block of a causal sequence is the dearest
+                } else if (ids <= gridDim.x) {
+                    order.find_any(rank, seq, block);
+                } else {
+                    order.find(rank, seq, block);
+                }
                 PromptSequence q = {0, 0, 0, 0};
                 if (seq >= 0) q = prompt_sequence(a, seq);  // (starts that descend can count more blocks than there are)
                 else block = 0;
@@ -771,6 +820,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                 mbarrier_arrive(&item_full[n % kPromptItems]);
             }
             __syncwarp();
+            if (n == 0 && blockIdx.x == 0) order.report();
             if (!item.valid) break;
         }
     }
