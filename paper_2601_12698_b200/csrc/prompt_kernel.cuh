@@ -346,11 +346,11 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         for (int n = 0; next_item(n, item); ++n) {
             const int first_token = kSplitDims ? 0 : s * a.stream_tokens;
             const int my_tiles = max(stream_tiles(item, s), 0);
-            // [token][head] index of row i of this stream's 128, -1: no such row
-            const auto row_index = [&](int i) -> long long {
+            // Row i of this stream's 128 counted in [token][head] rows from the item's first token and head, -1: no such row.
+            const auto row_index = [&](int i) -> int {
                 const int t = i * a.group_inverse >> 16, token = first_token + t;
                 if (t >= a.stream_tokens || token >= item.tokens) return -1;
-                return (long long)(item.q_row + token) * n_heads + item.kv_head * a.group + (i - t * a.group);
+                return token * n_heads + (i - t * a.group);
             };
             // last key that this row sees; rows that are not there see all
             const bool there = row_token < a.stream_tokens && first_token + row_token < item.tokens;
@@ -499,20 +499,22 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                 done_with_item(n);
                 continue;
             }
-            const long long my_row = row_index(r);
+            const int my_row = row_index(r);
+            const long long first_row = (long long)item.q_row * n_heads + item.kv_head * a.group;
             const bool none = l == 0.f;
-            const float inv = none ? 0.f : 1.0f / l, total = none ? -INFINITY : m + log2f(l);
+            const float inv = none ? 0.f : __frcp_rn(l), total = none ? -INFINITY : m + log2f(l);
             if (my_row >= 0 && (!kSplitDims || s == 0)) {
-                if (a.parts > 1) a.part_lse[item.part * n_rows + my_row] = total;
-                else if (a.lse) a.lse[my_row] = total * 0.69314718055994531f;
+                if (a.parts > 1) a.part_lse[item.part * n_rows + first_row + my_row] = total;
+                else if (a.lse) a.lse[first_row + my_row] = total * 0.69314718055994531f;
             }
             // A thread holds a row, and rows lie apart: 128 bytes of every row at a time go through shared memory, so that eight lanes
             // write them side by side.
-            long long to_row[8];
+            int to_row[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) to_row[k] = row_index((warp & 3) * 32 + k * 4 + (lane >> 3));
             const int dim0 = kSplitDims ? s * 128 : 0;
             if (a.parts > 1) {
+                float* const part_at = a.part_out + (item.part * n_rows + first_row) * a.dim;
 #pragma unroll 1
                 for (int q = 0; q < S::kCols / 32; ++q) {
                     uint32_t o[32];
@@ -534,11 +536,12 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                     for (int k = 0; k < 8; ++k) {
                         const int row = k * 4 + (lane >> 3);
                         const float4 x = *reinterpret_cast<const float4*>(stage + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
-                        if (to_row[k] >= 0 && col < a.dim) *reinterpret_cast<float4*>(a.part_out + (item.part * n_rows + to_row[k]) * a.dim + col) = x;
+                        if (to_row[k] >= 0 && col < a.dim) *reinterpret_cast<float4*>(part_at + (size_t)(unsigned)to_row[k] * (unsigned)a.dim + col) = x;
                     }
                     __syncwarp();
                 }
             } else {
+                unsigned char* const out_at = static_cast<unsigned char*>(a.out) + first_row * a.dim * 2;
 #pragma unroll 1
                 for (int q = 0; q < S::kCols / 64; ++q) {
 #pragma unroll
@@ -565,7 +568,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                     for (int k = 0; k < 8; ++k) {
                         const int row = k * 4 + (lane >> 3);
                         const uint4 x = *reinterpret_cast<const uint4*>(stage + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
-                        if (to_row[k] >= 0 && col < a.dim) *reinterpret_cast<uint4*>(reinterpret_cast<unsigned char*>(a.out) + (to_row[k] * a.dim + col) * 2) = x;
+                        if (to_row[k] >= 0 && col < a.dim) *reinterpret_cast<uint4*>(out_at + (size_t)(unsigned)to_row[k] * (unsigned)(2 * a.dim) + 2 * col) = x;
                     }
                     __syncwarp();
                 }
@@ -782,7 +785,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
             PromptItem item;
             item.valid = 0;
             if (id < ids) {
-                const long long rank = id / per_block;
+                const long long rank = ids <= 0xFFFFFFFFLL ? (long long)((unsigned)id / (unsigned)per_block) : id / per_block;
                 const int rest = (int)(id - rank * per_block);
                 int seq, block;
                 if (a.n_seqs == 1) {
