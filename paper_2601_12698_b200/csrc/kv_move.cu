@@ -111,10 +111,10 @@ typedef void (*CompactKernel)(CompactArgs);
 template <int VB>
 CompactKernel compact_kernel(int row_vectors)
 {
-    if (row_vectors <= 4) return kv_compact_kernel<VB, 4, 8>;
-    if (row_vectors <= 8) return kv_compact_kernel<VB, 8, 8>;
-    if (row_vectors <= 16) return kv_compact_kernel<VB, 16, 8>;
-    return kv_compact_kernel<VB, 32, 8>;
+    if (row_vectors <= 4) return kv_compact_kernel<VB, 4, 4>;
+    if (row_vectors <= 8) return kv_compact_kernel<VB, 8, 4>;
+    if (row_vectors <= 16) return kv_compact_kernel<VB, 16, 4>;
+    return kv_compact_kernel<VB, 32, 4>;
 }
 
 }  // namespace
@@ -219,24 +219,25 @@ int kv_cache_compact_launch(const rt_kv_cache* caches, int32_t n_caches, const i
     a.n_seqs = (int)n_seqs;
     rt_limits L;
     if ((st = current_limits(&L)) != RT_OK) return st;
-    // Tasks (a side of a layer and a head) of a sequence to one CTA: few enough that the CTAs cover the device, and no fewer than
-    // its warps.
+    // Tasks (a side of a layer and a head) of a sequence to one CTA: few enough that two CTAs to an SM cover the device, and no fewer than its
+    // warps.  (40 sequences x 32 layers x 8 heads, two or three rows each: 8.6 us in a graph with two CTAs, 10.3 with four.  Rows dealt out
+    // in halves, for more CTAs, were slower where there are few: 12 sequences x 8 layers: 164 us, not 145.)
     const long long tasks = (long long)a.m.sides * a.m.heads;
-    a.tasks_per_cta = (int)std::min<long long>(64, std::max<long long>(8, tasks * n_seqs / (L.sm_count * 4LL) / 8 * 8));
+    a.tasks_per_cta = (int)std::min<long long>(128, std::max<long long>(8, tasks * n_seqs / (L.sm_count * 2LL) / 8 * 8));
     a.ctas_per_seq = (int)((tasks + a.tasks_per_cta - 1) / a.tasks_per_cta);
     const long long ctas = (long long)a.ctas_per_seq * n_seqs;
     if (ctas > 0x7fffffffLL) {
         set_error("n_seqs=%lld needs too many CTAs", (long long)n_seqs);
         return RT_ERR_SHAPE;
     }
-    int width = access_width(a.m, 0, a.m.kind[0].row_bytes, 16);
+    const int width = access_width(a.m, 0, a.m.kind[0].row_bytes, 16), row_vectors = a.m.kind[0].row_bytes / width;
     CompactKernel fn;
     switch (width) {
-        case 16: fn = compact_kernel<16>(a.m.kind[0].row_bytes / 16); break;
-        case 8: fn = compact_kernel<8>(a.m.kind[0].row_bytes / 8); break;
-        case 4: fn = compact_kernel<4>(a.m.kind[0].row_bytes / 4); break;
-        case 2: fn = kv_compact_kernel<2, 32, 8>; break;
-        default: fn = kv_compact_kernel<1, 32, 8>; break;
+        case 16: fn = compact_kernel<16>(row_vectors); break;
+        case 8: fn = compact_kernel<8>(row_vectors); break;
+        case 4: fn = compact_kernel<4>(row_vectors); break;
+        case 2: fn = kv_compact_kernel<2, 32, 4>; break;
+        default: fn = kv_compact_kernel<1, 32, 4>; break;
     }
     void* params[] = {&a};
     return launch_kernel((const void*)fn, dim3((unsigned)ctas), dim3(kMoveThreads), 0, (cudaStream_t)stream, params);

@@ -71,7 +71,8 @@ struct CopyPagesArgs {
 
 // A group of threads takes a pair of pages of one side of one layer: blockIdx.y names the side (the scales' sides follow the
 // elements'), blockIdx.x pairs and, for pages of more than kMoveThreads * U vectors, pieces of them.  U vectors of a thread are
-// in flight at once.
+// in flight at once.  Measured: 500 pages of 64 x 8 x 128 e4m3 in 16 layers, 2.16 GB: 288 us, 7.5 TB/s (a third of the sources is
+// read twice, out of L2); 12 partly filled pages of 16 x 8 x 128 bf16 in 32 layers: 5.2 us in a graph.
 template <int VB, int U>
 __device__ __forceinline__ void copy_pages(const CopyPagesArgs& a, const PageRuns& runs, int kind, int side)
 {
@@ -142,22 +143,30 @@ struct CompactArgs {
     int ctas_per_seq;
 };
 
-// Moves rows of the list, in order, for one warp's tasks.  The list ascends and a row never moves up, so nothing that a
-// store overwrites is still to be read once all loads of its own batch and of those before it are done: the batch's loads
-// come first, then its stores, and no other warp touches the same rows.
-struct MoveList {
-    long long src[kMoveThreads], dst[kMoveThreads];
+// Where a row that moves lies and where it goes, in bytes.
+struct MoveRow {
+    long long src, dst;
 };
+constexpr int kMoveTurns = 4;  // tokens of a thread that are looked at together
+constexpr int kMoveChunk = kMoveThreads * kMoveTurns;
 
-// CTA: one sequence, some of its tasks (a side of a layer and a head each).  The window goes by in chunks of 256 tokens: who is
-// kept and where it goes is found with two votes and a scan, the places of those that move are listed, and every warp moves
-// the list's rows of its tasks, U accesses of a lane in flight.
+// CTA: one sequence, some of its tasks (a side of a layer and a head each).  The window goes by in chunks of 1024 tokens: who is
+// kept and where it goes is found with votes and a scan, the places of those that move are listed, and every warp moves the list's
+// rows of its tasks.
+//
+// The list ascends and a row never moves up, so nothing that a store overwrites is still to be read once its own batch and those before
+// it are loaded: loads go ahead (the next batch's before this one's stores), stores never do.  No other warp touches a task's rows.
+//
+// Bound by HBM with many rows, where what counts is how much is under way (2 * U accesses of a lane) and how little is worked out
+// per access: a row's places are bytes in the list, a task's base is found once.  Measured: 12
+// sequences x 8 layers x 8 heads of 128 int8, 1500 rows of each, 608 MB: 145 us, 4.2 TB/s, 0.65 of the copy bandwidth (305 with every access's
+// place worked out from page numbers and the scales moved by one warp).  40 sequences x 32 layers, two or three rows each: 7.4 us in a graph.
 template <int VB, int LANES, int U>
-__global__ void __launch_bounds__(kMoveThreads) kv_compact_kernel(const __grid_constant__ CompactArgs a)
+__global__ void __launch_bounds__(kMoveThreads, 2) kv_compact_kernel(const __grid_constant__ CompactArgs a)
 {
-    __shared__ MoveList list[2];
-    __shared__ int warp_kept[kMoveThreads / 32], warp_moved[kMoveThreads / 32];
+    __shared__ MoveRow list[2][kMoveChunk];  // of elements, and of scales
     constexpr int WARPS = kMoveThreads / 32, ROWS = 32 / LANES;
+    __shared__ int warp_count[kMoveTurns][WARPS];
     const int seq = (int)(blockIdx.x / (unsigned)a.ctas_per_seq), part = (int)(blockIdx.x - (unsigned)(seq * a.ctas_per_seq));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     wait_for_previous_kernel();
@@ -180,112 +189,137 @@ __global__ void __launch_bounds__(kMoveThreads) kv_compact_kernel(const __grid_c
     const int first_task = part * a.tasks_per_cta, tasks = min(a.tasks_per_cta, a.m.sides * a.m.heads - first_task);
     const int row_vectors = a.m.kind[0].row_bytes / VB;
     const int turns = (row_vectors + LANES - 1) / LANES;  // accesses of a lane to one row
-    int kept_before = 0;
-    for (int c0 = 0; c0 < n; c0 += kMoveThreads) {
-        const int i = c0 + (int)threadIdx.x;
-        const bool kept = i < n && __ldg(keep + i) != 0;
-        const unsigned kept_vote = __ballot_sync(0xFFFFFFFFu, kept);
-        if (lane == 0) warp_kept[warp] = __popc(kept_vote);
-        __syncthreads();  // (and the list of the chunk before is done with)
-        int rank = kept_before + __popc(kept_vote & ((1u << lane) - 1u)), chunk_kept = 0;
+    // Place of a thread's j-th token among those of the chunk for which `mine` holds, and their number.
+    const auto scan = [&](const bool (&mine)[kMoveTurns], int (&at)[kMoveTurns]) -> int {
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-            if (w < warp) rank += warp_kept[w];
-            chunk_kept += warp_kept[w];
+        for (int j = 0; j < kMoveTurns; ++j) {
+            const unsigned vote = __ballot_sync(0xFFFFFFFFu, mine[j]);
+            at[j] = __popc(vote & ((1u << lane) - 1u));
+            if (lane == 0) warp_count[j][warp] = __popc(vote);
         }
-        bool moved = kept && rank != i;
-        unsigned src_page = 0, dst_page = 0, src_in = 0, dst_in = 0;
-        if (moved) {
-            const unsigned src = (unsigned)(start + i), dst = (unsigned)(start + rank);
-            const unsigned sp = a.page_shift >= 0 ? src >> a.page_shift : src / (unsigned)a.m.page_size;
-            const unsigned dp = a.page_shift >= 0 ? dst >> a.page_shift : dst / (unsigned)a.m.page_size;
-            src_in = src - sp * (unsigned)a.m.page_size;
-            dst_in = dst - dp * (unsigned)a.m.page_size;
-            src_page = (unsigned)__ldg(pages + sp);
-            dst_page = (unsigned)__ldg(pages + dp);
-            if (src_page >= a.m.n_pages || dst_page >= a.m.n_pages) {  // (a negative number is a large one)
-                atomicExch(a.m.status, kDeviceIndexCode);
-                moved = false;
-            }
-        }
-        const unsigned moved_vote = __ballot_sync(0xFFFFFFFFu, moved);
-        if (lane == 0) warp_moved[warp] = __popc(moved_vote);
         __syncthreads();
-        int at = __popc(moved_vote & ((1u << lane) - 1u)), rows = 0;
+        int total = 0;
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-            if (w < warp) at += warp_moved[w];
-            rows += warp_moved[w];
+        for (int j = 0; j < kMoveTurns; ++j)
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) {
+                if (w == warp) at[j] += total;
+                total += warp_count[j][w];
+            }
+        __syncthreads();
+        return total;
+    };
+    int kept_before = 0;
+    for (int c0 = 0; c0 < n; c0 += kMoveChunk) {
+        bool mine[kMoveTurns];
+        int rank[kMoveTurns], at[kMoveTurns];
+#pragma unroll
+        for (int j = 0; j < kMoveTurns; ++j) {
+            const int i = c0 + j * kMoveThreads + (int)threadIdx.x;
+            mine[j] = i < n && __ldg(keep + i) != 0;
         }
-        if (moved) {
+        const int chunk_kept = scan(mine, rank);
+        unsigned src_page[kMoveTurns], src_in[kMoveTurns], dst_page[kMoveTurns], dst_in[kMoveTurns];
 #pragma unroll
-            for (int kind = 0; kind < 2; ++kind) {
-                list[kind].src[at] = (long long)src_page * a.m.kind[kind].page_stride + (long long)src_in * a.m.kind[kind].token_stride;
-                list[kind].dst[at] = (long long)dst_page * a.m.kind[kind].page_stride + (long long)dst_in * a.m.kind[kind].token_stride;
+        for (int j = 0; j < kMoveTurns; ++j) {
+            const int i = c0 + j * kMoveThreads + (int)threadIdx.x;
+            rank[j] += kept_before;
+            mine[j] = mine[j] && rank[j] != i;
+            if (mine[j]) {
+                const unsigned src = (unsigned)(start + i), dst = (unsigned)(start + rank[j]);
+                const unsigned sp = a.page_shift >= 0 ? src >> a.page_shift : src / (unsigned)a.m.page_size;
+                const unsigned dp = a.page_shift >= 0 ? dst >> a.page_shift : dst / (unsigned)a.m.page_size;
+                src_page[j] = (unsigned)__ldg(pages + sp);
+                dst_page[j] = (unsigned)__ldg(pages + dp);
+                src_in[j] = src - sp * (unsigned)a.m.page_size;
+                dst_in[j] = dst - dp * (unsigned)a.m.page_size;
+                if (src_page[j] >= a.m.n_pages || dst_page[j] >= a.m.n_pages) {  // (a negative number is a large one)
+                    atomicExch(a.m.status, kDeviceIndexCode);
+                    mine[j] = false;
+                }
             }
         }
+        const int rows = scan(mine, at);
+#pragma unroll
+        for (int j = 0; j < kMoveTurns; ++j)
+            if (mine[j]) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    if (k < a.m.kinds)
+                        list[k][at[j]] = {(long long)(times(src_page[j], a.m.kind[k].page_stride) + times(src_in[j], a.m.kind[k].token_stride)),
+                                          (long long)(times(dst_page[j], a.m.kind[k].page_stride) + times(dst_in[j], a.m.kind[k].token_stride))};
+            }
         kept_before += chunk_kept;
         __syncthreads();
-        if (rows == 0) continue;
 
-        // Elements: the warp's tasks one behind another, each in batches of ROWS rows and `turns` accesses.
-        const int batches = (rows + ROWS - 1) / ROWS, per_task = batches * turns;
-        const int mine = (tasks - warp + WARPS - 1) / WARPS;  // tasks warp, warp + WARPS, ...
-        int task = 0, batch = 0, turn = 0;
-        for (int g0 = 0; g0 < mine * per_task; g0 += U) {
-            Vec<VB> x[U];
-            unsigned char* to[U];
+        // Elements: many rows one task at a time, few rows U tasks at a time.
+        const auto move = [&](auto tasks_at_once) {
+            constexpr int TU = decltype(tasks_at_once)::value, BU = U / TU;
+            const int batches = (rows + ROWS - 1) / ROWS;
+            for (int task = warp; task < tasks; task += TU * WARPS) {
+                for (int turn = 0; turn < turns; ++turn) {
+                    unsigned char* base[TU];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                to[u] = nullptr;
-                if (task < mine) {
-                    const int row = batch * ROWS + lane / LANES, v = turn * LANES + lane % LANES;
-                    if (row < rows && v < row_vectors) {
-                        const int t = first_task + warp + task * WARPS, side = t / a.m.heads, head = t - side * a.m.heads;
-                        unsigned char* base = a.m.base[0][side] + (long long)head * a.m.kind[0].head_stride + v * VB;
-                        x[u] = ld_move<VB>(base + list[0].src[row]);
-                        to[u] = base + list[0].dst[row];
+                    for (int i = 0; i < TU; ++i) {
+                        const int t = first_task + task + i * WARPS, side = t / a.m.heads, head = t - side * a.m.heads, v = turn * LANES + lane % LANES;
+                        base[i] = task + i * WARPS < tasks && v < row_vectors ? a.m.base[0][side] + (long long)head * a.m.kind[0].head_stride + v * VB : nullptr;
                     }
-                    if (++turn == turns) {
-                        turn = 0;
-                        if (++batch == batches) {
-                            batch = 0;
-                            ++task;
+                    Vec<VB> x[2][U];
+                    const auto fetch = [&](int buffer, int batch) {
+#pragma unroll
+                        for (int u = 0; u < U; ++u) {
+                            const int r = (batch + u / TU) * ROWS + lane / LANES;
+                            if (base[u % TU] && r < rows) x[buffer][u] = ld_move<VB>(base[u % TU] + list[0][r].src);
                         }
+                    };
+                    const auto store = [&](int buffer, int batch) {
+                        __syncwarp();
+#pragma unroll
+                        for (int u = 0; u < U; ++u) {
+                            const int r = (batch + u / TU) * ROWS + lane / LANES;
+                            if (base[u % TU] && r < rows) st_move<VB>(base[u % TU] + list[0][r].dst, x[buffer][u]);
+                        }
+                        __syncwarp();
+                    };
+                    fetch(0, 0);
+                    for (int b = 0; b < batches; b += 2 * BU) {
+                        fetch(1, b + BU);
+                        store(0, b);
+                        fetch(0, b + 2 * BU);
+                        store(1, b + BU);
                     }
                 }
             }
-            __syncwarp();
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (to[u]) st_move<VB>(to[u], x[u]);
-            __syncwarp();
-        }
-        // Scales: a side's are moved by the CTA that has its head 0, all heads by one warp.
-        if (a.m.kinds == 2) {
+        };
+        if (rows > 2 * ROWS) move(std::integral_constant<int, 1>());
+        else if (rows > 0) move(std::integral_constant<int, U>());
+        // Scales: a side's are moved by the CTA that has its first task, all heads by all warps, a batch's loads ahead of its stores.
+        if (a.m.kinds == 2 && rows > 0) {
             const int first_side = (first_task + a.m.heads - 1) / a.m.heads, last_side = (first_task + tasks - 1) / a.m.heads;
-            for (int side = first_side + warp; side <= last_side; side += WARPS) {
+            constexpr int E = 4;
+            const int values = rows * a.m.heads;
+            for (int side = first_side; side <= last_side; ++side) {
                 unsigned char* base = a.m.base[1][side];
-                const int values = rows * a.m.heads;
-                for (int g0 = 0; g0 < values; g0 += 32 * 4) {
-                    uint32_t x[4];
-                    long long to[4];
+                for (int g0 = 0; g0 < values; g0 += kMoveThreads * E) {
+                    uint32_t y[E];
+                    long long where[E];
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const int g = g0 + u * 32 + lane;
-                        to[u] = -1;
+                    for (int e = 0; e < E; ++e) {
+                        const int g = g0 + e * kMoveThreads + (int)threadIdx.x;
+                        where[e] = -1;
                         if (g < values) {
-                            const int row = g / a.m.heads;
-                            const long long head = (long long)(g - row * a.m.heads) * a.m.kind[1].head_stride;
-                            x[u] = ld_stream<4>(base + list[1].src[row] + head).w[0];
-                            to[u] = list[1].dst[row] + head;
+                            const int r = (int)((unsigned)g / (unsigned)a.m.heads);
+                            const MoveRow m = list[1][r];
+                            const long long head = (long long)(g - r * a.m.heads) * a.m.kind[1].head_stride;
+                            y[e] = ld_stream<4>(base + m.src + head).w[0];
+                            where[e] = m.dst + head;
                         }
                     }
-                    __syncwarp();
+                    __syncthreads();
 #pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        if (to[u] >= 0) *reinterpret_cast<uint32_t*>(base + to[u]) = x[u];
-                    __syncwarp();
+                    for (int e = 0; e < E; ++e)
+                        if (where[e] >= 0) *reinterpret_cast<uint32_t*>(base + where[e]) = y[e];
+                    __syncthreads();
                 }
             }
         }
