@@ -514,19 +514,24 @@ typedef struct {
     float magnitude;
 } rt_rotary;
 
+/* The queries or the keys of one call: in and out [n_tokens, heads, head_dim], device, the last axis contiguous, outer strides in
+ * elements.  out may be in with the same strides; otherwise the tensors of a call must not overlap. */
+typedef struct {
+    const void* in;
+    void* out;
+    int64_t in_token_stride, in_head_stride, out_token_stride, out_head_stride;
+    int64_t heads; /* 0: there are none, and the pointers are ignored */
+} rt_rotary_side;
+
 /*
  * Turns the pairs of every head of every token by its position's angles:  y1 = m (x1 cos - x2 sin), y2 = m (x2 cos + x1 sin),
  * in binary32, rounded once to `dtype`; elements from rot_dim on are copied.
  *   positions  device, int64 [n_tokens]; negative = a padded token, whose rows of out are left as they were.
- *   q, k       device, [n_tokens, q_heads or k_heads, head_dim] of `dtype`, the last axis contiguous, outer strides in elements; q_out
- *              and k_out likewise.  Either side may have no heads (its pointers are then ignored).  q_out may be q with the same
- *              strides, and k_out k; otherwise the tensors must not overlap.
+ *   sides      host, two of them (queries and keys), tensors of `dtype`.
  * Asynchronous on `stream`, allocates nothing.  n_tokens == 0 is a successful no-op.
  */
-int rotary_launch(const rt_rotary* rotary, const int64_t* positions, int64_t n_tokens, int32_t head_dim, const void* q,
-                  int64_t q_token_stride, int64_t q_head_stride, void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride,
-                  int32_t q_heads, const void* k, int64_t k_token_stride, int64_t k_head_stride, void* k_out,
-                  int64_t k_out_token_stride, int64_t k_out_head_stride, int32_t k_heads, int dtype, void* stream);
+int rotary_launch(const rt_rotary* rotary, const int64_t* positions, int64_t n_tokens, int32_t head_dim, const rt_rotary_side* sides, int dtype,
+                  void* stream);
 
 /* Sequences packed behind one another: sequence b has the query rows q_starts[b] .. q_starts[b + 1] - 1 and the key rows
  * k_starts[b] .. k_starts[b + 1] - 1.  More keys than queries: the queries are the sequence's last tokens. */

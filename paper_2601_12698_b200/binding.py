@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_uint64, c_void_p
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -136,6 +137,11 @@ class rt_rotary(Structure):
     _fields_ = [("turns", c_void_p), ("rot_dim", c_int32), ("interleaved", c_int32), ("backward", c_int32), ("magnitude", c_float)]
 
 
+class rt_rotary_side(Structure):
+    _fields_ = [("in_", c_void_p), ("out", c_void_p), ("in_token_stride", c_int64), ("in_head_stride", c_int64),
+                ("out_token_stride", c_int64), ("out_head_stride", c_int64), ("heads", c_int64)]
+
+
 class rt_prompt_batch(Structure):
     _fields_ = [("q_starts", c_void_p), ("k_starts", c_void_p), ("n_seqs", c_int64), ("q_tokens", c_int64), ("k_tokens", c_int64),
                 ("max_q_len", c_int64), ("max_k_len", c_int64), ("causal", c_int32), ("reserved", c_int32)]
@@ -162,8 +168,7 @@ _SIGNATURES = {
                                                c_int32, c_void_p, c_void_p, c_float, c_int, c_void_p, c_int64, c_void_p]),
     "shared_prefix_attention_workspace_bytes": (c_int64, [POINTER(rt_kv_cache), POINTER(rt_prefix_batch), c_int32]),
     "rotary_frequencies": (c_int, [POINTER(rt_rotary_spec), POINTER(c_uint64), POINTER(c_float)]),
-    "rotary_launch": (c_int, [POINTER(rt_rotary), c_void_p, c_int64, c_int32, c_void_p, c_int64, c_int64, c_void_p, c_int64, c_int64, c_int32,
-                              c_void_p, c_int64, c_int64, c_void_p, c_int64, c_int64, c_int32, c_int, c_void_p]),
+    "rotary_launch": (c_int, [POINTER(rt_rotary), c_void_p, c_int64, c_int32, c_void_p, c_int, c_void_p]),
     "prompt_attention_launch": (c_int, [POINTER(rt_prompt_batch), c_void_p, c_int64, c_int64, c_int32, c_void_p, c_int64, c_int64, c_void_p,
                                         c_int64, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_float, c_int, c_void_p, c_int64, c_void_p]),
     "prompt_attention_workspace_bytes": (c_int64, [POINTER(rt_prompt_batch), c_int32, c_int32, c_int32]),
@@ -643,34 +648,38 @@ def _refuse_rotary(positions, x, out, index: int):
                      "head_dim on the table's device, the last axis contiguous")
 
 
+_pack_sides = struct.Struct("=14q").pack  # two rt_rotary_side
+
+
 def rotary_launch(table: RotaryTable, positions, q, k=None, q_out=None, k_out=None, backward: bool = False, stream=None) -> None:
     """Turn the heads of q [n_tokens, q_heads, head_dim] and k [n_tokens, k_heads, head_dim] (or of q alone) by the positions
     (int64 [n_tokens]; negative = a padded token, whose rows are left as they were) into q_out and k_out, by default in place.
     `backward` is the gradient: the opposite angle.  Asynchronous."""
     index = table.device_index
-    if q_out is None:
-        q_out = q
-    shape, qs, os, dtype = q.shape, q.stride(), q_out.stride(), q.dtype
+    shape, (q0, q1, q2), dtype = q.shape, q.stride() if q.dim() == 3 else (0, 0, 0), q.dtype
     code = _TORCH_CODES.get(dtype)
-    if not (len(shape) == 3 and code is not None and q_out.shape == shape and q_out.dtype is dtype and (qs[2] == os[2] == 1 or shape[2] == 1)
-            and positions.dtype is _torch.int64 and positions.shape == shape[:1] and positions.is_contiguous()
-            and (0 not in os or 1 in shape or 0 in shape) and q.get_device() == q_out.get_device() == positions.get_device() == index):
+    if q_out is None or q_out is q:
+        q_out, (o0, o1, o2) = q, (q0, q1, q2)
+    else:
+        (o0, o1, o2) = q_out.stride() if q_out.shape == shape and q_out.dtype is dtype and q_out.get_device() == index and len(shape) == 3 else (0, 0, 0)
+    if not (len(shape) == 3 and code is not None and positions.dtype is _torch.int64 and positions.shape == shape[:1] and q2 == o2 == 1
+            and positions.is_contiguous() and q.get_device() == positions.get_device() == index):
         _refuse_rotary(positions, q, q_out, index)
     if k is None:
         if k_out is not None:
             raise ValueError("rotary_launch: k_out without k")
-        side = (None, 0, 0, None, 0, 0, 0)
+        sides = _pack_sides(q.data_ptr(), q_out.data_ptr(), q0, q1, o0, o1, shape[1], 0, 0, 0, 0, 0, 0, 0)
     else:
-        if k_out is None:
-            k_out = k
-        k_shape, ks, kos = k.shape, k.stride(), k_out.stride()
-        if not (len(k_shape) == 3 and k_shape[0] == shape[0] and k_shape[2] == shape[2] and k.dtype is dtype and k_out.shape == k_shape
-                and k_out.dtype is dtype and (ks[2] == kos[2] == 1 or k_shape[2] == 1) and (0 not in kos or 1 in k_shape or 0 in k_shape)
-                and k.get_device() == k_out.get_device() == index):
+        k_shape, (k0, k1, k2) = k.shape, k.stride() if k.dim() == 3 else (0, 0, 0)
+        if k_out is None or k_out is k:
+            k_out, (p0, p1, p2) = k, (k0, k1, k2)
+        else:
+            (p0, p1, p2) = k_out.stride() if k_out.shape == k_shape and k_out.dtype is dtype and k_out.get_device() == index and len(k_shape) == 3 else (0, 0, 0)
+        if not (k.dtype is dtype and len(k_shape) == 3 and k_shape[0] == shape[0] and k_shape[2] == shape[2] and k2 == p2 == 1 and k.get_device() == index):
             _refuse_rotary(positions, k, k_out, index)
-        side = (k.data_ptr(), ks[0], ks[1], k_out.data_ptr(), kos[0], kos[1], k_shape[1])
-    status = _call_on(index, lib.rotary_launch, table._refs[1 if backward else 0], positions.data_ptr(), shape[0], shape[2], q.data_ptr(), qs[0],
-                      qs[1], q_out.data_ptr(), os[0], os[1], shape[1], *side, code, _stream_of(index, stream))
+        sides = _pack_sides(q.data_ptr(), q_out.data_ptr(), q0, q1, o0, o1, shape[1], k.data_ptr(), k_out.data_ptr(), k0, k1, p0, p1, k_shape[1])
+    status = _call_on(index, lib.rotary_launch, table._refs[1 if backward else 0], positions.data_ptr(), shape[0], shape[2], sides, code,
+                      _stream_of(index, stream))
     if status:
         raise TunerError(status, "rotary_launch")
 
@@ -695,14 +704,19 @@ class PromptBatch:
         self.max_q_len = int(max_q_len)
         self.max_k_len = self.max_q_len if max_k_len is None else int(max_k_len)
         self._fixed = (self.q_starts.data_ptr(), self.k_starts.data_ptr(), self.n_seqs)
+        self._last = (None, None)
 
     def _struct(self, q_tokens: int, k_tokens: int):
-        return rt_prompt_batch(*self._fixed, q_tokens, k_tokens, self.max_q_len, self.max_k_len, self.causal, 0)
+        """The struct of a call with tensors of these sizes: the last call's, where it had the same."""
+        last = self._last
+        if last[0] != (q_tokens, k_tokens):
+            last = self._last = ((q_tokens, k_tokens), byref(rt_prompt_batch(*self._fixed, q_tokens, k_tokens, self.max_q_len, self.max_k_len, self.causal, 0)))
+        return last[1]
 
 
 def prompt_attention_workspace_bytes(batch: PromptBatch, q, k) -> int:
     """Bytes of workspace of a call with queries like q and keys like k."""
-    n = _call_on(batch.device_index, lib.prompt_attention_workspace_bytes, byref(batch._struct(q.shape[0], k.shape[0])), q.shape[1], k.shape[1], q.shape[2])
+    n = _call_on(batch.device_index, lib.prompt_attention_workspace_bytes, batch._struct(q.shape[0], k.shape[0]), q.shape[1], k.shape[1], q.shape[2])
     if n < 0:
         raise ValueError(f"prompt_attention: {lib.rt_last_error().decode()}")
     return int(n)
@@ -744,7 +758,7 @@ def prompt_attention_launch(batch: PromptBatch, q, k, v, out, lse=None, workspac
                 workspace = prompt_attention_workspace(batch, q, k)
     elif workspace.get_device() != index or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on q's device")
-    status = _call_on(index, lib.prompt_attention_launch, byref(batch._struct(shape[0], k_shape[0])), q.data_ptr(), qs[0], qs[1], shape[1],
+    status = _call_on(index, lib.prompt_attention_launch, batch._struct(shape[0], k_shape[0]), q.data_ptr(), qs[0], qs[1], shape[1],
                       k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], k_shape[1], shape[2], out.data_ptr(), lse_ptr,
                       shape[2] ** -0.5 if softmax_scale is None else softmax_scale, _TORCH_CODES[dtype], workspace.data_ptr(), workspace.nbytes, handle)
     if status:

@@ -1,4 +1,5 @@
 // Entry points of the moves inside a paged cache: argument checks, launch rules and the kernels' instances.
+#include <stddef.h>
 #include <string.h>
 
 #include "kv_move_kernels.cuh"
@@ -32,11 +33,10 @@ int gather_caches(const rt_kv_cache* caches, int n, MoveArgs* m)
         const rt_kv_cache& x = caches[i];
         const int st = check_cache(&x, true);
         if (st != RT_OK) return st;
-        if (x.n_pages != c.n_pages || x.page_size != c.page_size || x.kv_heads != c.kv_heads || x.head_dim != c.head_dim || x.format != c.format ||
-            (!quantised && x.dtype != c.dtype) || x.page_stride != c.page_stride || x.token_stride != c.token_stride ||
-            x.head_stride != c.head_stride ||
-            (quantised && (x.scale_page_stride != c.scale_page_stride || x.scale_token_stride != c.scale_token_stride ||
-                           x.scale_head_stride != c.scale_head_stride))) {
+        // (shape, format and the elements' strides lie side by side, so do the scales' strides)
+        if (memcmp(&x.n_pages, &c.n_pages, offsetof(rt_kv_cache, dtype) - offsetof(rt_kv_cache, n_pages)) || (!quantised && x.dtype != c.dtype) ||
+            memcmp(&x.page_stride, &c.page_stride, 3 * sizeof(int64_t)) ||
+            (quantised && memcmp(&x.scale_page_stride, &c.scale_page_stride, 3 * sizeof(int64_t)))) {
             set_error("cache %d is not like the first", i);
             return RT_ERR_SHAPE;
         }

@@ -122,14 +122,12 @@ int rotary_frequencies(const rt_rotary_spec* s, uint64_t* turns, float* magnitud
     return RT_OK;
 }
 
-int rotary_launch(const rt_rotary* r, const int64_t* positions, int64_t n_tokens, int32_t head_dim, const void* q, int64_t q_token_stride,
-                  int64_t q_head_stride, void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride, int32_t q_heads, const void* k,
-                  int64_t k_token_stride, int64_t k_head_stride, void* k_out, int64_t k_out_token_stride, int64_t k_out_head_stride,
-                  int32_t k_heads, int dtype, void* stream)
+int rotary_launch(const rt_rotary* r, const int64_t* positions, int64_t n_tokens, int32_t head_dim, const rt_rotary_side* sides, int dtype,
+                  void* stream)
 {
     using namespace rt;
-    if (!r) {
-        set_error("rotary is NULL");
+    if (!r || !sides) {
+        set_error("rotary or sides is NULL");
         return RT_ERR_NULL;
     }
     if (dtype < RT_BF16 || dtype > RT_FP32) {
@@ -140,13 +138,6 @@ int rotary_launch(const rt_rotary* r, const int64_t* positions, int64_t n_tokens
         set_error("n_tokens=%lld head_dim=%d rot_dim=%d out of range", (long long)n_tokens, (int)head_dim, (int)r->rot_dim);
         return RT_ERR_SHAPE;
     }
-    const struct {
-        const void* in;
-        void* out;
-        int64_t in_token_stride, in_head_stride, out_token_stride, out_head_stride;
-        int32_t heads;
-    } sides[2] = {{q, q_out, q_token_stride, q_head_stride, q_out_token_stride, q_out_head_stride, q_heads},
-                  {k, k_out, k_token_stride, k_head_stride, k_out_token_stride, k_out_head_stride, k_heads}};
     const int64_t size = elem_bytes_of(dtype);
     RotaryArgs a;
     memset(&a, 0, sizeof(a));
@@ -156,11 +147,11 @@ int rotary_launch(const rt_rotary* r, const int64_t* positions, int64_t n_tokens
     uintptr_t places = 0;
     bool copies = false;
     for (int i = 0; i < 2; ++i) {
-        const auto* s = &sides[i];
+        const rt_rotary_side* s = &sides[i];
         if (s->heads == 0) continue;
         if (s->heads < 0 || s->heads > 65535 || s->in_token_stride < 0 || s->in_head_stride < 0 || s->out_token_stride < 0 || s->out_head_stride < 0 ||
             (n_tokens > 1 && s->out_token_stride == 0) || (s->heads > 1 && s->out_head_stride == 0)) {
-            set_error("heads=%d or a stride out of range", (int)s->heads);
+            set_error("heads=%lld or a stride out of range", (long long)s->heads);
             return RT_ERR_SHAPE;
         }
         if (n_tokens == 0) continue;
@@ -179,7 +170,7 @@ int rotary_launch(const rt_rotary* r, const int64_t* positions, int64_t n_tokens
         d.in_head = s->in_head_stride * size;
         d.out_token = s->out_token_stride * size;
         d.out_head = s->out_head_stride * size;
-        d.heads = s->heads;
+        d.heads = (int)s->heads;
         const bool same = s->in == s->out && (n_tokens == 1 || d.in_token == d.out_token) && (d.heads == 1 || d.in_head == d.out_head);
         if (s->in == s->out && !same) {
             set_error("in and out overlap with different strides");

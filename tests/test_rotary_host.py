@@ -75,7 +75,8 @@ def test_frequency_refusals(change):
 
 def _call(rotary=None, tokens=5, dim=128, q=(P, 512, 128, P, 512, 128, 4), k=(P, 256, 128, P, 256, 128, 2), dtype=0, positions=P):
     r = B.rt_rotary(P, 128, 0, 0, 1.0) if rotary is None else rotary
-    return B.lib.rotary_launch(ctypes.byref(r), positions, tokens, dim, *q, *k, dtype, None)
+    sides = (B.rt_rotary_side * 2)(*[B.rt_rotary_side(s[0], s[3], s[1], s[2], *s[4:]) for s in (q, k)])
+    return B.lib.rotary_launch(ctypes.byref(r), positions, tokens, dim, ctypes.cast(sides, ctypes.c_void_p), dtype, None)
 
 
 @pytest.mark.parametrize("kw,status", [
@@ -95,6 +96,8 @@ def test_nothing_to_do_is_no_error():
     none = (None, 0, 0, None, 0, 0, 0)
     assert _call(q=none, k=none) == B.RT_OK
     assert _call(tokens=0, positions=None) == B.RT_OK
+    assert B.lib.rotary_launch(None, P, 5, 128, P, 0, None) == B.RT_ERR_NULL
+    assert B.lib.rotary_launch(ctypes.byref(B.rt_rotary(P, 128, 0, 0, 1.0)), P, 5, 128, None, 0, None) == B.RT_ERR_NULL
     with pytest.raises(ValueError):
         B.RotaryTable(64, scaling="other", device="cpu")
     with pytest.raises(B.TunerError):
