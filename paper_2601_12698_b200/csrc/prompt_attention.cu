@@ -215,6 +215,8 @@ int prompt_attention_launch(const rt_prompt_batch* b, const void* q, int64_t q_t
         a.part_out = (float*)workspace;
         a.part_lse = a.part_out + (int64_t)p.parts * b->q_tokens * q_heads * head_dim;
     }
+    // (binary32 parts of heads that are multiples of 8 are)
+    a.wide_rows = p.parts > 1 ? (uintptr_t)workspace % 32 == 0 : head_dim % 16 == 0 && (uintptr_t)out % 32 == 0;
     a.status = device_status_word();
     if (!a.status) return RT_ERR_NO_DEVICE;
     a.wait_polls = wait_poll_limit();

@@ -40,6 +40,7 @@ namespace rt {
 constexpr int kPromptThreads = 512;
 constexpr int kPromptTile = 128;  // keys of a tile, rows of a stream
 constexpr int kPromptItems = 4;   // ring of items
+constexpr int kPromptLanded = 8;  // masked tiles whose values can be under way: more than the ring holds
 constexpr int kPromptMaxParts = 32;
 
 struct PromptArgs {
@@ -60,6 +61,7 @@ struct PromptArgs {
     float* lse;       // [token][head] or NULL
     float* part_out;  // parts > 1: [part][token][head][dim], normalised
     float* part_lse;  // [part][token][head], base 2
+    int wide_rows;    // rows of out, or of part_out, are multiples of 32 bytes
     int* status;
     unsigned wait_polls;
     int drop_copies;
@@ -80,15 +82,19 @@ struct PromptItem {
 
 template <int DP>
 struct PromptShape {
-    static constexpr int kHalves = DP == 256 ? 2 : 1;      // column halves of a tile of keys or values, a ring slot each
-    static constexpr int kCols = DP == 256 ? 128 : DP;     // columns of a slot, and dims of a stream's output
-    static constexpr int kSlotBytes = kPromptTile * kCols * 2;
-    static constexpr int kSlots = DP == 64 ? 8 : 4;
-    static constexpr int kQueryBytes = kPromptTile * DP * 2;  // of one stream
+    static constexpr int kBlocks = DP / 64;               // column blocks of a tile of queries, keys or values
+    static constexpr int kCols = DP == 256 ? 128 : DP;    // dims of a stream's output
+    static constexpr int kBlockBytes = kPromptTile * 128;
+    // The ring: 160 KB, a block to a slot, or both of heads of 128.  (Heads of 128, 8192 tokens: 435 us with two, 445 with one; heads of 256, 256
+    // tokens behind 8000: 102 us with one, as they are asked for and freed one after the other, 115 with two; 128 KB: 110.)
+    static constexpr int kSlotBlocks = DP == 128 ? 2 : 1;
+    static constexpr int kUnits = kBlocks / kSlotBlocks;  // slots of a tile
+    static constexpr int kSlotBytes = kSlotBlocks * kBlockBytes;
+    static constexpr int kSlots = 10 / kSlotBlocks;
+    static constexpr int kQueryBytes = kBlocks * kBlockBytes;  // of one stream
     static constexpr int kQueries = DP == 256 ? 1 : 2;
     static constexpr size_t kRingAt = (size_t)kQueries * kQueryBytes;
-    static constexpr size_t kStageAt = kRingAt + (size_t)kSlots * kSlotBytes;  // 4 KB per softmax warp, where results wait to be written row by row
-    static constexpr size_t kSmem = kStageAt + 8 * 4096 + 1024;                // 1024: alignment of the tiles
+    static constexpr size_t kSmem = kRingAt + (size_t)kSlots * kSlotBytes + 1024;  // 1024: alignment of the tiles
     static constexpr int kSoftmaxRegs = 160;  // of 2 * 128 for a softmax thread and one of another role
 };
 
@@ -96,6 +102,22 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, i
 {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
                  "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z) : "memory");
+}
+
+// 32 bytes of a row, of `columns` columns from `col` on, in one access or, where places are multiples of 16 bytes only, in two.
+template <int WORDS>
+__device__ __forceinline__ void store_row(unsigned char* to, const uint32_t* x, int col, int columns, const PromptArgs& a)
+{
+    if (a.wide_rows) {
+        Vec<32> v;
+#pragma unroll
+        for (int k = 0; k < WORDS; ++k) v.w[k] = x[k];
+        if (col < a.dim) st_stream<32>(to, v);
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (col + h * columns / 2 < a.dim) *reinterpret_cast<uint4*>(to + h * 16) = make_uint4(x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]);
+    }
 }
 
 // A sequence as the items see it: its rows cut to the tensors, its number of blocks and what its first block costs.
@@ -256,41 +278,43 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
 {
     using S = PromptShape<DP>;
     constexpr bool kSplitDims = DP == 256;
-    constexpr int kBlockBytes = kTileBlockBytes;  // one 64-dim column block of a tile
+    constexpr int kBlocks = S::kBlocks, kSlotBlocks = S::kSlotBlocks, kUnits = S::kUnits;
     constexpr uint32_t kScoreIdesc = tc_instruction<T>(kPromptTile / 2, false, false);
     constexpr uint32_t kColO = 2 * kPromptTile;
 
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     unsigned char* ring = smem + S::kRingAt;
-    __shared__ __align__(8) uint64_t full[S::kSlots], empty[S::kSlots], item_full[kPromptItems], item_free[kPromptItems], landed[4], q_full, q_free, s_full[2][2],
+    __shared__ __align__(8) uint64_t full[S::kSlots], empty[S::kSlots], item_full[kPromptItems], item_free[kPromptItems], landed[kPromptLanded], q_full, q_free, s_full[2][2],
         p_full[2][2], o_done[2], o_full[2], drained[2];
     __shared__ PromptItem items[kPromptItems];
     __shared__ uint32_t tmem_base;
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
-    if (tid == 0) {
-        for (int i = 0; i < S::kSlots; ++i) {
-            mbarrier_init(&full[i], 1);
-            mbarrier_init(&empty[i], 2);
-        }
-        for (int i = 0; i < kPromptItems; ++i) {
-            mbarrier_init(&item_full[i], 1);
-            mbarrier_init(&item_free[i], 15);  // warps that read it: 8 softmax, 4 looking, 2 issuing, 1 fetching
-            mbarrier_init(&landed[i], 1);
-            items[i].valid = 0;
-        }
-        for (int i = 0; i < 2; ++i) {
-            mbarrier_init(&s_full[i][0], 1);
-            mbarrier_init(&s_full[i][1], 1);
-            mbarrier_init(&p_full[i][0], 128);
-            mbarrier_init(&p_full[i][1], 128);
-            mbarrier_init(&o_done[i], 1);
-            mbarrier_init(&o_full[i], 1);
-            mbarrier_init(&drained[i], 1);
-        }
+    if (tid < S::kSlots) {
+        mbarrier_init(&full[tid], 1);
+        mbarrier_init(&empty[tid], 2);
+    } else if (tid >= 32 && tid < 32 + kPromptItems) {
+        mbarrier_init(&item_full[tid - 32], 1);
+        mbarrier_init(&item_free[tid - 32], 15);  // warps that read it: 8 softmax, 4 looking, 2 issuing, 1 fetching
+        items[tid - 32].valid = 0;
+    } else if (tid >= 64 && tid < 66) {
+        const int i = tid - 64;
+        mbarrier_init(&s_full[i][0], 1);
+        mbarrier_init(&s_full[i][1], 1);
+        mbarrier_init(&p_full[i][0], 128);
+        mbarrier_init(&p_full[i][1], 128);
+        mbarrier_init(&o_done[i], 1);
+        mbarrier_init(&o_full[i], 1);
+        mbarrier_init(&drained[i], 1);
+    } else if (tid >= 96 && tid < 96 + kPromptLanded) {
+        mbarrier_init(&landed[tid - 96], 1);
+    } else if (tid == 127) {
         mbarrier_init(&q_full, 1);
         mbarrier_init(&q_free, 2);
+    } else if (tid >= 128 && tid < 131) {
+        const CUtensorMap* map = tid == 128 ? &q_map : tid == 129 ? &k_map : &v_map;
+        asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
     }
     if (warp == 12) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_base)) : "memory");
@@ -339,7 +363,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         const float c = fmaxf(a.score_scale, 1.17549435e-38f);  // (a scale of zero would make NaN of hidden scores: the smallest normal number does instead)
         const float2x c2 = pack_f2(c, c);
         const int row_token = r * a.group_inverse >> 16;
-        unsigned char* stage = smem + S::kStageAt + warp * 4096;
         const long long n_rows = (long long)a.q_tokens * n_heads;
         uint32_t tiles_done = 0, results_done = 0;  // of this stream
         PromptItem item;
@@ -507,70 +530,35 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                 if (a.parts > 1) a.part_lse[item.part * n_rows + first_row + my_row] = total;
                 else if (a.lse) a.lse[first_row + my_row] = total * 0.69314718055994531f;
             }
-            // A thread holds a row, and rows lie apart: 128 bytes of every row at a time go through shared memory, so that eight lanes
-            // write them side by side.
-            int to_row[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) to_row[k] = row_index((warp & 3) * 32 + k * 4 + (lane >> 3));
-            const int dim0 = kSplitDims ? s * 128 : 0;
-            if (a.parts > 1) {
-                float* const part_at = a.part_out + (item.part * n_rows + first_row) * a.dim;
+            // A thread holds a row, and rows lie apart; 32 bytes at a time are whole sectors all the same.  (Results that went through shared
+            // memory, so that eight lanes wrote 128 bytes of a row side by side, took twice as long to leave, 1.6 us.)
+            const int dim0 = kSplitDims ? s * 128 : 0, elem = a.parts > 1 ? 4 : 2;
+            unsigned char* const to = (a.parts > 1 ? reinterpret_cast<unsigned char*>(a.part_out) + item.part * n_rows * a.dim * 4 : static_cast<unsigned char*>(a.out)) +
+                                      (first_row + max(my_row, 0)) * a.dim * elem;
 #pragma unroll 1
-                for (int q = 0; q < S::kCols / 32; ++q) {
-                    uint32_t o[32];
+            for (int q = 0; q < S::kCols; q += 32) {
+                uint32_t o[32];
+                if (my_tiles > 0) {
+                    tmem_load32(o_col + q, o);
+                    tmem_wait_load(o);
+                } else {
 #pragma unroll
                     for (int k = 0; k < 32; ++k) o[k] = 0;
-                    if (my_tiles > 0) {
-                        tmem_load32(o_col + q * 32, o);
-                        tmem_wait_load(o);
-                    }
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        float4 x = make_float4(__uint_as_float(o[4 * k]) * inv, __uint_as_float(o[4 * k + 1]) * inv, __uint_as_float(o[4 * k + 2]) * inv, __uint_as_float(o[4 * k + 3]) * inv);
-                        if (none) x = make_float4(0.f, 0.f, 0.f, 0.f);
-                        *reinterpret_cast<float4*>(stage + lane * 128 + ((k ^ (lane & 7)) << 4)) = x;
-                    }
-                    __syncwarp();
-                    const int col = dim0 + q * 32 + (lane & 7) * 4;
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const int row = k * 4 + (lane >> 3);
-                        const float4 x = *reinterpret_cast<const float4*>(stage + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
-                        if (to_row[k] >= 0 && col < a.dim) *reinterpret_cast<float4*>(part_at + (size_t)(unsigned)to_row[k] * (unsigned)a.dim + col) = x;
-                    }
-                    __syncwarp();
                 }
-            } else {
-                unsigned char* const out_at = static_cast<unsigned char*>(a.out) + first_row * a.dim * 2;
-#pragma unroll 1
-                for (int q = 0; q < S::kCols / 64; ++q) {
+                if (my_row < 0) continue;  // (the loads are the whole warp's)
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        uint32_t o[32];
+                for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * inv);
+                if (a.parts > 1) {
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) o[k] = 0;
-                        if (my_tiles > 0) {
-                            tmem_load32(o_col + q * 64 + half * 32, o);
-                            tmem_wait_load(o);
-                        }
+                    for (int k = 0; k < 32; k += 8)
+                        store_row<8>(to + (dim0 + q + k) * 4, o + k, dim0 + q + k, 8, a);
+                } else {
+                    uint32_t y[16];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            uint32_t y[4];
+                    for (int k = 0; k < 16; ++k) y[k] = pack2<T>(__uint_as_float(o[2 * k]), __uint_as_float(o[2 * k + 1]));
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                y[j] = none ? 0u : pack2<T>(__uint_as_float(o[8 * k + 2 * j]) * inv, __uint_as_float(o[8 * k + 2 * j + 1]) * inv);
-                            *reinterpret_cast<uint4*>(stage + lane * 128 + (((half * 4 + k) ^ (lane & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
-                        }
-                    }
-                    __syncwarp();
-                    const int col = dim0 + q * 64 + (lane & 7) * 8;
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const int row = k * 4 + (lane >> 3);
-                        const uint4 x = *reinterpret_cast<const uint4*>(stage + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
-                        if (to_row[k] >= 0 && col < a.dim) *reinterpret_cast<uint4*>(out_at + (size_t)(unsigned)to_row[k] * (unsigned)(2 * a.dim) + 2 * col) = x;
-                    }
-                    __syncwarp();
+                    for (int k = 0; k < 16; k += 8)
+                        store_row<8>(to + (dim0 + q + 2 * k) * 2, y + k, dim0 + q + 2 * k, 16, a);
                 }
             }
             tc_fence_before();  // the output's columns have been read before the next item's weights are announced
@@ -589,24 +577,22 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         for (int n = 0; next_item(n, item); ++n) {
             for (int tile = max(item.tile0, item.masked_from); tile < item.tile1; ++tile) {
                 bool found = false;
-                wait(&landed[looked_at % 4], (looked_at / 4) & 1);
+                wait(&landed[looked_at % kPromptLanded], (looked_at / kPromptLanded) & 1);
                 ++looked_at;
+                const uint32_t unit = (2 * (tiles_before + tile - item.tile0) + 1) * kUnits;
+                if (tile * kPromptTile + p > item.last_key) {
+#pragma unroll 1
+                    for (int b = 0; b < kBlocks; ++b) {
+                        unsigned char* row = ring + (unit + b / kSlotBlocks) % S::kSlots * S::kSlotBytes + b % kSlotBlocks * S::kBlockBytes + p * 128;
 #pragma unroll
-                for (int half = 0; half < S::kHalves; ++half) {
-                    const uint32_t unit = (tiles_before + tile - item.tile0) * 2 * S::kHalves + S::kHalves + half, slot = unit % S::kSlots;
-                    if (tile * kPromptTile + p > item.last_key) {
-#pragma unroll
-                        for (int b = 0; b < S::kCols / 64; ++b) {
-#pragma unroll
-                            for (int u = 0; u < 8; ++u) {
-                                uint4* at = reinterpret_cast<uint4*>(ring + slot * S::kSlotBytes + b * kBlockBytes + p * 128 + ((u ^ (p & 7)) << 4));
-                                uint4 x = *at;
-                                const uint4 bad = make_uint4(__vcmpeq2(x.x & kExponent, kExponent), __vcmpeq2(x.y & kExponent, kExponent),
-                                                             __vcmpeq2(x.z & kExponent, kExponent), __vcmpeq2(x.w & kExponent, kExponent));
-                                if (bad.x | bad.y | bad.z | bad.w) {
-                                    *at = make_uint4(x.x & ~bad.x, x.y & ~bad.y, x.z & ~bad.z, x.w & ~bad.w);
-                                    found = true;
-                                }
+                        for (int u = 0; u < 8; ++u) {
+                            uint4* at = reinterpret_cast<uint4*>(row + ((u ^ (p & 7)) << 4));
+                            const uint4 x = *at;
+                            const uint4 bad = make_uint4(__vcmpeq2(x.x & kExponent, kExponent), __vcmpeq2(x.y & kExponent, kExponent),
+                                                         __vcmpeq2(x.z & kExponent, kExponent), __vcmpeq2(x.w & kExponent, kExponent));
+                            if (bad.x | bad.y | bad.z | bad.w) {
+                                *at = make_uint4(x.x & ~bad.x, x.y & ~bad.y, x.z & ~bad.z, x.w & ~bad.w);
+                                found = true;
                             }
                         }
                     }
@@ -614,7 +600,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                 if (found && tile * kPromptTile + p < item.end_key) *reinterpret_cast<volatile int*>(&items[n % kPromptItems].bad_values) = 1;
                 fence_async_proxy();
                 asm volatile("barrier.cta.sync 1, 128;" ::: "memory");
-                if (p < S::kHalves) mbarrier_arrive(&full[((tiles_before + tile - item.tile0) * 2 * S::kHalves + S::kHalves + p) % S::kSlots]);
+                if (p < kUnits) mbarrier_arrive(&full[(unit + p) % S::kSlots]);
             }
             tiles_before += item.tile1 - item.tile0;
             done_with_item(n);
@@ -622,8 +608,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
     } else if (warp >= 12 && warp < 14) {
         // ---- warps that issue the products of the two streams ----
         const int s = warp - 12;
-        constexpr uint64_t kRowsLayout = tc_layout(16, 1024), kColsLayout = tc_layout(kBlockBytes, 1024);
-        constexpr uint32_t kSlot16 = S::kSlotBytes / 16, kBlock = kBlockBytes / 16;
+        constexpr uint64_t kRowsLayout = tc_layout(16, 1024), kColsLayout = tc_layout(S::kBlockBytes, 1024);
+        constexpr uint32_t kSlot16 = S::kSlotBytes / 16, kBlock16 = S::kBlockBytes / 16;
+        constexpr int kValueUnits = S::kCols / 64 / kSlotBlocks;  // of the values, those of this stream's dims
         const uint32_t q16 = smem_u32(smem) >> 4, ring16 = smem_u32(ring) >> 4;
         const uint64_t q_at = tc_descriptor(kRowsLayout, q16 + (kSplitDims ? 0 : s) * (S::kQueryBytes / 16));
         const uint64_t k_base = tc_descriptor(kRowsLayout, ring16), v_base = tc_descriptor(kColsLayout, ring16);
@@ -632,7 +619,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         const int out_dims = max(16, min((a.dim - (kSplitDims ? s * 128 : 0) + 15) / 16 * 16, S::kCols));
         const uint32_t out_idesc = tc_instruction<T>(out_dims, false, true);
         uint32_t tiles_before = 0, my_tiles_before = 0, items_before = 0;
-        auto unit_of = [&](uint32_t tile, int which) { return tile * 2 * S::kHalves + which; };
         auto wait_unit = [&](uint32_t unit) {
             wait(&full[unit % S::kSlots], (unit / S::kSlots) & 1);
             tc_fence_after();
@@ -649,48 +635,43 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                 wait(&q_full, items_before & 1);
                 tc_fence_after();
             }
-            // Half h of S = Q K^T with the item's tile number i
+            // Half h of S = Q K^T with the item's tile number i; its blocks are waited for, and freed, one after the other
             auto scores = [&](int i, int h) {
-                const uint32_t unit = unit_of(tiles_before + i, 0);
-                if (h == 0) {
+                const uint32_t unit = 2 * (tiles_before + i) * kUnits;
 #pragma unroll
-                    for (int half = 0; half < S::kHalves; ++half) wait_unit(unit + half);
-                }
-                if (elect_one()) {
+                for (int b = 0; b < kBlocks; ++b) {
+                    const uint32_t slot = (unit + b / kSlotBlocks) % S::kSlots;
+                    if (h == 0 && b % kSlotBlocks == 0) wait_unit(unit + b / kSlotBlocks);
+                    if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < DP / 16; ++k) {
-                        const uint32_t slot = (unit + k / 8) % S::kSlots;  // (heads of 256: dims from 128 on are in the second half's slot)
-                        if (k < steps)
-                            tc_mma_ss(d_scores + h * 64, q_at + ((k >> 2) * kBlock + (k & 3) * 2),
-                                      k_base + (slot * kSlot16 + ((k >> 2) & 1) * kBlock + (k & 3) * 2 + h * (64 * 128 / 16)), kScoreIdesc, k > 0);
+                        for (int k = 0; k < 4; ++k)
+                            if (b * 4 + k < steps)
+                                tc_mma_ss(d_scores + h * 64, q_at + (b * kBlock16 + k * 2), k_base + (slot * kSlot16 + b % kSlotBlocks * kBlock16 + k * 2 + h * (64 * 128 / 16)),
+                                          kScoreIdesc, b + k > 0);
+                        if (h == 1 && (b + 1) % kSlotBlocks == 0) tc_commit(&empty[slot]);
+                        if (b == kBlocks - 1) {
+                            tc_commit(&s_full[s][h]);
+                            if (h == 1 && i + 1 == mine) tc_commit(&q_free);
+                        }
                     }
-                    tc_commit(&s_full[s][h]);
-                    if (h == 1) {
-#pragma unroll
-                        for (int half = 0; half < S::kHalves; ++half) tc_commit(&empty[(unit + half) % S::kSlots]);
-                        if (i + 1 == mine) tc_commit(&q_free);
-                    }
+                    __syncwarp();
                 }
-                __syncwarp();
             };
             if (mine > 0) {
                 scores(0, 0);
                 scores(0, 1);
             } else if (tiles > 0 && lane == 0) mbarrier_arrive(&q_free);
             for (int i = 0; i < tiles; ++i) {
-                const uint32_t unit = unit_of(tiles_before + i, S::kHalves);
+                const uint32_t unit = (2 * (tiles_before + i) + 1) * kUnits;  // the values'
                 if (i >= mine) {
-#pragma unroll
-                    for (int half = 0; half < S::kHalves; ++half) skip_unit(unit - S::kHalves + half);
-#pragma unroll
-                    for (int half = 0; half < S::kHalves; ++half) {
-                        skip_unit(unit + half);
-                    }
+#pragma unroll 1
+                    for (int b = 0; b < 2 * kUnits; ++b) skip_unit(unit - kUnits + b);
                     continue;
                 }
                 // O += W V.  Heads of 256: this stream's half of the dims; the other half is the other stream's.
-                const uint32_t my_unit = unit + (kSplitDims ? s : 0), slot = my_unit % S::kSlots;
-                wait_unit(my_unit);
+                const uint32_t my_unit = unit + (kSplitDims ? s * kValueUnits : 0), slot = my_unit % S::kSlots;  // (of two slots the even one: they lie side by side)
+#pragma unroll
+                for (int b = 0; b < kValueUnits; ++b) wait_unit(my_unit + b);
                 const uint64_t v_at = v_base + slot * kSlot16;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -702,8 +683,11 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                             tc_mma_ts(d_out, d_scores + h * 64 + k * 8, v_at + (h * 64 * 128 / 16 + k * 128), out_idesc, i + h + k > 0);
                         tc_commit(&o_done[s]);
                         if (h == 1) {
-                            tc_commit(&empty[slot]);
-                            if (kSplitDims) tc_commit(&empty[slot]);  // (the only stream that reads it)
+#pragma unroll
+                            for (int b = 0; b < kValueUnits; ++b) {
+                                tc_commit(&empty[slot + b]);
+                                if (kSplitDims) tc_commit(&empty[slot + b]);  // (the only stream that reads it)
+                            }
                             if (i + 1 == mine) tc_commit(&o_full[s]);
                         }
                     }
@@ -724,20 +708,23 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         // ---- the warp that fetches ----
         uint32_t units = 0, items_before = 0, looks = 0;
         bool posted = false;
-        const uint32_t query_bytes = (uint32_t)(a.stream_tokens * a.group) * 128u * (DP / 64);
-        // One half of a tile; `bar` is told of its bytes, and first of how many to expect (0: it knows).
-        auto fetch = [&](const CUtensorMap* map, int col0, const PromptItem& item, int tile, uint64_t* bar, uint32_t expected) {
-            const uint32_t slot = units % S::kSlots;
-            wait(&empty[slot], ((units / S::kSlots) & 1) ^ 1);
-            if (!a.drop_copies && elect_one()) {
-                if (!bar) bar = &full[slot];
-                if (expected) mbarrier_expect_tx(bar, expected);
+        const uint32_t query_bytes = (uint32_t)(a.stream_tokens * a.group) * 128u * kBlocks;
+        // A tile of keys or values from row `row` on; `bar`, where there is one, is told of all its bytes, otherwise each slot of its own.
+        auto fetch = [&](const CUtensorMap* map, int head, int row, uint64_t* bar) {
 #pragma unroll
-                for (int b = 0; b < S::kCols / 64; ++b)
-                    tma_load_3d(ring + slot * S::kSlotBytes + b * kBlockBytes, map, col0 + b * 64, item.kv_head, item.k_row + tile * kPromptTile, bar);
+            for (int u = 0; u < kUnits; ++u) {
+                const uint32_t slot = units % S::kSlots;
+                wait(&empty[slot], ((units / S::kSlots) & 1) ^ 1);
+                if (!a.drop_copies && elect_one()) {
+                    if (!bar) mbarrier_expect_tx(&full[slot], S::kSlotBytes);
+                    else if (u == 0) mbarrier_expect_tx(bar, S::kSlotBytes * kUnits);
+#pragma unroll
+                    for (int b = 0; b < kSlotBlocks; ++b)
+                        tma_load_3d(ring + slot * S::kSlotBytes + b * S::kBlockBytes, map, (u * kSlotBlocks + b) * 64, head, row, bar ? bar : &full[slot]);
+                }
+                __syncwarp();
+                ++units;
             }
-            __syncwarp();
-            ++units;
         };
         PromptItem item;
         for (int n = 0; next_item(n, item); ++n) {
@@ -749,28 +736,26 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
 #pragma unroll
                     for (int s = 0; s < S::kQueries; ++s)
 #pragma unroll
-                        for (int b = 0; b < DP / 64; ++b)
-                            tma_load_3d(smem + s * S::kQueryBytes + b * kBlockBytes, &q_map, b * 64, item.kv_head * a.group, item.q_row + s * a.stream_tokens, &q_full);
+                        for (int b = 0; b < kBlocks; ++b)
+                            tma_load_3d(smem + s * S::kQueryBytes + b * S::kBlockBytes, &q_map, b * 64, item.kv_head * a.group, item.q_row + s * a.stream_tokens, &q_full);
                 }
                 __syncwarp();
                 posted = !a.drop_copies;
                 ++items_before;
             }
             for (int i = 0; i < tiles; ++i) {
-#pragma unroll
-                for (int half = 0; half < S::kHalves; ++half) fetch(&k_map, half * 128, item, item.tile0 + i, nullptr, S::kSlotBytes);
+                const int row = item.k_row + (item.tile0 + i) * kPromptTile;
+                fetch(&k_map, item.kv_head, row, nullptr);
                 const bool masked = item.tile0 + i >= item.masked_from;  // then those who look through the values tell the others
-#pragma unroll
-                for (int half = 0; half < S::kHalves; ++half)
-                    fetch(&v_map, half * 128, item, item.tile0 + i, masked ? &landed[looks % 4] : nullptr,
-                          masked ? (half == 0 ? S::kSlotBytes * S::kHalves : 0) : S::kSlotBytes);
+                fetch(&v_map, item.kv_head, row, masked ? &landed[looks % kPromptLanded] : nullptr);
                 if (masked) ++looks;
             }
             done_with_item(n);
         }
         // no copy is under way when the CTA ends
         if (posted) {
-            for (uint32_t m = looks > 4 ? looks - 4 : 0; m < looks; ++m) ok = mbarrier_wait_sleeping(&landed[m % 4], (m / 4) & 1) && ok;
+            for (uint32_t m = looks > kPromptLanded ? looks - kPromptLanded : 0; m < looks; ++m)
+                ok = mbarrier_wait_sleeping(&landed[m % kPromptLanded], (m / kPromptLanded) & 1) && ok;
             ok = mbarrier_wait_sleeping(&q_full, (items_before - 1) & 1) && ok;
             for (uint32_t u = units > S::kSlots ? units - S::kSlots : 0; u < units; ++u) ok = mbarrier_wait_sleeping(&full[u % S::kSlots], (u / S::kSlots) & 1) && ok;
         }
