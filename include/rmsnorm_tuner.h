@@ -588,22 +588,29 @@ int64_t prompt_attention_workspace_bytes(const rt_prompt_batch* batch, int32_t q
 int kv_cache_copy_pages_launch(const rt_kv_cache* caches, int32_t n_caches, const int32_t* src, const int32_t* dst,
                                const int32_t* tokens, int64_t n_pages, void* stream);
 
+/* Sequences whose tokens are given up in part. */
+typedef struct {
+    const int32_t* page_table; /* device, [n_seqs, page_table_width], row stride page_table_stride: the pages of each sequence from its
+                                  first token on.  Pages that hold any of the tokens from starts[b] on must belong to it alone */
+    const int32_t* starts;     /* device, [n_seqs]: tokens before this one stay where they are */
+    const int32_t* lens;       /* device, [n_seqs]; negative = a padded sequence */
+    const unsigned char* keep; /* device, bytes [n_seqs, window], row stride keep_stride: token starts[b] + i stays if keep[b, i] is not 0 */
+    int32_t* new_lens;         /* device, [n_seqs], overlapping none of the inputs */
+    int64_t n_seqs;            /* 0 .. 2^24 */
+    int64_t window;            /* 0 .. 2^30 */
+    int64_t page_table_stride, page_table_width, keep_stride; /* elements */
+} rt_compact_batch;
+
 /*
- * Closes the gaps that given-up tokens leave: of the tokens starts[b] .. lens[b] - 1 of sequence b those whose keep[b, i] is not 0
- * (token starts[b] + i) move, in every cache, to the positions starts[b], starts[b] + 1, ... in their order;
+ * Closes the gaps that given-up tokens leave: of the tokens starts[b] .. lens[b] - 1 of sequence b those that stay move, in every one of
+ * the n_caches caches (as above), to the positions starts[b], starts[b] + 1, ... in their order, scales included;
  * new_lens[b] = starts[b] + their number.  In place; what lies behind the new length is not defined.
- *   page_table      device, int32 [n_seqs, page_table_width], row stride page_table_stride: the pages of each sequence from its
- *                   first token on.  Pages that hold any of the tokens from starts[b] on must belong to the sequence alone.
- *   starts, lens, new_lens  device, int32 [n_seqs]; new_lens must overlap none of the inputs.
- *   keep            device, bytes [n_seqs, window], row stride keep_stride.
- * lens[b] < 0 is a padded sequence: new_lens[b] = lens[b].  A sequence with starts[b] outside 0 .. lens[b], more than `window` tokens
- * behind it or more than its table row has pages for, or a page number outside the cache is reported as RT_ERR_INDEX: of the latter only that
- * token is not moved, the others are left as they are with new_lens[b] = lens[b].
+ * A padded sequence: new_lens[b] = lens[b].  A sequence with starts[b] outside 0 .. lens[b], more than `window` tokens behind it or more
+ * tokens than its table row has pages for is left as it is with new_lens[b] = lens[b], a token whose old or new page is not in the cache is
+ * not moved; both are reported as RT_ERR_INDEX in the device status word.
  * Asynchronous on `stream`, allocates nothing.  n_seqs == 0 is a successful no-op.
  */
-int kv_cache_compact_launch(const rt_kv_cache* caches, int32_t n_caches, const int32_t* page_table, int64_t page_table_stride,
-                            int32_t page_table_width, const int32_t* starts, const int32_t* lens, const unsigned char* keep,
-                            int64_t keep_stride, int64_t window, int32_t* new_lens, int64_t n_seqs, void* stream);
+int kv_cache_compact_launch(const rt_kv_cache* caches, int32_t n_caches, const rt_compact_batch* batch, void* stream);
 
 /* ---- 2. the feasible region ----------------------------------------------------- */
 

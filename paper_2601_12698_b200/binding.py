@@ -147,6 +147,11 @@ class rt_prompt_batch(Structure):
                 ("max_q_len", c_int64), ("max_k_len", c_int64), ("causal", c_int32), ("reserved", c_int32)]
 
 
+class rt_compact_batch(Structure):
+    _fields_ = [("page_table", c_void_p), ("starts", c_void_p), ("lens", c_void_p), ("keep", c_void_p), ("new_lens", c_void_p), ("n_seqs", c_int64),
+                ("window", c_int64), ("page_table_stride", c_int64), ("page_table_width", c_int64), ("keep_stride", c_int64)]
+
+
 SOURCE_NAMES = {0: "table_exact", 1: "table_nearest", 2: "general", 3: "feasible_set"}
 
 rt_evaluate_fn = ctypes.CFUNCTYPE(c_double, POINTER(rt_params), c_void_p)
@@ -173,8 +178,7 @@ _SIGNATURES = {
                                         c_int64, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_float, c_int, c_void_p, c_int64, c_void_p]),
     "prompt_attention_workspace_bytes": (c_int64, [POINTER(rt_prompt_batch), c_int32, c_int32, c_int32]),
     "kv_cache_copy_pages_launch": (c_int, [POINTER(rt_kv_cache), c_int32, c_void_p, c_void_p, c_void_p, c_int64, c_void_p]),
-    "kv_cache_compact_launch": (c_int, [POINTER(rt_kv_cache), c_int32, c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_void_p, c_int64, c_int64,
-                                        c_void_p, c_int64, c_void_p]),
+    "kv_cache_compact_launch": (c_int, [POINTER(rt_kv_cache), c_int32, c_void_p, c_void_p]),
     "rt_kernel_instance_parts": (c_int32, [c_int32]),
     "rt_set_option": (c_int, [c_int32, c_int32]),
     "rt_get_option": (c_int32, [c_int32]),
@@ -642,8 +646,6 @@ class RotaryTable:
 def _refuse_rotary(positions, x, out, index: int):
     if positions.dim() != 1 or positions.dtype != _torch.int64 or not positions.is_contiguous() or positions.get_device() != index:
         raise ValueError("rotary_launch: positions must be a contiguous int64 [n_tokens] tensor on the table's device")
-    if x.dim() == 3 and out.shape == x.shape and out.dtype is x.dtype and x.dtype in _TORCH_CODES and x.get_device() == out.get_device() == index:
-        _no_overlap(out, "rotary_launch: out")
     raise ValueError("rotary_launch: q, k and their outputs must be [n_tokens, heads, head_dim] tensors of one dtype (bf16, fp16, fp32) and "
                      "head_dim on the table's device, the last axis contiguous")
 
@@ -655,30 +657,42 @@ def rotary_launch(table: RotaryTable, positions, q, k=None, q_out=None, k_out=No
     """Turn the heads of q [n_tokens, q_heads, head_dim] and k [n_tokens, k_heads, head_dim] (or of q alone) by the positions
     (int64 [n_tokens]; negative = a padded token, whose rows are left as they were) into q_out and k_out, by default in place.
     `backward` is the gradient: the opposite angle.  Asynchronous."""
-    index = table.device_index
-    shape, (q0, q1, q2), dtype = q.shape, q.stride() if q.dim() == 3 else (0, 0, 0), q.dtype
+    index, dtype, shape = table.device_index, q.dtype, q.shape
     code = _TORCH_CODES.get(dtype)
-    if q_out is None or q_out is q:
-        q_out, (o0, o1, o2) = q, (q0, q1, q2)
-    else:
-        (o0, o1, o2) = q_out.stride() if q_out.shape == shape and q_out.dtype is dtype and q_out.get_device() == index and len(shape) == 3 else (0, 0, 0)
-    if not (len(shape) == 3 and code is not None and positions.dtype is _torch.int64 and positions.shape == shape[:1] and q2 == o2 == 1
-            and positions.is_contiguous() and q.get_device() == positions.get_device() == index):
+    try:
+        n, heads, dim = shape
+        q0, q1, q2 = q.stride()
+        if q_out is None or q_out is q:
+            q_out, o0, o1 = q, q0, q1
+        else:
+            o0, o1, o2 = q_out.stride()
+            if not (o2 == 1 and q_out.dtype is dtype and q_out.shape == shape and q_out.get_device() == index):
+                raise ValueError
+        if not (q2 == 1 and code is not None and positions.dtype is _torch.int64 and positions.shape == (n,) and positions.is_contiguous()
+                and q.get_device() == positions.get_device() == index):
+            raise ValueError
+    except ValueError:
         _refuse_rotary(positions, q, q_out, index)
     if k is None:
         if k_out is not None:
             raise ValueError("rotary_launch: k_out without k")
-        sides = _pack_sides(q.data_ptr(), q_out.data_ptr(), q0, q1, o0, o1, shape[1], 0, 0, 0, 0, 0, 0, 0)
+        sides = _pack_sides(q.data_ptr(), q_out.data_ptr(), q0, q1, o0, o1, heads, 0, 0, 0, 0, 0, 0, 0)
     else:
-        k_shape, (k0, k1, k2) = k.shape, k.stride() if k.dim() == 3 else (0, 0, 0)
-        if k_out is None or k_out is k:
-            k_out, (p0, p1, p2) = k, (k0, k1, k2)
-        else:
-            (p0, p1, p2) = k_out.stride() if k_out.shape == k_shape and k_out.dtype is dtype and k_out.get_device() == index and len(k_shape) == 3 else (0, 0, 0)
-        if not (k.dtype is dtype and len(k_shape) == 3 and k_shape[0] == shape[0] and k_shape[2] == shape[2] and k2 == p2 == 1 and k.get_device() == index):
+        try:
+            k_n, k_heads, k_dim = k_shape = k.shape
+            k0, k1, k2 = k.stride()
+            if k_out is None or k_out is k:
+                k_out, p0, p1 = k, k0, k1
+            else:
+                p0, p1, p2 = k_out.stride()
+                if not (p2 == 1 and k_out.dtype is dtype and k_out.shape == k_shape and k_out.get_device() == index):
+                    raise ValueError
+            if not (k2 == 1 and k.dtype is dtype and k_n == n and k_dim == dim and k.get_device() == index):
+                raise ValueError
+        except ValueError:
             _refuse_rotary(positions, k, k_out, index)
-        sides = _pack_sides(q.data_ptr(), q_out.data_ptr(), q0, q1, o0, o1, shape[1], k.data_ptr(), k_out.data_ptr(), k0, k1, p0, p1, k_shape[1])
-    status = _call_on(index, lib.rotary_launch, table._refs[1 if backward else 0], positions.data_ptr(), shape[0], shape[2], sides, code,
+        sides = _pack_sides(q.data_ptr(), q_out.data_ptr(), q0, q1, o0, o1, heads, k.data_ptr(), k_out.data_ptr(), k0, k1, p0, p1, k_heads)
+    status = _call_on(index, lib.rotary_launch, table._refs[1 if backward else 0], positions.data_ptr(), n, dim, sides, code,
                       _stream_of(index, stream))
     if status:
         raise TunerError(status, "rotary_launch")
@@ -778,25 +792,25 @@ class KvCacheStack:
             if c.device_index != first.device_index or any(getattr(c.struct, n) != getattr(first.struct, n) for n in alike):
                 raise ValueError("the caches of a stack must have one device, shape, format and strides")
         self.device_index = first.device_index
-        self._array = (rt_kv_cache * len(self.caches))(*[c.struct for c in self.caches])
-
-
-def _page_list(t, shape, index: int, name: str):
-    if t.shape != shape or t.dtype is not _torch.int32 or not t.is_contiguous() or t.get_device() != index:
-        raise ValueError(f"{name} must be a contiguous int32 {list(shape)} tensor on the caches' device")
+        self._array, self._count = (rt_kv_cache * len(self.caches))(*[c.struct for c in self.caches]), len(self.caches)
 
 
 def kv_cache_copy_pages_launch(stack: KvCacheStack, src, dst, tokens=None, stream=None) -> None:
     """In every cache of the stack, copy page src[i] to page dst[i] (int32 [n]; negative = skipped), or only its first tokens[i]
     entries.  A destination must be neither a source nor another destination of the call.  Asynchronous."""
-    index = stack.device_index
-    for t, name in ((src, "src"), (dst, "dst"), (tokens, "tokens")):
-        if t is not None or name != "tokens":
-            _page_list(t, src.shape[:1] if len(src.shape) == 1 else (0,), index, name)
-    status = _call_on(index, lib.kv_cache_copy_pages_launch, stack._array, len(stack.caches), src.data_ptr(), dst.data_ptr(),
-                      None if tokens is None else tokens.data_ptr(), src.shape[0], _stream_of(index, stream))
+    index, int32, shape = stack.device_index, _torch.int32, src.shape
+    if not (len(shape) == 1 and dst.shape == shape and src.dtype is dst.dtype is int32 and src.is_contiguous() and dst.is_contiguous()
+            and src.get_device() == dst.get_device() == index):
+        raise ValueError("src and dst must be contiguous int32 [n] tensors on the caches' device")
+    if tokens is not None and not (tokens.shape == shape and tokens.dtype is int32 and tokens.is_contiguous() and tokens.get_device() == index):
+        raise ValueError("tokens must be a contiguous int32 [n] tensor on the caches' device")
+    status = _call_on(index, lib.kv_cache_copy_pages_launch, stack._array, stack._count, src.data_ptr(), dst.data_ptr(),
+                      None if tokens is None else tokens.data_ptr(), shape[0], _stream_of(index, stream))
     if status:
         raise TunerError(status, "kv_cache_copy_pages_launch")
+
+
+_pack_compact = struct.Struct("=10q").pack  # an rt_compact_batch
 
 
 def kv_cache_compact_launch(stack: KvCacheStack, page_table, starts, lens, keep, new_lens, stream=None) -> None:
@@ -804,18 +818,20 @@ def kv_cache_compact_launch(stack: KvCacheStack, page_table, starts, lens, keep,
     with keep[b, i] (bool or uint8 [n_seqs, window]; token starts[b] + i) move to starts[b], starts[b] + 1, ...; new_lens[b] is the new
     length.  page_table: int32 [n_seqs, width], the sequence's pages from its first token on.  lens[b] < 0: a padded sequence.
     Asynchronous."""
-    index, n = stack.device_index, starts.shape[0] if starts.dim() == 1 else -1
-    for t, name in ((starts, "starts"), (lens, "lens"), (new_lens, "new_lens")):
-        _page_list(t, (n,), index, name)
-    if (page_table.dim() != 2 or page_table.dtype is not _torch.int32 or page_table.shape[0] != n or page_table.get_device() != index
-            or (page_table.shape[1] > 1 and page_table.stride(1) != 1)):
+    index, int32, shape = stack.device_index, _torch.int32, starts.shape
+    table_shape, keep_shape = page_table.shape, keep.shape
+    if not (len(shape) == 1 and lens.shape == new_lens.shape == shape and starts.dtype is lens.dtype is new_lens.dtype is int32 and starts.is_contiguous()
+            and lens.is_contiguous() and new_lens.is_contiguous() and starts.get_device() == lens.get_device() == new_lens.get_device() == index):
+        raise ValueError("starts, lens and new_lens must be contiguous int32 [n_seqs] tensors on the caches' device")
+    n, (table_stride, table_step), (keep_stride, keep_step) = shape[0], page_table.stride() if len(table_shape) == 2 else (0, 0), keep.stride() if len(keep_shape) == 2 else (0, 0)
+    if len(table_shape) != 2 or page_table.dtype is not int32 or table_shape[0] != n or page_table.get_device() != index or (table_step != 1 and table_shape[1] > 1):
         raise ValueError("page_table must be an int32 [n_seqs, width] tensor on the caches' device, rows contiguous")
-    if (keep.dim() != 2 or keep.dtype not in (_torch.bool, _torch.uint8) or keep.shape[0] != n or keep.get_device() != index
-            or (keep.shape[1] > 1 and keep.stride(1) != 1)):
+    if (len(keep_shape) != 2 or (keep.dtype is not _torch.bool and keep.dtype is not _torch.uint8) or keep_shape[0] != n or keep.get_device() != index
+            or (keep_step != 1 and keep_shape[1] > 1)):
         raise ValueError("keep must be a bool or uint8 [n_seqs, window] tensor on the caches' device, rows contiguous")
-    status = _call_on(index, lib.kv_cache_compact_launch, stack._array, len(stack.caches), page_table.data_ptr(), page_table.stride(0),
-                      page_table.shape[1], starts.data_ptr(), lens.data_ptr(), keep.data_ptr(), keep.stride(0), keep.shape[1], new_lens.data_ptr(),
-                      n, _stream_of(index, stream))
+    batch = _pack_compact(page_table.data_ptr(), starts.data_ptr(), lens.data_ptr(), keep.data_ptr(), new_lens.data_ptr(), n, keep_shape[1], table_stride,
+                          table_shape[1], keep_stride)
+    status = _call_on(index, lib.kv_cache_compact_launch, stack._array, stack._count, batch, _stream_of(index, stream))
     if status:
         raise TunerError(status, "kv_cache_compact_launch")
 

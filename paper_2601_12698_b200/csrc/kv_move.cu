@@ -178,45 +178,49 @@ int kv_cache_copy_pages_launch(const rt_kv_cache* caches, int32_t n_caches, cons
     return launch_kernel((const void*)fn, dim3((unsigned)ctas, (unsigned)(a.m.sides * a.m.kinds)), dim3(kMoveThreads), 0, (cudaStream_t)stream, params);
 }
 
-int kv_cache_compact_launch(const rt_kv_cache* caches, int32_t n_caches, const int32_t* page_table, int64_t page_table_stride,
-                            int32_t page_table_width, const int32_t* starts, const int32_t* lens, const unsigned char* keep, int64_t keep_stride,
-                            int64_t window, int32_t* new_lens, int64_t n_seqs, void* stream)
+int kv_cache_compact_launch(const rt_kv_cache* caches, int32_t n_caches, const rt_compact_batch* b, void* stream)
 {
     using namespace rt;
     CompactArgs a;
     memset(&a, 0, sizeof(a));
+    if (!b) {
+        set_error("batch is NULL");
+        return RT_ERR_NULL;
+    }
     int st = gather_caches(caches, n_caches, &a.m);
     if (st != RT_OK) return st;
-    if (n_seqs < 0 || n_seqs > (1LL << 24) || window < 0 || window > (1LL << 30) || page_table_width < 0 || page_table_stride < 0 || keep_stride < 0) {
-        set_error("n_seqs=%lld window=%lld or a width or stride out of range", (long long)n_seqs, (long long)window);
+    if (b->n_seqs < 0 || b->n_seqs > (1LL << 24) || b->window < 0 || b->window > (1LL << 30) || b->page_table_width < 0 ||
+        b->page_table_width > 0x7fffffffLL || b->page_table_stride < 0 || b->keep_stride < 0) {
+        set_error("n_seqs=%lld window=%lld or a width or stride out of range", (long long)b->n_seqs, (long long)b->window);
         return RT_ERR_SHAPE;
     }
-    if (n_seqs == 0) return RT_OK;
-    if (!starts || !lens || !new_lens || (page_table_width > 0 && !page_table) || (window > 0 && !keep)) {
+    if (b->n_seqs == 0) return RT_OK;
+    if (!b->starts || !b->lens || !b->new_lens || (b->page_table_width > 0 && !b->page_table) || (b->window > 0 && !b->keep)) {
         set_error("a tensor pointer is NULL");
         return RT_ERR_NULL;
     }
-    if (((uintptr_t)page_table | (uintptr_t)starts | (uintptr_t)lens | (uintptr_t)new_lens) & 3u) {
+    if (((uintptr_t)b->page_table | (uintptr_t)b->starts | (uintptr_t)b->lens | (uintptr_t)b->new_lens) & 3u) {
         set_error("page_table, starts, lens or new_lens is not aligned to its element size");
         return RT_ERR_ALIGN;
     }
-    if (new_lens == lens || new_lens == starts) {
+    if (b->new_lens == b->lens || b->new_lens == b->starts) {
         set_error("new_lens must not be one of the inputs");
         return RT_ERR_SHAPE;
     }
     a.m.status = device_status_word();
     if (!a.m.status) return RT_ERR_NO_DEVICE;
-    a.page_table = page_table;
-    a.page_table_stride = page_table_stride;
-    a.page_table_width = page_table_width;
+    a.page_table = b->page_table;
+    a.page_table_stride = b->page_table_stride;
+    a.page_table_width = (int)b->page_table_width;
     a.page_shift = log2_or_minus1((unsigned)a.m.page_size);
-    a.starts = starts;
-    a.lens = lens;
-    a.keep = keep;
-    a.keep_stride = keep_stride;
-    a.window = (int)window;
-    a.new_lens = new_lens;
-    a.n_seqs = (int)n_seqs;
+    a.starts = b->starts;
+    a.lens = b->lens;
+    a.keep = b->keep;
+    a.keep_stride = b->keep_stride;
+    a.window = (int)b->window;
+    a.new_lens = b->new_lens;
+    a.n_seqs = (int)b->n_seqs;
+    const long long n_seqs = b->n_seqs;
     rt_limits L;
     if ((st = current_limits(&L)) != RT_OK) return st;
     // Tasks (a side of a layer and a head) of a sequence to one CTA: few enough that two CTAs to an SM cover the device, and no fewer than its
@@ -227,7 +231,7 @@ int kv_cache_compact_launch(const rt_kv_cache* caches, int32_t n_caches, const i
     a.ctas_per_seq = (int)((tasks + a.tasks_per_cta - 1) / a.tasks_per_cta);
     const long long ctas = (long long)a.ctas_per_seq * n_seqs;
     if (ctas > 0x7fffffffLL) {
-        set_error("n_seqs=%lld needs too many CTAs", (long long)n_seqs);
+        set_error("n_seqs=%lld needs too many CTAs", n_seqs);
         return RT_ERR_SHAPE;
     }
     const int width = access_width(a.m, 0, a.m.kind[0].row_bytes, 16), row_vectors = a.m.kind[0].row_bytes / width;

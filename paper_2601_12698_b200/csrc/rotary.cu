@@ -36,7 +36,7 @@ typedef void (*RotaryKernel)(RotaryArgs);
 template <typename T, int P, int U>
 int launch_rotary(RotaryArgs a, cudaStream_t stream)
 {
-    const int heads = a.side[0].heads + a.side[1].heads, groups = kRotaryThreads / a.items;
+    const int heads = a.side[0].heads + a.side[1].heads, groups = kRotaryThreads / a.lanes;
     a.split = std::min(groups, (heads + U - 1) / U);
     a.tokens_per_cta = groups / a.split;
     const long long ctas = (a.n_tokens + a.tokens_per_cta - 1) / a.tokens_per_cta;
@@ -44,7 +44,7 @@ int launch_rotary(RotaryArgs a, cudaStream_t stream)
         set_error("n_tokens=%lld needs too many CTAs", (long long)a.n_tokens);
         return RT_ERR_SHAPE;
     }
-    const int threads = (a.tokens_per_cta * a.split * a.items + 31) / 32 * 32;
+    const int threads = (a.tokens_per_cta * a.split * a.lanes + 31) / 32 * 32;
     void* params[] = {&a};
     return launch_kernel((const void*)(RotaryKernel)rotary_kernel<T, P, U>, dim3((unsigned)ctas), dim3((unsigned)threads), 0, stream, params);
 }
@@ -61,6 +61,7 @@ int launch_width(RotaryArgs a, int rot, int tail_elems, bool interleaved, cudaSt
     a.interleaved = interleaved;
     a.first_step = interleaved ? 2 * VB : VB;
     a.tail = tail_elems / P;
+    a.lanes = a.items + (a.tail + 1) / 2;
     rt_limits L;
     const int st = current_limits(&L);
     if (st != RT_OK) return st;

@@ -7,7 +7,8 @@
 //
 // Bound by HBM: every element is read and written once.  A thread owns P pairs of one token (two vectors of P elements: j and
 // j + rot / 2, or two neighbouring ones) and walks over the heads with them, so that sines and cosines are computed once per
-// token and pair and stay in registers; U heads are fetched before the first is turned.
+// token and pair and stay in registers; U heads are fetched before the first is turned.  Elements behind the turned ones go through
+// threads of their own, two vectors each.
 //
 // Measured: 16384 tokens x 40 heads of 128, bf16, 336 MB: 56.5 us, 5.9 TB/s, 0.92 of the copy bandwidth.  64 tokens: 2.7 us in a graph,
 // the round trip for the position and the angles' arithmetic.
@@ -29,7 +30,8 @@ struct RotaryArgs {
     const unsigned long long* turns;
     const long long* positions;
     long long n_tokens;
-    int items;           // threads of one token and head group: rot / 2 / P
+    int items;           // threads of one token and head group that turn: rot / 2 / P
+    int lanes;           // those and the ones that copy what is behind
     int second;          // bytes from a thread's first vector to its second
     int first_step;      // bytes from one item's first vector to the next one's
     int rot_bytes;
@@ -44,16 +46,15 @@ struct RotaryArgs {
 constexpr int kRotaryThreads = 256;
 
 template <typename T, int P, int U>
-__global__ void __launch_bounds__(kRotaryThreads, U == 2 ? 4 : 2) rotary_kernel(const RotaryArgs a)
+__global__ void __launch_bounds__(kRotaryThreads, U == 2 ? 3 : 2) rotary_kernel(const RotaryArgs a)
 {
     constexpr int VB = P * (int)sizeof(T);
-    const int item = threadIdx.x % a.items, group = threadIdx.x / a.items;
+    const int item = threadIdx.x % a.lanes, group = threadIdx.x / a.lanes;
     const int part = group % a.split, in_cta = group / a.split;
     const long long token = (long long)blockIdx.x * a.tokens_per_cta + in_cta;
     wait_for_previous_kernel();
     if (in_cta >= a.tokens_per_cta || token >= a.n_tokens) return;
     const long long position = __ldg(a.positions + token);
-    if (position < 0) return;
 
     const int n_q = a.side[0].heads, heads = n_q + a.side[1].heads;
     const auto in_at = [&](int h) {
@@ -64,8 +65,32 @@ __global__ void __launch_bounds__(kRotaryThreads, U == 2 ? 4 : 2) rotary_kernel(
         const RotarySide& s = a.side[h >= n_q];
         return s.out + token * s.out_token + (long long)(h >= n_q ? h - n_q : h) * s.out_head;
     };
-    const int first = item * a.first_step;
     Vec<VB> x[U][2];
+    if (item >= a.items) {  // what is behind the turned elements
+        const int vector = (item - a.items) * 2, first = a.rot_bytes + vector * VB;
+        const bool pair = vector + 1 < a.tail;
+        if (position < 0) return;
+        for (int h0 = part; h0 < heads; h0 += U * a.split) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int h = h0 + u * a.split;
+                if (h < heads && a.side[h >= n_q].copy_tail) {
+                    x[u][0] = ld_stream<VB>(in_at(h) + first);
+                    if (pair) x[u][1] = ld_stream<VB>(in_at(h) + first + VB);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int h = h0 + u * a.split;
+                if (h < heads && a.side[h >= n_q].copy_tail) {
+                    st_stream<VB>(out_at(h) + first, x[u][0]);
+                    if (pair) st_stream<VB>(out_at(h) + first + VB, x[u][1]);
+                }
+            }
+        }
+        return;
+    }
+    const int first = item * a.first_step;
     const auto fetch = [&](int h0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -77,7 +102,8 @@ __global__ void __launch_bounds__(kRotaryThreads, U == 2 ? 4 : 2) rotary_kernel(
             }
         }
     };
-    fetch(part);  // under way while the angles are worked out
+    fetch(part);  // under way while the position comes and the angles are worked out
+    if (position < 0) return;
     float c[P], s[P];
 #pragma unroll
     for (int i = 0; i < P; ++i) {
@@ -116,14 +142,6 @@ __global__ void __launch_bounds__(kRotaryThreads, U == 2 ? 4 : 2) rotary_kernel(
             unsigned char* p = out_at(h) + first;
             st_stream<VB>(p, Codec<T, VB>::pack(y));
             st_stream<VB>(p + a.second, Codec<T, VB>::pack(z));
-        }
-    }
-    if (a.tail > 0) {
-        for (int h = part; h < heads; h += a.split) {
-            if (!a.side[h >= n_q].copy_tail) continue;
-            const unsigned char* from = in_at(h) + a.rot_bytes;
-            unsigned char* to = out_at(h) + a.rot_bytes;
-            for (int i = item; i < a.tail; i += a.items) st_stream<VB>(to + i * VB, ld_stream<VB>(from + i * VB));
         }
     }
 }

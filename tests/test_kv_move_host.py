@@ -16,7 +16,8 @@ def _copy(caches=None, src=P, dst=P, tokens=None, n=3):
 
 
 def _compact(caches=None, table=P, stride=4, width=4, starts=P, lens=P + 64, keep=P, keep_stride=8, window=8, new_lens=P + 128, n=3):
-    return B.lib.kv_cache_compact_launch(*(caches or _array(_cache(), _cache())), table, stride, width, starts, lens, keep, keep_stride, window, new_lens, n, None)
+    batch = B.rt_compact_batch(table, starts, lens, keep, new_lens, n, window, stride, width, keep_stride)
+    return B.lib.kv_cache_compact_launch(*(caches or _array(_cache(), _cache())), ctypes.byref(batch), None)
 
 
 @pytest.mark.parametrize("kw,status", [
@@ -29,7 +30,7 @@ def test_copy_refusals(kw, status):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(n=-1), "RT_ERR_SHAPE"), (dict(n=(1 << 24) + 1), "RT_ERR_SHAPE"), (dict(window=-1), "RT_ERR_SHAPE"), (dict(window=(1 << 30) + 1), "RT_ERR_SHAPE"),
-    (dict(width=-1), "RT_ERR_SHAPE"), (dict(stride=-1), "RT_ERR_SHAPE"), (dict(keep_stride=-8), "RT_ERR_SHAPE"), (dict(table=None), "RT_ERR_NULL"),
+    (dict(width=-1), "RT_ERR_SHAPE"), (dict(width=1 << 31), "RT_ERR_SHAPE"), (dict(stride=-1), "RT_ERR_SHAPE"), (dict(keep_stride=-8), "RT_ERR_SHAPE"), (dict(table=None), "RT_ERR_NULL"),
     (dict(starts=None), "RT_ERR_NULL"), (dict(lens=None), "RT_ERR_NULL"), (dict(keep=None), "RT_ERR_NULL"), (dict(new_lens=None), "RT_ERR_NULL"),
     (dict(table=P + 2), "RT_ERR_ALIGN"), (dict(new_lens=P + 2), "RT_ERR_ALIGN"), (dict(new_lens=P), "RT_ERR_SHAPE"), (dict(new_lens=P + 64), "RT_ERR_SHAPE")])
 def test_compact_refusals(kw, status):
@@ -51,3 +52,4 @@ def test_caches_that_differ_are_refused(change):
 def test_nothing_to_do_is_no_error():
     assert _copy(src=None, dst=None, n=0) == B.RT_OK
     assert _compact(table=None, starts=None, lens=None, keep=None, new_lens=None, n=0) == B.RT_OK
+    assert B.lib.kv_cache_compact_launch(*_array(_cache()), None, None) == B.RT_ERR_NULL

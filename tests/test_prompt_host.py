@@ -62,7 +62,7 @@ def test_null_batch_and_nothing_to_do():
 
 def test_struct_layouts_match_the_header():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-    structs = {n: getattr(B, n) for n in ("rt_rotary_spec", "rt_rotary", "rt_rotary_side", "rt_prompt_batch")}
+    structs = {n: getattr(B, n) for n in ("rt_rotary_spec", "rt_rotary", "rt_rotary_side", "rt_prompt_batch", "rt_compact_batch")}
     lines = [f'printf("%zu\\n", sizeof({n}));' + "".join(f'printf("%zu\\n", offsetof({n}, {f.rstrip(chr(95))}));' for f, _ in t._fields_) for n, t in structs.items()]
     src = '#include <stdio.h>\n#include <stddef.h>\n#include "rmsnorm_tuner.h"\nint main(void){' + "".join(lines) + 'printf("%d\\n", RT_MAX_LAYERS);return 0;}\n'
     with tempfile.TemporaryDirectory() as d:
