@@ -229,7 +229,7 @@ int prompt_attention_launch(const rt_prompt_batch* b, const void* q, int64_t q_t
     if ((st = make_map(&q_map, q, dtype, head_dim, q_heads, b->q_tokens, q_head_stride, q_token_stride, p.group, p.stream_tokens)) != RT_OK) return st;
     if (b->k_tokens > 0) {  // (without keys no tile is fetched)
         if ((st = make_map(&k_map, k, dtype, head_dim, kv_heads, b->k_tokens, k_head_stride, k_token_stride, 1, kPromptTile)) != RT_OK) return st;
-        if ((st = make_map(&v_map, v, dtype, head_dim, kv_heads, b->k_tokens, v_head_stride, v_token_stride, 1, kPromptTile)) != RT_OK) return st;
+        if ((st = make_map(&v_map, v, dtype, head_dim, kv_heads, b->k_tokens, v_head_stride, v_token_stride, 1, p.form == 2 ? PromptShape<256>::kValueRows : kPromptTile)) != RT_OK) return st;
     }
     void* params[] = {&q_map, &k_map, &v_map, &a};
     st = launch_kernel(kernels.attention[p.form], dim3((unsigned)p.ctas), dim3(kPromptThreads), kernels.smem[p.form], (cudaStream_t)stream, params);

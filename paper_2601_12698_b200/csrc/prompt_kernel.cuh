@@ -17,10 +17,13 @@
 // The streams share keys and values and take turns on the tensor cores: while one's scores are exponentiated the other's products
 // run.  The queries and first tiles of the next item are fetched, and its first scores computed, while this one's results leave.
 //
-// Heads of more than 128 (DP = 256): both streams take the same 128 rows, each all scores and one half of the dims, as tensor memory
-// has no room for two outputs of 256 (a quarter of the products is done twice).
+// Heads of more than 128 (DP = 256): tensor memory has no room for two outputs of 256, so both streams take the same 128 rows and one output,
+// the first the first 64 keys of every tile and the second the others.
 //
-// The reference m is moved only when a score exceeds it by 8, as in the prefix kernel: weights reach 2^8.
+// The reference m is moved only when a score exceeds it by 8, as in the prefix kernel: weights reach 2^8.  Streams that share rows share
+// the reference, as if the second's keys came behind the first's: a stream works with the reference that it knows, and before it
+// announces its weights it waits until the other has announced those that come before, looks whether the reference has been moved, and
+// if so works again.
 //
 // Values that a row does not see meet a weight of zero in the product, and 0 * inf is NaN.  Where a tile has such values (the diagonal, the
 // sequence's end), warps 8-11 replace infinities and NaN among the keys that not all rows see by zeros before the product, and
@@ -83,7 +86,9 @@ struct PromptItem {
 template <int DP>
 struct PromptShape {
     static constexpr int kBlocks = DP / 64;               // column blocks of a tile of queries, keys or values
-    static constexpr int kCols = DP == 256 ? 128 : DP;    // dims of a stream's output
+    static constexpr bool kSharedRows = DP == 256;        // both streams take the same rows
+    static constexpr int kCols = DP == 256 ? 128 : DP;    // dims that a stream writes
+    static constexpr int kValueRows = kSharedRows ? kPromptTile / 2 : kPromptTile;  // keys of a box of values: those of a stream
     static constexpr int kBlockBytes = kPromptTile * 128;
     // The ring: 160 KB, a block to a slot, or both of heads of 128.  (Heads of 128, 8192 tokens: 435 us with two, 445 with one; heads of 256, 256
     // tokens behind 8000: 102 us with one, as they are asked for and freed one after the other, 115 with two; 128 KB: 110.)
@@ -277,7 +282,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                                                                             const __grid_constant__ CUtensorMap v_map, const __grid_constant__ PromptArgs a)
 {
     using S = PromptShape<DP>;
-    constexpr bool kSplitDims = DP == 256;
+    constexpr bool kSharedRows = S::kSharedRows;
+    constexpr int kHalves = kSharedRows ? 1 : 2;  // halves of a tile that a stream takes
     constexpr int kBlocks = S::kBlocks, kSlotBlocks = S::kSlotBlocks, kUnits = S::kUnits;
     constexpr uint32_t kScoreIdesc = tc_instruction<T>(kPromptTile / 2, false, false);
     constexpr uint32_t kColO = 2 * kPromptTile;
@@ -286,17 +292,18 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
     unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     unsigned char* ring = smem + S::kRingAt;
     __shared__ __align__(8) uint64_t full[S::kSlots], empty[S::kSlots], item_full[kPromptItems], item_free[kPromptItems], landed[kPromptLanded], q_full, q_free, s_full[2][2],
-        p_full[2][2], o_done[2], o_full[2], drained[2];
+        p_full[2][2], o_done[2], o_full[2], sums_full[2], drained[2];
     __shared__ PromptItem items[kPromptItems];
     __shared__ uint32_t tmem_base;
+    __shared__ float row_reference[kSharedRows ? kPromptTile : 1], row_sum[kSharedRows ? kPromptTile : 1];  // what streams that share rows tell one another
 
     const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
     if (tid < S::kSlots) {
         mbarrier_init(&full[tid], 1);
-        mbarrier_init(&empty[tid], 2);
+        mbarrier_init(&empty[tid], kSharedRows ? 1 : 2);
     } else if (tid >= 32 && tid < 32 + kPromptItems) {
         mbarrier_init(&item_full[tid - 32], 1);
-        mbarrier_init(&item_free[tid - 32], 15);  // warps that read it: 8 softmax, 4 looking, 2 issuing, 1 fetching
+        mbarrier_init(&item_free[tid - 32], kSharedRows ? 14 : 15);  // warps that read it: 8 softmax, 4 looking, 1 or 2 issuing, 1 fetching
         items[tid - 32].valid = 0;
     } else if (tid >= 64 && tid < 66) {
         const int i = tid - 64;
@@ -311,7 +318,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         mbarrier_init(&landed[tid - 96], 1);
     } else if (tid == 127) {
         mbarrier_init(&q_full, 1);
-        mbarrier_init(&q_free, 2);
+        mbarrier_init(&q_free, kSharedRows ? 1 : 2);
+        mbarrier_init(&sums_full[0], 128);
+        mbarrier_init(&sums_full[1], 128);
     } else if (tid >= 128 && tid < 131) {
         const CUtensorMap* map = tid == 128 ? &q_map : tid == 129 ? &k_map : &v_map;
         asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
@@ -346,9 +355,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
     };
     // Key tiles that a stream's rows see: all of the item's but the last ones, or none.
     auto stream_tiles = [&](const PromptItem& item, int s) -> int {
-        const int first = kSplitDims ? 0 : s * a.stream_tokens;
+        const int first = kSharedRows ? 0 : s * a.stream_tokens;
         if (first >= item.tokens) return 0;
-        const int last_token = kSplitDims ? item.tokens - 1 : min(item.tokens, first + a.stream_tokens) - 1;
+        const int last_token = kSharedRows ? item.tokens - 1 : min(item.tokens, first + a.stream_tokens) - 1;
         const int last = min(item.last_key + item.key_step * last_token, item.end_key - 1);
         return min(item.tile1, (last + kPromptTile) / kPromptTile) - item.tile0;  // (last >= -kPromptTile where it matters: none is cut to 0 by its users)
     };
@@ -359,6 +368,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         const int s = warp >> 2, r = (warp & 3) * 32 + lane;
         const uint32_t lane_base = tmem + ((uint32_t)(warp & 3) << 21);
         const uint32_t s_col = lane_base + s * kPromptTile, o_col = lane_base + kColO + s * S::kCols;
+        const int first_key = kSharedRows ? s * 64 : 0;  // of a tile's, the first that this stream takes
         const int n_heads = a.kv_heads * a.group;
         const float c = fmaxf(a.score_scale, 1.17549435e-38f);  // (a scale of zero would make NaN of hidden scores: the smallest normal number does instead)
         const float2x c2 = pack_f2(c, c);
@@ -367,7 +377,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         uint32_t tiles_done = 0, results_done = 0;  // of this stream
         PromptItem item;
         for (int n = 0; next_item(n, item); ++n) {
-            const int first_token = kSplitDims ? 0 : s * a.stream_tokens;
+            const int first_token = kSharedRows ? 0 : s * a.stream_tokens;
             const int my_tiles = max(stream_tiles(item, s), 0);
             // Row i of this stream's 128 counted in [token][head] rows from the item's first token and head, -1: no such row.
             const auto row_index = [&](int i) -> int {
@@ -384,7 +394,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                 for (int k = 0; k < 32; ++k)
                     if (k > seen) v[k] = 0xFF800000u;
             };
-            if (my_tiles > 0) {  // the row's first scores give it its first reference
+            if (kSharedRows && s == 1 && my_tiles > 0) {  // its first reference is what the first stream has found
+                wait(&p_full[0][0], tiles_done & 1);
+                m = *const_cast<volatile float*>(&row_reference[r]);
+            } else if (my_tiles > 0) {  // the row's first scores give it its first reference
                 wait(&s_full[s][0], tiles_done & 1);
                 tc_fence_after();
                 float top = -INFINITY;
@@ -398,17 +411,18 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                     for (int k = 0; k < 32; k += 2) top = fmaxf(fmaxf(top, __uint_as_float(v[k])), __uint_as_float(v[k + 1]));
                 }
                 if (top != -INFINITY) m = top * c;
+                if (kSharedRows) *const_cast<volatile float*>(&row_reference[r]) = m;
             }
             for (int i = 0; i < my_tiles; ++i) {
                 const int tile = item.tile0 + i;
                 const bool masked = tile >= item.masked_from;
-                const int lim = last - tile * kPromptTile;  // columns up to this one are seen
-                const uint32_t half0 = 2 * (tiles_done + i);
+                const int lim = last - tile * kPromptTile - first_key;  // columns up to this one are seen
+                const uint32_t count = tiles_done + i;
                 // Half a tile at a time: its product with the values and the next tile's scores of that half run while the other half is
                 // exponentiated.
 #pragma unroll 1
-                for (int h = 0; h < 2; ++h) {
-                    wait(&s_full[s][h], (tiles_done + i) & 1);
+                for (int h = 0; h < kHalves; ++h) {
+                    wait(&s_full[s][h], count & 1);
                     tc_fence_after();
                     const uint32_t col = s_col + h * 64;
                     // One pass over the row's 64 scores gives their maximum and, with the reference as it is, the weights and their sum.
@@ -416,7 +430,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                     // that has been moved there; the scores are still in tensor memory, the weights go over them at the end.
                     uint32_t w[2][16];
                     float2x sum[2];
-                    for (;;) {
+                    for (bool settled = false;;) {
                         // No key of the row so far: the reference is -inf, every score is -inf, and so must every weight's logarithm be.
                         const float reference = m == -INFINITY ? 0.f : m;
                         const float2x minus2 = pack_f2(-reference, -reference);
@@ -456,24 +470,38 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                         }
                         float top = fmaxf(t4[0], t4[1]);
                         top = top == -INFINITY ? top : top * c;
-                        const bool move = top > m + 8.f;
-                        if (!__any_sync(0xFFFFFFFFu, move)) break;
-                        const float alpha = move ? ex2(m - top) : 1.f;
-                        if (i + h > 0) {  // the products so far are complete before they are rescaled
-                            wait(&o_done[s], (half0 + h - 1) & 1);
-                            tc_fence_after();
-#pragma unroll 1
-                            for (int q = 0; q < S::kCols / 16; ++q) {
-                                uint32_t o[16];
-                                tmem_load16(o_col + q * 16, o);
-                                tmem_wait_load(o);
-#pragma unroll
-                                for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
-                                tmem_store16(o_col + q * 16, o);
-                            }
+                        if (settled) break;
+                        float known = m;
+                        if constexpr (kSharedRows) {  // the weights before these have been announced: the reference is what they left
+                            if (s == 1) wait(&p_full[0][0], count & 1);
+                            else if (i > 0) wait(&p_full[1][0], (count - 1) & 1);
+                            m = *const_cast<volatile float*>(&row_reference[r]);
                         }
-                        l *= alpha;
-                        if (move) m = top;
+                        const bool move = top > m + 8.f;
+                        if (!__any_sync(0xFFFFFFFFu, move || (kSharedRows && m != known))) break;
+                        settled = kSharedRows;  // (a row of a stream of its own is found settled by its maximum)
+                        if (!kSharedRows || __any_sync(0xFFFFFFFFu, move)) {
+                            const float alpha = move ? ex2(m - top) : 1.f;
+                            if (i + h + (kSharedRows ? s : 0) > 0) {  // the products so far are complete before they are rescaled
+                                // (The phase before that one is complete: scores come behind the products of the tile before.)
+                                if constexpr (kSharedRows) wait(&o_done[s ^ 1], (s == 1 ? count : count - 1) & 1);
+                                else wait(&o_done[s], (2 * count + h - 1) & 1);
+                                tc_fence_after();
+#pragma unroll 1
+                                for (int q = 0; q < (kSharedRows ? DP : S::kCols) / 16; ++q) {
+                                    const uint32_t col = kSharedRows ? lane_base + kColO : o_col;
+                                    uint32_t o[16];
+                                    tmem_load16(col + q * 16, o);
+                                    tmem_wait_load(o);
+#pragma unroll
+                                    for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
+                                    tmem_store16(col + q * 16, o);
+                                }
+                            }
+                            if (move) m = top;
+                            if (kSharedRows && move) *const_cast<volatile float*>(&row_reference[r]) = m;
+                        }
+                        if (m != known) l *= ex2(known - m);
                     }
 #pragma unroll
                     for (int q = 0; q < 2; ++q) tmem_store16(col + q * 16, w[q]);
@@ -490,14 +518,30 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
             // the item's rows
             if (my_tiles > 0) {
                 wait(&o_full[s], results_done & 1);
-                ++results_done;
                 tc_fence_after();
+                if constexpr (kSharedRows) {
+                    const float known = m;
+                    m = *const_cast<volatile float*>(&row_reference[r]);
+                    if (m != known) l *= ex2(known - m);
+                    volatile float* const sum_of_row = &row_sum[r];  // the second stream's first, then both's
+                    if (s == 0) {
+                        wait(&sums_full[1], results_done & 1);
+                        l += *sum_of_row;
+                    }
+                    *sum_of_row = l;
+                    mbarrier_arrive(&sums_full[s]);
+                    if (s == 1) {
+                        wait(&sums_full[0], results_done & 1);
+                        l = *sum_of_row;
+                    }
+                }
+                ++results_done;
                 if (*reinterpret_cast<volatile int*>(&items[n % kPromptItems].bad_values) != 0) {
                     // Infinities and NaN among the keys that not all rows see were left out of the product: the rows that see them get them now.
                     const int from = max(item.last_key + 1, item.tile0 * kPromptTile);
                     const int to = there ? min(last + 1, item.tile1 * kPromptTile) : from;
-                    const unsigned char* values = a.v + (long long)item.k_row * a.v_token_stride + (long long)item.kv_head * a.v_head_stride + (kSplitDims ? s * 256 : 0);
-                    const int dims = min(a.dim - (kSplitDims ? s * 128 : 0), S::kCols);
+                    const unsigned char* values = a.v + (long long)item.k_row * a.v_token_stride + (long long)item.kv_head * a.v_head_stride + (kSharedRows ? s * 256 : 0);
+                    const int dims = min(a.dim - (kSharedRows ? s * 128 : 0), S::kCols);
 #pragma unroll 1
                     for (int q = 0; q < S::kCols / 16; ++q) {
                         uint32_t o[16];
@@ -526,13 +570,13 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
             const long long first_row = (long long)item.q_row * n_heads + item.kv_head * a.group;
             const bool none = l == 0.f;
             const float inv = none ? 0.f : __frcp_rn(l), total = none ? -INFINITY : m + log2f(l);
-            if (my_row >= 0 && (!kSplitDims || s == 0)) {
+            if (my_row >= 0 && (!kSharedRows || s == 0)) {
                 if (a.parts > 1) a.part_lse[item.part * n_rows + first_row + my_row] = total;
                 else if (a.lse) a.lse[first_row + my_row] = total * 0.69314718055994531f;
             }
             // A thread holds a row, and rows lie apart; 32 bytes at a time are whole sectors all the same.  (Results that went through shared
             // memory, so that eight lanes wrote 128 bytes of a row side by side, took twice as long to leave, 1.6 us.)
-            const int dim0 = kSplitDims ? s * 128 : 0, elem = a.parts > 1 ? 4 : 2;
+            const int dim0 = kSharedRows ? s * 128 : 0, elem = a.parts > 1 ? 4 : 2;
             unsigned char* const to = (a.parts > 1 ? reinterpret_cast<unsigned char*>(a.part_out) + item.part * n_rows * a.dim * 4 : static_cast<unsigned char*>(a.out)) +
                                       (first_row + max(my_row, 0)) * a.dim * elem;
 #pragma unroll 1
@@ -584,6 +628,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
 #pragma unroll 1
                     for (int b = 0; b < kBlocks; ++b) {
                         unsigned char* row = ring + (unit + b / kSlotBlocks) % S::kSlots * S::kSlotBytes + b % kSlotBlocks * S::kBlockBytes + p * 128;
+                        if (kSharedRows)  // two slots to a stream's keys, blocks of 64 of them
+                            row = ring + (unit + p / 64 * 2) % S::kSlots * S::kSlotBytes + b * (64 * 128) + p % 64 * 128;
 #pragma unroll
                         for (int u = 0; u < 8; ++u) {
                             uint4* at = reinterpret_cast<uint4*>(row + ((u ^ (p & 7)) << 4));
@@ -605,19 +651,98 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
             tiles_before += item.tile1 - item.tile0;
             done_with_item(n);
         }
+    }
+    if constexpr (kSharedRows) {
+        if (warp == 12) {
+            // ---- the warp that issues the products of both streams ----
+            constexpr uint64_t kRowsLayout = tc_layout(16, 1024), kColsLayout = tc_layout(S::kValueRows * 128, 1024);
+            constexpr uint32_t kSlot16 = S::kSlotBytes / 16;
+            const uint64_t q_at = tc_descriptor(kRowsLayout, smem_u32(smem) >> 4);
+            const uint64_t k_base = tc_descriptor(kRowsLayout, smem_u32(ring) >> 4), v_base = tc_descriptor(kColsLayout, smem_u32(ring) >> 4);
+            const int steps = (a.dim + 15) / 16;  // of 16 dims
+            const uint32_t out_idesc = tc_instruction<T>(steps * 16, false, true);
+            uint32_t tiles_before = 0, items_before = 0;
+            auto wait_unit = [&](uint32_t unit) {
+                wait(&full[unit % S::kSlots], (unit / S::kSlots) & 1);
+                tc_fence_after();
+            };
+            PromptItem item;
+            for (int n = 0; next_item(n, item); ++n) {
+                const int tiles = item.tile1 - item.tile0;
+                if (tiles > 0) {
+                    wait(&q_full, items_before & 1);
+                    tc_fence_after();
+                    ++items_before;
+                }
+                // S = Q K^T of stream s with its keys of the item's tile number i
+                auto scores = [&](int i, int s) {
+                    const uint32_t unit = 2 * (tiles_before + i) * kUnits;
+#pragma unroll
+                    for (int b = 0; b < kBlocks; ++b) {
+                        const uint32_t slot = (unit + b) % S::kSlots;
+                        if (s == 0) wait_unit(unit + b);
+                        if (elect_one()) {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                if (b * 4 + k < steps)
+                                    tc_mma_ss(tmem + s * kPromptTile, q_at + (b * (S::kBlockBytes / 16) + k * 2), k_base + (slot * kSlot16 + k * 2 + s * (64 * 128 / 16)), kScoreIdesc, b + k > 0);
+                            if (s == 1) tc_commit(&empty[slot]);
+                            if (b == kBlocks - 1) {
+                                tc_commit(&s_full[s][0]);
+                                if (s == 1 && i + 1 == tiles) tc_commit(&q_free);
+                            }
+                        }
+                        __syncwarp();
+                    }
+                };
+                if (tiles > 0) {
+                    scores(0, 0);
+                    scores(0, 1);
+                }
+                for (int i = 0; i < tiles; ++i) {
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        // O += W V with the stream's values: two slots, side by side
+                        const uint32_t unit = (2 * (tiles_before + i) + 1) * kUnits + 2 * s, slot = unit % S::kSlots;
+                        wait_unit(unit);
+                        wait_unit(unit + 1);
+                        wait(&p_full[s][0], (tiles_before + i) & 1);
+                        tc_fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int k = 0; k < kPromptTile / 32; ++k)
+                                tc_mma_ts(tmem + kColO, tmem + s * kPromptTile + k * 8, v_base + (slot * kSlot16 + k * 128), out_idesc, i + s + k > 0);
+                            tc_commit(&o_done[s]);
+                            tc_commit(&empty[slot]);
+                            tc_commit(&empty[slot + 1]);
+                            if (s == 1 && i + 1 == tiles) {
+                                tc_commit(&o_full[0]);
+                                tc_commit(&o_full[1]);
+                            }
+                        }
+                        __syncwarp();
+                        if (i + 1 < tiles) scores(i + 1, s);
+                    }
+                }
+                tiles_before += tiles;
+                done_with_item(n);
+            }
+            // the tensor memory is given back only when nothing writes it any more
+            if (elect_one()) tc_commit(&drained[0]);
+            __syncwarp();
+            ok = mbarrier_wait_sleeping(&drained[0], 0) && ok;
+        }
     } else if (warp >= 12 && warp < 14) {
         // ---- warps that issue the products of the two streams ----
         const int s = warp - 12;
         constexpr uint64_t kRowsLayout = tc_layout(16, 1024), kColsLayout = tc_layout(S::kBlockBytes, 1024);
         constexpr uint32_t kSlot16 = S::kSlotBytes / 16, kBlock16 = S::kBlockBytes / 16;
-        constexpr int kValueUnits = S::kCols / 64 / kSlotBlocks;  // of the values, those of this stream's dims
         const uint32_t q16 = smem_u32(smem) >> 4, ring16 = smem_u32(ring) >> 4;
-        const uint64_t q_at = tc_descriptor(kRowsLayout, q16 + (kSplitDims ? 0 : s) * (S::kQueryBytes / 16));
+        const uint64_t q_at = tc_descriptor(kRowsLayout, q16 + s * (S::kQueryBytes / 16));
         const uint64_t k_base = tc_descriptor(kRowsLayout, ring16), v_base = tc_descriptor(kColsLayout, ring16);
         const uint32_t d_scores = tmem + s * kPromptTile, d_out = tmem + kColO + s * S::kCols;
         const int steps = (a.dim + 15) / 16;  // of 16 dims
-        const int out_dims = max(16, min((a.dim - (kSplitDims ? s * 128 : 0) + 15) / 16 * 16, S::kCols));
-        const uint32_t out_idesc = tc_instruction<T>(out_dims, false, true);
+        const uint32_t out_idesc = tc_instruction<T>(steps * 16, false, true);
         uint32_t tiles_before = 0, my_tiles_before = 0, items_before = 0;
         auto wait_unit = [&](uint32_t unit) {
             wait(&full[unit % S::kSlots], (unit / S::kSlots) & 1);
@@ -668,10 +793,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                     for (int b = 0; b < 2 * kUnits; ++b) skip_unit(unit - kUnits + b);
                     continue;
                 }
-                // O += W V.  Heads of 256: this stream's half of the dims; the other half is the other stream's.
-                const uint32_t my_unit = unit + (kSplitDims ? s * kValueUnits : 0), slot = my_unit % S::kSlots;  // (of two slots the even one: they lie side by side)
+                // O += W V
+                const uint32_t slot = unit % S::kSlots;
 #pragma unroll
-                for (int b = 0; b < kValueUnits; ++b) wait_unit(my_unit + b);
+                for (int u = 0; u < kUnits; ++u) wait_unit(unit + u);
                 const uint64_t v_at = v_base + slot * kSlot16;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -684,10 +809,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                         tc_commit(&o_done[s]);
                         if (h == 1) {
 #pragma unroll
-                            for (int b = 0; b < kValueUnits; ++b) {
-                                tc_commit(&empty[slot + b]);
-                                if (kSplitDims) tc_commit(&empty[slot + b]);  // (the only stream that reads it)
-                            }
+                            for (int u = 0; u < kUnits; ++u) tc_commit(&empty[slot + u]);
                             if (i + 1 == mine) tc_commit(&o_full[s]);
                         }
                     }
@@ -704,13 +826,14 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         if (elect_one()) tc_commit(&drained[s]);
         __syncwarp();
         ok = mbarrier_wait_sleeping(&drained[s], 0) && ok;
-    } else if (warp == 14) {
+    }
+    if (warp == 14) {
         // ---- the warp that fetches ----
         uint32_t units = 0, items_before = 0, looks = 0;
         bool posted = false;
         const uint32_t query_bytes = (uint32_t)(a.stream_tokens * a.group) * 128u * kBlocks;
         // A tile of keys or values from row `row` on; `bar`, where there is one, is told of all its bytes, otherwise each slot of its own.
-        auto fetch = [&](const CUtensorMap* map, int head, int row, uint64_t* bar) {
+        auto fetch = [&](const CUtensorMap* map, int head, int row, uint64_t* bar, bool by_stream) {
 #pragma unroll
             for (int u = 0; u < kUnits; ++u) {
                 const uint32_t slot = units % S::kSlots;
@@ -719,8 +842,13 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                     if (!bar) mbarrier_expect_tx(&full[slot], S::kSlotBytes);
                     else if (u == 0) mbarrier_expect_tx(bar, S::kSlotBytes * kUnits);
 #pragma unroll
-                    for (int b = 0; b < kSlotBlocks; ++b)
+                    for (int b = 0; b < (by_stream ? 0 : kSlotBlocks); ++b)
                         tma_load_3d(ring + slot * S::kSlotBytes + b * S::kBlockBytes, map, (u * kSlotBlocks + b) * 64, head, row, bar ? bar : &full[slot]);
+                    if (by_stream) {  // half of the columns of a stream's values
+#pragma unroll
+                        for (int b = 0; b < 2; ++b)
+                            tma_load_3d(ring + slot * S::kSlotBytes + b * (64 * 128), map, (u % 2 * 2 + b) * 64, head, row + u / 2 * 64, bar ? bar : &full[slot]);
+                    }
                 }
                 __syncwarp();
                 ++units;
@@ -745,9 +873,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
             }
             for (int i = 0; i < tiles; ++i) {
                 const int row = item.k_row + (item.tile0 + i) * kPromptTile;
-                fetch(&k_map, item.kv_head, row, nullptr);
+                fetch(&k_map, item.kv_head, row, nullptr, false);
                 const bool masked = item.tile0 + i >= item.masked_from;  // then those who look through the values tell the others
-                fetch(&v_map, item.kv_head, row, masked ? &landed[looks % kPromptLanded] : nullptr);
+                fetch(&v_map, item.kv_head, row, masked ? &landed[looks % kPromptLanded] : nullptr, kSharedRows);
                 if (masked) ++looks;
             }
             done_with_item(n);
