@@ -541,8 +541,8 @@ typedef struct {
     int64_t n_seqs;          /* 0 .. 2^24 */
     int64_t q_tokens;        /* rows of q, out and lse: 0 .. 2^30 */
     int64_t k_tokens;        /* rows of k and v: 0 .. 2^30 */
-    int64_t max_q_len;       /* about the largest number of queries and of keys of a sequence; the launch shape follows */
-    int64_t max_k_len;       /* them, the results do not */
+    int64_t max_q_len;       /* about the largest number of queries and of keys of a sequence: the launch shape follows them, */
+    int64_t max_k_len;       /* and of the results the roundings alone */
     int32_t causal;          /* 1: query i of n_q sees the keys j <= n_k - n_q + i; 0: all keys of its sequence */
     int32_t reserved;        /* 0 */
 } rt_prompt_batch;
@@ -562,8 +562,8 @@ typedef struct {
  *              contiguous, or NULL.
  *   workspace  device memory of prompt_attention_workspace_bytes(...) bytes, 16-byte aligned.  It carries nothing from one call to the
  *              next; calls that may overlap on the device need one each.
- * Starts that descend or lie outside the tensors are cut to them and leave RT_ERR_INDEX in the device status word; nothing outside the
- * tensors is read or written.  From call to call the results are bit-identical.  Asynchronous on `stream`, allocates nothing.
+ * Starts that descend or lie outside the tensors, of whichever sequence: nothing is computed or written, and RT_ERR_INDEX is left in
+ * the device status word.  From call to call the results are bit-identical.  Asynchronous on `stream`, allocates nothing.
  */
 int prompt_attention_launch(const rt_prompt_batch* batch, const void* q, int64_t q_token_stride, int64_t q_head_stride, int32_t q_heads,
                             const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,

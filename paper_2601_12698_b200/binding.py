@@ -701,7 +701,7 @@ def rotary_launch(table: RotaryTable, positions, q, k=None, q_out=None, k_out=No
 class PromptBatch:
     """Sequences packed behind one another: the first query row of each and, last, the row behind them all (int32 [n_seqs + 1], not
     descending), and the same for keys (k_starts None: the queries' own).  max_q_len and max_k_len are about the largest lengths, on the
-    host's side: the launch shape follows them, the results do not.  causal: the queries are the last tokens of their sequence and see the
+    host's side: the launch shape follows them, and of the results the roundings alone.  causal: the queries are the last tokens of their sequence and see the
     keys up to their own; otherwise all of the sequence's.  One object serves every layer of the step."""
 
     def __init__(self, q_starts, max_q_len: int, k_starts=None, max_k_len: int | None = None, causal: bool = True):

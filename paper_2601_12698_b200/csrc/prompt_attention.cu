@@ -63,7 +63,7 @@ int make_prompt_plan(const rt_prompt_batch* b, int q_heads, int kv_heads, int di
     // the time to write and read them at 5 TB/s.  512 tokens behind 16000, 40 heads on 8 of 128, 88 blocks: 240 us in one part, 172 in three.
     // Blocks of two waves and more are left whole: their order evens them out.
     p->parts = 1;
-    if (expected > 0 && expected < 2LL * L.sm_count && tiles >= 8) {
+    if (expected > 0 && expected < 2LL * L.sm_count && b->q_tokens / p->block_tokens * kv_heads < 2LL * L.sm_count && tiles >= 8) {
         const double tile_us = p->form == 2 ? 3.2 : 1.7, part_us = (double)b->q_tokens * q_heads * dim * 8 / 5e6;
         double best = 0;
         for (int parts = 1; parts <= std::min<long long>(kPromptMaxParts, tiles / 2); ++parts) {
@@ -76,7 +76,7 @@ int make_prompt_plan(const rt_prompt_batch* b, int q_heads, int kv_heads, int di
     }
     p->ctas = std::min<long long>(L.sm_count, blocks * kv_heads * p->parts);
     const int64_t rows = b->q_tokens * q_heads;
-    if (p->parts > 1) p->workspace = (int64_t)p->parts * rows * dim * 4 + ((int64_t)p->parts * rows * 4 + 15) / 16 * 16;
+    if (p->parts > 1) p->workspace = (int64_t)p->parts * rows * dim * 4 + ((int64_t)p->parts * rows * 4 + 4 + 15) / 16 * 16;  // results, logarithms, a flag
     return RT_OK;
 }
 
@@ -214,6 +214,7 @@ int prompt_attention_launch(const rt_prompt_batch* b, const void* q, int64_t q_t
     if (p.parts > 1) {
         a.part_out = (float*)workspace;
         a.part_lse = a.part_out + (int64_t)p.parts * b->q_tokens * q_heads * head_dim;
+        a.part_ready = (int*)(a.part_lse + (int64_t)p.parts * b->q_tokens * q_heads);
     }
     // (binary32 parts of heads that are multiples of 8 are)
     a.wide_rows = p.parts > 1 ? (uintptr_t)workspace % 32 == 0 : head_dim % 16 == 0 && (uintptr_t)out % 32 == 0;
@@ -235,10 +236,6 @@ int prompt_attention_launch(const rt_prompt_batch* b, const void* q, int64_t q_t
     st = launch_kernel(kernels.attention[p.form], dim3((unsigned)p.ctas), dim3(kPromptThreads), kernels.smem[p.form], (cudaStream_t)stream, params);
     if (st != RT_OK || p.parts == 1) return st;
     const long long merge_ctas = ceil_div(b->q_tokens * q_heads, kPromptMergeThreads / 32);
-    if (merge_ctas > 0x7fffffffLL) {
-        set_error("q_tokens=%lld needs too many CTAs", (long long)b->q_tokens);
-        return RT_ERR_SHAPE;
-    }
     void* merge_params[] = {&a};
     return launch_kernel(kernels.merge, dim3((unsigned)merge_ctas), dim3(kPromptMergeThreads), 0, (cudaStream_t)stream, merge_params);
 }

@@ -64,6 +64,7 @@ struct PromptArgs {
     float* lse;       // [token][head] or NULL
     float* part_out;  // parts > 1: [part][token][head][dim], normalised
     float* part_lse;  // [part][token][head], base 2
+    int* part_ready;  // parts > 1: set to 1 when the starts are sound, or to 0, and then nothing is written
     int wide_rows;    // rows of out, or of part_out, are multiples of 32 bytes
     int* status;
     unsigned wait_polls;
@@ -125,15 +126,16 @@ __device__ __forceinline__ void store_row(unsigned char* to, const uint32_t* x, 
     }
 }
 
-// A sequence as the items see it: its rows cut to the tensors, its number of blocks and what its first block costs.
+// A sequence as the items see it.  `sound`: its starts do not descend and lie in the tensors; otherwise it has no rows.
 struct PromptSequence {
     int q_row, q_len, k_row, k_len;
+    bool sound;
 };
 __device__ __forceinline__ PromptSequence prompt_sequence(const PromptArgs& a, int i)
 {
-    const int q0 = min(max(__ldg(a.q_starts + i), 0), a.q_tokens), q1 = min(max(__ldg(a.q_starts + i + 1), 0), a.q_tokens);
-    const int k0 = min(max(__ldg(a.k_starts + i), 0), a.k_tokens), k1 = min(max(__ldg(a.k_starts + i + 1), 0), a.k_tokens);
-    return {q0, max(q1 - q0, 0), k0, max(k1 - k0, 0)};
+    const int q0 = __ldg(a.q_starts + i), q1 = __ldg(a.q_starts + i + 1), k0 = __ldg(a.k_starts + i), k1 = __ldg(a.k_starts + i + 1);
+    const bool sound = 0 <= q0 && q0 <= q1 && q1 <= a.q_tokens && 0 <= k0 && k0 <= k1 && k1 <= a.k_tokens;
+    return {sound ? q0 : 0, sound ? q1 - q0 : 0, sound ? k0 : 0, sound ? k1 - k0 : 0, sound};
 }
 
 // The order in which blocks are taken, whole warps: the most expensive first, so that the CTAs end together.  A block's cost is
@@ -147,11 +149,12 @@ struct PromptOrder {
     long long dearer;      // blocks that cost more than `cost`
     long long not_cheaper; // blocks that cost `cost` or more
 
-    __device__ __forceinline__ void shape(int i, int& n, int& first) const
+    __device__ __forceinline__ bool shape(int i, int& n, int& first) const
     {
         const PromptSequence s = prompt_sequence(a, i);
         n = (s.q_len + a.block_tokens - 1) / a.block_tokens;
         first = a.causal ? max(s.k_len - s.q_len, 0) / a.block_tokens : s.k_len / a.block_tokens;
+        return s.sound;
     }
     __device__ __forceinline__ int count(int n, int first, int c) const  // blocks that cost c or more
     {
@@ -176,28 +179,28 @@ struct PromptOrder {
         each([&](int, int n, int first) { sum += __reduce_add_sync(0xFFFFFFFFu, (unsigned)count(n, first, c)); });
         return sum;
     }
+    bool sound;  // all sequences are; otherwise there are no blocks
     __device__ __forceinline__ explicit PromptOrder(const PromptArgs& args) : a(args)
     {
         const int lane = threadIdx.x & 31;
+        bool mine = true;
 #pragma unroll
         for (int j = 0; j < kKept; ++j) {
             blocks[j] = base[j] = 0;
-            if (j * 32 + lane < a.n_seqs) shape(j * 32 + lane, blocks[j], base[j]);
+            if (j * 32 + lane < a.n_seqs) mine = shape(j * 32 + lane, blocks[j], base[j]) && mine;
         }
-        total = all(0);
+        long long sum = 0;
+        for (int i0 = kKept * 32; i0 < a.n_seqs; i0 += 32) {
+            int n = 0, first = 0;
+            if (i0 + lane < a.n_seqs) mine = shape(i0 + lane, n, first) && mine;
+            sum += __reduce_add_sync(0xFFFFFFFFu, (unsigned)n);
+        }
+#pragma unroll
+        for (int j = 0; j < kKept; ++j) sum += __reduce_add_sync(0xFFFFFFFFu, (unsigned)blocks[j]);
+        sound = __all_sync(0xFFFFFFFFu, mine);
+        total = sound ? sum : 0;
         cost = -1;
         dearer = not_cheaper = 0;
-    }
-    // Starts that descend or lie outside are reported (by one warp of the grid).
-    __device__ __forceinline__ void report() const
-    {
-        bool bad = false;
-        for (int i = threadIdx.x & 31; i <= a.n_seqs; i += 32) {
-            const int q = __ldg(a.q_starts + i), k = __ldg(a.k_starts + i);
-            bad = bad || q < 0 || q > a.q_tokens || k < 0 || k > a.k_tokens ||
-                  (i < a.n_seqs && (__ldg(a.q_starts + i + 1) < q || __ldg(a.k_starts + i + 1) < k));
-        }
-        if (bad) atomicExch(a.status, kDeviceIndexCode);
     }
     // The same without an order, for a grid that takes all blocks at once.
     __device__ __forceinline__ void find_any(long long rank, int& seq, int& block) const
@@ -909,9 +912,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                 } else {
                     order.find(rank, seq, block);
                 }
-                PromptSequence q = {0, 0, 0, 0};
-                if (seq >= 0) q = prompt_sequence(a, seq);  // (starts that descend can count more blocks than there are)
-                else block = 0;
+                const PromptSequence q = prompt_sequence(a, seq);
                 item.valid = 1;
                 item.tokens = min(a.block_tokens, q.q_len - block * a.block_tokens);
                 item.q_row = q.q_row + block * a.block_tokens;
@@ -936,7 +937,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                 mbarrier_arrive(&item_full[n % kPromptItems]);
             }
             __syncwarp();
-            if (n == 0 && blockIdx.x == 0) order.report();
+            if (n == 0 && blockIdx.x == 0 && lane == 0) {
+                if (!order.sound) atomicExch(a.status, kDeviceIndexCode);
+                if (a.parts > 1) *a.part_ready = order.sound;
+            }
             if (!item.valid) break;
         }
     }
@@ -957,7 +961,7 @@ __global__ void __launch_bounds__(kPromptMergeThreads) prompt_merge_kernel(const
     const long long row = (long long)blockIdx.x * (kPromptMergeThreads / 32) + (threadIdx.x >> 5), n_rows = (long long)a.q_tokens * n_heads;
     wait_for_previous_kernel();
     const int token = (int)(row / n_heads);
-    if (row >= n_rows || token < __ldg(a.q_starts) || token >= __ldg(a.q_starts + a.n_seqs)) return;  // a row of no sequence
+    if (row >= n_rows || token < __ldg(a.q_starts) || token >= __ldg(a.q_starts + a.n_seqs) || *a.part_ready == 0) return;  // a row of no sequence
     const float lse = lane < a.parts ? a.part_lse[lane * n_rows + row] : -INFINITY;
     float top = lse;
 #pragma unroll

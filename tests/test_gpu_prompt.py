@@ -215,18 +215,35 @@ def test_many_sequences_and_many_blocks(B):
         p.check(*p.launch())
 
 
-def test_starts_that_descend_or_lie_outside_are_cut_and_reported(B):
-    p = Problem(B, [(50, 50), (60, 60), (70, 70)], 2, 1, 64, seed=1)
+@pytest.mark.parametrize("keys", [70, 3000])
+def test_starts_that_descend_or_lie_outside_are_reported_and_nothing_is_written(B, keys):
+    """With parts (many keys) and without."""
+    p = Problem(B, [(50, 50), (60, 60), (70, keys)], 2, 1, 64, seed=1)
     q, k = p.starts()
+    end = 110 + keys
     B.rt_device_status()
-    for bad_q, bad_k in (([0, 50, 110, 5000], None), ([0, 50, 40, 180], None), ([-5, 50, 110, 180], None), (None, [0, 50, 110, 1 << 30]), (None, [0, 120, 110, 180])):
+    for bad_q, bad_k in (([0, 50, 110, 5000], None), ([0, 50, 40, 180], None), ([-5, 50, 110, 180], None), (None, [0, 50, 110, 1 << 30]), (None, [0, 120, 110, end]),
+                         ([0, 180, 0, 180], None), ([0, 50, 110, -1], None)):
         qs = q if bad_q is None else torch.tensor(bad_q, dtype=torch.int32, device="cuda")
         ks = k if bad_k is None else torch.tensor(bad_k, dtype=torch.int32, device="cuda")
-        out = torch.zeros_like(p.q)
-        B.prompt_attention_launch(B.PromptBatch(qs, 70, ks, 70), p.q, p.k, p.v, out)
+        out, lse = torch.full_like(p.q, 5.0), torch.full(p.q.shape[:2], 5.0, device="cuda")
+        B.prompt_attention_launch(B.PromptBatch(qs, 70, ks, keys), p.q, p.k, p.v, out, lse)
         assert B.rt_device_status() == B.RT_ERR_INDEX
+        assert bool((out == 5.0).all()) and bool((lse == 5.0).all())
     p.check(*p.launch())
     assert B.rt_device_status() == 0
+
+
+def test_bad_starts_among_many_sequences(B):
+    """The one that is wrong is looked up, not kept in a register."""
+    p = Problem(B, [(3, 3)] * 400, 2, 2, 64, seed=1)
+    q, _ = p.starts()
+    for at in (5, 200, 399):
+        bad = q.clone()
+        bad[at] = 1 << 20
+        out = torch.full_like(p.q, 5.0)
+        B.prompt_attention_launch(B.PromptBatch(bad, 3), p.q, p.k, p.v, out)
+        assert B.rt_device_status() == B.RT_ERR_INDEX and bool((out == 5.0).all())
 
 
 def test_streams_graphs_and_workspaces(B):
