@@ -2,6 +2,8 @@
 #include <stddef.h>
 #include <string.h>
 
+#include <atomic>
+
 #include "kv_move_kernels.cuh"
 #include "tuner_internal.h"
 
@@ -109,12 +111,35 @@ CopyKernel copy_kernel(int vb)
 
 typedef void (*CompactKernel)(CompactArgs);
 template <int VB>
-CompactKernel compact_kernel(int row_vectors)
+CompactKernel compact_kernel(int lanes)  // of 32
 {
-    if (row_vectors <= 4) return kv_compact_kernel<VB, 4, 4>;
-    if (row_vectors <= 8) return kv_compact_kernel<VB, 8, 4>;
-    if (row_vectors <= 16) return kv_compact_kernel<VB, 16, 4>;
-    return kv_compact_kernel<VB, 32, 4>;
+    if constexpr (VB < 4) return kv_compact_kernel<VB, 32>;
+    else return lanes == 0 ? kv_compact_kernel<VB, 4> : lanes == 1 ? kv_compact_kernel<VB, 8> : lanes == 2 ? kv_compact_kernel<VB, 16> : kv_compact_kernel<VB, 32>;
+}
+
+// The kernel for accesses of `width` bytes and rows of `row_vectors` of them.  Shared memory beyond the default limit is asked for once per
+// device and kernel.
+int find_compact_kernel(int width, int row_vectors, int kinds, CompactKernel* fn)
+{
+    static std::atomic<unsigned char> done[kDeviceSlots][5][4];
+    const int lanes = row_vectors <= 4 ? 0 : row_vectors <= 8 ? 1 : row_vectors <= 16 ? 2 : 3;
+    switch (width) {
+        case 16: *fn = compact_kernel<16>(lanes); break;
+        case 8: *fn = compact_kernel<8>(lanes); break;
+        case 4: *fn = compact_kernel<4>(lanes); break;
+        case 2: *fn = compact_kernel<2>(lanes); break;
+        default: *fn = compact_kernel<1>(lanes); break;
+    }
+    if (compact_smem(kinds, width) <= 48 * 1024) return RT_OK;
+    int device;
+    const int st = current_device_index(&device);
+    if (st != RT_OK) return st;
+    std::atomic<unsigned char>& mine = done[device][log2_or_minus1((unsigned)width)][lanes];
+    if (!mine.load(std::memory_order_acquire)) {
+        RT_CUDA_OK(cudaFuncSetAttribute((const void*)*fn, cudaFuncAttributeMaxDynamicSharedMemorySize, compact_smem(2, width)));
+        mine.store(1, std::memory_order_release);
+    }
+    return RT_OK;
 }
 
 }  // namespace
@@ -236,15 +261,9 @@ int kv_cache_compact_launch(const rt_kv_cache* caches, int32_t n_caches, const r
     }
     const int width = access_width(a.m, 0, a.m.kind[0].row_bytes, 16), row_vectors = a.m.kind[0].row_bytes / width;
     CompactKernel fn;
-    switch (width) {
-        case 16: fn = compact_kernel<16>(row_vectors); break;
-        case 8: fn = compact_kernel<8>(row_vectors); break;
-        case 4: fn = compact_kernel<4>(row_vectors); break;
-        case 2: fn = kv_compact_kernel<2, 32, 4>; break;
-        default: fn = kv_compact_kernel<1, 32, 4>; break;
-    }
+    if ((st = find_compact_kernel(width, row_vectors, a.m.kinds, &fn)) != RT_OK) return st;
     void* params[] = {&a};
-    return launch_kernel((const void*)fn, dim3((unsigned)ctas), dim3(kMoveThreads), 0, (cudaStream_t)stream, params);
+    return launch_kernel((const void*)fn, dim3((unsigned)ctas), dim3(kMoveThreads), (size_t)compact_smem(a.m.kinds, width), (cudaStream_t)stream, params);
 }
 
 }  // extern "C"

@@ -150,23 +150,53 @@ struct MoveRow {
 constexpr int kMoveTurns = 4;  // tokens of a thread that are looked at together
 constexpr int kMoveChunk = kMoveThreads * kMoveTurns;
 
+constexpr int kMoveStages = 3;    // items of a warp under way
+constexpr int kMoveAccesses = 4;  // accesses of a lane in an item
+constexpr int kMoveScales = 16;   // scales of a thread under way
+
+// Shared memory of a CTA: the lists, of elements and of scales, and the items under way.
+inline int compact_smem(int kinds, int vector_bytes)
+{
+    return kinds * kMoveChunk * (int)sizeof(MoveRow) + (vector_bytes >= 4 ? kMoveThreads * kMoveStages * kMoveAccesses * vector_bytes : 0);
+}
+
+template <int VB>
+__device__ __forceinline__ void cp_async(uint32_t to, const unsigned char* from)
+{
+    if constexpr (VB == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(VB) : "memory");
+}
+template <int VB>
+__device__ __forceinline__ Vec<VB> ld_slot(uint32_t at)
+{
+    Vec<VB> v;
+    if constexpr (VB == 16) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]) : "r"(at) : "memory");
+    else if constexpr (VB == 8) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.w[0]), "=r"(v.w[1]) : "r"(at) : "memory");
+    else asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v.w[0]) : "r"(at) : "memory");
+    return v;
+}
 // CTA: one sequence, some of its tasks (a side of a layer and a head each).  The window goes by in chunks of 1024 tokens: who is
 // kept and where it goes is found with votes and a scan, the places of those that move are listed, and every warp moves the list's
-// rows of its tasks.
+// rows of its tasks, through shared memory (accesses narrower than 4 bytes: through registers).
 //
-// The list ascends and a row never moves up, so nothing that a store overwrites is still to be read once its own batch and those before
-// it are loaded: loads go ahead (the next batch's before this one's stores), stores never do.  No other warp touches a task's rows.
+// The list ascends and a row never moves up, so nothing that a store overwrites is still to be read once its own item and those before
+// it are loaded: loads go ahead, stores never do.  No other warp touches a task's rows.
 //
-// Bound by HBM with many rows, where what counts is how much is under way (2 * U accesses of a lane) and how little is worked out
-// per access: a row's places are bytes in the list, a task's base is found once.  Measured: 12
-// sequences x 8 layers x 8 heads of 128 int8, 1500 rows of each, 608 MB: 145 us, 4.2 TB/s, 0.65 of the copy bandwidth (305 with every access's
-// place worked out from page numbers and the scales moved by one warp).  40 sequences x 32 layers, two or three rows each: 7.4 us in a graph.
-template <int VB, int LANES, int U>
+// Bound by HBM with many rows, where what counts is how much is under way and how little is worked out per access: a row's places are
+// bytes in the list, a task's base is found once, a chunk's first scales are loaded ahead of its elements.  Measured: 12 sequences x 8
+// layers x 8 heads of 128 int8, 1500 rows of each, 608 MB: 124 us, 4.9 TB/s, 0.76 of the copy bandwidth (145 with two items of a warp under
+// way, in registers; 305 with every access's place worked out from page numbers and the scales moved by one warp; chunks of 512 tokens
+// 131, of 2048 139; CTAs of 4 warps 141, of 16 141).  What is left: beginnings and ends of chunks, and sequences of unequal lengths.
+// 40 sequences x 32 layers, two or three rows each: 6.7 us in a graph.
+template <int VB, int LANES>
 __global__ void __launch_bounds__(kMoveThreads, 2) kv_compact_kernel(const __grid_constant__ CompactArgs a)
 {
-    __shared__ MoveRow list[2][kMoveChunk];  // of elements, and of scales
-    constexpr int WARPS = kMoveThreads / 32, ROWS = 32 / LANES;
+    constexpr int WARPS = kMoveThreads / 32, ROWS = 32 / LANES, U = kMoveAccesses;
     __shared__ int warp_count[kMoveTurns][WARPS];
+    extern __shared__ __align__(16) unsigned char shared[];
+    MoveRow(*const list)[kMoveChunk] = reinterpret_cast<MoveRow(*)[kMoveChunk]>(shared);  // of elements, and of scales
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(shared) + (uint32_t)(a.m.kinds * sizeof(MoveRow) * kMoveChunk) +
+                          (threadIdx.x >> 5) * (kMoveStages * U * 32 * VB) + (threadIdx.x & 31) * VB;
     const int seq = (int)(blockIdx.x / (unsigned)a.ctas_per_seq), part = (int)(blockIdx.x - (unsigned)(seq * a.ctas_per_seq));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     wait_for_previous_kernel();
@@ -252,77 +282,113 @@ __global__ void __launch_bounds__(kMoveThreads, 2) kv_compact_kernel(const __gri
         kept_before += chunk_kept;
         __syncthreads();
 
-        // Elements: many rows one task at a time, few rows U tasks at a time.
+        // Elements: many rows one task at a time, few rows U tasks at a time.  An item is U accesses of a lane: TU tasks, BU batches of ROWS
+        // rows.  A warp goes through its items in order, kMoveStages under way.
         const auto move = [&](auto tasks_at_once) {
             constexpr int TU = decltype(tasks_at_once)::value, BU = U / TU;
-            const int batches = (rows + ROWS - 1) / ROWS;
-            for (int task = warp; task < tasks; task += TU * WARPS) {
-                for (int turn = 0; turn < turns; ++turn) {
-                    unsigned char* base[TU];
+            const int batches = (rows + ROWS * BU - 1) / (ROWS * BU);
+            struct Cursor {
+                int task, turn, batch;
+                unsigned char* base[TU];
+            };
+            const auto place = [&](Cursor& c) {
 #pragma unroll
-                    for (int i = 0; i < TU; ++i) {
-                        const int t = first_task + task + i * WARPS, side = t / a.m.heads, head = t - side * a.m.heads, v = turn * LANES + lane % LANES;
-                        base[i] = task + i * WARPS < tasks && v < row_vectors ? a.m.base[0][side] + (long long)head * a.m.kind[0].head_stride + v * VB : nullptr;
-                    }
-                    Vec<VB> x[2][U];
-                    const auto fetch = [&](int buffer, int batch) {
+                for (int i = 0; i < TU; ++i) {
+                    const int t = first_task + c.task + i * WARPS, side = t / a.m.heads, head = t - side * a.m.heads, v = c.turn * LANES + lane % LANES;
+                    c.base[i] = c.task + i * WARPS < tasks && v < row_vectors ? a.m.base[0][side] + (long long)head * a.m.kind[0].head_stride + v * VB : nullptr;
+                }
+            };
+            const auto next = [&](Cursor& c) {
+                if (++c.batch < batches) return;
+                c.batch = 0;
+                if (++c.turn == turns) {
+                    c.turn = 0;
+                    c.task += TU * WARPS;
+                }
+                place(c);
+            };
+            const int items = warp < tasks ? (tasks - warp + TU * WARPS - 1) / (TU * WARPS) * turns * batches : 0;
+            Cursor to = {warp, 0, 0, {}};
+            place(to);
+            if constexpr (VB >= 4) {
+                Cursor from = to;
+                int fetched = 0, slot = 0;
+                const auto fetch = [&](int stage) {
+                    if (fetched < items) {
 #pragma unroll
                         for (int u = 0; u < U; ++u) {
-                            const int r = (batch + u / TU) * ROWS + lane / LANES;
-                            if (base[u % TU] && r < rows) x[buffer][u] = ld_move<VB>(base[u % TU] + list[0][r].src);
+                            const int r = (from.batch * BU + u / TU) * ROWS + lane / LANES;
+                            if (from.base[u % TU] && r < rows) cp_async<VB>(ring + (stage * U + u) * 32 * VB, from.base[u % TU] + list[0][r].src);
                         }
-                    };
-                    const auto store = [&](int buffer, int batch) {
-                        __syncwarp();
-#pragma unroll
-                        for (int u = 0; u < U; ++u) {
-                            const int r = (batch + u / TU) * ROWS + lane / LANES;
-                            if (base[u % TU] && r < rows) st_move<VB>(base[u % TU] + list[0][r].dst, x[buffer][u]);
-                        }
-                        __syncwarp();
-                    };
-                    fetch(0, 0);
-                    for (int b = 0; b < batches; b += 2 * BU) {
-                        fetch(1, b + BU);
-                        store(0, b);
-                        fetch(0, b + 2 * BU);
-                        store(1, b + BU);
+                        ++fetched;
+                        next(from);
                     }
+                    asm volatile("cp.async.commit_group;" ::: "memory");
+                };
+#pragma unroll
+                for (int s = 0; s < kMoveStages; ++s) fetch(s);
+                for (int n = 0; n < items; ++n) {
+                    asm volatile("cp.async.wait_group %0;" ::"n"(kMoveStages - 1) : "memory");
+                    __syncwarp();
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const int r = (to.batch * BU + u / TU) * ROWS + lane / LANES;
+                        if (to.base[u % TU] && r < rows) st_move<VB>(to.base[u % TU] + list[0][r].dst, ld_slot<VB>(ring + (slot * U + u) * 32 * VB));
+                    }
+                    next(to);
+                    fetch(slot);
+                    slot = slot + 1 == kMoveStages ? 0 : slot + 1;
+                }
+            } else {
+                for (int n = 0; n < items; ++n, next(to)) {
+                    Vec<VB> x[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const int r = (to.batch * BU + u / TU) * ROWS + lane / LANES;
+                        if (to.base[u % TU] && r < rows) x[u] = ld_move<VB>(to.base[u % TU] + list[0][r].src);
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const int r = (to.batch * BU + u / TU) * ROWS + lane / LANES;
+                        if (to.base[u % TU] && r < rows) st_move<VB>(to.base[u % TU] + list[0][r].dst, x[u]);
+                    }
+                    __syncwarp();
                 }
             }
         };
+        // Scales: a side's are moved by the CTA that has its first task, all heads by all warps, a batch's loads ahead of its stores; the
+        // first batch's ahead of the elements, which cover their wait.
+        const int values = a.m.kinds == 2 ? rows * a.m.heads : 0;
+        const int first_side = (first_task + a.m.heads - 1) / a.m.heads, last_side = (first_task + tasks - 1) / a.m.heads;
+        uint32_t y[kMoveScales];
+        const auto scale_place = [&](int g, bool to) -> long long {
+            const int r = (int)((unsigned)g / (unsigned)a.m.heads);
+            return (to ? list[1][r].dst : list[1][r].src) + (long long)(g - r * a.m.heads) * a.m.kind[1].head_stride;
+        };
+        const auto fetch_scales = [&](int side, int g0) {
+#pragma unroll
+            for (int e = 0; e < kMoveScales; ++e) {
+                const int g = g0 + e * kMoveThreads + (int)threadIdx.x;
+                if (g < values) y[e] = ld_stream<4>(a.m.base[1][side] + scale_place(g, false)).w[0];
+            }
+        };
+        const auto store_scales = [&](int side, int g0) {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < kMoveScales; ++e) {
+                const int g = g0 + e * kMoveThreads + (int)threadIdx.x;
+                if (g < values) *reinterpret_cast<uint32_t*>(a.m.base[1][side] + scale_place(g, true)) = y[e];
+            }
+        };
+        if (values > 0 && first_side <= last_side) fetch_scales(first_side, 0);
         if (rows > 2 * ROWS) move(std::integral_constant<int, 1>());
         else if (rows > 0) move(std::integral_constant<int, U>());
-        // Scales: a side's are moved by the CTA that has its first task, all heads by all warps, a batch's loads ahead of its stores.
-        if (a.m.kinds == 2 && rows > 0) {
-            const int first_side = (first_task + a.m.heads - 1) / a.m.heads, last_side = (first_task + tasks - 1) / a.m.heads;
-            constexpr int E = 4;
-            const int values = rows * a.m.heads;
-            for (int side = first_side; side <= last_side; ++side) {
-                unsigned char* base = a.m.base[1][side];
-                for (int g0 = 0; g0 < values; g0 += kMoveThreads * E) {
-                    uint32_t y[E];
-                    long long where[E];
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const int g = g0 + e * kMoveThreads + (int)threadIdx.x;
-                        where[e] = -1;
-                        if (g < values) {
-                            const int r = (int)((unsigned)g / (unsigned)a.m.heads);
-                            const MoveRow m = list[1][r];
-                            const long long head = (long long)(g - r * a.m.heads) * a.m.kind[1].head_stride;
-                            y[e] = ld_stream<4>(base + m.src + head).w[0];
-                            where[e] = m.dst + head;
-                        }
-                    }
-                    __syncthreads();
-#pragma unroll
-                    for (int e = 0; e < E; ++e)
-                        if (where[e] >= 0) *reinterpret_cast<uint32_t*>(base + where[e]) = y[e];
-                    __syncthreads();
-                }
+        for (int side = first_side; side <= last_side; ++side)
+            for (int g0 = 0; g0 < values; g0 += kMoveThreads * kMoveScales) {
+                if (side != first_side || g0 != 0) fetch_scales(side, g0);
+                store_scales(side, g0);
             }
-        }
     }
     if (part == 0 && threadIdx.x == 0) a.new_lens[seq] = start + kept_before;
 }
