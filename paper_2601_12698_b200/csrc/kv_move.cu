@@ -228,8 +228,10 @@ int kv_cache_compact_launch(const rt_kv_cache* caches, int32_t n_caches, const r
         set_error("page_table, starts, lens or new_lens is not aligned to its element size");
         return RT_ERR_ALIGN;
     }
-    if (b->new_lens == b->lens || b->new_lens == b->starts) {
-        set_error("new_lens must not be one of the inputs");
+    // (every CTA of a sequence reads its start and length, one writes the new length)
+    const uint64_t own = (uint64_t)b->n_seqs * 4, to_lens = (uintptr_t)b->new_lens - (uintptr_t)b->lens, to_starts = (uintptr_t)b->new_lens - (uintptr_t)b->starts;
+    if (to_lens < own || 0 - to_lens < own || to_starts < own || 0 - to_starts < own) {
+        set_error("new_lens must not overlap the inputs");
         return RT_ERR_SHAPE;
     }
     a.m.status = device_status_word();

@@ -139,6 +139,12 @@ def test_gaps_are_closed(B, layers, layout, page, heads, dim, dtype, fmt, seqs, 
     assert B.rt_device_status() == 0
 
 
+@pytest.mark.parametrize("layers,layout,page,heads,dim,dtype,fmt", SHAPES)
+def test_gaps_are_closed_in_long_windows(B, layers, layout, page, heads, dim, dtype, fmt):
+    """Windows of several thousand tokens, which go by in pieces."""
+    test_gaps_are_closed(B, layers, layout, page, heads, dim, dtype, fmt, 2, 2600, 0.7)
+
+
 def test_a_wide_layer_stack_is_compacted_by_many_ctas(B):
     stack, _ = _stack(B, 40, "token", 30, 16, 8, 128, "bf16", "int8")
     g = torch.Generator().manual_seed(5)

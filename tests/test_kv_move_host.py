@@ -53,3 +53,8 @@ def test_nothing_to_do_is_no_error():
     assert _copy(src=None, dst=None, n=0) == B.RT_OK
     assert _compact(table=None, starts=None, lens=None, keep=None, new_lens=None, n=0) == B.RT_OK
     assert B.lib.kv_cache_compact_launch(*_array(_cache()), None, None) == B.RT_ERR_NULL
+
+
+@pytest.mark.parametrize("at", [P + 4, P - 8, P + 60, P + 72, P + 56])
+def test_new_lengths_that_overlap_the_inputs_are_refused(at):
+    assert _compact(new_lens=at) == B.RT_ERR_SHAPE and "overlap" in B.lib.rt_last_error().decode()
