@@ -60,6 +60,8 @@ struct PromptArgs {
     float score_scale;  // softmax_scale * log2(e)
     const unsigned char* v;
     long long v_token_stride, v_head_stride;  // bytes
+    const unsigned char* q;  // (heads of more than 128)
+    long long q_token_stride, q_head_stride;
     void* out;        // [token][head][dim]
     float* lse;       // [token][head] or NULL
     float* part_out;  // parts > 1: [part][token][head][dim], normalised
@@ -96,9 +98,9 @@ struct PromptShape {
     static constexpr int kSlotBlocks = DP == 128 ? 2 : 1;
     static constexpr int kUnits = kBlocks / kSlotBlocks;  // slots of a tile
     static constexpr int kSlotBytes = kSlotBlocks * kBlockBytes;
-    static constexpr int kSlots = 10 / kSlotBlocks;
+    static constexpr int kSlots = kSharedRows ? 12 : 10 / kSlotBlocks;
     static constexpr int kQueryBytes = kBlocks * kBlockBytes;  // of one stream
-    static constexpr int kQueries = DP == 256 ? 1 : 2;
+    static constexpr int kQueries = kSharedRows ? 0 : 2;       // tiles of queries in shared memory
     static constexpr size_t kRingAt = (size_t)kQueries * kQueryBytes;
     static constexpr size_t kSmem = kRingAt + (size_t)kSlots * kSlotBytes + 1024;  // 1024: alignment of the tiles
     static constexpr int kSoftmaxRegs = 160;  // of 2 * 128 for a softmax thread and one of another role
@@ -280,6 +282,9 @@ struct PromptOrder {
     }
 };
 
+// Where heads of more than 128 have the queries' dims 64 b .. 64 b + 63 in tensor memory: behind the 64 columns of each stream's scores.
+__device__ __forceinline__ constexpr uint32_t query_column(int b) { return 64 + b / 2 * kPromptTile + b % 2 * 32; }
+
 template <typename T, int DP>
 __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
                                                                             const __grid_constant__ CUtensorMap v_map, const __grid_constant__ PromptArgs a)
@@ -295,7 +300,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
     unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     unsigned char* ring = smem + S::kRingAt;
     __shared__ __align__(8) uint64_t full[S::kSlots], empty[S::kSlots], item_full[kPromptItems], item_free[kPromptItems], landed[kPromptLanded], q_full, q_free, s_full[2][2],
-        p_full[2][2], o_done[2], o_full[2], sums_full[2], drained[2];
+        p_full[2][2], o_done[2], o_full[2], sums_full[2], results_read, drained[2];
     __shared__ PromptItem items[kPromptItems];
     __shared__ uint32_t tmem_base;
     __shared__ float row_reference[kSharedRows ? kPromptTile : 1], row_sum[kSharedRows ? kPromptTile : 1];  // what streams that share rows tell one another
@@ -306,7 +311,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         mbarrier_init(&empty[tid], kSharedRows ? 1 : 2);
     } else if (tid >= 32 && tid < 32 + kPromptItems) {
         mbarrier_init(&item_full[tid - 32], 1);
-        mbarrier_init(&item_free[tid - 32], kSharedRows ? 14 : 15);  // warps that read it: 8 softmax, 4 looking, 1 or 2 issuing, 1 fetching
+        mbarrier_init(&item_free[tid - 32], 15);  // warps that read it: 8 softmax, 4 looking, 2 issuing, 1 fetching
         items[tid - 32].valid = 0;
     } else if (tid >= 64 && tid < 66) {
         const int i = tid - 64;
@@ -320,13 +325,14 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
     } else if (tid >= 96 && tid < 96 + kPromptLanded) {
         mbarrier_init(&landed[tid - 96], 1);
     } else if (tid == 127) {
-        mbarrier_init(&q_full, 1);
+        mbarrier_init(&q_full, kSharedRows ? 128 : 1);
         mbarrier_init(&q_free, kSharedRows ? 1 : 2);
         mbarrier_init(&sums_full[0], 128);
         mbarrier_init(&sums_full[1], 128);
+        mbarrier_init(&results_read, 128);
     } else if (tid >= 128 && tid < 131) {
-        const CUtensorMap* map = tid == 128 ? &q_map : tid == 129 ? &k_map : &v_map;
-        asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+        const CUtensorMap* map = tid == 128 ? &k_map : tid == 129 ? &v_map : &q_map;
+        if (!kSharedRows || tid < 130) asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
     }
     if (warp == 12) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_base)) : "memory");
@@ -520,7 +526,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
 
             // the item's rows
             if (my_tiles > 0) {
-                wait(&o_full[s], results_done & 1);
+                wait(&o_full[kSharedRows ? 0 : s], results_done & 1);
                 tc_fence_after();
                 if constexpr (kSharedRows) {
                     const float known = m;
@@ -609,6 +615,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                 }
             }
             tc_fence_before();  // the output's columns have been read before the next item's weights are announced
+            if (kSharedRows && s == 1 && my_tiles > 0) mbarrier_arrive(&results_read);  // (the first weights are the first stream's)
             done_with_item(n);
         }
     } else {
@@ -620,8 +627,38 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         const int p = tid - 256;  // the tile's key
         constexpr uint32_t kExponent = std::is_same<T, __nv_bfloat16>::value ? 0x7F807F80u : 0x7C007C00u;
         uint32_t tiles_before = 0, looked_at = 0;  // (tiles that every row sees go past these warps: a barrier of their own tells them of the others)
+        uint32_t items_before = 0;
         PromptItem item;
         for (int n = 0; next_item(n, item); ++n) {
+            if constexpr (kSharedRows) {
+                if (item.tile1 > item.tile0) {  // the item's queries, as soon as the last item's scores are done
+                    const int token = p * a.group_inverse >> 16, head = p - token * a.group;
+                    const bool there = token < a.stream_tokens && token < item.tokens;
+                    const unsigned char* from = a.q + (long long)(item.q_row + token) * a.q_token_stride + (long long)(item.kv_head * a.group + head) * a.q_head_stride;
+                    wait(&q_free, (items_before & 1) ^ 1);
+                    tc_fence_after();
+                    ++items_before;
+#pragma unroll 2
+                    for (int b = 0; b < kBlocks; ++b) {
+                        uint32_t x[2][16];
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) {
+                            uint4 y = make_uint4(0, 0, 0, 0);
+                            if (there && b * 64 + u * 8 < a.dim) y = __ldg(reinterpret_cast<const uint4*>(from + b * 128 + u * 16));
+                            x[u / 4][u % 4 * 4] = y.x;
+                            x[u / 4][u % 4 * 4 + 1] = y.y;
+                            x[u / 4][u % 4 * 4 + 2] = y.z;
+                            x[u / 4][u % 4 * 4 + 3] = y.w;
+                        }
+                        const uint32_t to = tmem + ((uint32_t)(warp & 3) << 21) + query_column(b);
+                        tmem_store16(to, x[0]);
+                        tmem_store16(to + 16, x[1]);
+                    }
+                    tmem_wait_store();
+                    tc_fence_before();
+                    mbarrier_arrive(&q_full);
+                }
+            }
             for (int tile = max(item.tile0, item.masked_from); tile < item.tile1; ++tile) {
                 bool found = false;
                 wait(&landed[looked_at % kPromptLanded], (looked_at / kPromptLanded) & 1);
@@ -656,59 +693,75 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         }
     }
     if constexpr (kSharedRows) {
-        if (warp == 12) {
-            // ---- the warp that issues the products of both streams ----
-            constexpr uint64_t kRowsLayout = tc_layout(16, 1024), kColsLayout = tc_layout(S::kValueRows * 128, 1024);
-            constexpr uint32_t kSlot16 = S::kSlotBytes / 16;
-            const uint64_t q_at = tc_descriptor(kRowsLayout, smem_u32(smem) >> 4);
-            const uint64_t k_base = tc_descriptor(kRowsLayout, smem_u32(ring) >> 4), v_base = tc_descriptor(kColsLayout, smem_u32(ring) >> 4);
-            const int steps = (a.dim + 15) / 16;  // of 16 dims
-            const uint32_t out_idesc = tc_instruction<T>(steps * 16, false, true);
-            uint32_t tiles_before = 0, items_before = 0;
-            auto wait_unit = [&](uint32_t unit) {
-                wait(&full[unit % S::kSlots], (unit / S::kSlots) & 1);
-                tc_fence_after();
-            };
-            PromptItem item;
+        // ---- warps that issue the products of both streams: one the scores', one the outputs' ----
+        // (One warp for both kinds spent more time issuing than the tensor cores computing: 4096 tokens, 32 heads on 4 of 256: 307 us.)
+        // A tile's keys, and its values, are four slots in a row, of a ring of three times four.
+        constexpr uint32_t kQuads = S::kSlots / 4, kSlot16 = S::kSlotBytes / 16;
+        static_assert(!kSharedRows || (S::kSlots % 4 == 0 && kUnits == 4), "a tile of keys or values is four slots in a row");
+        const int steps = (a.dim + 15) / 16;  // of 16 dims
+        uint32_t tiles_before = 0, items_before = 0, quad = 0, lap = 0;
+        const auto next_quads = [&]() {  // the next tile's
+            quad += 2;
+            if (quad >= kQuads) {
+                quad -= kQuads;
+                lap ^= 1;
+            }
+        };
+        PromptItem item;
+        if (warp == 13) {
+            const uint64_t k_base = tc_descriptor(tc_layout(16, 1024), smem_u32(ring) >> 4);
             for (int n = 0; next_item(n, item); ++n) {
                 const int tiles = item.tile1 - item.tile0;
                 if (tiles > 0) {
                     wait(&q_full, items_before & 1);
-                    tc_fence_after();
                     ++items_before;
                 }
-                // S = Q K^T of stream s with its keys of the item's tile number i
-                auto scores = [&](int i, int s) {
-                    const uint32_t unit = 2 * (tiles_before + i) * kUnits;
+                for (int i = 0; i < tiles; ++i) {
+                    // S = Q K^T with each stream's keys, as soon as its weights of the tile before, which lie where they go, have been used
+                    const uint64_t k_at = k_base + quad * 4 * kSlot16;
 #pragma unroll
-                    for (int b = 0; b < kBlocks; ++b) {
-                        const uint32_t slot = (unit + b) % S::kSlots;
-                        if (s == 0) wait_unit(unit + b);
-                        if (elect_one()) {
+                    for (int s = 0; s < 2; ++s) {
+                        if (tiles_before + i > 0) wait(&o_done[s], (tiles_before + i - 1) & 1);
 #pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                if (b * 4 + k < steps)
-                                    tc_mma_ss(tmem + s * kPromptTile, q_at + (b * (S::kBlockBytes / 16) + k * 2), k_base + (slot * kSlot16 + k * 2 + s * (64 * 128 / 16)), kScoreIdesc, b + k > 0);
-                            if (s == 1) tc_commit(&empty[slot]);
-                            if (b == kBlocks - 1) {
-                                tc_commit(&s_full[s][0]);
-                                if (s == 1 && i + 1 == tiles) tc_commit(&q_free);
+                        for (int b = 0; b < kBlocks; ++b) {
+                            if (s == 0) wait(&full[quad * 4 + b], lap);
+                            if (s == 0 || b == 0) tc_fence_after();
+                            if (elect_one()) {
+#pragma unroll
+                                for (int k = 0; k < 4; ++k)
+                                    if (b * 4 + k < steps)
+                                        tc_mma_ts(tmem + s * kPromptTile, tmem + query_column(b) + k * 8, k_at + (b * kSlot16 + k * 2 + s * (64 * 128 / 16)), kScoreIdesc, b + k > 0);
+                                if (s == 1 && b % 2 == 1) tc_commit(&empty[quad * 4 + b - 1]);
+                                if (b == kBlocks - 1) {
+                                    tc_commit(&s_full[s][0]);
+                                    if (s == 1 && i + 1 == tiles) tc_commit(&q_free);
+                                }
                             }
+                            __syncwarp();
                         }
-                        __syncwarp();
                     }
-                };
+                    next_quads();
+                }
+                tiles_before += tiles;
+                done_with_item(n);
+            }
+        } else if (warp == 12) {
+            const uint64_t v_base = tc_descriptor(tc_layout(S::kValueRows * 128, 1024), smem_u32(ring) >> 4);
+            const uint32_t out_idesc = tc_instruction<T>(steps * 16, false, true);
+            quad = 1;
+            for (int n = 0; next_item(n, item); ++n) {
+                const int tiles = item.tile1 - item.tile0;
                 if (tiles > 0) {
-                    scores(0, 0);
-                    scores(0, 1);
+                    wait(&results_read, (items_before & 1) ^ 1);  // the second stream's of the item before
+                    ++items_before;
                 }
                 for (int i = 0; i < tiles; ++i) {
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
                         // O += W V with the stream's values: two slots, side by side
-                        const uint32_t unit = (2 * (tiles_before + i) + 1) * kUnits + 2 * s, slot = unit % S::kSlots;
-                        wait_unit(unit);
-                        wait_unit(unit + 1);
+                        const uint32_t slot = quad * 4 + 2 * s;
+                        wait(&full[slot], lap);
+                        wait(&full[slot + 1], lap);
                         wait(&p_full[s][0], (tiles_before + i) & 1);
                         tc_fence_after();
                         if (elect_one()) {
@@ -717,23 +770,21 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                                 tc_mma_ts(tmem + kColO, tmem + s * kPromptTile + k * 8, v_base + (slot * kSlot16 + k * 128), out_idesc, i + s + k > 0);
                             tc_commit(&o_done[s]);
                             tc_commit(&empty[slot]);
-                            tc_commit(&empty[slot + 1]);
-                            if (s == 1 && i + 1 == tiles) {
-                                tc_commit(&o_full[0]);
-                                tc_commit(&o_full[1]);
-                            }
+                            if (s == 1 && i + 1 == tiles) tc_commit(&o_full[0]);
                         }
                         __syncwarp();
-                        if (i + 1 < tiles) scores(i + 1, s);
                     }
+                    next_quads();
                 }
                 tiles_before += tiles;
                 done_with_item(n);
             }
-            // the tensor memory is given back only when nothing writes it any more
-            if (elect_one()) tc_commit(&drained[0]);
+        }
+        // the tensor memory is given back only when nothing writes it any more
+        if (warp == 12 || warp == 13) {
+            if (elect_one()) tc_commit(&drained[warp - 12]);
             __syncwarp();
-            ok = mbarrier_wait_sleeping(&drained[0], 0) && ok;
+            ok = mbarrier_wait_sleeping(&drained[warp - 12], 0) && ok;
         }
     } else if (warp >= 12 && warp < 14) {
         // ---- warps that issue the products of the two streams ----
@@ -840,7 +891,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
 #pragma unroll
             for (int u = 0; u < kUnits; ++u) {
                 const uint32_t slot = units % S::kSlots;
-                wait(&empty[slot], ((units / S::kSlots) & 1) ^ 1);
+                if (!kSharedRows || u % 2 == 0) wait(&empty[slot], ((units / S::kSlots) & 1) ^ 1);  // (heads of more than 128: two slots at a time)
                 if (!a.drop_copies && elect_one()) {
                     if (!bar) mbarrier_expect_tx(&full[slot], S::kSlotBytes);
                     else if (u == 0) mbarrier_expect_tx(bar, S::kSlotBytes * kUnits);
@@ -860,7 +911,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         PromptItem item;
         for (int n = 0; next_item(n, item); ++n) {
             const int tiles = item.tile1 - item.tile0;
-            if (tiles > 0) {
+            if (!kSharedRows && tiles > 0) {
                 wait(&q_free, (items_before & 1) ^ 1);
                 if (!a.drop_copies && elect_one()) {
                     mbarrier_expect_tx(&q_full, query_bytes * S::kQueries);
@@ -871,9 +922,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                             tma_load_3d(smem + s * S::kQueryBytes + b * S::kBlockBytes, &q_map, b * 64, item.kv_head * a.group, item.q_row + s * a.stream_tokens, &q_full);
                 }
                 __syncwarp();
-                posted = !a.drop_copies;
                 ++items_before;
             }
+            posted = posted || (tiles > 0 && !a.drop_copies);
             for (int i = 0; i < tiles; ++i) {
                 const int row = item.k_row + (item.tile0 + i) * kPromptTile;
                 fetch(&k_map, item.kv_head, row, nullptr, false);
@@ -887,7 +938,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         if (posted) {
             for (uint32_t m = looks > kPromptLanded ? looks - kPromptLanded : 0; m < looks; ++m)
                 ok = mbarrier_wait_sleeping(&landed[m % kPromptLanded], (m / kPromptLanded) & 1) && ok;
-            ok = mbarrier_wait_sleeping(&q_full, (items_before - 1) & 1) && ok;
+            if (!kSharedRows) ok = mbarrier_wait_sleeping(&q_full, (items_before - 1) & 1) && ok;
             for (uint32_t u = units > S::kSlots ? units - S::kSlots : 0; u < units; ++u) ok = mbarrier_wait_sleeping(&full[u % S::kSlots], (u / S::kSlots) & 1) && ok;
         }
     } else if (warp == 15) {
