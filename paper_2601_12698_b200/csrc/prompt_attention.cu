@@ -209,9 +209,6 @@ int prompt_attention_launch(const rt_prompt_batch* b, const void* q, int64_t q_t
     a.v = (const unsigned char*)v;
     a.v_token_stride = v_token_stride * 2;
     a.v_head_stride = kv_heads > 1 ? v_head_stride * 2 : 0;
-    a.q = (const unsigned char*)q;
-    a.q_token_stride = b->q_tokens > 1 ? q_token_stride * 2 : 0;
-    a.q_head_stride = q_heads > 1 ? q_head_stride * 2 : 0;
     a.out = out;
     a.lse = lse;
     if (p.parts > 1) {

@@ -60,8 +60,6 @@ struct PromptArgs {
     float score_scale;  // softmax_scale * log2(e)
     const unsigned char* v;
     long long v_token_stride, v_head_stride;  // bytes
-    const unsigned char* q;  // (heads of more than 128)
-    long long q_token_stride, q_head_stride;
     void* out;        // [token][head][dim]
     float* lse;       // [token][head] or NULL
     float* part_out;  // parts > 1: [part][token][head][dim], normalised
@@ -98,9 +96,9 @@ struct PromptShape {
     static constexpr int kSlotBlocks = DP == 128 ? 2 : 1;
     static constexpr int kUnits = kBlocks / kSlotBlocks;  // slots of a tile
     static constexpr int kSlotBytes = kSlotBlocks * kBlockBytes;
-    static constexpr int kSlots = kSharedRows ? 12 : 10 / kSlotBlocks;
+    static constexpr int kSlots = 10 / kSlotBlocks;
     static constexpr int kQueryBytes = kBlocks * kBlockBytes;  // of one stream
-    static constexpr int kQueries = kSharedRows ? 0 : 2;       // tiles of queries in shared memory
+    static constexpr int kQueries = kSharedRows ? 1 : 2;
     static constexpr size_t kRingAt = (size_t)kQueries * kQueryBytes;
     static constexpr size_t kSmem = kRingAt + (size_t)kSlots * kSlotBytes + 1024;  // 1024: alignment of the tiles
     static constexpr int kSoftmaxRegs = 160;  // of 2 * 128 for a softmax thread and one of another role
@@ -282,9 +280,6 @@ struct PromptOrder {
     }
 };
 
-// Where heads of more than 128 have the queries' dims 64 b .. 64 b + 63 in tensor memory: behind the 64 columns of each stream's scores.
-__device__ __forceinline__ constexpr uint32_t query_column(int b) { return 64 + b / 2 * kPromptTile + b % 2 * 32; }
-
 template <typename T, int DP>
 __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
                                                                             const __grid_constant__ CUtensorMap v_map, const __grid_constant__ PromptArgs a)
@@ -300,7 +295,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
     unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     unsigned char* ring = smem + S::kRingAt;
     __shared__ __align__(8) uint64_t full[S::kSlots], empty[S::kSlots], item_full[kPromptItems], item_free[kPromptItems], landed[kPromptLanded], q_full, q_free, s_full[2][2],
-        p_full[2][2], o_done[2], o_full[2], sums_full[2], results_read, drained[2];
+        p_full[2][2], o_done[2][2], o_full[2], sums_full[2], results_read, drained[2];
     __shared__ PromptItem items[kPromptItems];
     __shared__ uint32_t tmem_base;
     __shared__ float row_reference[kSharedRows ? kPromptTile : 1], row_sum[kSharedRows ? kPromptTile : 1];  // what streams that share rows tell one another
@@ -319,20 +314,21 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         mbarrier_init(&s_full[i][1], 1);
         mbarrier_init(&p_full[i][0], 128);
         mbarrier_init(&p_full[i][1], 128);
-        mbarrier_init(&o_done[i], 1);
+        mbarrier_init(&o_done[i][0], 1);
+        mbarrier_init(&o_done[i][1], 1);
         mbarrier_init(&o_full[i], 1);
         mbarrier_init(&drained[i], 1);
     } else if (tid >= 96 && tid < 96 + kPromptLanded) {
         mbarrier_init(&landed[tid - 96], 1);
     } else if (tid == 127) {
-        mbarrier_init(&q_full, kSharedRows ? 128 : 1);
+        mbarrier_init(&q_full, 1);
         mbarrier_init(&q_free, kSharedRows ? 1 : 2);
         mbarrier_init(&sums_full[0], 128);
         mbarrier_init(&sums_full[1], 128);
         mbarrier_init(&results_read, 128);
     } else if (tid >= 128 && tid < 131) {
         const CUtensorMap* map = tid == 128 ? &k_map : tid == 129 ? &v_map : &q_map;
-        if (!kSharedRows || tid < 130) asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
     }
     if (warp == 12) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_base)) : "memory");
@@ -404,16 +400,17 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                     if (k > seen) v[k] = 0xFF800000u;
             };
             if (kSharedRows && s == 1 && my_tiles > 0) {  // its first reference is what the first stream has found
-                wait(&p_full[0][0], tiles_done & 1);
+                wait(&p_full[0][tiles_done & 1], (tiles_done >> 1) & 1);
                 m = *const_cast<volatile float*>(&row_reference[r]);
             } else if (my_tiles > 0) {  // the row's first scores give it its first reference
-                wait(&s_full[s][0], tiles_done & 1);
+                const int buffer = kSharedRows ? tiles_done & 1 : 0;
+                wait(&s_full[s][buffer], (kSharedRows ? tiles_done >> 1 : tiles_done) & 1);
                 tc_fence_after();
                 float top = -INFINITY;
 #pragma unroll 1
                 for (int q = 0; q < 2; ++q) {
                     uint32_t v[32];
-                    tmem_load32(s_col + q * 32, v);
+                    tmem_load32(s_col + buffer * 64 + q * 32, v);
                     tmem_wait_load(v);
                     if (item.tile0 >= item.masked_from) hide(v, last - item.tile0 * kPromptTile - q * 32);
 #pragma unroll
@@ -431,9 +428,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                 // exponentiated.
 #pragma unroll 1
                 for (int h = 0; h < kHalves; ++h) {
-                    wait(&s_full[s][h], count & 1);
+                    const int buffer = kSharedRows ? count & 1 : h;  // of the stream's two
+                    wait(&s_full[s][buffer], (kSharedRows ? count >> 1 : count) & 1);
                     tc_fence_after();
-                    const uint32_t col = s_col + h * 64;
+                    const uint32_t col = s_col + buffer * 64;
                     // One pass over the row's 64 scores gives their maximum and, with the reference as it is, the weights and their sum.
                     // Only when the maximum turns out to be more than 8 above the reference is the pass made again, with a reference
                     // that has been moved there; the scores are still in tensor memory, the weights go over them at the end.
@@ -482,8 +480,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                         if (settled) break;
                         float known = m;
                         if constexpr (kSharedRows) {  // the weights before these have been announced: the reference is what they left
-                            if (s == 1) wait(&p_full[0][0], count & 1);
-                            else if (i > 0) wait(&p_full[1][0], (count - 1) & 1);
+                            if (s == 1) wait(&p_full[0][count & 1], (count >> 1) & 1);
+                            else if (i > 0) wait(&p_full[1][(count - 1) & 1], ((count - 1) >> 1) & 1);
                             m = *const_cast<volatile float*>(&row_reference[r]);
                         }
                         const bool move = top > m + 8.f;
@@ -492,9 +490,13 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                         if (!kSharedRows || __any_sync(0xFFFFFFFFu, move)) {
                             const float alpha = move ? ex2(m - top) : 1.f;
                             if (i + h + (kSharedRows ? s : 0) > 0) {  // the products so far are complete before they are rescaled
-                                // (The phase before that one is complete: scores come behind the products of the tile before.)
-                                if constexpr (kSharedRows) wait(&o_done[s ^ 1], (s == 1 ? count : count - 1) & 1);
-                                else wait(&o_done[s], (2 * count + h - 1) & 1);
+                                // (The phase before that one is complete: the scores came behind the products whose weights they replaced.)
+                                if constexpr (kSharedRows) {
+                                    const uint32_t last = s == 1 ? count : count - 1;  // tile of the other stream's last weights
+                                    wait(&o_done[s ^ 1][last & 1], (last >> 1) & 1);
+                                } else {
+                                    wait(&o_done[s][0], (2 * count + h - 1) & 1);
+                                }
                                 tc_fence_after();
 #pragma unroll 1
                                 for (int q = 0; q < (kSharedRows ? DP : S::kCols) / 16; ++q) {
@@ -519,7 +521,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                     l += part_sum[0] + part_sum[1];
                     tmem_wait_store();
                     tc_fence_before();
-                    mbarrier_arrive(&p_full[s][h]);
+                    mbarrier_arrive(&p_full[s][buffer]);
                 }
             }
             tiles_done += my_tiles;
@@ -627,38 +629,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         const int p = tid - 256;  // the tile's key
         constexpr uint32_t kExponent = std::is_same<T, __nv_bfloat16>::value ? 0x7F807F80u : 0x7C007C00u;
         uint32_t tiles_before = 0, looked_at = 0;  // (tiles that every row sees go past these warps: a barrier of their own tells them of the others)
-        uint32_t items_before = 0;
         PromptItem item;
         for (int n = 0; next_item(n, item); ++n) {
-            if constexpr (kSharedRows) {
-                if (item.tile1 > item.tile0) {  // the item's queries, as soon as the last item's scores are done
-                    const int token = p * a.group_inverse >> 16, head = p - token * a.group;
-                    const bool there = token < a.stream_tokens && token < item.tokens;
-                    const unsigned char* from = a.q + (long long)(item.q_row + token) * a.q_token_stride + (long long)(item.kv_head * a.group + head) * a.q_head_stride;
-                    wait(&q_free, (items_before & 1) ^ 1);
-                    tc_fence_after();
-                    ++items_before;
-#pragma unroll 2
-                    for (int b = 0; b < kBlocks; ++b) {
-                        uint32_t x[2][16];
-#pragma unroll
-                        for (int u = 0; u < 8; ++u) {
-                            uint4 y = make_uint4(0, 0, 0, 0);
-                            if (there && b * 64 + u * 8 < a.dim) y = __ldg(reinterpret_cast<const uint4*>(from + b * 128 + u * 16));
-                            x[u / 4][u % 4 * 4] = y.x;
-                            x[u / 4][u % 4 * 4 + 1] = y.y;
-                            x[u / 4][u % 4 * 4 + 2] = y.z;
-                            x[u / 4][u % 4 * 4 + 3] = y.w;
-                        }
-                        const uint32_t to = tmem + ((uint32_t)(warp & 3) << 21) + query_column(b);
-                        tmem_store16(to, x[0]);
-                        tmem_store16(to + 16, x[1]);
-                    }
-                    tmem_wait_store();
-                    tc_fence_before();
-                    mbarrier_arrive(&q_full);
-                }
-            }
             for (int tile = max(item.tile0, item.masked_from); tile < item.tile1; ++tile) {
                 bool found = false;
                 wait(&landed[looked_at % kPromptLanded], (looked_at / kPromptLanded) & 1);
@@ -694,22 +666,23 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
     }
     if constexpr (kSharedRows) {
         // ---- warps that issue the products of both streams: one the scores', one the outputs' ----
-        // (One warp for both kinds spent more time issuing than the tensor cores computing: 4096 tokens, 32 heads on 4 of 256: 307 us.)
-        // A tile's keys, and its values, are four slots in a row, of a ring of three times four.
-        constexpr uint32_t kQuads = S::kSlots / 4, kSlot16 = S::kSlotBytes / 16;
-        static_assert(!kSharedRows || (S::kSlots % 4 == 0 && kUnits == 4), "a tile of keys or values is four slots in a row");
+        // The scores have two buffers a stream, which the tiles take in turn, so that they are there when the softmax comes to them.
+        // (4096 tokens, 32 heads on 4 of 256: one buffer and one warp for both kinds of products, which spent more time issuing than the tensor
+        // cores computing, 307 us; two warps 279.)
+        // The ring goes by in pairs of slots: two of a tile's keys, then one of each stream's values.
+        constexpr uint32_t kPairs = S::kSlots / 2, kSlot16 = S::kSlotBytes / 16;
+        static_assert(!kSharedRows || (S::kSlots % 2 == 0 && kUnits == 4), "a tile of keys or values is two pairs of slots");
         const int steps = (a.dim + 15) / 16;  // of 16 dims
-        uint32_t tiles_before = 0, items_before = 0, quad = 0, lap = 0;
-        const auto next_quads = [&]() {  // the next tile's
-            quad += 2;
-            if (quad >= kQuads) {
-                quad -= kQuads;
+        uint32_t tiles_before = 0, items_before = 0, pair = 0, lap = 0;
+        const auto next_pair = [&]() {
+            if (++pair == kPairs) {
+                pair = 0;
                 lap ^= 1;
             }
         };
         PromptItem item;
         if (warp == 13) {
-            const uint64_t k_base = tc_descriptor(tc_layout(16, 1024), smem_u32(ring) >> 4);
+            const uint64_t q_at = tc_descriptor(tc_layout(16, 1024), smem_u32(smem) >> 4), k_base = tc_descriptor(tc_layout(16, 1024), smem_u32(ring) >> 4);
             for (int n = 0; next_item(n, item); ++n) {
                 const int tiles = item.tile1 - item.tile0;
                 if (tiles > 0) {
@@ -717,30 +690,37 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                     ++items_before;
                 }
                 for (int i = 0; i < tiles; ++i) {
-                    // S = Q K^T with each stream's keys, as soon as its weights of the tile before, which lie where they go, have been used
-                    const uint64_t k_at = k_base + quad * 4 * kSlot16;
+                    // S = Q K^T with each stream's keys, as soon as the weights that lie where they go have been used
+                    const uint32_t count = tiles_before + i, buffer = count & 1;
+                    uint32_t slot[2];
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
-                        if (tiles_before + i > 0) wait(&o_done[s], (tiles_before + i - 1) & 1);
+                        if (count >= 2) wait(&o_done[s][buffer], ((count >> 1) - 1) & 1);
+                        tc_fence_after();
 #pragma unroll
                         for (int b = 0; b < kBlocks; ++b) {
-                            if (s == 0) wait(&full[quad * 4 + b], lap);
-                            if (s == 0 || b == 0) tc_fence_after();
+                            if (s == 0) {
+                                if (b % 2 == 0) slot[b / 2 % 2] = 2 * pair;
+                                wait(&full[2 * pair + b % 2], lap);
+                                if (b % 2 == 1) next_pair();
+                                tc_fence_after();
+                            }
                             if (elect_one()) {
+                                const uint64_t k_at = k_base + (slot[b / 2 % 2] + b % 2) * kSlot16 + s * (64 * 128 / 16);
 #pragma unroll
                                 for (int k = 0; k < 4; ++k)
-                                    if (b * 4 + k < steps)
-                                        tc_mma_ts(tmem + s * kPromptTile, tmem + query_column(b) + k * 8, k_at + (b * kSlot16 + k * 2 + s * (64 * 128 / 16)), kScoreIdesc, b + k > 0);
-                                if (s == 1 && b % 2 == 1) tc_commit(&empty[quad * 4 + b - 1]);
+                                    if (b * 4 + k < steps) tc_mma_ss(tmem + s * kPromptTile + buffer * 64, q_at + (b * (S::kBlockBytes / 16) + k * 2), k_at + k * 2, kScoreIdesc, b + k > 0);
+                                if (s == 1 && b % 2 == 1) tc_commit(&empty[slot[b / 2 % 2]]);
                                 if (b == kBlocks - 1) {
-                                    tc_commit(&s_full[s][0]);
+                                    tc_commit(&s_full[s][buffer]);
                                     if (s == 1 && i + 1 == tiles) tc_commit(&q_free);
                                 }
                             }
                             __syncwarp();
                         }
                     }
-                    next_quads();
+                    next_pair();
+                    next_pair();
                 }
                 tiles_before += tiles;
                 done_with_item(n);
@@ -748,7 +728,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         } else if (warp == 12) {
             const uint64_t v_base = tc_descriptor(tc_layout(S::kValueRows * 128, 1024), smem_u32(ring) >> 4);
             const uint32_t out_idesc = tc_instruction<T>(steps * 16, false, true);
-            quad = 1;
             for (int n = 0; next_item(n, item); ++n) {
                 const int tiles = item.tile1 - item.tile0;
                 if (tiles > 0) {
@@ -756,25 +735,28 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                     ++items_before;
                 }
                 for (int i = 0; i < tiles; ++i) {
+                    const uint32_t count = tiles_before + i, buffer = count & 1;
+                    next_pair();
+                    next_pair();
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
-                        // O += W V with the stream's values: two slots, side by side
-                        const uint32_t slot = quad * 4 + 2 * s;
+                        // O += W V with the stream's values
+                        const uint32_t slot = 2 * pair;
                         wait(&full[slot], lap);
                         wait(&full[slot + 1], lap);
-                        wait(&p_full[s][0], (tiles_before + i) & 1);
+                        wait(&p_full[s][buffer], (count >> 1) & 1);
                         tc_fence_after();
                         if (elect_one()) {
 #pragma unroll
                             for (int k = 0; k < kPromptTile / 32; ++k)
-                                tc_mma_ts(tmem + kColO, tmem + s * kPromptTile + k * 8, v_base + (slot * kSlot16 + k * 128), out_idesc, i + s + k > 0);
-                            tc_commit(&o_done[s]);
+                                tc_mma_ts(tmem + kColO, tmem + s * kPromptTile + buffer * 64 + k * 8, v_base + (slot * kSlot16 + k * 128), out_idesc, i + s + k > 0);
+                            tc_commit(&o_done[s][buffer]);
                             tc_commit(&empty[slot]);
                             if (s == 1 && i + 1 == tiles) tc_commit(&o_full[0]);
                         }
                         __syncwarp();
+                        next_pair();
                     }
-                    next_quads();
                 }
                 tiles_before += tiles;
                 done_with_item(n);
@@ -860,7 +842,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
 #pragma unroll
                         for (int k = 0; k < kPromptTile / 32; ++k)
                             tc_mma_ts(d_out, d_scores + h * 64 + k * 8, v_at + (h * 64 * 128 / 16 + k * 128), out_idesc, i + h + k > 0);
-                        tc_commit(&o_done[s]);
+                        tc_commit(&o_done[s][0]);
                         if (h == 1) {
 #pragma unroll
                             for (int u = 0; u < kUnits; ++u) tc_commit(&empty[slot + u]);
@@ -911,7 +893,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         PromptItem item;
         for (int n = 0; next_item(n, item); ++n) {
             const int tiles = item.tile1 - item.tile0;
-            if (!kSharedRows && tiles > 0) {
+            if (tiles > 0) {
                 wait(&q_free, (items_before & 1) ^ 1);
                 if (!a.drop_copies && elect_one()) {
                     mbarrier_expect_tx(&q_full, query_bytes * S::kQueries);
@@ -922,9 +904,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                             tma_load_3d(smem + s * S::kQueryBytes + b * S::kBlockBytes, &q_map, b * 64, item.kv_head * a.group, item.q_row + s * a.stream_tokens, &q_full);
                 }
                 __syncwarp();
+                posted = !a.drop_copies;
                 ++items_before;
             }
-            posted = posted || (tiles > 0 && !a.drop_copies);
             for (int i = 0; i < tiles; ++i) {
                 const int row = item.k_row + (item.tile0 + i) * kPromptTile;
                 fetch(&k_map, item.kv_head, row, nullptr, false);
@@ -938,7 +920,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         if (posted) {
             for (uint32_t m = looks > kPromptLanded ? looks - kPromptLanded : 0; m < looks; ++m)
                 ok = mbarrier_wait_sleeping(&landed[m % kPromptLanded], (m / kPromptLanded) & 1) && ok;
-            if (!kSharedRows) ok = mbarrier_wait_sleeping(&q_full, (items_before - 1) & 1) && ok;
+            ok = mbarrier_wait_sleeping(&q_full, (items_before - 1) & 1) && ok;
             for (uint32_t u = units > S::kSlots ? units - S::kSlots : 0; u < units; ++u) ok = mbarrier_wait_sleeping(&full[u % S::kSlots], (u / S::kSlots) & 1) && ok;
         }
     } else if (warp == 15) {
