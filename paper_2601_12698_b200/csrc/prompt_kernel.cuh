@@ -288,8 +288,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
     constexpr bool kSharedRows = S::kSharedRows;
     constexpr int kHalves = kSharedRows ? 1 : 2;  // halves of a tile that a stream takes
     constexpr int kBlocks = S::kBlocks, kSlotBlocks = S::kSlotBlocks, kUnits = S::kUnits;
-    constexpr uint32_t kScoreIdesc = tc_instruction<T>(kPromptTile / 2, false, false);
-    constexpr uint32_t kColO = 2 * kPromptTile;
+    constexpr uint32_t kScoreIdesc = tc_instruction<T>(kSharedRows ? kPromptTile : kPromptTile / 2, false, false);
+    constexpr uint32_t kColO = 2 * kPromptTile, kBufferCols = kSharedRows ? kPromptTile : 64;  // columns of a buffer of scores, of both streams where they share rows
 
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -372,7 +372,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kSoftmaxRegs));
         const int s = warp >> 2, r = (warp & 3) * 32 + lane;
         const uint32_t lane_base = tmem + ((uint32_t)(warp & 3) << 21);
-        const uint32_t s_col = lane_base + s * kPromptTile, o_col = lane_base + kColO + s * S::kCols;
+        const uint32_t s_col = lane_base + s * (kSharedRows ? 64 : kPromptTile), o_col = lane_base + kColO + s * S::kCols;
         const int first_key = kSharedRows ? s * 64 : 0;  // of a tile's, the first that this stream takes
         const int n_heads = a.kv_heads * a.group;
         const float c = fmaxf(a.score_scale, 1.17549435e-38f);  // (a scale of zero would make NaN of hidden scores: the smallest normal number does instead)
@@ -404,13 +404,13 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                 m = *const_cast<volatile float*>(&row_reference[r]);
             } else if (my_tiles > 0) {  // the row's first scores give it its first reference
                 const int buffer = kSharedRows ? tiles_done & 1 : 0;
-                wait(&s_full[s][buffer], (kSharedRows ? tiles_done >> 1 : tiles_done) & 1);
+                wait(&s_full[kSharedRows ? 0 : s][buffer], (kSharedRows ? tiles_done >> 1 : tiles_done) & 1);
                 tc_fence_after();
                 float top = -INFINITY;
 #pragma unroll 1
                 for (int q = 0; q < 2; ++q) {
                     uint32_t v[32];
-                    tmem_load32(s_col + buffer * 64 + q * 32, v);
+                    tmem_load32(s_col + buffer * kBufferCols + q * 32, v);
                     tmem_wait_load(v);
                     if (item.tile0 >= item.masked_from) hide(v, last - item.tile0 * kPromptTile - q * 32);
 #pragma unroll
@@ -428,10 +428,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                 // exponentiated.
 #pragma unroll 1
                 for (int h = 0; h < kHalves; ++h) {
-                    const int buffer = kSharedRows ? count & 1 : h;  // of the stream's two
-                    wait(&s_full[s][buffer], (kSharedRows ? count >> 1 : count) & 1);
+                    const int buffer = kSharedRows ? count & 1 : h;
+                    wait(&s_full[kSharedRows ? 0 : s][buffer], (kSharedRows ? count >> 1 : count) & 1);
                     tc_fence_after();
-                    const uint32_t col = s_col + buffer * 64;
+                    const uint32_t col = s_col + buffer * kBufferCols;
                     // One pass over the row's 64 scores gives their maximum and, with the reference as it is, the weights and their sum.
                     // Only when the maximum turns out to be more than 8 above the reference is the pass made again, with a reference
                     // that has been moved there; the scores are still in tensor memory, the weights go over them at the end.
@@ -690,34 +690,29 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                     ++items_before;
                 }
                 for (int i = 0; i < tiles; ++i) {
-                    // S = Q K^T with each stream's keys, as soon as the weights that lie where they go have been used
+                    // S = Q K^T, as soon as the weights that lie where the scores go have been used
                     const uint32_t count = tiles_before + i, buffer = count & 1;
-                    uint32_t slot[2];
+                    if (count >= 2) {
+                        wait(&o_done[0][buffer], ((count >> 1) - 1) & 1);
+                        wait(&o_done[1][buffer], ((count >> 1) - 1) & 1);
+                    }
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        if (count >= 2) wait(&o_done[s][buffer], ((count >> 1) - 1) & 1);
+                    for (int b = 0; b < kBlocks; ++b) {
+                        wait(&full[2 * pair + b % 2], lap);
                         tc_fence_after();
+                        if (elect_one()) {
+                            const uint64_t k_at = k_base + (2 * pair + b % 2) * kSlot16;
 #pragma unroll
-                        for (int b = 0; b < kBlocks; ++b) {
-                            if (s == 0) {
-                                if (b % 2 == 0) slot[b / 2 % 2] = 2 * pair;
-                                wait(&full[2 * pair + b % 2], lap);
-                                if (b % 2 == 1) next_pair();
-                                tc_fence_after();
+                            for (int k = 0; k < 4; ++k)
+                                if (b * 4 + k < steps) tc_mma_ss(tmem + buffer * kBufferCols, q_at + (b * (S::kBlockBytes / 16) + k * 2), k_at + k * 2, kScoreIdesc, b + k > 0);
+                            if (b % 2 == 1) tc_commit(&empty[2 * pair]);
+                            if (b == kBlocks - 1) {
+                                tc_commit(&s_full[0][buffer]);
+                                if (i + 1 == tiles) tc_commit(&q_free);
                             }
-                            if (elect_one()) {
-                                const uint64_t k_at = k_base + (slot[b / 2 % 2] + b % 2) * kSlot16 + s * (64 * 128 / 16);
-#pragma unroll
-                                for (int k = 0; k < 4; ++k)
-                                    if (b * 4 + k < steps) tc_mma_ss(tmem + s * kPromptTile + buffer * 64, q_at + (b * (S::kBlockBytes / 16) + k * 2), k_at + k * 2, kScoreIdesc, b + k > 0);
-                                if (s == 1 && b % 2 == 1) tc_commit(&empty[slot[b / 2 % 2]]);
-                                if (b == kBlocks - 1) {
-                                    tc_commit(&s_full[s][buffer]);
-                                    if (s == 1 && i + 1 == tiles) tc_commit(&q_free);
-                                }
-                            }
-                            __syncwarp();
                         }
+                        __syncwarp();
+                        if (b % 2 == 1) next_pair();
                     }
                     next_pair();
                     next_pair();
@@ -749,7 +744,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                         if (elect_one()) {
 #pragma unroll
                             for (int k = 0; k < kPromptTile / 32; ++k)
-                                tc_mma_ts(tmem + kColO, tmem + s * kPromptTile + buffer * 64 + k * 8, v_base + (slot * kSlot16 + k * 128), out_idesc, i + s + k > 0);
+                                tc_mma_ts(tmem + kColO, tmem + buffer * kBufferCols + s * 64 + k * 8, v_base + (slot * kSlot16 + k * 128), out_idesc, i + s + k > 0);
                             tc_commit(&o_done[s][buffer]);
                             tc_commit(&empty[slot]);
                             if (s == 1 && i + 1 == tiles) tc_commit(&o_full[0]);
