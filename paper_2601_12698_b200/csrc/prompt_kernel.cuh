@@ -97,6 +97,9 @@ struct PromptShape {
     static constexpr int kUnits = kBlocks / kSlotBlocks;  // slots of a tile
     static constexpr int kSlotBytes = kSlotBlocks * kBlockBytes;
     static constexpr int kSlots = 10 / kSlotBlocks;
+    // Streams that share rows: a ring of its own for the keys, a tile of them, and one for the values, two slots to a stream's of a tile.  (Keys
+    // are done with long before the values fetched ahead of them.  One ring for both, 4096 tokens, 32 heads on 4 of 256: 248 us.)
+    static constexpr int kKeySlots = kBlocks, kValuePairs = (kSlots - kKeySlots) / 2;
     static constexpr int kQueryBytes = kBlocks * kBlockBytes;  // of one stream
     static constexpr int kQueries = kSharedRows ? 1 : 2;
     static constexpr size_t kRingAt = (size_t)kQueries * kQueryBytes;
@@ -627,6 +630,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
     if (warp >= 8 && warp < 12) {
         // ---- warps that look through the values of tiles that not every row sees ----
         const int p = tid - 256;  // the tile's key
+        // the first of two slots of a stream's values (shared rows)
+        const auto value_slot = [](uint32_t tile, int s) -> uint32_t { return S::kKeySlots + (2 * tile + s) % S::kValuePairs * 2; };
         constexpr uint32_t kExponent = std::is_same<T, __nv_bfloat16>::value ? 0x7F807F80u : 0x7C007C00u;
         uint32_t tiles_before = 0, looked_at = 0;  // (tiles that every row sees go past these warps: a barrier of their own tells them of the others)
         PromptItem item;
@@ -640,8 +645,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
 #pragma unroll 1
                     for (int b = 0; b < kBlocks; ++b) {
                         unsigned char* row = ring + (unit + b / kSlotBlocks) % S::kSlots * S::kSlotBytes + b % kSlotBlocks * S::kBlockBytes + p * 128;
-                        if (kSharedRows)  // two slots to a stream's keys, blocks of 64 of them
-                            row = ring + (unit + p / 64 * 2) % S::kSlots * S::kSlotBytes + b * (64 * 128) + p % 64 * 128;
+                        if (kSharedRows)  // two slots to a stream's values, blocks of 64 of them
+                            row = ring + value_slot(tiles_before + tile - item.tile0, p / 64) * S::kSlotBytes + b * (64 * 128) + p % 64 * 128;
 #pragma unroll
                         for (int u = 0; u < 8; ++u) {
                             uint4* at = reinterpret_cast<uint4*>(row + ((u ^ (p & 7)) << 4));
@@ -658,7 +663,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                 if (found && tile * kPromptTile + p < item.end_key) *reinterpret_cast<volatile int*>(&items[n % kPromptItems].bad_values) = 1;
                 fence_async_proxy();
                 asm volatile("barrier.cta.sync 1, 128;" ::: "memory");
-                if (p < kUnits) mbarrier_arrive(&full[(unit + p) % S::kSlots]);
+                if (p < kUnits) mbarrier_arrive(&full[kSharedRows ? value_slot(tiles_before + tile - item.tile0, p / 2) + p % 2 : (unit + p) % S::kSlots]);
             }
             tiles_before += item.tile1 - item.tile0;
             done_with_item(n);
@@ -669,17 +674,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         // The scores have two buffers a stream, which the tiles take in turn, so that they are there when the softmax comes to them.
         // (4096 tokens, 32 heads on 4 of 256: one buffer and one warp for both kinds of products, which spent more time issuing than the tensor
         // cores computing, 307 us; two warps 279.)
-        // The ring goes by in pairs of slots: two of a tile's keys, then one of each stream's values.
-        constexpr uint32_t kPairs = S::kSlots / 2, kSlot16 = S::kSlotBytes / 16;
-        static_assert(!kSharedRows || (S::kSlots % 2 == 0 && kUnits == 4), "a tile of keys or values is two pairs of slots");
+        constexpr uint32_t kSlot16 = S::kSlotBytes / 16;
         const int steps = (a.dim + 15) / 16;  // of 16 dims
-        uint32_t tiles_before = 0, items_before = 0, pair = 0, lap = 0;
-        const auto next_pair = [&]() {
-            if (++pair == kPairs) {
-                pair = 0;
-                lap ^= 1;
-            }
-        };
+        uint32_t tiles_before = 0, items_before = 0;
         PromptItem item;
         if (warp == 13) {
             const uint64_t q_at = tc_descriptor(tc_layout(16, 1024), smem_u32(smem) >> 4), k_base = tc_descriptor(tc_layout(16, 1024), smem_u32(ring) >> 4);
@@ -698,24 +695,21 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                     }
 #pragma unroll
                     for (int b = 0; b < kBlocks; ++b) {
-                        wait(&full[2 * pair + b % 2], lap);
+                        wait(&full[b], count & 1);
                         tc_fence_after();
                         if (elect_one()) {
-                            const uint64_t k_at = k_base + (2 * pair + b % 2) * kSlot16;
+                            const uint64_t k_at = k_base + b * kSlot16;
 #pragma unroll
                             for (int k = 0; k < 4; ++k)
                                 if (b * 4 + k < steps) tc_mma_ss(tmem + buffer * kBufferCols, q_at + (b * (S::kBlockBytes / 16) + k * 2), k_at + k * 2, kScoreIdesc, b + k > 0);
-                            if (b % 2 == 1) tc_commit(&empty[2 * pair]);
+                            if (b % 2 == 1) tc_commit(&empty[b - 1]);
                             if (b == kBlocks - 1) {
                                 tc_commit(&s_full[0][buffer]);
                                 if (i + 1 == tiles) tc_commit(&q_free);
                             }
                         }
                         __syncwarp();
-                        if (b % 2 == 1) next_pair();
                     }
-                    next_pair();
-                    next_pair();
                 }
                 tiles_before += tiles;
                 done_with_item(n);
@@ -723,6 +717,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         } else if (warp == 12) {
             const uint64_t v_base = tc_descriptor(tc_layout(S::kValueRows * 128, 1024), smem_u32(ring) >> 4);
             const uint32_t out_idesc = tc_instruction<T>(steps * 16, false, true);
+            uint32_t pair = 0, lap = 0;
             for (int n = 0; next_item(n, item); ++n) {
                 const int tiles = item.tile1 - item.tile0;
                 if (tiles > 0) {
@@ -731,12 +726,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                 }
                 for (int i = 0; i < tiles; ++i) {
                     const uint32_t count = tiles_before + i, buffer = count & 1;
-                    next_pair();
-                    next_pair();
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
                         // O += W V with the stream's values
-                        const uint32_t slot = 2 * pair;
+                        const uint32_t slot = S::kKeySlots + 2 * pair;
                         wait(&full[slot], lap);
                         wait(&full[slot + 1], lap);
                         wait(&p_full[s][buffer], (count >> 1) & 1);
@@ -750,7 +743,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                             if (s == 1 && i + 1 == tiles) tc_commit(&o_full[0]);
                         }
                         __syncwarp();
-                        next_pair();
+                        if (++pair == S::kValuePairs) {
+                            pair = 0;
+                            lap ^= 1;
+                        }
                     }
                 }
                 tiles_before += tiles;
@@ -864,26 +860,51 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         bool posted = false;
         const uint32_t query_bytes = (uint32_t)(a.stream_tokens * a.group) * 128u * kBlocks;
         // A tile of keys or values from row `row` on; `bar`, where there is one, is told of all its bytes, otherwise each slot of its own.
-        auto fetch = [&](const CUtensorMap* map, int head, int row, uint64_t* bar, bool by_stream) {
+        auto fetch = [&](const CUtensorMap* map, int head, int row, uint64_t* bar) {
 #pragma unroll
             for (int u = 0; u < kUnits; ++u) {
                 const uint32_t slot = units % S::kSlots;
-                if (!kSharedRows || u % 2 == 0) wait(&empty[slot], ((units / S::kSlots) & 1) ^ 1);  // (heads of more than 128: two slots at a time)
+                wait(&empty[slot], ((units / S::kSlots) & 1) ^ 1);
                 if (!a.drop_copies && elect_one()) {
                     if (!bar) mbarrier_expect_tx(&full[slot], S::kSlotBytes);
                     else if (u == 0) mbarrier_expect_tx(bar, S::kSlotBytes * kUnits);
 #pragma unroll
-                    for (int b = 0; b < (by_stream ? 0 : kSlotBlocks); ++b)
+                    for (int b = 0; b < kSlotBlocks; ++b)
                         tma_load_3d(ring + slot * S::kSlotBytes + b * S::kBlockBytes, map, (u * kSlotBlocks + b) * 64, head, row, bar ? bar : &full[slot]);
-                    if (by_stream) {  // half of the columns of a stream's values
-#pragma unroll
-                        for (int b = 0; b < 2; ++b)
-                            tma_load_3d(ring + slot * S::kSlotBytes + b * (64 * 128), map, (u % 2 * 2 + b) * 64, head, row + u / 2 * 64, bar ? bar : &full[slot]);
-                    }
                 }
                 __syncwarp();
                 ++units;
             }
+        };
+        // The same with shared rows: the tile's keys, two slots freed at a time, and a stream's values.
+        uint32_t key_tiles = 0, value_pairs = 0;
+        auto fetch_keys = [&](int head, int row) {
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) {
+                if (b % 2 == 0) wait(&empty[b], (key_tiles & 1) ^ 1);
+                if (!a.drop_copies && elect_one()) {
+                    mbarrier_expect_tx(&full[b], S::kSlotBytes);
+                    tma_load_3d(ring + b * S::kSlotBytes, &k_map, b * 64, head, row, &full[b]);
+                }
+                __syncwarp();
+            }
+            ++key_tiles;
+        };
+        auto fetch_values = [&](int s, int head, int row, uint64_t* bar) {
+            const uint32_t slot = S::kKeySlots + value_pairs % S::kValuePairs * 2;
+            wait(&empty[slot], ((value_pairs / S::kValuePairs) & 1) ^ 1);
+            if (!a.drop_copies && elect_one()) {
+                if (bar && s == 0) mbarrier_expect_tx(bar, S::kSlotBytes * 4);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    if (!bar) mbarrier_expect_tx(&full[slot + u], S::kSlotBytes);
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+                        tma_load_3d(ring + (slot + u) * S::kSlotBytes + b * (64 * 128), &v_map, (u * 2 + b) * 64, head, row + s * 64, bar ? bar : &full[slot + u]);
+                }
+            }
+            __syncwarp();
+            ++value_pairs;
         };
         PromptItem item;
         for (int n = 0; next_item(n, item); ++n) {
@@ -902,12 +923,22 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                 posted = !a.drop_copies;
                 ++items_before;
             }
+            uint64_t* late = nullptr;  // barrier of the last tile's values
             for (int i = 0; i < tiles; ++i) {
                 const int row = item.k_row + (item.tile0 + i) * kPromptTile;
-                fetch(&k_map, item.kv_head, row, nullptr, false);
                 const bool masked = item.tile0 + i >= item.masked_from;  // then those who look through the values tell the others
-                fetch(&v_map, item.kv_head, row, masked ? &landed[looks % kPromptLanded] : nullptr, kSharedRows);
+                uint64_t* const bar = masked ? &landed[looks % kPromptLanded] : nullptr;
                 if (masked) ++looks;
+                if constexpr (kSharedRows) {  // in the order in which slots become free
+                    fetch_keys(item.kv_head, row);
+                    if (i > 0) fetch_values(1, item.kv_head, row - kPromptTile, late);
+                    fetch_values(0, item.kv_head, row, bar);
+                    late = bar;
+                    if (i + 1 == tiles) fetch_values(1, item.kv_head, row, bar);
+                } else {
+                    fetch(&k_map, item.kv_head, row, nullptr);
+                    fetch(&v_map, item.kv_head, row, bar);
+                }
             }
             done_with_item(n);
         }
@@ -917,6 +948,11 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                 ok = mbarrier_wait_sleeping(&landed[m % kPromptLanded], (m / kPromptLanded) & 1) && ok;
             ok = mbarrier_wait_sleeping(&q_full, (items_before - 1) & 1) && ok;
             for (uint32_t u = units > S::kSlots ? units - S::kSlots : 0; u < units; ++u) ok = mbarrier_wait_sleeping(&full[u % S::kSlots], (u / S::kSlots) & 1) && ok;
+            if constexpr (kSharedRows) {
+                for (int b = 0; b < kBlocks; ++b) ok = mbarrier_wait_sleeping(&full[b], (key_tiles - 1) & 1) && ok;
+                for (uint32_t u = value_pairs > S::kValuePairs ? value_pairs - S::kValuePairs : 0; u < value_pairs; ++u)
+                    for (int k = 0; k < 2; ++k) ok = mbarrier_wait_sleeping(&full[S::kKeySlots + u % S::kValuePairs * 2 + k], (u / S::kValuePairs) & 1) && ok;
+            }
         }
     } else if (warp == 15) {
         // ---- the warp that works out the items ----
