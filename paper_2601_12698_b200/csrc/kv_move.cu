@@ -252,7 +252,7 @@ int kv_cache_compact_launch(const rt_kv_cache* caches, int32_t n_caches, const r
     if ((st = current_limits(&L)) != RT_OK) return st;
     // Tasks (a side of a layer and a head) of a sequence to one CTA: few enough that two CTAs to an SM cover the device, and no fewer than its
     // warps.  (40 sequences x 32 layers x 8 heads, two or three rows each: 8.6 us in a graph with two CTAs, 10.3 with four.  Rows dealt out
-    // in halves, for more CTAs, were slower where there are few: 12 sequences x 8 layers: 164 us, not 145.)
+    // in halves, for more CTAs, were slower where there are few: 12 sequences x 8 layers: 164 us, then 145 without.)
     const long long tasks = (long long)a.m.sides * a.m.heads;
     a.tasks_per_cta = (int)std::min<long long>(128, std::max<long long>(8, tasks * n_seqs / (L.sm_count * 2LL) / 8 * 8));
     a.ctas_per_seq = (int)((tasks + a.tasks_per_cta - 1) / a.tasks_per_cta);

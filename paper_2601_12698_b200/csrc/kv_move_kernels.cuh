@@ -71,7 +71,7 @@ struct CopyPagesArgs {
 
 // A group of threads takes a pair of pages of one side of one layer: blockIdx.y names the side (the scales' sides follow the
 // elements'), blockIdx.x pairs and, for pages of more than kMoveThreads * U vectors, pieces of them.  U vectors of a thread are
-// in flight at once.  Measured: 500 pages of 64 x 8 x 128 e4m3 in 16 layers, 2.16 GB: 288 us, 7.5 TB/s (a third of the sources is
+// in flight at once.  Measured: 500 pages of 64 x 8 x 128 e4m3 in 16 layers, 2.16 GB: 283 us, 7.6 TB/s (a third of the sources is
 // read twice, out of L2); 12 partly filled pages of 16 x 8 x 128 bf16 in 32 layers: 5.2 us in a graph.
 template <int VB, int U>
 __device__ __forceinline__ void copy_pages(const CopyPagesArgs& a, const PageRuns& runs, int kind, int side)

@@ -59,12 +59,12 @@ int make_prompt_plan(const rt_prompt_batch* b, int q_heads, int kv_heads, int di
     const long long blocks = b->q_tokens / p->block_tokens + b->n_seqs;
     const long long expected = std::min(blocks, b->n_seqs * ceil_div(b->max_q_len, p->block_tokens)) * kv_heads, tiles = ceil_div(b->max_k_len, kPromptTile);
     // Blocks that do not fill the device evenly, against many keys: the keys are cut into parts, as many as end first by a model of whole
-    // waves of items: a key tile takes 1.7 us (3.2 with heads of more than 128), beginning and ending an item 3, joining the parts 3 and
-    // the time to write and read them at 5 TB/s.  512 tokens behind 16000, 40 heads on 8 of 128, 88 blocks: 240 us in one part, 172 in three.
+    // waves of items: a key tile takes 1.7 us (2.3 with heads of more than 128), beginning and ending an item 3, joining the parts 3 and
+    // the time to write and read them at 5 TB/s.  512 tokens behind 16000, 40 heads on 8 of 128, 88 blocks: 237 us in one part, 185 in three.
     // Blocks of two waves and more are left whole: their order evens them out.
     p->parts = 1;
     if (expected > 0 && expected < 2LL * L.sm_count && b->q_tokens / p->block_tokens * kv_heads < 2LL * L.sm_count && tiles >= 8) {
-        const double tile_us = p->form == 2 ? 3.2 : 1.7, part_us = (double)b->q_tokens * q_heads * dim * 8 / 5e6;
+        const double tile_us = p->form == 2 ? 2.3 : 1.7, part_us = (double)b->q_tokens * q_heads * dim * 8 / 5e6;
         double best = 0;
         for (int parts = 1; parts <= std::min<long long>(kPromptMaxParts, tiles / 2); ++parts) {
             const double time = (double)ceil_div(expected * parts, L.sm_count) * (ceil_div(tiles, parts) * tile_us + 3) + (parts > 1 ? 3 + parts * part_us : 0);

@@ -11,14 +11,15 @@
 //   warps 0-3, 4-7   two softmax streams of 128 rows, one row to a thread (tensor memory lane = row): scores from tensor memory, m and
 //                    the sum in registers, the weights back over the scores as the 16-bit left operand of the second product;
 //   warps 8-11       look through the values of tiles that not every row sees (see below);
-//   warps 12, 13     issue the products, each for its stream;
-//   warp 14          fetches queries, keys and values with TMA into a ring of 128-byte-swizzled tiles;
+//   warps 12, 13     issue the products, each for its stream (heads of more than 128: one the outputs', one the scores');
+//   warp 14          fetches queries, keys and values with TMA into rings of 128-byte-swizzled tiles;
 //   warp 15          works out the items.
 // The streams share keys and values and take turns on the tensor cores: while one's scores are exponentiated the other's products
 // run.  The queries and first tiles of the next item are fetched, and its first scores computed, while this one's results leave.
 //
 // Heads of more than 128 (DP = 256): tensor memory has no room for two outputs of 256, so both streams take the same 128 rows and one output,
-// the first the first 64 keys of every tile and the second the others.
+// the first the first 64 keys of every tile and the second the others.  What is left of tensor memory holds the scores of two tiles: the
+// next tile's are computed while this one's are exponentiated.
 //
 // The reference m is moved only when a score exceeds it by 8, as in the prefix kernel: weights reach 2^8.  Streams that share rows share
 // the reference, as if the second's keys came behind the first's: a stream works with the reference that it knows, and before it
@@ -30,7 +31,16 @@
 // the rows that do see them add them when they are written.
 //
 // Bounds: 4 * 128 * 128 * dim flops and 128 * 128 exponentials per tile and stream; at dim 128 the tensor cores need 1024
-// cycles for that and the SM's 16 exponentials a cycle 1024 as well.
+// cycles for that and the SM's 16 exponentials a cycle 1024 as well.  Products read their operands from shared memory at 128 bytes a
+// cycle: 128 x 64 x 16 take 48 cycles instead of 32, 128 x 128 x 16 the 64 that they should, and with the left operand in tensor memory both
+// do.  Scores 64 keys at a time, which let the tensor cores go on while the other half is exponentiated, are worth that at dims up to 128
+// (one product of 128 keys: 563 us, not 440).
+//
+// Measured (TFLOP/s of the causal pairs; the clock drops to 1.64 GHz under the power limit in the long ones):
+//   8192 tokens, 32 heads on 8 of 128: 440 us, 1250; the tensor cores busy in 64 % of the cycles, the special function unit in 64 %;
+//   16384 tokens: 1700 .. 1970 us, 1290 .. 1120 by the box; heads of 64, 8192 tokens: 355 us, special function unit 74 %;
+//   32 heads on 4 of 256, 4096 tokens: 248 us, 1110; shared memory: 2560 cycles of a tile's 3600 go to operands and to what TMA writes;
+//   100 tokens: 9.9 us, one CTA's chain: beginning 0.4, item 1.2, first copies 0.7, products and softmax 3, results 1.2, launch.
 #pragma once
 
 #include <cuda.h>
@@ -91,8 +101,7 @@ struct PromptShape {
     static constexpr int kCols = DP == 256 ? 128 : DP;    // dims that a stream writes
     static constexpr int kValueRows = kSharedRows ? kPromptTile / 2 : kPromptTile;  // keys of a box of values: those of a stream
     static constexpr int kBlockBytes = kPromptTile * 128;
-    // The ring: 160 KB, a block to a slot, or both of heads of 128.  (Heads of 128, 8192 tokens: 435 us with two, 445 with one; heads of 256, 256
-    // tokens behind 8000: 102 us with one, as they are asked for and freed one after the other, 115 with two; 128 KB: 110.)
+    // The ring: 160 KB, a block to a slot, or both of heads of 128.  (Heads of 128, 8192 tokens: 435 us with two, 445 with one.)
     static constexpr int kSlotBlocks = DP == 128 ? 2 : 1;
     static constexpr int kUnits = kBlocks / kSlotBlocks;  // slots of a tile
     static constexpr int kSlotBytes = kSlotBlocks * kBlockBytes;
@@ -671,9 +680,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
     }
     if constexpr (kSharedRows) {
         // ---- warps that issue the products of both streams: one the scores', one the outputs' ----
-        // The scores have two buffers a stream, which the tiles take in turn, so that they are there when the softmax comes to them.
-        // (4096 tokens, 32 heads on 4 of 256: one buffer and one warp for both kinds of products, which spent more time issuing than the tensor
-        // cores computing, 307 us; two warps 279.)
+        // The scores have two buffers, which the tiles take in turn, so that they are there when the softmax comes to them.  (4096 tokens, 32
+        // heads on 4 of 256: one buffer, and one warp for all products, which spent more time issuing than the tensor cores computing: 307 us; two
+        // warps: 279; two buffers: 259; both streams' scores in one product of 128 keys: 248.)
         constexpr uint32_t kSlot16 = S::kSlotBytes / 16;
         const int steps = (a.dim + 15) / 16;  // of 16 dims
         uint32_t tiles_before = 0, items_before = 0;

