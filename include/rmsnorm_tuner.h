@@ -577,8 +577,9 @@ int64_t prompt_attention_workspace_bytes(const rt_prompt_batch* batch, int32_t q
 #define RT_MAX_LAYERS 128
 
 /*
- * Copies pages inside caches: in each of the n_caches caches (host array; alike in everything but their pointers) the first
- * tokens[i] entries of page src[i] become those of page dst[i], scales included, the rest of the page stays.
+ * Copies pages inside caches: in each of the n_caches caches (host array; alike in everything but their pointers, no memory twice;
+ * pages of at most 2^30 bytes) the first tokens[i] entries of page src[i] become those of page dst[i], scales included, the rest of the
+ * page stays.
  *   src, dst  device, int32 [n_pages].  A page may be a source any number of times; a destination must be neither a source nor another
  *             destination of the same call (its content would be a mixture).  A pair with a negative number is skipped; one
  *             beyond the cache is skipped and reported as RT_ERR_INDEX in the device status word.

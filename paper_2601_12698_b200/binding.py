@@ -701,8 +701,8 @@ def rotary_launch(table: RotaryTable, positions, q, k=None, q_out=None, k_out=No
 class PromptBatch:
     """Sequences packed behind one another: the first query row of each and, last, the row behind them all (int32 [n_seqs + 1], not
     descending), and the same for keys (k_starts None: the queries' own).  max_q_len and max_k_len are about the largest lengths, on the
-    host's side: the launch shape follows them, and of the results the roundings alone.  causal: the queries are the last tokens of their sequence and see the
-    keys up to their own; otherwise all of the sequence's.  One object serves every layer of the step."""
+    host's side: the launch shape follows them, and of the results the roundings alone.  causal: the queries are the last tokens of their
+    sequence and see the keys up to their own; otherwise all of the sequence's.  One object serves every layer of the step."""
 
     def __init__(self, q_starts, max_q_len: int, k_starts=None, max_k_len: int | None = None, causal: bool = True):
         _torch_ready()
@@ -791,6 +791,9 @@ class KvCacheStack:
         for c in self.caches:
             if c.device_index != first.device_index or any(getattr(c.struct, n) != getattr(first.struct, n) for n in alike):
                 raise ValueError("the caches of a stack must have one device, shape, format and strides")
+        held = [t.data_ptr() for c in self.caches for t in (c.k, c.v, c.k_scale, c.v_scale) if t is not None]
+        if len(set(held)) != len(held):
+            raise ValueError("a stack holds no cache twice")
         self.device_index = first.device_index
         self._array, self._count = (rt_kv_cache * len(self.caches))(*[c.struct for c in self.caches]), len(self.caches)
 

@@ -168,6 +168,11 @@ int kv_cache_copy_pages_launch(const rt_kv_cache* caches, int32_t n_caches, cons
         set_error("src, dst or tokens is not aligned to its element size");
         return RT_ERR_ALIGN;
     }
+    const long long largest = (long long)a.m.page_size * a.m.heads * std::max(a.m.kind[0].row_bytes, a.m.kind[1].row_bytes);
+    if (largest > (1LL << 30)) {  // places inside a page are ints
+        set_error("a page of %lld bytes is too large", largest);
+        return RT_ERR_SHAPE;
+    }
     a.m.status = device_status_word();
     if (!a.m.status) return RT_ERR_NO_DEVICE;
     a.src = src;
@@ -182,10 +187,6 @@ int kv_cache_copy_pages_launch(const rt_kv_cache* caches, int32_t n_caches, cons
         width[kind] = access_width(a.m, kind, r.run_bytes, 32);
         if (width[kind] == 2) width[kind] = 1;
         const long long page_bytes = (long long)a.m.page_size * a.m.heads * a.m.kind[kind].row_bytes;
-        if (page_bytes > 0x7fffffffLL) {
-            set_error("a page of %lld bytes is too large", page_bytes);
-            return RT_ERR_SHAPE;
-        }
         const long long vectors = (page_bytes + width[kind] - 1) / width[kind];
         int threads = 1;
         while (threads < kMoveThreads && threads * 4 < vectors) threads *= 2;

@@ -50,8 +50,8 @@ int launch_rotary(RotaryArgs a, cudaStream_t stream)
 }
 
 // A thread takes up to U heads of its token and fetches them all at once; its P sines and cosines are worked out meanwhile.  Eight heads to a
-// thread where that fills the device twice over, two otherwise: 16384 tokens x 40 heads of 128 bf16: 56.5 us, 63.8 with two (81.8 with four
-// heads at a time, ten times over); 64 tokens: 4.2 us in a graph with eight, 2.7 with two.
+// thread where that fills the device twice over, two otherwise: 16384 tokens x 40 heads of 128 bf16: 55.8 us, 63.8 with two (81.8 with four
+// heads at a time, ten times over); 64 tokens: 4.2 us in a graph with eight, 2.6 with two.
 template <typename T, int P>
 int launch_width(RotaryArgs a, int rot, int tail_elems, bool interleaved, cudaStream_t stream)
 {
@@ -191,6 +191,11 @@ int rotary_launch(const rt_rotary* r, const int64_t* positions, int64_t n_tokens
     if (((uintptr_t)positions | (uintptr_t)r->turns) & 7u) {
         set_error("positions or turns is not aligned to 8 bytes");
         return RT_ERR_ALIGN;
+    }
+    if (a.side[0].heads > 0 && a.side[1].heads > 0 &&
+        (a.side[0].out == a.side[1].out || a.side[0].out == a.side[1].in || a.side[1].out == a.side[0].in)) {
+        set_error("the two sides overlap");
+        return RT_ERR_SHAPE;
     }
     while (width > 1 && (places & (uintptr_t)(width * size - 1))) width /= 2;
     a.turns = (const unsigned long long*)r->turns;

@@ -214,3 +214,11 @@ def test_streams_graphs_and_refusals(B):
         B.KvCacheStack([])
     with pytest.raises(ValueError):
         B.KvCacheStack([stack.caches[0], B.KvCache.allocate(20, 8, 4, 64, torch.float8_e4m3fn)])
+
+
+def test_a_stack_holds_no_cache_twice(B):
+    cache = B.KvCache.allocate(4, 8, 2, 64, torch.int8)
+    with pytest.raises(ValueError):
+        B.KvCacheStack([cache, cache])
+    with pytest.raises(ValueError):
+        B.KvCacheStack([cache, B.KvCache(cache.v.clone(), cache.v, cache.k_scale.clone(), cache.v_scale.clone())])

@@ -58,3 +58,8 @@ def test_nothing_to_do_is_no_error():
 @pytest.mark.parametrize("at", [P + 4, P - 8, P + 60, P + 72, P + 56])
 def test_new_lengths_that_overlap_the_inputs_are_refused(at):
     assert _compact(new_lens=at) == B.RT_ERR_SHAPE and "overlap" in B.lib.rt_last_error().decode()
+
+
+def test_pages_that_are_too_large_are_refused():
+    wide = dict(page_size=1 << 16, kv_heads=256, head_dim=128, head_stride=128, token_stride=256 * 128, page_stride=256 * 128 << 16)
+    assert _copy(_array(_cache(**wide))) == B.RT_ERR_SHAPE and B.lib.rt_last_error()

@@ -102,3 +102,9 @@ def test_nothing_to_do_is_no_error():
         B.RotaryTable(64, scaling="other", device="cpu")
     with pytest.raises(B.TunerError):
         B.RotaryTable(63, device="cpu")
+
+
+@pytest.mark.parametrize("q,k", [((P, 512, 128, P, 512, 128, 4), (P, 256, 128, P, 256, 128, 2)), ((P, 512, 128, P + 4096, 512, 128, 4), (P + 4096, 256, 128, P + 4096, 256, 128, 2)),
+                                 ((P, 512, 128, P, 512, 128, 4), (P + 4096, 256, 128, P, 256, 128, 2))])
+def test_sides_that_are_one_another_are_refused(q, k):
+    assert _call(q=q, k=k) == B.RT_ERR_SHAPE and "overlap" in B.lib.rt_last_error().decode()
