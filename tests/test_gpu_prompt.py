@@ -305,3 +305,15 @@ def test_refusals(B):
     with pytest.raises(B.TunerError) as e:
         long.launch(workspace=small)
     assert e.value.status == B.RT_ERR_CAPACITY
+
+
+@pytest.mark.parametrize("dim,causal", [(256, True), (200, True), (256, False), (128, True)])
+def test_many_short_blocks_to_a_cta(B, dim, causal):
+    """One block's results leave while the next one's products are under way, eleven blocks to a CTA and more."""
+    lens = [(1 + 7 * i % 40, 1 + 7 * i % 40 + (61 * i % 190 if i % 3 else 0)) for i in range(420)]
+    p = Problem(B, lens, 4, 4, dim, seed=3, causal=causal)
+    first = p.launch()
+    p.check(*first)
+    for _ in range(4):
+        assert all(torch.equal(a, b) for a, b in zip(first, p.launch()))
+    assert B.rt_device_status() == 0
