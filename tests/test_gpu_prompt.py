@@ -317,3 +317,16 @@ def test_many_short_blocks_to_a_cta(B, dim, causal):
     for _ in range(4):
         assert all(torch.equal(a, b) for a, b in zip(first, p.launch()))
     assert B.rt_device_status() == 0
+
+
+@pytest.mark.parametrize("n", [127, 128, 129, 161, 700])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dim", [64, 256])
+def test_many_sequences_of_very_different_costs(B, n, causal, dim):
+    """Every block is taken once, whatever the order: costs from nothing to many blocks of keys, empty sequences among them."""
+    g = torch.Generator().manual_seed(n)
+    q = (torch.rand(n, generator=g) ** 12 * 900).int().tolist()
+    more = (torch.rand(n, generator=g) ** 6 * 1200).int().tolist()
+    p = Problem(B, [(a, a + b if i % 5 else b) for i, (a, b) in enumerate(zip(q, more))], 4, 2, dim, tail=3, seed=n, causal=causal)
+    p.check(*p.launch())
+    assert B.rt_device_status() == 0
