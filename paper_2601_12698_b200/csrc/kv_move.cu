@@ -110,33 +110,42 @@ CopyKernel copy_kernel(int vb)
 }
 
 typedef void (*CompactKernel)(CompactArgs);
-template <int VB>
-CompactKernel compact_kernel(int lanes)  // of 32
+template <int VB, int STAGES>
+CompactKernel compact_kernel(int lanes)
 {
-    if constexpr (VB < 4) return kv_compact_kernel<VB, 32>;
-    else return lanes == 0 ? kv_compact_kernel<VB, 4> : lanes == 1 ? kv_compact_kernel<VB, 8> : lanes == 2 ? kv_compact_kernel<VB, 16> : kv_compact_kernel<VB, 32>;
+    if constexpr (VB < 4) return kv_compact_kernel<VB, 32, STAGES>;
+    else
+        return lanes == 4    ? kv_compact_kernel<VB, 4, STAGES>
+               : lanes == 8  ? kv_compact_kernel<VB, 8, STAGES>
+               : lanes == 16 ? kv_compact_kernel<VB, 16, STAGES>
+                             : kv_compact_kernel<VB, 32, STAGES>;
+}
+template <int VB>
+CompactKernel compact_kernel(int lanes, bool deep)
+{
+    if constexpr (VB < 4) return compact_kernel<VB, kMoveStages>(lanes);
+    else return deep ? compact_kernel<VB, kMoveDeepStages>(lanes) : compact_kernel<VB, kMoveStages>(lanes);
 }
 
-// The kernel for accesses of `width` bytes and rows of `row_vectors` of them.  Shared memory beyond the default limit is asked for once per
+// The kernel for accesses of `width` bytes, `lanes` of them side by side.  Shared memory beyond the default limit is asked for once per
 // device and kernel.
-int find_compact_kernel(int width, int row_vectors, int kinds, CompactKernel* fn)
+int find_compact_kernel(int width, int lanes, bool deep, int smem, CompactKernel* fn)
 {
-    static std::atomic<unsigned char> done[kDeviceSlots][5][4];
-    const int lanes = row_vectors <= 4 ? 0 : row_vectors <= 8 ? 1 : row_vectors <= 16 ? 2 : 3;
+    static std::atomic<unsigned char> done[kDeviceSlots][5][6][2];
     switch (width) {
-        case 16: *fn = compact_kernel<16>(lanes); break;
-        case 8: *fn = compact_kernel<8>(lanes); break;
-        case 4: *fn = compact_kernel<4>(lanes); break;
-        case 2: *fn = compact_kernel<2>(lanes); break;
-        default: *fn = compact_kernel<1>(lanes); break;
+        case 16: *fn = compact_kernel<16>(lanes, deep); break;
+        case 8: *fn = compact_kernel<8>(lanes, deep); break;
+        case 4: *fn = compact_kernel<4>(lanes, deep); break;
+        case 2: *fn = compact_kernel<2>(lanes, deep); break;
+        default: *fn = compact_kernel<1>(lanes, deep); break;
     }
-    if (compact_smem(kinds, width) <= 48 * 1024) return RT_OK;
+    if (smem <= 48 * 1024) return RT_OK;
     int device;
     const int st = current_device_index(&device);
     if (st != RT_OK) return st;
-    std::atomic<unsigned char>& mine = done[device][log2_or_minus1((unsigned)width)][lanes];
+    std::atomic<unsigned char>& mine = done[device][log2_or_minus1((unsigned)width)][log2_or_minus1((unsigned)lanes)][deep];
     if (!mine.load(std::memory_order_acquire)) {
-        RT_CUDA_OK(cudaFuncSetAttribute((const void*)*fn, cudaFuncAttributeMaxDynamicSharedMemorySize, compact_smem(2, width)));
+        RT_CUDA_OK(cudaFuncSetAttribute((const void*)*fn, cudaFuncAttributeMaxDynamicSharedMemorySize, compact_smem(2, width, deep ? kMoveDeepStages : kMoveStages)));
         mine.store(1, std::memory_order_release);
     }
     return RT_OK;
@@ -251,22 +260,33 @@ int kv_cache_compact_launch(const rt_kv_cache* caches, int32_t n_caches, const r
     const long long n_seqs = b->n_seqs;
     rt_limits L;
     if ((st = current_limits(&L)) != RT_OK) return st;
-    // Tasks (a side of a layer and a head) of a sequence to one CTA: few enough that two CTAs to an SM cover the device, and no fewer than its
-    // warps.  (40 sequences x 32 layers x 8 heads, two or three rows each: 8.6 us in a graph with two CTAs, 10.3 with four.  Rows dealt out
-    // in halves, for more CTAs, were slower where there are few: 12 sequences x 8 layers: 164 us, then 145 without.)
-    const long long tasks = (long long)a.m.sides * a.m.heads;
-    a.tasks_per_cta = (int)std::min<long long>(128, std::max<long long>(8, tasks * n_seqs / (L.sm_count * 2LL) / 8 * 8));
-    a.ctas_per_seq = (int)((tasks + a.tasks_per_cta - 1) / a.tasks_per_cta);
-    const long long ctas = (long long)a.ctas_per_seq * n_seqs;
+    // A task is a side of a layer, a head and a piece of its rows: whole rows, or where that leaves SMs without a CTA, pieces down to 64 bytes.
+    // Tasks of a sequence to one CTA: few enough that two CTAs to an SM cover the device, and no fewer than its warps.  With no more CTAs than
+    // SMs each has more under way.  (40 sequences x 32 layers x 8 heads, two or three rows each: 8.6 us in a graph with two CTAs to an SM,
+    // 10.3 with four.  Rows in halves, for more CTAs than SMs, were slower: 12 sequences x 8 layers: 164 us, then 145 without.  One sequence of
+    // 100000 tokens x 4 layers x 8 heads of 128 bf16: 581 us, 1439 with whole rows and three items under way; 24000 x 32 layers: 421 and 590.)
+    const int width = access_width(a.m, 0, a.m.kind[0].row_bytes, 16), row_vectors = a.m.kind[0].row_bytes / width;
+    int lanes = 32;
+    while (width >= 4 && lanes > 4 && lanes / 2 >= row_vectors) lanes /= 2;
+    long long tasks, ctas;
+    for (;; lanes /= 2) {
+        a.pieces = (row_vectors + lanes - 1) / lanes;
+        tasks = (long long)a.m.sides * a.m.heads * a.pieces;
+        a.tasks_per_cta = (int)std::min<long long>(128, std::max<long long>(8, tasks * n_seqs / (L.sm_count * 2LL) / 8 * 8));
+        a.ctas_per_seq = (int)((tasks + a.tasks_per_cta - 1) / a.tasks_per_cta);
+        ctas = (long long)a.ctas_per_seq * n_seqs;
+        if (ctas * 2 > L.sm_count || width < 4 || lanes == 4 || lanes * width <= 64) break;
+    }
     if (ctas > 0x7fffffffLL) {
         set_error("n_seqs=%lld needs too many CTAs", n_seqs);
         return RT_ERR_SHAPE;
     }
-    const int width = access_width(a.m, 0, a.m.kind[0].row_bytes, 16), row_vectors = a.m.kind[0].row_bytes / width;
+    const bool deep = width >= 4 && ctas <= L.sm_count;
+    const int smem = compact_smem(a.m.kinds, width, deep ? kMoveDeepStages : kMoveStages);
     CompactKernel fn;
-    if ((st = find_compact_kernel(width, row_vectors, a.m.kinds, &fn)) != RT_OK) return st;
+    if ((st = find_compact_kernel(width, lanes, deep, smem, &fn)) != RT_OK) return st;
     void* params[] = {&a};
-    return launch_kernel((const void*)fn, dim3((unsigned)ctas), dim3(kMoveThreads), (size_t)compact_smem(a.m.kinds, width), (cudaStream_t)stream, params);
+    return launch_kernel((const void*)fn, dim3((unsigned)ctas), dim3(kMoveThreads), (size_t)smem, (cudaStream_t)stream, params);
 }
 
 }  // extern "C"

@@ -139,7 +139,8 @@ struct CompactArgs {
     int window;
     int32_t* new_lens;
     int n_seqs;
-    int tasks_per_cta;  // of the sides x heads of a sequence
+    int pieces;         // of a row, each a task of its own
+    int tasks_per_cta;  // of the sides x heads x pieces of a sequence
     int ctas_per_seq;
 };
 
@@ -150,14 +151,14 @@ struct MoveRow {
 constexpr int kMoveTurns = 4;  // tokens of a thread that are looked at together
 constexpr int kMoveChunk = kMoveThreads * kMoveTurns;
 
-constexpr int kMoveStages = 3;    // items of a warp under way
+constexpr int kMoveStages = 3, kMoveDeepStages = 10;  // items of a warp under way, with two CTAs to an SM and with one
 constexpr int kMoveAccesses = 4;  // accesses of a lane in an item
 constexpr int kMoveScales = 16;   // scales of a thread under way
 
 // Shared memory of a CTA: the lists, of elements and of scales, and the items under way.
-inline int compact_smem(int kinds, int vector_bytes)
+inline int compact_smem(int kinds, int vector_bytes, int stages)
 {
-    return kinds * kMoveChunk * (int)sizeof(MoveRow) + (vector_bytes >= 4 ? kMoveThreads * kMoveStages * kMoveAccesses * vector_bytes : 0);
+    return kinds * kMoveChunk * (int)sizeof(MoveRow) + (vector_bytes >= 4 ? kMoveThreads * stages * kMoveAccesses * vector_bytes : 0);
 }
 
 template <int VB>
@@ -175,7 +176,7 @@ __device__ __forceinline__ Vec<VB> ld_slot(uint32_t at)
     else asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v.w[0]) : "r"(at) : "memory");
     return v;
 }
-// CTA: one sequence, some of its tasks (a side of a layer and a head each).  The window goes by in chunks of 1024 tokens: who is
+// CTA: one sequence, some of its tasks (a side of a layer, a head and a piece of its rows each).  The window goes by in chunks of 1024 tokens: who is
 // kept and where it goes is found with votes and a scan, the places of those that move are listed, and every warp moves the list's
 // rows of its tasks, through shared memory (accesses narrower than 4 bytes: through registers).
 //
@@ -188,7 +189,7 @@ __device__ __forceinline__ Vec<VB> ld_slot(uint32_t at)
 // way, in registers; 305 with every access's place worked out from page numbers and the scales moved by one warp; chunks of 512 tokens
 // 131, of 2048 139; CTAs of 4 warps 141, of 16 141).  What is left: beginnings and ends of chunks, and sequences of unequal lengths.
 // 40 sequences x 32 layers, two or three rows each: 6.7 us in a graph.
-template <int VB, int LANES>
+template <int VB, int LANES, int STAGES>
 __global__ void __launch_bounds__(kMoveThreads, 2) kv_compact_kernel(const __grid_constant__ CompactArgs a)
 {
     constexpr int WARPS = kMoveThreads / 32, ROWS = 32 / LANES, U = kMoveAccesses;
@@ -196,7 +197,7 @@ __global__ void __launch_bounds__(kMoveThreads, 2) kv_compact_kernel(const __gri
     extern __shared__ __align__(16) unsigned char shared[];
     MoveRow(*const list)[kMoveChunk] = reinterpret_cast<MoveRow(*)[kMoveChunk]>(shared);  // of elements, and of scales
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(shared) + (uint32_t)(a.m.kinds * sizeof(MoveRow) * kMoveChunk) +
-                          (threadIdx.x >> 5) * (kMoveStages * U * 32 * VB) + (threadIdx.x & 31) * VB;
+                          (threadIdx.x >> 5) * (STAGES * U * 32 * VB) + (threadIdx.x & 31) * VB;
     const int seq = (int)(blockIdx.x / (unsigned)a.ctas_per_seq), part = (int)(blockIdx.x - (unsigned)(seq * a.ctas_per_seq));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     wait_for_previous_kernel();
@@ -216,9 +217,8 @@ __global__ void __launch_bounds__(kMoveThreads, 2) kv_compact_kernel(const __gri
     }
     const unsigned char* keep = a.keep + (long long)seq * a.keep_stride;
     const int32_t* pages = a.page_table + (long long)seq * a.page_table_stride;
-    const int first_task = part * a.tasks_per_cta, tasks = min(a.tasks_per_cta, a.m.sides * a.m.heads - first_task);
+    const int per_side = a.m.heads * a.pieces, first_task = part * a.tasks_per_cta, tasks = min(a.tasks_per_cta, a.m.sides * per_side - first_task);
     const int row_vectors = a.m.kind[0].row_bytes / VB;
-    const int turns = (row_vectors + LANES - 1) / LANES;  // accesses of a lane to one row
     // Place of a thread's j-th token among those of the chunk for which `mine` holds, and their number.
     const auto scan = [&](const bool (&mine)[kMoveTurns], int (&at)[kMoveTurns]) -> int {
 #pragma unroll
@@ -283,32 +283,34 @@ __global__ void __launch_bounds__(kMoveThreads, 2) kv_compact_kernel(const __gri
         __syncthreads();
 
         // Elements: many rows one task at a time, few rows U tasks at a time.  An item is U accesses of a lane: TU tasks, BU batches of ROWS
-        // rows.  A warp goes through its items in order, kMoveStages under way.
+        // rows.  A warp goes through its items in order, STAGES under way.
         const auto move = [&](auto tasks_at_once) {
             constexpr int TU = decltype(tasks_at_once)::value, BU = U / TU;
             const int batches = (rows + ROWS * BU - 1) / (ROWS * BU);
             struct Cursor {
-                int task, turn, batch;
+                int task, batch;
                 unsigned char* base[TU];
             };
             const auto place = [&](Cursor& c) {
 #pragma unroll
                 for (int i = 0; i < TU; ++i) {
-                    const int t = first_task + c.task + i * WARPS, side = t / a.m.heads, head = t - side * a.m.heads, v = c.turn * LANES + lane % LANES;
+                    const int t = first_task + c.task + i * WARPS, side = t / per_side, rest = t - side * per_side;
+                    int head = rest, v = lane % LANES;
+                    if (a.pieces > 1) {
+                        head = rest / a.pieces;
+                        v += (rest - head * a.pieces) * LANES;
+                    }
                     c.base[i] = c.task + i * WARPS < tasks && v < row_vectors ? a.m.base[0][side] + (long long)head * a.m.kind[0].head_stride + v * VB : nullptr;
                 }
             };
             const auto next = [&](Cursor& c) {
                 if (++c.batch < batches) return;
                 c.batch = 0;
-                if (++c.turn == turns) {
-                    c.turn = 0;
-                    c.task += TU * WARPS;
-                }
+                c.task += TU * WARPS;
                 place(c);
             };
-            const int items = warp < tasks ? (tasks - warp + TU * WARPS - 1) / (TU * WARPS) * turns * batches : 0;
-            Cursor to = {warp, 0, 0, {}};
+            const int items = warp < tasks ? (tasks - warp + TU * WARPS - 1) / (TU * WARPS) * batches : 0;
+            Cursor to = {warp, 0, {}};
             place(to);
             if constexpr (VB >= 4) {
                 Cursor from = to;
@@ -326,9 +328,9 @@ __global__ void __launch_bounds__(kMoveThreads, 2) kv_compact_kernel(const __gri
                     asm volatile("cp.async.commit_group;" ::: "memory");
                 };
 #pragma unroll
-                for (int s = 0; s < kMoveStages; ++s) fetch(s);
+                for (int s = 0; s < STAGES; ++s) fetch(s);
                 for (int n = 0; n < items; ++n) {
-                    asm volatile("cp.async.wait_group %0;" ::"n"(kMoveStages - 1) : "memory");
+                    asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
                     __syncwarp();
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
@@ -337,7 +339,7 @@ __global__ void __launch_bounds__(kMoveThreads, 2) kv_compact_kernel(const __gri
                     }
                     next(to);
                     fetch(slot);
-                    slot = slot + 1 == kMoveStages ? 0 : slot + 1;
+                    slot = slot + 1 == STAGES ? 0 : slot + 1;
                 }
             } else {
                 for (int n = 0; n < items; ++n, next(to)) {
@@ -360,7 +362,7 @@ __global__ void __launch_bounds__(kMoveThreads, 2) kv_compact_kernel(const __gri
         // Scales: a side's are moved by the CTA that has its first task, all heads by all warps, a batch's loads ahead of its stores; the
         // first batch's ahead of the elements, which cover their wait.
         const int values = a.m.kinds == 2 ? rows * a.m.heads : 0;
-        const int first_side = (first_task + a.m.heads - 1) / a.m.heads, last_side = (first_task + tasks - 1) / a.m.heads;
+        const int first_side = (first_task + per_side - 1) / per_side, last_side = (first_task + tasks - 1) / per_side;
         uint32_t y[kMoveScales];
         const auto scale_place = [&](int g, bool to) -> long long {
             const int r = (int)((unsigned)g / (unsigned)a.m.heads);

@@ -222,3 +222,9 @@ def test_a_stack_holds_no_cache_twice(B):
         B.KvCacheStack([cache, cache])
     with pytest.raises(ValueError):
         B.KvCacheStack([cache, B.KvCache(cache.v.clone(), cache.v, cache.k_scale.clone(), cache.v_scale.clone())])
+
+
+@pytest.mark.parametrize("layers,layout,page,heads,dim,dtype,fmt", SHAPES[:-1])
+def test_gaps_of_many_sequences_are_closed(B, layers, layout, page, heads, dim, dtype, fmt):
+    """More CTAs than SMs: whole rows, and less under way in each."""
+    test_gaps_are_closed(B, layers, layout, page, heads, dim, dtype, fmt, 320, 45, 0.6)
