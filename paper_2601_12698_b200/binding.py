@@ -644,6 +644,8 @@ class RotaryTable:
 
 
 def _refuse_rotary(positions, x, out, index: int):
+    if index < 0:
+        raise ValueError("rotary_launch: the table must be on a CUDA device")
     if positions.dim() != 1 or positions.dtype != _torch.int64 or not positions.is_contiguous() or positions.get_device() != index:
         raise ValueError("rotary_launch: positions must be a contiguous int64 [n_tokens] tensor on the table's device")
     raise ValueError("rotary_launch: q, k and their outputs must be [n_tokens, heads, head_dim] tensors of one dtype (bf16, fp16, fp32) and "
@@ -669,7 +671,7 @@ def rotary_launch(table: RotaryTable, positions, q, k=None, q_out=None, k_out=No
             if not (o2 == 1 and q_out.dtype is dtype and q_out.shape == shape and q_out.get_device() == index):
                 raise ValueError
         if not (q2 == 1 and code is not None and positions.dtype is _torch.int64 and positions.shape == (n,) and positions.is_contiguous()
-                and q.get_device() == positions.get_device() == index):
+                and q.get_device() == positions.get_device() == index >= 0):
             raise ValueError
     except ValueError:
         _refuse_rotary(positions, q, q_out, index)
