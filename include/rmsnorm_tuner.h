@@ -554,7 +554,8 @@ typedef struct {
  * sequence are left as they were.  Query head h reads key/value head h / (q_heads / kv_heads).  Keys that a row does not see have no
  * influence on it, whatever their values (infinities and NaN included).
  * Arithmetic as in shared_prefix_attention_launch: binary32, the weights rounded to `dtype` for the product with the values (no
- * exponential comes from a polynomial).
+ * exponential comes from a polynomial).  The largest weight of a row counted as 1, a weight w is off by at most 2^-8 w in bf16, 2^-11 w or
+ * 2^-32, whichever is more, in fp16.
  *   q          device, [q_tokens, q_heads, head_dim] of `dtype` (bf16 or fp16); k, v: [k_tokens, kv_heads, head_dim]; outer strides in
  *              elements, none of them 0 (unless its axis has one entry), pointers and strides multiples of 16 bytes.
  *   head_dim   a multiple of 8 up to RT_KV_MAX_HEAD_DIM; q_heads / kv_heads up to 128; softmax_scale finite and not negative.

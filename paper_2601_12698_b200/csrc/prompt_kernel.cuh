@@ -21,10 +21,13 @@
 // the first the first 64 keys of every tile and the second the others.  What is left of tensor memory holds the scores of two tiles: the
 // next tile's are computed while this one's are exponentiated.
 //
-// The reference m is moved only when a score exceeds it by 8, as in the prefix kernel: weights reach 2^8.  Streams that share rows share
+// The reference m is moved only when a score exceeds it by 8, as in the prefix kernel: weights reach 2^8 of its own.  Streams that share rows share
 // the reference, as if the second's keys came behind the first's: a stream works with the reference that it knows, and before it
 // announces its weights it waits until the other has announced those that come before, looks whether the reference has been moved, and
 // if so works again.
+//
+// fp16 weights are taken 2^7 times as large, up to 2^15, so that those far below the reference keep their bits: they are rounded to multiples
+// of 2^-31 of the reference's weight at the least, off by 2^-32 of it.  (Without the factor, weights e^-18 of the first key's became zeros.)
 //
 // Values that a row does not see meet a weight of zero in the product, and 0 * inf is NaN.  Where a tile has such values (the diagonal, the
 // sequence's end), warps 8-11 replace infinities and NaN among the keys that not all rows see by zeros before the product, and
@@ -116,6 +119,10 @@ struct PromptShape {
     static constexpr size_t kSmem = kRingAt + (size_t)kSlots * kSlotBytes + 1024;  // 1024: alignment of the tiles
     static constexpr int kSoftmaxRegs = 160;  // of 2 * 128 for a softmax thread and one of another role
 };
+
+// log2 of the factor that weights and their sum are held with.  (bf16 has binary32's range and needs none.)
+template <typename T>
+__device__ constexpr float kPromptWeightShift = std::is_same<T, __half>::value ? 7.f : 0.f;
 
 __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar)
 {
@@ -504,7 +511,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                     for (bool settled = false;;) {
                         // No key of the row so far: the reference is -inf, every score is -inf, and so must every weight's logarithm be.
                         const float reference = m == -INFINITY ? 0.f : m;
-                        const float2x minus2 = pack_f2(-reference, -reference);
+                        const float2x minus2 = pack_f2(kPromptWeightShift<T> - reference, kPromptWeightShift<T> - reference);
                         float t4[2] = {-INFINITY, -INFINITY};
                         sum[0] = sum[1] = pack_f2(0.f, 0.f);
                         uint32_t v2[2][32];
@@ -644,7 +651,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
             const int my_row = row_index(r);
             const long long first_row = (long long)item.q_row * n_heads + item.kv_head * a.group;
             const bool none = l == 0.f;
-            const float inv = none ? 0.f : __frcp_rn(l), total = none ? -INFINITY : m + log2f(l);
+            const float inv = none ? 0.f : __frcp_rn(l), total = none ? -INFINITY : m + (log2f(l) - kPromptWeightShift<T>);
             if (my_row >= 0 && (!kSharedRows || s == 0)) {
                 if (a.parts > 1) a.part_lse[item.part * n_rows + first_row + my_row] = total;
                 else if (a.lse) a.lse[first_row + my_row] = total * 0.69314718055994531f;
