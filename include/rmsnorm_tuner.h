@@ -501,8 +501,9 @@ typedef struct {
 
 /*
  * The frequencies of a spec, host only: turns[j] (rot_dim / 2 of them) is the part of a full turn that pair j makes per
- * position, as a 64-bit binary fraction.  Position p's angle is then the product p * turns[j] modulo 2^64, exact at any
- * distance, where a binary32 angle is off by 0.06 at a million.
+ * position, as a 64-bit binary fraction, off by less than 2^-63 of a turn (times theta_j, where a `factor` below 1 makes that larger than
+ * 1).  Position p's angle is then the product p * turns[j] modulo 2^64, which is exact: off by p * 2^-63 turns in all, at p = 2^37 as
+ * much as the 2^-26 of a turn that rotary_launch's binary32 has itself, where a binary32 angle is off by 0.06 at a million.
  */
 int rotary_frequencies(const rt_rotary_spec* spec, uint64_t* turns, float* magnitude);
 

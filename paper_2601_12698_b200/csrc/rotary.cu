@@ -1,4 +1,5 @@
 // Entry points of the rotary positions: frequencies, argument checks, the launch rule and the kernel's instances.
+#include <float.h>
 #include <math.h>
 #include <string.h>
 
@@ -8,7 +9,10 @@
 namespace rt {
 namespace {
 
-constexpr double kTwoPi = 6.283185307179586476925286766559;
+typedef long double Real;  // x87: 64 bits of mantissa
+static_assert(LDBL_MANT_DIG >= 64, "fractions of a turn are whole numbers of 64 bits");
+
+constexpr Real kTwoPi = 6.283185307179586476925286766559005768L;
 
 bool positive(double x) { return x > 0 && x < INFINITY; }
 
@@ -29,7 +33,7 @@ int check_spec(const rt_rotary_spec* s)
     return RT_OK;
 }
 
-double between_0_and_1(double x) { return x < 0 ? 0 : x > 1 ? 1 : x; }
+Real between_0_and_1(Real x) { return x < 0 ? 0 : x > 1 ? 1 : x; }
 
 typedef void (*RotaryKernel)(RotaryArgs);
 
@@ -95,29 +99,29 @@ int rotary_frequencies(const rt_rotary_spec* s, uint64_t* turns, float* magnitud
     }
     const int st = check_spec(s);
     if (st != RT_OK) return st;
+    // In 64 bits of mantissa: what is wrong with a fraction counts once for every position.
     const int rot = s->rot_dim;
-    const double base = s->scaling == RT_ROTARY_NTK ? s->base * pow(s->factor, (double)rot / (rot - 2)) : s->base;
-    double first = 0, last = 0;
+    const Real factor = s->factor, original_len = s->original_len;
+    const Real base = s->scaling == RT_ROTARY_NTK ? s->base * powl(factor, (Real)rot / (rot - 2)) : (Real)s->base;
+    Real first = 0, last = 0;
     if (s->scaling == RT_ROTARY_YARN) {
-        const auto pair = [&](double n) { return rot * log(s->original_len / (kTwoPi * n)) / (2 * log(base)); };
-        first = fmax(0.0, floor(pair(s->fast_turns)));
-        last = fmin(rot - 1.0, ceil(pair(s->slow_turns)));
+        const auto pair = [&](Real n) { return rot * logl(original_len / (kTwoPi * n)) / (2 * logl(base)); };
+        first = fmaxl(0, floorl(pair(s->fast_turns)));
+        last = fminl(rot - 1, ceill(pair(s->slow_turns)));
     }
     for (int j = 0; j < rot / 2; ++j) {
-        double theta = pow(base, -2.0 * j / rot);
-        if (s->scaling == RT_ROTARY_LINEAR) theta /= s->factor;
+        Real theta = powl(base, (Real)(-2 * j) / rot);
+        if (s->scaling == RT_ROTARY_LINEAR) theta /= factor;
         if (s->scaling == RT_ROTARY_BANDS) {
-            const double keep = between_0_and_1((s->original_len * theta / kTwoPi - s->low_turns) / (s->high_turns - s->low_turns));
-            theta = theta * keep + theta / s->factor * (1 - keep);
+            const Real keep = between_0_and_1((original_len * theta / kTwoPi - s->low_turns) / ((Real)s->high_turns - s->low_turns));
+            theta = theta * keep + theta / factor * (1 - keep);
         }
         if (s->scaling == RT_ROTARY_YARN) {
-            const double divided = between_0_and_1((j - first) / fmax(last - first, 0.001));
-            theta = theta / s->factor * divided + theta * (1 - divided);
+            const Real divided = between_0_and_1((j - first) / fmaxl(last - first, 0.001L));
+            theta = theta / factor * divided + theta * (1 - divided);
         }
-        double part = theta / kTwoPi;
-        part -= floor(part);
-        const double scaled = ldexp(part, 64);
-        turns[j] = scaled >= 18446744073709551616.0 ? 0 : (uint64_t)scaled;
+        const Real part = theta / kTwoPi, scaled = roundl(ldexpl(part - floorl(part), 64));
+        turns[j] = scaled >= 18446744073709551616.0L ? 0 : (uint64_t)scaled;
     }
     *magnitude = s->scaling == RT_ROTARY_YARN ? (float)(0.1 * log(s->factor) + 1) : 1.0f;
     return RT_OK;

@@ -2,8 +2,8 @@
 //
 //   y1 = m (x1 cos a - x2 sin a),  y2 = m (x2 cos a + x1 sin a),  a = 2 pi frac(position * turns_j)
 //
-// turns_j is a 64-bit binary fraction of a turn, so the product modulo 2^64 is the exact place on the circle at any position,
-// and its top 32 bits are the angle to 2^-32 of a turn: no range reduction, no binary64.
+// turns_j is a 64-bit binary fraction of a turn, so the product modulo 2^64 is the place on the circle with no more error than the fraction's
+// own, below 2^-63 of a turn, times the position; its top 32 bits, in binary32, are the angle to 2^-26 of a turn: no range reduction, no binary64.
 //
 // Bound by HBM: every element is read and written once.  A thread owns P pairs of one token (two vectors of P elements: j and
 // j + rot / 2, or two neighbouring ones) and walks over the heads with them, so that sines and cosines are computed once per
