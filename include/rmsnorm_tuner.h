@@ -504,6 +504,8 @@ typedef struct {
  * position, as a 64-bit binary fraction, off by less than 2^-63 of a turn (times theta_j, where a `factor` below 1 makes that larger than
  * 1).  Position p's angle is then the product p * turns[j] modulo 2^64, which is exact: off by p * 2^-63 turns in all, at p = 2^37 as
  * much as the 2^-26 of a turn that rotary_launch's binary32 has itself, where a binary32 angle is off by 0.06 at a million.
+ * magnitude: 1, or what the scaling's line above says at this factor.  YARN's is meant for factors above 1: below, where nothing is
+ * stretched, it falls below 1, and a caller puts 1 into rt_rotary instead (as the binding's RotaryTable does).
  */
 int rotary_frequencies(const rt_rotary_spec* spec, uint64_t* turns, float* magnitude);
 

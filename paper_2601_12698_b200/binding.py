@@ -622,7 +622,8 @@ _ROTARY_SCALINGS = {"none": RT_ROTARY_NONE, "linear": RT_ROTARY_LINEAR, "ntk": R
 class RotaryTable:
     """The frequencies of rotary positions for heads whose first rot_dim elements are turned: theta_j = base^(-2 j / rot_dim),
     stretched for long contexts by `scaling`: "linear", "ntk" (both by `factor`), "bands" (`factor`, `original_len`, `low_turns`,
-    `high_turns`) or "yarn" (`factor`, `original_len`, `fast_turns`, `slow_turns`; `magnitude` 0.1 ln(factor) + 1 unless given).
+    `high_turns`) or "yarn" (`factor`, `original_len`, `fast_turns`, `slow_turns`; `magnitude` 0.1 ln(factor) + 1 unless given,
+    and 1 for factors up to 1, which stretch nothing).
     Pairs are (j, j + rot_dim / 2), or (2 j, 2 j + 1) when interleaved.  One object serves every layer and every call."""
 
     def __init__(self, rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original_len: float = 0.0,
@@ -635,7 +636,7 @@ class RotaryTable:
         _check(lib.rotary_frequencies(byref(spec), fractions, byref(m)), "rotary_frequencies")
         _torch_ready()
         self.rot_dim, self.interleaved = int(rot_dim), bool(interleaved)
-        self.magnitude = m.value if magnitude is None else float(magnitude)
+        self.magnitude = (m.value if factor > 1 else 1.0) if magnitude is None else float(magnitude)
         self.fractions = list(fractions)[:self.rot_dim // 2]  # of a turn, times 2^64
         signed = [f - (1 << 64) if f >> 63 else f for f in self.fractions]
         self.turns = _torch.tensor(signed, dtype=_torch.int64, device=device)
