@@ -794,7 +794,7 @@ class KvCacheStack:
         for c in self.caches:
             if c.device_index != first.device_index or any(getattr(c.struct, n) != getattr(first.struct, n) for n in alike):
                 raise ValueError("the caches of a stack must have one device, shape, format and strides")
-        held = [t.data_ptr() for c in self.caches for t in (c.k, c.v, c.k_scale, c.v_scale) if t is not None]
+        held = [t.data_ptr() for c in self.caches for t in (c.k, c.v, c.k_scale, c.v_scale) if t is not None and t.numel()]
         if len(set(held)) != len(held):
             raise ValueError("a stack holds no cache twice")
         self.device_index = first.device_index
