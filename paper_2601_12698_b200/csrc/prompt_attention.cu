@@ -55,9 +55,11 @@ int make_prompt_plan(const rt_prompt_batch* b, int q_heads, int kv_heads, int di
     p->group = q_heads / kv_heads;
     p->stream_tokens = kPromptTile / p->group;
     p->block_tokens = p->form == 2 ? p->stream_tokens : 2 * p->stream_tokens;
+    // (no sequence is longer than the tensors, whatever the batch says)
+    const long long max_q_len = std::min(b->max_q_len, b->q_tokens), max_k_len = std::min(b->max_k_len, b->k_tokens);
     // Blocks: as many as there are full ones, and a ragged one of each sequence.
     const long long blocks = b->q_tokens / p->block_tokens + b->n_seqs;
-    const long long expected = std::min(blocks, b->n_seqs * ceil_div(b->max_q_len, p->block_tokens)) * kv_heads, tiles = ceil_div(b->max_k_len, kPromptTile);
+    const long long expected = std::min(blocks, b->n_seqs * ceil_div(max_q_len, p->block_tokens)) * kv_heads, tiles = ceil_div(max_k_len, kPromptTile);
     // Blocks that do not fill the device evenly, against many keys: the keys are cut into parts, as many as end first by a model of whole
     // waves of items: a key tile takes 1.7 us (2.3 with heads of more than 128), beginning and ending an item 3, joining the parts 3 and
     // the time to write and read them at 5 TB/s.  512 tokens behind 16000, 40 heads on 8 of 128, 88 blocks: 237 us in one part, 185 in three.
