@@ -223,6 +223,7 @@ int prompt_attention_launch(const rt_prompt_batch* b, const void* q, int64_t q_t
     a.status = device_status_word();
     if (!a.status) return RT_ERR_NO_DEVICE;
     a.wait_polls = wait_poll_limit();
+    a.more_waits = prompt_more_waits(b->k_tokens, b->n_seqs);
     a.drop_copies = drop_copies();
     const PromptKernels kernels = dtype == RT_BF16 ? prompt_kernels_bf16() : prompt_kernels_fp16();
     if ((st = allow_smem(kernels, dtype, p.form)) != RT_OK) return st;

@@ -81,8 +81,18 @@ struct PromptArgs {
     int wide_rows;    // rows of out, or of part_out, are multiples of 32 bytes
     int* status;
     unsigned wait_polls;
+    unsigned more_waits;  // what a wait for an item is given beyond the second of every wait: see prompt_more_waits
     int drop_copies;
 };
+
+// A warp may have to wait for an item from its beginning to its end, or until it is found.  That may take 16384 cycles for each key tile (one
+// takes 2500 to 6000, by the heads' size and where it is read from) and 1024 for each sequence (they are gone through 32 at a time, up
+// to 32 times, at about 800 cycles): as many more waits, of kMbarrierCycleLimit each.  None up to 15 million keys and 1.9 million sequences.  (With
+// a single one, 2^24 sequences whose blocks' costs lie in more than five powers of two ended as if a wait had been without hope.)
+inline unsigned prompt_more_waits(long long k_tokens, long long n_seqs)
+{
+    return (unsigned)((k_tokens / kPromptTile * 16384 + n_seqs * 1024) / kMbarrierCycleLimit);
+}
 
 struct PromptItem {
     int valid;
@@ -418,9 +428,12 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
     auto wait = [&](uint64_t* bar, uint32_t parity) {
         if (ok) ok = mbarrier_wait_sleeping(bar, parity, a.wait_polls);
     };
+    auto wait_item = [&](uint64_t* bar, uint32_t parity) {
+        for (unsigned more = a.more_waits; ok && !mbarrier_wait_sleeping(bar, parity, a.wait_polls); --more) ok = more > 0;
+    };
     // The next item (`n`-th of this CTA); false: there is none.
     auto next_item = [&](int n, PromptItem& item) -> bool {
-        wait(&item_full[n % kPromptItems], (n / kPromptItems) & 1);
+        wait_item(&item_full[n % kPromptItems], (n / kPromptItems) & 1);
         if (!__all_sync(0xFFFFFFFFu, ok)) return false;
         item = items[n % kPromptItems];
         return item.valid != 0;
@@ -706,7 +719,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         for (int n = 0; next_item(n, item); ++n) {
             for (int tile = max(item.tile0, item.masked_from); tile < item.tile1; ++tile) {
                 bool found = false;
-                wait(&landed[looked_at % kPromptLanded], (looked_at / kPromptLanded) & 1);
+                wait_item(&landed[looked_at % kPromptLanded], (looked_at / kPromptLanded) & 1);
                 ++looked_at;
                 const uint32_t unit = (2 * (tiles_before + tile - item.tile0) + 1) * kUnits;
                 if (tile * kPromptTile + p > item.last_key) {
@@ -1067,7 +1080,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
                 item.tile1 = min(item.tile0 + run, tiles);
                 item.bad_values = 0;
             }
-            wait(&item_free[n % kPromptItems], ((n / kPromptItems) & 1) ^ 1);
+            wait_item(&item_free[n % kPromptItems], ((n / kPromptItems) & 1) ^ 1);
             if (!__all_sync(0xFFFFFFFFu, ok)) break;
             if (lane == 0) {
                 items[n % kPromptItems] = item;

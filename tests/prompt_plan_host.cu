@@ -24,3 +24,5 @@ PromptKernels prompt_kernels_bf16() { return {}; }
 PromptKernels prompt_kernels_fp16() { return {}; }
 
 }  // namespace rt
+
+extern "C" unsigned harness_more_waits(int64_t k_tokens, int64_t n_seqs) { return rt::prompt_more_waits(k_tokens, n_seqs); }

@@ -16,12 +16,19 @@ MOST = (1 << 63) - 1
 
 
 @pytest.fixture(scope="module")
-def workspace(tmp_path_factory):
+def harness(tmp_path_factory):
     nvcc = shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"
     path = str(tmp_path_factory.mktemp("plan") / "plan.so")
     subprocess.run([nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-std=c++17", "-shared", "-Xcompiler", "-fPIC",
                     "-I", os.path.join(ROOT, "include"), "-o", path, os.path.join(HERE, "prompt_plan_host.cu")], check=True)
-    fn = ctypes.CDLL(path).prompt_attention_workspace_bytes
+    lib = ctypes.CDLL(path)
+    lib.harness_more_waits.argtypes = [ctypes.c_int64] * 2
+    return lib
+
+
+@pytest.fixture(scope="module")
+def workspace(harness):
+    fn = harness.prompt_attention_workspace_bytes
     fn.argtypes, fn.restype = B.lib.prompt_attention_workspace_bytes.argtypes, ctypes.c_int64
     return lambda seqs, q, k, max_q, max_k, heads=8, kv_heads=2, dim=128: fn(
         ctypes.byref(B.rt_prompt_batch(P, P, seqs, q, k, max_q, max_k, 1, 0)), heads, kv_heads, dim)
@@ -49,3 +56,16 @@ def test_the_workspace_holds_every_part(workspace):
             if size:
                 parts = size // (rows * (dim * 4 + 4))
                 assert 2 <= parts <= 32 and parts * rows * (dim * 4 + 4) + 4 <= size < parts * rows * (dim * 4 + 4) + 4 + 16
+
+
+@pytest.mark.parametrize("keys", [0, 1000, 1 << 20, 15 << 20, 1 << 27, 1 << 30])
+@pytest.mark.parametrize("seqs", [1, 1000, 1 << 20, 1 << 24])
+def test_a_wait_for_an_item_outlasts_it(harness, keys, seqs):
+    """Cycles: a key tile of an item takes up to 6000, and two items may have to pass; 32 sequences take about 800 to go through, once for each of
+    up to 31 powers of two of the blocks' costs and once to count."""
+    second = 2_000_000_000
+    most = -(-keys // 128) * 12000 + -(-seqs // 32) * 800 * 32
+    more = harness.harness_more_waits(keys, seqs)
+    assert (more + 1) * second >= most and (more <= 80)
+    if keys <= 15_000_000 and seqs <= 100_000:
+        assert more == 0  # what hangs is found within a second
