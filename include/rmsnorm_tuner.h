@@ -563,7 +563,7 @@ typedef struct {
  *              elements, none of them 0 (unless its axis has one entry), pointers and strides multiples of 16 bytes.
  *   head_dim   a multiple of 8 up to RT_KV_MAX_HEAD_DIM; q_heads / kv_heads up to 128; softmax_scale finite and not negative.
  *   out        device, [q_tokens, q_heads, head_dim] contiguous, 16-byte aligned.  lse: device, binary32 [q_tokens, q_heads]
- *              contiguous, or NULL.
+ *              contiguous, or NULL.  Neither may overlap another tensor of the call.
  *   workspace  device memory of prompt_attention_workspace_bytes(...) bytes, 16-byte aligned.  It carries nothing from one call to the
  *              next; calls that may overlap on the device need one each.
  * Starts that descend or lie outside the tensors, of whichever sequence: nothing is computed or written, and RT_ERR_INDEX is left in

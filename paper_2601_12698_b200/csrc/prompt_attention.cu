@@ -182,6 +182,10 @@ int prompt_attention_launch(const rt_prompt_batch* b, const void* q, int64_t q_t
         set_error("q, k, v, out and workspace must be multiples of 16 bytes, the other tensors of 4");
         return RT_ERR_ALIGN;
     }
+    if (b->k_tokens > 0 && (out == k || out == v)) {  // (some rows' keys and values would be other rows' results)
+        set_error("out overlaps k or v");
+        return RT_ERR_SHAPE;
+    }
     PromptPlan p;
     if ((st = make_prompt_plan(b, q_heads, kv_heads, head_dim, &p)) != RT_OK) return st;
     if (p.workspace > 0 && !workspace) {
