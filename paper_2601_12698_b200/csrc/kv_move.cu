@@ -262,8 +262,8 @@ int kv_cache_compact_launch(const rt_kv_cache* caches, int32_t n_caches, const r
     if ((st = current_limits(&L)) != RT_OK) return st;
     // A task is a side of a layer, a head and a piece of its rows: whole rows, or where that leaves SMs without a CTA, pieces down to 64 bytes.
     // Tasks of a sequence to one CTA: few enough that two CTAs to an SM cover the device, and no fewer than its warps.  With no more CTAs than
-    // SMs each has more under way.  (40 sequences x 32 layers x 8 heads, two or three rows each: 8.6 us in a graph with two CTAs to an SM,
-    // 10.3 with four.  Rows in halves, for more CTAs than SMs, were slower: 12 sequences x 8 layers: 164 us, then 145 without.  One sequence of
+    // SMs each has more under way.  (40 sequences x 32 layers x 8 heads, two or three rows each: 7.1 us in a graph with two CTAs to an SM,
+    // 8.8 with four.  Rows in halves, for more CTAs than SMs, were slower: 12 sequences x 8 layers: 164 us, then 145 without.  One sequence of
     // 100000 tokens x 4 layers x 8 heads of 128 bf16: 581 us, 1439 with whole rows and three items under way; 24000 x 32 layers: 421 and 590.)
     const int width = access_width(a.m, 0, a.m.kind[0].row_bytes, 16), row_vectors = a.m.kind[0].row_bytes / width;
     int lanes = 32;

@@ -188,7 +188,7 @@ __device__ __forceinline__ Vec<VB> ld_slot(uint32_t at)
 // layers x 8 heads of 128 int8, 1500 rows of each, 608 MB: 124 us, 4.9 TB/s, 0.76 of the copy bandwidth (145 with two items of a warp under
 // way, in registers; 305 with every access's place worked out from page numbers and the scales moved by one warp; chunks of 512 tokens
 // 131, of 2048 139; CTAs of 4 warps 141, of 16 141).  What is left: beginnings and ends of chunks, and sequences of unequal lengths.
-// 40 sequences x 32 layers, two or three rows each: 6.7 us in a graph.
+// 40 sequences x 32 layers, two or three rows each: 7.1 us in a graph.
 template <int VB, int LANES, int STAGES>
 __global__ void __launch_bounds__(kMoveThreads, 2) kv_compact_kernel(const __grid_constant__ CompactArgs a)
 {

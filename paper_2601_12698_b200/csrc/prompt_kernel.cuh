@@ -36,12 +36,13 @@
 // Bounds: 4 * 128 * 128 * dim flops and 128 * 128 exponentials per tile and stream; at dim 128 the tensor cores need 1024
 // cycles for that and the SM's 16 exponentials a cycle 1024 as well.  Products read their operands from shared memory at 128 bytes a
 // cycle: 128 x 64 x 16 take 48 cycles instead of 32, 128 x 128 x 16 the 64 that they should, and with the left operand in tensor memory both
-// do.  Scores 64 keys at a time, which let the tensor cores go on while the other half is exponentiated, are worth that at dims up to 128
-// (one product of 128 keys: 563 us, not 440).
+// do.  So at dim 128 a stream's products take 768 + 512 cycles, both streams' 2560 of the 3120 that a tile takes: operands first, then the chain
+// from scores to weights; the power limit decides how long a cycle is.  Scores 64 keys at a time, which let the tensor cores go on while the other half is
+// exponentiated, are worth that at dims up to 128 (one product of 128 keys: 563 us, not 440).
 //
 // Measured (TFLOP/s of the causal pairs; the clock drops to 1.64 GHz under the power limit in the long ones):
 //   8192 tokens, 32 heads on 8 of 128: 440 us, 1250; the tensor cores busy in 64 % of the cycles, the special function unit in 64 %;
-//   16384 tokens: 1700 .. 1970 us, 1290 .. 1120 by the box; heads of 64, 8192 tokens: 355 us, special function unit 74 %;
+//   16384 tokens: 1700 .. 2060 us, 1290 .. 1070 by the box; heads of 64, 8192 tokens: 355 us, special function unit 74 %;
 //   32 heads on 4 of 256, 4096 tokens: 248 us, 1110; shared memory: 2560 cycles of a tile's 3600 go to operands and to what TMA writes;
 //   100 tokens: 9.9 us, one CTA's chain: beginning 0.4, item 1.2, first copies 0.7, products and softmax 3, results 1.2, launch.
 #pragma once
@@ -168,8 +169,8 @@ __device__ __forceinline__ PromptSequence prompt_sequence(const PromptArgs& a, i
     return {sound ? q0 : 0, sound ? q1 - q0 : 0, sound ? k0 : 0, sound ? k1 - k0 : 0, sound};
 }
 
-// The order in which blocks are taken, whole warps: the most expensive first, so that the CTAs end together.  A block's cost is
-// counted in blocks of keys: causal blocks of a sequence cost base, base + 1, ...; otherwise all the same.
+// The order in which blocks are taken, whole warps: the most expensive first, so that the CTAs end together.  (17 sequences of up to 1500
+// tokens, 8 heads of 64: 42.8 us, 61.1 in the sequences' order.)  A block's cost is counted in blocks of keys: causal blocks of a sequence cost base, base + 1, ...; otherwise all the same.
 // Up to 128 sequences are kept in registers and the order is exact.  More are gone through 32 at a time, once for each power of two of the
 // cost that occurs, and a CTA's ranks ascend, so that it goes through them once in all (looked up for every block instead: 1000 sequences
 // of 16 tokens, 32 heads on 8 of 128, 854 us; 4000: 12.9 ms).
@@ -1041,7 +1042,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) prompt_attention_kernel(con
         const int per_block = a.kv_heads * a.parts;
         const long long ids = order.total * per_block;
         for (int n = 0;; ++n) {
-            // there and back again, so that the CTA that had the dearest item of one round has the cheapest of the next
+            // there and back again, so that the CTA that had the dearest item of one round has the cheapest of the next (the same: 49.6 us without)
             const long long id = (long long)n * gridDim.x + ((n & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
             PromptItem item;
             item.valid = 0;
