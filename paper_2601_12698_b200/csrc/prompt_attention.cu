@@ -62,7 +62,7 @@ int make_prompt_plan(const rt_prompt_batch* b, int q_heads, int kv_heads, int di
     const long long expected = std::min(blocks, b->n_seqs * ceil_div(max_q_len, p->block_tokens)) * kv_heads, tiles = ceil_div(max_k_len, kPromptTile);
     // Blocks that do not fill the device evenly, against many keys: the keys are cut into parts, as many as end first by a model of whole
     // waves of items: a key tile takes 1.7 us (2.3 with heads of more than 128), beginning and ending an item 3, joining the parts 3 and
-    // the time to write and read them at 5 TB/s.  512 tokens behind 16000, 40 heads on 8 of 128, 88 blocks: 242 us in one part, 215 in three (237 and 189 on another box).
+    // the time to write and read them at 5 TB/s.  512 tokens behind 16000, 40 heads on 8 of 128, 88 blocks: 242 us in one part, 215 in three (237 and 189 on another card).
     // Blocks of two waves and more are left whole: their order evens them out.
     p->parts = 1;
     if (expected > 0 && expected < 2LL * L.sm_count && b->q_tokens / p->block_tokens * kv_heads < 2LL * L.sm_count && tiles >= 8) {

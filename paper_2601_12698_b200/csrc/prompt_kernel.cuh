@@ -42,7 +42,7 @@
 //
 // Measured (TFLOP/s of the causal pairs; the clock drops to 1.64 GHz under the power limit in the long ones):
 //   8192 tokens, 32 heads on 8 of 128: 440 us, 1250; the tensor cores busy in 64 % of the cycles, the special function unit in 64 %;
-//   16384 tokens: 1700 .. 2060 us, 1290 .. 1070 by the box; heads of 64, 8192 tokens: 355 us, special function unit 74 %;
+//   16384 tokens: 1700 .. 2060 us, 1290 .. 1070 by the card; heads of 64, 8192 tokens: 355 us, special function unit 74 %;
 //   32 heads on 4 of 256, 4096 tokens: 248 us, 1110; shared memory: 2560 cycles of a tile's 3600 go to operands and to what TMA writes;
 //   100 tokens: 9.9 us, one CTA's chain: beginning 0.4, item 1.2, first copies 0.7, products and softmax 3, results 1.2, launch.
 #pragma once
